@@ -170,7 +170,7 @@ pt_status pt_kv_set_free_list(pt_kv_cache* c, const int32_t* order, int32_t n);
 /* Make sure sequence `seq` (any non-negative id) owns pages for positions < new_len.
  * PT_ERR_CACHE_FULL leaves the cache unchanged. */
 pt_status pt_kv_seq_reserve(pt_kv_cache* c, int32_t seq, int32_t new_len);
-/* Give a sequence's pages back and forget it. */
+/* Give a sequence's pages back and forget it.  A page that other sequences share stays with them. */
 pt_status pt_kv_seq_release(pt_kv_cache* c, int32_t seq);
 /* Tokens currently cached for `seq` (0 for an unknown sequence). */
 pt_status pt_kv_seq_len(const pt_kv_cache* c, int32_t seq, int32_t* len);
@@ -182,6 +182,29 @@ pt_status pt_kv_block_table(const pt_kv_cache* c, int32_t seq, int32_t* pages, i
  * kv = 0 for K / 1 for V, kv_head).  The position must lie inside the reserved pages. */
 pt_status pt_kv_slot(const pt_kv_cache* c, int32_t track, int32_t layer, int32_t seq, int32_t pos,
                      int32_t kv, int32_t kv_head, int64_t* elem_offset);
+
+/* A new sequence `dst` that shares the first `len` tokens of `src` (several answers of one prompt, a prompt that many
+ * requests begin with): its table holds the pages of those tokens, and nothing is copied.  Shared pages are copied on
+ * write: a forward call that would write to a page that another sequence shares first gives the sequence a page of its
+ * own (with the earlier positions copied, on the call's stream, all sequences of the call in one launch); the last
+ * sequence left on a page keeps it.  Such pages count as new ones: PT_ERR_CACHE_FULL where the free list is too short.
+ * A program that writes to the pool itself looks at pt_kv_page_refs first.  Host only.
+ * PT_ERR_STATE: unknown `src`, or `dst` exists (src included); PT_ERR_INVALID_ARG: len outside [0, length of src]. */
+pt_status pt_kv_seq_fork(pt_kv_cache* c, int32_t src, int32_t dst, int32_t len);
+/* Pages on the free list; sequences that own a page (0: it is free). */
+pt_status pt_kv_free_pages(const pt_kv_cache* c, int32_t* n);
+pt_status pt_kv_page_refs(const pt_kv_cache* c, int32_t page, int32_t* refs);
+/* Move every page in use to the front of the pool: with U pages in use, those with an id >= U are copied (in every
+ * (track, layer) slab, scales included, on `stream`) to free ids below U, both in ascending order, and the tables
+ * follow.  The free list becomes U, U+1, ...  *moved (may be NULL) = pages copied.  Block tables read before and graphs
+ * captured before hold the old ids. */
+pt_status pt_kv_compact(pt_kv_cache* c, int32_t* moved, void* stream);
+/* Continue the cache in another buffer with `num_pages` pages (grow it, or shrink it to what is in use and give the old
+ * buffer back): the pages in use are copied to ids 0, 1, ... of `dev_pool` in ascending order of their old ids, on
+ * `stream`; everything queued on `stream` before may still read the old pool, which the caller keeps until then.
+ * `dev_pool` as for pt_kv_cache_alloc, no overlap with the old one.  PT_ERR_CACHE_FULL: more pages in use than
+ * num_pages (the cache is unchanged, as after every error). */
+pt_status pt_kv_move_pool(pt_kv_cache* c, int32_t num_pages, void* dev_pool, size_t bytes, void* stream);
 
 /* E4M3 caches: byte offset, from the start of the pool, of the fp32 scale of the vector that pt_kv_slot
  * addresses (there the offset counts one-byte codes).  PT_ERR_STATE for a cache in the model dtype. */
@@ -227,6 +250,16 @@ pt_status pt_decode_step(pt_model* m, pt_kv_cache* c, const void* x, int64_t x_t
                          int32_t B, const int32_t* seq_ids, void* out_h,
                          void* workspace, size_t ws_bytes, void* stream);
 
+/* Algorithm 1 over a ragged batch: n_tokens[b] >= 1 new tokens (host int32[B]) of sequence seq_ids[b] - prompts that
+ * advance by a chunk beside sequences that decode one token or check several speculated ones.  The rows are packed:
+ * x [T][M][hidden] and out_h fp32 [M][hidden] with M = sum of n_tokens, sequence by sequence in the order of the call.
+ * Everything else as for pt_prefill; workspace >= pt_extend_workspace_bytes(M, B, page_size, kv_dtype, max_context), whose
+ * arguments are those of pt_workspace_bytes_ex.  A debug tap holds [T][M][hidden] blocks. */
+pt_status pt_extend_workspace_bytes(const pt_model* m, int64_t max_tokens, int32_t max_batch, int32_t page_size,
+                                    int32_t kv_dtype, int64_t max_context, size_t* bytes);
+pt_status pt_extend(pt_model* m, pt_kv_cache* c, const void* x, int64_t x_track_stride, int32_t B, const int32_t* n_tokens,
+                    const int32_t* seq_ids, void* out_h, void* workspace, size_t ws_bytes, void* stream);
+
 /* ---- ends of the model (bf16 models) -----------------------------------------------------------
  * Algorithm 1 takes the embedding output x and returns h; the paper's latency tables (time to first
  * token, time per output token: Tables 6-10) need the two ends it leaves to "standard" practice.
@@ -267,6 +300,42 @@ pt_status pt_generate_workspace_bytes(const pt_model* m, int32_t B, int32_t S, i
 pt_status pt_generate(pt_model* m, pt_kv_cache* c, const int32_t* dev_prompt, int32_t B, int32_t S, int32_t n_new,
                       const int32_t* seq_ids, int32_t* dev_tokens_out, float* dev_logits_out,
                       void* workspace, size_t ws_bytes, void* stream);
+
+/* Draw one token per row of logits.  With m the largest logit of a row and w_i = exp((x_i - m) / temperature), tokens
+ * ordered by (logit descending, index ascending):
+ *   top_k   keeps the first top_k tokens (<= 0 or >= vocab: off)
+ *   top_p   keeps, of those, the shortest prefix whose weights reach top_p times their sum (>= 1 or NaN: off; <= 0: one token)
+ *   min_p   keeps, of those, the tokens with w_i >= min_p (<= 0 or NaN: off; above 1: as 1)
+ * and the token drawn is the lowest index whose cumulative kept weight (summed in index order) exceeds u times the kept
+ * sum; u outside [0, 1) (or NaN) counts as the nearest end.  A temperature that is not a positive finite number chooses
+ * greedily (the lowest index of the largest logit, probability 1).  NaN and -inf logits are masked; a row with nothing else gives token 0
+ * and probability 0.  +inf logits share the whole weight.  Weights are held as multiples of 2^-44 of the largest: a token
+ * more than 31 nats (after the temperature) below it is never drawn.  The result does not depend on the batch, and every
+ * call with the same arguments gives the same bits.
+ *   logits       device [n] rows of `vocab` values `row_stride` elements apart, fp32 or bf16 (dtype: a pt_dtype)
+ *   u            device fp32 [n], the random numbers, uniform in [0, 1)
+ *   temperature, top_p, min_p   device fp32 [n] or NULL (off; temperature 1);  top_k   device int32 [n] or NULL
+ *   token        device int32 [n]
+ *   prob         device fp32 [n] or NULL: the drawn token's weight over the kept sum
+ * vocab up to 393216.  Needs no model and no workspace; asynchronous on `stream`. */
+pt_status pt_sample(const void* logits, int32_t dtype, int64_t row_stride, int64_t n, int32_t vocab, const float* u,
+                    const float* temperature, const int32_t* top_k, const float* top_p, const float* min_p,
+                    int32_t* token, float* prob, void* stream);
+
+/* pt_generate with sampled tokens.  The arrays are device memory, [B] each as in pt_sample (NULL: off), but
+ *   u     fp32 [n_new][B]: step i uses row i
+ *   prob  fp32 [B][n_new] or NULL: the probability every token was drawn with */
+typedef struct {
+    const float* u;
+    const float* temperature;
+    const int32_t* top_k;
+    const float* top_p;
+    const float* min_p;
+    float* prob;
+} pt_sampling;
+pt_status pt_generate_sample(pt_model* m, pt_kv_cache* c, const int32_t* dev_prompt, int32_t B, int32_t S, int32_t n_new,
+                             const int32_t* seq_ids, const pt_sampling* sampling, int32_t* dev_tokens_out, float* dev_logits_out,
+                             void* workspace, size_t ws_bytes, void* stream);
 
 /* ---- track parallelism across GPUs ---------------------------------------------------------------
  * The paper's deployment (Sections 2.2 and 3.3): each GPU holds some of the tracks and the track-sync is

@@ -62,6 +62,38 @@ pt_status pt_kernel_prefill_attn(const void* q, const void* pool_l, int64_t pool
                                  int32_t T, int32_t B, int32_t S, int32_t nq, int32_t nkv, int32_t dh, int32_t ps,
                                  int32_t num_pages, void* out, int32_t impl, void* status, void* stream);
 
+/* Attention of a ragged chunk of new tokens per sequence over the paged cache: the attention of a track layer in a call
+ * of pt_extend (every track attends only to its own cache - Section 2.2).  The rows of sequence b (q_len[b] of them, none
+ * is allowed) follow those of sequence b - 1; their K and V are the last q_len[b] of its kv_len[b] cached keys:
+ *   out[t][r][h] = softmax_{j <= pos}( q[t][r][h] . K[t][b][h / G][j] / sqrt(dh) ) V[t][b][h / G][j],
+ *   r = q_len[0] + .. + q_len[b - 1] + s,   pos = kv_len[b] - q_len[b] + s,   G = nq / nkv <= 8.
+ *   q, out        device bf16 [T][M][nq*dh], 16-byte aligned; rows behind the last sequence are not touched
+ *   pool_l, block_table   as for pt_kernel_decode_attn (entries behind a sequence's last page are not read)
+ *   q_len, kv_len DEVICE int32 [B]: a captured call may be replayed with other lengths.  Lengths out of range (negative,
+ *                 kv_len < q_len, kv_len > maxp*ps, sum of q_len > M) are reported in `status` and nothing is written
+ *   impl          0 = tensor-memory kernel (tcgen05; head_dim 64 or 128, pages of a multiple of 16 tokens), 1 = plain
+ *                 kernel, one warp per row and head (head_dim 32, 64, 128; any page size)
+ *   scratch       device, 256-byte aligned, >= pt_kernel_chunk_attn_scratch_bytes: partial results of key ranges; contents
+ *                 need not be kept, but calls that may run at the same time need one each
+ *   status        device int32[16], zeroed by the caller; PT_ERR_DEVICE_BOUNDS also for a page id outside [0, num_pages)
+ * Asynchronous on `stream`; nothing is allocated. */
+pt_status pt_kernel_chunk_attn_scratch_bytes(int32_t T, int32_t B, int32_t nq, int32_t dh, size_t* bytes);
+pt_status pt_kernel_chunk_attn(const void* q, const void* pool_l, int64_t pool_track_stride,
+                               const int32_t* block_table, int32_t maxp, const int32_t* q_len, const int32_t* kv_len,
+                               int32_t T, int32_t B, int32_t M, int32_t nq, int32_t nkv, int32_t dh, int32_t ps,
+                               int32_t num_pages, void* out, int32_t impl, void* scratch, size_t scratch_bytes,
+                               void* status, void* stream);
+
+/* Page copies of a KV pool (the library's own; the paper has no cache): for every slab s < slabs and pair i < n
+ *   dst_pool[s][dst[i]] = src_pool[s][src[i]]
+ * where a pool is [slabs][pages][page_bytes].  Both pools may be one (then no page is both read and written); two pools
+ * must not overlap, and no page is written twice (PT_ERR_INVALID_ARG, as for a page outside its pool).
+ *   src_pool, dst_pool  device, 16-byte aligned;  page_bytes a multiple of 16
+ *   src, dst            HOST int32 [n], consumed before return (they travel in the launch, so a captured call keeps them)
+ * A pool of an E4M3 cache takes two calls, codes and scales.  Asynchronous on `stream`; nothing is allocated. */
+pt_status pt_kernel_kv_copy_pages(const void* src_pool, int32_t src_pages, void* dst_pool, int32_t dst_pages,
+                                  int64_t slabs, int64_t page_bytes, const int32_t* src, const int32_t* dst, int32_t n, void* stream);
+
 /* The same decode attention for callers that cannot allocate device memory.  (The paper has no
  * counterpart: this is a packaging variant of pt_kernel_decode_attn.)
  *

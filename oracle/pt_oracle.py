@@ -252,6 +252,17 @@ class PagedKVCache:
         self.free.extend(self.block_table.pop(seq, []))
         self.length.pop(seq, None)
 
+    def fork(self, src: int, dst: int, n: int) -> None:
+        """A new sequence with the first n cached tokens of another, as a plain copy into pages of its own (what sharing
+        pages until one of the owners writes must be indistinguishable from)."""
+        if dst in self.block_table or not 0 <= n <= self.length[src]:
+            raise ValueError("fork")
+        self.reserve(dst, n)
+        for i, page in enumerate(self.block_table[dst]):
+            self.pool[:, :, page] = self.pool[:, :, self.block_table[src][i]]
+            self.scale[:, :, page] = self.scale[:, :, self.block_table[src][i]]
+        self.length[dst] = n
+
     def locate(self, seq: int, pos: int) -> tuple[int, int]:
         return self.block_table[seq][pos // self.page_size], pos % self.page_size
 
@@ -361,6 +372,13 @@ def pt_decode_step(cfg: PTConfig, weights, x: np.ndarray, cache: PagedKVCache, s
     return pt_prefill(cfg, weights, x[:, :, None, :], cache, seq_ids, taps)[:, 0, :]
 
 
+def pt_extend(cfg: PTConfig, weights, x: np.ndarray, n_tokens, cache: PagedKVCache, seq_ids) -> np.ndarray:
+    """A ragged batch: x[T, M, H] holds n_tokens[b] rows of sequence seq_ids[b] after another; h[M, H].  Sequences do
+    not see one another, so this is Algorithm 1 once per sequence."""
+    ends = np.cumsum(n_tokens)
+    return np.concatenate([pt_prefill(cfg, weights, x[:, None, e - n:e], cache, [s])[0] for e, n, s in zip(ends, n_tokens, seq_ids)])
+
+
 # ----------------------------------------------------------------------------- ends of the model
 # Algorithm 1 starts from the embedding output x and returns h; the paper measures time to first
 # token and time per output token (Tables 6-10), which need the two ends it does not spell out.
@@ -381,6 +399,47 @@ def lm_head(h: np.ndarray, gain: np.ndarray, w_out: np.ndarray, eps: float) -> n
 def greedy(logits: np.ndarray) -> np.ndarray:
     """Index of the largest logit per row (the lowest index when several are equal)."""
     return np.argmax(logits, axis=-1).astype(np.int64)
+
+
+def sample_kept(x: np.ndarray, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0):
+    """One row of logits -> (kept token ids ascending, their weights, margin).  Weights are exp((x - max) / temperature);
+    the filters apply in the order top-k, top-p, min-p, each to what the one before left (ties: the lower index first).
+    NaN and -inf are masked.  margin: how far, relative to the kept sum, the top-p and min-p decisions are from falling
+    the other way (inf without them)."""
+    x = np.where(np.isnan(x), -np.inf, np.asarray(x, np.float64))
+    m = x.max()
+    if m == -np.inf:
+        return np.zeros(0, np.int64), np.zeros(0), np.inf
+    if not 0 < temperature < np.inf:
+        return np.array([np.argmax(x)]), np.ones(1), np.inf
+    with np.errstate(invalid="ignore", over="ignore"):
+        w = np.where(x == m, 1.0, np.exp((x - m) / temperature))
+    order = np.lexsort((np.arange(len(x)), -x))
+    if 0 < top_k < len(x):
+        order = order[:top_k]
+    margin = np.inf
+    if top_p < 1:
+        c = np.cumsum(w[order])
+        n = max(1, int((c < top_p * c[-1]).sum()) + 1)
+        margin = min(margin, np.abs(c - top_p * c[-1]).min() / c[-1])
+        order = order[:n]
+    if min_p > 0:
+        margin = min(margin, np.abs(w[order][w[order] != 1] - min_p).min(initial=np.inf))
+        order = order[(w[order] >= min_p) | (x[order] == m)]
+    ids = np.sort(order)
+    return ids, w[ids], margin
+
+
+def sample(x: np.ndarray, u: float, **filters):
+    """(token, probability, margin): the lowest kept index whose cumulative weight exceeds u times the kept sum; margin as
+    in sample_kept, and the distance of u from the nearest step of the cumulative distribution."""
+    ids, w, margin = sample_kept(x, **filters)
+    if len(ids) == 0:
+        return 0, 0.0, margin
+    c = np.cumsum(w) / w.sum()
+    u = 0.0 if not u > 0 else min(float(u), 1.0)
+    i = min(int((c <= u).sum()), int(np.nonzero(w)[0][-1]))
+    return int(ids[i]), float(w[i] / w.sum()), min(margin, np.abs(np.concatenate([[0.0], c]) - u).min())
 
 
 def pt_generate(cfg: PTConfig, weights, table, gain, w_out, prompt: np.ndarray, n_new: int,

@@ -7,6 +7,7 @@
 #include <new>
 #include <unordered_set>
 
+#include "pt_chunk.h"
 #include "pt_internal.h"
 
 namespace pt {
@@ -26,7 +27,7 @@ void set_error(const char* fmt, ...) {
     pt::set_error("%s failed: %s", #call, cudaGetErrorString(e_)); return PT_ERR_CUDA; } } while (0)
 
 
-static size_t meta_bytes(int64_t M, int B, int maxp, bool fp8) {
+static size_t meta_bytes(int64_t M, int B, int maxp, bool fp8, bool ragged) {
     size_t b = 0;
     b += align_up((size_t)M * 8, 256);                 // row_kvoff
     b += align_up((size_t)M * 4, 256) * 2;             // row_pos, row_b
@@ -38,16 +39,17 @@ static size_t meta_bytes(int64_t M, int B, int maxp, bool fp8) {
         b += align_up((size_t)B * 4, 256);             // ctx_start
         b += align_up((size_t)B * ((size_t)maxp * 4 + 1) * 4, 256);   // pages of the attention copy (16 tokens each; cache pages hold up to 64)
     }
+    if (ragged) b += align_up((size_t)B * 4, 256);     // qlen
     return b;
 }
 
 // Carve the workspace; with base == nullptr only the size is computed.  fp8: the cache holds E4M3 codes;
-// ctx_keys: keys of the attention copy a prefill call needs (0 for a decode call).
-static size_t carve(const pt_model* m, int64_t M, int B, int maxp, bool fp8, int64_t ctx_keys, char* base, Work* w) {
+// ctx_keys: keys of the attention copy a prefill call needs (0 for a decode call); ragged: a call of pt_extend.
+static size_t carve(const pt_model* m, int64_t M, int B, int maxp, bool fp8, int64_t ctx_keys, bool ragged, char* base, Work* w) {
     const pt_config& c = m->cfg;
     size_t off = 0;
     auto take = [&](size_t bytes) { size_t o = off; off += align_up(bytes, 256); return base ? base + o : nullptr; };
-    char* meta = (char*)take(meta_bytes(M, B, maxp, fp8));
+    char* meta = (char*)take(meta_bytes(M, B, maxp, fp8, ragged));
     size_t TMH = (size_t)c.T * M * c.hidden;
     float* hT = (float*)take(TMH * 4);
     float* hS = (float*)take((size_t)M * c.hidden * 4);
@@ -72,13 +74,35 @@ static size_t carve(const pt_model* m, int64_t M, int B, int maxp, bool fp8, int
     float* part = m->tc ? (float*)take((size_t)c.T * B * kMaxSplits * c.heads * (m->dh + 2) * 4) : nullptr;
     void* kv_stage = fp8 ? take((size_t)c.T * 2 * m->KVD * M * 2) : nullptr;
     void* attn_kv = fp8 && ctx_keys > 0 ? take((size_t)c.T * 2 * m->KVD * (size_t)ctx_keys * 2) : nullptr;
+    void* chunk = ragged && m->tc ? take(chunk_scratch_bytes(c.T, B, c.heads, m->dh)) : nullptr;
     if (w) {
+        w->chunk = chunk;
         w->kv_stage = kv_stage; w->attn_kv = attn_kv; w->gates = gates; w->moe = mw;
         w->hT = hT; w->hS = hS; w->a = a; w->qkv = qkv; w->o = o; w->gu = gu; w->z = z;
         w->ssq = ssq; w->part = part; w->total = off;
         (void)meta;
     }
     return off;
+}
+
+// Bytes of the codes (or model-dtype values) of a pool; an E4M3 pool's scales follow, 256-byte aligned.
+pt_status kv_pool_layout(const pt_model* m, int32_t num_pages, int32_t page_size, int32_t kv_dtype,
+                         size_t* codes_bytes, size_t* total) {
+    if (!m) PT_FAIL(PT_ERR_INVALID_ARG, "null argument");
+    if (num_pages < 1) PT_FAIL(PT_ERR_INVALID_ARG, "num_pages must be >= 1");
+    if (page_size < 8 || page_size > 64 || page_size % 8) PT_FAIL(PT_ERR_INVALID_ARG, "page_size must be a multiple of 8 in [8, 64]");
+    if (kv_dtype != PT_KV_MODEL && kv_dtype != PT_KV_E4M3) PT_FAIL(PT_ERR_INVALID_ARG, "kv_dtype must be PT_KV_MODEL or PT_KV_E4M3");
+    const size_t vecs = (size_t)m->cfg.T * m->cfg.L * num_pages * 2 * m->cfg.kv_heads * page_size;
+    if (kv_dtype == PT_KV_E4M3) {
+        if (!m->tc) PT_FAIL(PT_ERR_UNSUPPORTED, "an E4M3 cache needs a bf16 model on the tensor-core path");
+        if (m->dh != 128 || page_size % 16) PT_FAIL(PT_ERR_UNSUPPORTED, "an E4M3 cache needs head_dim 128 and pages of a multiple of 16 tokens");
+        *codes_bytes = align_up(vecs * m->dh, 256);
+        *total = *codes_bytes + vecs * 4;
+    } else {
+        *codes_bytes = vecs * m->dh * m->esz;
+        *total = *codes_bytes;
+    }
+    return PT_OK;
 }
 
 void plan_decode_splits(const int32_t* lens, int B, int ps, int64_t units, int32_t* items, int32_t* nsplit,
@@ -313,26 +337,6 @@ pt_status pt_model_set_expert_weight(pt_model* m, int32_t track, int32_t layer, 
 
 /* ------------------------------------------------------------------ KV cache (host logic) */
 
-// Bytes of the codes (or model-dtype values) of a pool; an E4M3 pool's scales follow, 256-byte aligned.
-static pt_status kv_pool_layout(const pt_model* m, int32_t num_pages, int32_t page_size, int32_t kv_dtype,
-                                size_t* codes_bytes, size_t* total) {
-    if (!m) PT_FAIL(PT_ERR_INVALID_ARG, "null argument");
-    if (num_pages < 1) PT_FAIL(PT_ERR_INVALID_ARG, "num_pages must be >= 1");
-    if (page_size < 8 || page_size > 64 || page_size % 8) PT_FAIL(PT_ERR_INVALID_ARG, "page_size must be a multiple of 8 in [8, 64]");
-    if (kv_dtype != PT_KV_MODEL && kv_dtype != PT_KV_E4M3) PT_FAIL(PT_ERR_INVALID_ARG, "kv_dtype must be PT_KV_MODEL or PT_KV_E4M3");
-    const size_t vecs = (size_t)m->cfg.T * m->cfg.L * num_pages * 2 * m->cfg.kv_heads * page_size;
-    if (kv_dtype == PT_KV_E4M3) {
-        if (!m->tc) PT_FAIL(PT_ERR_UNSUPPORTED, "an E4M3 cache needs a bf16 model on the tensor-core path");
-        if (m->dh != 128 || page_size % 16) PT_FAIL(PT_ERR_UNSUPPORTED, "an E4M3 cache needs head_dim 128 and pages of a multiple of 16 tokens");
-        *codes_bytes = align_up(vecs * m->dh, 256);
-        *total = *codes_bytes + vecs * 4;
-    } else {
-        *codes_bytes = vecs * m->dh * m->esz;
-        *total = *codes_bytes;
-    }
-    return PT_OK;
-}
-
 pt_status pt_kv_cache_bytes_ex(const pt_model* m, int32_t num_pages, int32_t page_size, int32_t kv_dtype, size_t* bytes) {
     if (!bytes) PT_FAIL(PT_ERR_INVALID_ARG, "null argument");
     size_t codes = 0;
@@ -365,6 +369,7 @@ pt_status pt_kv_cache_alloc_ex(const pt_model* m, int32_t num_pages, int32_t pag
     c->page_elems = (int64_t)2 * m->cfg.kv_heads * page_size * m->dh;
     c->slab_elems = c->page_elems * num_pages;
     for (int i = 0; i < num_pages; ++i) c->free_list.push_back(i);
+    c->ref.assign(num_pages, 0);
     *out = c;
     return PT_OK;
 }
@@ -392,7 +397,7 @@ pt_status pt_kv_seq_reserve(pt_kv_cache* c, int32_t seq, int32_t new_len) {
     if (need > have && need - have > c->free_list.size())
         PT_FAIL(PT_ERR_CACHE_FULL, "sequence %d needs %zu more pages, %zu free", seq, need - have, c->free_list.size());
     Seq& s = c->seqs[seq];
-    while (s.pages.size() < need) { s.pages.push_back(c->free_list.front()); c->free_list.pop_front(); }
+    while (s.pages.size() < need) { s.pages.push_back(c->free_list.front()); c->ref[c->free_list.front()] = 1; c->free_list.pop_front(); }
     return PT_OK;
 }
 
@@ -400,7 +405,7 @@ pt_status pt_kv_seq_release(pt_kv_cache* c, int32_t seq) {
     if (!c) PT_FAIL(PT_ERR_INVALID_ARG, "null argument");
     auto it = c->seqs.find(seq);
     if (it == c->seqs.end()) PT_FAIL(PT_ERR_STATE, "unknown sequence %d", seq);
-    for (int32_t p : it->second.pages) c->free_list.push_back(p);
+    for (int32_t p : it->second.pages) if (--c->ref[p] == 0) c->free_list.push_back(p);    // a shared page stays with its other owners
     c->seqs.erase(it);
     return PT_OK;
 }
@@ -477,12 +482,24 @@ pt_status pt_workspace_bytes_ex(const pt_model* m, int64_t max_tokens, int32_t m
     int maxp = (m->cfg.max_pos + page_size - 1) / page_size;
     const bool fp8 = kv_dtype == PT_KV_E4M3;
     const int64_t ctx = fp8 ? std::max<int64_t>(max_context, max_tokens + 16 * (int64_t)max_batch) : 0;
-    *bytes = carve(m, max_tokens, max_batch, maxp, fp8, ctx, nullptr, nullptr);
+    *bytes = carve(m, max_tokens, max_batch, maxp, fp8, ctx, false, nullptr, nullptr);
     return PT_OK;
 }
 
+pt_status pt_extend_workspace_bytes(const pt_model* m, int64_t max_tokens, int32_t max_batch, int32_t page_size,
+                                    int32_t kv_dtype, int64_t max_context, size_t* bytes) {
+    pt_status s = pt_workspace_bytes_ex(m, max_tokens, max_batch, page_size, kv_dtype, max_context, bytes);   // checks the arguments
+    if (s != PT_OK) return s;
+    const int maxp = (m->cfg.max_pos + page_size - 1) / page_size;
+    const bool fp8 = kv_dtype == PT_KV_E4M3;
+    const int64_t ctx = fp8 ? std::max<int64_t>(max_context, max_tokens + 16 * (int64_t)max_batch) : 0;
+    *bytes = carve(m, max_tokens, max_batch, maxp, fp8, ctx, true, nullptr, nullptr);
+    return PT_OK;
+}
+
+// S new tokens for each of the B sequences, or n_tok[b] of them for sequence b (ragged: n_tok != null, rows packed).
 static pt_status forward(pt_model* m, pt_kv_cache* c, const void* x, int64_t x_stride, int32_t B, int32_t S,
-                         const int32_t* seq_ids, void* out_h, void* workspace, size_t ws_bytes, void* stream,
+                         const int32_t* n_tok, const int32_t* seq_ids, void* out_h, void* workspace, size_t ws_bytes, void* stream,
                          bool decode) {
     if (!m || !c || !x || !seq_ids || !out_h || !workspace) PT_FAIL(PT_ERR_INVALID_ARG, "null argument");
     if (c->m != m) PT_FAIL(PT_ERR_INVALID_ARG, "cache belongs to another model");
@@ -493,7 +510,13 @@ static pt_status forward(pt_model* m, pt_kv_cache* c, const void* x, int64_t x_s
         PT_FAIL(PT_ERR_MISALIGNED, "workspace must be 256-byte aligned, x 16-byte and out_h 32-byte aligned");
     const pt_config& g = m->cfg;
     if (x_stride % 8) PT_FAIL(PT_ERR_MISALIGNED, "x_track_stride must be a multiple of 8 elements");
-    int64_t M = (int64_t)B * S;
+    const bool ragged = n_tok != nullptr;
+    auto news = [&](int b) { return ragged ? n_tok[b] : S; };
+    int64_t M = 0;
+    for (int b = 0; b < B; ++b) {
+        if (news(b) < 1) PT_FAIL(PT_ERR_INVALID_ARG, "sequence %d of the call has %d new tokens", b, news(b));
+        M += news(b);
+    }
     if (M > (1 << 30)) PT_FAIL(PT_ERR_INVALID_ARG, "too many tokens");
     // validate ids and positions before touching the allocator
     std::unordered_set<int32_t> ids;
@@ -504,11 +527,18 @@ static pt_status forward(pt_model* m, pt_kv_cache* c, const void* x, int64_t x_s
         auto it = c->seqs.find(seq_ids[b]);
         int len = it == c->seqs.end() ? 0 : it->second.len;
         size_t have = it == c->seqs.end() ? 0 : it->second.pages.size();
-        if ((int64_t)len + S > g.max_pos) PT_FAIL(PT_ERR_INVALID_ARG, "sequence %d would reach position %d >= max_pos %d", seq_ids[b], len + S - 1, g.max_pos);
+        const int S = news(b);
+        if ((int64_t)len + S > g.max_pos) PT_FAIL(PT_ERR_INVALID_ARG, "sequence %d would reach position %lld >= max_pos %d", seq_ids[b], (long long)len + S - 1, g.max_pos);
         size_t need = ((size_t)len + S + c->ps - 1) / c->ps;
         if (need > have) pages_needed += need - have;
         maxlen = std::max(maxlen, len + S);
     }
+    // pages that the call writes and other sequences share are made the sequence's own (pt_kv_seq_fork)
+    std::vector<int32_t> adds(B);
+    for (int b = 0; b < B; ++b) adds[b] = news(b);
+    CowPlan cow;
+    cow.plan(c, seq_ids, adds.data(), B);
+    pages_needed += cow.pages_needed;
     if (pages_needed > c->free_list.size()) PT_FAIL(PT_ERR_CACHE_FULL, "call needs %zu new pages, %zu free", pages_needed, c->free_list.size());
     int maxp = (maxlen + c->ps - 1) / c->ps;
     const bool fp8 = c->kv_dtype == PT_KV_E4M3;
@@ -519,19 +549,25 @@ static pt_status forward(pt_model* m, pt_kv_cache* c, const void* x, int64_t x_s
         for (int b = 0; b < B; ++b) {
             auto it = c->seqs.find(seq_ids[b]);
             int len = it == c->seqs.end() ? 0 : it->second.len;
-            ctx_keys += ((int64_t)len + S + 15) / 16 * 16;
+            ctx_keys += ((int64_t)len + news(b) + 15) / 16 * 16;
         }
     Call k{};
-    size_t need_ws = carve(m, M, B, maxp, fp8, ctx_keys, (char*)workspace, &k.w);
+    size_t need_ws = carve(m, M, B, maxp, fp8, ctx_keys, ragged, (char*)workspace, &k.w);
     if (ws_bytes < need_ws) PT_FAIL(PT_ERR_BUFFER_TOO_SMALL, "workspace: %zu < %zu bytes", ws_bytes, need_ws);
+    if (!cow.entries.empty()) {
+        pt_status s = launch_copy_pages(c, c->pool, c->scales, c->num_pages, c->pool, c->scales, c->num_pages, cow.src.data(), cow.dst.data(),
+                                        (int)cow.src.size(), (cudaStream_t)stream);
+        if (s != PT_OK) return s;
+        cow.commit(c);
+    }
     for (int b = 0; b < B; ++b) {
         auto it = c->seqs.find(seq_ids[b]);
         int len = it == c->seqs.end() ? 0 : it->second.len;
-        pt_status s = pt_kv_seq_reserve(c, seq_ids[b], len + S);
+        pt_status s = pt_kv_seq_reserve(c, seq_ids[b], len + news(b));
         if (s != PT_OK) return s;
     }
     // per-call metadata, one upload
-    size_t mb = meta_bytes(M, B, maxp, fp8);
+    size_t mb = meta_bytes(M, B, maxp, fp8, ragged);
     m->meta_host.assign(mb, 0);
     char* hb = m->meta_host.data();
     char* db = (char*)workspace;
@@ -547,13 +583,14 @@ static pt_status forward(pt_model* m, pt_kv_cache* c, const void* x, int64_t x_s
     int32_t* h_nsp = (int32_t*)(hb + o_nsp);
     int32_t* h_bt = (int32_t*)(hb + o_bt);
     int32_t* h_items = (int32_t*)(hb + o_items);
+    int64_t r = 0;
     for (int b = 0; b < B; ++b) {
         const Seq& s = c->seqs[seq_ids[b]];
+        const int S = news(b);
         for (size_t i = 0; i < s.pages.size() && i < (size_t)maxp; ++i) h_bt[(size_t)b * maxp + i] = s.pages[i];
         h_len[b] = s.len + S;
-        for (int t = 0; t < S; ++t) {
+        for (int t = 0; t < S; ++t, ++r) {
             int pos = s.len + t;
-            int64_t r = (int64_t)b * S + t;
             h_pos[r] = pos;
             h_b[r] = b;
             h_kvoff[r] = slab_offset(c, s.pages[pos / c->ps], 0, 0, pos % c->ps);
@@ -570,21 +607,24 @@ static pt_status forward(pt_model* m, pt_kv_cache* c, const void* x, int64_t x_s
         int32_t* h_start = (int32_t*)(hb + o_start);
         int32_t* h_bta = (int32_t*)(hb + o_btattn);
         int32_t base = 0;                                 // first 16-token page of the sequence in the attention copy
+        r = 0;
         for (int b = 0; b < B; ++b) {
             const Seq& s = c->seqs[seq_ids[b]];
+            const int S = news(b);
             h_start[b] = s.len;
             max_start = std::max(max_start, s.len);
             const int np = (s.len + S + 15) / 16;
             for (int i = 0; i < np; ++i) h_bta[(size_t)b * maxp_attn + i] = base + i;
-            for (int t = 0; t < S; ++t) {
+            for (int t = 0; t < S; ++t, ++r) {
                 const int pos = s.len + t;
-                const int64_t r = (int64_t)b * S + t;
                 h_stage[r] = r * m->dh;
                 h_attn[r] = ((int64_t)(base + pos / 16) * 2 * g.kv_heads) * 16 * m->dh + (int64_t)(pos % 16) * m->dh;
             }
             base += np;
         }
     }
+    const size_t o_qlen = ragged ? sect((size_t)B * 4) : 0;
+    if (ragged) std::memcpy(hb + o_qlen, n_tok, (size_t)B * 4);
     int n_items = 0, max_splits = 1;
     if (decode) plan_decode_splits(h_len, B, c->ps, (int64_t)g.T * g.kv_heads, h_items, h_nsp, &n_items, &max_splits);
     cudaStream_t st = (cudaStream_t)stream;
@@ -604,26 +644,34 @@ static pt_status forward(pt_model* m, pt_kv_cache* c, const void* x, int64_t x_s
         k.w.meta.attn_pages = (int32_t)(ctx_keys / 16);
         k.w.meta.max_start = max_start;
     }
+    k.ragged = ragged;
+    k.w.meta.qlen = ragged ? (const int32_t*)(db + o_qlen) : nullptr;
     k.m = m; k.c = c; k.B = B; k.S = S; k.M = (int)M; k.x = x; k.x_stride = x_stride;
     k.out = (float*)out_h; k.st = st; k.decode = decode;
     k.n_items = n_items; k.max_splits = max_splits;
     k.items = (const int32_t*)(db + o_items); k.nsplit = (const int32_t*)(db + o_nsp);
     pt_status s = m->tc ? tc_forward(k) : simt_forward(k);
     if (s != PT_OK) return s;
-    for (int b = 0; b < B; ++b) c->seqs[seq_ids[b]].len += S;
+    for (int b = 0; b < B; ++b) c->seqs[seq_ids[b]].len += news(b);
     return PT_OK;
+}
+
+pt_status pt_extend(pt_model* m, pt_kv_cache* c, const void* x, int64_t x_track_stride, int32_t B, const int32_t* n_tokens,
+                    const int32_t* seq_ids, void* out_h, void* workspace, size_t ws_bytes, void* stream) {
+    if (!n_tokens) PT_FAIL(PT_ERR_INVALID_ARG, "null argument");
+    return forward(m, c, x, x_track_stride, B, 1, n_tokens, seq_ids, out_h, workspace, ws_bytes, stream, false);
 }
 
 pt_status pt_prefill(pt_model* m, pt_kv_cache* c, const void* x, int64_t x_track_stride,
                      int32_t B, int32_t S, const int32_t* seq_ids, void* out_h,
                      void* workspace, size_t ws_bytes, void* stream) {
-    return forward(m, c, x, x_track_stride, B, S, seq_ids, out_h, workspace, ws_bytes, stream, false);
+    return forward(m, c, x, x_track_stride, B, S, nullptr, seq_ids, out_h, workspace, ws_bytes, stream, false);
 }
 
 pt_status pt_decode_step(pt_model* m, pt_kv_cache* c, const void* x, int64_t x_track_stride,
                          int32_t B, const int32_t* seq_ids, void* out_h,
                          void* workspace, size_t ws_bytes, void* stream) {
-    return forward(m, c, x, x_track_stride, B, 1, seq_ids, out_h, workspace, ws_bytes, stream, true);
+    return forward(m, c, x, x_track_stride, B, 1, nullptr, seq_ids, out_h, workspace, ws_bytes, stream, true);
 }
 
 pt_status pt_set_debug_tap(pt_model* m, int32_t layer, void* dev_buf) {

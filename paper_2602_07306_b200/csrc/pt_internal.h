@@ -28,6 +28,7 @@ enum : int {
     LOC_FLASH_KEMPTY = 10, LOC_FLASH_VEMPTY = 11, LOC_FLASH_VRAW = 12, LOC_FLASH_KFULL = 13, LOC_FLASH_QFULL = 14,
     LOC_EMBED_TOKEN = 19, LOC_SELFTEST_WAIT = 20,
     LOC_FLASH_PFULL = 15, LOC_FLASH_VFULL = 16, LOC_FLASH_SFULL = 17, LOC_FLASH_OREADY = 18,
+    LOC_CHUNK_LEN = 21, LOC_CHUNK_PAGE = 22, LOC_CHUNK_WAIT = 23,
 };
 
 extern std::atomic<long long> g_launches;
@@ -109,6 +110,7 @@ struct pt_kv_cache {
     int64_t slab_elems;                   // num_pages * page_elems : one (track, layer)
     int64_t slab_vecs() const { return slab_elems / m->dh; }   // cached vectors (= scales) of one (track, layer)
     std::deque<int32_t> free_list;
+    std::vector<int32_t> ref;             // sequences that own each page (0: on the free list)
     std::unordered_map<int32_t, pt::Seq> seqs;
 };
 
@@ -128,6 +130,7 @@ struct Meta {
     const int32_t* bt_attn;       // [B][maxp_attn] 16-token pages of the attention copy
     const int32_t* ctx_start;     // [B] keys cached before the call (prefill)
     int32_t maxp_attn, attn_pages, max_start;
+    const int32_t* qlen;          // [B] ragged calls: new tokens per sequence
 };
 
 // PT-MoE with permuted tokens: R = moe_rows() rows per track, every (token, chosen expert) one row, experts in runs of
@@ -157,6 +160,7 @@ struct Work {
     void* kv_stage; // E4M3 caches: [T][K|V][kv_head][M][dh] bf16, this call's K and V as projected
     MoeWork moe;    // PT-MoE, permuted-token path (prefill calls of 512 rows or more)
     float* gates;   // PT-MoE: [T][M][E] routing weights of the current layer (0 for the experts a token did not choose)
+    void* chunk;    // ragged calls: scratch of the chunk attention
     void* attn_kv;  // E4M3 caches, prefill: [T][page][K|V][kv_head][16][dh] bf16 copy of code * scale of every key attended to
     size_t total;
 };
@@ -171,6 +175,7 @@ struct Call {
     Work w;
     cudaStream_t st;
     bool decode;
+    bool ragged;              // S differs between sequences: rows are packed, meta.qlen holds the counts (S is unused)
     // decode split plan (host): items of (b, first key, key count)
     int n_items, max_splits;
     const int32_t* items;     // device [n_items][4]: b, start, count, split index
@@ -198,6 +203,22 @@ struct ProfScope {
 // items gets 4 ints per range (batch row, first key, key count, range index); nsplit one per row.
 void plan_decode_splits(const int32_t* lens, int B, int ps, int64_t units, int32_t* items, int32_t* nsplit,
                         int* n_items, int* max_splits);
+
+// pt_api.cu: bytes of the codes (or model-dtype values) of a pool and of the whole pool
+pt_status kv_pool_layout(const pt_model* m, int32_t num_pages, int32_t page_size, int32_t kv_dtype, size_t* codes_bytes, size_t* total);
+
+// pt_kv_pages.cu: pages src[i] of one pool to pages dst[i] of another (or the same), in every (track, layer) slab, scales included
+pt_status launch_copy_pages(const pt_kv_cache* c, const char* src_pool, const float* src_scales, int32_t src_pages,
+                            char* dst_pool, float* dst_scales, int32_t dst_pages, const int32_t* src, const int32_t* dst, int n, cudaStream_t st);
+// Copy on write before a call appends adds[i] tokens to sequence seqs[i]; see pt_kv_pages.cu.
+struct CowPlan {
+    struct Entry { int32_t seq, index, page; };
+    std::vector<Entry> entries;           // table entry `index` of `seq` becomes `page`
+    std::vector<int32_t> src, dst;        // pages to copy
+    size_t pages_needed = 0;
+    void plan(const pt_kv_cache* c, const int32_t* seqs, const int32_t* adds, int n);
+    void commit(pt_kv_cache* c) const;
+};
 
 // pt_simt.cu
 pt_status simt_forward(Call& k);

@@ -3,6 +3,7 @@
 // that keeps the token ids on the device.  The LM head is the track-grouped tcgen05 GEMM with one
 // "track" (plain epilogue); everything else here is a small row-per-warp kernel.
 #include "pt_tc.h"
+#include "pt_sample.h"
 
 namespace pt {
 
@@ -219,9 +220,24 @@ pt_status pt_generate_workspace_bytes(const pt_model* m, int32_t B, int32_t S, i
     return PT_OK;
 }
 
-pt_status pt_generate(pt_model* m, pt_kv_cache* c, const int32_t* dev_prompt, int32_t B, int32_t S, int32_t n_new,
-                      const int32_t* seq_ids, int32_t* dev_tokens_out, float* dev_logits_out,
-                      void* workspace, size_t ws_bytes, void* stream) {
+// next token of every sequence from the step's logits: drawn with the given settings, or (sp == null) the largest logit
+static pt_status next_tokens(const pt_sampling* sp, const float* logits, int V, int32_t B, int step, int32_t n_new, int32_t* tok, int32_t* out, cudaStream_t st) {
+    if (sp) {
+        SampleP p{};
+        p.logits = logits; p.row_stride = V; p.vocab = V; p.u = sp->u + (size_t)step * B;
+        p.temperature = sp->temperature; p.top_k = sp->top_k; p.top_p = sp->top_p; p.min_p = sp->min_p;
+        p.token = tok; p.token2 = out + step; p.token2_stride = n_new;
+        p.prob = sp->prob ? sp->prob + step : nullptr; p.prob_stride = n_new;
+        return launch_sample(p, B, false, st);
+    }
+    k_argmax<<<B, 256, 0, st>>>(logits, V, tok, out + step, n_new);
+    g_launches.fetch_add(1, std::memory_order_relaxed);
+    return PT_OK;
+}
+
+static pt_status generate(pt_model* m, pt_kv_cache* c, const int32_t* dev_prompt, int32_t B, int32_t S, int32_t n_new,
+                          const int32_t* seq_ids, const pt_sampling* sp, int32_t* dev_tokens_out, float* dev_logits_out,
+                          void* workspace, size_t ws_bytes, void* stream) {
     pt_status s = lm_check(m);
     if (s != PT_OK) return s;
     if (!c || !dev_prompt || !seq_ids || !dev_tokens_out || !workspace || B < 1 || S < 1 || n_new < 1) { set_error("bad argument"); return PT_ERR_INVALID_ARG; }
@@ -240,8 +256,7 @@ pt_status pt_generate(pt_model* m, pt_kv_cache* c, const int32_t* dev_prompt, in
     if ((s = pt_prefill(m, c, x, 0, B, S, seq_ids, h, fwd, fwd_bytes, stream)) != PT_OK) return s;
     if ((s = pt_lm_head(m, (const float*)h + (size_t)(S - 1) * H, (int64_t)S * H, B, (float*)logits, nullptr, hn, hn_bytes, stream)) != PT_OK) return s;
     for (int i = 0; i < n_new; ++i) {
-        k_argmax<<<B, 256, 0, st>>>((const float*)logits, V, (int32_t*)tok, dev_tokens_out + i, n_new);
-        g_launches.fetch_add(1, std::memory_order_relaxed);
+        if ((s = next_tokens(sp, (const float*)logits, V, B, i, n_new, (int32_t*)tok, dev_tokens_out, st)) != PT_OK) return s;
         if (dev_logits_out)
             LM_CUDA(cudaMemcpy2DAsync(dev_logits_out + (size_t)i * V, (size_t)n_new * V * 4, logits, (size_t)V * 4, (size_t)V * 4, B, cudaMemcpyDeviceToDevice, st));
         if (i + 1 == n_new) break;
@@ -251,6 +266,20 @@ pt_status pt_generate(pt_model* m, pt_kv_cache* c, const int32_t* dev_prompt, in
     }
     LM_CUDA(cudaGetLastError());
     return PT_OK;
+}
+
+pt_status pt_generate(pt_model* m, pt_kv_cache* c, const int32_t* dev_prompt, int32_t B, int32_t S, int32_t n_new,
+                      const int32_t* seq_ids, int32_t* dev_tokens_out, float* dev_logits_out,
+                      void* workspace, size_t ws_bytes, void* stream) {
+    return generate(m, c, dev_prompt, B, S, n_new, seq_ids, nullptr, dev_tokens_out, dev_logits_out, workspace, ws_bytes, stream);
+}
+
+pt_status pt_generate_sample(pt_model* m, pt_kv_cache* c, const int32_t* dev_prompt, int32_t B, int32_t S, int32_t n_new,
+                             const int32_t* seq_ids, const pt_sampling* sampling, int32_t* dev_tokens_out, float* dev_logits_out,
+                             void* workspace, size_t ws_bytes, void* stream) {
+    if (!sampling || !sampling->u) { set_error("null argument"); return PT_ERR_INVALID_ARG; }
+    if (m && m->lm_buf && (sample_vocab_limit() < m->lm_vocab)) { set_error("vocab %d > %d", m->lm_vocab, sample_vocab_limit()); return PT_ERR_UNSUPPORTED; }
+    return generate(m, c, dev_prompt, B, S, n_new, seq_ids, sampling, dev_tokens_out, dev_logits_out, workspace, ws_bytes, stream);
 }
 
 }  // extern "C"

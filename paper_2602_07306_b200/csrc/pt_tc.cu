@@ -2,6 +2,7 @@
 // (QKV GEMM, attention, output-projection GEMM, gate/up GEMM, down GEMM); the track-sync of
 // Algorithm 1 is the down GEMM of every D-th layer run with its K loop over (track, k).
 #include "pt_tc.h"
+#include "pt_chunk.h"
 
 namespace pt {
 
@@ -248,7 +249,8 @@ pt_status tc_forward(Call& k) {
         }
         {
             ProfScope ps(m, st, 0);
-            if (fp8) s = k.decode ? launch_decode_attn_e4m3(k, q, l, o) : launch_flash_prefill_e4m3(k, q, o);
+            if (k.ragged) s = launch_chunk_attn_call(k, q, pool_l, o);
+            else if (fp8) s = k.decode ? launch_decode_attn_e4m3(k, q, l, o) : launch_flash_prefill_e4m3(k, q, o);
             else if (k.decode) s = launch_decode_attn(k, q, pool_l, o);
             else s = launch_flash_prefill(k, q, pool_l, o);
         }

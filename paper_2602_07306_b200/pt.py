@@ -38,6 +38,10 @@ class pt_config(C.Structure):
                 ("experts", C.c_int32), ("top_k", C.c_int32)]
 
 
+class pt_sampling(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in ("u", "temperature", "top_k", "top_p", "min_p", "prob")]
+
+
 _P, _I32, _I64, _SZ = C.c_void_p, C.c_int32, C.c_int64, C.c_size_t
 _PROTOS = {
     "pt_model_create": (_I32, [C.POINTER(pt_config), C.POINTER(_P)]),
@@ -74,6 +78,15 @@ _PROTOS = {
     "pt_lm_head": (_I32, [_P, _P, _I64, _I64, _P, _P, _P, _SZ, _P]),
     "pt_generate_workspace_bytes": (_I32, [_P, _I32, _I32, _I32, C.POINTER(_SZ)]),
     "pt_generate": (_I32, [_P, _P, _P, _I32, _I32, _I32, C.POINTER(_I32), _P, _P, _P, _SZ, _P]),
+    "pt_kv_seq_fork": (_I32, [_P, _I32, _I32, _I32]),
+    "pt_kv_free_pages": (_I32, [_P, C.POINTER(_I32)]),
+    "pt_kv_page_refs": (_I32, [_P, _I32, C.POINTER(_I32)]),
+    "pt_kv_compact": (_I32, [_P, C.POINTER(_I32), _P]),
+    "pt_kv_move_pool": (_I32, [_P, _I32, _P, _SZ, _P]),
+    "pt_extend_workspace_bytes": (_I32, [_P, _I64, _I32, _I32, _I32, _I64, C.POINTER(_SZ)]),
+    "pt_extend": (_I32, [_P, _P, _P, _I64, _I32, C.POINTER(_I32), C.POINTER(_I32), _P, _P, _SZ, _P]),
+    "pt_sample": (_I32, [_P, _I32, _I64, _I64, _I32, _P, _P, _P, _P, _P, _P, _P, _P]),
+    "pt_generate_sample": (_I32, [_P, _P, _P, _I32, _I32, _I32, C.POINTER(_I32), C.POINTER(pt_sampling), _P, _P, _P, _SZ, _P]),
     "pt_set_debug_tap": (_I32, [_P, _I32, _P]),
     "pt_device_status": (_I32, [_P, _P, C.POINTER(_I32), C.POINTER(_I32)]),
     "pt_profile_enable": (_I32, [_P, _I32]),
@@ -88,6 +101,10 @@ _PROTOS = {
                                             _P, _P, _P]),
     "pt_kernel_decode_attn_e4m3": (_I32, [_P, _P, _I64, _P, _I64, _P, _I32, C.POINTER(_I32), _I32, _I32, _I32, _I32, _I32, _I32,
                                           _P, _I32, _P, _SZ, _P, _P]),
+    "pt_kernel_chunk_attn_scratch_bytes": (_I32, [_I32, _I32, _I32, _I32, C.POINTER(_SZ)]),
+    "pt_kernel_chunk_attn": (_I32, [_P, _P, _I64, _P, _I32, _P, _P, _I32, _I32, _I32, _I32, _I32, _I32, _I32, _I32,
+                                    _P, _I32, _P, _SZ, _P, _P]),
+    "pt_kernel_kv_copy_pages": (_I32, [_P, _I32, _P, _I32, _I64, _I64, _P, _P, _I32, _P]),
     "pt_kernel_wait_selftest": (_I32, [_P, C.c_uint64, _P]),
     "pt_last_error": (C.c_char_p, []),
 }
@@ -283,6 +300,38 @@ class Model:
                                    ws.data_ptr(), ws.numel(), self._stream()))
         return out
 
+    def extend(self, cache: "Cache", x, n_tokens, seq_ids, out=None):
+        """A ragged batch: n_tokens[b] new tokens of sequence seq_ids[b], rows packed sequence by sequence.
+        x: torch tensor [T, M, H] (or [1, M, H] = shared input) in the model dtype, M = sum(n_tokens) -> fp32 [M, H]."""
+        torch = self.torch
+        assert x.is_cuda and x.dtype == self.tdtype and x.is_contiguous()
+        Tn, M, H = x.shape
+        assert Tn in (1, self.cfg.T) and H == self.cfg.hidden
+        stride = 0 if Tn == 1 and self.cfg.T > 1 else M * H
+        cnt, pcnt = _i32arr(n_tokens)
+        ids, pids = _i32arr(seq_ids)
+        assert len(ids) == len(cnt) and int(cnt.sum()) == M
+        if out is None:
+            out = torch.empty((M, H), dtype=torch.float32, device=self.device)
+        assert out.is_cuda and out.dtype == torch.float32 and out.is_contiguous() and out.numel() == M * H
+        ctx = 0
+        if cache.kv_dtype == PT_KV_E4M3:
+            ctx = sum((cache.length(int(s)) + int(n) + 15) // 16 * 16 for s, n in zip(ids, cnt))
+        key = (M, len(ids), cache.page_size, cache.kv_dtype, ctx)
+        have = getattr(self, "ext_key", None)
+        if have is None or have[2:4] != key[2:4] or any(a < b for a, b in zip((have[0], have[1], have[4]), (M, len(ids), ctx))):
+            if have is not None and have[2:4] == key[2:4]:
+                key = (max(M, have[0]), max(len(ids), have[1]), key[2], key[3], max(ctx, have[4]))
+            n = _SZ()
+            check(lib().pt_extend_workspace_bytes(self.h, *key, C.byref(n)))
+            self.ext_ws = None
+            self.ext_ws = torch.empty(n.value, dtype=torch.uint8, device=self.device)
+            self.ext_key = key
+        with torch.cuda.device(self.device):
+            check(lib().pt_extend(self.h, cache.h, x.data_ptr(), stride, len(ids), pcnt, pids, out.data_ptr(),
+                                  self.ext_ws.data_ptr(), self.ext_ws.numel(), self._stream()))
+        return out
+
     def decode_step(self, cache: "Cache", x, seq_ids, out=None):
         """x: torch tensor [T, B, H] (or [1, B, H]) in the model dtype -> fp32 [B, H]."""
         torch = self.torch
@@ -340,8 +389,11 @@ class Model:
                                    ws.data_ptr(), ws.numel(), self._stream()))
         return logits, tok
 
-    def generate(self, cache: "Cache", prompt, n_new: int, seq_ids, want_logits=False):
-        """prompt: int32 CUDA [B, S] -> (tokens int32 [B, n_new], logits fp32 [B, n_new, vocab] or None)."""
+    def generate(self, cache: "Cache", prompt, n_new: int, seq_ids, want_logits=False, *, u=None, temperature=None,
+                 top_k=None, top_p=None, min_p=None, prob=None):
+        """prompt: int32 CUDA [B, S] -> (tokens int32 [B, n_new], logits fp32 [B, n_new, vocab] or None).
+        Greedy, or with u (fp32 CUDA [n_new, B], uniform in [0, 1)) sampled: temperature, top_k, top_p, min_p are CUDA
+        tensors [B] as for sample(); prob (fp32 CUDA [B, n_new]) receives the tokens' probabilities."""
         torch = self.torch
         assert prompt.is_cuda and prompt.dtype == torch.int32 and prompt.is_contiguous()
         B, S = prompt.shape
@@ -353,6 +405,16 @@ class Model:
             self.gen_ws = None
             self.gen_ws = torch.empty(nb.value, dtype=torch.uint8, device=self.device)
         ids, pids = _i32arr(seq_ids)
+        if u is not None:
+            _sampling_args(torch, self.device, (n_new, B), u=u)
+            _sampling_args(torch, self.device, (B,), temperature=temperature, top_k=top_k, top_p=top_p, min_p=min_p)
+            _sampling_args(torch, self.device, (B, n_new), prob=prob)
+            sp = pt_sampling(*(None if a is None else a.data_ptr() for a in (u, temperature, top_k, top_p, min_p, prob)))
+            with torch.cuda.device(self.device):
+                check(lib().pt_generate_sample(self.h, cache.h, prompt.data_ptr(), B, S, n_new, pids, C.byref(sp), out.data_ptr(),
+                                               logits.data_ptr() if want_logits else None, self.gen_ws.data_ptr(), self.gen_ws.numel(), self._stream()))
+            return out, logits
+        assert temperature is None and top_k is None and top_p is None and min_p is None and prob is None, "sampling needs u"
         with torch.cuda.device(self.device):
             check(lib().pt_generate(self.h, cache.h, prompt.data_ptr(), B, S, n_new, pids, out.data_ptr(),
                                     logits.data_ptr() if want_logits else None, self.gen_ws.data_ptr(), self.gen_ws.numel(), self._stream()))
@@ -393,21 +455,23 @@ class Cache:
         n = _SZ()
         check(lib().pt_kv_cache_bytes_ex(model.h, num_pages, page_size, self.kv_dtype, C.byref(n)))
         self.bytes = n.value
-        if self.kv_dtype == PT_KV_E4M3:
-            # one byte buffer: the codes, then the fp32 scales (views below)
-            self.pool = torch.empty(n.value, dtype=torch.uint8, device=model.device)
-            c = model.cfg
-            vecs = c.T * c.L * num_pages * 2 * c.kv_heads * page_size
-            dh = c.hidden // c.heads
-            self.codes = self.pool[: vecs * dh]
-            self.scales = self.pool[n.value - vecs * 4:].view(torch.float32)
-        else:
-            self.pool = torch.empty(n.value // (2 if model.dtype == "bf16" else 4), dtype=model.tdtype, device=model.device)
+        self.pool, self.codes, self.scales = self._new_pool(num_pages, n.value)
         self.h = _P()
         check(lib().pt_kv_cache_alloc_ex(model.h, num_pages, page_size, self.kv_dtype, self.pool.data_ptr(), n.value, C.byref(self.h)))
         if free_order is not None:
             a, p = _i32arr(free_order)
             check(lib().pt_kv_set_free_list(self.h, p, len(a)))
+
+    def _new_pool(self, num_pages: int, nbytes: int):
+        """(pool, codes, scales) of a pool in the cache's format; codes and scales are None in the model dtype."""
+        model, torch = self.model, self.model.torch
+        if self.kv_dtype != PT_KV_E4M3:
+            return torch.empty(nbytes // (2 if model.dtype == "bf16" else 4), dtype=model.tdtype, device=model.device), None, None
+        # one byte buffer: the codes, then the fp32 scales (views)
+        pool = torch.empty(nbytes, dtype=torch.uint8, device=model.device)
+        c = model.cfg
+        vecs = c.T * c.L * num_pages * 2 * c.kv_heads * self.page_size
+        return pool, pool[: vecs * (c.hidden // c.heads)], pool[nbytes - vecs * 4:].view(torch.float32)
 
     def close(self):
         if self.h:
@@ -428,6 +492,38 @@ class Cache:
 
     def truncate(self, seq: int, n: int):
         check(lib().pt_kv_seq_truncate(self.h, seq, n))
+
+    def fork(self, src: int, dst: int, length: int | None = None):
+        """A new sequence dst that shares the first `length` (default: all) tokens of src; pages are copied on write."""
+        check(lib().pt_kv_seq_fork(self.h, src, dst, self.length(src) if length is None else length))
+
+    def free_pages(self) -> int:
+        v = _I32()
+        check(lib().pt_kv_free_pages(self.h, C.byref(v)))
+        return v.value
+
+    def page_refs(self, page: int) -> int:
+        v = _I32()
+        check(lib().pt_kv_page_refs(self.h, page, C.byref(v)))
+        return v.value
+
+    def compact(self) -> int:
+        """Move every page in use to the front of the pool (current stream); returns the pages copied."""
+        v = _I32()
+        with self.model.torch.cuda.device(self.model.device):
+            check(lib().pt_kv_compact(self.h, C.byref(v), self.model._stream()))
+        return v.value
+
+    def resize(self, num_pages: int) -> None:
+        """Continue in a new pool of num_pages pages, those in use at its front (current stream)."""
+        n = _SZ()
+        check(lib().pt_kv_cache_bytes_ex(self.model.h, num_pages, self.page_size, self.kv_dtype, C.byref(n)))
+        pool, codes, scales = self._new_pool(num_pages, n.value)
+        with self.model.torch.cuda.device(self.model.device):
+            check(lib().pt_kv_move_pool(self.h, num_pages, pool.data_ptr(), n.value, self.model._stream()))
+            self.pool.record_stream(self.model.torch.cuda.current_stream(self.model.device))
+        self.pool, self.codes, self.scales = pool, codes, scales
+        self.num_pages, self.bytes = num_pages, n.value
 
     def length(self, seq: int) -> int:
         v = _I32()
@@ -460,6 +556,95 @@ class Cache:
         shape = (c.T, c.L, self.num_pages, 2, c.kv_heads, self.page_size)
         codes = self.codes.view(torch.float8_e4m3fn).to(torch.float32).view(shape + (dh,))
         return codes * self.scales.view(shape + (1,))
+
+
+def _sampling_args(torch, device, shape, **arrays):
+    for name, a in arrays.items():
+        want = torch.int32 if name in ("top_k", "token") else torch.float32
+        if a is not None and (a.device != device or a.dtype != want or tuple(a.shape) != shape or not a.is_contiguous()):
+            raise ValueError(f"{name}: a contiguous {want} tensor of shape {shape} on {device} is wanted")
+
+
+def sample(logits, u, temperature=None, top_k=None, top_p=None, min_p=None, *, out=None, prob=None):
+    """One token per row of logits (fp32 or bf16 CUDA [n, vocab], rows may be strided) from the random numbers u (fp32 [n]):
+    temperature, then top_k, top_p and min_p, each a CUDA tensor [n] or None; see pt_sample in include/pt.h.
+    Returns (tokens int32 [n], probabilities fp32 [n]) in `out` and `prob` where given."""
+    import torch
+    if not logits.is_cuda or logits.dim() != 2 or logits.dtype not in (torch.float32, torch.bfloat16) or logits.stride(1) != 1:
+        raise ValueError("logits: an fp32 or bf16 CUDA tensor [n, vocab] with contiguous rows is wanted")
+    n, vocab = logits.shape
+    if out is None:
+        out = torch.empty(n, dtype=torch.int32, device=logits.device)
+    if prob is None:
+        prob = torch.empty(n, dtype=torch.float32, device=logits.device)
+    if u is None:
+        raise ValueError("u: random numbers are wanted")
+    _sampling_args(torch, logits.device, (n,), u=u, temperature=temperature, top_k=top_k, top_p=top_p, min_p=min_p, token=out, prob=prob)
+    ptr = lambda a: None if a is None else a.data_ptr()
+    with torch.cuda.device(logits.device):
+        check(lib().pt_sample(logits.data_ptr(), PT_F32 if logits.dtype == torch.float32 else PT_BF16, logits.stride(0) if n > 1 else vocab, n, vocab,
+                              u.data_ptr(), ptr(temperature), ptr(top_k), ptr(top_p), ptr(min_p), out.data_ptr(), prob.data_ptr(),
+                              torch.cuda.current_stream().cuda_stream))
+    return out, prob
+
+
+def kernel_kv_copy_pages(pool, src, dst, *, scales=None, out=None, out_scales=None):
+    """Pages src[i] of pool [T, L, pages, ...] (any type) to its pages dst[i] in every (track, layer) slab; `scales`
+    [T, L, pages, ...] likewise.  src, dst: host integers.  `out`, `out_scales`: another pool to copy to."""
+    import torch
+    src, dst = np.ascontiguousarray(src, np.int32), np.ascontiguousarray(dst, np.int32)
+    if src.ndim != 1 or src.shape != dst.shape:
+        raise ValueError("src and dst: two lists of the same length are wanted")
+    with torch.cuda.device(pool.device):
+        st = torch.cuda.current_stream().cuda_stream
+        for a, b in ((pool, out), (scales, out_scales)):
+            if a is None:
+                continue
+            b = a if b is None else b
+            if not (a.is_cuda and a.is_contiguous() and b.is_contiguous()) or a.dtype != b.dtype or a.device != pool.device or b.device != pool.device \
+                    or a.shape[:2] != b.shape[:2] or a.shape[3:] != b.shape[3:]:
+                raise ValueError("pools: contiguous CUDA tensors [T, L, pages, ...] that differ in their pages alone are wanted")
+            slabs = a.shape[0] * a.shape[1]
+            check(lib().pt_kernel_kv_copy_pages(a.data_ptr(), a.shape[2], b.data_ptr(), b.shape[2], slabs,
+                                                a.numel() * a.element_size() // (slabs * a.shape[2]), src.ctypes.data, dst.ctypes.data, len(src), st))
+
+
+def chunk_attn_scratch(T: int, B: int, nq: int, dh: int, device="cuda:0"):
+    """Scratch buffer for kernel_chunk_attn calls of up to B sequences (one per stream that calls at the same time)."""
+    import torch
+    n = _SZ()
+    check(lib().pt_kernel_chunk_attn_scratch_bytes(T, B, nq, dh, C.byref(n)))
+    return torch.empty(n.value, dtype=torch.uint8, device=device)
+
+
+def kernel_chunk_attn(q, pool_l, block_table, q_len, kv_len, *, nq, nkv, dh, ps, out=None, scratch=None, status=None, impl=None):
+    """q bf16 [T, M, nq*dh], rows packed by sequence; pool_l bf16 [T, pages, 2, nkv, ps, dh]; block_table int32 [B, maxp],
+    q_len, kv_len int32 [B] (all CUDA); impl 0 = tcgen05 kernel, 1 = plain kernel, None = the first where it serves the shape.
+    Returns (out bf16 [T, M, nq*dh], status int32[16])."""
+    import torch
+    T, M, width = q.shape
+    B, maxp = block_table.shape
+    pages = pool_l.shape[1]
+    assert q.is_cuda and q.is_contiguous() and pool_l[0].is_contiguous() and block_table.is_contiguous() and q_len.is_contiguous() and kv_len.is_contiguous()
+    assert q.dtype == pool_l.dtype == torch.bfloat16 and block_table.dtype == q_len.dtype == kv_len.dtype == torch.int32
+    assert width == nq * dh and tuple(pool_l.shape) == (T, pages, 2, nkv, ps, dh) and q_len.numel() == kv_len.numel() == B
+    assert q.device == pool_l.device == block_table.device == q_len.device == kv_len.device
+    if out is None:
+        out = torch.empty_like(q)
+    if scratch is None:
+        scratch = chunk_attn_scratch(T, B, nq, dh, q.device)
+    if status is None:
+        status = torch.zeros(16, dtype=torch.int32, device=q.device)
+    assert out.device == q.device and out.dtype == q.dtype and out.shape == q.shape and out.is_contiguous()
+    assert scratch.device == q.device and status.device == q.device and status.dtype == torch.int32 and status.numel() >= 16
+    if impl is None:
+        impl = 0 if dh in (64, 128) and ps % 16 == 0 else 1
+    with torch.cuda.device(q.device):
+        check(lib().pt_kernel_chunk_attn(q.data_ptr(), pool_l.data_ptr(), pool_l.stride(0), block_table.data_ptr(), maxp,
+                                         q_len.data_ptr(), kv_len.data_ptr(), T, B, M, nq, nkv, dh, ps, pages, out.data_ptr(), impl,
+                                         scratch.data_ptr(), scratch.numel() * scratch.element_size(), status.data_ptr(),
+                                         torch.cuda.current_stream().cuda_stream))
+    return out, status
 
 
 def kernel_gemm_bf16(a, w, bn: int = 0, fold_tracks: bool = False):
