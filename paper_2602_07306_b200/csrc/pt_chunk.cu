@@ -76,9 +76,13 @@ k_chunk_simple(const ChunkP p) {
 
 }  // namespace
 
-size_t chunk_scratch_bytes(int T, int B, int nq, int dh) { return 256; }
+static bool chunk_tc_supported(int dh, int ps) { return (dh == 64 || dh == 128) && ps % 16 == 0; }
+
+// The same whatever the batch: the tensor-memory kernel cuts its work once per block, not once per sequence.
+size_t chunk_scratch_bytes(int T, int B, int nq, int dh) { return dh == 32 ? 256 : chunk_tc_scratch_bytes(dh); }
 
 pt_status launch_chunk_attn(const ChunkP& p, int dh, void* scratch, bool simple, cudaStream_t st) {
+    if (!simple && chunk_tc_supported(dh, p.ps)) return launch_chunk_attn_tc(p, dh, scratch, st);
     const int64_t blocks = ((int64_t)p.M * p.nq + 3) / 4;
     if (blocks > 0x7fffffff || p.T > 65535) { set_error("chunk attention grid too large"); return PT_ERR_INVALID_ARG; }
     const dim3 grid((unsigned)blocks, p.T);
@@ -130,7 +134,7 @@ extern "C" pt_status pt_kernel_chunk_attn(const void* q, const void* pool_l, int
     if (dh != 32 && dh != 64 && dh != 128) { set_error("head_dim %d not in {32, 64, 128}", dh); return PT_ERR_UNSUPPORTED; }
     if (ps < 8 || ps > 64 || ps % 8) { set_error("page size must be a multiple of 8 in [8, 64]"); return PT_ERR_INVALID_ARG; }
     if (impl != 0 && impl != 1) { set_error("impl must be 0 or 1"); return PT_ERR_INVALID_ARG; }
-    if (impl == 0 && (dh == 32 || ps % 16)) { set_error("impl 0 needs head_dim 64 or 128 and pages of a multiple of 16 tokens"); return PT_ERR_UNSUPPORTED; }
+    if (impl == 0 && !chunk_tc_supported(dh, ps)) { set_error("impl 0 needs head_dim 64 or 128 and pages of a multiple of 16 tokens"); return PT_ERR_UNSUPPORTED; }
     if ((uintptr_t)q % 16 || (uintptr_t)pool_l % 16 || pool_track_stride % 8 || (uintptr_t)out % 16 || (uintptr_t)scratch % 256) {
         set_error("q, out and the pool must be 16-byte aligned (its track stride a multiple of 8 elements), scratch 256-byte"); return PT_ERR_MISALIGNED;
     }

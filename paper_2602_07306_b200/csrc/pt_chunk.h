@@ -18,8 +18,11 @@ struct ChunkP {
 };
 
 size_t chunk_scratch_bytes(int T, int B, int nq, int dh);
-// simple: the plain kernel (one warp per row and head), which takes any head_dim and page size
+// simple: the plain kernel (one warp per row and head), which takes any head_dim and page size and serves what the other does not
 pt_status launch_chunk_attn(const ChunkP& p, int dh, void* scratch, bool simple, cudaStream_t st);
+// pt_chunk_tc.cu: the tensor-memory kernel (head_dim 64 or 128, pages of a multiple of 16 tokens)
+size_t chunk_tc_scratch_bytes(int dh);
+pt_status launch_chunk_attn_tc(const ChunkP& p, int dh, void* scratch, cudaStream_t st);
 // the attention of one layer of a pt_extend call
 pt_status launch_chunk_attn_call(Call& k, const __nv_bfloat16* q, const __nv_bfloat16* pool_l, __nv_bfloat16* o);
 
