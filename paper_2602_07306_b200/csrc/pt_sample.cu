@@ -14,11 +14,20 @@
 // maximum) is zero: such a token is never drawn.  The exponential is evaluated in double; the multiple rounds it once,
 // an absolute error of 2^-45 against a sum of at least 1.
 //
-// One cluster of CL blocks takes a row (CL = 1 for short rows): each block reads its slice from global memory once and
-// keeps it in shared memory; everything after that runs there, and the blocks exchange histograms through distributed
-// shared memory.  A threshold is found by radix selection: a histogram of the distance to the maximum (counts alone
-// bound the cumulative weight within a bin's width), then histograms with exact counts and weights over the few bins
-// that may hold the threshold, down to a single key.
+// Two ways to hold a row.  SLICES: a cluster of up to 8 blocks takes it, each block reads its slice from global memory once
+// and keeps it in shared memory, and the blocks exchange what they found through distributed shared memory - for few rows,
+// whose time is latency.  ROWS: one block takes the whole row and streams over it, the first pass from HBM and the later
+// ones mostly from L2 - for many rows, where exchanging between blocks costs more than reading again.
+//
+// Two ways to find the kept set.
+// Few candidates (top-k up to kListK, or min-p alone): the k-th largest of the maxima that the threads found, four each, is a
+// lower bound of the k-th largest logit, so a second pass collects the logits above it - little more than k - and one block
+// sorts them and finishes the row alone.
+// Everything else (top-p over the whole vocabulary, a large k, no filter): a histogram of the distance to the maximum in
+// kBins bins bounds, from counts alone, which bins may hold the threshold: a weight in a bin is known to the bin's width,
+// 0.8 %, and so are the sums before and behind a bin.  One pass then sums the weights above those bins exactly and lists the logits inside them, and one block sorts
+// that list and cuts it.  Where the list is too long (many equal logits), or top-p follows a large top-k, histograms with
+// exact counts and weights narrow the threshold down to one key instead.
 #include <cooperative_groups.h>
 
 #include "pt_internal.h"
@@ -31,12 +40,18 @@ namespace pt {
 namespace {
 
 constexpr int kThreads = 512, kWarps = kThreads / 32;
-constexpr int kBins = 2048;                    // first histogram: distance to the maximum
-constexpr int kFine = 1024;                    // later histograms: keys
+constexpr int kBins = 4096;                    // first histogram: distance to the maximum
+constexpr int kFine = 2048;                    // later histograms: keys
+constexpr int kCoarse = kThreads;              // histogram of the threads' maxima
+constexpr int kList = 2048;                    // entries one block sorts
+constexpr int kListK = 1024;                   // largest top-k that goes that way
 constexpr int kFracBits = 44;
 constexpr float kRange = 31.5f;                // nats below the maximum that the bins cover; beyond it weights are zero
+constexpr float kSlack = 4e-7f;                // relative rounding of a distance and its bin number, three times over
 constexpr int kMaxCluster = 8;
-constexpr int kMaxSlice = 49152;               // elements of a slice: 192 KB
+constexpr int kRowsFrom = 48;                  // rows from which a block takes a whole row
+constexpr int kMaxSlice = 32768;               // elements of a slice: 128 KB
+constexpr int kMaxVocab = 393216;
 
 typedef unsigned long long u64;
 
@@ -45,45 +60,63 @@ __device__ __forceinline__ uint32_t key_of(float x) {
     const uint32_t b = __float_as_uint(x + 0.0f);
     return (b & 0x80000000u) ? b : ~b & 0x7fffffffu;
 }
+__device__ __forceinline__ float value_of(uint32_t key) { return __uint_as_float((key & 0x80000000u) ? key : ~key & 0x7fffffffu); }
 
 struct Row {
     float max, inv_bin;                        // bin of x = (max - x) * inv_bin
-    double inv_t;                              // log2(e) / temperature
+    double maxd, inv_t;                        // inv_t: log2(e) / temperature
     float x_min;                               // min-p: kept values are >= x_min
 };
 
-// w(x) * 2^44, rounded to the nearest whole number
+// w(x) * 2^44, rounded to the nearest whole number: 2^y with y = (x - max) log2(e) / temperature split into a whole number n
+// and f in [-1/2, 1/2]; 2^f by the polynomial of degree 9 that agrees with it at the ten Chebyshev nodes of the interval
+// (relative error 1.4e-14, a quarter of the last place kept of the largest weight); n goes into the exponent, and adding
+// 2^52 rounds to a whole number.
 __device__ __forceinline__ u64 weight(const Row& r, float x) {
-    if (x == r.max) return 1ull << kFracBits;  // also for an infinite maximum, whose distance to itself has no value
-    const double t = ((double)x - (double)r.max) * r.inv_t;
-    if (!(t > -46.0)) return 0;
-    return (u64)__double2ull_rn(exp2(t + (double)kFracBits));
-}
-__device__ __forceinline__ int bin_of(const Row& r, float x) {
-    if (x == r.max) return 0;
-    const float d = (r.max - x) * r.inv_bin;
-    return d < (float)(kBins - 1) ? (int)d : kBins - 1;      // also for an infinite distance
+    const double y = ((double)x - r.maxd) * r.inv_t;
+    const double magic = 6755399441055744.0;   // 1.5 * 2^52: the sum's low word is round(y)
+    const double k = y + magic;
+    const double f = y - (k - magic);
+    double p = 1.0205905413765595e-07;
+    p = fma(p, f, 1.325964524488711e-06);
+    p = fma(p, f, 1.5252672924850737e-05);
+    p = fma(p, f, 0.0001540343375125101);
+    p = fma(p, f, 0.0013333558200794592);
+    p = fma(p, f, 0.009618129193934313);
+    p = fma(p, f, 0.05550410866465167);
+    p = fma(p, f, 0.2402265069564034);
+    p = fma(p, f, 0.6931471805599462);
+    p = fma(p, f, 1.0000000000000135);
+    const double w = __hiloint2double(__double2hiint(p) + ((__double2loint(k) + kFracBits) << 20), __double2loint(p)) + 4503599627370496.0;
+    return y > -46.0 ? (u64)__double_as_longlong(w) & 0xfffffffffffffull : 0ull;      // also 0 for a masked x
 }
 
 struct Shared {
-    uint32_t hist[kBins];
-    u64 mass[kFine];
+    union {
+        uint32_t bins[kBins];
+        struct { u64 mass[kFine]; uint32_t hist[kFine]; };      // narrowing by keys
+        struct { u64 all[kList], list[kList]; };                // entries of the row (in the first block), of this block
+    };
+    uint32_t coarse[kCoarse];
     float red[kWarps];
-    int redi[kWarps];
-    u64 warp_sum[kWarps];                      // weight kept by each warp's part of the slice
+    u64 wsum[kMaxCluster * kWarps];            // first block: weight kept by the part of every warp of the cluster
+    u64 warp_tmp[kWarps], warp_tmp2[kWarps];
     uint32_t warp_cnt[kWarps];
-    u64 blk_mass;                              // weight of this block's elements above the searched bins
+    u64 blk_mass, blk_all;                     // weight of this block's elements above the searched bins, and of all
     u64 scan[kWarps + 1];
     double dscan[kWarps + 1];
+    double share[3];                           // totals of this block's share of the bins: counts, upper and lower bounds
+    float4 edge[2];                            // ROWS: the quads that the row does not fill
     float max;
-    int arg;
-    // found by a scan
+    int n_list, n_all;                         // entries of this block; of the row (in the first block)
+    // found by a scan, or handed over by the block that found it
     int bin;
     u64 before_mass, before_cnt, total;
-    int zone_a, zone_b;
-    int cut;
-    int token;
+    int zone_a, zone_b, tail_a, tail_b, cut, first;
+    uint32_t thr; int owner; u64 target, obefore, Z;
 };
+
+static_assert(((sizeof(Shared) + 15) & ~15) + (kMaxSlice + 4) * 4 <= 232448, "shared memory of one block");
 
 template <class V> __device__ __forceinline__ V warp_incl(V v) {
     const int lane = threadIdx.x & 31;
@@ -91,379 +124,678 @@ template <class V> __device__ __forceinline__ V warp_incl(V v) {
     for (int o = 1; o < 32; o <<= 1) { const V u = __shfl_up_sync(0xffffffffu, v, o); if (lane >= o) v += u; }
     return v;
 }
-// exclusive prefix of v over the block's threads; *total = the block's sum.  buf holds kWarps + 1 values.
-template <class V> __device__ __forceinline__ V block_excl(V v, V* buf, V* total) {
+template <class V> __device__ __forceinline__ V warp_sum(V v) {
+#pragma unroll
+    for (int o = 16; o; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+    return v;
+}
+// exclusive prefix of v over the block's threads; total = the block's sum.  buf holds kWarps + 1 values.
+template <class V> __device__ __forceinline__ V block_excl(V v, V* buf, V& total) {
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const V incl = warp_incl(v);
     __syncthreads();
     if (lane == 31) buf[warp] = incl;
     __syncthreads();
-    if (warp == 0) {
-        V w = lane < kWarps ? buf[lane] : V(0);
-        const V wi = warp_incl(w);
-        if (lane < kWarps) buf[lane] = wi - w;
-        if (lane == kWarps - 1) buf[kWarps] = wi;
-    }
-    __syncthreads();
-    *total = buf[kWarps];
-    return buf[warp] + incl - v;
+    V w = lane < kWarps ? buf[lane] : V(0);
+    const V wi = warp_incl(w);
+    total = __shfl_sync(0xffffffffu, wi, kWarps - 1);
+    return __shfl_sync(0xffffffffu, wi - w, warp) + incl - v;
 }
 
-template <class E>
-__global__ void __launch_bounds__(kThreads)
+// a[0 .. n) ascending, n a power of two >= 64; pairs closer than 64 apart stay inside a warp's 64 elements
+__device__ __forceinline__ void sort_block(u64* a, int n) {
+    for (int size = 2; size <= n; size <<= 1)
+        for (int stride = size >> 1; stride; stride >>= 1) {
+            for (int i = threadIdx.x; i < n / 2; i += kThreads) {
+                const int lo = 2 * i - (i & (stride - 1)), hi = lo + stride;
+                const u64 x = a[lo], y = a[hi];
+                if ((x > y) == ((lo & size) == 0)) { a[lo] = y; a[hi] = x; }
+            }
+            if (stride > 32 || (stride == 1 && size >= 64)) __syncthreads(); else __syncwarp();
+        }
+}
+
+// Four logits at p (which is aligned to them): -inf in place of NaN.
+__device__ __forceinline__ float4 load4(const float* p) {
+    const float4 v = __ldcg(reinterpret_cast<const float4*>(p));
+    return make_float4(fmaxf(v.x, -INFINITY), fmaxf(v.y, -INFINITY), fmaxf(v.z, -INFINITY), fmaxf(v.w, -INFINITY));
+}
+__device__ __forceinline__ float4 load4(const __nv_bfloat16* p) {
+    const uint2 b = __ldcg(reinterpret_cast<const uint2*>(p));
+    return make_float4(fmaxf(__uint_as_float(b.x << 16), -INFINITY), fmaxf(__uint_as_float(b.x & 0xffff0000u), -INFINITY),
+                       fmaxf(__uint_as_float(b.y << 16), -INFINITY), fmaxf(__uint_as_float(b.y & 0xffff0000u), -INFINITY));
+}
+
+template <class E, bool SLICES>
+__global__ void __launch_bounds__(kThreads, 2)
 k_sample(const SampleP p, const int slice) {
     extern __shared__ __align__(16) unsigned char smem_raw[];
     Shared& sh = *reinterpret_cast<Shared*>(smem_raw);
-    float* xs = reinterpret_cast<float*>(smem_raw + ((sizeof(Shared) + 15) & ~15));
+    float4* xs = reinterpret_cast<float4*>(smem_raw + ((sizeof(Shared) + 15) & ~15));
     cg::cluster_group cluster = cg::this_cluster();
-    const int CL = (int)cluster.num_blocks(), rank = (int)cluster.block_rank();
+    const int CL = SLICES ? (int)cluster.num_blocks() : 1, rank = SLICES ? (int)cluster.block_rank() : 0;
+    auto sync_row = [&]() { if (SLICES) cluster.sync(); else __syncthreads(); };
+    auto remote = [&](auto* ptr, int q) { return SLICES ? cluster.map_shared_rank(ptr, q) : ptr; };
     const int64_t row = blockIdx.x / CL;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    const int base = rank * slice;
-    const int count = max(0, min(slice, p.vocab - base));
-    const E* src = reinterpret_cast<const E*>(p.logits) + row * p.row_stride + base;
-    const int per_warp = (count + kWarps - 1) / kWarps;       // every warp owns a contiguous part of the slice
-    const int w0 = min(count, warp * per_warp), w1 = min(count, w0 + per_warp);
+    const int count = max(0, min(slice, p.vocab - rank * slice));
+    const E* src = reinterpret_cast<const E*>(p.logits) + row * p.row_stride + rank * slice;
+    // quads of four, aligned as in global memory: element i of the slice is component (i + shift) % 4 of quad (i + shift) / 4
+    // (slices are a multiple of four long: the same shift in every block)
+    const int shift = (int)((reinterpret_cast<uintptr_t>(src) / sizeof(E)) & 3);
+    const int base = rank * slice - shift;                    // index of component 0 of quad 0
+    const int quads = count ? (count + shift + 3) >> 2 : 0;
+    const int per_warp = (quads + kWarps - 1) / kWarps;       // every warp owns a contiguous part of the slice
+    const int v0 = min(quads, warp * per_warp), v1 = min(quads, v0 + per_warp);
+    const E* quad0 = src - shift;
+    const int full0 = shift ? 1 : 0, full1 = (count + shift) >> 2;     // quads [full0, full1) lie inside the row
 
-    // ---- the slice, and the maximum with its lowest index (NaN counts as masked)
-    float best = -INFINITY; int arg = 0x7fffffff;
-    for (int i = tid; i < count; i += kThreads) {
-        float x = (float)src[i];
-        if (!(x == x)) x = -INFINITY;
-        xs[i] = x;
-        if (x > best) { best = x; arg = base + i; }
-    }
-    auto better = [](float v, int i, float bv, int bi) { return v > bv || (v == bv && i < bi); };
+    // ---- the slice (NaN counts as masked) and its maximum
+    sh.coarse[tid] = 0;
+    if (tid == 0) { sh.n_list = 0; sh.n_all = 0; sh.first = 0x7fffffff; }
+    if (tid < 2) {                                            // the quads at the ends: filled up with -inf
+        const int v = tid ? quads - 1 : 0;
+        float e[4];
 #pragma unroll
-    for (int o = 16; o; o >>= 1) {
-        const float v = __shfl_xor_sync(0xffffffffu, best, o); const int i = __shfl_xor_sync(0xffffffffu, arg, o);
-        if (better(v, i, best, arg)) { best = v; arg = i; }
+        for (int c = 0; c < 4; ++c) { const int i = v * 4 + c - shift; e[c] = v >= 0 && i >= 0 && i < count ? fmaxf((float)src[i], -INFINITY) : -INFINITY; }
+        sh.edge[tid] = make_float4(e[0], e[1], e[2], e[3]);
     }
-    if (lane == 0) { sh.red[warp] = best; sh.redi[warp] = arg; }
     __syncthreads();
-    if (tid == 0) {
-        for (int w = 1; w < kWarps; ++w) if (better(sh.red[w], sh.redi[w], best, arg)) { best = sh.red[w]; arg = sh.redi[w]; }
-        sh.max = best; sh.arg = arg;
+    bool pos_inf = false;                                     // the row's maximum is +inf: 0 in its places, -inf elsewhere
+    auto fetch = [&](int v) {                                 // quad v from global memory
+        float4 q = sh.edge[v == 0 ? 0 : 1];
+        if (v >= full0 && v < full1) q = load4(quad0 + v * 4);
+        return q;
+    };
+    auto get = [&](int v) {
+        if (SLICES) return xs[v];
+        float4 q = fetch(v);
+        if (pos_inf) q = make_float4(q.x == INFINITY ? 0.f : -INFINITY, q.y == INFINITY ? 0.f : -INFINITY, q.z == INFINITY ? 0.f : -INFINITY, q.w == INFINITY ? 0.f : -INFINITY);
+        return q;
+    };
+    float4 tmax = make_float4(-INFINITY, -INFINITY, -INFINITY, -INFINITY);
+#pragma unroll 8
+    for (int v = v0 + lane; v < v1; v += 32) {
+        const float4 q = fetch(v);
+        if (SLICES) xs[v] = q;
+        tmax = make_float4(fmaxf(tmax.x, q.x), fmaxf(tmax.y, q.y), fmaxf(tmax.z, q.z), fmaxf(tmax.w, q.w));
     }
-    cluster.sync();
-    best = -INFINITY; arg = 0x7fffffff;
-    for (int r = 0; r < CL; ++r) {
-        const Shared* o = cluster.map_shared_rank(&sh, r);
-        if (better(o->max, o->arg, best, arg)) { best = o->max; arg = o->arg; }
+    {
+        float m = fmaxf(fmaxf(tmax.x, tmax.y), fmaxf(tmax.z, tmax.w));
+#pragma unroll
+        for (int o = 16; o; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
+        if (lane == 0) sh.red[warp] = m;
+        __syncthreads();
+        m = lane < kWarps ? sh.red[lane] : -INFINITY;
+#pragma unroll
+        for (int o = 8; o; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
+        if (tid == 0) sh.max = m;
     }
-    const float temperature = p.temperature ? p.temperature[row] : 1.0f;
-    const bool nothing = best == -INFINITY;                   // every logit masked: token 0, probability 0
-    const bool greedy = !(temperature > 0.f && temperature < INFINITY);
-    if (nothing || greedy) {
-        if (rank == 0 && tid == 0) {
-            const int tok = nothing ? 0 : arg;
-            if (p.token) p.token[row] = tok;
-            if (p.token2) p.token2[row * p.token2_stride] = tok;
-            if (p.prob) p.prob[row * p.prob_stride] = nothing ? 0.f : 1.f;
+    sync_row();
+    Row r;
+    {
+        float m = lane < CL ? *remote(&sh.max, lane) : -INFINITY;
+#pragma unroll
+        for (int o = kMaxCluster / 2; o; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
+        r.max = __shfl_sync(0xffffffffu, m, 0);
+    }
+    float temperature = p.temperature ? p.temperature[row] : 1.0f;
+    const bool nothing = r.max == -INFINITY;                  // every logit masked: token 0, probability 0
+    if (nothing || !(temperature > 0.f && temperature < INFINITY)) {
+        // greedy: the lowest index of the maximum, in the parts of the threads that met it
+        if (!nothing && fmaxf(fmaxf(tmax.x, tmax.y), fmaxf(tmax.z, tmax.w)) == r.max) {
+            for (int v = v0 + lane; v < v1; v += 32) {
+                const float4 q = get(v);
+                const int i = q.x == r.max ? 0 : q.y == r.max ? 1 : q.z == r.max ? 2 : q.w == r.max ? 3 : -1;
+                if (i >= 0) { atomicMin(&sh.first, base + v * 4 + i); break; }
+            }
         }
-        cluster.sync();                                       // no block leaves while another still reads its maximum
+        sync_row();
+        if (rank == 0 && warp == 0) {
+            int at = lane < CL ? *remote(&sh.first, lane) : 0x7fffffff;
+            at = nothing ? 0 : __reduce_min_sync(0xffffffffu, at);
+            if (lane == 0) {
+                if (p.token) p.token[row] = at;
+                if (p.token2) p.token2[row * p.token2_stride] = at;
+                if (p.prob) p.prob[row * p.prob_stride] = nothing ? 0.f : 1.f;
+            }
+        }
+        sync_row();                                           // no block leaves while another still reads its shared memory
         return;
     }
-    Row r;
-    r.max = best;
+    if (r.max == INFINITY) {                                  // +inf shares the whole weight: the same row with 0 and -inf
+        pos_inf = true;
+        auto flat = [](float x) { return x == INFINITY ? 0.f : -INFINITY; };
+        if (SLICES)
+            for (int v = v0 + lane; v < v1; v += 32) { const float4 q = xs[v]; xs[v] = make_float4(flat(q.x), flat(q.y), flat(q.z), flat(q.w)); }
+        tmax = make_float4(flat(tmax.x), flat(tmax.y), flat(tmax.z), flat(tmax.w));
+        r.max = 0.f;
+    }
+    temperature = fminf(fmaxf(temperature, 1e-30f), 1e36f);   // so that bin widths are finite and not zero
+    r.maxd = (double)r.max;
     r.inv_t = 1.4426950408889634 / (double)temperature;
     r.inv_bin = (float)(kBins - 1) / (kRange * temperature);
     r.x_min = -INFINITY;
     if (p.min_p) {
         const float mp = p.min_p[row];
-        if (mp > 0.f) r.x_min = mp >= 1.f ? best : __double2float_ru((double)best + (double)temperature * log((double)mp));
+        if (mp > 0.f) r.x_min = mp >= 1.f ? r.max : __double2float_ru(r.maxd + (double)temperature * log((double)mp));
     }
-    const int k = p.top_k ? p.top_k[row] : 0;
     const float tp = p.top_p ? p.top_p[row] : 1.0f;
-    const bool use_k = k > 0 && k < p.vocab, use_p = tp < 1.0f;
-    // kept so far: key < thr, or key == thr and index <= cut
-    uint32_t thr = 0xffffffffu; int cut = 0x7fffffff;
-
-    // ---- counts by distance to the maximum
-    if (use_k || use_p) {
-        for (int i = tid; i < kBins; i += kThreads) sh.hist[i] = 0;
-        __syncthreads();
-        for (int i = tid; i < count; i += kThreads) {
-            const int b = bin_of(r, xs[i]);
-            if (b < kBins - 1) atomicAdd(&sh.hist[b], 1u);
-        }
-    }
-    // a thread's four bins of the whole row
-    uint32_t c4[4] = {0, 0, 0, 0};
-    auto row_hist = [&]() {
-        cluster.sync();
-        for (int q = 0; q < CL; ++q) {
-            const uint4 v = *reinterpret_cast<const uint4*>(cluster.map_shared_rank(sh.hist, q) + tid * 4);
-            c4[0] += v.x; c4[1] += v.y; c4[2] += v.z; c4[3] += v.w;
-        }
-        cluster.sync();
+    const int k = tp <= 0.f ? 1 : p.top_k ? p.top_k[row] : 0; // a reach of nothing keeps one token
+    const bool use_k = k > 0 && k < p.vocab, use_p = tp < 1.0f && tp > 0.f;
+    const u64 frac64 = use_p ? (u64)__double2ull_rz((double)tp * 18446744073709551616.0) : 0ull;
+    const float u = p.u[row];
+    const u64 U = u >= 1.f ? ~0ull : (u > 0.f ? (u64)__double2ull_rz((double)u * 18446744073709551616.0) : 0ull);
+    auto store = [&](int tok, float x, u64 Z) {
+        if (p.token) p.token[row] = tok;
+        if (p.token2) p.token2[row * p.token2_stride] = tok;
+        if (p.prob) p.prob[row * p.prob_stride] = (float)(exp2(((double)x - r.maxd) * r.inv_t) / ((double)Z * 0x1p-44));
     };
-    if (use_k || use_p) row_hist();
+    // the reach of top-p: ceil(whole * p), at least 1
+    auto reach = [&](u64 whole) { const u64 hi = __umul64hi(whole, frac64); return max((u64)1, hi + (whole * frac64 != 0)); };
+    auto entry = [&](float x, int idx) {                      // one more entry of this block's list
+        const int at = atomicAdd(&sh.n_list, 1);
+        if (at < kList) sh.list[at] = (u64)key_of(x) << 32 | (uint32_t)idx;
+    };
+    // brings the blocks' lists together in the first block; returns the entries of the row (more than kList: not brought)
+    auto gather = [&]() {
+        __syncthreads();
+        const int n = sh.n_list;
+        if (tid == 0) sh.bin = n ? atomicAdd(remote(&sh.n_all, 0), n) : 0;
+        __syncthreads();
+        u64* to = remote(&sh.all[0], 0) + sh.bin;
+        if (n <= kList && sh.bin + n <= kList)
+            for (int i = tid; i < n; i += kThreads) to[i] = sh.list[i];
+        sync_row();
+        return *remote(&sh.n_all, 0);
+    };
+    // sorts the n entries of `all`: descending logits, ascending indices
+    auto sort_all = [&](int n) {
+        int size = 64;
+        while (size < n) size <<= 1;
+        for (int i = n + tid; i < size; i += kThreads) sh.all[i] = ~0ull;
+        __syncthreads();
+        sort_block(sh.all, size);
+    };
 
-    // Narrows (thr, cut) to the prefix whose count (by_mass false) or weight (true) first reaches `target`, searching the
-    // elements of bins [za, zb] that are kept so far; `above_cnt` elements lie in earlier bins, all kept.  By weight the
-    // target is frac64 / 2^64 of the weight of everything kept so far: of `target` where that is known, else of the sum
-    // that the first pass takes.  Returns the weight of the new prefix.
-    auto refine = [&](bool by_mass, int za, int zb, u64 above_cnt, u64 target, bool whole_known, u64 frac64) -> u64 {
-        // keys that the zone can hold: its distances, widened by the rounding of the subtraction and the product
-        const float slack = 4e-7f;
-        const float hi = za <= 0 ? r.max : r.max - ((float)za * (1.f - slack)) / r.inv_bin + fabsf(r.max) * slack;
-        const float lo = r.max - ((float)(zb + 1) * (1.f + slack)) / r.inv_bin - fabsf(r.max) * slack;
-        uint32_t klo = key_of(hi < r.max ? hi : r.max), khi = lo > -INFINITY ? key_of(lo) : 0xff800000u;   // the key of -inf is the largest used
-        int shift = 0;
-        while ((((uint64_t)khi - klo) >> shift) >= kFine) ++shift;
-        u64 above_mass = 0;
-        bool first = true;
-        for (;;) {
-            for (int i = tid; i < kFine; i += kThreads) { sh.hist[i] = 0; sh.mass[i] = 0; }
-            if (tid == 0) sh.blk_mass = 0;
-            __syncthreads();
-            u64 am = 0, rest = 0;
-            for (int i = tid; i < count; i += kThreads) {
-                const float x = xs[i];
-                const int b = bin_of(r, x);
-                if (b > zb) { if (first && by_mass && !whole_known && b < kBins - 1) rest += weight(r, x); continue; }
-                if (b < za) { if (first) am += weight(r, x); continue; }
-                const uint32_t key = key_of(x);
-                if (key > thr || (key == thr && base + i > cut)) continue;
-                if (key < klo || key > khi) continue;
-                const int f = (int)((key - klo) >> shift);
-                if (f >= kFine) continue;
-                atomicAdd(&sh.hist[f], 1u);
-                atomicAdd(&sh.mass[f], weight(r, x));
-            }
-            if (first) {
+    // ---- few candidates
+    if ((use_k && k <= kListK) || (!use_k && !use_p && r.x_min > -INFINITY)) {
+        float tau = r.max - kRange * (1.f + kSlack) * temperature - fabsf(r.max) * kSlack;      // below it weights are zero
+        if (use_k) {
+            const float inv = r.inv_bin * ((float)(kCoarse - 1) / (float)(kBins - 1));
+            const float tm[4] = {tmax.x, tmax.y, tmax.z, tmax.w};
 #pragma unroll
-                for (int o = 16; o; o >>= 1) { am += __shfl_xor_sync(0xffffffffu, am, o); rest += __shfl_xor_sync(0xffffffffu, rest, o); }
-                if (lane == 0) { sh.warp_sum[warp] = am; sh.scan[warp] = rest; }
-                __syncthreads();
-                if (tid == 0) { u64 s = 0, q = 0; for (int w = 0; w < kWarps; ++w) { s += sh.warp_sum[w]; q += sh.scan[w]; } sh.blk_mass = s; sh.total = q; }
+            for (int c = 0; c < 4; ++c) {
+                const float d = (r.max - tm[c]) * inv;
+                if (d < (float)(kCoarse - 1)) atomicAdd(&sh.coarse[(int)d], 1u);
             }
-            cluster.sync();
-            uint32_t c2[2] = {0, 0}; u64 m2[2] = {0, 0}, below = 0;
-            for (int q = 0; q < CL; ++q) {
-                const uint2 c = *reinterpret_cast<const uint2*>(cluster.map_shared_rank(sh.hist, q) + tid * 2);
-                const ulonglong2 m = *reinterpret_cast<const ulonglong2*>(cluster.map_shared_rank(sh.mass, q) + tid * 2);
-                c2[0] += c.x; c2[1] += c.y; m2[0] += m.x; m2[1] += m.y;
-                if (first) { above_mass += *cluster.map_shared_rank(&sh.blk_mass, q); below += *cluster.map_shared_rank(&sh.total, q); }
-            }
-            cluster.sync();                                   // everybody has read: the arrays may be overwritten
-            u64 tot_c, tot_m;
-            const u64 ec = block_excl<u64>((u64)c2[0] + c2[1], sh.scan, &tot_c) + above_cnt;
-            const u64 em = block_excl<u64>(m2[0] + m2[1], sh.scan, &tot_m) + above_mass;
-            if (first && by_mass) {                           // the target from the whole weight
-                const u64 whole = whole_known ? target : above_mass + tot_m + below;
-                const u64 lo64 = whole * frac64, hi64 = __umul64hi(whole, frac64);
-                target = max((u64)1, hi64 + (lo64 != 0));
-            }
-            if (tid == 0) sh.bin = -1;
+            sync_row();
+            u64 c = 0, tot;
+            for (int q = 0; q < CL; ++q) c += remote(&sh.coarse[0], q)[tid];
+            const u64 e = block_excl<u64>(c, sh.scan, tot);
+            if (e < (u64)k && e + c >= (u64)k) sh.zone_a = tid;
             __syncthreads();
-            const u64 e0 = by_mass ? em : ec, a0 = by_mass ? m2[0] : (u64)c2[0], a1 = by_mass ? m2[1] : (u64)c2[1];
-            if (e0 < target && e0 + a0 + a1 >= target) {
-                const int sec = e0 + a0 >= target ? 0 : 1;
-                sh.bin = tid * 2 + sec;
-                sh.before_cnt = ec + (sec ? c2[0] : 0);
-                sh.before_mass = em + (sec ? m2[0] : 0);
-                sh.total = sec ? c2[1] : c2[0];
+            if (tot >= (u64)k) {                              // so at least k logits are above the far edge of that bin
+                const float t2 = r.max - ((float)(sh.zone_a + 1) * (1.f + kSlack)) / inv - fabsf(r.max) * kSlack;
+                if (t2 > tau) tau = t2;                       // (an infinite or undefined edge leaves tau)
             }
-            __syncthreads();
-            if (sh.bin < 0) return above_mass + tot_m;        // everything kept so far is needed: no narrower threshold
-            above_cnt = sh.before_cnt; above_mass = sh.before_mass;
-            const uint32_t nlo = klo + ((uint32_t)sh.bin << shift);
-            const u64 in_bin = sh.total;
-            __syncthreads();
-            if (shift == 0) {                                 // one key: of its `in_bin` elements the first `take` by index
-                const float x = __uint_as_float((nlo & 0x80000000u) ? nlo : ~nlo & 0x7fffffffu);
-                const u64 w = weight(r, x);
-                u64 take = in_bin;
-                if (!by_mass) take = target - above_cnt;
-                else if (w > 0) take = (target - above_mass + w - 1) / w;
-                const bool all = take >= in_bin;
-                const uint32_t old_thr = thr; const int old_cut = cut;
-                thr = nlo;
-                if (all) { cut = old_thr == thr ? old_cut : 0x7fffffff; return above_mass + in_bin * w; }
-                // index of the take-th element with that key: counts by warp, in index order
-                uint32_t mine = 0;
-                for (int i = w0 + lane; i < w1; i += 32) mine += key_of(xs[i]) == thr;
+        }
+        if (!use_p && r.x_min > tau) tau = r.x_min;
+#pragma unroll 8
+        for (int v = v0 + lane; v < v1; v += 32) {
+            const float4 q = get(v);
+            if (fmaxf(fmaxf(q.x, q.y), fmaxf(q.z, q.w)) >= tau) {
+                const float e[4] = {q.x, q.y, q.z, q.w};
 #pragma unroll
-                for (int o = 16; o; o >>= 1) mine += __shfl_xor_sync(0xffffffffu, mine, o);
-                if (lane == 0) sh.warp_cnt[warp] = mine;
-                cluster.sync();
-                u64 seen = 0;
-                for (int q = 0; q < CL * kWarps; ++q) {
-                    const u64 c = cluster.map_shared_rank(sh.warp_cnt, q / kWarps)[q % kWarps];
-                    if (seen + c >= take) {
-                        if (q / kWarps == rank && q % kWarps == warp) {
-                            u64 left = take - seen;           // 1 .. c
-                            for (int i = w0; i < w1; i += 32) {
-                                const bool hit = i + lane < w1 && key_of(xs[i + lane]) == thr;
-                                const unsigned bal = __ballot_sync(0xffffffffu, hit);
-                                if (left <= (u64)__popc(bal)) {
-                                    if (hit && (u64)__popc(bal & ((2u << lane) - 1)) == left)
-                                        for (int z = 0; z < CL; ++z) *cluster.map_shared_rank(&sh.cut, z) = base + i + lane;
-                                    break;
-                                }
-                                left -= __popc(bal);
-                            }
-                        }
-                        break;
+                for (int c = 0; c < 4; ++c) if (e[c] >= tau && e[c] > -INFINITY) entry(e[c], base + v * 4 + c);
+            }
+        }
+        const int n = gather();
+        sync_row();                                           // everybody has read it: from here the first block needs no other
+        if (n <= kList) {
+            if (rank != 0) return;
+            sort_all(n);
+            // four consecutive places a thread, in descending order of logits
+            u64* wt = sh.list;
+            u64 w4[4], mine = 0, tot;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const int i = tid * 4 + j;
+                w4[j] = i < n && (!use_k || i < k) ? weight(r, value_of((uint32_t)(sh.all[i] >> 32))) : 0;
+                mine += w4[j];
+            }
+            u64 cum = block_excl<u64>(mine, sh.scan, tot);
+            const u64 lim = use_p ? reach(tot) : ~0ull;       // kept: places whose predecessors' weight is below the reach
+            u64 ksum = 0;
+            uint32_t idx4[4];
+            int kept = 0;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const int i = tid * 4 + j;
+                const u64 a = i < n ? sh.all[i] : 0;
+                const bool in = cum < lim && value_of((uint32_t)(a >> 32)) >= r.x_min;
+                cum += w4[j];
+                if (!in) w4[j] = 0;
+                idx4[j] = (uint32_t)a;
+                ksum += w4[j];
+                kept += w4[j] > 0;
+                if (i < kList) wt[i] = w4[j];
+            }
+            u64 Z;
+            block_excl<u64>(ksum, sh.scan, Z);                // (its barriers also separate the reads of `all` from the writes below)
+            // in index order: (index, place) of what is kept
+            u64 kn;
+            int at = (int)block_excl<u64>((u64)kept, sh.scan, kn);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) if (w4[j] > 0) sh.all[at++] = (u64)idx4[j] << 32 | (uint32_t)(tid * 4 + j);
+            sort_all((int)kn);
+            const u64 target = __umul64hi(Z, U);
+            mine = 0;
+            u64 s4[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) { const int i = tid * 4 + j; s4[j] = i < (int)kn ? wt[(uint32_t)sh.all[i]] : 0; mine += s4[j]; }
+            cum = block_excl<u64>(mine, sh.scan, tot);
+            if (cum <= target && cum + mine > target) {
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    if (cum <= target && cum + s4[j] > target) {
+                        const int tok = (int)(sh.all[tid * 4 + j] >> 32);     // its slice may be another block's: the logit from global memory
+                        store(tok, pos_inf ? 0.f : (float)reinterpret_cast<const E*>(p.logits)[row * p.row_stride + tok], Z);
                     }
-                    seen += c;
+                    cum += s4[j];
                 }
-                cluster.sync();
-                cut = sh.cut;
-                return above_mass + take * w;
             }
-            klo = nlo;
-            khi = min(khi, (uint32_t)(klo + ((1u << shift) - 1)));
-            shift = 0;
-            while ((((uint64_t)khi - klo) >> shift) >= kFine) ++shift;
-            first = false;
+            return;
         }
-    };
+        if (tid == 0) { sh.n_list = 0; if (rank == 0) sh.n_all = 0; }
+        sync_row();
+    }
 
-    u64 kept_mass = 0; bool mass_known = false;
-    if (use_k) {
-        u64 tot;
-        const u64 mine = (u64)c4[0] + c4[1] + c4[2] + c4[3];
-        u64 e = block_excl<u64>(mine, sh.scan, &tot);
-        if (tot > (u64)k) {                                   // fewer elements with weight than k: top-k removes nothing that counts
-            if (tid == 0) sh.bin = -1;
-            __syncthreads();
-            if (e < (u64)k && e + mine >= (u64)k)
-                for (int j = 0; j < 4; ++j) { if (e + c4[j] >= (u64)k) { sh.bin = tid * 4 + j; sh.before_cnt = e; break; } e += c4[j]; }
-            __syncthreads();
-            const int zb = sh.bin; const u64 before = sh.before_cnt;
-            __syncthreads();
-            kept_mass = refine(false, zb, zb, before, (u64)k, false, 0);
-            mass_known = true;
-        }
-    }
-    if (use_p) {
-        const u64 frac64 = tp > 0.f ? (u64)__double2ull_rz((double)tp * 18446744073709551616.0) : 0ull;
-        // bins that may hold the threshold, from counts alone: an element of bin b weighs between e^-(b+1)d and e^-bd
-        // (one more bin on either side for the rounding of the bin's number)
-        const double d = (double)kRange / (kBins - 1);
-        double up = 0, dn = 0;
-        double u4[4], l4[4];
-        for (int j = 0; j < 4; ++j) {
-            const int b = tid * 4 + j;
-            u4[j] = (double)c4[j] * exp(-d * max(0, b - 1)); l4[j] = (double)c4[j] * exp(-d * (b + 2));
-            up += u4[j]; dn += l4[j];
-        }
-        double tot_up, tot_dn;
-        double eu = block_excl<double>(up, sh.dscan, &tot_up), el = block_excl<double>(dn, sh.dscan, &tot_dn);
-        const double t_lo = mass_known ? (double)kept_mass * 0x1p-44 * tp * (1 - 1e-9) : tot_dn * tp, t_hi = mass_known ? (double)kept_mass * 0x1p-44 * tp * (1 + 1e-9) : tot_up * tp;
-        if (tid == 0) { sh.zone_a = kBins - 2; sh.zone_b = kBins - 2; }
-        __syncthreads();
-        for (int j = 0; j < 4; ++j) {
-            const int b = tid * 4 + j;
-            if (b < kBins - 1 && eu < t_lo && eu + u4[j] >= t_lo) atomicMin(&sh.zone_a, b);
-            if (b < kBins - 1 && el < t_hi && el + l4[j] >= t_hi) atomicMin(&sh.zone_b, b);
-            eu += u4[j]; el += l4[j];
-        }
-        __syncthreads();
-        int za = max(0, min(sh.zone_a, sh.zone_b) - 1), zb = min(kBins - 2, max(sh.zone_a, sh.zone_b) + 1);
-        if (!(t_lo > 0)) za = 0;
-        if (mass_known) {                                     // the threshold of top-k bounds the zone from below
-            const float xk = __uint_as_float((thr & 0x80000000u) ? thr : ~thr & 0x7fffffffu);
-            zb = max(za, min(zb, bin_of(r, xk)));
-            za = min(za, bin_of(r, xk));
-        }
-        __syncthreads();
-        u64 before = 0, tot;
-        {
-            u64 mine = 0;
-            for (int j = 0; j < 4; ++j) if (tid * 4 + j < za) mine += c4[j];
-            block_excl<u64>(mine, sh.scan, &tot);
-            before = tot;
-        }
-        __syncthreads();
-        refine(true, za, zb, before, kept_mass, mass_known, frac64);
-    }
-    // ---- weight kept by every warp's part, then the draw
+    // ---- whole distributions
+    uint32_t thr = 0xffffffffu; int cut = 0x7fffffff;         // kept so far: key < thr, or key == thr and index <= cut
+    int za = 0, zb = kBins;                                   // bins that may hold the last threshold: elements before them are kept
+    bool searched = false;                                    // za, zb hold a zone
+    u64 ws = 0;                                               // weight of this warp's kept elements (before bin za, once searched)
     auto kept = [&](float x, int idx) {
         const uint32_t key = key_of(x);
         return x >= r.x_min && (key < thr || (key == thr && idx <= cut));
     };
-    u64 ws = 0;
-    for (int i = w0 + lane; i < w1; i += 32) if (kept(xs[i], base + i)) ws += weight(r, xs[i]);
+    // the weights before bin za (`above`; into ws those that min-p keeps) and, with sum_all, of all; `inside` is called for
+    // the elements of bins [za, zb].  No branch around the polynomials, four at a time: their chain is long.
+    auto weigh = [&](bool sum_all, u64& above, u64& whole, auto&& inside) {
+        const float fa = (float)za, fb = (float)(zb + 1), stop = sum_all ? (float)(kBins - 1) : fa;
+        above = whole = ws = 0;
+#pragma unroll 2
+        for (int v = v0 + lane; v < v1; v += 32) {
+            const float4 q = get(v);
+            const float e[4] = {q.x, q.y, q.z, q.w};
+            const float d[4] = {(r.max - q.x) * r.inv_bin, (r.max - q.y) * r.inv_bin, (r.max - q.z) * r.inv_bin, (r.max - q.w) * r.inv_bin};
+            const float dm = fminf(fminf(d[0], d[1]), fminf(d[2], d[3]));
+            if (dm < stop) {
 #pragma unroll
-    for (int o = 16; o; o >>= 1) ws += __shfl_xor_sync(0xffffffffu, ws, o);
-    __syncthreads();
-    if (lane == 0) sh.warp_sum[warp] = ws;
-    cluster.sync();
-    u64 sum[kMaxCluster * kWarps / 32], Z = 0;
-#pragma unroll
-    for (int j = 0; j < kMaxCluster * kWarps / 32; ++j) {
-        const int q = lane * (kMaxCluster * kWarps / 32) + j;
-        sum[j] = q < CL * kWarps ? cluster.map_shared_rank(sh.warp_sum, q / kWarps)[q % kWarps] : 0;
-        Z += sum[j];
-    }
-    const u64 mine = Z;
-    const u64 incl = warp_incl(mine);
-    Z = __shfl_sync(0xffffffffu, incl, 31);
-    const float u = p.u[row];
-    const u64 U = u >= 1.f ? ~0ull : (u > 0.f ? (u64)__double2ull_rz((double)u * 18446744073709551616.0) : 0ull);
-    const u64 target = __umul64hi(Z, U);                      // the token: lowest index with cumulative weight > target
-    u64 before = incl - mine; int owner = -1; u64 obefore = 0;
-#pragma unroll
-    for (int j = 0; j < kMaxCluster * kWarps / 32; ++j) {
-        if (before <= target && before + sum[j] > target) { owner = lane * (kMaxCluster * kWarps / 32) + j; obefore = before; }
-        before += sum[j];
-    }
-    const unsigned who = __ballot_sync(0xffffffffu, owner >= 0);
-    owner = __shfl_sync(0xffffffffu, owner, __ffs(who) - 1);
-    obefore = __shfl_sync(0xffffffffu, obefore, __ffs(who) - 1);
-    if (owner / kWarps == rank && owner % kWarps == warp) {
-        u64 run = obefore;
-        for (int i = w0; i < w1; i += 32) {
-            const float x = i + lane < w1 ? xs[i + lane] : -INFINITY;
-            const u64 w = i + lane < w1 && kept(x, base + i + lane) ? weight(r, x) : 0;
-            const u64 c = warp_incl(w) + run;
-            const unsigned over = __ballot_sync(0xffffffffu, c > target);
-            if (over) {
-                if (lane == __ffs(over) - 1) {
-                    const int tok = base + i + lane;
-                    if (p.token) p.token[row] = tok;
-                    if (p.token2) p.token2[row * p.token2_stride] = tok;
-                    if (p.prob) p.prob[row * p.prob_stride] = (float)((x == r.max ? 1.0 : exp2(((double)x - (double)r.max) * r.inv_t)) / ((double)Z * 0x1p-44));
+                for (int c = 0; c < 4; ++c) {
+                    const u64 w = weight(r, e[c]);
+                    whole += w;
+                    if (d[c] < fa) { above += w; if (e[c] >= r.x_min) ws += w; }
                 }
-                break;
             }
-            run = __shfl_sync(0xffffffffu, c, 31);
+            if (dm < fb)
+#pragma unroll
+                for (int c = 0; c < 4; ++c) if (d[c] >= fa && d[c] < fb) inside(e[c], base + v * 4 + c);
+        }
+        ws = warp_sum(ws);
+        above = warp_sum(above); whole = warp_sum(whole);
+        if (lane == 0) { sh.warp_tmp[warp] = above; sh.warp_tmp2[warp] = whole; }
+        __syncthreads();
+        if (tid == 0) { u64 s = 0, q = 0; for (int w = 0; w < kWarps; ++w) { s += sh.warp_tmp[w]; q += sh.warp_tmp2[w]; } sh.blk_mass = s; sh.blk_all = q; }
+    };
+    auto row_sum = [&](u64 Shared::*field) { u64 s = 0; for (int q = 0; q < CL; ++q) s += remote(&sh, q)->*field; return s; };
+
+    bool by_keys = false;
+    u64 above_cnt = 0;                                        // elements of the row before bin za
+    int k_bin = -1;                                           // bin of the k-th element, with k_before elements before it
+    u64 k_before = 0;
+    if (use_k || use_p) {
+        for (int i = tid; i < kBins / 4; i += kThreads) reinterpret_cast<uint4*>(sh.bins)[i] = make_uint4(0, 0, 0, 0);
+        __syncthreads();
+#pragma unroll 4
+        for (int v = v0 + lane; v < v1; v += 32) {
+            const float4 q = get(v);
+            const float d[4] = {(r.max - q.x) * r.inv_bin, (r.max - q.y) * r.inv_bin, (r.max - q.z) * r.inv_bin, (r.max - q.w) * r.inv_bin};
+#pragma unroll
+            for (int c = 0; c < 4; ++c) if (d[c] < (float)(kBins - 1)) atomicAdd(&sh.bins[(int)d[c]], 1u);
+        }
+        sync_row();
+        // every block sums its share of the bins over the blocks: PER of them a thread.  An element of bin b weighs between
+        // e^-(b + 1)d and e^-bd (a hundredth of a bin more on either side for the rounding of its number).
+        constexpr int MAXPER = kBins / kThreads;
+        const int per = MAXPER / CL, b0 = rank * (kBins / CL) + tid * per;
+        uint32_t c[MAXPER];
+        const float d = kRange / (kBins - 1), step = __expf(-d);
+        double up = 0, dn = 0; u64 cnt = 0;
+        {
+            float fu = __expf(-d * ((float)b0 - 0.01f)), fd = __expf(-d * ((float)b0 + 1.01f));
+#pragma unroll
+            for (int j = 0; j < MAXPER; ++j) {
+                c[j] = 0;
+                if (j < per) for (int q = 0; q < CL; ++q) c[j] += remote(&sh.bins[0], q)[b0 + j];
+                cnt += c[j]; up += (double)((float)c[j] * fu); dn += (double)((float)c[j] * fd);
+                fu *= step; fd *= step;
+            }
+        }
+        u64 tc; double tu, td;
+        u64 ec = block_excl<u64>(cnt, sh.scan, tc);
+        double eu = block_excl<double>(up, sh.dscan, tu), el = block_excl<double>(dn, sh.dscan, td);
+        if (tid == 0) { sh.share[0] = (double)tc; sh.share[1] = tu; sh.share[2] = td; sh.zone_a = sh.zone_b = sh.tail_a = sh.tail_b = kBins - 2; sh.bin = -1; sh.before_cnt = 0; }
+        sync_row();
+        tc = 0; tu = td = 0;
+        for (int q = 0; q < CL; ++q) {
+            const double* s = remote(&sh.share[0], q);
+            if (q < rank) { ec += (u64)s[0]; eu += s[1]; el += s[2]; }
+            tc += (u64)s[0]; tu += s[1]; td += s[2];
+        }
+        // (1e-5: the rounding of the bounds themselves, a product of up to 16 steps and a sum)
+        // The threshold lies in the first bin through which the weight reaches p times the whole, or, the same, behind which
+        // at most 1 - p of it is left: both bounds are taken, the smaller part is the sharper one.
+        const double t_lo = td * tp * (1 - 1e-5), t_hi = tu * tp * (1 + 1e-5);
+        const double s_lo = td * (1.0 - (double)tp) * (1 - 1e-5), s_hi = tu * (1.0 - (double)tp) * (1 + 1e-5);
+        float fu = __expf(-d * ((float)b0 - 0.01f)), fd = __expf(-d * ((float)b0 + 1.01f));
+        const bool k_cuts = use_k && tc > (u64)k;             // otherwise top-k removes nothing that has weight
+#pragma unroll
+        for (int j = 0; j < MAXPER; ++j) {
+            const double u1 = (double)((float)c[j] * fu), l1 = (double)((float)c[j] * fd);
+            if (j < per) {
+                const int b = b0 + j;
+                if (k_cuts && ec < (u64)k && ec + c[j] >= (u64)k)
+                    for (int q = 0; q < CL; ++q) { Shared* o = remote(&sh, q); o->bin = b; o->before_cnt = ec; }
+                if (use_p && eu < t_lo && eu + u1 >= t_lo) for (int q = 0; q < CL; ++q) atomicMin(&remote(&sh, q)->zone_a, b);
+                if (use_p && el < t_hi && el + l1 >= t_hi) for (int q = 0; q < CL; ++q) atomicMin(&remote(&sh, q)->zone_b, b);
+                if (use_p && td - el > s_hi && td - (el + l1) <= s_hi) for (int q = 0; q < CL; ++q) atomicMin(&remote(&sh, q)->tail_a, b);
+                if (use_p && tu - eu > s_lo && tu - (eu + u1) <= s_lo) for (int q = 0; q < CL; ++q) atomicMin(&remote(&sh, q)->tail_b, b);
+            }
+            ec += c[j]; eu += u1; el += l1;
+            fu *= step; fd *= step;
+        }
+        sync_row();
+        if (k_cuts) { k_bin = sh.bin; k_before = sh.before_cnt; }
+        if (use_p && k_bin < 0) {
+            const int ta = td <= s_hi ? 0 : sh.tail_a;        // already at most 1 - p before the first bin
+            za = max(sh.zone_a, ta); zb = min(sh.zone_b, sh.tail_b);
+            if (za > zb) { za = min(sh.zone_a, ta); zb = max(sh.zone_b, sh.tail_b); }
+            searched = true;
+        } else if (k_bin >= 0 && !use_p) {
+            za = zb = k_bin; above_cnt = k_before;
+            searched = true;
+        } else by_keys = k_bin >= 0;                          // top-p behind a top-k that cuts
+        __syncthreads();
+    }
+
+    u64 above, whole;
+    if (!by_keys) {
+        // ---- one pass: exact weights, and a list of the zone (without a filter: everything is kept)
+        if (!searched) { za = kBins; zb = kBins - 1; }
+        weigh(use_p || !searched, above, whole, [&](float x, int idx) { entry(x, idx); });
+        if (lane == 0) remote(&sh.wsum[0], 0)[rank * kWarps + warp] = ws;
+        const int n = searched ? gather() : 0;
+        if (!searched) sync_row();
+        by_keys = n > kList;
+        if (!by_keys && searched && rank == 0) {
+            sort_all(n);
+            const u64 above_mass = row_sum(&Shared::blk_mass);
+            const u64 need = use_p ? reach(row_sum(&Shared::blk_all)) : 0;
+            u64 w4[4], mine = 0, tot;
+            uint32_t key4[4], idx4[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const int i = tid * 4 + j;
+                const u64 a = i < n ? sh.all[i] : ~0ull;
+                key4[j] = (uint32_t)(a >> 32); idx4[j] = (uint32_t)a;
+                w4[j] = i < n ? weight(r, value_of(key4[j])) : 0;
+                mine += w4[j];
+            }
+            u64 cum = block_excl<u64>(mine, sh.scan, tot) + above_mass;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const int i = tid * 4 + j;
+                const bool in = i < n && (use_p ? cum < need : above_cnt + i < (u64)k);
+                const bool last = in && (use_p ? cum + w4[j] >= need : above_cnt + i + 1 == (u64)k);
+                if (last) { sh.thr = key4[j]; sh.cut = (int)idx4[j]; }
+                cum += w4[j];
+                if (in && value_of(key4[j]) >= r.x_min) {     // into the sum of the warp that owns it
+                    const int q = (int)idx4[j] / slice, i2 = (int)idx4[j] - q * slice + shift;
+                    const int qc = min(slice, p.vocab - q * slice), pw = (((qc + shift + 3) >> 2) + kWarps - 1) / kWarps;
+                    atomicAdd(&sh.wsum[q * kWarps + (i2 >> 2) / pw], w4[j]);
+                }
+            }
+            __syncthreads();
+            thr = sh.thr; cut = sh.cut;
         }
     }
-    cluster.sync();                                           // no block leaves while another still reads its sums
+    if (by_keys) {
+        // ---- narrowing by keys.  Narrows (thr, cut) to the prefix whose count (by_mass false) or weight (true) first reaches
+        // `target`, searching the elements of bins [za, zb] that are kept so far; `before` elements lie in earlier bins, all
+        // kept.  By weight the target is the reach of top-p in the weight of everything kept so far: of `target` where that is
+        // known, else of the sum that the first pass takes.  Returns the weight of the new prefix.
+        auto refine = [&](bool by_mass, u64 before, u64 target, bool whole_known) -> u64 {
+            // keys that the zone can hold: its distances, widened by the rounding of the subtraction and the product
+            const float hi = za <= 0 ? r.max : r.max - ((float)za * (1.f - kSlack)) / r.inv_bin + fabsf(r.max) * kSlack;
+            const float lo = r.max - ((float)(zb + 1) * (1.f + kSlack)) / r.inv_bin - fabsf(r.max) * kSlack;
+            uint32_t klo = key_of(hi < r.max ? hi : r.max), khi = lo > -INFINITY ? key_of(lo) : 0xff800000u;   // the key of -inf is the largest used
+            int shf = 0;
+            while ((((uint64_t)khi - klo) >> shf) >= kFine) ++shf;
+            u64 above_mass = 0;
+            for (bool first = true;; first = false) {
+                __syncthreads();
+                for (int i = tid; i < kFine; i += kThreads) { sh.hist[i] = 0; sh.mass[i] = 0; }
+                __syncthreads();
+                auto inside = [&](float x, int idx) {
+                    const uint32_t key = key_of(x);
+                    if (key > thr || (key == thr && idx > cut) || key < klo || key > khi) return;
+                    const int f = (int)((key - klo) >> shf);
+                    if (f >= kFine) return;
+                    atomicAdd(&sh.hist[f], 1u);
+                    atomicAdd(&sh.mass[f], weight(r, x));
+                };
+                if (first) weigh(by_mass && !whole_known, above, whole, inside);
+                else {
+                    const float fa = (float)za, fb = (float)(zb + 1);
+                    for (int v = v0 + lane; v < v1; v += 32) {
+                        const float4 q = get(v);
+                        const float e[4] = {q.x, q.y, q.z, q.w};
+#pragma unroll
+                        for (int c = 0; c < 4; ++c) { const float d = (r.max - e[c]) * r.inv_bin; if (d >= fa && d < fb) inside(e[c], base + v * 4 + c); }
+                    }
+                }
+                sync_row();
+                constexpr int PB = kFine / kThreads;          // bins of this thread
+                uint32_t cb[PB] = {}; u64 mb[PB] = {};
+                for (int q = 0; q < CL; ++q)
+#pragma unroll
+                    for (int j = 0; j < PB; ++j) { cb[j] += remote(&sh.hist[0], q)[tid * PB + j]; mb[j] += remote(&sh.mass[0], q)[tid * PB + j]; }
+                if (first) {
+                    above_mass = row_sum(&Shared::blk_mass);
+                    if (by_mass) target = reach(whole_known ? target : row_sum(&Shared::blk_all));
+                }
+                sync_row();                                   // everybody has read: the arrays may be overwritten
+                u64 tot_c, tot_m, sc = 0, sm = 0;
+#pragma unroll
+                for (int j = 0; j < PB; ++j) { sc += cb[j]; sm += mb[j]; }
+                u64 ec = block_excl<u64>(sc, sh.scan, tot_c) + before, em = block_excl<u64>(sm, sh.scan, tot_m) + above_mass;
+                if (tid == 0) sh.bin = -1;
+                __syncthreads();
+#pragma unroll
+                for (int j = 0; j < PB; ++j) {
+                    const u64 e0 = by_mass ? em : ec, a = by_mass ? mb[j] : (u64)cb[j];
+                    if (e0 < target && e0 + a >= target) { sh.bin = tid * PB + j; sh.before_cnt = ec; sh.before_mass = em; sh.total = cb[j]; }
+                    ec += cb[j]; em += mb[j];
+                }
+                __syncthreads();
+                if (sh.bin < 0) return above_mass + tot_m;    // everything kept so far is needed: no narrower threshold
+                before = sh.before_cnt; above_mass = sh.before_mass;
+                const uint32_t nlo = klo + ((uint32_t)sh.bin << shf);
+                const u64 in_bin = sh.total;
+                __syncthreads();
+                if (shf == 0) {                               // one key: of its `in_bin` elements the first `take` by index
+                    const u64 w = weight(r, value_of(nlo));
+                    u64 take = in_bin;
+                    if (!by_mass) take = target - before;
+                    else if (w > 0) take = (target - above_mass + w - 1) / w;
+                    const uint32_t old_thr = thr; const int old_cut = cut;
+                    thr = nlo;
+                    if (take >= in_bin) { cut = old_thr == thr ? old_cut : 0x7fffffff; return above_mass + in_bin * w; }
+                    // index of the take-th element with that key: counts by warp, in index order
+                    uint32_t mine = 0;
+                    for (int v = v0 + lane; v < v1; v += 32) {
+                        const float4 q = get(v);
+                        mine += (key_of(q.x) == thr) + (key_of(q.y) == thr) + (key_of(q.z) == thr) + (key_of(q.w) == thr);
+                    }
+                    mine = warp_sum(mine);
+                    if (lane == 0) sh.warp_cnt[warp] = mine;
+                    sync_row();
+                    u64 seen = 0;
+                    for (int q = 0; q < CL * kWarps; ++q) {
+                        const u64 cq = remote(&sh.warp_cnt[0], q / kWarps)[q % kWarps];
+                        if (seen + cq >= take) {
+                            if (q / kWarps == rank && q % kWarps == warp) {
+                                uint32_t left = (uint32_t)(take - seen);      // 1 .. cq
+                                for (int v = v0; v < v1; v += 32) {
+                                    uint32_t hit = 0;
+                                    if (v + lane < v1) {
+                                        const float4 x = get(v + lane);
+                                        hit = (key_of(x.x) == thr) | (key_of(x.y) == thr) << 1 | (key_of(x.z) == thr) << 2 | (key_of(x.w) == thr) << 3;
+                                    }
+                                    const uint32_t incl = warp_incl((uint32_t)__popc(hit)), here = __shfl_sync(0xffffffffu, incl, 31);
+                                    if (left <= here) {
+                                        uint32_t need = left - (incl - __popc(hit));
+                                        if (left > incl - __popc(hit) && left <= incl)
+                                            for (int c = 0; c < 4; ++c)
+                                                if (hit >> c & 1 && --need == 0)
+                                                    for (int z = 0; z < CL; ++z) *remote(&sh.cut, z) = base + (v + lane) * 4 + c;
+                                        break;
+                                    }
+                                    left -= here;
+                                }
+                            }
+                            break;
+                        }
+                        seen += cq;
+                    }
+                    sync_row();
+                    cut = sh.cut;
+                    return above_mass + take * w;
+                }
+                klo = nlo;
+                khi = min(khi, (uint32_t)(klo + ((1u << shf) - 1)));
+                shf = 0;
+                while ((((uint64_t)khi - klo) >> shf) >= kFine) ++shf;
+            }
+        };
+        u64 kept_mass = 0;
+        if (k_bin >= 0) {
+            za = zb = k_bin;
+            kept_mass = refine(false, k_before, (u64)k, false);
+        }
+        if (use_p) {
+            if (k_bin >= 0) { za = 0; zb = min(kBins - 2, (int)((r.max - value_of(thr)) * r.inv_bin)); }   // anywhere above the k-th
+            refine(true, 0, kept_mass, k_bin >= 0);           // (otherwise the zone that the histogram gave)
+        }
+        // what every warp keeps: before the zone it is known
+        const float fa = (float)za, fb = (float)(zb + 1);
+        u64 z = 0;
+        for (int v = v0 + lane; v < v1; v += 32) {
+            const float4 q = get(v);
+            const float e[4] = {q.x, q.y, q.z, q.w};
+#pragma unroll
+            for (int c = 0; c < 4; ++c) { const float d = (r.max - e[c]) * r.inv_bin; if (d >= fa && d < fb && kept(e[c], base + v * 4 + c)) z += weight(r, e[c]); }
+        }
+        z = warp_sum(z);
+        if (lane == 0) remote(&sh.wsum[0], 0)[rank * kWarps + warp] = ws + z;
+        sync_row();
+    }
+
+    // ---- the draw: the first block finds the warp whose part holds the token, that warp's block the token
+    if (rank == 0 && warp == 0) {
+        constexpr int PL = kMaxCluster * kWarps / 32;
+        u64 sum[PL], mine = 0;
+#pragma unroll
+        for (int j = 0; j < PL; ++j) { sum[j] = lane * PL + j < CL * kWarps ? sh.wsum[lane * PL + j] : 0; mine += sum[j]; }
+        const u64 incl = warp_incl(mine), Z = __shfl_sync(0xffffffffu, incl, 31);
+        const u64 target = __umul64hi(Z, U);                  // the token: lowest index with cumulative weight > target
+        u64 before = incl - mine;
+#pragma unroll
+        for (int j = 0; j < PL; ++j) {
+            if (before <= target && before + sum[j] > target) {
+                Shared* o = remote(&sh, (lane * PL + j) / kWarps);
+                o->thr = thr; o->cut = cut; o->target = target - before; o->Z = Z;
+                const int own = (lane * PL + j) % kWarps;
+                for (int q = 0; q < CL; ++q) remote(&sh, q)->owner = q == (lane * PL + j) / kWarps ? own : -1;
+            }
+            before += sum[j];
+        }
+    }
+    sync_row();
+    if (sh.owner < 0) return;
+    thr = sh.thr; cut = sh.cut;
+    const u64 target = sh.target;
+    const int r0 = min(quads, sh.owner * per_warp), r1 = min(quads, r0 + per_warp), each = (r1 - r0 + kThreads - 1) / kThreads;
+    const int q0 = min(r1, r0 + tid * each), q1 = min(r1, q0 + each);      // consecutive quads of this thread
+    u64 mine = 0, tot;
+    for (int v = q0; v < q1; ++v) {
+        const float4 q = get(v);
+        const float e[4] = {q.x, q.y, q.z, q.w};
+#pragma unroll
+        for (int c = 0; c < 4; ++c) { const u64 w = weight(r, e[c]); mine += kept(e[c], base + v * 4 + c) ? w : 0; }
+    }
+    u64 cum = block_excl<u64>(mine, sh.scan, tot);
+    if (cum <= target && cum + mine > target) {
+        for (int v = q0; v < q1; ++v) {
+            const float4 q = get(v);
+            const float e[4] = {q.x, q.y, q.z, q.w};
+#pragma unroll
+            for (int c = 0; c < 4; ++c) {
+                const u64 w = kept(e[c], base + v * 4 + c) ? weight(r, e[c]) : 0;
+                if (cum <= target && cum + w > target) store(base + v * 4 + c, e[c], sh.Z);
+                cum += w;
+            }
+        }
+    }
 }
 
-template <class E>
-pt_status launch_t(const SampleP& p, int64_t n, cudaStream_t st) {
-    int cl = 1;
-    while (cl < kMaxCluster && (p.vocab + cl - 1) / cl > 16384) cl *= 2;
+template <class E, bool SLICES>
+pt_status launch_kind(const SampleP& p, int64_t n, int cl, cudaStream_t st) {
     const int slice = ((p.vocab + cl - 1) / cl + 3) & ~3;
-    const size_t smem = ((sizeof(Shared) + 15) & ~15) + (size_t)slice * 4;
+    const size_t head = (sizeof(Shared) + 15) & ~15;
     static bool done_[kMaxDevices] = {};
     bool& done = done_[current_device()];
     if (!done) {
-        cudaError_t e = cudaFuncSetAttribute(k_sample<E>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)(((sizeof(Shared) + 15) & ~15) + kMaxSlice * 4));
+        cudaError_t e = cudaFuncSetAttribute(k_sample<E, SLICES>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)(head + (SLICES ? (kMaxSlice + 4) * 4 : 0)));
         if (e != cudaSuccess) { set_error("cudaFuncSetAttribute: %s", cudaGetErrorString(e)); return PT_ERR_CUDA; }
         done = true;
     }
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)(n * cl)); cfg.blockDim = dim3(kThreads); cfg.dynamicSmemBytes = smem; cfg.stream = st;
+    cfg.gridDim = dim3((unsigned)(n * cl)); cfg.blockDim = dim3(kThreads); cfg.dynamicSmemBytes = head + (SLICES ? (size_t)(slice + 4) * 4 : 0); cfg.stream = st;
     cudaLaunchAttribute at[1];
     at[0].id = cudaLaunchAttributeClusterDimension; at[0].val.clusterDim.x = cl; at[0].val.clusterDim.y = 1; at[0].val.clusterDim.z = 1;
-    cfg.attrs = at; cfg.numAttrs = 1;
-    cudaError_t e = cudaLaunchKernelEx(&cfg, k_sample<E>, p, slice);
+    cfg.attrs = at; cfg.numAttrs = SLICES ? 1 : 0;
+    cudaError_t e = cudaLaunchKernelEx(&cfg, k_sample<E, SLICES>, p, slice);
     if (e != cudaSuccess) { set_error("k_sample launch: %s", cudaGetErrorString(e)); return PT_ERR_CUDA; }
     g_launches.fetch_add(1, std::memory_order_relaxed);
     return PT_OK;
 }
 
+template <class E>
+pt_status launch_t(const SampleP& p, int64_t n, cudaStream_t st) {
+    if (n >= kRowsFrom || p.vocab > kMaxCluster * kMaxSlice) return launch_kind<E, false>(p, n, 1, st);
+    // slices of at most 16384 logits (64 KB: two blocks per SM); while a launch leaves SMs idle a row is spread further,
+    // down to slices of 2048
+    int cl = 1;
+    while (cl < kMaxCluster && ((p.vocab + cl - 1) / cl > 16384 || (n * cl * 2 <= 148 && (p.vocab + cl - 1) / cl > 2048))) cl *= 2;
+    return launch_kind<E, true>(p, n, cl, st);
+}
+
 }  // namespace
 
-int sample_vocab_limit() { return kMaxCluster * kMaxSlice; }
+int sample_vocab_limit() { return kMaxVocab; }
 
 pt_status launch_sample(const SampleP& p, int64_t n, bool bf16, cudaStream_t st) {
     return bf16 ? launch_t<__nv_bfloat16>(p, n, st) : launch_t<float>(p, n, st);
