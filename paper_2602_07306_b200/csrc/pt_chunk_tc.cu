@@ -10,11 +10,14 @@
 // running maximum, sum and unnormalised output in scratch, and k_chunk_combine merges the parts.  The same code serves four
 // speculated tokens on a long context (all ranges are parts of few segments) and a long prompt (hardly any segment is cut).
 // Blocks find their range themselves from the lengths in device memory: nothing is planned on the host, and a captured
-// launch may be replayed with other lengths.
+// launch may be replayed with other lengths.  One warp walks the range and hands the segments to the others through a ring
+// in shared memory, so that the softmax threads, which hold a row of 128 scores each, carry nothing of the walk.
 //
-// Inside a block the roles are those of the prefill kernel: warp 0 copies Q, K and V with TMA, warp 1 issues the products
-// S = Q K^T and O += P V, warps 4-7 and 8-11 are the softmax of the two tiles, one thread per row.  Barriers count over all
-// segments of a block, so the copies of the next segment start while the last one's output is being written.
+// Inside a block the roles are those of the prefill kernel: warps 0 and 3 copy Q and K, and V, with TMA, warp 1 issues the products
+// S = Q K^T and O += P V, warps 4-7 and 8-11 are two softmax groups, one thread per row.  In a segment of two row tiles each
+// group has one; in a segment of one, which is bound by the latency from a score to the next product, the groups take
+// turns on its key tiles with a running maximum, sum and accumulator each, and the first merges both at the end.  Barriers
+// count over all segments of a block, so the copies of the next segment start while the last one's output is being written.
 // Every wait is bounded; on a timeout the block records PT_ERR_DEVICE_TIMEOUT and every role leaves.
 #include "pt_chunk.h"
 #include "pt_tcgen05.cuh"
@@ -30,29 +33,21 @@ constexpr int kMaxBlocks = 148;
 constexpr int kCostSeg = 4, kCost1 = 4, kCost2 = 7;
 constexpr int kMinUnits = kCostSeg + kCost1;   // a range is no shorter
 
-enum { C_QFULL = 0, C_QEMPTY = 2, C_KFULL = 4, C_KEMPTY = 7, C_VFULL = 10, C_VEMPTY = 12, C_SFULL = 14, C_PFULL = 16, C_OREADY = 18, C_VRAW = 20, C_COUNT = 21 };
+enum { C_QFULL = 0, C_QEMPTY = 2, C_KFULL = 4, C_KEMPTY = 7, C_VFULL = 10, C_VEMPTY = 12, C_SFULL = 14, C_PFULL = 16, C_OREADY = 18, C_VRAW = 20, C_MREADY = 21, C_MDONE = 22,
+       C_SEGFULL = 23, C_SEGEMPTY = 27, C_COUNT = 31 };
+constexpr int kSegRing = 4;                    // segments handed out ahead
+constexpr int kSegReaders = 11;                // warps 0, 1, 3 and the eight of the softmax
 
-struct Plan { int64_t total, p0; int ranges, b, qrow0, tk, qb, u, len, pad; };
+// Cost of one segment, of `left` tokens from its first one on and `keys` keys seen by its last row.
+__device__ __forceinline__ int seg_cost(int left, int keys, int tpt) { return kCostSeg + ((keys + 127) >> 7) * (left > tpt ? kCost2 : kCost1); }
 
-// cost of all segments of one (sequence, track, KV head)
-__device__ __forceinline__ int64_t row_cost(int ql, int kl, int tpt) {
-    int64_t c = 0;
-    for (int t0 = 0; t0 < ql; t0 += 2 * tpt) {
-        const int n = (kl - ql + min(t0 + 2 * tpt, ql) + 127) >> 7;
-        c += kCostSeg + (int64_t)n * (t0 + tpt < ql ? kCost2 : kCost1);
-    }
-    return c;
-}
-
-// Walks the segments of a block's range.  Position of key tile k of a segment that starts at u (relative to the range):
-// u for k = 0, u + kCostSeg + k w for the others; a tile belongs to the range its position lies in.
-struct Seg {
+// Walks the segments of a range.  Position of key tile k of a segment that starts at u (relative to the range): u for k = 0,
+// u + kCostSeg + k w for the others; a tile belongs to the range its position lies in.
+struct Walk {
+    int64_t total, p0;                             // cost of everything, start of the range
+    int ranges;
     int b, qrow0, qlen, kvlen, tk, qb, u, len;     // len: length of the range
     int tok0, n0, n1, n, w, lo, hi;                // key tiles of the two row tiles, and the part [lo, hi) of max(n0, n1) that is ours
-    __device__ __forceinline__ void start(const Plan& pl, const ChunkP& p, int tpt) {
-        b = pl.b; qrow0 = pl.qrow0; tk = pl.tk; qb = pl.qb; u = pl.u; len = pl.len;
-        if (len > 0) { qlen = p.qlen[b]; kvlen = p.kvlen[b]; derive(tpt); }
-    }
     __device__ __forceinline__ static int first_at(int rel, int w) {       // first tile whose position, relative to the segment, is >= rel
         return rel <= 0 ? 0 : max(1, (rel - kCostSeg + w - 1) / w);
     }
@@ -84,80 +79,108 @@ struct Seg {
         derive(tpt);
         return true;
     }
+    // where range c starts, of `total` cut into `ranges` (the product stays below 2^53)
+    __device__ __forceinline__ int64_t border(int c) const { return c >= ranges ? total : (int64_t)((double)total * c / ranges); }
+
+    // Finds range c of the launch; all lanes of a warp call it and get the same.  False: nothing in it.  Bad lengths are
+    // reported by `reporter` and leave every range empty.
+    __device__ bool find(const ChunkP& p, int tpt, int blocks, int c, bool reporter) {
+        const int lane = threadIdx.x & 31, tkn = p.T * p.nkv, span = 2 * tpt;
+        auto row_cost = [&](int ql, int kl, bool in) {         // cost of a sequence's segments of one (track, KV head), for every lane's sequence
+            int64_t c1 = 0;
+            const int nb = in ? (ql + span - 1) / span : 0;
+            if (nb <= 8)
+                for (int i = 0; i < nb; ++i) c1 += seg_cost(ql - i * span, kl - ql + min((i + 1) * span, ql), tpt);
+            for (unsigned m = __ballot_sync(0xffffffffu, nb > 8); m; m &= m - 1) {        // long chunks: the warp together
+                const int who = __ffs(m) - 1;
+                const int q1 = __shfl_sync(0xffffffffu, ql, who), k1 = __shfl_sync(0xffffffffu, kl, who), n1 = __shfl_sync(0xffffffffu, nb, who);
+                int64_t s = 0;
+                for (int i = lane; i < n1; i += 32) s += seg_cost(q1 - i * span, k1 - q1 + min((i + 1) * span, q1), tpt);
+#pragma unroll
+                for (int o = 16; o; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
+                if (lane == who) c1 = s;
+            }
+            return c1;
+        };
+        int64_t sum = 0, rows = 0, one = 0;
+        int ql = 0, kl = 0;
+        bool bad = false;
+        for (int b0 = 0; b0 < p.B; b0 += 32) {
+            const bool in = b0 + lane < p.B;
+            ql = in ? p.qlen[b0 + lane] : 0; kl = in ? p.kvlen[b0 + lane] : 0;
+            const bool ok = ql >= 0 && kl >= ql && (int64_t)kl <= (int64_t)p.maxp * p.ps && ql <= p.M;
+            bad |= !ok;
+            one = row_cost(ql, kl, ok);
+            sum += one; rows += ok ? ql : 0;
+        }
+#pragma unroll
+        for (int o = 16; o; o >>= 1) { sum += __shfl_xor_sync(0xffffffffu, sum, o); rows += __shfl_xor_sync(0xffffffffu, rows, o); }
+        if (__any_sync(0xffffffffu, bad) || rows > p.M) {
+            if (reporter && lane == 0) report(p.status, PT_ERR_DEVICE_BOUNDS, LOC_CHUNK_LEN);
+            return false;
+        }
+        total = sum * tkn;
+        ranges = (int)min((int64_t)blocks, max((int64_t)1, total / kMinUnits));
+        if (total == 0 || c >= ranges) return false;
+        p0 = border(c);
+        len = (int)(border(c + 1) - p0);
+        if (len == 0) return false;
+        int64_t base = 0;
+        int row0 = 0;
+        for (int b0 = 0; b0 < p.B; b0 += 32) {
+            if (p.B > 32) {
+                const bool in = b0 + lane < p.B;
+                ql = in ? p.qlen[b0 + lane] : 0; kl = in ? p.kvlen[b0 + lane] : 0;
+                one = row_cost(ql, kl, true);
+            }
+            int64_t incl = one * tkn;
+            int rincl = ql;
+#pragma unroll
+            for (int o = 1; o < 32; o <<= 1) {
+                const int64_t x = __shfl_up_sync(0xffffffffu, incl, o); const int y = __shfl_up_sync(0xffffffffu, rincl, o);
+                if (lane >= o) { incl += x; rincl += y; }
+            }
+            const unsigned m = __ballot_sync(0xffffffffu, p0 < base + incl);
+            if (!m) { base += __shfl_sync(0xffffffffu, incl, 31); row0 += __shfl_sync(0xffffffffu, rincl, 31); continue; }
+            const int who = __ffs(m) - 1;                      // the sequence in which the range starts
+            b = b0 + who;
+            qlen = __shfl_sync(0xffffffffu, ql, who); kvlen = __shfl_sync(0xffffffffu, kl, who);
+            qrow0 = row0 + __shfl_sync(0xffffffffu, rincl, who) - qlen;
+            const int64_t per = __shfl_sync(0xffffffffu, one, who), rem = p0 - (base + __shfl_sync(0xffffffffu, incl, who) - per * tkn);
+            tk = (int)((double)rem / (double)per);             // exact up to one either way
+            while ((int64_t)tk * per > rem) --tk;
+            while ((int64_t)(tk + 1) * per <= rem) ++tk;
+            int64_t in = rem - tk * per;
+            const int nb = (qlen + span - 1) / span;
+            for (int q0 = 0; q0 < nb; q0 += 32) {              // its block of rows
+                const int i = q0 + lane;
+                int64_t cst = i < nb ? seg_cost(qlen - i * span, kvlen - qlen + min((i + 1) * span, qlen), tpt) : 0;
+                int64_t cin = cst;
+#pragma unroll
+                for (int o = 1; o < 32; o <<= 1) { const int64_t x = __shfl_up_sync(0xffffffffu, cin, o); if (lane >= o) cin += x; }
+                const unsigned mq = __ballot_sync(0xffffffffu, in < cin);
+                if (mq) {
+                    const int w2 = __ffs(mq) - 1;
+                    qb = q0 + w2;
+                    u = -(int)(in - (__shfl_sync(0xffffffffu, cin, w2) - __shfl_sync(0xffffffffu, cst, w2)));
+                    break;
+                }
+                in -= __shfl_sync(0xffffffffu, cin, 31);
+            }
+            derive(tpt);
+            return true;
+        }
+        return false;
+    }
 };
 
-// Where range `c` of the launch starts: all threads of the block call it.  buf: 2 * (THREADS / 32 + 1) values.
-template <int THREADS>
-__device__ __forceinline__ void make_plan(const ChunkP& p, int tpt, int blocks, int c, Plan* out, int64_t* buf) {
-    constexpr int NW = THREADS / 32;
-    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    const int tkn = p.T * p.nkv;
-    int64_t total = 0, rows = 0;
-    int bad = 0;
-    for (int b = tid; b < p.B; b += THREADS) {
-        const int ql = p.qlen[b], kl = p.kvlen[b];
-        const bool ok = ql >= 0 && kl >= ql && (int64_t)kl <= (int64_t)p.maxp * p.ps && ql <= p.M;
-        bad |= !ok;
-        rows += ok ? ql : 0;
-        if (ok) total += row_cost(ql, kl, tpt);
-    }
-    bad = __syncthreads_or(bad);
-    auto excl = [&](int64_t v, int64_t* b2, int64_t& sum) {                // exclusive prefix over the block
-        int64_t incl = v;
-#pragma unroll
-        for (int o = 1; o < 32; o <<= 1) { const int64_t x = __shfl_up_sync(0xffffffffu, incl, o); if (lane >= o) incl += x; }
-        __syncthreads();
-        if (lane == 31) b2[warp] = incl;
-        __syncthreads();
-        int64_t before = 0, all = 0;
-        for (int i = 0; i < NW; ++i) { if (i < warp) before += b2[i]; all += b2[i]; }
-        sum = all;
-        return before + incl - v;
-    };
-    int64_t all_rows;
-    excl(total, buf, total);
-    excl(rows, buf + NW, all_rows);
-    total *= tkn;
-    if (tid == 0) {
-        out->len = 0;
-        if ((bad || all_rows > p.M) && blockIdx.x == 0) report(p.status, PT_ERR_DEVICE_BOUNDS, LOC_CHUNK_LEN);
-    }
-    if (bad || all_rows > p.M || total == 0) { __syncthreads(); return; }
-    const int64_t ranges = min((int64_t)blocks, max((int64_t)1, total / kMinUnits));
-    if (c >= ranges) { __syncthreads(); return; }
-    const int64_t p0 = total * c / ranges, p1 = total * (c + 1) / ranges;
-    int64_t base = 0, row_base = 0;
-    for (int b0 = 0; b0 < p.B; b0 += THREADS) {
-        const int b = b0 + tid;
-        const int ql = b < p.B ? p.qlen[b] : 0, kl = b < p.B ? p.kvlen[b] : 0;
-        const int64_t one = row_cost(ql, kl, tpt), cost = one * tkn;
-        int64_t sum, rsum;
-        const int64_t at = base + excl(cost, buf, sum), row = row_base + excl((int64_t)ql, buf + NW, rsum);
-        if (p0 >= at && p0 < at + cost) {
-            const int64_t rem = p0 - at;
-            const int tk = (int)(rem / one);
-            int64_t in = rem - tk * one;
-            int qb = 0;
-            for (;; ++qb) {
-                const int t0 = qb * 2 * tpt;
-                const int n = (kl - ql + min(t0 + 2 * tpt, ql) + 127) >> 7;
-                const int64_t cst = kCostSeg + (int64_t)n * (t0 + tpt < ql ? kCost2 : kCost1);
-                if (in < cst) break;
-                in -= cst;
-            }
-            out->b = b; out->qrow0 = (int)row; out->tk = tk; out->qb = qb; out->u = -(int)in; out->len = (int)(p1 - p0);
-            out->total = total; out->ranges = (int)ranges; out->p0 = p0;
-        }
-        base += sum; row_base += rsum;
-        if (base > p0) break;
-    }
-    __syncthreads();
-}
+// What the other warps need of a segment; lo < 0: the end.
+struct Seg { int row0, t, kvh, kvlen, pos0, left, n0, n1, lo, hi, b, pad; };
 
 template <int DH> struct ChunkCfg {
     static constexpr int HALVES = DH / 64;
     static constexpr int TILE = HALVES * kHalfBytes;               // one Q, K or V tile of 128 rows
-    static constexpr int SMEM = (2 + kStK + kStV) * TILE + 1024 + 1024;
+    static constexpr int SMEM = (2 + kStK + kStV) * TILE + 1024 + 2048;
     static_assert(SMEM <= 232448, "shared memory of one block");
 };
 
@@ -178,7 +201,7 @@ __device__ __forceinline__ void tma_load_4d(uint32_t dst, const CUtensorMap* map
 template <int DH>
 __global__ void __launch_bounds__(kChunkThreads, 1)
 k_chunk_tc(const __grid_constant__ CUtensorMap qmap, const __grid_constant__ CUtensorMap kvmap, const ChunkP p, float* scratch, const int tpt,
-           const uint32_t q_bytes) {
+           const uint32_t q_bytes, const int box) {
     using C = ChunkCfg<DH>;
     constexpr int HALVES = C::HALVES, TILE = C::TILE;
     extern __shared__ uint8_t smem_raw[];
@@ -187,21 +210,20 @@ k_chunk_tc(const __grid_constant__ CUtensorMap qmap, const __grid_constant__ CUt
     uint8_t* sk = sq + 2 * TILE;
     uint8_t* sv = sk + kStK * TILE;
     uint64_t* bars = (uint64_t*)(sv + kStV * TILE);
-    int64_t* buf = (int64_t*)(bars + C_COUNT);                     // 2 * 12 values
-    Plan* plan = (Plan*)(buf + 24);
-    uint32_t* tmem_slot = (uint32_t*)(plan + 1);
+    uint32_t* tmem_slot = (uint32_t*)(bars + C_COUNT);
     volatile int* abort_flag = (volatile int*)(tmem_slot + 1);
+    Seg* ring = (Seg*)(bars + 40);                                 // kSegRing segments
+    float2* odd_stats = (float2*)(bars + 80);                      // maximum and sum of the second group, one-tile segments
 
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int G = p.nq / p.nkv;
     if (threadIdx.x == 0) {
-        for (int i = 0; i < C_COUNT; ++i) mbar_init(&bars[i], (i == C_PFULL || i == C_PFULL + 1) ? 4 : 1);
+        for (int i = 0; i < C_COUNT; ++i)
+            mbar_init(&bars[i], (i == C_PFULL || i == C_PFULL + 1 || i == C_MREADY || i == C_MDONE) ? 4 : i >= C_SEGEMPTY ? kSegReaders : 1);
         *abort_flag = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
     }
-    make_plan<kChunkThreads>(p, tpt, gridDim.x, blockIdx.x, plan, buf);
-    if (plan->len == 0) return;                                    // nothing for this block, or bad lengths
     if (warp == 2) {
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(tmem_slot)), "r"(512) : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
@@ -210,136 +232,193 @@ k_chunk_tc(const __grid_constant__ CUtensorMap qmap, const __grid_constant__ CUt
     __syncthreads();
     tc_fence_after();
     const uint32_t tmem_base = *tmem_slot;
+    // the next segment of the block; false at the end, or after a wait that ran out
+    int seg_i = 0;
+    auto next_seg = [&](Seg& sg) {
+        const int s = seg_i % kSegRing;
+        if (!__all_sync(0xffffffffu, mbar_wait(&bars[C_SEGFULL + s], (uint32_t)(seg_i / kSegRing) & 1u, abort_flag))) {
+            if (lane == 0) { report(p.status, PT_ERR_DEVICE_TIMEOUT, LOC_CHUNK_WAIT); *abort_flag = 1; }
+            return false;
+        }
+        sg = ring[s];
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&bars[C_SEGEMPTY + s]);
+        ++seg_i;
+        return sg.lo >= 0;
+    };
     Seg sg;
-    sg.start(*plan, p, tpt);
-    bool more = true;
 
     if (warp < 4) {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
-    if (warp == 0) {
-        // ------------------------------------------------------------------ copies
+    if (warp == 0 || warp == 3) {
+        // ------------------------------------------------------------------ copies: warp 0 Q and K, warp 3 V
+        // A key tile is 128 / box boxes of `box` keys (a divisor of the page, so a box lies in one page), one lane each; the
+        // page numbers of the next tile are fetched before this one's ring slot is waited for.
+        const bool is_v = warp == 3;
         bool bad_page = false, ok = true;
-        int jj = 0, qc[2] = {0, 0}, raw = 0;
+        int jj = 0, qc[2] = {0, 0}, raw = 0, turn = 0;
         auto wait = [&](int bar, uint32_t parity) {
-            if (!mbar_wait(&bars[bar], parity, abort_flag, true)) { if (lane == 0) { report(p.status, PT_ERR_DEVICE_TIMEOUT, LOC_CHUNK_WAIT); *abort_flag = 1; } ok = false; }
+            if (!mbar_wait(&bars[bar], parity, abort_flag, true, 32)) { if (lane == 0) { report(p.status, PT_ERR_DEVICE_TIMEOUT, LOC_CHUNK_WAIT); *abort_flag = 1; } ok = false; }
             ok = __all_sync(0xffffffffu, ok);
             return ok;
         };
-        for (; more && ok; more = sg.advance(p, tpt)) {
-            if (sg.lo >= sg.hi) continue;
-            const int t = sg.tk / p.nkv, kvh = sg.tk % p.nkv;
-#pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                if (sg.lo >= (i ? sg.n1 : sg.n0)) continue;
-                if (!wait(C_QEMPTY + i, (uint32_t)(qc[i] & 1) ^ 1u)) break;
-                if (lane == 0) {
-                    mbar_expect_tx(&bars[C_QFULL + i], q_bytes);
-#pragma unroll
-                    for (int h = 0; h < HALVES; ++h)
-                        tma_load_4d(smem_u32(sq + i * TILE + h * kHalfBytes), &qmap, &bars[C_QFULL + i], h * 64, kvh * G, sg.qrow0 + sg.tok0 + i * tpt, t);
-                }
-                ++qc[i];
-            }
+        while (ok && next_seg(sg)) {
+            const int t = sg.t, kvh = sg.kvh;
             const int32_t* bt = p.bt + (size_t)sg.b * p.maxp;
+            auto row_of = [&](int j) {                             // first cache row of this lane's box of tile j
+                const int key = j * 128 + lane * box;
+                if (lane * box >= 128 || key >= sg.kvlen) return -1;
+                int page = bt[key / p.ps];
+                if (page < 0 || page >= p.num_pages) { bad_page = true; page = 0; }
+                return ((page * 2 + (is_v ? 1 : 0)) * p.nkv + kvh) * p.ps + key % p.ps;
+            };
+            int row = row_of(sg.lo);
+            if (!is_v) {
+                const bool one = sg.n1 == 0;                       // one row tile: the two Q buffers take turns
+                if (one) turn ^= 1;
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    if (one ? i != turn : sg.lo >= (i ? sg.n1 : sg.n0)) continue;
+                    if (!wait(C_QEMPTY + i, (uint32_t)(qc[i] & 1) ^ 1u)) break;
+                    if (lane == 0) {
+                        mbar_expect_tx(&bars[C_QFULL + i], q_bytes);
+#pragma unroll
+                        for (int h = 0; h < HALVES; ++h)
+                            tma_load_4d(smem_u32(sq + i * TILE + h * kHalfBytes), &qmap, &bars[C_QFULL + i], h * 64, kvh * G, sg.row0 + (one ? 0 : i) * tpt, t);
+                    }
+                    ++qc[i];
+                }
+            }
             for (int j = sg.lo; j < sg.hi && ok; ++j, ++jj) {
-                const int sK = jj % kStK, s = jj % kStV;
                 const int key0 = j * 128;
-                const int ng = min(8, (sg.kvlen - key0 + 15) >> 4);    // 16-key groups of this tile that hold keys
-                int row_k = 0;
-                if (lane < ng) {
-                    const int key = key0 + lane * 16;
-                    int page = bt[key / p.ps];
-                    if (page < 0 || page >= p.num_pages) { bad_page = true; page = 0; }
-                    row_k = (page * 2 * p.nkv + kvh) * p.ps + key % p.ps;
-                }
-                const uint32_t bytes = (uint32_t)ng * 16u * DH * 2u;
-                if (!wait(C_KEMPTY + sK, (uint32_t)(jj / kStK & 1) ^ 1u)) break;
-                if (lane == 0) mbar_expect_tx(&bars[C_KFULL + sK], bytes);
+                const int next = j + 1 < sg.hi ? row_of(j + 1) : -1;
+                const int ng = min(128 / box, (sg.kvlen - key0 + box - 1) / box);     // boxes of this tile that hold keys
+                const uint32_t bytes = (uint32_t)(ng * box) * DH * 2u;
+                const int s = jj % (is_v ? kStV : kStK);
+                uint8_t* dst = is_v ? sv + s * TILE : sk + s * TILE;
+                if (is_v ? !wait(C_VEMPTY + s, (uint32_t)(jj / kStV & 1) ^ 1u) : !wait(C_KEMPTY + s, (uint32_t)(jj / kStK & 1) ^ 1u)) break;
+                // rows of the last 16-key group past the last key must read as zero where P (also zero) meets them
+                const bool partial = is_v && key0 + 128 > sg.kvlen && ((sg.kvlen - key0) & 15);
+                uint64_t* bar = &bars[partial ? C_VRAW : is_v ? C_VFULL + s : C_KFULL + s];
+                if (lane == 0) mbar_expect_tx(bar, bytes);
                 __syncwarp();
-                if (lane < ng) {
+                if (row >= 0) {
 #pragma unroll
                     for (int h = 0; h < HALVES; ++h)
-                        tma_load_3d(smem_u32(sk + sK * TILE + h * kHalfBytes + lane * 2048), &kvmap, &bars[C_KFULL + sK], h * 64, row_k, t);
-                }
-                if (!wait(C_VEMPTY + s, (uint32_t)(jj / kStV & 1) ^ 1u)) break;
-                const bool partial = ((sg.kvlen - key0) & 15) && key0 + 128 > sg.kvlen;    // rows of the last group past the last key must read as zero
-                uint64_t* vbar = partial ? &bars[C_VRAW] : &bars[C_VFULL + s];
-                if (lane == 0) mbar_expect_tx(vbar, bytes);
-                __syncwarp();
-                if (lane < ng) {
-#pragma unroll
-                    for (int h = 0; h < HALVES; ++h)
-                        tma_load_3d(smem_u32(sv + s * TILE + h * kHalfBytes + lane * 2048), &kvmap, vbar, h * 64, row_k + p.nkv * p.ps, t);
+                        tma_load_3d(smem_u32(dst + h * kHalfBytes + lane * box * 128), &kvmap, bar, h * 64, row, t);
                 }
                 if (partial) {
                     if (!wait(C_VRAW, (uint32_t)raw & 1u)) break;
                     ++raw;
-                    const int nvalid = sg.kvlen - key0;
-                    for (int idx = lane; idx < (ng * 16 - nvalid) * HALVES * 8; idx += 32) {
-                        const int row = nvalid + idx / (HALVES * 8), rem = idx % (HALVES * 8);
-                        *reinterpret_cast<uint4*>(sv + s * TILE + (rem >> 3) * kHalfBytes + row * 128 + (rem & 7) * 16) = make_uint4(0, 0, 0, 0);
+                    const int nvalid = sg.kvlen - key0, top = (nvalid + 15) & ~15;
+                    for (int idx = lane; idx < (top - nvalid) * HALVES * 8; idx += 32) {
+                        const int rr = nvalid + idx / (HALVES * 8), rem = idx % (HALVES * 8);
+                        *reinterpret_cast<uint4*>(dst + (rem >> 3) * kHalfBytes + rr * 128 + (rem & 7) * 16) = make_uint4(0, 0, 0, 0);
                     }
                     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                     __syncwarp();
                     if (lane == 0) mbar_arrive(&bars[C_VFULL + s]);
                 }
+                row = next;
             }
         }
         if (bad_page) report(p.status, PT_ERR_DEVICE_BOUNDS, LOC_CHUNK_PAGE);
         if (!ok) {                                                 // copies still in flight get a bounded time to land
             WaitClock clock;
-            for (int b = C_KFULL; b < C_VFULL + kStV; ++b)
-                for (uint32_t i = 0; i < (1u << 16) && !clock.expired(100000000ull); ++i) __nanosleep(64);
+            for (uint32_t i = 0; i < (1u << 16) && !clock.expired(100000000ull); ++i) __nanosleep(64);
+        }
+    } else if (warp == 2) {
+        // ------------------------------------------------------------------ the walk
+        Walk wk;
+        bool more = wk.find(p, tpt, gridDim.x, blockIdx.x, blockIdx.x == 0), ok = true;
+        for (int i = 0; ok; ++i) {
+            while (more && wk.lo >= wk.hi) more = wk.advance(p, tpt);
+            const int s = i % kSegRing;
+            ok = __all_sync(0xffffffffu, mbar_wait(&bars[C_SEGEMPTY + s], ((uint32_t)(i / kSegRing) & 1u) ^ 1u, abort_flag, true));
+            if (!ok) { if (lane == 0) { report(p.status, PT_ERR_DEVICE_TIMEOUT, LOC_CHUNK_WAIT); *abort_flag = 1; } break; }
+            if (lane == 0) {
+                Seg o;
+                o.row0 = wk.qrow0 + wk.tok0; o.t = wk.tk / p.nkv; o.kvh = wk.tk % p.nkv; o.kvlen = wk.kvlen;
+                o.pos0 = wk.kvlen - wk.qlen + wk.tok0; o.left = wk.qlen - wk.tok0;
+                o.n0 = wk.n0; o.n1 = wk.n1; o.lo = more ? wk.lo : -1; o.hi = wk.hi; o.b = wk.b; o.pad = 0;
+                ring[s] = o;
+                mbar_arrive(&bars[C_SEGFULL + s]);
+            }
+            __syncwarp();
+            if (!more) break;
+            more = wk.advance(p, tpt);
         }
     } else if (warp == 1) {
         // ------------------------------------------------------------------ MMA issuer
         constexpr uint32_t idesc_qk = (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(128 >> 3) << 17) | ((uint32_t)(128 >> 4) << 24);
         constexpr uint32_t idesc_pv = (1u << 4) | (1u << 7) | (1u << 10) | (1u << 16) | ((uint32_t)(DH >> 3) << 17) | ((uint32_t)(128 >> 4) << 24);
         bool ok = true;
-        int jj = 0, qc[2] = {0, 0}, cnt[2] = {0, 0};
+        int jj = 0, qc[2] = {0, 0}, cnt[2] = {0, 0}, turn = 0;
         auto wait = [&](int bar, uint32_t parity) {
             if (!ok) return;
             if (!__all_sync(0xffffffffu, mbar_wait(&bars[bar], parity, abort_flag))) { ok = false; if (lane == 0) { report(p.status, PT_ERR_DEVICE_TIMEOUT, LOC_CHUNK_WAIT); *abort_flag = 1; } }
             tc_fence_after();
         };
-        auto qk = [&](int i, int s, bool last) {                   // S_i = Q_i K_s^T
+        auto qk = [&](int i, int qb, int s, bool last) {           // S_i = Q_qb K_s^T
             if (!ok) return;
-            const uint32_t qa = smem_u32(sq + i * TILE), ka = smem_u32(sk + s * TILE);
+            const uint32_t qa = smem_u32(sq + qb * TILE), ka = smem_u32(sk + s * TILE);
 #pragma unroll
             for (int ks = 0; ks < DH / 16; ++ks) {
                 const uint32_t off = (uint32_t)(ks >> 2) * kHalfBytes + (uint32_t)(ks & 3) * 32u;
                 mma_ss(tmem_base + i * 128, desc_kmajor(qa + off), desc_kmajor(ka + off), idesc_qk, ks != 0);
             }
             tc_commit(&bars[C_SFULL + i]);
-            if (last) tc_commit(&bars[C_QEMPTY + i]);
+            if (last) tc_commit(&bars[C_QEMPTY + qb]);
         };
-        for (; more && ok; more = sg.advance(p, tpt)) {
-            if (sg.lo >= sg.hi) continue;
+        auto pv = [&](int i, int jv, int ng, bool fresh) {         // O_i (+)= P_i V over the groups that hold keys
+            wait(C_PFULL + i, (uint32_t)cnt[i] & 1u);
+            wait(C_VFULL + jv % kStV, (uint32_t)(jv / kStV) & 1u);
+            ++cnt[i];
+            if (!ok) return;
+            const uint32_t va = smem_u32(sv + (jv % kStV) * TILE);
+            for (int ks = 0; ks < ng; ++ks)
+                mma_ts(tmem_base + 256 + i * DH, tmem_base + i * 128 + ks * 8, desc_mnmajor(va + ks * 2048), idesc_pv, !fresh || ks != 0);
+            tc_commit(&bars[C_OREADY + i]);
+        };
+        while (ok && next_seg(sg)) {
+            if (sg.n1 == 0) {                                      // one row tile: scores two key tiles ahead, in turns
+                turn ^= 1;
+                const int qb = turn;
+                wait(C_QFULL + qb, (uint32_t)qc[qb] & 1u);
+                ++qc[qb];
+                for (int j = sg.lo; j < sg.hi + 2 && ok; ++j) {
+                    if (j - 2 >= sg.lo) {
+                        pv((j - sg.lo) & 1, jj, min(8, (sg.kvlen - (j - 2) * 128 + 15) >> 4), j - 4 < sg.lo);
+                        if (ok) tc_commit(&bars[C_VEMPTY + jj % kStV]);
+                        ++jj;
+                    }
+                    if (j < sg.hi) {
+                        const int jk = jj + min(j - sg.lo, 1);          // jj: the tile behind the last product with V
+                        wait(C_KFULL + jk % kStK, (uint32_t)(jk / kStK) & 1u);
+                        qk((j - sg.lo) & 1, qb, jk % kStK, j + 1 == sg.hi);
+                        if (ok) tc_commit(&bars[C_KEMPTY + jk % kStK]);
+                    }
+                }
+                continue;
+            }
             const int end[2] = {min(sg.hi, sg.n0), min(sg.hi, sg.n1)};
             wait(C_KFULL + jj % kStK, (uint32_t)(jj / kStK) & 1u);
 #pragma unroll
             for (int i = 0; i < 2; ++i)
-                if (sg.lo < end[i]) { wait(C_QFULL + i, (uint32_t)qc[i] & 1u); ++qc[i]; qk(i, jj % kStK, sg.lo + 1 == end[i]); }
+                if (sg.lo < end[i]) { wait(C_QFULL + i, (uint32_t)qc[i] & 1u); ++qc[i]; qk(i, i, jj % kStK, sg.lo + 1 == end[i]); }
             if (ok) tc_commit(&bars[C_KEMPTY + jj % kStK]);
             for (int j = sg.lo; j < sg.hi && ok; ++j, ++jj) {
-                const int s = jj % kStV, sn = (jj + 1) % kStK;
+                const int sn = (jj + 1) % kStK;
                 const uint32_t phn = (uint32_t)((jj + 1) / kStK) & 1u;
                 const int ng = min(8, (sg.kvlen - j * 128 + 15) >> 4);
 #pragma unroll
                 for (int i = 0; i < 2; ++i) {
                     if (j >= end[i]) continue;
-                    const uint32_t va = smem_u32(sv + s * TILE);   // O_i (+)= P_i V_s over the groups that hold keys
-                    wait(C_PFULL + i, (uint32_t)cnt[i] & 1u);
-                    wait(C_VFULL + s, (uint32_t)(jj / kStV) & 1u);
-                    ++cnt[i];
-                    if (!ok) break;
-                    for (int ks = 0; ks < ng; ++ks)
-                        mma_ts(tmem_base + 256 + i * DH, tmem_base + i * 128 + ks * 8, desc_mnmajor(va + ks * 2048), idesc_pv, j > sg.lo || ks != 0);
-                    tc_commit(&bars[C_OREADY + i]);
-                    if (j + 1 < end[i]) { wait(C_KFULL + sn, phn); qk(i, sn, j + 2 == end[i]); }
+                    pv(i, jj, ng, j == sg.lo);
+                    if (j + 1 < end[i]) { wait(C_KFULL + sn, phn); qk(i, i, sn, j + 2 == end[i]); }
                 }
                 if (ok) {
-                    tc_commit(&bars[C_VEMPTY + s]);
+                    tc_commit(&bars[C_VEMPTY + jj % kStV]);
                     if (j + 1 < sg.hi) tc_commit(&bars[C_KEMPTY + sn]);
                 }
             }
@@ -349,7 +428,7 @@ k_chunk_tc(const __grid_constant__ CUtensorMap qmap, const __grid_constant__ CUt
     } else {
         // ------------------------------------------------------------------ softmax groups
         asm volatile("setmaxnreg.inc.sync.aligned.u32 216;");
-        const int i = (warp - 4) >> 2;                             // row tile of this warp group
+        const int i = (warp - 4) >> 2;                             // group: its row tile, or its share of the key tiles
         const int w4 = warp & 3;                                   // tensor-memory lane quarter of this warp
         const int r = w4 * 32 + lane;                              // row inside the tile: token r / G, head r % G of the group
         const int tok = r / G, gh = r % G;
@@ -358,23 +437,27 @@ k_chunk_tc(const __grid_constant__ CUtensorMap qmap, const __grid_constant__ CUt
         const float c = p.scale_log2;
         const Slots<DH> slots{scratch};
         bool ok = true;
-        int cnt = 0;
+        int cnt = 0, merges = 0;
         auto wait = [&](int bar, uint32_t parity) {
             ok = __all_sync(0xffffffffu, mbar_wait(&bars[bar], parity, abort_flag));
             if (!ok && lane == 0) { report(p.status, PT_ERR_DEVICE_TIMEOUT, LOC_CHUNK_WAIT); *abort_flag = 1; }
             tc_fence_after();
             return ok;
         };
-        for (; more && ok; more = sg.advance(p, tpt)) {
-            const int n_i = i ? sg.n1 : sg.n0, end = min(sg.hi, n_i);
+        while (ok && next_seg(sg)) {
+            const bool one = sg.n1 == 0;
+            const int n_i = !one && i ? sg.n1 : sg.n0, end = min(sg.hi, n_i);
             if (sg.lo >= end) continue;
-            const int start = sg.kvlen - sg.qlen, tok_i = sg.tok0 + i * tpt;
-            const bool live = tok < tpt && tok_i + tok < sg.qlen;
-            const int limit = min(start + tok_i + tok, sg.kvlen - 1);  // last visible key of this row
-            const int tile_limit = min(start + tok_i, sg.kvlen - 1);   // last visible key of the tile's first row
+            const int tok_i = (one ? 0 : i) * tpt;                     // first token of the tile, from the segment's first
+            const bool live = tok < tpt && tok_i + tok < sg.left;
+            const bool any = __any_sync(0xffffffffu, live);            // a warp without rows only keeps the barriers going
+            const int limit = min(sg.pos0 + tok_i + tok, sg.kvlen - 1);  // last visible key of this row
+            const int tile_limit = min(sg.pos0 + tok_i, sg.kvlen - 1);   // last visible key of the tile's first row
+            const int first = sg.lo + (one ? i : 0), step = one ? 2 : 1;
             float m_ref = -INFINITY, l_run = 0.f;
-            for (int j = sg.lo; j < end; ++j, ++cnt) {
+            for (int j = first; j < end; j += step, ++cnt) {
                 if (!wait(C_SFULL + i, (uint32_t)cnt & 1u)) break;
+                if (!any) { if (lane == 0) mbar_arrive(&bars[C_PFULL + i]); continue; }
                 const int key0 = j * 128;
                 float v[128];
 #pragma unroll
@@ -391,7 +474,7 @@ k_chunk_tc(const __grid_constant__ CUtensorMap qmap, const __grid_constant__ CUt
                     mx2 = max3(mx2, v[e + 4], v[e + 5]); mx3 = max3(mx3, v[e + 6], v[e + 7]);
                 }
                 const float mx = fmaxf(fmaxf(mx0, mx1), fmaxf(mx2, mx3));
-                if (j == sg.lo) {
+                if (j == first) {
                     m_ref = mx;                                    // -inf where the row sees nothing of this tile
                 } else {
                     const bool grow = live && (mx - m_ref) * c > 8.0f;     // also from -inf, when mx is finite
@@ -436,16 +519,44 @@ k_chunk_tc(const __grid_constant__ CUtensorMap qmap, const __grid_constant__ CUt
                 __syncwarp();
                 if (lane == 0) mbar_arrive(&bars[C_PFULL + i]);
             }
-            if (!ok || !wait(C_OREADY + i, (uint32_t)(cnt - 1) & 1u)) break;
+            if (!ok || (first < end && !wait(C_OREADY + i, (uint32_t)(cnt - 1) & 1u))) break;
+            float m = m_ref * c, f0 = 1.f, f1 = 0.f;                   // the maximum in powers of two, the groups' factors
+            if (one) {
+                if (i == 1) {
+                    odd_stats[r] = make_float2(m, l_run);
+                    tc_fence_before();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(&bars[C_MREADY]);
+                    if (!wait(C_MDONE, (uint32_t)merges++ & 1u)) break;
+                    continue;
+                }
+                if (!wait(C_MREADY, (uint32_t)merges++ & 1u)) break;
+                const float2 odd = odd_stats[r];
+                const float top = fmaxf(m, odd.x);
+                f0 = m > -INFINITY ? ex2(m - top) : 0.f;
+                f1 = odd.x > -INFINITY ? ex2(odd.x - top) : 0.f;
+                m = top;
+                l_run = l_run * f0 + odd.y * f1;
+            }
+            // 32 columns of the output, merged
+            auto columns = [&](int cc, float* o) {
+                tm_ld32(t_o + cc * 32, o);
+                if (one && sg.lo + 1 < end) {
+                    float o1[32];
+                    tm_ld32(t_o + DH + cc * 32, o1);
+                    tm_wait_ld();
+#pragma unroll
+                    for (int e = 0; e < 32; ++e) o[e] = o[e] * f0 + (f1 > 0.f ? o1[e] * f1 : 0.f);
+                } else tm_wait_ld();
+            };
+            if (any) {
             if (sg.lo == 0 && end == n_i) {                        // all of the tile's keys: the result
                 const float inv = l_run > 0.f ? 1.0f / l_run : 0.f;
-                const int t = sg.tk / p.nkv, head = (sg.tk % p.nkv) * G + gh;
-                __nv_bfloat16* dst = p.o + ((size_t)t * p.M + sg.qrow0 + tok_i + tok) * (size_t)(p.nq * DH) + (size_t)head * DH;
+                __nv_bfloat16* dst = p.o + ((size_t)sg.t * p.M + sg.row0 + tok_i + tok) * (size_t)(p.nq * DH) + (size_t)(sg.kvh * G + gh) * DH;
 #pragma unroll 1
                 for (int cc = 0; cc < DH / 32; ++cc) {
                     float o[32];
-                    tm_ld32(t_o + cc * 32, o);
-                    tm_wait_ld();
+                    columns(cc, o);
                     if (live) {
 #pragma unroll
                         for (int e = 0; e < 32; e += 8) {
@@ -458,18 +569,24 @@ k_chunk_tc(const __grid_constant__ CUtensorMap qmap, const __grid_constant__ CUt
                 }
             } else {                                               // a part: merged by k_chunk_combine
                 const int which = sg.lo > 0 ? 0 : 1;
-                if (live) slots.stats(blockIdx.x, which)[i * 128 + r] = make_float2(m_ref * c, l_run);
-                float* dst = slots.out(blockIdx.x, which) + (size_t)(i * 128 + r) * DH;
+                const int slot_row = (one ? 0 : i) * 128 + r;
+                if (live) slots.stats(blockIdx.x, which)[slot_row] = make_float2(m, l_run);
+                float* dst = slots.out(blockIdx.x, which) + (size_t)slot_row * DH;
 #pragma unroll 1
                 for (int cc = 0; cc < DH / 32; ++cc) {
                     float o[32];
-                    tm_ld32(t_o + cc * 32, o);
-                    tm_wait_ld();
+                    columns(cc, o);
                     if (live) {
 #pragma unroll
                         for (int e = 0; e < 32; e += 4) *reinterpret_cast<float4*>(dst + cc * 32 + e) = make_float4(o[e], o[e + 1], o[e + 2], o[e + 3]);
                     }
                 }
+            }
+            }
+            if (one) {
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(&bars[C_MDONE]);
             }
             tc_fence_before();                                     // the accumulator has been read: the next segment's P may follow
         }
@@ -489,16 +606,13 @@ constexpr int kCombineThreads = 256;
 template <int DH>
 __global__ void __launch_bounds__(kCombineThreads)
 k_chunk_combine(const ChunkP p, float* scratch, const int tpt, const int blocks) {
-    __shared__ int64_t buf[2 * (kCombineThreads / 32)];
-    __shared__ Plan plan;
-    make_plan<kCombineThreads>(p, tpt, blocks, blockIdx.x + 1, &plan, buf);
-    Seg sg;
-    bool mine = plan.len > 0;
+    Walk sg;
+    bool mine = sg.find(p, tpt, blocks, blockIdx.x + 1, false);    // every warp for itself
     int64_t seg_start = 0;
-    auto lo_of = [&](int c) { const int64_t rel = plan.total * c / plan.ranges - seg_start; return rel >= (int64_t)0x7fffffff - sg.w ? sg.n : min(sg.n, Seg::first_at((int)max(rel, (int64_t)0), sg.w)); };
+    // first key tile of the segment that belongs to range c or a later one
+    auto lo_of = [&](int c) { return min(sg.n, Walk::first_at((int)max((int64_t)0, min(sg.border(c) - seg_start, (int64_t)0x3fffffff)), sg.w)); };
     if (mine) {
-        sg.start(plan, p, tpt);
-        seg_start = plan.p0 + plan.u;
+        seg_start = sg.p0 + sg.u;
         mine = sg.lo > 0 && sg.lo < sg.n && lo_of(blockIdx.x) == 0;     // cut at this range's start and at no earlier one
     }
     grid_dep_wait();
@@ -561,7 +675,8 @@ pt_status launch_t(const ChunkP& p, float* scratch, cudaStream_t st) {
     if (r != CUDA_SUCCESS) { set_error("cuTensorMapEncodeTiled (q) failed with code %d", (int)r); return PT_ERR_CUDA; }
     const int64_t rows = (int64_t)p.num_pages * 2 * p.nkv * p.ps;
     if (rows > 0x7fffffff) { set_error("a layer's slab of more than 2^31 cached vectors"); return PT_ERR_UNSUPPORTED; }
-    pt_status s = make_map_bf16_strided(&kvmap, p.pool_l, DH, rows, p.T, p.pool_tstride * 2, 16);
+    const int kv_box = p.ps % 64 == 0 ? 64 : p.ps % 32 == 0 ? 32 : 16;      // a divisor of the page and of the key tile: fewer, larger copies
+    pt_status s = make_map_bf16_strided(&kvmap, p.pool_l, DH, rows, p.T, p.pool_tstride * 2, kv_box);
     if (s != PT_OK) return s;
     static int sms_[kMaxDevices] = {};
     int& sms = sms_[current_device()];
@@ -573,7 +688,7 @@ pt_status launch_t(const ChunkP& p, float* scratch, cudaStream_t st) {
         sms = n;
     }
     const int blocks = std::min(sms, kMaxBlocks);
-    k_chunk_tc<DH><<<blocks, kChunkThreads, ChunkCfg<DH>::SMEM, st>>>(qmap, kvmap, p, scratch, tpt, (uint32_t)(128 * ChunkCfg<DH>::HALVES * G * box));
+    k_chunk_tc<DH><<<blocks, kChunkThreads, ChunkCfg<DH>::SMEM, st>>>(qmap, kvmap, p, scratch, tpt, (uint32_t)(128 * ChunkCfg<DH>::HALVES * G * box), kv_box);
     g_launches.fetch_add(1, std::memory_order_relaxed);
     cudaError_t e = cudaGetLastError();
     if (e == cudaSuccess && blocks > 1) {

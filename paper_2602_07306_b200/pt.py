@@ -406,9 +406,10 @@ class Model:
             self.gen_ws = torch.empty(nb.value, dtype=torch.uint8, device=self.device)
         ids, pids = _i32arr(seq_ids)
         if u is not None:
-            _sampling_args(torch, self.device, (n_new, B), u=u)
-            _sampling_args(torch, self.device, (B,), temperature=temperature, top_k=top_k, top_p=top_p, min_p=min_p)
-            _sampling_args(torch, self.device, (B, n_new), prob=prob)
+            index = prompt.get_device()
+            _sampling_args(index, (n_new, B), u=u)
+            _sampling_args(index, (B,), temperature=temperature, top_k=top_k, top_p=top_p, min_p=min_p)
+            _sampling_args(index, (B, n_new), prob=prob)
             sp = pt_sampling(*(None if a is None else a.data_ptr() for a in (u, temperature, top_k, top_p, min_p, prob)))
             with torch.cuda.device(self.device):
                 check(lib().pt_generate_sample(self.h, cache.h, prompt.data_ptr(), B, S, n_new, pids, C.byref(sp), out.data_ptr(),
@@ -558,11 +559,47 @@ class Cache:
         return codes * self.scales.view(shape + (1,))
 
 
-def _sampling_args(torch, device, shape, **arrays):
+def _raw_stream(index: int) -> int:
+    """Handle of torch's current stream of a device."""
+    import torch
+    return torch._C._cuda_getCurrentRawStream(index)
+
+
+def _call(index: int, fn, *args) -> None:
+    """fn(*args, current stream) with device `index` current, checked.  The device is switched only where it has to be: a
+    guard costs as much as a small call."""
+    import torch
+    if torch._C._cuda_getDevice() == index:
+        check(fn(*args, _raw_stream(index)))
+    else:
+        with torch.cuda.device(index):
+            check(fn(*args, _raw_stream(index)))
+
+
+_status_blocks = {}
+
+
+def _new_status(index: int):
+    """A zeroed int32[16] of its own on the device, for a call on its current stream: cut from a block that one fill zeroes
+    for 256 calls of that stream (inside a capture, whose memory belongs to the graph: from none)."""
+    import torch
+    if torch.cuda.is_current_stream_capturing():
+        return torch.zeros(16, dtype=torch.int32, device=index)
+    key = (index, _raw_stream(index))
+    left = _status_blocks.get(key)
+    if not left:
+        left = _status_blocks[key] = list(torch.zeros((256, 16), dtype=torch.int32, device=index).unbind(0))
+    return left.pop()
+
+
+def _sampling_args(index, shape, **arrays):
+    import torch
     for name, a in arrays.items():
-        want = torch.int32 if name in ("top_k", "token") else torch.float32
-        if a is not None and (a.device != device or a.dtype != want or tuple(a.shape) != shape or not a.is_contiguous()):
-            raise ValueError(f"{name}: a contiguous {want} tensor of shape {shape} on {device} is wanted")
+        if a is None:
+            continue
+        want = torch.int32 if name == "top_k" or name == "token" else torch.float32
+        if a.dtype is not want or a.shape != shape or a.get_device() != index or not a.is_contiguous():
+            raise ValueError(f"{name}: a contiguous {want} tensor of shape {shape} on CUDA device {index} is wanted")
 
 
 def sample(logits, u, temperature=None, top_k=None, top_p=None, min_p=None, *, out=None, prob=None):
@@ -570,43 +607,45 @@ def sample(logits, u, temperature=None, top_k=None, top_p=None, min_p=None, *, o
     temperature, then top_k, top_p and min_p, each a CUDA tensor [n] or None; see pt_sample in include/pt.h.
     Returns (tokens int32 [n], probabilities fp32 [n]) in `out` and `prob` where given."""
     import torch
-    if not logits.is_cuda or logits.dim() != 2 or logits.dtype not in (torch.float32, torch.bfloat16) or logits.stride(1) != 1:
+    dt = logits.dtype
+    if not logits.is_cuda or logits.dim() != 2 or (dt is not torch.float32 and dt is not torch.bfloat16) or logits.stride(1) != 1:
         raise ValueError("logits: an fp32 or bf16 CUDA tensor [n, vocab] with contiguous rows is wanted")
     n, vocab = logits.shape
+    index = logits.get_device()
     if out is None:
         out = torch.empty(n, dtype=torch.int32, device=logits.device)
     if prob is None:
         prob = torch.empty(n, dtype=torch.float32, device=logits.device)
     if u is None:
         raise ValueError("u: random numbers are wanted")
-    _sampling_args(torch, logits.device, (n,), u=u, temperature=temperature, top_k=top_k, top_p=top_p, min_p=min_p, token=out, prob=prob)
-    ptr = lambda a: None if a is None else a.data_ptr()
-    with torch.cuda.device(logits.device):
-        check(lib().pt_sample(logits.data_ptr(), PT_F32 if logits.dtype == torch.float32 else PT_BF16, logits.stride(0) if n > 1 else vocab, n, vocab,
-                              u.data_ptr(), ptr(temperature), ptr(top_k), ptr(top_p), ptr(min_p), out.data_ptr(), prob.data_ptr(),
-                              torch.cuda.current_stream().cuda_stream))
+    _sampling_args(index, (n,), u=u, temperature=temperature, top_k=top_k, top_p=top_p, min_p=min_p, token=out, prob=prob)
+    _call(index, lib().pt_sample, logits.data_ptr(), PT_F32 if dt is torch.float32 else PT_BF16, logits.stride(0) if n > 1 else vocab, n, vocab,
+          u.data_ptr(), None if temperature is None else temperature.data_ptr(), None if top_k is None else top_k.data_ptr(),
+          None if top_p is None else top_p.data_ptr(), None if min_p is None else min_p.data_ptr(), out.data_ptr(), prob.data_ptr())
     return out, prob
 
 
 def kernel_kv_copy_pages(pool, src, dst, *, scales=None, out=None, out_scales=None):
     """Pages src[i] of pool [T, L, pages, ...] (any type) to its pages dst[i] in every (track, layer) slab; `scales`
     [T, L, pages, ...] likewise.  src, dst: host integers.  `out`, `out_scales`: another pool to copy to."""
-    import torch
     src, dst = np.ascontiguousarray(src, np.int32), np.ascontiguousarray(dst, np.int32)
     if src.ndim != 1 or src.shape != dst.shape:
         raise ValueError("src and dst: two lists of the same length are wanted")
-    with torch.cuda.device(pool.device):
-        st = torch.cuda.current_stream().cuda_stream
-        for a, b in ((pool, out), (scales, out_scales)):
-            if a is None:
-                continue
-            b = a if b is None else b
-            if not (a.is_cuda and a.is_contiguous() and b.is_contiguous()) or a.dtype != b.dtype or a.device != pool.device or b.device != pool.device \
-                    or a.shape[:2] != b.shape[:2] or a.shape[3:] != b.shape[3:]:
-                raise ValueError("pools: contiguous CUDA tensors [T, L, pages, ...] that differ in their pages alone are wanted")
-            slabs = a.shape[0] * a.shape[1]
-            check(lib().pt_kernel_kv_copy_pages(a.data_ptr(), a.shape[2], b.data_ptr(), b.shape[2], slabs,
-                                                a.numel() * a.element_size() // (slabs * a.shape[2]), src.ctypes.data, dst.ctypes.data, len(src), st))
+    index = pool.get_device()
+    ps, pd, n = src.__array_interface__["data"][0], dst.__array_interface__["data"][0], len(src)
+    for a, b in ((pool, out), (scales, out_scales)):
+        if a is None:
+            continue
+        sa = a.shape
+        if b is None:
+            b, sb = a, sa
+        else:
+            sb = b.shape
+        if not (a.is_cuda and a.is_contiguous()) or a.get_device() != index or b is not a and \
+                (not b.is_contiguous() or a.dtype != b.dtype or b.get_device() != index or sa[:2] != sb[:2] or sa[3:] != sb[3:]):
+            raise ValueError("pools: contiguous CUDA tensors [T, L, pages, ...] that differ in their pages alone are wanted")
+        slabs = sa[0] * sa[1]
+        _call(index, lib().pt_kernel_kv_copy_pages, a.data_ptr(), sa[2], b.data_ptr(), sb[2], slabs, a.numel() * a.element_size() // (slabs * sa[2]), ps, pd, n)
 
 
 def chunk_attn_scratch(T: int, B: int, nq: int, dh: int, device="cuda:0"):
@@ -625,25 +664,26 @@ def kernel_chunk_attn(q, pool_l, block_table, q_len, kv_len, *, nq, nkv, dh, ps,
     T, M, width = q.shape
     B, maxp = block_table.shape
     pages = pool_l.shape[1]
-    assert q.is_cuda and q.is_contiguous() and pool_l[0].is_contiguous() and block_table.is_contiguous() and q_len.is_contiguous() and kv_len.is_contiguous()
-    assert q.dtype == pool_l.dtype == torch.bfloat16 and block_table.dtype == q_len.dtype == kv_len.dtype == torch.int32
-    assert width == nq * dh and tuple(pool_l.shape) == (T, pages, 2, nkv, ps, dh) and q_len.numel() == kv_len.numel() == B
-    assert q.device == pool_l.device == block_table.device == q_len.device == kv_len.device
+    index = q.get_device()
+    i32, bf16 = torch.int32, torch.bfloat16
+    assert q.is_cuda and q.is_contiguous() and block_table.is_contiguous() and q_len.is_contiguous() and kv_len.is_contiguous()
+    assert q.dtype is bf16 and pool_l.dtype is bf16 and block_table.dtype is i32 and q_len.dtype is i32 and kv_len.dtype is i32
+    assert width == nq * dh and pool_l.shape == (T, pages, 2, nkv, ps, dh) and q_len.numel() == kv_len.numel() == B
+    assert pool_l.stride()[1:] == (2 * nkv * ps * dh, nkv * ps * dh, ps * dh, dh, 1) or pool_l[0].is_contiguous()
+    assert index == pool_l.get_device() == block_table.get_device() == q_len.get_device() == kv_len.get_device()
     if out is None:
         out = torch.empty_like(q)
     if scratch is None:
         scratch = chunk_attn_scratch(T, B, nq, dh, q.device)
     if status is None:
-        status = torch.zeros(16, dtype=torch.int32, device=q.device)
-    assert out.device == q.device and out.dtype == q.dtype and out.shape == q.shape and out.is_contiguous()
-    assert scratch.device == q.device and status.device == q.device and status.dtype == torch.int32 and status.numel() >= 16
+        status = _new_status(index)
+    assert out.get_device() == index and out.dtype is bf16 and out.shape == q.shape and out.is_contiguous()
+    assert scratch.get_device() == index and status.get_device() == index and status.dtype is i32 and status.numel() >= 16
     if impl is None:
         impl = 0 if dh in (64, 128) and ps % 16 == 0 else 1
-    with torch.cuda.device(q.device):
-        check(lib().pt_kernel_chunk_attn(q.data_ptr(), pool_l.data_ptr(), pool_l.stride(0), block_table.data_ptr(), maxp,
-                                         q_len.data_ptr(), kv_len.data_ptr(), T, B, M, nq, nkv, dh, ps, pages, out.data_ptr(), impl,
-                                         scratch.data_ptr(), scratch.numel() * scratch.element_size(), status.data_ptr(),
-                                         torch.cuda.current_stream().cuda_stream))
+    _call(index, lib().pt_kernel_chunk_attn, q.data_ptr(), pool_l.data_ptr(), pool_l.stride(0), block_table.data_ptr(), maxp,
+          q_len.data_ptr(), kv_len.data_ptr(), T, B, M, nq, nkv, dh, ps, pages, out.data_ptr(), impl,
+          scratch.data_ptr(), scratch.numel() * scratch.element_size(), status.data_ptr())
     return out, status
 
 
