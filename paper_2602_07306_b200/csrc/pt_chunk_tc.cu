@@ -38,31 +38,35 @@ enum { C_QFULL = 0, C_QEMPTY = 2, C_KFULL = 4, C_KEMPTY = 7, C_VFULL = 10, C_VEM
 constexpr int kSegRing = 4;                    // segments handed out ahead
 constexpr int kSegReaders = 11;                // warps 0, 1, 3 and the eight of the softmax
 
-// Cost of one segment, of `left` tokens from its first one on and `keys` keys seen by its last row.
-__device__ __forceinline__ int seg_cost(int left, int keys, int tpt) { return kCostSeg + ((keys + 127) >> 7) * (left > tpt ? kCost2 : kCost1); }
+// Cost of one segment, of `left` tokens from its first one on and `keys` keys seen by its last row, in units of 2^sh (the
+// host picks sh so that the sum over everything fits 31 bits); the + 1 keeps it above its last tile's position.
+__device__ __forceinline__ int seg_cost(int left, int keys, int tpt, int sh) {
+    return ((kCostSeg + ((keys + 127) >> 7) * (left > tpt ? kCost2 : kCost1)) >> sh) + 1;
+}
 
 // Walks the segments of a range.  Position of key tile k of a segment that starts at u (relative to the range): u for k = 0,
-// u + kCostSeg + k w for the others; a tile belongs to the range its position lies in.
+// u + (kCostSeg + k w) / 2^sh for the others; a tile belongs to the range its position lies in.
+// This code runs once per block and launch, so what it costs is fetching its instructions: it is written to be short.
 struct Walk {
-    int64_t total, p0;                             // cost of everything, start of the range
-    int ranges;
-    int b, qrow0, qlen, kvlen, tk, qb, u, len;     // len: length of the range
+    int u, len, p0;                                // start of the segment relative to the range, length and start of the range
+    int b, qrow0, qlen, kvlen, tk, qb;
     int tok0, n0, n1, n, w, lo, hi;                // key tiles of the two row tiles, and the part [lo, hi) of max(n0, n1) that is ours
-    __device__ __forceinline__ static int first_at(int rel, int w) {       // first tile whose position, relative to the segment, is >= rel
-        return rel <= 0 ? 0 : max(1, (rel - kCostSeg + w - 1) / w);
+    __device__ __forceinline__ static int first_at(int rel, int w, int sh) {   // first tile whose position, relative to the segment, is >= rel
+        return rel <= 0 ? 0 : max(1, ((rel << sh) - kCostSeg + w - 1) / w);
     }
-    __device__ __forceinline__ void derive(int tpt) {
+    __device__ __forceinline__ void derive(int tpt, int sh) {
         tok0 = qb * 2 * tpt;
         n0 = (kvlen - qlen + min(tok0 + tpt, qlen) + 127) >> 7;
         n1 = tok0 + tpt < qlen ? (kvlen - qlen + min(tok0 + 2 * tpt, qlen) + 127) >> 7 : 0;
         n = max(n0, n1);
         w = n1 ? kCost2 : kCost1;
-        lo = min(n, first_at(-u, w));
-        hi = min(n, first_at(len - u, w));
+        lo = u < 0 ? min(n, first_at(-u, w, sh)) : 0;
+        const int cost = ((kCostSeg + n * w) >> sh) + 1;
+        hi = len - u >= cost ? n : min(n, first_at(len - u, w, sh));
     }
     // the next segment that starts inside the range
-    __device__ __forceinline__ bool advance(const ChunkP& p, int tpt) {
-        u += kCostSeg + n * w;
+    __device__ __forceinline__ bool advance(const ChunkP& p, int tpt, int sh) {
+        u += ((kCostSeg + n * w) >> sh) + 1;
         if (u >= len) return false;
         if ((qb + 1) * 2 * tpt < qlen) ++qb;
         else {
@@ -76,99 +80,82 @@ struct Walk {
                 qlen = p.qlen[b]; kvlen = p.kvlen[b];
             }
         }
-        derive(tpt);
+        derive(tpt, sh);
         return true;
     }
-    // where range c starts, of `total` cut into `ranges` (the product stays below 2^53)
-    __device__ __forceinline__ int64_t border(int c) const { return c >= ranges ? total : (int64_t)((double)total * c / ranges); }
 
     // Finds range c of the launch; all lanes of a warp call it and get the same.  False: nothing in it.  Bad lengths are
     // reported by `reporter` and leave every range empty.
-    __device__ bool find(const ChunkP& p, int tpt, int blocks, int c, bool reporter) {
+    __device__ __forceinline__ bool find(const ChunkP& p, int tpt, int sh, int blocks, int c, bool reporter) {
         const int lane = threadIdx.x & 31, tkn = p.T * p.nkv, span = 2 * tpt;
-        auto row_cost = [&](int ql, int kl, bool in) {         // cost of a sequence's segments of one (track, KV head), for every lane's sequence
-            int64_t c1 = 0;
-            const int nb = in ? (ql + span - 1) / span : 0;
-            if (nb <= 8)
-                for (int i = 0; i < nb; ++i) c1 += seg_cost(ql - i * span, kl - ql + min((i + 1) * span, ql), tpt);
-            for (unsigned m = __ballot_sync(0xffffffffu, nb > 8); m; m &= m - 1) {        // long chunks: the warp together
-                const int who = __ffs(m) - 1;
-                const int q1 = __shfl_sync(0xffffffffu, ql, who), k1 = __shfl_sync(0xffffffffu, kl, who), n1 = __shfl_sync(0xffffffffu, nb, who);
-                int64_t s = 0;
-                for (int i = lane; i < n1; i += 32) s += seg_cost(q1 - i * span, k1 - q1 + min((i + 1) * span, q1), tpt);
-#pragma unroll
-                for (int o = 16; o; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
-                if (lane == who) c1 = s;
-            }
-            return c1;
-        };
-        int64_t sum = 0, rows = 0, one = 0;
-        int ql = 0, kl = 0;
+        int base = 0, row0 = 0, total = 0, start = 0;
+        int64_t rows = 0;
         bool bad = false;
-        for (int b0 = 0; b0 < p.B; b0 += 32) {
-            const bool in = b0 + lane < p.B;
-            ql = in ? p.qlen[b0 + lane] : 0; kl = in ? p.kvlen[b0 + lane] : 0;
-            const bool ok = ql >= 0 && kl >= ql && (int64_t)kl <= (int64_t)p.maxp * p.ps && ql <= p.M;
-            bad |= !ok;
-            one = row_cost(ql, kl, ok);
-            sum += one; rows += ok ? ql : 0;
-        }
-#pragma unroll
-        for (int o = 16; o; o >>= 1) { sum += __shfl_xor_sync(0xffffffffu, sum, o); rows += __shfl_xor_sync(0xffffffffu, rows, o); }
-        if (__any_sync(0xffffffffu, bad) || rows > p.M) {
-            if (reporter && lane == 0) report(p.status, PT_ERR_DEVICE_BOUNDS, LOC_CHUNK_LEN);
-            return false;
-        }
-        total = sum * tkn;
-        ranges = (int)min((int64_t)blocks, max((int64_t)1, total / kMinUnits));
-        if (total == 0 || c >= ranges) return false;
-        p0 = border(c);
-        len = (int)(border(c + 1) - p0);
-        if (len == 0) return false;
-        int64_t base = 0;
-        int row0 = 0;
-        for (int b0 = 0; b0 < p.B; b0 += 32) {
-            if (p.B > 32) {
+        // the first round over the sequences sums the costs, the second finds the one in which the range starts
+        for (int round = 0; round < 2; ++round) {
+#pragma unroll 1
+            for (int b0 = 0; b0 < p.B; b0 += 32) {
                 const bool in = b0 + lane < p.B;
-                ql = in ? p.qlen[b0 + lane] : 0; kl = in ? p.kvlen[b0 + lane] : 0;
-                one = row_cost(ql, kl, true);
-            }
-            int64_t incl = one * tkn;
-            int rincl = ql;
-#pragma unroll
-            for (int o = 1; o < 32; o <<= 1) {
-                const int64_t x = __shfl_up_sync(0xffffffffu, incl, o); const int y = __shfl_up_sync(0xffffffffu, rincl, o);
-                if (lane >= o) { incl += x; rincl += y; }
-            }
-            const unsigned m = __ballot_sync(0xffffffffu, p0 < base + incl);
-            if (!m) { base += __shfl_sync(0xffffffffu, incl, 31); row0 += __shfl_sync(0xffffffffu, rincl, 31); continue; }
-            const int who = __ffs(m) - 1;                      // the sequence in which the range starts
-            b = b0 + who;
-            qlen = __shfl_sync(0xffffffffu, ql, who); kvlen = __shfl_sync(0xffffffffu, kl, who);
-            qrow0 = row0 + __shfl_sync(0xffffffffu, rincl, who) - qlen;
-            const int64_t per = __shfl_sync(0xffffffffu, one, who), rem = p0 - (base + __shfl_sync(0xffffffffu, incl, who) - per * tkn);
-            tk = (int)((double)rem / (double)per);             // exact up to one either way
-            while ((int64_t)tk * per > rem) --tk;
-            while ((int64_t)(tk + 1) * per <= rem) ++tk;
-            int64_t in = rem - tk * per;
-            const int nb = (qlen + span - 1) / span;
-            for (int q0 = 0; q0 < nb; q0 += 32) {              // its block of rows
-                const int i = q0 + lane;
-                int64_t cst = i < nb ? seg_cost(qlen - i * span, kvlen - qlen + min((i + 1) * span, qlen), tpt) : 0;
-                int64_t cin = cst;
-#pragma unroll
-                for (int o = 1; o < 32; o <<= 1) { const int64_t x = __shfl_up_sync(0xffffffffu, cin, o); if (lane >= o) cin += x; }
-                const unsigned mq = __ballot_sync(0xffffffffu, in < cin);
-                if (mq) {
-                    const int w2 = __ffs(mq) - 1;
-                    qb = q0 + w2;
-                    u = -(int)(in - (__shfl_sync(0xffffffffu, cin, w2) - __shfl_sync(0xffffffffu, cst, w2)));
-                    break;
+                int ql = in ? p.qlen[b0 + lane] : 0;
+                const int kl = in ? p.kvlen[b0 + lane] : 0;
+                if (ql < 0 || kl < ql || (int64_t)kl > (int64_t)p.maxp * p.ps || ql > p.M) { bad = true; ql = 0; }
+                int one = 0;                                   // cost of this lane's sequence for one (track, KV head)
+                for (unsigned m = __ballot_sync(0xffffffffu, ql > span); m; m &= m - 1) {      // long chunks: the warp together
+                    const int who = __ffs(m) - 1, q1 = __shfl_sync(0xffffffffu, ql, who), k1 = __shfl_sync(0xffffffffu, kl, who);
+                    int s = 0;
+#pragma unroll 1
+                    for (int t0 = lane * span; t0 < q1; t0 += 32 * span) s += seg_cost(q1 - t0, k1 - q1 + min(t0 + span, q1), tpt, sh);
+                    s = __reduce_add_sync(0xffffffffu, s);
+                    if (lane == who) one = s;
                 }
-                in -= __shfl_sync(0xffffffffu, cin, 31);
+                if (ql > 0 && ql <= span) one = seg_cost(ql, kl, tpt, sh);
+                if (round == 0) { total += one; rows += ql; continue; }
+                int incl = one * tkn, rincl = ql;
+#pragma unroll
+                for (int o = 1; o < 32; o <<= 1) {
+                    const int x = __shfl_up_sync(0xffffffffu, incl, o), y = __shfl_up_sync(0xffffffffu, rincl, o);
+                    if (lane >= o) { incl += x; rincl += y; }
+                }
+                const unsigned m = __ballot_sync(0xffffffffu, start < base + incl);
+                const int who = m ? __ffs(m) - 1 : 31;
+                const int at = base + __shfl_sync(0xffffffffu, incl, who), rat = row0 + __shfl_sync(0xffffffffu, rincl, who);
+                if (!m) { base = at; row0 = rat; continue; }
+                const int per = __shfl_sync(0xffffffffu, one, who), rem = start - (at - per * tkn);
+                b = b0 + who;
+                qlen = __shfl_sync(0xffffffffu, ql, who); kvlen = __shfl_sync(0xffffffffu, kl, who);
+                qrow0 = rat - qlen;
+                tk = (int)((unsigned)rem / (unsigned)per);
+                int left = rem - tk * per;                     // inside its segments of that (track, KV head)
+#pragma unroll 1
+                for (qb = 0;; qb += 32) {
+                    const int t0 = (qb + lane) * span;
+                    const int cst = t0 < qlen ? seg_cost(qlen - t0, kvlen - qlen + min(t0 + span, qlen), tpt, sh) : 0;
+                    int cin = cst;
+#pragma unroll
+                    for (int o = 1; o < 32; o <<= 1) { const int x = __shfl_up_sync(0xffffffffu, cin, o); if (lane >= o) cin += x; }
+                    const unsigned mq = __ballot_sync(0xffffffffu, left < cin);
+                    if (mq) {
+                        const int w2 = __ffs(mq) - 1;
+                        qb += w2;
+                        u = __shfl_sync(0xffffffffu, cin - cst, w2) - left;
+                        return true;
+                    }
+                    left -= __shfl_sync(0xffffffffu, cin, 31);
+                }
             }
-            derive(tpt);
-            return true;
+            if (round) break;
+            total = __reduce_add_sync(0xffffffffu, total) * tkn;
+#pragma unroll
+            for (int o = 16; o; o >>= 1) rows += __shfl_xor_sync(0xffffffffu, rows, o);
+            if (__any_sync(0xffffffffu, bad) || rows > p.M) {
+                if (reporter && lane == 0) report(p.status, PT_ERR_DEVICE_BOUNDS, LOC_CHUNK_LEN);
+                return false;
+            }
+            const int ranges = max(1, min(blocks, total / (((kMinUnits - 1) >> sh) + 1)));
+            if (total == 0 || c >= ranges) return false;
+            const int each = total / ranges, more = total - each * ranges;     // the first `more` ranges are one longer
+            start = p0 = each * c + min(c, more);
+            len = each + (c < more);
         }
         return false;
     }
@@ -184,12 +171,16 @@ template <int DH> struct ChunkCfg {
     static_assert(SMEM <= 232448, "shared memory of one block");
 };
 
+// Where a range starts: the segment that holds its start, and what of it lies in earlier ranges.
+struct Start { int p0, u, len, row0, t, kvh, left, n0, n1, lo, pad[6]; };
+
 // Scratch: two slots per block (the part of a segment that began in an earlier range, the part of one that continues in
-// a later range), each 256 rows of (maximum in powers of two, sum) and 256 rows of DH outputs.
+// a later range), each 256 rows of (maximum in powers of two, sum) and 256 rows of DH outputs; behind them the starts.
 template <int DH> struct Slots {
     float* base;
     __device__ __host__ static constexpr size_t floats() { return 256 * (2 + (size_t)DH); }
     __device__ __forceinline__ float2* stats(int block, int which) const { return reinterpret_cast<float2*>(base + ((size_t)block * 2 + which) * floats()); }
+    __device__ __forceinline__ Start* start(int block) const { return reinterpret_cast<Start*>(base + (size_t)kMaxBlocks * 2 * floats()) + block; }
     __device__ __forceinline__ float* out(int block, int which) const { return base + ((size_t)block * 2 + which) * floats() + 512; }
 };
 
@@ -201,7 +192,7 @@ __device__ __forceinline__ void tma_load_4d(uint32_t dst, const CUtensorMap* map
 template <int DH>
 __global__ void __launch_bounds__(kChunkThreads, 1)
 k_chunk_tc(const __grid_constant__ CUtensorMap qmap, const __grid_constant__ CUtensorMap kvmap, const ChunkP p, float* scratch, const int tpt,
-           const uint32_t q_bytes, const int box) {
+           const uint32_t q_bytes, const int box, const int sh) {
     using C = ChunkCfg<DH>;
     constexpr int HALVES = C::HALVES, TILE = C::TILE;
     extern __shared__ uint8_t smem_raw[];
@@ -330,9 +321,17 @@ k_chunk_tc(const __grid_constant__ CUtensorMap qmap, const __grid_constant__ CUt
     } else if (warp == 2) {
         // ------------------------------------------------------------------ the walk
         Walk wk;
-        bool more = wk.find(p, tpt, gridDim.x, blockIdx.x, blockIdx.x == 0), ok = true;
+        bool more = wk.find(p, tpt, sh, gridDim.x, blockIdx.x, blockIdx.x == 0), ok = true;
+        if (more) wk.derive(tpt, sh);
+        if (lane == 0) {                                           // for the blocks that merge cut segments
+            Start st;
+            st.p0 = wk.p0; st.u = wk.u; st.len = more ? wk.len : 0;
+            st.row0 = wk.qrow0 + wk.tok0; st.t = wk.tk / p.nkv; st.kvh = wk.tk % p.nkv; st.left = wk.qlen - wk.tok0;
+            st.n0 = wk.n0; st.n1 = wk.n1; st.lo = wk.lo;
+            Slots<DH>{scratch}.start(blockIdx.x)[0] = st;
+        }
         for (int i = 0; ok; ++i) {
-            while (more && wk.lo >= wk.hi) more = wk.advance(p, tpt);
+            while (more && wk.lo >= wk.hi) more = wk.advance(p, tpt, sh);
             const int s = i % kSegRing;
             ok = __all_sync(0xffffffffu, mbar_wait(&bars[C_SEGEMPTY + s], ((uint32_t)(i / kSegRing) & 1u) ^ 1u, abort_flag, true));
             if (!ok) { if (lane == 0) { report(p.status, PT_ERR_DEVICE_TIMEOUT, LOC_CHUNK_WAIT); *abort_flag = 1; } break; }
@@ -346,7 +345,7 @@ k_chunk_tc(const __grid_constant__ CUtensorMap qmap, const __grid_constant__ CUt
             }
             __syncwarp();
             if (!more) break;
-            more = wk.advance(p, tpt);
+            more = wk.advance(p, tpt, sh);
         }
     } else if (warp == 1) {
         // ------------------------------------------------------------------ MMA issuer
@@ -605,30 +604,30 @@ k_chunk_tc(const __grid_constant__ CUtensorMap qmap, const __grid_constant__ CUt
 constexpr int kCombineThreads = 256;
 template <int DH>
 __global__ void __launch_bounds__(kCombineThreads)
-k_chunk_combine(const ChunkP p, float* scratch, const int tpt, const int blocks) {
-    Walk sg;
-    bool mine = sg.find(p, tpt, blocks, blockIdx.x + 1, false);    // every warp for itself
-    int64_t seg_start = 0;
-    // first key tile of the segment that belongs to range c or a later one
-    auto lo_of = [&](int c) { return min(sg.n, Walk::first_at((int)max((int64_t)0, min(sg.border(c) - seg_start, (int64_t)0x3fffffff)), sg.w)); };
-    if (mine) {
-        seg_start = sg.p0 + sg.u;
-        mine = sg.lo > 0 && sg.lo < sg.n && lo_of(blockIdx.x) == 0;     // cut at this range's start and at no earlier one
-    }
+k_chunk_combine(const ChunkP p, float* scratch, const int tpt, const int blocks, const int sh) {
     grid_dep_wait();
     grid_dep_launch();
-    if (!mine) return;
+    const Slots<DH> at{scratch};
+    const Start sg = *at.start(blockIdx.x + 1);
+    const int n = max(sg.n0, sg.n1), w = sg.n1 ? kCost2 : kCost1;
+    if (sg.len == 0 || sg.lo == 0 || sg.lo >= n) return;           // the segment is not cut at this range's start
+    const int seg_start = sg.p0 + sg.u;
+    // first key tile of the segment that belongs to range c or a later one; behind the last range, all are before
+    auto lo_of = [&](int c) {
+        if (c >= blocks || at.start(c)->len == 0) return n;
+        return min(n, Walk::first_at(min(at.start(c)->p0 - seg_start, ((kCostSeg + n * w) >> sh) + 1), w, sh));
+    };
+    if (lo_of(blockIdx.x) > 0) return;                             // an earlier range's start cuts it already
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int G = p.nq / p.nkv;
     const Slots<DH> slots{scratch};
     const int i = blockIdx.y >> 2;                                 // row tile
     const int n_i = i ? sg.n1 : sg.n0;
     if (sg.lo >= n_i) return;                                      // this tile's keys all lie in the first part: written there
-    const int t = sg.tk / p.nkv, kvh = sg.tk % p.nkv;
     for (int rr = warp; rr < 32; rr += kCombineThreads / 32) {
         const int r = (blockIdx.y & 3) * 32 + rr;
-        const int tok = r / G, tok_i = sg.tok0 + i * tpt;
-        if (tok >= tpt || tok_i + tok >= sg.qlen) continue;
+        const int tok = r / G, tok_i = i * tpt;
+        if (tok >= tpt || tok_i + tok >= sg.left) continue;
         float m = -INFINITY, l = 0.f, o[DH / 32];
 #pragma unroll
         for (int e = 0; e < DH / 32; ++e) o[e] = 0.f;
@@ -655,7 +654,7 @@ k_chunk_combine(const ChunkP p, float* scratch, const int tpt, const int blocks)
             lo = hi;
         }
         const float inv = l > 0.f ? 1.0f / l : 0.f;
-        __nv_bfloat16* dst = p.o + ((size_t)t * p.M + sg.qrow0 + tok_i + tok) * (size_t)(p.nq * DH) + (size_t)(kvh * G + r % G) * DH + lane;
+        __nv_bfloat16* dst = p.o + ((size_t)sg.t * p.M + sg.row0 + tok_i + tok) * (size_t)(p.nq * DH) + (size_t)(sg.kvh * G + r % G) * DH + lane;
 #pragma unroll
         for (int e = 0; e < DH / 32; ++e) dst[32 * e] = __float2bfloat16_rn(o[e] * inv);
     }
@@ -688,11 +687,16 @@ pt_status launch_t(const ChunkP& p, float* scratch, cudaStream_t st) {
         sms = n;
     }
     const int blocks = std::min(sms, kMaxBlocks);
-    k_chunk_tc<DH><<<blocks, kChunkThreads, ChunkCfg<DH>::SMEM, st>>>(qmap, kvmap, p, scratch, tpt, (uint32_t)(128 * ChunkCfg<DH>::HALVES * G * box), kv_box);
+    // no more than this can be asked of a launch: every block of rows with every key that the table can name
+    const double most = (double)p.T * p.nkv * ((double)p.M / (2 * tpt) + p.B + 1) * (kCostSeg + 1 + ((double)p.maxp * p.ps / 128 + 1) * kCost2);
+    int sh = 0;
+    while (most / (double)(1ll << sh) + (double)p.T * p.nkv * ((double)p.M / (2 * tpt) + p.B + 1) > 1e9 && sh < 20) ++sh;
+    if (most / (double)(1ll << sh) > 1e9) { set_error("chunk attention: too many sequences, rows or pages for one call"); return PT_ERR_UNSUPPORTED; }
+    k_chunk_tc<DH><<<blocks, kChunkThreads, ChunkCfg<DH>::SMEM, st>>>(qmap, kvmap, p, scratch, tpt, (uint32_t)(128 * ChunkCfg<DH>::HALVES * G * box), kv_box, sh);
     g_launches.fetch_add(1, std::memory_order_relaxed);
     cudaError_t e = cudaGetLastError();
     if (e == cudaSuccess && blocks > 1) {
-        e = launch_dependent(k_chunk_combine<DH>, dim3(blocks - 1, 8), dim3(kCombineThreads), (size_t)0, st, p, scratch, tpt, blocks);
+        e = launch_dependent(k_chunk_combine<DH>, dim3(blocks - 1, 8), dim3(kCombineThreads), (size_t)0, st, p, scratch, tpt, blocks, sh);
         g_launches.fetch_add(1, std::memory_order_relaxed);
     }
     if (e != cudaSuccess) { set_error("chunk attention launch: %s", cudaGetErrorString(e)); return PT_ERR_CUDA; }
@@ -701,7 +705,7 @@ pt_status launch_t(const ChunkP& p, float* scratch, cudaStream_t st) {
 
 }  // namespace
 
-size_t chunk_tc_scratch_bytes(int dh) { return (dh == 64 ? Slots<64>::floats() : Slots<128>::floats()) * 4 * 2 * kMaxBlocks; }
+size_t chunk_tc_scratch_bytes(int dh) { return (dh == 64 ? Slots<64>::floats() : Slots<128>::floats()) * 4 * 2 * kMaxBlocks + kMaxBlocks * sizeof(Start); }
 
 pt_status launch_chunk_attn_tc(const ChunkP& p, int dh, void* scratch, cudaStream_t st) {
     return dh == 64 ? launch_t<64>(p, (float*)scratch, st) : launch_t<128>(p, (float*)scratch, st);
