@@ -67,7 +67,7 @@ pt_status pt_kernel_prefill_attn(const void* q, const void* pool_l, int64_t pool
  * is allowed) follow those of sequence b - 1; their K and V are the last q_len[b] of its kv_len[b] cached keys:
  *   out[t][r][h] = softmax_{j <= pos}( q[t][r][h] . K[t][b][h / G][j] / sqrt(dh) ) V[t][b][h / G][j],
  *   r = q_len[0] + .. + q_len[b - 1] + s,   pos = kv_len[b] - q_len[b] + s,   G = nq / nkv <= 8.
- *   q, out        device bf16 [T][M][nq*dh], 16-byte aligned; rows behind the last sequence are not touched
+ *   q, out        device bf16 [T][M][nq*dh], 16-byte and 32-byte aligned; rows behind the last sequence are not touched
  *   pool_l, block_table   as for pt_kernel_decode_attn (entries behind a sequence's last page are not read)
  *   q_len, kv_len DEVICE int32 [B]: a captured call may be replayed with other lengths.  Lengths out of range (negative,
  *                 kv_len < q_len, kv_len > maxp*ps, sum of q_len > M) are reported in `status` and nothing is written

@@ -135,8 +135,8 @@ extern "C" pt_status pt_kernel_chunk_attn(const void* q, const void* pool_l, int
     if (ps < 8 || ps > 64 || ps % 8) { set_error("page size must be a multiple of 8 in [8, 64]"); return PT_ERR_INVALID_ARG; }
     if (impl != 0 && impl != 1) { set_error("impl must be 0 or 1"); return PT_ERR_INVALID_ARG; }
     if (impl == 0 && !chunk_tc_supported(dh, ps)) { set_error("impl 0 needs head_dim 64 or 128 and pages of a multiple of 16 tokens"); return PT_ERR_UNSUPPORTED; }
-    if ((uintptr_t)q % 16 || (uintptr_t)pool_l % 16 || pool_track_stride % 8 || (uintptr_t)out % 16 || (uintptr_t)scratch % 256) {
-        set_error("q, out and the pool must be 16-byte aligned (its track stride a multiple of 8 elements), scratch 256-byte"); return PT_ERR_MISALIGNED;
+    if ((uintptr_t)q % 16 || (uintptr_t)pool_l % 16 || pool_track_stride % 8 || (uintptr_t)out % 32 || (uintptr_t)scratch % 256) {
+        set_error("q and the pool must be 16-byte aligned (its track stride a multiple of 8 elements), out 32-byte, scratch 256-byte"); return PT_ERR_MISALIGNED;
     }
     const size_t need = chunk_scratch_bytes(T, B, nq, dh);
     if (scratch_bytes < need) { set_error("scratch: %zu < %zu bytes", scratch_bytes, need); return PT_ERR_BUFFER_TOO_SMALL; }

@@ -29,9 +29,11 @@ namespace {
 constexpr int kChunkThreads = 384;
 constexpr int kStK = 3, kStV = 2;              // ring depths: head_dim 128: 2 Q + 3 K + 2 V tiles of 32 KB fill a block's shared memory
 constexpr int kMaxBlocks = 148;
-// Cost of a segment in units: kCostSeg once, and per key tile kCost1 with one row tile, kCost2 with two.
-constexpr int kCostSeg = 4, kCost1 = 4, kCost2 = 7;
-constexpr int kMinUnits = kCostSeg + kCost1;   // a range is no shorter
+// Cost of a segment in units of about 0.37 us: once for starting and writing it, and per key tile, with one row tile (bound
+// by its share of the HBM bandwidth) and with two (bound by the softmax and the products).
+// (Measured: a batch of 27 decoding sequences and a 777-token chunk takes 206 us with kCost2 = 7, 177 with 9, 187 with 11.)
+constexpr int kSeg1 = 9, kSeg2 = 20, kCost1 = 4, kCost2 = 9;
+constexpr int kMinUnits = kSeg1 + kCost1;      // a range is no shorter
 
 enum { C_QFULL = 0, C_QEMPTY = 2, C_KFULL = 4, C_KEMPTY = 7, C_VFULL = 10, C_VEMPTY = 12, C_SFULL = 14, C_PFULL = 16, C_OREADY = 18, C_VRAW = 20, C_MREADY = 21, C_MDONE = 22,
        C_SEGFULL = 23, C_SEGEMPTY = 27, C_COUNT = 31 };
@@ -41,32 +43,33 @@ constexpr int kSegReaders = 11;                // warps 0, 1, 3 and the eight of
 // Cost of one segment, of `left` tokens from its first one on and `keys` keys seen by its last row, in units of 2^sh (the
 // host picks sh so that the sum over everything fits 31 bits); the + 1 keeps it above its last tile's position.
 __device__ __forceinline__ int seg_cost(int left, int keys, int tpt, int sh) {
-    return ((kCostSeg + ((keys + 127) >> 7) * (left > tpt ? kCost2 : kCost1)) >> sh) + 1;
+    const int n = (keys + 127) >> 7;
+    return ((left > tpt ? kSeg2 + n * kCost2 : kSeg1 + n * kCost1) >> sh) + 1;
 }
 
 // Walks the segments of a range.  Position of key tile k of a segment that starts at u (relative to the range): u for k = 0,
-// u + (kCostSeg + k w) / 2^sh for the others; a tile belongs to the range its position lies in.
+// u + (kSeg + k w) / 2^sh for the others; a tile belongs to the range its position lies in.
 // This code runs once per block and launch, so what it costs is fetching its instructions: it is written to be short.
 struct Walk {
     int u, len, p0;                                // start of the segment relative to the range, length and start of the range
     int b, qrow0, qlen, kvlen, tk, qb;
-    int tok0, n0, n1, n, w, lo, hi;                // key tiles of the two row tiles, and the part [lo, hi) of max(n0, n1) that is ours
-    __device__ __forceinline__ static int first_at(int rel, int w, int sh) {   // first tile whose position, relative to the segment, is >= rel
-        return rel <= 0 ? 0 : max(1, ((rel << sh) - kCostSeg + w - 1) / w);
+    int tok0, n0, n1, n, cost, lo, hi;                // key tiles of the two row tiles, and the part [lo, hi) of max(n0, n1) that is ours
+    __device__ __forceinline__ static int first_at(int rel, bool two, int sh) {    // first tile whose position, relative to the segment, is >= rel
+        const int w = two ? kCost2 : kCost1;
+        return rel <= 0 ? 0 : max(1, ((rel << sh) - (two ? kSeg2 : kSeg1) + w - 1) / w);
     }
     __device__ __forceinline__ void derive(int tpt, int sh) {
         tok0 = qb * 2 * tpt;
         n0 = (kvlen - qlen + min(tok0 + tpt, qlen) + 127) >> 7;
         n1 = tok0 + tpt < qlen ? (kvlen - qlen + min(tok0 + 2 * tpt, qlen) + 127) >> 7 : 0;
         n = max(n0, n1);
-        w = n1 ? kCost2 : kCost1;
-        lo = u < 0 ? min(n, first_at(-u, w, sh)) : 0;
-        const int cost = ((kCostSeg + n * w) >> sh) + 1;
-        hi = len - u >= cost ? n : min(n, first_at(len - u, w, sh));
+        cost = seg_cost(qlen - tok0, n * 128, tpt, sh);
+        lo = u < 0 ? min(n, first_at(-u, n1 > 0, sh)) : 0;
+        hi = len - u >= cost ? n : min(n, first_at(len - u, n1 > 0, sh));
     }
     // the next segment that starts inside the range
     __device__ __forceinline__ bool advance(const ChunkP& p, int tpt, int sh) {
-        u += ((kCostSeg + n * w) >> sh) + 1;
+        u += cost;
         if (u >= len) return false;
         if ((qb + 1) * 2 * tpt < qlen) ++qb;
         else {
@@ -175,7 +178,9 @@ template <int DH> struct ChunkCfg {
 struct Start { int p0, u, len, row0, t, kvh, left, n0, n1, lo, pad[6]; };
 
 // Scratch: two slots per block (the part of a segment that began in an earlier range, the part of one that continues in
-// a later range), each 256 rows of (maximum in powers of two, sum) and 256 rows of DH outputs; behind them the starts.
+// a later range), each (maximum in powers of two, sum) of 256 rows and DH columns of 256 outputs; behind them the starts.
+// Columns, because a thread holds a row: a warp's store is then 128 contiguous bytes, not 32 lines (a row-wise layout took
+// 7 us per part of 256 rows, as long as three steps of the loop).
 template <int DH> struct Slots {
     float* base;
     __device__ __host__ static constexpr size_t floats() { return 256 * (2 + (size_t)DH); }
@@ -187,6 +192,16 @@ template <int DH> struct Slots {
 __device__ __forceinline__ void tma_load_4d(uint32_t dst, const CUtensorMap* map, uint64_t* bar, int c0, int c1, int c2, int c3) {
     asm volatile("cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5}], [%6];"
                  ::"r"(dst), "l"((uint64_t)map), "r"(c0), "r"(c1), "r"(c2), "r"(c3), "r"(smem_u32(bar)) : "memory");
+}
+
+__device__ __forceinline__ void st_global_32(void* p, const uint32_t* u) {
+    asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};"
+                 ::"l"(p), "r"(u[0]), "r"(u[1]), "r"(u[2]), "r"(u[3]), "r"(u[4]), "r"(u[5]), "r"(u[6]), "r"(u[7]) : "memory");
+}
+// An arrival that orders nothing but itself: for hand-offs of what was read, so that it does not wait for the stores of an
+// output that are still on their way.
+__device__ __forceinline__ void mbar_arrive_relaxed(uint64_t* bar) {
+    asm volatile("mbarrier.arrive.relaxed.cta.shared::cta.b64 _, [%0];" ::"r"(smem_u32(bar)) : "memory");
 }
 
 template <int DH>
@@ -223,6 +238,8 @@ k_chunk_tc(const __grid_constant__ CUtensorMap qmap, const __grid_constant__ CUt
     __syncthreads();
     tc_fence_after();
     const uint32_t tmem_base = *tmem_slot;
+    grid_dep_wait();                                               // everything that this kernel reads or writes may be an earlier kernel's
+    grid_dep_launch();
     // the next segment of the block; false at the end, or after a wait that ran out
     int seg_i = 0;
     auto next_seg = [&](Seg& sg) {
@@ -233,7 +250,7 @@ k_chunk_tc(const __grid_constant__ CUtensorMap qmap, const __grid_constant__ CUt
         }
         sg = ring[s];
         __syncwarp();
-        if (lane == 0) mbar_arrive(&bars[C_SEGEMPTY + s]);
+        if (lane == 0) mbar_arrive_relaxed(&bars[C_SEGEMPTY + s]);
         ++seg_i;
         return sg.lo >= 0;
     };
@@ -558,11 +575,11 @@ k_chunk_tc(const __grid_constant__ CUtensorMap qmap, const __grid_constant__ CUt
                     columns(cc, o);
                     if (live) {
 #pragma unroll
-                        for (int e = 0; e < 32; e += 8) {
-                            uint4 u;
-                            u.x = pack_bf16(o[e] * inv, o[e + 1] * inv); u.y = pack_bf16(o[e + 2] * inv, o[e + 3] * inv);
-                            u.z = pack_bf16(o[e + 4] * inv, o[e + 5] * inv); u.w = pack_bf16(o[e + 6] * inv, o[e + 7] * inv);
-                            *reinterpret_cast<uint4*>(dst + cc * 32 + e) = u;
+                        for (int e = 0; e < 32; e += 16) {         // whole 32-byte sectors: a warp's store touches 32 rows
+                            uint32_t u[8];
+#pragma unroll
+                            for (int x = 0; x < 8; ++x) u[x] = pack_bf16(o[e + 2 * x] * inv, o[e + 2 * x + 1] * inv);
+                            st_global_32(dst + cc * 32 + e, u);
                         }
                     }
                 }
@@ -570,14 +587,14 @@ k_chunk_tc(const __grid_constant__ CUtensorMap qmap, const __grid_constant__ CUt
                 const int which = sg.lo > 0 ? 0 : 1;
                 const int slot_row = (one ? 0 : i) * 128 + r;
                 if (live) slots.stats(blockIdx.x, which)[slot_row] = make_float2(m, l_run);
-                float* dst = slots.out(blockIdx.x, which) + (size_t)slot_row * DH;
+                float* dst = slots.out(blockIdx.x, which) + slot_row;
 #pragma unroll 1
                 for (int cc = 0; cc < DH / 32; ++cc) {
                     float o[32];
                     columns(cc, o);
                     if (live) {
 #pragma unroll
-                        for (int e = 0; e < 32; e += 4) *reinterpret_cast<float4*>(dst + cc * 32 + e) = make_float4(o[e], o[e + 1], o[e + 2], o[e + 3]);
+                        for (int e = 0; e < 32; ++e) dst[(cc * 32 + e) * 256] = o[e];
                     }
                 }
             }
@@ -585,7 +602,7 @@ k_chunk_tc(const __grid_constant__ CUtensorMap qmap, const __grid_constant__ CUt
             if (one) {
                 tc_fence_before();
                 __syncwarp();
-                if (lane == 0) mbar_arrive(&bars[C_MDONE]);
+                if (lane == 0) mbar_arrive_relaxed(&bars[C_MDONE]);
             }
             tc_fence_before();                                     // the accumulator has been read: the next segment's P may follow
         }
@@ -600,7 +617,7 @@ k_chunk_tc(const __grid_constant__ CUtensorMap qmap, const __grid_constant__ CUt
 
 // Merges the parts of cut segments.  Block (c, g) handles the segment that is cut at the start of range c + 1, if no earlier
 // range's start cuts it too: parts lie in range c (second slot) and, as long as the segment goes on, in c + 1, c + 2, ...
-// (first slot).  g: rows 32 g .. 32 g + 31 of its 256; one warp per row.
+// (first slot).  g: rows 32 g .. 32 g + 31 of its 256, a lane each, 16 columns a warp.
 constexpr int kCombineThreads = 256;
 template <int DH>
 __global__ void __launch_bounds__(kCombineThreads)
@@ -609,13 +626,13 @@ k_chunk_combine(const ChunkP p, float* scratch, const int tpt, const int blocks,
     grid_dep_launch();
     const Slots<DH> at{scratch};
     const Start sg = *at.start(blockIdx.x + 1);
-    const int n = max(sg.n0, sg.n1), w = sg.n1 ? kCost2 : kCost1;
+    const int n = max(sg.n0, sg.n1);
     if (sg.len == 0 || sg.lo == 0 || sg.lo >= n) return;           // the segment is not cut at this range's start
     const int seg_start = sg.p0 + sg.u;
     // first key tile of the segment that belongs to range c or a later one; behind the last range, all are before
     auto lo_of = [&](int c) {
         if (c >= blocks || at.start(c)->len == 0) return n;
-        return min(n, Walk::first_at(min(at.start(c)->p0 - seg_start, ((kCostSeg + n * w) >> sh) + 1), w, sh));
+        return min(n, Walk::first_at(min(at.start(c)->p0 - seg_start, seg_cost(sg.left, n * 128, tpt, sh)), sg.n1 > 0, sh));
     };
     if (lo_of(blockIdx.x) > 0) return;                             // an earlier range's start cuts it already
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
@@ -624,39 +641,37 @@ k_chunk_combine(const ChunkP p, float* scratch, const int tpt, const int blocks,
     const int i = blockIdx.y >> 2;                                 // row tile
     const int n_i = i ? sg.n1 : sg.n0;
     if (sg.lo >= n_i) return;                                      // this tile's keys all lie in the first part: written there
-    for (int rr = warp; rr < 32; rr += kCombineThreads / 32) {
-        const int r = (blockIdx.y & 3) * 32 + rr;
-        const int tok = r / G, tok_i = i * tpt;
-        if (tok >= tpt || tok_i + tok >= sg.left) continue;
-        float m = -INFINITY, l = 0.f, o[DH / 32];
+    const int r = (blockIdx.y & 3) * 32 + lane, tok = r / G, tok_i = i * tpt;
+    const bool live = tok < tpt && tok_i + tok < sg.left;
+    for (int col = warp * 16; col < DH; col += kCombineThreads / 32 * 16) {
+        float m = -INFINITY, l = 0.f, o[16];
 #pragma unroll
-        for (int e = 0; e < DH / 32; ++e) o[e] = 0.f;
+        for (int e = 0; e < 16; ++e) o[e] = 0.f;
         for (int c = blockIdx.x, lo = 0; lo < n_i; ++c) {
             const int hi = c == (int)blockIdx.x ? sg.lo : lo_of(c + 1);     // tiles [lo, hi) belong to range c
-            const int top = min(hi, n_i);
-            if (lo < top) {
+            if (lo < min(hi, n_i) && live) {
                 const int which = c == (int)blockIdx.x ? 1 : 0;
                 const float2 st = slots.stats(c, which)[i * 128 + r];
-                const float* src = slots.out(c, which) + (size_t)(i * 128 + r) * DH + lane;
-                if (st.x > m) {
-                    const float f = exp2f(m - st.x);
-                    m = st.x; l *= f;
+                const float* src = slots.out(c, which) + (size_t)col * 256 + i * 128 + r;
+                float x[16];
 #pragma unroll
-                    for (int e = 0; e < DH / 32; ++e) o[e] *= f;
-                }
-                if (st.x > -INFINITY) {
-                    const float f = exp2f(st.x - m);
-                    l += st.y * f;
+                for (int e = 0; e < 16; ++e) x[e] = src[e * 256];
+                const float top = fmaxf(m, st.x);
+                if (top > -INFINITY) {
+                    const float f0 = exp2f(m - top), f1 = exp2f(st.x - top);
+                    m = top; l = l * f0 + st.y * f1;
 #pragma unroll
-                    for (int e = 0; e < DH / 32; ++e) o[e] += src[32 * e] * f;
+                    for (int e = 0; e < 16; ++e) o[e] = o[e] * f0 + x[e] * f1;
                 }
             }
             lo = hi;
         }
+        if (!live) continue;
         const float inv = l > 0.f ? 1.0f / l : 0.f;
-        __nv_bfloat16* dst = p.o + ((size_t)sg.t * p.M + sg.row0 + tok_i + tok) * (size_t)(p.nq * DH) + (size_t)(sg.kvh * G + r % G) * DH + lane;
+        uint32_t u[8];
 #pragma unroll
-        for (int e = 0; e < DH / 32; ++e) dst[32 * e] = __float2bfloat16_rn(o[e] * inv);
+        for (int e = 0; e < 8; ++e) u[e] = pack_bf16(o[2 * e] * inv, o[2 * e + 1] * inv);
+        st_global_32(p.o + ((size_t)sg.t * p.M + sg.row0 + tok_i + tok) * (size_t)(p.nq * DH) + (size_t)(sg.kvh * G + r % G) * DH + col, u);
     }
 }
 
@@ -688,13 +703,12 @@ pt_status launch_t(const ChunkP& p, float* scratch, cudaStream_t st) {
     }
     const int blocks = std::min(sms, kMaxBlocks);
     // no more than this can be asked of a launch: every block of rows with every key that the table can name
-    const double most = (double)p.T * p.nkv * ((double)p.M / (2 * tpt) + p.B + 1) * (kCostSeg + 1 + ((double)p.maxp * p.ps / 128 + 1) * kCost2);
+    const double most = (double)p.T * p.nkv * ((double)p.M / (2 * tpt) + p.B + 1) * (kSeg2 + 1 + ((double)p.maxp * p.ps / 128 + 1) * kCost2);
     int sh = 0;
     while (most / (double)(1ll << sh) + (double)p.T * p.nkv * ((double)p.M / (2 * tpt) + p.B + 1) > 1e9 && sh < 20) ++sh;
     if (most / (double)(1ll << sh) > 1e9) { set_error("chunk attention: too many sequences, rows or pages for one call"); return PT_ERR_UNSUPPORTED; }
-    k_chunk_tc<DH><<<blocks, kChunkThreads, ChunkCfg<DH>::SMEM, st>>>(qmap, kvmap, p, scratch, tpt, (uint32_t)(128 * ChunkCfg<DH>::HALVES * G * box), kv_box, sh);
+    cudaError_t e = launch_dependent(k_chunk_tc<DH>, dim3(blocks), dim3(kChunkThreads), (size_t)ChunkCfg<DH>::SMEM, st, qmap, kvmap, p, scratch, tpt, (uint32_t)(128 * ChunkCfg<DH>::HALVES * G * box), kv_box, sh);
     g_launches.fetch_add(1, std::memory_order_relaxed);
-    cudaError_t e = cudaGetLastError();
     if (e == cudaSuccess && blocks > 1) {
         e = launch_dependent(k_chunk_combine<DH>, dim3(blocks - 1, 8), dim3(kCombineThreads), (size_t)0, st, p, scratch, tpt, blocks, sh);
         g_launches.fetch_add(1, std::memory_order_relaxed);

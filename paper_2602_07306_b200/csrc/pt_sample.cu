@@ -202,24 +202,39 @@ k_sample(const SampleP p, const int slice) {
     }
     __syncthreads();
     bool pos_inf = false;                                     // the row's maximum is +inf: 0 in its places, -inf elsewhere
-    auto fetch = [&](int v) {                                 // quad v from global memory
+    auto flat = [](float x) { return x == INFINITY ? 0.f : -INFINITY; };
+    auto flat4 = [&](float4 q) { return pos_inf ? make_float4(flat(q.x), flat(q.y), flat(q.z), flat(q.w)) : q; };
+    // f(v, quad v) for the quads [a, b) that this thread sees, `stride` apart: from global memory, the full ones first
+    auto from_global = [&](int a, int b, int at, int stride, auto&& f) {
+        const int lo = max(a, full0), hi = min(b, full1);
+#pragma unroll 8
+        for (int v = lo + at; v < hi; v += stride) f(v, flat4(load4(quad0 + v * 4)));
+        if (at == 0) {
+#pragma unroll 1
+            for (int k = 0; k < 2; ++k) {
+                const int v = k ? quads - 1 : 0;
+                if (v >= a && v < b && (v < full0 || v >= full1) && !(k && quads == 1)) f(v, flat4(sh.edge[k]));
+            }
+        }
+    };
+    // the same for the warp's part, from wherever the row is held
+    auto each = [&](auto&& f) {
+        if (SLICES) {
+#pragma unroll 4
+            for (int v = v0 + lane; v < v1; v += 32) f(v, xs[v]);
+        } else from_global(v0, v1, lane, 32, f);
+    };
+    auto get = [&](int v) {                                   // one quad, wherever the row is held
+        if (SLICES) return xs[v];
         float4 q = sh.edge[v == 0 ? 0 : 1];
         if (v >= full0 && v < full1) q = load4(quad0 + v * 4);
-        return q;
-    };
-    auto get = [&](int v) {
-        if (SLICES) return xs[v];
-        float4 q = fetch(v);
-        if (pos_inf) q = make_float4(q.x == INFINITY ? 0.f : -INFINITY, q.y == INFINITY ? 0.f : -INFINITY, q.z == INFINITY ? 0.f : -INFINITY, q.w == INFINITY ? 0.f : -INFINITY);
-        return q;
+        return flat4(q);
     };
     float4 tmax = make_float4(-INFINITY, -INFINITY, -INFINITY, -INFINITY);
-#pragma unroll 8
-    for (int v = v0 + lane; v < v1; v += 32) {
-        const float4 q = fetch(v);
+    from_global(v0, v1, lane, 32, [&](int v, float4 q) {
         if (SLICES) xs[v] = q;
         tmax = make_float4(fmaxf(tmax.x, q.x), fmaxf(tmax.y, q.y), fmaxf(tmax.z, q.z), fmaxf(tmax.w, q.w));
-    }
+    });
     {
         float m = fmaxf(fmaxf(tmax.x, tmax.y), fmaxf(tmax.z, tmax.w));
 #pragma unroll
@@ -265,9 +280,8 @@ k_sample(const SampleP p, const int slice) {
     }
     if (r.max == INFINITY) {                                  // +inf shares the whole weight: the same row with 0 and -inf
         pos_inf = true;
-        auto flat = [](float x) { return x == INFINITY ? 0.f : -INFINITY; };
         if (SLICES)
-            for (int v = v0 + lane; v < v1; v += 32) { const float4 q = xs[v]; xs[v] = make_float4(flat(q.x), flat(q.y), flat(q.z), flat(q.w)); }
+            for (int v = v0 + lane; v < v1; v += 32) xs[v] = flat4(xs[v]);
         tmax = make_float4(flat(tmax.x), flat(tmax.y), flat(tmax.z), flat(tmax.w));
         r.max = 0.f;
     }
@@ -341,15 +355,13 @@ k_sample(const SampleP p, const int slice) {
             }
         }
         if (!use_p && r.x_min > tau) tau = r.x_min;
-#pragma unroll 8
-        for (int v = v0 + lane; v < v1; v += 32) {
-            const float4 q = get(v);
+        each([&](int v, float4 q) {
             if (fmaxf(fmaxf(q.x, q.y), fmaxf(q.z, q.w)) >= tau) {
                 const float e[4] = {q.x, q.y, q.z, q.w};
 #pragma unroll
                 for (int c = 0; c < 4; ++c) if (e[c] >= tau && e[c] > -INFINITY) entry(e[c], base + v * 4 + c);
             }
-        }
+        });
         const int n = gather();
         sync_row();                                           // everybody has read it: from here the first block needs no other
         if (n <= kList) {
@@ -425,9 +437,7 @@ k_sample(const SampleP p, const int slice) {
     auto weigh = [&](bool sum_all, u64& above, u64& whole, auto&& inside) {
         const float fa = (float)za, fb = (float)(zb + 1), stop = sum_all ? (float)(kBins - 1) : fa;
         above = whole = ws = 0;
-#pragma unroll 2
-        for (int v = v0 + lane; v < v1; v += 32) {
-            const float4 q = get(v);
+        each([&](int v, float4 q) {
             const float e[4] = {q.x, q.y, q.z, q.w};
             const float d[4] = {(r.max - q.x) * r.inv_bin, (r.max - q.y) * r.inv_bin, (r.max - q.z) * r.inv_bin, (r.max - q.w) * r.inv_bin};
             const float dm = fminf(fminf(d[0], d[1]), fminf(d[2], d[3]));
@@ -442,7 +452,7 @@ k_sample(const SampleP p, const int slice) {
             if (dm < fb)
 #pragma unroll
                 for (int c = 0; c < 4; ++c) if (d[c] >= fa && d[c] < fb) inside(e[c], base + v * 4 + c);
-        }
+        });
         ws = warp_sum(ws);
         above = warp_sum(above); whole = warp_sum(whole);
         if (lane == 0) { sh.warp_tmp[warp] = above; sh.warp_tmp2[warp] = whole; }
@@ -458,13 +468,11 @@ k_sample(const SampleP p, const int slice) {
     if (use_k || use_p) {
         for (int i = tid; i < kBins / 4; i += kThreads) reinterpret_cast<uint4*>(sh.bins)[i] = make_uint4(0, 0, 0, 0);
         __syncthreads();
-#pragma unroll 4
-        for (int v = v0 + lane; v < v1; v += 32) {
-            const float4 q = get(v);
+        each([&](int, float4 q) {
             const float d[4] = {(r.max - q.x) * r.inv_bin, (r.max - q.y) * r.inv_bin, (r.max - q.z) * r.inv_bin, (r.max - q.w) * r.inv_bin};
 #pragma unroll
             for (int c = 0; c < 4; ++c) if (d[c] < (float)(kBins - 1)) atomicAdd(&sh.bins[(int)d[c]], 1u);
-        }
+        });
         sync_row();
         // every block sums its share of the bins over the blocks: PER of them a thread.  An element of bin b weighs between
         // e^-(b + 1)d and e^-bd (a hundredth of a bin more on either side for the rounding of its number).
@@ -737,8 +745,8 @@ k_sample(const SampleP p, const int slice) {
     if (sh.owner < 0) return;
     thr = sh.thr; cut = sh.cut;
     const u64 target = sh.target;
-    const int r0 = min(quads, sh.owner * per_warp), r1 = min(quads, r0 + per_warp), each = (r1 - r0 + kThreads - 1) / kThreads;
-    const int q0 = min(r1, r0 + tid * each), q1 = min(r1, q0 + each);      // consecutive quads of this thread
+    const int r0 = min(quads, sh.owner * per_warp), r1 = min(quads, r0 + per_warp), share = (r1 - r0 + kThreads - 1) / kThreads;
+    const int q0 = min(r1, r0 + tid * share), q1 = min(r1, q0 + share);      // consecutive quads of this thread
     u64 mine = 0, tot;
     for (int v = q0; v < q1; ++v) {
         const float4 q = get(v);

@@ -135,7 +135,7 @@ def test_chunk_attention_refusals(lib):
     for bad in (dict(T=0), dict(B=0), dict(M=0), dict(nq=0), dict(nkv=0), dict(nkv=3), dict(maxp=0), dict(pages=0), dict(ps=12), dict(ps=72), dict(impl=2), dict(stride=-8)):
         assert go(**bad) == 1, bad
     assert go(dh=96) == 3 and go(nq=18) == 3 and go(dh=32) == 3 and go(ps=24) == 3
-    assert go(q=C.c_void_p(0x10008)) == 6 and go(out=C.c_void_p(0x10008)) == 6 and go(pool=C.c_void_p(0x10008)) == 6 and go(stride=(1 << 20) + 4) == 6 and go(scratch=C.c_void_p(0x10080)) == 6
+    assert go(q=C.c_void_p(0x10008)) == 6 and go(out=C.c_void_p(0x10010)) == 6 and go(pool=C.c_void_p(0x10008)) == 6 and go(stride=(1 << 20) + 4) == 6 and go(scratch=C.c_void_p(0x10080)) == 6
     assert go(sb=n.value - 1) == 4
 
 
