@@ -45,6 +45,8 @@ constexpr int kFine = 2048;                    // later histograms: keys
 constexpr int kCoarse = kThreads;              // histogram of the threads' maxima
 constexpr int kList = 2048;                    // entries one block sorts
 constexpr int kListK = 1024;                   // largest top-k that goes that way
+constexpr int kBatch = 4;                      // quads a thread loads before it looks at them
+constexpr int kFew = 256;                      // entries that are ranked by counting, not sorted
 constexpr int kFracBits = 44;
 constexpr float kRange = 31.5f;                // nats below the maximum that the bins cover; beyond it weights are zero
 constexpr float kSlack = 4e-7f;                // relative rounding of a distance and its bin number, three times over
@@ -97,7 +99,11 @@ struct Shared {
         struct { u64 mass[kFine]; uint32_t hist[kFine]; };      // narrowing by keys
         struct { u64 all[kList], list[kList]; };                // entries of the row (in the first block), of this block
     };
-    uint32_t coarse[kCoarse];
+    union {
+        uint32_t coarse[kCoarse];
+        struct { uint32_t rank[kFew]; };
+    };
+    u64 few_w[kFew], few_sum[kFew], few_total[2];
     float red[kWarps];
     u64 wsum[kMaxCluster * kWarps];            // first block: weight kept by the part of every warp of the cluster
     u64 warp_tmp[kWarps], warp_tmp2[kWarps];
@@ -190,6 +196,11 @@ k_sample(const SampleP p, const int slice) {
     const E* quad0 = src - shift;
     const int full0 = shift ? 1 : 0, full1 = (count + shift) >> 2;     // quads [full0, full1) lie inside the row
 
+    // the row's settings, early: their latency hides behind the logits'
+    float temperature = p.temperature ? p.temperature[row] : 1.0f;
+    const float tp = p.top_p ? p.top_p[row] : 1.0f, mp = p.min_p ? p.min_p[row] : 0.f, u = p.u[row];
+    const int k = tp <= 0.f ? 1 : p.top_k ? p.top_k[row] : 0; // a reach of nothing keeps one token
+
     // ---- the slice (NaN counts as masked) and its maximum
     sh.coarse[tid] = 0;
     if (tid == 0) { sh.n_list = 0; sh.n_all = 0; sh.first = 0x7fffffff; }
@@ -207,8 +218,16 @@ k_sample(const SampleP p, const int slice) {
     // f(v, quad v) for the quads [a, b) that this thread sees, `stride` apart: from global memory, the full ones first
     auto from_global = [&](int a, int b, int at, int stride, auto&& f) {
         const int lo = max(a, full0), hi = min(b, full1);
-#pragma unroll 8
-        for (int v = lo + at; v < hi; v += stride) f(v, flat4(load4(quad0 + v * 4)));
+        int v = lo + at;
+        for (; v + (kBatch - 1) * stride < hi; v += kBatch * stride) {       // the loads first: f may write to shared memory
+            float4 q[kBatch];
+#pragma unroll
+            for (int i = 0; i < kBatch; ++i) q[i] = load4(quad0 + (v + i * stride) * 4);
+#pragma unroll
+            for (int i = 0; i < kBatch; ++i) f(v + i * stride, flat4(q[i]));
+        }
+#pragma unroll 1
+        for (; v < hi; v += stride) f(v, flat4(load4(quad0 + v * 4)));
         if (at == 0) {
 #pragma unroll 1
             for (int k = 0; k < 2; ++k) {
@@ -254,7 +273,6 @@ k_sample(const SampleP p, const int slice) {
         for (int o = kMaxCluster / 2; o; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
         r.max = __shfl_sync(0xffffffffu, m, 0);
     }
-    float temperature = p.temperature ? p.temperature[row] : 1.0f;
     const bool nothing = r.max == -INFINITY;                  // every logit masked: token 0, probability 0
     if (nothing || !(temperature > 0.f && temperature < INFINITY)) {
         // greedy: the lowest index of the maximum, in the parts of the threads that met it
@@ -290,15 +308,9 @@ k_sample(const SampleP p, const int slice) {
     r.inv_t = 1.4426950408889634 / (double)temperature;
     r.inv_bin = (float)(kBins - 1) / (kRange * temperature);
     r.x_min = -INFINITY;
-    if (p.min_p) {
-        const float mp = p.min_p[row];
-        if (mp > 0.f) r.x_min = mp >= 1.f ? r.max : __double2float_ru(r.maxd + (double)temperature * log((double)mp));
-    }
-    const float tp = p.top_p ? p.top_p[row] : 1.0f;
-    const int k = tp <= 0.f ? 1 : p.top_k ? p.top_k[row] : 0; // a reach of nothing keeps one token
+    if (mp > 0.f) r.x_min = mp >= 1.f ? r.max : __double2float_ru(r.maxd + (double)temperature * log((double)mp));
     const bool use_k = k > 0 && k < p.vocab, use_p = tp < 1.0f && tp > 0.f;
     const u64 frac64 = use_p ? (u64)__double2ull_rz((double)tp * 18446744073709551616.0) : 0ull;
-    const float u = p.u[row];
     const u64 U = u >= 1.f ? ~0ull : (u > 0.f ? (u64)__double2ull_rz((double)u * 18446744073709551616.0) : 0ull);
     auto store = [&](int tok, float x, u64 Z) {
         if (p.token) p.token[row] = tok;
@@ -330,6 +342,26 @@ k_sample(const SampleP p, const int slice) {
         for (int i = n + tid; i < size; i += kThreads) sh.all[i] = ~0ull;
         __syncthreads();
         sort_block(sh.all, size);
+    };
+
+    // Few entries (n <= kFew) are ranked by counting.  Thread (i, part) compares entry i with every parts-th entry: `rank` and
+    // few_sum get the number and the weight of the entries before it.  All threads call it; few_w holds the weights after.
+    const auto few = [&](int n, int& i, bool& mine) {
+        const int n2 = n <= 64 ? 64 : n <= 128 ? 128 : 256;
+        i = tid & (n2 - 1);
+        const int part = tid / n2;
+        mine = part == 0 && i < n;
+        if (tid < n2) { sh.rank[tid] = 0; sh.few_sum[tid] = 0; sh.few_w[tid] = tid < n ? weight(r, value_of((uint32_t)(sh.all[tid] >> 32))) : 0; }
+        if (tid < 2) sh.few_total[tid] = 0;
+        __syncthreads();
+        if (i < n) {
+            const u64 a = sh.all[i];
+            uint32_t before = 0; u64 sum = 0;
+            for (int j = part; j < n; j += kThreads / n2)
+                if (sh.all[j] < a) { ++before; sum += sh.few_w[j]; }
+            if (before) { atomicAdd(&sh.rank[i], before); atomicAdd(&sh.few_sum[i], sum); }
+        }
+        __syncthreads();
     };
 
     // ---- few candidates
@@ -366,6 +398,33 @@ k_sample(const SampleP p, const int slice) {
         sync_row();                                           // everybody has read it: from here the first block needs no other
         if (n <= kList) {
             if (rank != 0) return;
+            if (n <= kFew) {
+                int i; bool mine;
+                few(n, i, mine);
+                const u64 a = i < n ? sh.all[i] : 0, w = i < n ? sh.few_w[i] : 0;
+                const bool in_k = i < n && (!use_k || sh.rank[i] < (uint32_t)k);
+                u64 s = warp_sum(mine && in_k ? w : 0);
+                if (lane == 0 && s) atomicAdd(&sh.few_total[0], s);
+                __syncthreads();
+                // kept: entries whose predecessors' weight is below the reach
+                const bool in = in_k && (!use_p || sh.few_sum[i] < reach(sh.few_total[0])) && value_of((uint32_t)(a >> 32)) >= r.x_min;
+                s = warp_sum(mine && in ? w : 0);
+                if (lane == 0 && s) atomicAdd(&sh.few_total[1], s);
+                __syncthreads();
+                if (mine) { sh.few_sum[i] = 0; if (!in) sh.few_w[i] = 0; }
+                __syncthreads();
+                const u64 Z = sh.few_total[1], target = __umul64hi(Z, U);
+                const int n2 = n <= 64 ? 64 : n <= 128 ? 128 : 256;
+                if (in) {                                     // the kept weight in front of the entry, in index order
+                    u64 sum = 0;
+                    for (int j = tid / n2; j < n; j += kThreads / n2)
+                        if ((uint32_t)sh.all[j] < (uint32_t)a) sum += sh.few_w[j];
+                    if (sum) atomicAdd(&sh.few_sum[i], sum);
+                }
+                __syncthreads();
+                if (mine && in && sh.few_sum[i] <= target && sh.few_sum[i] + w > target) store((int)(uint32_t)a, value_of((uint32_t)(a >> 32)), Z);
+                return;
+            }
             sort_all(n);
             // four consecutive places a thread, in descending order of logits
             u64* wt = sh.list;
@@ -548,31 +607,40 @@ k_sample(const SampleP p, const int slice) {
         if (!searched) sync_row();
         by_keys = n > kList;
         if (!by_keys && searched && rank == 0) {
-            sort_all(n);
             const u64 above_mass = row_sum(&Shared::blk_mass);
             const u64 need = use_p ? reach(row_sum(&Shared::blk_all)) : 0;
-            u64 w4[4], mine = 0, tot;
-            uint32_t key4[4], idx4[4];
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const int i = tid * 4 + j;
-                const u64 a = i < n ? sh.all[i] : ~0ull;
-                key4[j] = (uint32_t)(a >> 32); idx4[j] = (uint32_t)a;
-                w4[j] = i < n ? weight(r, value_of(key4[j])) : 0;
-                mine += w4[j];
-            }
-            u64 cum = block_excl<u64>(mine, sh.scan, tot) + above_mass;
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const int i = tid * 4 + j;
-                const bool in = i < n && (use_p ? cum < need : above_cnt + i < (u64)k);
-                const bool last = in && (use_p ? cum + w4[j] >= need : above_cnt + i + 1 == (u64)k);
-                if (last) { sh.thr = key4[j]; sh.cut = (int)idx4[j]; }
-                cum += w4[j];
-                if (in && value_of(key4[j]) >= r.x_min) {     // into the sum of the warp that owns it
-                    const int q = (int)idx4[j] / slice, i2 = (int)idx4[j] - q * slice + shift;
+            // entry `place` of the zone, `cum` the weight before it: in front of the threshold, on it, or behind
+            auto decide = [&](u64 a, int place, u64 w, u64 cum) {
+                const bool in = use_p ? cum < need : above_cnt + place < (u64)k;
+                const bool last = in && (use_p ? cum + w >= need : above_cnt + place + 1 == (u64)k);
+                const uint32_t key = (uint32_t)(a >> 32);
+                const int idx = (int)(uint32_t)a;
+                if (last) { sh.thr = key; sh.cut = idx; }
+                if (in && value_of(key) >= r.x_min) {         // into the sum of the warp that owns it
+                    const int q = idx / slice, i2 = idx - q * slice + shift;
                     const int qc = min(slice, p.vocab - q * slice), pw = (((qc + shift + 3) >> 2) + kWarps - 1) / kWarps;
-                    atomicAdd(&sh.wsum[q * kWarps + (i2 >> 2) / pw], w4[j]);
+                    atomicAdd(&sh.wsum[q * kWarps + (i2 >> 2) / pw], w);
+                }
+            };
+            if (n <= kFew) {
+                int i; bool mine;
+                few(n, i, mine);
+                if (mine) decide(sh.all[i], (int)sh.rank[i], sh.few_w[i], sh.few_sum[i] + above_mass);
+            } else {
+                sort_all(n);
+                u64 w4[4], mine = 0, tot;
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const int i = tid * 4 + j;
+                    w4[j] = i < n ? weight(r, value_of((uint32_t)(sh.all[i] >> 32))) : 0;
+                    mine += w4[j];
+                }
+                u64 cum = block_excl<u64>(mine, sh.scan, tot) + above_mass;
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const int i = tid * 4 + j;
+                    if (i < n) decide(sh.all[i], i, w4[j], cum);
+                    cum += w4[j];
                 }
             }
             __syncthreads();
