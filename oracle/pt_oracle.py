@@ -404,8 +404,8 @@ def greedy(logits: np.ndarray) -> np.ndarray:
 def sample_kept(x: np.ndarray, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0):
     """One row of logits -> (kept token ids ascending, their weights, margin).  Weights are exp((x - max) / temperature);
     the filters apply in the order top-k, top-p, min-p, each to what the one before left (ties: the lower index first).
-    NaN and -inf are masked.  margin: how far, relative to the kept sum, the top-p and min-p decisions are from falling
-    the other way (inf without them)."""
+    NaN and -inf are masked.  margin: how far the top-p decision (relative to the sum it cuts) and the min-p decisions
+    (relative to min_p; they compare single weights, not sums) are from falling the other way; inf without them."""
     x = np.where(np.isnan(x), -np.inf, np.asarray(x, np.float64))
     m = x.max()
     if m == -np.inf:
@@ -424,7 +424,7 @@ def sample_kept(x: np.ndarray, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0):
         margin = min(margin, np.abs(c - top_p * c[-1]).min() / c[-1])
         order = order[:n]
     if min_p > 0:
-        margin = min(margin, np.abs(w[order][w[order] != 1] - min_p).min(initial=np.inf))
+        margin = min(margin, np.abs(w[order][w[order] != 1] / min_p - 1).min(initial=np.inf))
         order = order[(w[order] >= min_p) | (x[order] == m)]
     ids = np.sort(order)
     return ids, w[ids], margin

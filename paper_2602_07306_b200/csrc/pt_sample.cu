@@ -51,7 +51,6 @@ constexpr int kFracBits = 44;
 constexpr float kRange = 31.5f;                // nats below the maximum that the bins cover; beyond it weights are zero
 constexpr float kSlack = 4e-7f;                // relative rounding of a distance and its bin number, three times over
 constexpr int kMaxCluster = 8;
-constexpr int kRowsFrom = 48;                  // rows from which a block takes a whole row
 constexpr int kMaxSlice = 32768;               // elements of a slice: 128 KB
 constexpr int kMaxVocab = 393216;
 
@@ -67,30 +66,36 @@ __device__ __forceinline__ float value_of(uint32_t key) { return __uint_as_float
 struct Row {
     float max, inv_bin;                        // bin of x = (max - x) * inv_bin
     double maxd, inv_t;                        // inv_t: log2(e) / temperature
+    double inv16;                              // 16 inv_t
+    float x_zero;                              // weights are zero below it
     float x_min;                               // min-p: kept values are >= x_min
+    const double* root;                        // 2^(j / 16), in shared memory
 };
 
-// w(x) * 2^44, rounded to the nearest whole number: 2^y with y = (x - max) log2(e) / temperature split into a whole number n
-// and f in [-1/2, 1/2]; 2^f by the polynomial of degree 9 that agrees with it at the ten Chebyshev nodes of the interval
-// (relative error 1.4e-14, a quarter of the last place kept of the largest weight); n goes into the exponent, and adding
-// 2^52 rounds to a whole number.
+__constant__ double kRoot[16] = {1, 1.0442737824274138, 1.0905077326652577, 1.1387886347566916,
+                                  1.189207115002721, 1.241857812073484, 1.2968395546510096, 1.3542555469368927,
+                                  1.4142135623730951, 1.4768261459394993, 1.5422108254079407, 1.6104903319492543,
+                                  1.681792830507429, 1.7562521603732995, 1.8340080864093424, 1.9152065613971474};
+
+// w(x) * 2^44, rounded to the nearest whole number: 2^y with 16 y = 16 (x - max) log2(e) / temperature split into a whole
+// number k and g in [-1/2, 1/2]; 2^(g / 16) by the polynomial of degree 5 that agrees with it at the six Chebyshev nodes of
+// the interval (relative error 4.6e-15, a twelfth of the last place kept of the largest weight), 2^(k / 16) from a table
+// of sixteen and the exponent; adding 2^52 rounds to a whole number.  Below x_zero the rounding gives 0.
 __device__ __forceinline__ u64 weight(const Row& r, float x) {
-    const double y = ((double)x - r.maxd) * r.inv_t;
-    const double magic = 6755399441055744.0;   // 1.5 * 2^52: the sum's low word is round(y)
-    const double k = y + magic;
-    const double f = y - (k - magic);
-    double p = 1.0205905413765595e-07;
-    p = fma(p, f, 1.325964524488711e-06);
-    p = fma(p, f, 1.5252672924850737e-05);
-    p = fma(p, f, 0.0001540343375125101);
-    p = fma(p, f, 0.0013333558200794592);
-    p = fma(p, f, 0.009618129193934313);
-    p = fma(p, f, 0.05550410866465167);
-    p = fma(p, f, 0.2402265069564034);
-    p = fma(p, f, 0.6931471805599462);
-    p = fma(p, f, 1.0000000000000135);
-    const double w = __hiloint2double(__double2hiint(p) + ((__double2loint(k) + kFracBits) << 20), __double2loint(p)) + 4503599627370496.0;
-    return y > -46.0 ? (u64)__double_as_longlong(w) & 0xfffffffffffffull : 0ull;      // also 0 for a masked x
+    const double d = (double)x - r.maxd;
+    const double magic = 6755399441055744.0;   // 1.5 * 2^52: the sum's low word is round(16 y)
+    const double k = fma(d, r.inv16, magic);
+    const double g = fma(d, r.inv16, -(k - magic));
+    double p = 1.2716085030349987e-09;
+    p = fma(p, g, 1.467644462189871e-07);
+    p = fma(p, g, 1.355080777749983e-05);
+    p = fma(p, g, 0.000938384792486206);
+    p = fma(p, g, 0.04332169878499661);
+    p = fma(p, g, 1.0000000000000044);
+    const int ki = __double2loint(k);
+    p *= r.root[ki & 15];
+    const double w = __hiloint2double(__double2hiint(p) + (((ki >> 4) + kFracBits) << 20), __double2loint(p)) + 4503599627370496.0;
+    return x >= r.x_zero ? (u64)__double_as_longlong(w) & 0xfffffffffffffull : 0ull;
 }
 
 struct Shared {
@@ -111,6 +116,7 @@ struct Shared {
     u64 blk_mass, blk_all;                     // weight of this block's elements above the searched bins, and of all
     u64 scan[kWarps + 1];
     double dscan[kWarps + 1];
+    double root[16];
     double share[3];                           // totals of this block's share of the bins: counts, upper and lower bounds
     float4 edge[2];                            // ROWS: the quads that the row does not fill
     float max;
@@ -203,6 +209,7 @@ k_sample(const SampleP p, const int slice) {
 
     // ---- the slice (NaN counts as masked) and its maximum
     sh.coarse[tid] = 0;
+    if (tid < 16) sh.root[tid] = kRoot[tid];
     if (tid == 0) { sh.n_list = 0; sh.n_all = 0; sh.first = 0x7fffffff; }
     if (tid < 2) {                                            // the quads at the ends: filled up with -inf
         const int v = tid ? quads - 1 : 0;
@@ -250,10 +257,19 @@ k_sample(const SampleP p, const int slice) {
         return flat4(q);
     };
     float4 tmax = make_float4(-INFINITY, -INFINITY, -INFINITY, -INFINITY);
-    from_global(v0, v1, lane, 32, [&](int v, float4 q) {
-        if (SLICES) xs[v] = q;
-        tmax = make_float4(fmaxf(tmax.x, q.x), fmaxf(tmax.y, q.y), fmaxf(tmax.z, q.z), fmaxf(tmax.w, q.w));
-    });
+    const bool choose = !(temperature > 0.f && temperature < INFINITY);      // greedy
+    int top = -1;                                             // greedy: the first of this thread's quads that holds its maximum
+    if (choose) {
+        from_global(v0, v1, lane, 32, [&](int v, float4 q) {
+            const float m = fmaxf(fmaxf(q.x, q.y), fmaxf(q.z, q.w));
+            if (m > tmax.x || (m == tmax.x && v < top)) { tmax.x = m; top = v; }
+        });
+    } else {
+        from_global(v0, v1, lane, 32, [&](int v, float4 q) {
+            if (SLICES) xs[v] = q;
+            tmax = make_float4(fmaxf(tmax.x, q.x), fmaxf(tmax.y, q.y), fmaxf(tmax.z, q.z), fmaxf(tmax.w, q.w));
+        });
+    }
     {
         float m = fmaxf(fmaxf(tmax.x, tmax.y), fmaxf(tmax.z, tmax.w));
 #pragma unroll
@@ -274,14 +290,12 @@ k_sample(const SampleP p, const int slice) {
         r.max = __shfl_sync(0xffffffffu, m, 0);
     }
     const bool nothing = r.max == -INFINITY;                  // every logit masked: token 0, probability 0
-    if (nothing || !(temperature > 0.f && temperature < INFINITY)) {
-        // greedy: the lowest index of the maximum, in the parts of the threads that met it
-        if (!nothing && fmaxf(fmaxf(tmax.x, tmax.y), fmaxf(tmax.z, tmax.w)) == r.max) {
-            for (int v = v0 + lane; v < v1; v += 32) {
-                const float4 q = get(v);
-                const int i = q.x == r.max ? 0 : q.y == r.max ? 1 : q.z == r.max ? 2 : q.w == r.max ? 3 : -1;
-                if (i >= 0) { atomicMin(&sh.first, base + v * 4 + i); break; }
-            }
+    if (nothing || choose) {
+        // greedy: the lowest index of the maximum
+        if (choose && !nothing && tmax.x == r.max) {
+            float4 q = sh.edge[top == 0 ? 0 : 1];
+            if (top >= full0 && top < full1) q = load4(quad0 + top * 4);
+            atomicMin(&sh.first, base + top * 4 + (q.x == r.max ? 0 : q.y == r.max ? 1 : q.z == r.max ? 2 : 3));
         }
         sync_row();
         if (rank == 0 && warp == 0) {
@@ -306,6 +320,9 @@ k_sample(const SampleP p, const int slice) {
     temperature = fminf(fmaxf(temperature, 1e-30f), 1e36f);   // so that bin widths are finite and not zero
     r.maxd = (double)r.max;
     r.inv_t = 1.4426950408889634 / (double)temperature;
+    r.inv16 = 16.0 * r.inv_t;
+    r.x_zero = fmaxf(r.max - 31.538f * temperature, -3.4028235e38f);      // 2^-45.5 of the largest; -inf is below it
+    r.root = sh.root;
     r.inv_bin = (float)(kBins - 1) / (kRange * temperature);
     r.x_min = -INFINITY;
     if (mp > 0.f) r.x_min = mp >= 1.f ? r.max : __double2float_ru(r.maxd + (double)temperature * log((double)mp));
@@ -495,6 +512,7 @@ k_sample(const SampleP p, const int slice) {
     // the elements of bins [za, zb].  No branch around the polynomials, four at a time: their chain is long.
     auto weigh = [&](bool sum_all, u64& above, u64& whole, auto&& inside) {
         const float fa = (float)za, fb = (float)(zb + 1), stop = sum_all ? (float)(kBins - 1) : fa;
+        const bool with_min = r.x_min > -INFINITY;
         above = whole = ws = 0;
         each([&](int v, float4 q) {
             const float e[4] = {q.x, q.y, q.z, q.w};
@@ -505,13 +523,14 @@ k_sample(const SampleP p, const int slice) {
                 for (int c = 0; c < 4; ++c) {
                     const u64 w = weight(r, e[c]);
                     whole += w;
-                    if (d[c] < fa) { above += w; if (e[c] >= r.x_min) ws += w; }
+                    if (d[c] < fa) { above += w; if (with_min && e[c] >= r.x_min) ws += w; }
                 }
             }
             if (dm < fb)
 #pragma unroll
                 for (int c = 0; c < 4; ++c) if (d[c] >= fa && d[c] < fb) inside(e[c], base + v * 4 + c);
         });
+        if (!with_min) ws = above;
         ws = warp_sum(ws);
         above = warp_sum(above); whole = warp_sum(whole);
         if (lane == 0) { sh.warp_tmp[warp] = above; sh.warp_tmp2[warp] = whole; }
@@ -861,11 +880,15 @@ pt_status launch_kind(const SampleP& p, int64_t n, int cl, cudaStream_t st) {
 
 template <class E>
 pt_status launch_t(const SampleP& p, int64_t n, cudaStream_t st) {
-    if (n >= kRowsFrom || p.vocab > kMaxCluster * kMaxSlice) return launch_kind<E, false>(p, n, 1, st);
+    // SLICES while a block per 4096 logits, up to 8 a row, leaves every SM with two blocks at most.  Measured with top-k 50 /
+    // top-p 0.9 in us, SLICES against ROWS: 32 x 32000 12.1 / 30.8 against 12.5 / 35.7, 64 x 32000 13.5 / 38 against 12.7 / 35;
+    // 32 x 128000 16.5 / 52 against 18.7 / 94, 48 x 128000 27 / 93 against 18.9 / 94.
+    int cl = 1;
+    while (cl < kMaxCluster && (int64_t)cl * 4096 < p.vocab) cl *= 2;
+    if (n * cl > 2 * 148 || p.vocab > kMaxCluster * kMaxSlice) return launch_kind<E, false>(p, n, 1, st);
     // slices of at most 16384 logits (64 KB: two blocks per SM); while a launch leaves SMs idle a row is spread further,
     // down to slices of 2048
-    int cl = 1;
-    while (cl < kMaxCluster && ((p.vocab + cl - 1) / cl > 16384 || (n * cl * 2 <= 148 && (p.vocab + cl - 1) / cl > 2048))) cl *= 2;
+    for (cl = 1; cl < kMaxCluster && ((p.vocab + cl - 1) / cl > 16384 || (n * cl * 2 <= 148 && (p.vocab + cl - 1) / cl > 2048));) cl *= 2;
     return launch_kind<E, true>(p, n, cl, st);
 }
 

@@ -3,9 +3,9 @@
 tell apart.
 
 How close is that?  A weight is held to 2^-45 of the largest (rounded to a multiple of 2^-44) and computed in double, so a
-sum of n weights is off by at most n 2^-45 (1 + small) and the kept sum is at least 1: a relative 2^-45 n, 1.2e-8 at the
-largest vocabulary here.  Both sides of a decision carry it: MARGIN = 2 n 2^-45 + 1e-13 for the double arithmetic of either
-side.  Inputs are drawn so that hardly any row is closer (the share skipped is checked)."""
+sum of n weights is off by at most n 2^-45 (1 + small): relative to the kept sum Z, n 2^-45 / Z.  Both sides of a decision
+carry it: 2 n 2^-45 / Z + 1e-13 for the double arithmetic of either side.  Inputs are drawn so that hardly any row is closer
+(the share skipped is checked)."""
 import numpy as np
 import pytest
 
@@ -40,7 +40,6 @@ def run(x, u, bf16=False, pad=0, **f):
 def check(x, u, bf16=False, pad=0, most_skipped=0.02, **f):
     n, V = x.shape
     tok, prob = run(x, u, bf16, pad, **f)
-    margin_ok = 2 * V * 2.0 ** -45 + 1e-13
     skipped = 0
     for r in range(n):
         g = {}
@@ -48,7 +47,8 @@ def check(x, u, bf16=False, pad=0, most_skipped=0.02, **f):
             if f.get(k) is not None:
                 g[k] = np.broadcast_to(np.asarray(f[k], dt), (n,))[r].astype(np.float64 if dt is np.float32 else np.int64)
         want, p, margin = O.sample(x[r].astype(np.float64), float(np.float32(u[r])), **g)
-        if margin < margin_ok:
+        Z = O.sample_kept(x[r].astype(np.float64), **g)[1].sum() or 1.0
+        if margin < 2 * V * 2.0 ** -45 / Z + 1e-13:
             skipped += 1
             continue
         assert tok[r] == want, (r, tok[r], want, margin, g)
@@ -82,6 +82,17 @@ def test_rows_with_their_own_settings(bf16, scale):
     pick = lambda a: rng.choice(a, n)
     check(x, rng.random(n), bf16=bf16, pad=5, temperature=pick([0.0, 0.2, 1.0, 1.7]), top_k=pick([0, 1, 2, 37, 5000, 20010]),
           top_p=pick([1.0, 0.3, 0.9, 0.999]), min_p=pick([0.0, 0.01, 0.5]))
+
+
+@pytest.mark.parametrize("n,V", [(3, 50001), (40, 70003), (300, 4099), (2, 300007)])
+@pytest.mark.parametrize("f", [dict(top_k=5000, top_p=0.9), dict(top_k=3000, temperature=1.4), dict(top_p=0.5), dict(top_p=0.9999, min_p=1e-4), dict(top_p=1e-7), dict(top_k=700, min_p=0.02),
+                               dict(temperature=3.0), dict(top_p=1 - 2.0 ** -24)], ids=str)
+def test_long_selections_in_few_and_in_many_rows(n, V, f):
+    """A large top-k with and without top-p behind it, reaches close to 0 and 1, both ways of holding a row, odd strides."""
+    rng = np.random.default_rng(n + V)
+    x = (rng.standard_normal((n, V)) * 2).astype(np.float32)
+    x[:, rng.integers(0, V, V // 5)] = -np.inf
+    check(x, rng.random(n), pad=3, most_skipped=0.05, **f)
 
 
 def test_every_kept_token_is_reached_and_no_other():
