@@ -46,7 +46,7 @@ constexpr int kCoarse = kThreads;              // histogram of the threads' maxi
 constexpr int kList = 2048;                    // entries one block sorts
 constexpr int kListK = 1024;                   // largest top-k that goes that way
 constexpr int kBatch = 4;                      // quads a thread loads before it looks at them
-constexpr int kFew = 256;                      // entries that are ranked by counting, not sorted
+constexpr int kFew = 512;                      // entries that are ranked by counting, not sorted
 constexpr int kFracBits = 44;
 constexpr float kRange = 31.5f;                // nats below the maximum that the bins cover; beyond it weights are zero
 constexpr float kSlack = 4e-7f;                // relative rounding of a distance and its bin number, three times over
@@ -69,7 +69,7 @@ struct Row {
     double inv16;                              // 16 inv_t
     float x_zero;                              // weights are zero below it
     float x_min;                               // min-p: kept values are >= x_min
-    const double* root;                        // 2^(j / 16), in shared memory
+    const double* root;                        // 2^(44 + j / 16), in shared memory
 };
 
 __constant__ double kRoot[16] = {1, 1.0442737824274138, 1.0905077326652577, 1.1387886347566916,
@@ -77,12 +77,16 @@ __constant__ double kRoot[16] = {1, 1.0442737824274138, 1.0905077326652577, 1.13
                                   1.4142135623730951, 1.4768261459394993, 1.5422108254079407, 1.6104903319492543,
                                   1.681792830507429, 1.7562521603732995, 1.8340080864093424, 1.9152065613971474};
 
-// w(x) * 2^44, rounded to the nearest whole number: 2^y with 16 y = 16 (x - max) log2(e) / temperature split into a whole
-// number k and g in [-1/2, 1/2]; 2^(g / 16) by the polynomial of degree 5 that agrees with it at the six Chebyshev nodes of
-// the interval (relative error 4.6e-15, a twelfth of the last place kept of the largest weight), 2^(k / 16) from a table
-// of sixteen and the exponent; adding 2^52 rounds to a whole number.  Below x_zero the rounding gives 0.
-__device__ __forceinline__ u64 weight(const Row& r, float x) {
-    const double d = (double)x - r.maxd;
+// w(x) * 2^44, rounded to the nearest whole number, as the low 52 bits of a double in [2^52, 2^53): 2^y with 16 y =
+// 16 (x - max) log2(e) / temperature split into a whole number k and g in [-1/2, 1/2]; 2^(g / 16) by the polynomial of
+// degree 5 that agrees with it at the six Chebyshev nodes of the interval (relative error 4.6e-15, a twelfth of the last
+// place kept of the largest weight), 2^(44 + k / 16) from a table of sixteen and the exponent; adding 2^52 rounds to a whole
+// number.  Logits below x_zero, where that gives 0, count as x_zero.  The loops are bound by the instructions they issue
+// (70 a logit with the bits masked, compared and selected; the double-precision pipe was 19 % busy), so sums add the doubles'
+// bits as they are and take kOffset off per term.
+constexpr u64 kOffset = 0x4330000000000000ull;
+__device__ __forceinline__ u64 weight_bits(const Row& r, float x) {
+    const double d = (double)fmaxf(x, r.x_zero) - r.maxd;
     const double magic = 6755399441055744.0;   // 1.5 * 2^52: the sum's low word is round(16 y)
     const double k = fma(d, r.inv16, magic);
     const double g = fma(d, r.inv16, -(k - magic));
@@ -94,9 +98,9 @@ __device__ __forceinline__ u64 weight(const Row& r, float x) {
     p = fma(p, g, 1.0000000000000044);
     const int ki = __double2loint(k);
     p *= r.root[ki & 15];
-    const double w = __hiloint2double(__double2hiint(p) + (((ki >> 4) + kFracBits) << 20), __double2loint(p)) + 4503599627370496.0;
-    return x >= r.x_zero ? (u64)__double_as_longlong(w) & 0xfffffffffffffull : 0ull;
+    return (u64)__double_as_longlong(__hiloint2double(__double2hiint(p) + (ki & ~15) * 65536, __double2loint(p)) + 4503599627370496.0);
 }
+__device__ __forceinline__ u64 weight(const Row& r, float x) { return weight_bits(r, x) - kOffset; }
 
 struct Shared {
     union {
@@ -209,7 +213,7 @@ k_sample(const SampleP p, const int slice) {
 
     // ---- the slice (NaN counts as masked) and its maximum
     sh.coarse[tid] = 0;
-    if (tid < 16) sh.root[tid] = kRoot[tid];
+    if (tid < 16) sh.root[tid] = kRoot[tid] * 17592186044416.0;     // 2^44
     if (tid == 0) { sh.n_list = 0; sh.n_all = 0; sh.first = 0x7fffffff; }
     if (tid < 2) {                                            // the quads at the ends: filled up with -inf
         const int v = tid ? quads - 1 : 0;
@@ -219,9 +223,6 @@ k_sample(const SampleP p, const int slice) {
         sh.edge[tid] = make_float4(e[0], e[1], e[2], e[3]);
     }
     __syncthreads();
-    bool pos_inf = false;                                     // the row's maximum is +inf: 0 in its places, -inf elsewhere
-    auto flat = [](float x) { return x == INFINITY ? 0.f : -INFINITY; };
-    auto flat4 = [&](float4 q) { return pos_inf ? make_float4(flat(q.x), flat(q.y), flat(q.z), flat(q.w)) : q; };
     // f(v, quad v) for the quads [a, b) that this thread sees, `stride` apart: from global memory, the full ones first
     auto from_global = [&](int a, int b, int at, int stride, auto&& f) {
         const int lo = max(a, full0), hi = min(b, full1);
@@ -231,15 +232,15 @@ k_sample(const SampleP p, const int slice) {
 #pragma unroll
             for (int i = 0; i < kBatch; ++i) q[i] = load4(quad0 + (v + i * stride) * 4);
 #pragma unroll
-            for (int i = 0; i < kBatch; ++i) f(v + i * stride, flat4(q[i]));
+            for (int i = 0; i < kBatch; ++i) f(v + i * stride, q[i]);
         }
 #pragma unroll 1
-        for (; v < hi; v += stride) f(v, flat4(load4(quad0 + v * 4)));
+        for (; v < hi; v += stride) f(v, load4(quad0 + v * 4));
         if (at == 0) {
 #pragma unroll 1
             for (int k = 0; k < 2; ++k) {
                 const int v = k ? quads - 1 : 0;
-                if (v >= a && v < b && (v < full0 || v >= full1) && !(k && quads == 1)) f(v, flat4(sh.edge[k]));
+                if (v >= a && v < b && (v < full0 || v >= full1) && !(k && quads == 1)) f(v, sh.edge[k]);
             }
         }
     };
@@ -254,7 +255,7 @@ k_sample(const SampleP p, const int slice) {
         if (SLICES) return xs[v];
         float4 q = sh.edge[v == 0 ? 0 : 1];
         if (v >= full0 && v < full1) q = load4(quad0 + v * 4);
-        return flat4(q);
+        return q;
     };
     float4 tmax = make_float4(-INFINITY, -INFINITY, -INFINITY, -INFINITY);
     const bool choose = !(temperature > 0.f && temperature < INFINITY);      // greedy
@@ -310,18 +311,15 @@ k_sample(const SampleP p, const int slice) {
         sync_row();                                           // no block leaves while another still reads its shared memory
         return;
     }
-    if (r.max == INFINITY) {                                  // +inf shares the whole weight: the same row with 0 and -inf
-        pos_inf = true;
-        if (SLICES)
-            for (int v = v0 + lane; v < v1; v += 32) xs[v] = flat4(xs[v]);
-        tmax = make_float4(flat(tmax.x), flat(tmax.y), flat(tmax.z), flat(tmax.w));
-        r.max = 0.f;
-    }
-    temperature = fminf(fmaxf(temperature, 1e-30f), 1e36f);   // so that bin widths are finite and not zero
+    // so that bin widths are finite and not zero, a step of the logits below the maximum is no more than 600 temperatures (its
+    // weight is zero either way) and x_zero is a number
+    temperature = fminf(fmaxf(temperature, 1e-30f), 1e36f);
+    temperature = fmaxf(temperature, (r.max - __fsub_rd(r.max, 1e-45f)) * (1.0f / 600.0f));
+    temperature = fminf(temperature, (r.max + 3.4028235e38f) * (1.0f / 33.0f));
     r.maxd = (double)r.max;
     r.inv_t = 1.4426950408889634 / (double)temperature;
     r.inv16 = 16.0 * r.inv_t;
-    r.x_zero = fmaxf(r.max - 31.538f * temperature, -3.4028235e38f);      // 2^-45.5 of the largest; -inf is below it
+    r.x_zero = __fsub_rd(r.max, 31.885f * temperature);       // 2^-46 of the largest or less, and below it
     r.root = sh.root;
     r.inv_bin = (float)(kBins - 1) / (kRange * temperature);
     r.x_min = -INFINITY;
@@ -329,6 +327,7 @@ k_sample(const SampleP p, const int slice) {
     const bool use_k = k > 0 && k < p.vocab, use_p = tp < 1.0f && tp > 0.f;
     const u64 frac64 = use_p ? (u64)__double2ull_rz((double)tp * 18446744073709551616.0) : 0ull;
     const u64 U = u >= 1.f ? ~0ull : (u > 0.f ? (u64)__double2ull_rz((double)u * 18446744073709551616.0) : 0ull);
+    uint32_t thr = 0xffffffffu; int cut = 0x7fffffff;         // kept so far: key < thr, or key == thr and index <= cut
     auto store = [&](int tok, float x, u64 Z) {
         if (p.token) p.token[row] = tok;
         if (p.token2) p.token2[row * p.token2_stride] = tok;
@@ -336,6 +335,73 @@ k_sample(const SampleP p, const int slice) {
     };
     // the reach of top-p: ceil(whole * p), at least 1
     auto reach = [&](u64 whole) { const u64 hi = __umul64hi(whole, frac64); return max((u64)1, hi + (whole * frac64 != 0)); };
+    // The draw from the weights that the warps' parts keep (wsum, in the first block): that block finds the warp whose part
+    // holds the token, that warp's block the token.  kept_of: what of the sum is kept (the first of it); weight_of: a logit's
+    // kept weight.
+    auto draw = [&](auto&& kept_of, auto&& weight_of, auto&& put) {
+        if (rank == 0 && warp == 0) {
+            constexpr int PL = kMaxCluster * kWarps / 32;
+            u64 sum[PL], mine = 0;
+#pragma unroll
+            for (int j = 0; j < PL; ++j) { sum[j] = lane * PL + j < CL * kWarps ? sh.wsum[lane * PL + j] : 0; mine += sum[j]; }
+            const u64 incl = warp_incl(mine), Z = kept_of(__shfl_sync(0xffffffffu, incl, 31));
+            const u64 target = __umul64hi(Z, U);              // the token: lowest index with cumulative weight > target
+            u64 before = incl - mine;
+#pragma unroll
+            for (int j = 0; j < PL; ++j) {
+                if (before <= target && before + sum[j] > target) {
+                    Shared* o = remote(&sh, (lane * PL + j) / kWarps);
+                    o->thr = thr; o->cut = cut; o->target = target - before; o->Z = Z;
+                    const int own = (lane * PL + j) % kWarps;
+                    for (int q = 0; q < CL; ++q) remote(&sh, q)->owner = q == (lane * PL + j) / kWarps ? own : -1;
+                }
+                before += sum[j];
+            }
+        }
+        sync_row();
+        if (sh.owner < 0) return;
+        thr = sh.thr; cut = sh.cut;
+        const u64 target = sh.target;
+        const int r0 = min(quads, sh.owner * per_warp), r1 = min(quads, r0 + per_warp), share = (r1 - r0 + kThreads - 1) / kThreads;
+        const int q0 = min(r1, r0 + tid * share), q1 = min(r1, q0 + share);      // consecutive quads of this thread
+        u64 mine = 0, tot;
+        for (int v = q0; v < q1; ++v) {
+            const float4 q = get(v);
+            const float e[4] = {q.x, q.y, q.z, q.w};
+#pragma unroll
+            for (int c = 0; c < 4; ++c) mine += weight_of(e[c], base + v * 4 + c);
+        }
+        u64 cum = block_excl<u64>(mine, sh.scan, tot);
+        if (cum <= target && cum + mine > target) {
+            for (int v = q0; v < q1; ++v) {
+                const float4 q = get(v);
+                const float e[4] = {q.x, q.y, q.z, q.w};
+#pragma unroll
+                for (int c = 0; c < 4; ++c) {
+                    const u64 w = weight_of(e[c], base + v * 4 + c);
+                    if (cum <= target && cum + w > target) put(base + v * 4 + c, e[c], sh.Z);
+                    cum += w;
+                }
+            }
+        }
+    };
+
+    if (r.max == INFINITY || r.max == -3.4028235e38f) {
+        // +inf shares the whole weight, and nothing but a mask lies below the lowest number: every weight is 1 or 0
+        u64 n = 0;
+        each([&](int, float4 q) { n += (q.x == r.max) + (q.y == r.max) + (q.z == r.max) + (q.w == r.max); });
+        n = warp_sum(n);
+        if (lane == 0) remote(&sh.wsum[0], 0)[rank * kWarps + warp] = n;
+        sync_row();
+        draw([&](u64 all) { const u64 m = use_k ? min(all, (u64)k) : all; return use_p ? min(m, reach(m)) : m; },
+             [&](float x, int) { return x == r.max ? 1ull : 0ull; },
+             [&](int tok, float, u64 Z) {
+                 if (p.token) p.token[row] = tok;
+                 if (p.token2) p.token2[row * p.token2_stride] = tok;
+                 if (p.prob) p.prob[row * p.prob_stride] = 1.0f / (float)Z;
+             });
+        return;
+    }
     auto entry = [&](float x, int idx) {                      // one more entry of this block's list
         const int at = atomicAdd(&sh.n_list, 1);
         if (at < kList) sh.list[at] = (u64)key_of(x) << 32 | (uint32_t)idx;
@@ -364,7 +430,7 @@ k_sample(const SampleP p, const int slice) {
     // Few entries (n <= kFew) are ranked by counting.  Thread (i, part) compares entry i with every parts-th entry: `rank` and
     // few_sum get the number and the weight of the entries before it.  All threads call it; few_w holds the weights after.
     const auto few = [&](int n, int& i, bool& mine) {
-        const int n2 = n <= 64 ? 64 : n <= 128 ? 128 : 256;
+        const int n2 = n <= 64 ? 64 : n <= 128 ? 128 : n <= 256 ? 256 : 512;
         i = tid & (n2 - 1);
         const int part = tid / n2;
         mine = part == 0 && i < n;
@@ -431,7 +497,7 @@ k_sample(const SampleP p, const int slice) {
                 if (mine) { sh.few_sum[i] = 0; if (!in) sh.few_w[i] = 0; }
                 __syncthreads();
                 const u64 Z = sh.few_total[1], target = __umul64hi(Z, U);
-                const int n2 = n <= 64 ? 64 : n <= 128 ? 128 : 256;
+                const int n2 = n <= 64 ? 64 : n <= 128 ? 128 : n <= 256 ? 256 : 512;
                 if (in) {                                     // the kept weight in front of the entry, in index order
                     u64 sum = 0;
                     for (int j = tid / n2; j < n; j += kThreads / n2)
@@ -488,7 +554,7 @@ k_sample(const SampleP p, const int slice) {
                 for (int j = 0; j < 4; ++j) {
                     if (cum <= target && cum + s4[j] > target) {
                         const int tok = (int)(sh.all[tid * 4 + j] >> 32);     // its slice may be another block's: the logit from global memory
-                        store(tok, pos_inf ? 0.f : (float)reinterpret_cast<const E*>(p.logits)[row * p.row_stride + tok], Z);
+                        store(tok, (float)reinterpret_cast<const E*>(p.logits)[row * p.row_stride + tok], Z);
                     }
                     cum += s4[j];
                 }
@@ -500,7 +566,6 @@ k_sample(const SampleP p, const int slice) {
     }
 
     // ---- whole distributions
-    uint32_t thr = 0xffffffffu; int cut = 0x7fffffff;         // kept so far: key < thr, or key == thr and index <= cut
     int za = 0, zb = kBins;                                   // bins that may hold the last threshold: elements before them are kept
     bool searched = false;                                    // za, zb hold a zone
     u64 ws = 0;                                               // weight of this warp's kept elements (before bin za, once searched)
@@ -514,22 +579,28 @@ k_sample(const SampleP p, const int slice) {
         const float fa = (float)za, fb = (float)(zb + 1), stop = sum_all ? (float)(kBins - 1) : fa;
         const bool with_min = r.x_min > -INFINITY;
         above = whole = ws = 0;
+        unsigned n_above = 0, n_whole = 0, n_ws = 0;
         each([&](int v, float4 q) {
             const float e[4] = {q.x, q.y, q.z, q.w};
             const float d[4] = {(r.max - q.x) * r.inv_bin, (r.max - q.y) * r.inv_bin, (r.max - q.z) * r.inv_bin, (r.max - q.w) * r.inv_bin};
             const float dm = fminf(fminf(d[0], d[1]), fminf(d[2], d[3]));
             if (dm < stop) {
+                u64 w[4];
 #pragma unroll
-                for (int c = 0; c < 4; ++c) {
-                    const u64 w = weight(r, e[c]);
-                    whole += w;
-                    if (d[c] < fa) { above += w; if (with_min && e[c] >= r.x_min) ws += w; }
-                }
+                for (int c = 0; c < 4; ++c) w[c] = weight_bits(r, e[c]);
+                if (sum_all) { whole += (w[0] + w[1]) + (w[2] + w[3]); n_whole += 4; }
+#pragma unroll
+                for (int c = 0; c < 4; ++c)
+                    if (d[c] < fa) {
+                        above += w[c]; ++n_above;
+                        if (with_min && e[c] >= r.x_min) { ws += w[c]; ++n_ws; }
+                    }
             }
             if (dm < fb)
 #pragma unroll
                 for (int c = 0; c < 4; ++c) if (d[c] >= fa && d[c] < fb) inside(e[c], base + v * 4 + c);
         });
+        above -= n_above * kOffset; whole -= n_whole * kOffset; ws -= n_ws * kOffset;
         if (!with_min) ws = above;
         ws = warp_sum(ws);
         above = warp_sum(above); whole = warp_sum(whole);
@@ -808,52 +879,8 @@ k_sample(const SampleP p, const int slice) {
         sync_row();
     }
 
-    // ---- the draw: the first block finds the warp whose part holds the token, that warp's block the token
-    if (rank == 0 && warp == 0) {
-        constexpr int PL = kMaxCluster * kWarps / 32;
-        u64 sum[PL], mine = 0;
-#pragma unroll
-        for (int j = 0; j < PL; ++j) { sum[j] = lane * PL + j < CL * kWarps ? sh.wsum[lane * PL + j] : 0; mine += sum[j]; }
-        const u64 incl = warp_incl(mine), Z = __shfl_sync(0xffffffffu, incl, 31);
-        const u64 target = __umul64hi(Z, U);                  // the token: lowest index with cumulative weight > target
-        u64 before = incl - mine;
-#pragma unroll
-        for (int j = 0; j < PL; ++j) {
-            if (before <= target && before + sum[j] > target) {
-                Shared* o = remote(&sh, (lane * PL + j) / kWarps);
-                o->thr = thr; o->cut = cut; o->target = target - before; o->Z = Z;
-                const int own = (lane * PL + j) % kWarps;
-                for (int q = 0; q < CL; ++q) remote(&sh, q)->owner = q == (lane * PL + j) / kWarps ? own : -1;
-            }
-            before += sum[j];
-        }
-    }
-    sync_row();
-    if (sh.owner < 0) return;
-    thr = sh.thr; cut = sh.cut;
-    const u64 target = sh.target;
-    const int r0 = min(quads, sh.owner * per_warp), r1 = min(quads, r0 + per_warp), share = (r1 - r0 + kThreads - 1) / kThreads;
-    const int q0 = min(r1, r0 + tid * share), q1 = min(r1, q0 + share);      // consecutive quads of this thread
-    u64 mine = 0, tot;
-    for (int v = q0; v < q1; ++v) {
-        const float4 q = get(v);
-        const float e[4] = {q.x, q.y, q.z, q.w};
-#pragma unroll
-        for (int c = 0; c < 4; ++c) { const u64 w = weight(r, e[c]); mine += kept(e[c], base + v * 4 + c) ? w : 0; }
-    }
-    u64 cum = block_excl<u64>(mine, sh.scan, tot);
-    if (cum <= target && cum + mine > target) {
-        for (int v = q0; v < q1; ++v) {
-            const float4 q = get(v);
-            const float e[4] = {q.x, q.y, q.z, q.w};
-#pragma unroll
-            for (int c = 0; c < 4; ++c) {
-                const u64 w = kept(e[c], base + v * 4 + c) ? weight(r, e[c]) : 0;
-                if (cum <= target && cum + w > target) store(base + v * 4 + c, e[c], sh.Z);
-                cum += w;
-            }
-        }
-    }
+    draw([&](u64 Z) { return Z; }, [&](float x, int idx) { return kept(x, idx) ? weight(r, x) : 0ull; },
+         [&](int tok, float x, u64 Z) { store(tok, x, Z); });
 }
 
 template <class E, bool SLICES>

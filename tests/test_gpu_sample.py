@@ -52,7 +52,7 @@ def check(x, u, bf16=False, pad=0, most_skipped=0.02, **f):
             skipped += 1
             continue
         assert tok[r] == want, (r, tok[r], want, margin, g)
-        assert abs(prob[r] - p) <= PROB_REL(V) * p, (r, prob[r], p)
+        assert abs(float(prob[r]) - p) <= PROB_REL(V) * p, (r, prob[r], p)         # (in double: fp32 would round the difference)
     assert skipped <= most_skipped * n, skipped
 
 
@@ -158,6 +158,25 @@ def test_masked_rows_and_special_values():
             assert tok[3] == V // 2 and tok[7] in (V // 2, V // 2 + 1) and tok[8] in (V // 2 - 1, V // 2, V // 2 + 1)
         assert tok[9] == 0
         assert np.all(np.isfinite(prob)) and np.all((tok >= 0) & (tok < V))
+
+
+def test_rows_at_the_ends_of_the_number_range():
+    """Rows of the type's lowest value with and without -inf among it, logits whose steps are coarse next to the temperature."""
+    inf, low, V = np.inf, np.float32(-3.4028235e38), 4000
+    for bf16 in (False, True):
+        lo = np.float32(-3.3895314e38) if bf16 else low
+        x = np.full((4, V), lo, np.float32)
+        x[1, ::2] = -inf
+        x[2, :] = -inf; x[2, [7, 9]] = lo
+        x[3, 5] = 0.0
+        tok, prob = run(x, np.array([0.5, 0.5, 0.75, 0.9], np.float32), bf16=bf16)
+        assert tok.tolist() == [V // 2, V // 2 + 1, 9, 5], tok
+        assert np.allclose(prob, [1 / V, 2 / V, 0.5, 1.0], rtol=1e-6, atol=0)
+    big = np.float32(1e8)                                     # steps of 8
+    x = np.repeat((big - 8 * np.arange(V)[::-1]).astype(np.float32)[None], 6, 0)
+    check(x, np.linspace(0.05, 0.95, 6), temperature=4.0)
+    check(x, np.linspace(0.05, 0.95, 6), temperature=np.array([1e-6, 0.3, 1.0, 100.0, 1e5, 1e9]), top_k=900)
+    check(x, np.linspace(0.05, 0.95, 6), temperature=np.array([1e-6, 0.3, 1.0, 100.0, 1e5, 1e9]), top_p=0.8)
 
 
 def test_edges_of_u_and_of_the_settings():
