@@ -46,6 +46,7 @@ constexpr int kCoarse = kThreads;              // histogram of the threads' maxi
 constexpr int kList = 2048;                    // entries one block sorts
 constexpr int kListK = 1024;                   // largest top-k that goes that way
 constexpr int kBatch = 4;                      // quads a thread loads before it looks at them
+constexpr int kBuckets = 1024;
 constexpr int kFew = 512;                      // entries that are ranked by counting, not sorted
 constexpr int kFracBits = 44;
 constexpr float kRange = 31.5f;                // nats below the maximum that the bins cover; beyond it weights are zero
@@ -158,17 +159,43 @@ template <class V> __device__ __forceinline__ V block_excl(V v, V* buf, V& total
     return __shfl_sync(0xffffffffu, wi - w, warp) + incl - v;
 }
 
-// a[0 .. n) ascending, n a power of two >= 64; pairs closer than 64 apart stay inside a warp's 64 elements
-__device__ __forceinline__ void sort_block(u64* a, int n) {
-    for (int size = 2; size <= n; size <<= 1)
-        for (int stride = size >> 1; stride; stride >>= 1) {
-            for (int i = threadIdx.x; i < n / 2; i += kThreads) {
-                const int lo = 2 * i - (i & (stride - 1)), hi = lo + stride;
-                const u64 x = a[lo], y = a[hi];
-                if ((x > y) == ((lo & size) == 0)) { a[lo] = y; a[hi] = x; }
+// The kList entries of a, ascending (bitonic).  A thread holds four neighbours: pairs up to 2 apart meet in its registers, up
+// to 64 apart by shuffles, and only the ten steps of wider pairs go through shared memory and a barrier.
+__device__ __forceinline__ void sort_list(u64* a) {
+    static_assert(kList == 4 * kThreads, "four entries a thread");
+    const int t = threadIdx.x;
+    ulonglong2* mem = reinterpret_cast<ulonglong2*>(a);
+    u64 x[4];
+    { const ulonglong2 p = mem[2 * t], q = mem[2 * t + 1]; x[0] = p.x; x[1] = p.y; x[2] = q.x; x[3] = q.y; }
+    auto order = [](u64& lo, u64& hi, bool up) { const u64 l = lo, h = hi; const bool swap = (l > h) == up; lo = swap ? h : l; hi = swap ? l : h; };
+#pragma unroll 1
+    for (int size = 2; size <= kList; size <<= 1) {
+        const bool up = (4 * t & size) == 0;                  // (size 2 below: the thread's second pair the other way)
+#pragma unroll 1
+        for (int stride = size >> 1; stride >= 4; stride >>= 1) {
+            const bool low = (4 * t & stride) == 0, take_min = low == up;
+            u64 y[4];
+            if (stride >= 128) {
+                __syncthreads();                              // the last step's reads are done
+                mem[2 * t] = make_ulonglong2(x[0], x[1]); mem[2 * t + 1] = make_ulonglong2(x[2], x[3]);
+                __syncthreads();
+                const int o = t ^ (stride >> 2);
+                const ulonglong2 p = mem[2 * o], q = mem[2 * o + 1];
+                y[0] = p.x; y[1] = p.y; y[2] = q.x; y[3] = q.y;
+            } else {
+#pragma unroll
+                for (int c = 0; c < 4; ++c) y[c] = __shfl_xor_sync(0xffffffffu, x[c], stride >> 2);
             }
-            if (stride > 32 || (stride == 1 && size >= 64)) __syncthreads(); else __syncwarp();
+#pragma unroll
+            for (int c = 0; c < 4; ++c) x[c] = (x[c] < y[c]) == take_min ? x[c] : y[c];
         }
+        if (size > 2) { order(x[0], x[2], up); order(x[1], x[3], up); }
+        order(x[0], x[1], size > 2 ? up : true);
+        order(x[2], x[3], size > 2 ? up : false);
+    }
+    __syncthreads();
+    mem[2 * t] = make_ulonglong2(x[0], x[1]); mem[2 * t + 1] = make_ulonglong2(x[2], x[3]);
+    __syncthreads();
 }
 
 // Four logits at p (which is aligned to them): -inf in place of NaN.
@@ -181,6 +208,9 @@ __device__ __forceinline__ float4 load4(const __nv_bfloat16* p) {
     return make_float4(fmaxf(__uint_as_float(b.x << 16), -INFINITY), fmaxf(__uint_as_float(b.x & 0xffff0000u), -INFINITY),
                        fmaxf(__uint_as_float(b.y << 16), -INFINITY), fmaxf(__uint_as_float(b.y & 0xffff0000u), -INFINITY));
 }
+
+struct Full { static constexpr int value = kBatch; };
+struct One { static constexpr int value = 1; };
 
 template <class E, bool SLICES>
 __global__ void __launch_bounds__(kThreads, 2)
@@ -223,34 +253,48 @@ k_sample(const SampleP p, const int slice) {
         sh.edge[tid] = make_float4(e[0], e[1], e[2], e[3]);
     }
     __syncthreads();
-    // f(v, quad v) for the quads [a, b) that this thread sees, `stride` apart: from global memory, the full ones first
-    auto from_global = [&](int a, int b, int at, int stride, auto&& f) {
-        const int lo = max(a, full0), hi = min(b, full1);
-        int v = lo + at;
-        for (; v + (kBatch - 1) * stride < hi; v += kBatch * stride) {       // the loads first: f may write to shared memory
+    // f(v, n, q): up to kBatch quads of the warp's part, q[i] being quad v + 32 i, all lanes together (past the end: v = -1 and
+    // quads of -inf), from global memory: the full quads first
+    const float4 none = make_float4(-INFINITY, -INFINITY, -INFINITY, -INFINITY);
+    auto from_global = [&](auto&& f) {
+        const int lo = max(v0, full0), hi = min(v1, full1);
+        int vb = lo;
+        for (; vb + 32 * kBatch <= hi; vb += 32 * kBatch) {   // the loads first: f may write to shared memory
             float4 q[kBatch];
 #pragma unroll
-            for (int i = 0; i < kBatch; ++i) q[i] = load4(quad0 + (v + i * stride) * 4);
-#pragma unroll
-            for (int i = 0; i < kBatch; ++i) f(v + i * stride, q[i]);
+            for (int i = 0; i < kBatch; ++i) q[i] = load4(quad0 + (vb + i * 32 + lane) * 4);
+            f(vb + lane, q, Full{});
         }
 #pragma unroll 1
-        for (; v < hi; v += stride) f(v, load4(quad0 + v * 4));
-        if (at == 0) {
+        for (; vb < hi; vb += 32) { const int v = vb + lane; const float4 q = v < hi ? load4(quad0 + v * 4) : none; f(v < hi ? v : -1, &q, One{}); }
 #pragma unroll 1
-            for (int k = 0; k < 2; ++k) {
-                const int v = k ? quads - 1 : 0;
-                if (v >= a && v < b && (v < full0 || v >= full1) && !(k && quads == 1)) f(v, sh.edge[k]);
-            }
+        for (int k = 0; k < 2; ++k) {
+            const int v = k ? quads - 1 : 0;
+            if (v >= v0 && v < v1 && (v < full0 || v >= full1) && !(k && quads == 1)) { const float4 q = lane ? none : sh.edge[k]; f(lane ? -1 : v, &q, One{}); }
         }
     };
-    // the same for the warp's part, from wherever the row is held
-    auto each = [&](auto&& f) {
+    // the same from wherever the row is held
+    auto each_batch = [&](auto&& f) {
         if (SLICES) {
-#pragma unroll 4
-            for (int v = v0 + lane; v < v1; v += 32) f(v, xs[v]);
-        } else from_global(v0, v1, lane, 32, f);
+            int vb = v0;
+            for (; vb + 32 * kBatch <= v1; vb += 32 * kBatch) {
+                float4 q[kBatch];
+#pragma unroll
+                for (int i = 0; i < kBatch; ++i) q[i] = xs[vb + i * 32 + lane];
+                f(vb + lane, q, Full{});
+            }
+#pragma unroll 1
+            for (; vb < v1; vb += 32) { const int v = vb + lane; const float4 q = v < v1 ? xs[v] : none; f(v < v1 ? v : -1, &q, One{}); }
+        } else from_global(f);
     };
+    // quad by quad
+    auto single = [](auto&& f) {
+        return [&f](int v, const float4* q, auto n) {
+#pragma unroll
+            for (int i = 0; i < decltype(n)::value; ++i) f(v + i * 32, q[i]);
+        };
+    };
+    auto each = [&](auto&& f) { each_batch(single(f)); };
     auto get = [&](int v) {                                   // one quad, wherever the row is held
         if (SLICES) return xs[v];
         float4 q = sh.edge[v == 0 ? 0 : 1];
@@ -261,15 +305,15 @@ k_sample(const SampleP p, const int slice) {
     const bool choose = !(temperature > 0.f && temperature < INFINITY);      // greedy
     int top = -1;                                             // greedy: the first of this thread's quads that holds its maximum
     if (choose) {
-        from_global(v0, v1, lane, 32, [&](int v, float4 q) {
+        from_global(single([&](int v, float4 q) {
             const float m = fmaxf(fmaxf(q.x, q.y), fmaxf(q.z, q.w));
             if (m > tmax.x || (m == tmax.x && v < top)) { tmax.x = m; top = v; }
-        });
+        }));
     } else {
-        from_global(v0, v1, lane, 32, [&](int v, float4 q) {
-            if (SLICES) xs[v] = q;
+        from_global(single([&](int v, float4 q) {
+            if (SLICES && v >= 0) xs[v] = q;
             tmax = make_float4(fmaxf(tmax.x, q.x), fmaxf(tmax.y, q.y), fmaxf(tmax.z, q.z), fmaxf(tmax.w, q.w));
-        });
+        }));
     }
     {
         float m = fmaxf(fmaxf(tmax.x, tmax.y), fmaxf(tmax.z, tmax.w));
@@ -402,9 +446,22 @@ k_sample(const SampleP p, const int slice) {
              });
         return;
     }
-    auto entry = [&](float x, int idx) {                      // one more entry of this block's list
-        const int at = atomicAdd(&sh.n_list, 1);
-        if (at < kList) sh.list[at] = (u64)key_of(x) << 32 | (uint32_t)idx;
+    // the logits of a batch whose bits (4 i + c for component c of quad v + 32 i) are set in `hit` into this block's list; all
+    // lanes of the warp call it.  One atomic a warp and batch: one a logit took 30 us for a list of 1400.
+    auto append = [&](unsigned hit, int v, const float4* q) {
+        if (!__any_sync(0xffffffffu, hit != 0)) return;
+        const int incl = warp_incl(__popc(hit));
+        int at = 0;
+        if (lane == 31) at = atomicAdd(&sh.n_list, incl);
+        at = __shfl_sync(0xffffffffu, at, 31) + incl - __popc(hit);
+#pragma unroll
+        for (int i = 0; i < kBatch; ++i)
+            if (hit >> 4 * i & 15) {
+                const float e[4] = {q[i].x, q[i].y, q[i].z, q[i].w};
+#pragma unroll
+                for (int c = 0; c < 4; ++c)
+                    if (hit >> (4 * i + c) & 1) { if (at < kList) sh.list[at] = (u64)key_of(e[c]) << 32 | (uint32_t)(base + (v + i * 32) * 4 + c); ++at; }
+            }
     };
     // brings the blocks' lists together in the first block; returns the entries of the row (more than kList: not brought)
     auto gather = [&]() {
@@ -418,15 +475,53 @@ k_sample(const SampleP p, const int slice) {
         sync_row();
         return *remote(&sh.n_all, 0);
     };
-    // sorts the n entries of `all`: descending logits, ascending indices
-    auto sort_all = [&](int n) {
-        int size = 64;
-        while (size < n) size <<= 1;
-        for (int i = n + tid; i < size; i += kThreads) sh.all[i] = ~0ull;
+    // Sorts the n entries of `all`, ascending.  bin_of is monotone: entries are spread over kBuckets bins and ranked inside
+    // theirs by counting; where a bin gets more than 64 (equal logits), by the sorting network, which takes eight times as long.
+    auto sort_all = [&](int n, auto&& bin_of) {
+        uint32_t* cnt = reinterpret_cast<uint32_t*>(sh.few_w);
+        uint32_t* pre = reinterpret_cast<uint32_t*>(sh.few_sum);
+        for (int i = tid; i < kBuckets; i += kThreads) cnt[i] = 0;
         __syncthreads();
-        sort_block(sh.all, size);
+        u64 x[4]; int bin[4]; uint32_t slot[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const int i = tid + j * kThreads;
+            bin[j] = -1;
+            if (i < n) { x[j] = sh.all[i]; bin[j] = max(0, min(kBuckets - 1, bin_of(x[j]))); slot[j] = atomicAdd(&cnt[bin[j]], 1u); }
+        }
+        __syncthreads();
+        const uint32_t c0 = cnt[2 * tid], c1 = cnt[2 * tid + 1];
+        if (__syncthreads_or(max(c0, c1) > 64)) {
+            for (int i = n + tid; i < kList; i += kThreads) sh.all[i] = ~0ull;
+            __syncthreads();
+            sort_list(sh.all);
+            return;
+        }
+        u64 tot;
+        const uint32_t e = (uint32_t)block_excl<u64>(c0 + c1, sh.scan, tot);
+        pre[2 * tid] = e; pre[2 * tid + 1] = e + c0;
+        __syncthreads();
+#pragma unroll
+        for (int j = 0; j < 4; ++j) if (bin[j] >= 0) sh.all[pre[bin[j]] + slot[j]] = x[j];
+        __syncthreads();
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+            if (bin[j] >= 0) {
+                const uint32_t lo = pre[bin[j]], m = cnt[bin[j]];
+                uint32_t before = 0;
+                for (uint32_t i = 0; i < m; ++i) before += sh.all[lo + i] < x[j];
+                slot[j] = lo + before;
+            }
+        __syncthreads();
+#pragma unroll
+        for (int j = 0; j < 4; ++j) if (bin[j] >= 0) sh.all[slot[j]] = x[j];
+        __syncthreads();
     };
-
+    auto by_value = [&](float from, float to) {               // bins over the logits from `from` down to `to`
+        const float inv = from > to && to > -INFINITY ? (float)(kBuckets - 1) / (from - to) : 0.f;
+        return [from, inv](u64 a) { return (int)fminf((from - value_of((uint32_t)(a >> 32))) * inv, (float)kBuckets); };
+    };
+    auto by_index = [&](u64 a) { return (int)(a >> 32) / ((p.vocab + kBuckets - 1) / kBuckets); };
     // Few entries (n <= kFew) are ranked by counting.  Thread (i, part) compares entry i with every parts-th entry: `rank` and
     // few_sum get the number and the weight of the entries before it.  All threads call it; few_w holds the weights after.
     const auto few = [&](int n, int& i, bool& mine) {
@@ -470,12 +565,15 @@ k_sample(const SampleP p, const int slice) {
             }
         }
         if (!use_p && r.x_min > tau) tau = r.x_min;
-        each([&](int v, float4 q) {
-            if (fmaxf(fmaxf(q.x, q.y), fmaxf(q.z, q.w)) >= tau) {
-                const float e[4] = {q.x, q.y, q.z, q.w};
+        each_batch([&](int v, const float4* q, auto n) {
+            unsigned hit = 0;
 #pragma unroll
-                for (int c = 0; c < 4; ++c) if (e[c] >= tau && e[c] > -INFINITY) entry(e[c], base + v * 4 + c);
+            for (int i = 0; i < decltype(n)::value; ++i) {
+                const float e[4] = {q[i].x, q[i].y, q[i].z, q[i].w};
+#pragma unroll
+                for (int c = 0; c < 4; ++c) if (e[c] >= tau && e[c] > -INFINITY) hit |= 1u << (4 * i + c);
             }
+            append(hit, v, q);
         });
         const int n = gather();
         sync_row();                                           // everybody has read it: from here the first block needs no other
@@ -508,7 +606,7 @@ k_sample(const SampleP p, const int slice) {
                 if (mine && in && sh.few_sum[i] <= target && sh.few_sum[i] + w > target) store((int)(uint32_t)a, value_of((uint32_t)(a >> 32)), Z);
                 return;
             }
-            sort_all(n);
+            sort_all(n, by_value(r.max, tau));
             // four consecutive places a thread, in descending order of logits
             u64* wt = sh.list;
             u64 w4[4], mine = 0, tot;
@@ -542,7 +640,7 @@ k_sample(const SampleP p, const int slice) {
             int at = (int)block_excl<u64>((u64)kept, sh.scan, kn);
 #pragma unroll
             for (int j = 0; j < 4; ++j) if (w4[j] > 0) sh.all[at++] = (u64)idx4[j] << 32 | (uint32_t)(tid * 4 + j);
-            sort_all((int)kn);
+            sort_all((int)kn, by_index);
             const u64 target = __umul64hi(Z, U);
             mine = 0;
             u64 s4[4];
@@ -573,14 +671,14 @@ k_sample(const SampleP p, const int slice) {
         const uint32_t key = key_of(x);
         return x >= r.x_min && (key < thr || (key == thr && idx <= cut));
     };
-    // the weights before bin za (`above`; into ws those that min-p keeps) and, with sum_all, of all; `inside` is called for
-    // the elements of bins [za, zb].  No branch around the polynomials, four at a time: their chain is long.
+    // the weights before bin za (`above`; into ws those that min-p keeps) and, with sum_all, of all; `inside` gets every
+    // quad with a bit set for its elements of bins [za, zb], all lanes together.  No branch around the polynomials, four at a time: their chain is long.
     auto weigh = [&](bool sum_all, u64& above, u64& whole, auto&& inside) {
         const float fa = (float)za, fb = (float)(zb + 1), stop = sum_all ? (float)(kBins - 1) : fa;
         const bool with_min = r.x_min > -INFINITY;
         above = whole = ws = 0;
         unsigned n_above = 0, n_whole = 0, n_ws = 0;
-        each([&](int v, float4 q) {
+        each([&](int v, const float4& q) {
             const float e[4] = {q.x, q.y, q.z, q.w};
             const float d[4] = {(r.max - q.x) * r.inv_bin, (r.max - q.y) * r.inv_bin, (r.max - q.z) * r.inv_bin, (r.max - q.w) * r.inv_bin};
             const float dm = fminf(fminf(d[0], d[1]), fminf(d[2], d[3]));
@@ -596,9 +694,10 @@ k_sample(const SampleP p, const int slice) {
                         if (with_min && e[c] >= r.x_min) { ws += w[c]; ++n_ws; }
                     }
             }
-            if (dm < fb)
+            unsigned in = 0;
 #pragma unroll
-                for (int c = 0; c < 4; ++c) if (d[c] >= fa && d[c] < fb) inside(e[c], base + v * 4 + c);
+            for (int c = 0; c < 4; ++c) if (d[c] >= fa && d[c] < fb) in |= 1u << c;
+            inside(in, v, &q);
         });
         above -= n_above * kOffset; whole -= n_whole * kOffset; ws -= n_ws * kOffset;
         if (!with_min) ws = above;
@@ -691,7 +790,7 @@ k_sample(const SampleP p, const int slice) {
     if (!by_keys) {
         // ---- one pass: exact weights, and a list of the zone (without a filter: everything is kept)
         if (!searched) { za = kBins; zb = kBins - 1; }
-        weigh(use_p || !searched, above, whole, [&](float x, int idx) { entry(x, idx); });
+        weigh(use_p || !searched, above, whole, append);
         if (lane == 0) remote(&sh.wsum[0], 0)[rank * kWarps + warp] = ws;
         const int n = searched ? gather() : 0;
         if (!searched) sync_row();
@@ -717,7 +816,7 @@ k_sample(const SampleP p, const int slice) {
                 few(n, i, mine);
                 if (mine) decide(sh.all[i], (int)sh.rank[i], sh.few_w[i], sh.few_sum[i] + above_mass);
             } else {
-                sort_all(n);
+                sort_all(n, by_value(r.max - (float)za / r.inv_bin, r.max - (float)(zb + 1) / r.inv_bin));
                 u64 w4[4], mine = 0, tot;
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
@@ -762,7 +861,12 @@ k_sample(const SampleP p, const int slice) {
                     atomicAdd(&sh.hist[f], 1u);
                     atomicAdd(&sh.mass[f], weight(r, x));
                 };
-                if (first) weigh(by_mass && !whole_known, above, whole, inside);
+                if (first)
+                    weigh(by_mass && !whole_known, above, whole, [&](unsigned in, int v, const float4* q) {
+                        const float e[4] = {q->x, q->y, q->z, q->w};
+#pragma unroll
+                        for (int c = 0; c < 4; ++c) if (in >> c & 1) inside(e[c], base + v * 4 + c);
+                    });
                 else {
                     const float fa = (float)za, fb = (float)(zb + 1);
                     for (int v = v0 + lane; v < v1; v += 32) {
