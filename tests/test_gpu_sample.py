@@ -123,6 +123,11 @@ def test_ties_take_the_lowest_indices():
     assert tok[0] == V // 2 - 1
     tok, _ = run(x[:1], u[:1], top_k=64, top_p=0.25)          # dyadic: sixteen of sixty-four exactly
     assert tok[0] == 15
+    for V2, k in ((1500, 1000), (2048, 1024), (2000, 700)):  # lists of nothing but ties
+        y = np.zeros((3, V2), np.float32)
+        y[1, 100:] = -0.5
+        tok, prob = run(y, np.array([0.5, 0.999999, 0.0], np.float32), top_k=k)
+        assert tok[0] == k // 2 and tok[1] == k - 1 and tok[2] == 0, (V2, k, tok)
     # ties that straddle several blocks' slices, with larger values in front and behind
     y = np.full((1, 120000), -3.0, np.float32)
     y[0, 70000:90000] = 1.0
