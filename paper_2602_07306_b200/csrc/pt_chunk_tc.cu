@@ -204,6 +204,42 @@ __device__ __forceinline__ void mbar_arrive_relaxed(uint64_t* bar) {
     asm volatile("mbarrier.arrive.relaxed.cta.shared::cta.b64 _, [%0];" ::"r"(smem_u32(bar)) : "memory");
 }
 
+// Eight products of 16 along the contraction with one election: an election and fresh descriptors for each product take the
+// issuing warp longer than the tensor core takes for the product (88 cycles against 64 at 128 x 128).
+// D[tmem] (+)= A[smem] * B[smem], 64 elements of the contraction at a time (HALVES of them, kHalfBytes apart)
+template <int HALVES>
+__device__ __forceinline__ void mma_ss_tile(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc) {
+    static_assert(kHalfBytes >> 4 == 1024, "the second half's offset below");
+    if constexpr (HALVES == 2)
+        asm volatile("{\n .reg .pred e, o, z;\n .reg .b64 a<8>, b<8>;\n elect.sync _|e, 0xffffffff;\n setp.eq.b32 o, 0, 0;\n setp.ne.b32 z, 0, 0;\n"
+                     " add.s64 a1, %1, 2;\n add.s64 b1, %2, 2;\n add.s64 a2, %1, 4;\n add.s64 b2, %2, 4;\n add.s64 a3, %1, 6;\n add.s64 b3, %2, 6;\n"
+                     " add.s64 a4, %1, 1024;\n add.s64 b4, %2, 1024;\n add.s64 a5, %1, 1026;\n add.s64 b5, %2, 1026;\n"
+                     " add.s64 a6, %1, 1028;\n add.s64 b6, %2, 1028;\n add.s64 a7, %1, 1030;\n add.s64 b7, %2, 1030;\n"
+                     " @e tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, z;\n @e tcgen05.mma.cta_group::1.kind::f16 [%0], a1, b1, %3, o;\n"
+                     " @e tcgen05.mma.cta_group::1.kind::f16 [%0], a2, b2, %3, o;\n @e tcgen05.mma.cta_group::1.kind::f16 [%0], a3, b3, %3, o;\n"
+                     " @e tcgen05.mma.cta_group::1.kind::f16 [%0], a4, b4, %3, o;\n @e tcgen05.mma.cta_group::1.kind::f16 [%0], a5, b5, %3, o;\n"
+                     " @e tcgen05.mma.cta_group::1.kind::f16 [%0], a6, b6, %3, o;\n @e tcgen05.mma.cta_group::1.kind::f16 [%0], a7, b7, %3, o;\n}"
+                     ::"r"(d), "l"(a), "l"(b), "r"(idesc) : "memory");
+    else
+        asm volatile("{\n .reg .pred e, o, z;\n .reg .b64 a<4>, b<4>;\n elect.sync _|e, 0xffffffff;\n setp.eq.b32 o, 0, 0;\n setp.ne.b32 z, 0, 0;\n"
+                     " add.s64 a1, %1, 2;\n add.s64 b1, %2, 2;\n add.s64 a2, %1, 4;\n add.s64 b2, %2, 4;\n add.s64 a3, %1, 6;\n add.s64 b3, %2, 6;\n"
+                     " @e tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, z;\n @e tcgen05.mma.cta_group::1.kind::f16 [%0], a1, b1, %3, o;\n"
+                     " @e tcgen05.mma.cta_group::1.kind::f16 [%0], a2, b2, %3, o;\n @e tcgen05.mma.cta_group::1.kind::f16 [%0], a3, b3, %3, o;\n}"
+                     ::"r"(d), "l"(a), "l"(b), "r"(idesc) : "memory");
+}
+// D[tmem] (+)= A[tmem] * B[smem] over 128 keys; acc = 0: D starts at zero
+__device__ __forceinline__ void mma_ts_tile(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, uint32_t acc) {
+    asm volatile("{\n .reg .pred p, e, o;\n .reg .b64 b<8>;\n .reg .b32 a<8>;\n elect.sync _|e, 0xffffffff;\n setp.eq.b32 o, 0, 0;\n setp.ne.b32 p, %4, 0;\n"
+                 " add.u32 a1, %1, 8;\n add.s64 b1, %2, 128;\n add.u32 a2, %1, 16;\n add.s64 b2, %2, 256;\n add.u32 a3, %1, 24;\n add.s64 b3, %2, 384;\n"
+                 " add.u32 a4, %1, 32;\n add.s64 b4, %2, 512;\n add.u32 a5, %1, 40;\n add.s64 b5, %2, 640;\n add.u32 a6, %1, 48;\n add.s64 b6, %2, 768;\n"
+                 " add.u32 a7, %1, 56;\n add.s64 b7, %2, 896;\n"
+                 " @e tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n @e tcgen05.mma.cta_group::1.kind::f16 [%0], [a1], b1, %3, o;\n"
+                 " @e tcgen05.mma.cta_group::1.kind::f16 [%0], [a2], b2, %3, o;\n @e tcgen05.mma.cta_group::1.kind::f16 [%0], [a3], b3, %3, o;\n"
+                 " @e tcgen05.mma.cta_group::1.kind::f16 [%0], [a4], b4, %3, o;\n @e tcgen05.mma.cta_group::1.kind::f16 [%0], [a5], b5, %3, o;\n"
+                 " @e tcgen05.mma.cta_group::1.kind::f16 [%0], [a6], b6, %3, o;\n @e tcgen05.mma.cta_group::1.kind::f16 [%0], [a7], b7, %3, o;\n}"
+                 ::"r"(d), "r"(a), "l"(b), "r"(idesc), "r"(acc) : "memory");
+}
+
 template <int DH>
 __global__ void __launch_bounds__(kChunkThreads, 1)
 k_chunk_tc(const __grid_constant__ CUtensorMap qmap, const __grid_constant__ CUtensorMap kvmap, const ChunkP p, float* scratch, const int tpt,
@@ -378,23 +414,19 @@ k_chunk_tc(const __grid_constant__ CUtensorMap qmap, const __grid_constant__ CUt
         auto qk = [&](int i, int qb, int s, bool last) {           // S_i = Q_qb K_s^T
             if (!ok) return;
             const uint32_t qa = smem_u32(sq + qb * TILE), ka = smem_u32(sk + s * TILE);
-#pragma unroll
-            for (int ks = 0; ks < DH / 16; ++ks) {
-                const uint32_t off = (uint32_t)(ks >> 2) * kHalfBytes + (uint32_t)(ks & 3) * 32u;
-                mma_ss(tmem_base + i * 128, desc_kmajor(qa + off), desc_kmajor(ka + off), idesc_qk, ks != 0);
-            }
+            mma_ss_tile<HALVES>(tmem_base + i * 128, desc_kmajor(qa), desc_kmajor(ka), idesc_qk);
             tc_commit(&bars[C_SFULL + i]);
             if (last) tc_commit(&bars[C_QEMPTY + qb]);
         };
-        auto pv = [&](int i, int jv, int ng, bool fresh) {         // O_i (+)= P_i V over the groups that hold keys
+        auto pv = [&](int i, int jv, int ng, bool fresh, bool last) {   // O_i (+)= P_i V over the groups that hold keys
             wait(C_PFULL + i, (uint32_t)cnt[i] & 1u);
-            wait(C_VFULL + jv % kStV, (uint32_t)(jv / kStV) & 1u);
             ++cnt[i];
             if (!ok) return;
             const uint32_t va = smem_u32(sv + (jv % kStV) * TILE);
-            for (int ks = 0; ks < ng; ++ks)
+            if (ng == 8) mma_ts_tile(tmem_base + 256 + i * DH, tmem_base + i * 128, desc_mnmajor(va), idesc_pv, !fresh);
+            else for (int ks = 0; ks < ng; ++ks)
                 mma_ts(tmem_base + 256 + i * DH, tmem_base + i * 128 + ks * 8, desc_mnmajor(va + ks * 2048), idesc_pv, !fresh || ks != 0);
-            tc_commit(&bars[C_OREADY + i]);
+            if (last) tc_commit(&bars[C_OREADY + i]);              // before: the next scores say that this product is done
         };
         while (ok && next_seg(sg)) {
             if (sg.n1 == 0) {                                      // one row tile: scores two key tiles ahead, in turns
@@ -404,7 +436,8 @@ k_chunk_tc(const __grid_constant__ CUtensorMap qmap, const __grid_constant__ CUt
                 ++qc[qb];
                 for (int j = sg.lo; j < sg.hi + 2 && ok; ++j) {
                     if (j - 2 >= sg.lo) {
-                        pv((j - sg.lo) & 1, jj, min(8, (sg.kvlen - (j - 2) * 128 + 15) >> 4), j - 4 < sg.lo);
+                        wait(C_VFULL + jj % kStV, (uint32_t)(jj / kStV) & 1u);
+                        pv((j - sg.lo) & 1, jj, min(8, (sg.kvlen - (j - 2) * 128 + 15) >> 4), j - 4 < sg.lo, j >= sg.hi);
                         if (ok) tc_commit(&bars[C_VEMPTY + jj % kStV]);
                         ++jj;
                     }
@@ -423,21 +456,24 @@ k_chunk_tc(const __grid_constant__ CUtensorMap qmap, const __grid_constant__ CUt
             for (int i = 0; i < 2; ++i)
                 if (sg.lo < end[i]) { wait(C_QFULL + i, (uint32_t)qc[i] & 1u); ++qc[i]; qk(i, i, jj % kStK, sg.lo + 1 == end[i]); }
             if (ok) tc_commit(&bars[C_KEMPTY + jj % kStK]);
+            // What does not depend on the softmax groups is waited for before their P, and a tile's stages are given back
+            // behind the next product: between two products the tensor core has nothing to do.
             for (int j = sg.lo; j < sg.hi && ok; ++j, ++jj) {
                 const int sn = (jj + 1) % kStK;
-                const uint32_t phn = (uint32_t)((jj + 1) / kStK) & 1u;
                 const int ng = min(8, (sg.kvlen - j * 128 + 15) >> 4);
+                wait(C_VFULL + jj % kStV, (uint32_t)(jj / kStV) & 1u);
+                if (j + 1 < sg.hi) wait(C_KFULL + sn, (uint32_t)((jj + 1) / kStK) & 1u);
 #pragma unroll
                 for (int i = 0; i < 2; ++i) {
-                    if (j >= end[i]) continue;
-                    pv(i, jj, ng, j == sg.lo);
-                    if (j + 1 < end[i]) { wait(C_KFULL + sn, phn); qk(i, i, sn, j + 2 == end[i]); }
-                }
-                if (ok) {
-                    tc_commit(&bars[C_VEMPTY + jj % kStV]);
-                    if (j + 1 < sg.hi) tc_commit(&bars[C_KEMPTY + sn]);
+                    if (j < end[i]) pv(i, jj, ng, j == sg.lo, j + 1 == end[i]);
+                    if (i == 0 && ok && j > sg.lo) {
+                        tc_commit(&bars[C_VEMPTY + (jj - 1) % kStV]);
+                        tc_commit(&bars[C_KEMPTY + jj % kStK]);
+                    }
+                    if (j + 1 < end[i]) qk(i, i, sn, j + 2 == end[i]);
                 }
             }
+            if (ok) tc_commit(&bars[C_VEMPTY + (jj - 1) % kStV]);
         }
         __syncwarp();
     }
@@ -453,7 +489,7 @@ k_chunk_tc(const __grid_constant__ CUtensorMap qmap, const __grid_constant__ CUt
         const float c = p.scale_log2;
         const Slots<DH> slots{scratch};
         bool ok = true;
-        int cnt = 0, merges = 0;
+        int cnt = 0, merges = 0, segs = 0;                         // tiles, one-tile segments, segments with a tile of this group
         auto wait = [&](int bar, uint32_t parity) {
             ok = __all_sync(0xffffffffu, mbar_wait(&bars[bar], parity, abort_flag));
             if (!ok && lane == 0) { report(p.status, PT_ERR_DEVICE_TIMEOUT, LOC_CHUNK_WAIT); *abort_flag = 1; }
@@ -495,8 +531,7 @@ k_chunk_tc(const __grid_constant__ CUtensorMap qmap, const __grid_constant__ CUt
                 } else {
                     const bool grow = live && (mx - m_ref) * c > 8.0f;     // also from -inf, when mx is finite
                     if (__any_sync(0xffffffffu, grow)) {
-                        // the previous P V product must have landed before the accumulator is rescaled
-                        if (!wait(C_OREADY + i, (uint32_t)(cnt - 1) & 1u)) break;
+                        // (these scores were issued behind the previous P V, so that has landed)
                         const float corr = grow ? ex2((m_ref - mx) * c) : 1.0f;
                         if (grow) { m_ref = mx; l_run *= corr; }
 #pragma unroll 1
@@ -535,7 +570,7 @@ k_chunk_tc(const __grid_constant__ CUtensorMap qmap, const __grid_constant__ CUt
                 __syncwarp();
                 if (lane == 0) mbar_arrive(&bars[C_PFULL + i]);
             }
-            if (!ok || (first < end && !wait(C_OREADY + i, (uint32_t)(cnt - 1) & 1u))) break;
+            if (!ok || (first < end && !wait(C_OREADY + i, (uint32_t)segs++ & 1u))) break;
             float m = m_ref * c, f0 = 1.f, f1 = 0.f;                   // the maximum in powers of two, the groups' factors
             if (one) {
                 if (i == 1) {
