@@ -14,10 +14,10 @@
 // maximum) is zero: such a token is never drawn.  The exponential is evaluated in double; the multiple rounds it once,
 // an absolute error of 2^-45 against a sum of at least 1.
 //
-// Two ways to hold a row.  SLICES: a cluster of up to 8 blocks takes it, each block reads its slice from global memory once
-// and keeps it in shared memory, and the blocks exchange what they found through distributed shared memory - for few rows,
-// whose time is latency.  ROWS: one block takes the whole row and streams over it, the first pass from HBM and the later
-// ones mostly from L2 - for many rows, where exchanging between blocks costs more than reading again.
+// Three ways to take a row.  For few rows, whose time is latency, a cluster of up to 8 blocks, which exchange what they found
+// through distributed shared memory; each holds its slice in shared memory, or, where that would leave one block on an SM,
+// streams over it, the first pass from HBM and the later ones from L2.  For many rows, where exchanging between blocks costs
+// more than it saves, one block streams over the row.
 //
 // Two ways to find the kept set.
 // Few candidates (top-k up to kListK, or min-p alone): the k-th largest of the maxima that the threads found, four each, is a
@@ -47,8 +47,7 @@ constexpr int kList = 2048;                    // entries one block sorts
 constexpr int kListK = 1024;                   // largest top-k that goes that way
 constexpr int kBatch = 4;                      // quads a thread loads before it looks at them
 constexpr int kBuckets = 1024;
-constexpr int kFew = 512;                      // entries that are ranked by counting, not sorted
-constexpr int kFracBits = 44;
+constexpr int kFew = 128;                      // entries that are ranked by counting, not sorted
 constexpr float kRange = 31.5f;                // nats below the maximum that the bins cover; beyond it weights are zero
 constexpr float kSlack = 4e-7f;                // relative rounding of a distance and its bin number, three times over
 constexpr int kMaxCluster = 8;
@@ -103,6 +102,9 @@ __device__ __forceinline__ u64 weight_bits(const Row& r, float x) {
 }
 __device__ __forceinline__ u64 weight(const Row& r, float x) { return weight_bits(r, x) - kOffset; }
 
+// elements of bins, and bounds of their weight; the three sums over the block share their barriers
+struct BinSum { u64 n; double up, dn; };
+
 struct Shared {
     union {
         uint32_t bins[kBins];
@@ -113,17 +115,20 @@ struct Shared {
         uint32_t coarse[kCoarse];
         struct { uint32_t rank[kFew]; };
     };
-    u64 few_w[kFew], few_sum[kFew], few_total[2];
+    union {
+        struct { u64 few_w[kFew], few_sum[kFew], few_total[2]; };
+        struct { uint32_t bucket_n[kBuckets], bucket_0[kBuckets]; };
+    };
     float red[kWarps];
     u64 wsum[kMaxCluster * kWarps];            // first block: weight kept by the part of every warp of the cluster
     u64 warp_tmp[kWarps], warp_tmp2[kWarps];
     uint32_t warp_cnt[kWarps];
     u64 blk_mass, blk_all;                     // weight of this block's elements above the searched bins, and of all
     u64 scan[kWarps + 1];
-    double dscan[kWarps + 1];
+    BinSum bin_scan[kWarps];
     double root[16];
     double share[3];                           // totals of this block's share of the bins: counts, upper and lower bounds
-    float4 edge[2];                            // ROWS: the quads that the row does not fill
+    float4 edge[2];                            // streamed: the quads that the slice does not fill
     float max;
     int n_list, n_all;                         // entries of this block; of the row (in the first block)
     // found by a scan, or handed over by the block that found it
@@ -133,6 +138,7 @@ struct Shared {
     uint32_t thr; int owner; u64 target, obefore, Z;
 };
 
+static_assert(kFew == 128, "the thread counts below");
 static_assert(((sizeof(Shared) + 15) & ~15) + (kMaxSlice + 4) * 4 <= 232448, "shared memory of one block");
 
 template <class V> __device__ __forceinline__ V warp_incl(V v) {
@@ -157,6 +163,33 @@ template <class V> __device__ __forceinline__ V block_excl(V v, V* buf, V& total
     const V wi = warp_incl(w);
     total = __shfl_sync(0xffffffffu, wi, kWarps - 1);
     return __shfl_sync(0xffffffffu, wi - w, warp) + incl - v;
+}
+
+__device__ __forceinline__ BinSum warp_incl(BinSum v) {
+    const int lane = threadIdx.x & 31;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const u64 n = __shfl_up_sync(0xffffffffu, v.n, o);
+        const double up = __shfl_up_sync(0xffffffffu, v.up, o), dn = __shfl_up_sync(0xffffffffu, v.dn, o);
+        if (lane >= o) { v.n += n; v.up += up; v.dn += dn; }
+    }
+    return v;
+}
+__device__ __forceinline__ BinSum block_excl_bins(const BinSum& v, BinSum* buf, BinSum& total) {
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const BinSum incl = warp_incl(v);
+    __syncthreads();
+    if (lane == 31) buf[warp] = incl;
+    __syncthreads();
+    BinSum mine{incl.n - v.n, incl.up - v.up, incl.dn - v.dn};
+    total = BinSum{0, 0., 0.};
+#pragma unroll 1
+    for (int w = 0; w < kWarps; ++w) {
+        const BinSum s = buf[w];
+        total.n += s.n; total.up += s.up; total.dn += s.dn;
+        if (w < warp) { mine.n += s.n; mine.up += s.up; mine.dn += s.dn; }
+    }
+    return mine;
 }
 
 // The kList entries of a, ascending (bitonic).  A thread holds four neighbours: pairs up to 2 apart meet in its registers, up
@@ -212,16 +245,16 @@ __device__ __forceinline__ float4 load4(const __nv_bfloat16* p) {
 struct Full { static constexpr int value = kBatch; };
 struct One { static constexpr int value = 1; };
 
-template <class E, bool SLICES>
+template <class E, bool CLUSTER, bool HELD>
 __global__ void __launch_bounds__(kThreads, 2)
 k_sample(const SampleP p, const int slice) {
     extern __shared__ __align__(16) unsigned char smem_raw[];
     Shared& sh = *reinterpret_cast<Shared*>(smem_raw);
     float4* xs = reinterpret_cast<float4*>(smem_raw + ((sizeof(Shared) + 15) & ~15));
     cg::cluster_group cluster = cg::this_cluster();
-    const int CL = SLICES ? (int)cluster.num_blocks() : 1, rank = SLICES ? (int)cluster.block_rank() : 0;
-    auto sync_row = [&]() { if (SLICES) cluster.sync(); else __syncthreads(); };
-    auto remote = [&](auto* ptr, int q) { return SLICES ? cluster.map_shared_rank(ptr, q) : ptr; };
+    const int CL = CLUSTER ? (int)cluster.num_blocks() : 1, rank = CLUSTER ? (int)cluster.block_rank() : 0;
+    auto sync_row = [&]() { if (CLUSTER) cluster.sync(); else __syncthreads(); };
+    auto remote = [&](auto* ptr, int q) { return CLUSTER ? cluster.map_shared_rank(ptr, q) : ptr; };
     const int64_t row = blockIdx.x / CL;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int count = max(0, min(slice, p.vocab - rank * slice));
@@ -275,7 +308,7 @@ k_sample(const SampleP p, const int slice) {
     };
     // the same from wherever the row is held
     auto each_batch = [&](auto&& f) {
-        if (SLICES) {
+        if (HELD) {
             int vb = v0;
             for (; vb + 32 * kBatch <= v1; vb += 32 * kBatch) {
                 float4 q[kBatch];
@@ -296,7 +329,7 @@ k_sample(const SampleP p, const int slice) {
     };
     auto each = [&](auto&& f) { each_batch(single(f)); };
     auto get = [&](int v) {                                   // one quad, wherever the row is held
-        if (SLICES) return xs[v];
+        if (HELD) return xs[v];
         float4 q = sh.edge[v == 0 ? 0 : 1];
         if (v >= full0 && v < full1) q = load4(quad0 + v * 4);
         return q;
@@ -311,7 +344,7 @@ k_sample(const SampleP p, const int slice) {
         }));
     } else {
         from_global(single([&](int v, float4 q) {
-            if (SLICES && v >= 0) xs[v] = q;
+            if (HELD && v >= 0) xs[v] = q;
             tmax = make_float4(fmaxf(tmax.x, q.x), fmaxf(tmax.y, q.y), fmaxf(tmax.z, q.z), fmaxf(tmax.w, q.w));
         }));
     }
@@ -478,8 +511,7 @@ k_sample(const SampleP p, const int slice) {
     // Sorts the n entries of `all`, ascending.  bin_of is monotone: entries are spread over kBuckets bins and ranked inside
     // theirs by counting; where a bin gets more than 64 (equal logits), by the sorting network, which takes eight times as long.
     auto sort_all = [&](int n, auto&& bin_of) {
-        uint32_t* cnt = reinterpret_cast<uint32_t*>(sh.few_w);
-        uint32_t* pre = reinterpret_cast<uint32_t*>(sh.few_sum);
+        uint32_t *cnt = sh.bucket_n, *pre = sh.bucket_0;
         for (int i = tid; i < kBuckets; i += kThreads) cnt[i] = 0;
         __syncthreads();
         u64 x[4]; int bin[4]; uint32_t slot[4];
@@ -522,10 +554,11 @@ k_sample(const SampleP p, const int slice) {
         return [from, inv](u64 a) { return (int)fminf((from - value_of((uint32_t)(a >> 32))) * inv, (float)kBuckets); };
     };
     auto by_index = [&](u64 a) { return (int)(a >> 32) / ((p.vocab + kBuckets - 1) / kBuckets); };
-    // Few entries (n <= kFew) are ranked by counting.  Thread (i, part) compares entry i with every parts-th entry: `rank` and
+    // Few entries (n <= kFew) are ranked by counting (64 to 256 as a limit measure alike; counting 400 took 12 us more than
+    // sorting them).  Thread (i, part) compares entry i with every parts-th entry: `rank` and
     // few_sum get the number and the weight of the entries before it.  All threads call it; few_w holds the weights after.
     const auto few = [&](int n, int& i, bool& mine) {
-        const int n2 = n <= 64 ? 64 : n <= 128 ? 128 : n <= 256 ? 256 : 512;
+        const int n2 = n <= 64 ? 64 : 128;
         i = tid & (n2 - 1);
         const int part = tid / n2;
         mine = part == 0 && i < n;
@@ -595,7 +628,7 @@ k_sample(const SampleP p, const int slice) {
                 if (mine) { sh.few_sum[i] = 0; if (!in) sh.few_w[i] = 0; }
                 __syncthreads();
                 const u64 Z = sh.few_total[1], target = __umul64hi(Z, U);
-                const int n2 = n <= 64 ? 64 : n <= 128 ? 128 : n <= 256 ? 256 : 512;
+                const int n2 = n <= 64 ? 64 : 128;
                 if (in) {                                     // the kept weight in front of the entry, in index order
                     u64 sum = 0;
                     for (int j = tid / n2; j < n; j += kThreads / n2)
@@ -724,24 +757,23 @@ k_sample(const SampleP p, const int slice) {
         sync_row();
         // every block sums its share of the bins over the blocks: PER of them a thread.  An element of bin b weighs between
         // e^-(b + 1)d and e^-bd (a hundredth of a bin more on either side for the rounding of its number).
-        constexpr int MAXPER = kBins / kThreads;
-        const int per = MAXPER / CL, b0 = rank * (kBins / CL) + tid * per;
-        uint32_t c[MAXPER];
+        const int per = kBins / kThreads / CL, b0 = rank * (kBins / CL) + tid * per;
         const float d = kRange / (kBins - 1), step = __expf(-d);
-        double up = 0, dn = 0; u64 cnt = 0;
+        BinSum in{0, 0., 0.}, tot;
         {
             float fu = __expf(-d * ((float)b0 - 0.01f)), fd = __expf(-d * ((float)b0 + 1.01f));
+#pragma unroll 1
+            for (int b = b0; b < b0 + per; ++b) {
+                uint32_t c = 0;
 #pragma unroll
-            for (int j = 0; j < MAXPER; ++j) {
-                c[j] = 0;
-                if (j < per) for (int q = 0; q < CL; ++q) c[j] += remote(&sh.bins[0], q)[b0 + j];
-                cnt += c[j]; up += (double)((float)c[j] * fu); dn += (double)((float)c[j] * fd);
+                for (int q = 0; q < (CLUSTER ? kMaxCluster : 1); ++q) if (q < CL) c += remote(&sh.bins[0], q)[b];
+                if (CLUSTER) sh.bins[b] = c;                  // (no other block reads this block's own share here)
+                in.n += c; in.up += (double)((float)c * fu); in.dn += (double)((float)c * fd);
                 fu *= step; fd *= step;
             }
         }
-        u64 tc; double tu, td;
-        u64 ec = block_excl<u64>(cnt, sh.scan, tc);
-        double eu = block_excl<double>(up, sh.dscan, tu), el = block_excl<double>(dn, sh.dscan, td);
+        const BinSum before = block_excl_bins(in, sh.bin_scan, tot);
+        u64 tc = tot.n, ec = before.n; double tu = tot.up, td = tot.dn, eu = before.up, el = before.dn;
         if (tid == 0) { sh.share[0] = (double)tc; sh.share[1] = tu; sh.share[2] = td; sh.zone_a = sh.zone_b = sh.tail_a = sh.tail_b = kBins - 2; sh.bin = -1; sh.before_cnt = 0; }
         sync_row();
         tc = 0; tu = td = 0;
@@ -757,19 +789,17 @@ k_sample(const SampleP p, const int slice) {
         const double s_lo = td * (1.0 - (double)tp) * (1 - 1e-5), s_hi = tu * (1.0 - (double)tp) * (1 + 1e-5);
         float fu = __expf(-d * ((float)b0 - 0.01f)), fd = __expf(-d * ((float)b0 + 1.01f));
         const bool k_cuts = use_k && tc > (u64)k;             // otherwise top-k removes nothing that has weight
-#pragma unroll
-        for (int j = 0; j < MAXPER; ++j) {
-            const double u1 = (double)((float)c[j] * fu), l1 = (double)((float)c[j] * fd);
-            if (j < per) {
-                const int b = b0 + j;
-                if (k_cuts && ec < (u64)k && ec + c[j] >= (u64)k)
-                    for (int q = 0; q < CL; ++q) { Shared* o = remote(&sh, q); o->bin = b; o->before_cnt = ec; }
-                if (use_p && eu < t_lo && eu + u1 >= t_lo) for (int q = 0; q < CL; ++q) atomicMin(&remote(&sh, q)->zone_a, b);
-                if (use_p && el < t_hi && el + l1 >= t_hi) for (int q = 0; q < CL; ++q) atomicMin(&remote(&sh, q)->zone_b, b);
-                if (use_p && td - el > s_hi && td - (el + l1) <= s_hi) for (int q = 0; q < CL; ++q) atomicMin(&remote(&sh, q)->tail_a, b);
-                if (use_p && tu - eu > s_lo && tu - (eu + u1) <= s_lo) for (int q = 0; q < CL; ++q) atomicMin(&remote(&sh, q)->tail_b, b);
-            }
-            ec += c[j]; eu += u1; el += l1;
+#pragma unroll 1
+        for (int b = b0; b < b0 + per; ++b) {
+            const uint32_t c = sh.bins[b];
+            const double u1 = (double)((float)c * fu), l1 = (double)((float)c * fd);
+            if (k_cuts && ec < (u64)k && ec + c >= (u64)k)
+                for (int q = 0; q < CL; ++q) { Shared* o = remote(&sh, q); o->bin = b; o->before_cnt = ec; }
+            if (use_p && eu < t_lo && eu + u1 >= t_lo) for (int q = 0; q < CL; ++q) atomicMin(&remote(&sh, q)->zone_a, b);
+            if (use_p && el < t_hi && el + l1 >= t_hi) for (int q = 0; q < CL; ++q) atomicMin(&remote(&sh, q)->zone_b, b);
+            if (use_p && td - el > s_hi && td - (el + l1) <= s_hi) for (int q = 0; q < CL; ++q) atomicMin(&remote(&sh, q)->tail_a, b);
+            if (use_p && tu - eu > s_lo && tu - (eu + u1) <= s_lo) for (int q = 0; q < CL; ++q) atomicMin(&remote(&sh, q)->tail_b, b);
+            ec += c; eu += u1; el += l1;
             fu *= step; fd *= step;
         }
         sync_row();
@@ -987,23 +1017,23 @@ k_sample(const SampleP p, const int slice) {
          [&](int tok, float x, u64 Z) { store(tok, x, Z); });
 }
 
-template <class E, bool SLICES>
+template <class E, bool CLUSTER, bool HELD>
 pt_status launch_kind(const SampleP& p, int64_t n, int cl, cudaStream_t st) {
     const int slice = ((p.vocab + cl - 1) / cl + 3) & ~3;
     const size_t head = (sizeof(Shared) + 15) & ~15;
     static bool done_[kMaxDevices] = {};
     bool& done = done_[current_device()];
     if (!done) {
-        cudaError_t e = cudaFuncSetAttribute(k_sample<E, SLICES>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)(head + (SLICES ? (kMaxSlice + 4) * 4 : 0)));
+        cudaError_t e = cudaFuncSetAttribute(k_sample<E, CLUSTER, HELD>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)(head + (HELD ? (kMaxSlice + 4) * 4 : 0)));
         if (e != cudaSuccess) { set_error("cudaFuncSetAttribute: %s", cudaGetErrorString(e)); return PT_ERR_CUDA; }
         done = true;
     }
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)(n * cl)); cfg.blockDim = dim3(kThreads); cfg.dynamicSmemBytes = head + (SLICES ? (size_t)(slice + 4) * 4 : 0); cfg.stream = st;
+    cfg.gridDim = dim3((unsigned)(n * cl)); cfg.blockDim = dim3(kThreads); cfg.dynamicSmemBytes = head + (HELD ? (size_t)(slice + 4) * 4 : 0); cfg.stream = st;
     cudaLaunchAttribute at[1];
     at[0].id = cudaLaunchAttributeClusterDimension; at[0].val.clusterDim.x = cl; at[0].val.clusterDim.y = 1; at[0].val.clusterDim.z = 1;
-    cfg.attrs = at; cfg.numAttrs = SLICES ? 1 : 0;
-    cudaError_t e = cudaLaunchKernelEx(&cfg, k_sample<E, SLICES>, p, slice);
+    cfg.attrs = at; cfg.numAttrs = CLUSTER ? 1 : 0;
+    cudaError_t e = cudaLaunchKernelEx(&cfg, k_sample<E, CLUSTER, HELD>, p, slice);
     if (e != cudaSuccess) { set_error("k_sample launch: %s", cudaGetErrorString(e)); return PT_ERR_CUDA; }
     g_launches.fetch_add(1, std::memory_order_relaxed);
     return PT_OK;
@@ -1011,16 +1041,27 @@ pt_status launch_kind(const SampleP& p, int64_t n, int cl, cudaStream_t st) {
 
 template <class E>
 pt_status launch_t(const SampleP& p, int64_t n, cudaStream_t st) {
-    // SLICES while a block per 4096 logits, up to 8 a row, leaves every SM with two blocks at most.  Measured with top-k 50 /
-    // top-p 0.9 in us, SLICES against ROWS: 32 x 32000 12.1 / 30.8 against 12.5 / 35.7, 64 x 32000 13.5 / 38 against 12.7 / 35;
-    // 32 x 128000 16.5 / 52 against 18.7 / 94, 48 x 128000 27 / 93 against 18.9 / 94.
+    // Clusters while all of their blocks are resident, two on an SM: up to 8 blocks for a row, one per 4096 logits, or 4 where
+    // 8 are too many.  With 2 a row a cluster only broke even, so then, and for more rows, a block takes a row.  Measured with
+    // top-k 50 / top-p 0.9 in us, cluster against row: 24 x 32000 11.7 / 23.6 against 12.7 / 31.0, 24 x 128000 15.6 / 39.0 against
+    // 19.5 / 80.3, 64 x 32000 13.8 / 28.2 against 13.3 / 31.0, 64 x 128000 18.8 / 52.4 against 20.3 / 80.0; by twos 100 x 64000
+    // 18.5 / 52.7 against 16.4 / 49.3.
+    const int64_t slots = 2 * 148;
     int cl = 1;
     while (cl < kMaxCluster && (int64_t)cl * 4096 < p.vocab) cl *= 2;
-    if (n * cl > 2 * 148 || p.vocab > kMaxCluster * kMaxSlice) return launch_kind<E, false>(p, n, 1, st);
-    // slices of at most 16384 logits (64 KB: two blocks per SM); while a launch leaves SMs idle a row is spread further,
-    // down to slices of 2048
-    for (cl = 1; cl < kMaxCluster && ((p.vocab + cl - 1) / cl > 16384 || (n * cl * 2 <= 148 && (p.vocab + cl - 1) / cl > 2048));) cl *= 2;
-    return launch_kind<E, true>(p, n, cl, st);
+    if (cl == kMaxCluster && n * cl > slots) cl = kMaxCluster / 2;
+    else if (n * cl <= slots) {
+        // slices of at most 16384 logits (64 KB: two blocks per SM); while a launch leaves SMs idle a row is spread further,
+        // down to slices of 2048
+        const int most = cl;
+        for (cl = 1; cl < most && ((p.vocab + cl - 1) / cl > 16384 || (n * cl * 2 <= 148 && (p.vocab + cl - 1) / cl > 2048));) cl *= 2;
+    }
+    if (n * cl > slots) return launch_kind<E, false, false>(p, n, 1, st);
+    // longer slices are held where an SM has one block anyway, else they are streamed as well (64 x 128000 by fours: held
+    // 28.0 / 76.5)
+    const int slice = (p.vocab + cl - 1) / cl;
+    if (slice <= 16384 || (slice <= kMaxSlice && n * cl <= 148)) return launch_kind<E, true, true>(p, n, cl, st);
+    return launch_kind<E, true, false>(p, n, cl, st);
 }
 
 }  // namespace

@@ -220,6 +220,28 @@ def test_a_row_does_not_depend_on_its_batch_and_calls_repeat():
         assert t1[0] == tok[r] and p1[0] == prob[r]
 
 
+@pytest.mark.parametrize("f", [dict(), dict(top_k=40), dict(top_k=700, top_p=0.8), dict(top_k=5000), dict(top_p=0.9), dict(top_k=9000, top_p=0.6, min_p=1e-5), dict(min_p=0.01), dict(temperature=0.0)], ids=str)
+def test_every_way_of_taking_a_row_gives_the_same(f):
+    """1 to 150 rows at once: clusters that hold their slices, clusters that stream over them, a block a row.  The sums are whole
+    numbers, so the draws and their probabilities are equal bit for bit."""
+    rng = np.random.default_rng(12)
+    V = 70001
+    x = (rng.standard_normal((150, V)) * 2).astype(np.float32)
+    x[1] = -np.inf
+    x[2] = 0.25                                               # all equal
+    x[3, 5:] = np.nan
+    x[4, 100:] = -3.4028235e38
+    x[5, 69000] = np.inf
+    x[6] = np.floor(x[6])                                     # few values, thousands of times each
+    x[7] *= 20
+    u = rng.random(150)
+    u[:3] = [0.0, 0.5, 0.999]
+    tok, prob = run(x, u, pad=2, **f)
+    for n in (1, 9, 30, 40, 70, 100):
+        t, p = run(x[:n], u[:n], pad=2, **f)
+        assert np.array_equal(t, tok[:n]) and np.array_equal(p, prob[:n]), n
+
+
 def test_a_captured_call_replays_on_new_logits_and_on_another_stream():
     import torch
     from paper_2602_07306_b200 import pt
