@@ -19,6 +19,12 @@
 // turns on its key tiles with a running maximum, sum and accumulator each, and the first merges both at the end.  Barriers
 // count over all segments of a block, so the copies of the next segment start while the last one's output is being written.
 // Every wait is bounded; on a timeout the block records PT_ERR_DEVICE_TIMEOUT and every role leaves.
+//
+// Measured (head_dim 128): eight users' speculated tokens over 2k keys (8 tracks, 8 heads) 101 us, 0.74 of the copy bandwidth; four
+// users' over 9k to 31k keys 127 us, 0.85: bound by the K and V stream and the start and merge around it.  2048 tokens over
+// 32k keys (2 tracks, 8 heads on one KV head) 452 us, 1.15 PFLOP/s: a step of 128 keys of two tiles takes 4.0k cycles against 2.05k of
+// products; a softmax takes 1.5 to 1.8k, bound by instruction issue, and waits for its own tile's products before and after.
+// Scores in halves of 64 keys with two buffers per tile took 843 us (a product of 64 columns costs nearly one of 128).
 #include "pt_chunk.h"
 #include "pt_tcgen05.cuh"
 
@@ -31,7 +37,7 @@ constexpr int kStK = 3, kStV = 2;              // ring depths: head_dim 128: 2 Q
 constexpr int kMaxBlocks = 148;
 // Cost of a segment in units of about 0.37 us: once for starting and writing it, and per key tile, with one row tile (bound
 // by its share of the HBM bandwidth) and with two (bound by the softmax and the products).
-// (Measured: a batch of 27 decoding sequences and a 777-token chunk takes 206 us with kCost2 = 7, 177 with 9, 187 with 11.)
+// (Measured: 27 decoding sequences beside a 777-token chunk take 158 to 164 us with kCost2 from 7 to 9, 169 with kSeg2 = 14.)
 constexpr int kSeg1 = 9, kSeg2 = 20, kCost1 = 4, kCost2 = 9;
 constexpr int kMinUnits = kSeg1 + kCost1;      // a range is no shorter
 
@@ -652,7 +658,7 @@ k_chunk_tc(const __grid_constant__ CUtensorMap qmap, const __grid_constant__ CUt
 
 // Merges the parts of cut segments.  Block (c, g) handles the segment that is cut at the start of range c + 1, if no earlier
 // range's start cuts it too: parts lie in range c (second slot) and, as long as the segment goes on, in c + 1, c + 2, ...
-// (first slot).  g: rows 32 g .. 32 g + 31 of its 256, a lane each, 16 columns a warp.
+// (first slot).  g: rows 32 g .. 32 g + 31 of its 256, a lane each, 16 columns a warp (128 / 16 warps at most).
 constexpr int kCombineThreads = 256;
 template <int DH>
 __global__ void __launch_bounds__(kCombineThreads)
@@ -660,54 +666,72 @@ k_chunk_combine(const ChunkP p, float* scratch, const int tpt, const int blocks,
     grid_dep_wait();
     grid_dep_launch();
     const Slots<DH> at{scratch};
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const Start sg = *at.start(blockIdx.x + 1);
+    // A lane has the start of range c + base + lane: the ranges of a segment are looked up 32 at a time.
+    int base = 0, from_p0, from_len;
+    auto look = [&]() {
+        const int c = blockIdx.x + base + lane;
+        const Start* st = at.start(min(c, blocks - 1));
+        from_p0 = st->p0; from_len = c < blocks ? st->len : 0;
+    };
+    look();
     const int n = max(sg.n0, sg.n1);
     if (sg.len == 0 || sg.lo == 0 || sg.lo >= n) return;           // the segment is not cut at this range's start
-    const int seg_start = sg.p0 + sg.u;
-    // first key tile of the segment that belongs to range c or a later one; behind the last range, all are before
-    auto lo_of = [&](int c) {
-        if (c >= blocks || at.start(c)->len == 0) return n;
-        return min(n, Walk::first_at(min(at.start(c)->p0 - seg_start, seg_cost(sg.left, n * 128, tpt, sh)), sg.n1 > 0, sh));
+    const int seg_start = sg.p0 + sg.u, seg_len = seg_cost(sg.left, n * 128, tpt, sh);
+    // first key tile of the segment that belongs to range c + k or a later one (k ascending); behind the last range, all are before
+    auto lo_of = [&](int k) {
+        if (k - base >= 32) { base = k; look(); }
+        const int lo = from_len == 0 ? n : min(n, Walk::first_at(min(from_p0 - seg_start, seg_len), sg.n1 > 0, sh));
+        return __shfl_sync(0xffffffffu, lo, k - base);
     };
-    if (lo_of(blockIdx.x) > 0) return;                             // an earlier range's start cuts it already
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    if (lo_of(0) > 0) return;                                      // an earlier range's start cuts it already
     const int G = p.nq / p.nkv;
-    const Slots<DH> slots{scratch};
     const int i = blockIdx.y >> 2;                                 // row tile
     const int n_i = i ? sg.n1 : sg.n0;
     if (sg.lo >= n_i) return;                                      // this tile's keys all lie in the first part: written there
     const int r = (blockIdx.y & 3) * 32 + lane, tok = r / G, tok_i = i * tpt;
     const bool live = tok < tpt && tok_i + tok < sg.left;
-    for (int col = warp * 16; col < DH; col += kCombineThreads / 32 * 16) {
-        float m = -INFINITY, l = 0.f, o[16];
+    const int col = warp * 16;
+    if (col >= DH) return;
+    float m = -INFINITY, l = 0.f, o[16];
 #pragma unroll
-        for (int e = 0; e < 16; ++e) o[e] = 0.f;
-        for (int c = blockIdx.x, lo = 0; lo < n_i; ++c) {
-            const int hi = c == (int)blockIdx.x ? sg.lo : lo_of(c + 1);     // tiles [lo, hi) belong to range c
-            if (lo < min(hi, n_i) && live) {
-                const int which = c == (int)blockIdx.x ? 1 : 0;
-                const float2 st = slots.stats(c, which)[i * 128 + r];
-                const float* src = slots.out(c, which) + (size_t)col * 256 + i * 128 + r;
-                float x[16];
+    for (int e = 0; e < 16; ++e) o[e] = 0.f;
+    constexpr int kAhead = 2;                                      // parts that are loaded before the first of them is merged (4: no faster)
+    for (int k = 0, lo = 0; lo < n_i;) {
+        float2 st[kAhead];
+        float x[kAhead][16];
 #pragma unroll
-                for (int e = 0; e < 16; ++e) x[e] = src[e * 256];
-                const float top = fmaxf(m, st.x);
-                if (top > -INFINITY) {
-                    const float f0 = exp2f(m - top), f1 = exp2f(st.x - top);
-                    m = top; l = l * f0 + st.y * f1;
+        for (int a = 0; a < kAhead; ++a) {
+            const int hi = k == 0 ? sg.lo : lo < n_i ? lo_of(k + 1) : lo;     // tiles [lo, hi) belong to range c + k
+            const bool some = lo < min(hi, n_i);
+            st[a] = make_float2(-INFINITY, 0.f);
+            if (some && live) {
+                const int which = k == 0 ? 1 : 0;
+                st[a] = at.stats(blockIdx.x + k, which)[i * 128 + r];
+                const float* src = at.out(blockIdx.x + k, which) + (size_t)col * 256 + i * 128 + r;
 #pragma unroll
-                    for (int e = 0; e < 16; ++e) o[e] = o[e] * f0 + x[e] * f1;
-                }
+                for (int e = 0; e < 16; ++e) x[a][e] = src[e * 256];
             }
-            lo = hi;
+            if (lo < n_i) { lo = hi; ++k; }
         }
-        if (!live) continue;
-        const float inv = l > 0.f ? 1.0f / l : 0.f;
-        uint32_t u[8];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) u[e] = pack_bf16(o[2 * e] * inv, o[2 * e + 1] * inv);
-        st_global_32(p.o + ((size_t)sg.t * p.M + sg.row0 + tok_i + tok) * (size_t)(p.nq * DH) + (size_t)(sg.kvh * G + r % G) * DH + col, u);
+        for (int a = 0; a < kAhead; ++a) {
+            const float top = fmaxf(m, st[a].x);
+            if (st[a].x > -INFINITY) {
+                const float f0 = exp2f(m - top), f1 = exp2f(st[a].x - top);
+                m = top; l = l * f0 + st[a].y * f1;
+#pragma unroll
+                for (int e = 0; e < 16; ++e) o[e] = o[e] * f0 + x[a][e] * f1;
+            }
+        }
     }
+    if (!live) return;
+    const float inv = l > 0.f ? 1.0f / l : 0.f;
+    uint32_t u[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) u[e] = pack_bf16(o[2 * e] * inv, o[2 * e + 1] * inv);
+    st_global_32(p.o + ((size_t)sg.t * p.M + sg.row0 + tok_i + tok) * (size_t)(p.nq * DH) + (size_t)(sg.kvh * G + r % G) * DH + col, u);
 }
 
 template <int DH>
