@@ -308,10 +308,10 @@ pt_status pt_generate(pt_model* m, pt_kv_cache* c, const int32_t* dev_prompt, in
  *   min_p   keeps, of those, the tokens with w_i >= min_p (<= 0 or NaN: off; above 1: as 1)
  * and the token drawn is the lowest index whose cumulative kept weight (summed in index order) exceeds u times the kept
  * sum; u outside [0, 1) (or NaN) counts as the nearest end.  A temperature that is not a positive finite number chooses
- * greedily (the lowest index of the largest logit, probability 1); others count as the nearest value in [1e-30, 1e36].  NaN and -inf logits are masked; a row with nothing else gives token 0
- * and probability 0.  +inf logits share the whole weight.  Weights are held as multiples of 2^-44 of the largest: a token
- * more than 31 nats (after the temperature) below it is never drawn.  The result does not depend on the batch, and every
- * call with the same arguments gives the same bits.
+ * greedily (the lowest index of the largest logit, probability 1); others count as the nearest value in [1e-30, 1e36].
+ * NaN and -inf logits are masked; a row with nothing else gives token 0 and probability 0.  +inf logits share the whole
+ * weight.  Weights are held as multiples of 2^-44 of the largest: a token more than 31 nats (after the temperature) below
+ * it is never drawn.  The result does not depend on the batch, and every call with the same arguments gives the same bits.
  *   logits       device [n] rows of `vocab` values `row_stride` elements apart, fp32 or bf16 (dtype: a pt_dtype)
  *   u            device fp32 [n], the random numbers, uniform in [0, 1)
  *   temperature, top_p, min_p   device fp32 [n] or NULL (off; temperature 1);  top_k   device int32 [n] or NULL

@@ -68,7 +68,9 @@ pt_status pt_kernel_prefill_attn(const void* q, const void* pool_l, int64_t pool
  *   out[t][r][h] = softmax_{j <= pos}( q[t][r][h] . K[t][b][h / G][j] / sqrt(dh) ) V[t][b][h / G][j],
  *   r = q_len[0] + .. + q_len[b - 1] + s,   pos = kv_len[b] - q_len[b] + s,   G = nq / nkv <= 8.
  *   q, out        device bf16 [T][M][nq*dh], 16-byte and 32-byte aligned; rows behind the last sequence are not touched
- *   pool_l, block_table   as for pt_kernel_decode_attn (entries behind a sequence's last page are not read)
+ *   pool_l, block_table   as for pt_kernel_decode_attn (entries behind a sequence's last page are not read).  What lies
+ *                 behind a sequence's last key is never used; a V of a later token of the sequence meets the weight 0, so
+ *                 V that is not finite may make earlier rows NaN (in a plain softmax as well), K that is not cannot
  *   q_len, kv_len DEVICE int32 [B]: a captured call may be replayed with other lengths.  Lengths out of range (negative,
  *                 kv_len < q_len, kv_len > maxp*ps, sum of q_len > M) are reported in `status` and nothing is written
  *   impl          0 = tensor-memory kernel (tcgen05; head_dim 64 or 128, pages of a multiple of 16 tokens), 1 = plain

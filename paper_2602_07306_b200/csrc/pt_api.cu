@@ -657,9 +657,11 @@ static pt_status forward(pt_model* m, pt_kv_cache* c, const void* x, int64_t x_s
 }
 
 pt_status pt_extend(pt_model* m, pt_kv_cache* c, const void* x, int64_t x_track_stride, int32_t B, const int32_t* n_tokens,
-                    const int32_t* seq_ids, void* out_h, void* workspace, size_t ws_bytes, void* stream) {
+                    const int32_t* seq_ids, void* out_h, void* workspace, size_t ws_bytes, void* stream) try {
     if (!n_tokens) PT_FAIL(PT_ERR_INVALID_ARG, "null argument");
     return forward(m, c, x, x_track_stride, B, 1, n_tokens, seq_ids, out_h, workspace, ws_bytes, stream, false);
+} catch (const std::bad_alloc&) {
+    PT_FAIL(PT_ERR_INVALID_ARG, "out of host memory");
 }
 
 pt_status pt_prefill(pt_model* m, pt_kv_cache* c, const void* x, int64_t x_track_stride,

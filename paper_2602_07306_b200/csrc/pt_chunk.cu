@@ -138,6 +138,7 @@ extern "C" pt_status pt_kernel_chunk_attn(const void* q, const void* pool_l, int
     if ((uintptr_t)q % 16 || (uintptr_t)pool_l % 16 || pool_track_stride % 8 || (uintptr_t)out % 32 || (uintptr_t)scratch % 256) {
         set_error("q and the pool must be 16-byte aligned (its track stride a multiple of 8 elements), out 32-byte, scratch 256-byte"); return PT_ERR_MISALIGNED;
     }
+    if (((uintptr_t)block_table | (uintptr_t)q_len | (uintptr_t)kv_len | (uintptr_t)status) % 4) { set_error("block_table, q_len, kv_len and status must be 4-byte aligned"); return PT_ERR_MISALIGNED; }
     const size_t need = chunk_scratch_bytes(T, B, nq, dh);
     if (scratch_bytes < need) { set_error("scratch: %zu < %zu bytes", scratch_bytes, need); return PT_ERR_BUFFER_TOO_SMALL; }
     ChunkP p{};

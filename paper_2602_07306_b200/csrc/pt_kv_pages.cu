@@ -6,6 +6,7 @@
 // (no upload, no buffer, and a captured launch keeps its own list).
 #include <algorithm>
 #include <cstring>
+#include <new>
 #include <vector>
 
 #include "pt_internal.h"
@@ -103,11 +104,10 @@ void CowPlan::plan(const pt_kv_cache* c, const int32_t* seqs, const int32_t* add
             if (l->second <= 1) continue;
             l->second -= 1;
             const bool keep = (int64_t)p * c->ps < s.len;
-            const int32_t fresh = c->free_list[pages_needed < c->free_list.size() ? pages_needed : 0];
-            ++pages_needed;
+            if (++pages_needed > c->free_list.size()) return;     // too many: the call is refused
+            const int32_t fresh = c->free_list[pages_needed - 1];
             entries.push_back({seqs[i], (int32_t)p, fresh});
             if (keep) { src.push_back(page); dst.push_back(fresh); }
-            if (pages_needed > c->free_list.size()) return;
         }
     }
 }
@@ -127,10 +127,12 @@ void CowPlan::commit(pt_kv_cache* c) const {
 using namespace pt;
 
 #define KV_FAIL(code, ...) do { set_error(__VA_ARGS__); return (code); } while (0)
+// Host memory that runs out ends a call here, with the cache as it was: what can throw comes before what changes it.
+#define KV_CATCH catch (const std::bad_alloc&) { KV_FAIL(PT_ERR_INVALID_ARG, "out of host memory"); }
 
 extern "C" {
 
-pt_status pt_kv_seq_fork(pt_kv_cache* c, int32_t src, int32_t dst, int32_t len) {
+pt_status pt_kv_seq_fork(pt_kv_cache* c, int32_t src, int32_t dst, int32_t len) try {
     if (!c) KV_FAIL(PT_ERR_INVALID_ARG, "null argument");
     auto it = c->seqs.find(src);
     if (it == c->seqs.end()) KV_FAIL(PT_ERR_STATE, "unknown sequence %d", src);
@@ -140,10 +142,10 @@ pt_status pt_kv_seq_fork(pt_kv_cache* c, int32_t src, int32_t dst, int32_t len) 
     Seq s;
     s.len = len;
     s.pages.assign(it->second.pages.begin(), it->second.pages.begin() + (len + c->ps - 1) / c->ps);
-    for (int32_t p : s.pages) c->ref[p] += 1;
-    c->seqs.emplace(dst, std::move(s));
+    const auto& pages = c->seqs.emplace(dst, std::move(s)).first->second.pages;
+    for (int32_t p : pages) c->ref[p] += 1;
     return PT_OK;
-}
+} KV_CATCH
 
 pt_status pt_kv_free_pages(const pt_kv_cache* c, int32_t* n) {
     if (!c || !n) KV_FAIL(PT_ERR_INVALID_ARG, "null argument");
@@ -158,7 +160,7 @@ pt_status pt_kv_page_refs(const pt_kv_cache* c, int32_t page, int32_t* refs) {
     return PT_OK;
 }
 
-pt_status pt_kv_compact(pt_kv_cache* c, int32_t* moved, void* stream) {
+pt_status pt_kv_compact(pt_kv_cache* c, int32_t* moved, void* stream) try {
     if (!c) KV_FAIL(PT_ERR_INVALID_ARG, "null argument");
     const int32_t used = c->num_pages - (int32_t)c->free_list.size();
     std::vector<int32_t> src, dst, to(c->num_pages, -1);
@@ -169,18 +171,19 @@ pt_status pt_kv_compact(pt_kv_cache* c, int32_t* moved, void* stream) {
         src.push_back(p); dst.push_back(hole);
         to[p] = hole++;
     }
+    std::deque<int32_t> free_list;
+    for (int32_t p = used; p < c->num_pages; ++p) free_list.push_back(p);
     pt_status s = launch_copy_pages(c, c->pool, c->scales, c->num_pages, c->pool, c->scales, c->num_pages, src.data(), dst.data(), (int)src.size(), (cudaStream_t)stream);
     if (s != PT_OK) return s;
     for (auto& e : c->seqs)
         for (int32_t& p : e.second.pages) if (to[p] >= 0) p = to[p];
     for (size_t i = 0; i < src.size(); ++i) { c->ref[dst[i]] = c->ref[src[i]]; c->ref[src[i]] = 0; }
-    c->free_list.clear();
-    for (int32_t p = used; p < c->num_pages; ++p) c->free_list.push_back(p);
+    c->free_list.swap(free_list);
     if (moved) *moved = (int32_t)src.size();
     return PT_OK;
-}
+} KV_CATCH
 
-pt_status pt_kv_move_pool(pt_kv_cache* c, int32_t num_pages, void* dev_pool, size_t bytes, void* stream) {
+pt_status pt_kv_move_pool(pt_kv_cache* c, int32_t num_pages, void* dev_pool, size_t bytes, void* stream) try {
     if (!c || !dev_pool) KV_FAIL(PT_ERR_INVALID_ARG, "null argument");
     size_t need = 0, codes = 0;
     pt_status s = kv_pool_layout(c->m, num_pages, c->ps, c->kv_dtype, &codes, &need);
@@ -193,6 +196,8 @@ pt_status pt_kv_move_pool(pt_kv_cache* c, int32_t num_pages, void* dev_pool, siz
     std::vector<int32_t> src, dst, to(c->num_pages, -1), ref(num_pages, 0);
     for (int32_t p = 0; p < c->num_pages; ++p)
         if (c->ref[p]) { to[p] = (int32_t)src.size(); ref[src.size()] = c->ref[p]; dst.push_back(to[p]); src.push_back(p); }
+    std::deque<int32_t> free_list;
+    for (int32_t p = used; p < num_pages; ++p) free_list.push_back(p);
     float* scales = c->scales ? (float*)((char*)dev_pool + codes) : nullptr;
     s = launch_copy_pages(c, c->pool, c->scales, c->num_pages, (char*)dev_pool, scales, num_pages, src.data(), dst.data(), (int)src.size(), (cudaStream_t)stream);
     if (s != PT_OK) return s;
@@ -201,16 +206,16 @@ pt_status pt_kv_move_pool(pt_kv_cache* c, int32_t num_pages, void* dev_pool, siz
     c->pool = (char*)dev_pool; c->scales = scales; c->bytes = bytes; c->num_pages = num_pages;
     c->slab_elems = c->page_elems * num_pages;
     c->ref.swap(ref);
-    c->free_list.clear();
-    for (int32_t p = used; p < num_pages; ++p) c->free_list.push_back(p);
+    c->free_list.swap(free_list);
     return PT_OK;
-}
+} KV_CATCH
 
 pt_status pt_kernel_kv_copy_pages(const void* src_pool, int32_t src_pages, void* dst_pool, int32_t dst_pages,
-                                  int64_t slabs, int64_t page_bytes, const int32_t* src, const int32_t* dst, int32_t n, void* stream) {
+                                  int64_t slabs, int64_t page_bytes, const int32_t* src, const int32_t* dst, int32_t n, void* stream) try {
     if (!src_pool || !dst_pool || n < 0 || (n > 0 && (!src || !dst))) KV_FAIL(PT_ERR_INVALID_ARG, "bad argument");
     if (src_pages < 1 || dst_pages < 1 || slabs < 1 || page_bytes < 16 || page_bytes % 16 || page_bytes > (1 << 30))
         KV_FAIL(PT_ERR_INVALID_ARG, "sizes must be positive, page_bytes a multiple of 16 up to 2^30");
+    if (slabs > (1ll << 62) / page_bytes / std::max(src_pages, dst_pages)) KV_FAIL(PT_ERR_INVALID_ARG, "a pool of more than 2^62 bytes");
     if ((uintptr_t)src_pool % 16 || (uintptr_t)dst_pool % 16) KV_FAIL(PT_ERR_MISALIGNED, "pools must be 16-byte aligned");
     const bool same = src_pool == dst_pool;
     if (same && src_pages != dst_pages) KV_FAIL(PT_ERR_INVALID_ARG, "one pool, two page counts");
@@ -227,6 +232,6 @@ pt_status pt_kernel_kv_copy_pages(const void* src_pool, int32_t src_pages, void*
         if (written[src[i] >> 6] >> (src[i] & 63) & 1) KV_FAIL(PT_ERR_INVALID_ARG, "page %d is read and written", src[i]);
     Plane pl{a, (char*)dst_pool, src_pages * page_bytes, dst_pages * page_bytes, page_bytes};
     return copy_plane(pl, slabs, src, dst, n, (cudaStream_t)stream);
-}
+} KV_CATCH
 
 }  // extern "C"

@@ -278,6 +278,9 @@ pt_status pt_generate_sample(pt_model* m, pt_kv_cache* c, const int32_t* dev_pro
                              const int32_t* seq_ids, const pt_sampling* sampling, int32_t* dev_tokens_out, float* dev_logits_out,
                              void* workspace, size_t ws_bytes, void* stream) {
     if (!sampling || !sampling->u) { set_error("null argument"); return PT_ERR_INVALID_ARG; }
+    if (((uintptr_t)sampling->u | (uintptr_t)sampling->temperature | (uintptr_t)sampling->top_k | (uintptr_t)sampling->top_p | (uintptr_t)sampling->min_p | (uintptr_t)sampling->prob) % 4) {
+        set_error("the sampling arrays must be aligned to their types"); return PT_ERR_MISALIGNED;
+    }
     if (m && m->lm_buf && (sample_vocab_limit() < m->lm_vocab)) { set_error("vocab %d > %d", m->lm_vocab, sample_vocab_limit()); return PT_ERR_UNSUPPORTED; }
     return generate(m, c, dev_prompt, B, S, n_new, seq_ids, sampling, dev_tokens_out, dev_logits_out, workspace, ws_bytes, stream);
 }

@@ -1083,7 +1083,9 @@ extern "C" pt_status pt_sample(const void* logits, int32_t dtype, int64_t row_st
     if (dtype != PT_F32 && dtype != PT_BF16) { set_error("dtype must be PT_F32 or PT_BF16"); return PT_ERR_INVALID_ARG; }
     if (n < 1 || n > (1 << 24) || vocab < 1 || row_stride < vocab) { set_error("n outside [1, 2^24], vocab < 1 or row_stride < vocab"); return PT_ERR_INVALID_ARG; }
     if (vocab > sample_vocab_limit()) { set_error("vocab %d > %d", vocab, sample_vocab_limit()); return PT_ERR_UNSUPPORTED; }
-    if ((uintptr_t)logits % (dtype == PT_F32 ? 4 : 2) || (uintptr_t)token % 4) { set_error("logits must be aligned to their type, token 4-byte aligned"); return PT_ERR_MISALIGNED; }
+    if ((uintptr_t)logits % (dtype == PT_F32 ? 4 : 2) || ((uintptr_t)u | (uintptr_t)temperature | (uintptr_t)top_k | (uintptr_t)top_p | (uintptr_t)min_p | (uintptr_t)token | (uintptr_t)prob) % 4) {
+        set_error("the arrays must be aligned to their types"); return PT_ERR_MISALIGNED;
+    }
     SampleP p{};
     p.logits = logits; p.row_stride = row_stride; p.vocab = vocab; p.u = u;
     p.temperature = temperature; p.top_k = top_k; p.top_p = top_p; p.min_p = min_p;

@@ -625,10 +625,19 @@ def sample(logits, u, temperature=None, top_k=None, top_p=None, min_p=None, *, o
     return out, prob
 
 
+def _page_ids(ids):
+    """ids as a contiguous int32 array; numbers that are not whole or do not fit are refused, not cut."""
+    a = np.asarray(ids)
+    b = np.ascontiguousarray(a, np.int32)
+    if a.dtype != np.int32 and not np.array_equal(a, b):
+        raise ValueError("page numbers: whole numbers of 32 bits are wanted")
+    return b
+
+
 def kernel_kv_copy_pages(pool, src, dst, *, scales=None, out=None, out_scales=None):
     """Pages src[i] of pool [T, L, pages, ...] (any type) to its pages dst[i] in every (track, layer) slab; `scales`
     [T, L, pages, ...] likewise.  src, dst: host integers.  `out`, `out_scales`: another pool to copy to."""
-    src, dst = np.ascontiguousarray(src, np.int32), np.ascontiguousarray(dst, np.int32)
+    src, dst = _page_ids(src), _page_ids(dst)
     if src.ndim != 1 or src.shape != dst.shape:
         raise ValueError("src and dst: two lists of the same length are wanted")
     index = pool.get_device()
@@ -645,6 +654,8 @@ def kernel_kv_copy_pages(pool, src, dst, *, scales=None, out=None, out_scales=No
                 (not b.is_contiguous() or a.dtype != b.dtype or b.get_device() != index or sa[:2] != sb[:2] or sa[3:] != sb[3:]):
             raise ValueError("pools: contiguous CUDA tensors [T, L, pages, ...] that differ in their pages alone are wanted")
         slabs = sa[0] * sa[1]
+        if a.numel() == 0 or b.numel() == 0:
+            raise ValueError("pools: at least one page is wanted")
         _call(index, lib().pt_kernel_kv_copy_pages, a.data_ptr(), sa[2], b.data_ptr(), sb[2], slabs, a.numel() * a.element_size() // (slabs * sa[2]), ps, pd, n)
 
 

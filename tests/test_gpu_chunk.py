@@ -131,6 +131,40 @@ def test_random_ragged_batches():
 
 
 @pytest.mark.parametrize("impl", [0, 1])
+def test_hundreds_of_sequences(impl):
+    """More sequences than a warp scans at once, most of them one token or none: a decode step in chunk form."""
+    rng = np.random.default_rng(3)
+    kv = rng.integers(0, 200, 515)
+    ql = np.minimum(rng.choice([0, 1, 1, 1, 2, 130], 515), kv)
+    kv[500:], ql[500:] = 0, 0                                 # the call's end owns nothing
+    check(1, 4, 1, 64, 16, ql.tolist(), kv.tolist(), impl, seed=4)
+
+
+def test_two_calls_at_once_with_a_scratch_each():
+    import torch
+    from paper_2602_07306_b200 import pt
+    d = lambda a: torch.from_numpy(np.ascontiguousarray(a)).cuda()
+    calls = []
+    for i, (ql, kl) in enumerate((([300, 1, 5], [3000, 900, 4000]), ([4, 4, 250], [5000, 40, 260]))):
+        q, pool, bt = case(2, 8, 2, 128, 16, ql, kl, seed=20 + i)
+        calls.append((d(q.reshape(2, sum(ql), -1)).bfloat16(), d(pool).bfloat16(), d(bt), d(np.array(ql, np.int32)), d(np.array(kl, np.int32))))
+    kw = dict(nq=8, nkv=2, dh=128, ps=16)
+    want = [pt.kernel_chunk_attn(*c, **kw)[0].clone() for c in calls]
+    streams = [torch.cuda.Stream() for _ in calls]
+    scratch = [pt.chunk_attn_scratch(2, 3, 8, 128, "cuda") for _ in calls]
+    status = torch.zeros((2, 16), dtype=torch.int32, device="cuda")
+    outs = [[torch.zeros_like(c[0]) for _ in range(10)] for c in calls]
+    torch.cuda.synchronize()
+    for r in range(10):
+        for i, c in enumerate(calls):
+            with torch.cuda.stream(streams[i]):
+                pt.kernel_chunk_attn(*c, **kw, out=outs[i][r], scratch=scratch[i], status=status[i])
+    torch.cuda.synchronize()
+    assert status.any().item() is False
+    assert all(torch.equal(o, want[i]) for i in range(2) for o in outs[i])
+
+
+@pytest.mark.parametrize("impl", [0, 1])
 def test_scores_that_climb_and_large_scores(impl):
     """Running maxima that have to be raised again and again, and scores far beyond what exp2 takes unshifted."""
     T, nq, nkv, dh, ps, q_len, kv_len = 1, 4, 2, 128, 16, [6, 140], [900, 1700]

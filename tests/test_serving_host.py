@@ -115,6 +115,39 @@ def test_page_copy_refusals(lib):
     assert lib.pt_kernel_kv_copy_pages(None, 4, FAKE, 4, 2, 512, None, None, 0, None) == 1
 
 
+def test_sizes_that_overflow_and_pointers_off_their_type_are_refused(lib):
+    ids = [C.cast(i32([i]), C.c_void_p) for i in (0, 1)]
+    for slabs, pages, pb in ((1 << 62, 4, 512), (1 << 40, 1 << 30, 1 << 29), ((1 << 63) - 1, 2, 16)):
+        assert lib.pt_kernel_kv_copy_pages(FAKE, pages, FAKE, pages, slabs, pb, ids[0], ids[1], 1, None) == 1 and b"2^62" in lib.pt_last_error()
+    odd = C.c_void_p(0x10002)
+    for i in range(5, 12):                                        # u, temperature, top_k, top_p, min_p, token, prob
+        args = [FAKE, 0, 10, 3, 10, FAKE, None, None, None, None, FAKE, None, None]
+        args[i] = odd
+        assert lib.pt_sample(*args) == 6, i
+    n = C.c_size_t()
+    assert lib.pt_kernel_chunk_attn_scratch_bytes(2, 3, 8, 128, C.byref(n)) == 0
+    for i in (3, 5, 6, 19):                                       # block_table, q_len, kv_len, status
+        args = [FAKE, FAKE, 1 << 20, FAKE, 4, FAKE, FAKE, 2, 3, 5, 8, 2, 128, 16, 9, FAKE, 0, FAKE, n.value, FAKE, None]
+        args[i] = odd
+        assert lib.pt_kernel_chunk_attn(*args) == 6, i
+    rc, h = make(lib, dtype=pt.PT_BF16)
+    c, _ = _cache(lib, h, 6, 16, esz=2)
+    for f in ("u", "temperature", "top_k", "top_p", "min_p", "prob"):
+        sp = pt.pt_sampling(u=FAKE.value)
+        setattr(sp, f, odd.value)
+        assert lib.pt_generate_sample(h, c, FAKE, 1, 4, 2, i32([0]), C.byref(sp), FAKE, None, FAKE, 1 << 30, None) == 6, f
+    lib.pt_kv_cache_free(c)
+    lib.pt_model_destroy(h)
+
+
+def test_python_page_numbers_are_not_cut():
+    assert pt._page_ids([]).dtype == np.int32 and pt._page_ids(range(3)).tolist() == [0, 1, 2]
+    assert pt._page_ids(np.array([5.0, 7.0])).tolist() == [5, 7]
+    for bad in (np.array([2 ** 32 + 1]), np.array([0.5]), [1.25, 2]):
+        with pytest.raises(ValueError):
+            pt._page_ids(bad)
+
+
 def test_sample_refusals(lib):
     def go(logits=FAKE, dtype=0, stride=10, n=3, vocab=10, u=FAKE, token=FAKE):
         return lib.pt_sample(logits, dtype, stride, n, vocab, u, None, None, None, None, token, None, None)
