@@ -627,11 +627,32 @@ def sample(logits, u, temperature=None, top_k=None, top_p=None, min_p=None, *, o
 
 def _page_ids(ids):
     """ids as a contiguous int32 array; numbers that are not whole or do not fit are refused, not cut."""
+    if type(ids) is np.ndarray and ids.dtype == np.int32 and ids.flags.c_contiguous:
+        return ids
     a = np.asarray(ids)
     b = np.ascontiguousarray(a, np.int32)
     if a.dtype != np.int32 and not np.array_equal(a, b):
         raise ValueError("page numbers: whole numbers of 32 bits are wanted")
     return b
+
+
+def _host_ptr(a):
+    """A call's argument for the data of a contiguous int32 array (which the caller keeps)."""
+    try:
+        return C.byref(_I32.from_buffer(a))      # a third of the time of a.ctypes
+    except (TypeError, ValueError, BufferError):  # read-only, or empty
+        return a.ctypes.data
+
+
+def _copy_plane(index, a, b, src, dst, n):
+    sa, sb = a.shape, b.shape
+    if a.get_device() != index or not a.is_contiguous() or index < 0 or b is not a and \
+            (not b.is_contiguous() or a.dtype != b.dtype or b.get_device() != index or sa[:2] != sb[:2] or sa[3:] != sb[3:]):
+        raise ValueError("pools: contiguous CUDA tensors [T, L, pages, ...] that differ in their pages alone are wanted")
+    slabs = sa[0] * sa[1]
+    if a.numel() == 0 or sb[2] == 0:
+        raise ValueError("pools: at least one page is wanted")
+    _call(index, lib().pt_kernel_kv_copy_pages, a.data_ptr(), sa[2], b.data_ptr(), sb[2], slabs, a.nbytes // (slabs * sa[2]), src, dst, n)
 
 
 def kernel_kv_copy_pages(pool, src, dst, *, scales=None, out=None, out_scales=None):
@@ -640,23 +661,10 @@ def kernel_kv_copy_pages(pool, src, dst, *, scales=None, out=None, out_scales=No
     src, dst = _page_ids(src), _page_ids(dst)
     if src.ndim != 1 or src.shape != dst.shape:
         raise ValueError("src and dst: two lists of the same length are wanted")
-    index = pool.get_device()
-    ps, pd, n = src.__array_interface__["data"][0], dst.__array_interface__["data"][0], len(src)
-    for a, b in ((pool, out), (scales, out_scales)):
-        if a is None:
-            continue
-        sa = a.shape
-        if b is None:
-            b, sb = a, sa
-        else:
-            sb = b.shape
-        if not (a.is_cuda and a.is_contiguous()) or a.get_device() != index or b is not a and \
-                (not b.is_contiguous() or a.dtype != b.dtype or b.get_device() != index or sa[:2] != sb[:2] or sa[3:] != sb[3:]):
-            raise ValueError("pools: contiguous CUDA tensors [T, L, pages, ...] that differ in their pages alone are wanted")
-        slabs = sa[0] * sa[1]
-        if a.numel() == 0 or b.numel() == 0:
-            raise ValueError("pools: at least one page is wanted")
-        _call(index, lib().pt_kernel_kv_copy_pages, a.data_ptr(), sa[2], b.data_ptr(), sb[2], slabs, a.numel() * a.element_size() // (slabs * sa[2]), ps, pd, n)
+    index, ps, pd, n = pool.get_device(), _host_ptr(src), _host_ptr(dst), len(src)
+    _copy_plane(index, pool, pool if out is None else out, ps, pd, n)
+    if scales is not None:
+        _copy_plane(index, scales, scales if out_scales is None else out_scales, ps, pd, n)
 
 
 def chunk_attn_scratch(T: int, B: int, nq: int, dh: int, device="cuda:0"):
