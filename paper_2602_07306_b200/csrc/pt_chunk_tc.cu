@@ -521,6 +521,7 @@ k_chunk_tc(const __grid_constant__ CUtensorMap qmap, const __grid_constant__ CUt
 #pragma unroll
                 for (int cc = 0; cc < 4; ++cc) tm_ld32(t_s + cc * 32, v + cc * 32);
                 tm_wait_ld();
+                tm_pin<128>(v);
                 if (key0 + 127 > tile_limit) {
 #pragma unroll
                     for (int e = 0; e < 128; ++e) if (key0 + e > limit) v[e] = -INFINITY;
@@ -545,6 +546,7 @@ k_chunk_tc(const __grid_constant__ CUtensorMap qmap, const __grid_constant__ CUt
                             float o[32];
                             tm_ld32(t_o + cc * 32, o);
                             tm_wait_ld();
+                            tm_pin<32>(o);
 #pragma unroll
                             for (int e = 0; e < 32; ++e) o[e] *= corr;
                             tm_st32(t_o + cc * 32, o);
@@ -602,9 +604,14 @@ k_chunk_tc(const __grid_constant__ CUtensorMap qmap, const __grid_constant__ CUt
                     float o1[32];
                     tm_ld32(t_o + DH + cc * 32, o1);
                     tm_wait_ld();
+                    tm_pin<32>(o);
+                    tm_pin<32>(o1);
 #pragma unroll
                     for (int e = 0; e < 32; ++e) o[e] = o[e] * f0 + (f1 > 0.f ? o1[e] * f1 : 0.f);
-                } else tm_wait_ld();
+                } else {
+                    tm_wait_ld();
+                    tm_pin<32>(o);
+                }
             };
             if (any) {
             if (sg.lo == 0 && end == n_i) {                        // all of the tile's keys: the result
