@@ -819,8 +819,20 @@ k_sample(const SampleP p, const int slice) {
     u64 above, whole;
     if (!by_keys) {
         // ---- one pass: exact weights, and a list of the zone (without a filter: everything is kept)
-        if (!searched) { za = kBins; zb = kBins - 1; }
-        weigh(use_p || !searched, above, whole, append);
+        if (!searched && r.x_min == -INFINITY) {              // no filter: everything is kept (309 to 230 us for 1000 x 128000)
+            ws = 0;
+            unsigned n = 0;
+            each([&](int, const float4& q) {
+                if (fmaxf(fmaxf(q.x, q.y), fmaxf(q.z, q.w)) > r.x_zero) {
+                    ws += (weight_bits(r, q.x) + weight_bits(r, q.y)) + (weight_bits(r, q.z) + weight_bits(r, q.w));
+                    n += 4;
+                }
+            });
+            ws = warp_sum(ws - n * kOffset);
+        } else {
+            if (!searched) { za = kBins; zb = kBins - 1; }
+            weigh(use_p || !searched, above, whole, append);
+        }
         if (lane == 0) remote(&sh.wsum[0], 0)[rank * kWarps + warp] = ws;
         const int n = searched ? gather() : 0;
         if (!searched) sync_row();
