@@ -25,9 +25,13 @@
 // sorts them and finishes the row alone.
 // Everything else (top-p over the whole vocabulary, a large k, no filter): a histogram of the distance to the maximum in
 // kBins bins bounds, from counts alone, which bins may hold the threshold: a weight in a bin is known to the bin's width,
-// 0.8 %, and so are the sums before and behind a bin.  One pass then sums the weights above those bins exactly and lists the logits inside them, and one block sorts
-// that list and cuts it.  Where the list is too long (many equal logits), or top-p follows a large top-k, histograms with
-// exact counts and weights narrow the threshold down to one key instead.
+// 0.8 %, and so are the sums before and behind a bin.  One pass then sums the weights above those bins exactly and lists the
+// logits inside them, and one block sorts that list and cuts it.  Where the list is too long (many equal logits), or top-p
+// follows a large top-k, histograms with exact counts and weights narrow the threshold down to one key instead.
+//
+// Measured, top-k 50 / top-p 0.9 / no filter, in us: 1 x 32000 10.6 / 21 / 8.6 and 64 x 128000 19 / 53 / 24, latency of the
+// exchanges and barriers; 1000 x 128000 181 / 457 / 230 (greedy 85; reading the logits once takes 79), bound by the instructions of
+// the weights, with top-k by reading the rows twice: 296 rows in work at a time do not fit the L2.
 #include <cooperative_groups.h>
 
 #include "pt_internal.h"
@@ -135,7 +139,7 @@ struct Shared {
     int bin;
     u64 before_mass, before_cnt, total;
     int zone_a, zone_b, tail_a, tail_b, cut, first;
-    uint32_t thr; int owner; u64 target, obefore, Z;
+    uint32_t thr; int owner; u64 target, Z;
 };
 
 static_assert(kFew == 128, "the thread counts below");
