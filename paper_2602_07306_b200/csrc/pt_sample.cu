@@ -281,7 +281,7 @@ k_sample(const SampleP p, const int slice) {
     // ---- the slice (NaN counts as masked) and its maximum
     sh.coarse[tid] = 0;
     if (tid < 16) sh.root[tid] = kRoot[tid] * 17592186044416.0;     // 2^44
-    if (tid == 0) { sh.n_list = 0; sh.n_all = 0; sh.first = 0x7fffffff; }
+    if (tid == 0) { sh.n_list = 0; sh.n_all = 0; sh.first = 0x7fffffff; sh.thr = 0xffffffffu; sh.cut = 0x7fffffff; }
     if (tid < 2) {                                            // the quads at the ends: filled up with -inf
         const int v = tid ? quads - 1 : 0;
         float e[4];
@@ -759,8 +759,12 @@ k_sample(const SampleP p, const int slice) {
             for (int c = 0; c < 4; ++c) if (d[c] < (float)(kBins - 1)) atomicAdd(&sh.bins[(int)d[c]], 1u);
         });
         sync_row();
-        // every block sums its share of the bins over the blocks: PER of them a thread.  An element of bin b weighs between
-        // e^-(b + 1)d and e^-bd (a hundredth of a bin more on either side for the rounding of its number).
+        // every block sums its share of the bins over the blocks: `per` of them a thread.  An element of bin b weighs between
+        // e^-(b + 1)d and e^-bd (a hundredth of a bin more on either side for the rounding of its number), and its whole
+        // number of units, which is what decides, lies up to half a unit outside (kHalf; the exponential's last bits are
+        // relative, below).  Every one of many equal logits is rounded the same way: without it a reach within 1e-6 of 1
+        // had its threshold in another bin than the bounds said.
+        constexpr float kUnit = 0x1p-44f, kHalf = 0.5625f * kUnit;
         const int per = kBins / kThreads / CL, b0 = rank * (kBins / CL) + tid * per;
         const float d = kRange / (kBins - 1), step = __expf(-d);
         BinSum in{0, 0., 0.}, tot;
@@ -772,7 +776,7 @@ k_sample(const SampleP p, const int slice) {
 #pragma unroll
                 for (int q = 0; q < (CLUSTER ? kMaxCluster : 1); ++q) if (q < CL) c += remote(&sh.bins[0], q)[b];
                 if (CLUSTER) sh.bins[b] = c;                  // (no other block reads this block's own share here)
-                in.n += c; in.up += (double)((float)c * fu); in.dn += (double)((float)c * fd);
+                in.n += c; in.up += (double)((float)c * (fu + kHalf)); in.dn += (double)((float)c * fmaxf(fd - kHalf, 0.f));
                 fu *= step; fd *= step;
             }
         }
@@ -786,23 +790,27 @@ k_sample(const SampleP p, const int slice) {
             if (q < rank) { ec += (u64)s[0]; eu += s[1]; el += s[2]; }
             tc += (u64)s[0]; tu += s[1]; td += s[2];
         }
-        // (1e-5: the rounding of the bounds themselves, a product of up to 16 steps and a sum)
+        // (1e-5: the rounding of the bounds themselves, a product of up to 16 steps and a sum; a unit: the reach is a whole number)
         // The threshold lies in the first bin through which the weight reaches p times the whole, or, the same, behind which
         // at most 1 - p of it is left: both bounds are taken, the smaller part is the sharper one.
-        const double t_lo = td * tp * (1 - 1e-5), t_hi = tu * tp * (1 + 1e-5);
-        const double s_lo = td * (1.0 - (double)tp) * (1 - 1e-5), s_hi = tu * (1.0 - (double)tp) * (1 + 1e-5);
+        const double t_lo = td * tp * (1 - 1e-5) - kUnit, t_hi = tu * tp * (1 + 1e-5) + kUnit;
+        const double s_lo = td * (1.0 - (double)tp) * (1 - 1e-5) - kUnit, s_hi = tu * (1.0 - (double)tp) * (1 + 1e-5) + kUnit;
+        // A bin is where a sum passes its limit if the sum before it does not and the sum through it does.  A thread's first sum
+        // comes from the scan and the last of the thread before it from that thread: `eps`, far above their difference (1e-14
+        // of the whole) and far below the 1e-5, keeps the passing from falling between the two.
+        const double eps = 1e-11 * tu;
         float fu = __expf(-d * ((float)b0 - 0.01f)), fd = __expf(-d * ((float)b0 + 1.01f));
         const bool k_cuts = use_k && tc > (u64)k;             // otherwise top-k removes nothing that has weight
 #pragma unroll 1
         for (int b = b0; b < b0 + per; ++b) {
             const uint32_t c = sh.bins[b];
-            const double u1 = (double)((float)c * fu), l1 = (double)((float)c * fd);
+            const double u1 = (double)((float)c * (fu + kHalf)), l1 = (double)((float)c * fmaxf(fd - kHalf, 0.f));
             if (k_cuts && ec < (u64)k && ec + c >= (u64)k)
                 for (int q = 0; q < CL; ++q) { Shared* o = remote(&sh, q); o->bin = b; o->before_cnt = ec; }
-            if (use_p && eu < t_lo && eu + u1 >= t_lo) for (int q = 0; q < CL; ++q) atomicMin(&remote(&sh, q)->zone_a, b);
-            if (use_p && el < t_hi && el + l1 >= t_hi) for (int q = 0; q < CL; ++q) atomicMin(&remote(&sh, q)->zone_b, b);
-            if (use_p && td - el > s_hi && td - (el + l1) <= s_hi) for (int q = 0; q < CL; ++q) atomicMin(&remote(&sh, q)->tail_a, b);
-            if (use_p && tu - eu > s_lo && tu - (eu + u1) <= s_lo) for (int q = 0; q < CL; ++q) atomicMin(&remote(&sh, q)->tail_b, b);
+            if (use_p && eu - eps < t_lo && eu + u1 >= t_lo) for (int q = 0; q < CL; ++q) atomicMin(&remote(&sh, q)->zone_a, b);
+            if (use_p && el - eps < t_hi && el + l1 >= t_hi) for (int q = 0; q < CL; ++q) atomicMin(&remote(&sh, q)->zone_b, b);
+            if (use_p && td - el + eps > s_hi && td - (el + l1) <= s_hi) for (int q = 0; q < CL; ++q) atomicMin(&remote(&sh, q)->tail_a, b);
+            if (use_p && tu - eu + eps > s_lo && tu - (eu + u1) <= s_lo) for (int q = 0; q < CL; ++q) atomicMin(&remote(&sh, q)->tail_b, b);
             ec += c; eu += u1; el += l1;
             fu *= step; fd *= step;
         }
