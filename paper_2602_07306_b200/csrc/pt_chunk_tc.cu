@@ -615,7 +615,7 @@ k_chunk_tc(const __grid_constant__ CUtensorMap qmap, const __grid_constant__ CUt
             };
             if (any) {
             if (sg.lo == 0 && end == n_i) {                        // all of the tile's keys: the result
-                const float inv = l_run > 0.f ? 1.0f / l_run : 0.f;
+                const float inv = 1.0f / l_run;                    // every live row sees a key: a sum of 0 or NaN is NaN in the definition too
                 __nv_bfloat16* dst = p.o + ((size_t)sg.t * p.M + sg.row0 + tok_i + tok) * (size_t)(p.nq * DH) + (size_t)(sg.kvh * G + gh) * DH;
 #pragma unroll 1
                 for (int cc = 0; cc < DH / 32; ++cc) {
@@ -730,11 +730,13 @@ k_chunk_combine(const ChunkP p, float* scratch, const int tpt, const int blocks,
                 m = top; l = l * f0 + st[a].y * f1;
 #pragma unroll
                 for (int e = 0; e < 16; ++e) o[e] = o[e] * f0 + x[a][e] * f1;
+            } else {
+                l += st[a].y;                                      // 0, or NaN: the maximum skips scores that are NaN, the sum does not
             }
         }
     }
     if (!live) return;
-    const float inv = l > 0.f ? 1.0f / l : 0.f;
+    const float inv = 1.0f / l;
     uint32_t u[8];
 #pragma unroll
     for (int e = 0; e < 8; ++e) u[e] = pack_bf16(o[2 * e] * inv, o[2 * e + 1] * inv);
