@@ -162,6 +162,7 @@ class Model:
             check(lib().pt_model_bind_weights(self.h, self.wbuf.data_ptr(), n.value))
         self.ws = None
         self.ws_key = (0, 0, 0)
+        self.ext_ws = self.gen_ws = None                # of ragged calls, of the generate loop
         self._tap = None
 
     def close(self):
@@ -237,9 +238,14 @@ class Model:
 
         def hook(user, ptr, count, stream):
             try:
-                off = ptr - self.ws.data_ptr()
-                assert 0 <= off and off + 4 * count <= self.ws.numel(), "buffer outside the workspace"
-                allreduce(self.ws[off:off + 4 * count].view(torch.float32))
+                # the buffer lies in the workspace of the call that runs: one of the model's three
+                for ws in (self.ws, self.ext_ws, self.gen_ws):
+                    off = -1 if ws is None else ptr - ws.data_ptr()
+                    if 0 <= off and off + 4 * count <= ws.numel():
+                        break
+                else:
+                    raise RuntimeError("buffer outside the workspaces")
+                allreduce(ws[off:off + 4 * count].view(torch.float32))
                 return 0
             except Exception as e:      # never let an exception cross the C boundary
                 self._ar_error = e
@@ -401,7 +407,7 @@ class Model:
         logits = torch.empty((B, n_new, self.vocab), dtype=torch.float32, device=self.device) if want_logits else None
         nb = _SZ()
         check(lib().pt_generate_workspace_bytes(self.h, B, S, cache.page_size, C.byref(nb)))
-        if getattr(self, "gen_ws", None) is None or self.gen_ws.numel() < nb.value:
+        if self.gen_ws is None or self.gen_ws.numel() < nb.value:
             self.gen_ws = None
             self.gen_ws = torch.empty(nb.value, dtype=torch.uint8, device=self.device)
         ids, pids = _i32arr(seq_ids)
