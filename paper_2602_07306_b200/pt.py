@@ -650,7 +650,8 @@ def _host_ptr(a):
         return a.ctypes.data
 
 
-def _copy_plane(index, a, b, src, dst, n):
+def _plane_args(index, a, b):
+    """Arguments of a page copy from pool a to pool b in front of its pairs, checked as far as shapes go."""
     sa, sb = a.shape, b.shape
     if a.get_device() != index or not a.is_contiguous() or index < 0 or b is not a and \
             (not b.is_contiguous() or a.dtype != b.dtype or b.get_device() != index or sa[:2] != sb[:2] or sa[3:] != sb[3:]):
@@ -658,19 +659,31 @@ def _copy_plane(index, a, b, src, dst, n):
     slabs = sa[0] * sa[1]
     if a.numel() == 0 or sb[2] == 0:
         raise ValueError("pools: at least one page is wanted")
-    _call(index, lib().pt_kernel_kv_copy_pages, a.data_ptr(), sa[2], b.data_ptr(), sb[2], slabs, a.nbytes // (slabs * sa[2]), src, dst, n)
+    return a.data_ptr(), sa[2], b.data_ptr(), sb[2], slabs, a.nbytes // (slabs * sa[2])
 
 
 def kernel_kv_copy_pages(pool, src, dst, *, scales=None, out=None, out_scales=None):
     """Pages src[i] of pool [T, L, pages, ...] (any type) to its pages dst[i] in every (track, layer) slab; `scales`
-    [T, L, pages, ...] likewise.  src, dst: host integers.  `out`, `out_scales`: another pool to copy to."""
+    [T, L, pages, ...] likewise.  src, dst: host integers.  `out`, `out_scales`: another pool to copy to (with scales: both).
+    A call that is refused has copied nothing."""
     src, dst = _page_ids(src), _page_ids(dst)
     if src.ndim != 1 or src.shape != dst.shape:
         raise ValueError("src and dst: two lists of the same length are wanted")
-    index, ps, pd, n = pool.get_device(), _host_ptr(src), _host_ptr(dst), len(src)
-    _copy_plane(index, pool, pool if out is None else out, ps, pd, n)
-    if scales is not None:
-        _copy_plane(index, scales, scales if out_scales is None else out_scales, ps, pd, n)
+    index, ps, pd, n, fn = pool.get_device(), _host_ptr(src), _host_ptr(dst), len(src), lib().pt_kernel_kv_copy_pages
+    codes = _plane_args(index, pool, pool if out is None else out)
+    if scales is None:
+        if out_scales is not None:
+            raise ValueError("out_scales without scales")
+        _call(index, fn, *codes, ps, pd, n)
+        return
+    if (out is None) != (out_scales is None):
+        raise ValueError("scales: out and out_scales are wanted together")
+    fine = _plane_args(index, scales, scales if out_scales is None else out_scales)
+    if tuple(scales.shape[:2]) != tuple(pool.shape[:2]) or fine[1] != codes[1] or fine[3] != codes[3]:
+        raise ValueError("scales: the tracks, layers and pages of the pool are wanted")
+    _call(index, fn, *fine, None, None, 0)          # without pairs: checks alignment, sizes and overlap, and launches nothing
+    _call(index, fn, *codes, ps, pd, n)
+    _call(index, fn, *fine, ps, pd, n)
 
 
 def chunk_attn_scratch(T: int, B: int, nq: int, dh: int, device="cuda:0"):
