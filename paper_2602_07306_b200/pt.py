@@ -585,17 +585,29 @@ def _call(index: int, fn, *args) -> None:
 _status_blocks = {}
 
 
+def _capturing(index: int) -> bool:
+    """Whether torch's current stream of a device is being captured into a graph."""
+    import torch
+    if torch._C._cuda_getDevice() == index:
+        return torch.cuda.is_current_stream_capturing()
+    with torch.cuda.device(index):
+        return torch.cuda.is_current_stream_capturing()
+
+
 def _new_status(index: int):
     """A zeroed int32[16] of its own on the device, for a call on its current stream: cut from a block that one fill zeroes
     for 256 calls of that stream (inside a capture, whose memory belongs to the graph: from none)."""
     import torch
-    if torch.cuda.is_current_stream_capturing():
+    if _capturing(index):
         return torch.zeros(16, dtype=torch.int32, device=index)
     key = (index, _raw_stream(index))
-    left = _status_blocks.get(key)
-    if not left:
-        left = _status_blocks[key] = list(torch.zeros((256, 16), dtype=torch.int32, device=index).unbind(0))
-    return left.pop()
+    try:
+        return _status_blocks[key].pop()            # one step: another thread may take the last
+    except (KeyError, IndexError):
+        left = list(torch.zeros((256, 16), dtype=torch.int32, device=index).unbind(0))
+        mine = left.pop()
+        _status_blocks[key] = left
+        return mine
 
 
 def _sampling_args(index, shape, **arrays):
