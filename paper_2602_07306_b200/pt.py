@@ -137,6 +137,18 @@ def _i32arr(a):
     return a, a.ctypes.data_as(C.POINTER(_I32))
 
 
+def _grown(have, want):
+    """Sizes (tokens, sequences, page size, cache format, context) of the workspace that serves `want` and what `have` served
+    (None: nothing); `have` itself where it serves.  A context that grows does so by a quarter at least: a decoding loop
+    raises it by a few tokens at a time."""
+    if have is None:
+        return want
+    most = (max(want[0], have[0]), max(want[1], have[1]), min(want[2], have[2]), max(want[3], have[3]))
+    if most == have[:4] and want[4] <= have[4]:
+        return have
+    return most + (have[4] if want[4] <= have[4] else max(want[4], have[4] + have[4] // 4),)
+
+
 class Model:
     """A PT model with its packed weights on one CUDA device (torch owns the memory)."""
 
@@ -162,7 +174,7 @@ class Model:
             check(lib().pt_model_bind_weights(self.h, self.wbuf.data_ptr(), n.value))
         self.ws = None
         self.ws_key = (0, 0, 0)
-        self.ext_ws = self.gen_ws = None                # of ragged calls, of the generate loop
+        self.ext_ws = self.gen_ws = self.ext_key = None     # of ragged calls, of the generate loop
         self._tap = None
 
     def close(self):
@@ -323,11 +335,8 @@ class Model:
         ctx = 0
         if cache.kv_dtype == PT_KV_E4M3:
             ctx = sum((cache.length(int(s)) + int(n) + 15) // 16 * 16 for s, n in zip(ids, cnt))
-        key = (M, len(ids), cache.page_size, cache.kv_dtype, ctx)
-        have = getattr(self, "ext_key", None)
-        if have is None or have[2:4] != key[2:4] or any(a < b for a, b in zip((have[0], have[1], have[4]), (M, len(ids), ctx))):
-            if have is not None and have[2:4] == key[2:4]:
-                key = (max(M, have[0]), max(len(ids), have[1]), key[2], key[3], max(ctx, have[4]))
+        key = _grown(self.ext_key, (M, len(ids), cache.page_size, cache.kv_dtype, ctx))
+        if self.ext_ws is None or key != self.ext_key:
             n = _SZ()
             check(lib().pt_extend_workspace_bytes(self.h, *key, C.byref(n)))
             self.ext_ws = None
