@@ -191,6 +191,12 @@ class Model:
     def _stream(self):
         return self.torch.cuda.current_stream(self.device).cuda_stream
 
+    def _borrow(self, ws):
+        """(address, bytes) of a workspace for a call on the current stream.  A larger one may replace it before that stream
+        has come to the call: its memory must not be handed out meanwhile."""
+        ws.record_stream(self.torch.cuda.current_stream(self.device))
+        return ws.data_ptr(), ws.numel()
+
     def set_weight(self, t: int, l: int, kind: str, w) -> None:
         """w: numpy float32 array or torch tensor, [out, in] (gains: [hidden])."""
         torch = self.torch
@@ -315,7 +321,7 @@ class Model:
         ws = self.workspace(B * S, B, cache.page_size, cache.kv_dtype, ctx)
         with torch.cuda.device(self.device):
             check(lib().pt_prefill(self.h, cache.h, x.data_ptr(), stride, B, S, pids, out.data_ptr(),
-                                   ws.data_ptr(), ws.numel(), self._stream()))
+                                   *self._borrow(ws), self._stream()))
         return out
 
     def extend(self, cache: "Cache", x, n_tokens, seq_ids, out=None):
@@ -344,7 +350,7 @@ class Model:
             self.ext_key = key
         with torch.cuda.device(self.device):
             check(lib().pt_extend(self.h, cache.h, x.data_ptr(), stride, len(ids), pcnt, pids, out.data_ptr(),
-                                  self.ext_ws.data_ptr(), self.ext_ws.numel(), self._stream()))
+                                  *self._borrow(self.ext_ws), self._stream()))
         return out
 
     def decode_step(self, cache: "Cache", x, seq_ids, out=None):
@@ -360,7 +366,7 @@ class Model:
         assert len(ids) == B
         with torch.cuda.device(self.device):
             check(lib().pt_decode_step(self.h, cache.h, x.data_ptr(), stride, B, pids, out.data_ptr(),
-                                       ws.data_ptr(), ws.numel(), self._stream()))
+                                       *self._borrow(ws), self._stream()))
         return out
 
     # ---- ends of the model -------------------------------------------------------------------
@@ -428,12 +434,12 @@ class Model:
             sp = pt_sampling(*(None if a is None else a.data_ptr() for a in (u, temperature, top_k, top_p, min_p, prob)))
             with torch.cuda.device(self.device):
                 check(lib().pt_generate_sample(self.h, cache.h, prompt.data_ptr(), B, S, n_new, pids, C.byref(sp), out.data_ptr(),
-                                               logits.data_ptr() if want_logits else None, self.gen_ws.data_ptr(), self.gen_ws.numel(), self._stream()))
+                                               logits.data_ptr() if want_logits else None, *self._borrow(self.gen_ws), self._stream()))
             return out, logits
         assert temperature is None and top_k is None and top_p is None and min_p is None and prob is None, "sampling needs u"
         with torch.cuda.device(self.device):
             check(lib().pt_generate(self.h, cache.h, prompt.data_ptr(), B, S, n_new, pids, out.data_ptr(),
-                                    logits.data_ptr() if want_logits else None, self.gen_ws.data_ptr(), self.gen_ws.numel(), self._stream()))
+                                    logits.data_ptr() if want_logits else None, *self._borrow(self.gen_ws), self._stream()))
         return out, logits
 
     PROF_NAMES = ("attention", "gemm_qkv", "gemm_out", "gemm_gate_up", "gemm_down", "gemm_down_sync", "other")
