@@ -204,12 +204,6 @@ __device__ __forceinline__ void st_global_32(void* p, const uint32_t* u) {
     asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};"
                  ::"l"(p), "r"(u[0]), "r"(u[1]), "r"(u[2]), "r"(u[3]), "r"(u[4]), "r"(u[5]), "r"(u[6]), "r"(u[7]) : "memory");
 }
-// An arrival that orders nothing but itself: for hand-offs of what was read, so that it does not wait for the stores of an
-// output that are still on their way.
-__device__ __forceinline__ void mbar_arrive_relaxed(uint64_t* bar) {
-    asm volatile("mbarrier.arrive.relaxed.cta.shared::cta.b64 _, [%0];" ::"r"(smem_u32(bar)) : "memory");
-}
-
 // Eight products of 16 along the contraction with one election: an election and fresh descriptors for each product take the
 // issuing warp longer than the tensor core takes for the product (88 cycles against 64 at 128 x 128).
 // D[tmem] (+)= A[smem] * B[smem], 64 elements of the contraction at a time (HALVES of them, kHalfBytes apart)
@@ -292,7 +286,7 @@ k_chunk_tc(const __grid_constant__ CUtensorMap qmap, const __grid_constant__ CUt
         }
         sg = ring[s];
         __syncwarp();
-        if (lane == 0) mbar_arrive_relaxed(&bars[C_SEGEMPTY + s]);
+        if (lane == 0) mbar_arrive(&bars[C_SEGEMPTY + s]);
         ++seg_i;
         return sg.lo >= 0;
     };
@@ -650,7 +644,7 @@ k_chunk_tc(const __grid_constant__ CUtensorMap qmap, const __grid_constant__ CUt
             if (one) {
                 tc_fence_before();
                 __syncwarp();
-                if (lane == 0) mbar_arrive_relaxed(&bars[C_MDONE]);
+                if (lane == 0) mbar_arrive(&bars[C_MDONE]);
             }
             tc_fence_before();                                     // the accumulator has been read: the next segment's P may follow
         }
