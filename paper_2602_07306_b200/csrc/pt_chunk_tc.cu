@@ -514,8 +514,7 @@ k_chunk_tc(const __grid_constant__ CUtensorMap qmap, const __grid_constant__ CUt
                 float v[128];
 #pragma unroll
                 for (int cc = 0; cc < 4; ++cc) tm_ld32(t_s + cc * 32, v + cc * 32);
-                tm_wait_ld();
-                tm_pin<128>(v);
+                tm_wait_ld<128>(v);
                 if (key0 + 127 > tile_limit) {
 #pragma unroll
                     for (int e = 0; e < 128; ++e) if (key0 + e > limit) v[e] = -INFINITY;
@@ -539,8 +538,7 @@ k_chunk_tc(const __grid_constant__ CUtensorMap qmap, const __grid_constant__ CUt
                         for (int cc = 0; cc < DH / 32; ++cc) {
                             float o[32];
                             tm_ld32(t_o + cc * 32, o);
-                            tm_wait_ld();
-                            tm_pin<32>(o);
+                            tm_wait_ld<32>(o);
 #pragma unroll
                             for (int e = 0; e < 32; ++e) o[e] *= corr;
                             tm_st32(t_o + cc * 32, o);
@@ -597,14 +595,11 @@ k_chunk_tc(const __grid_constant__ CUtensorMap qmap, const __grid_constant__ CUt
                 if (one && sg.lo + 1 < end) {
                     float o1[32];
                     tm_ld32(t_o + DH + cc * 32, o1);
-                    tm_wait_ld();
-                    tm_pin<32>(o);
-                    tm_pin<32>(o1);
+                    tm_wait_ld<32>(o, o1);
 #pragma unroll
                     for (int e = 0; e < 32; ++e) o[e] = o[e] * f0 + (f1 > 0.f ? o1[e] * f1 : 0.f);
                 } else {
-                    tm_wait_ld();
-                    tm_pin<32>(o);
+                    tm_wait_ld<32>(o);
                 }
             };
             if (any) {

@@ -304,7 +304,7 @@ k_flash_prefill_tc(const __grid_constant__ CUtensorMap qmap, const __grid_consta
             float v[128];
 #pragma unroll
             for (int cc = 0; cc < 4; ++cc) tm_ld32(t_s + cc * 32, v + cc * 32);
-            tm_wait_ld();
+            tm_wait_ld<128>(v);
             if (need_mask) {
 #pragma unroll
                 for (int e = 0; e < 128; ++e) if (key0 + e > limit) v[e] = -INFINITY;
@@ -332,7 +332,7 @@ k_flash_prefill_tc(const __grid_constant__ CUtensorMap qmap, const __grid_consta
                     for (int cc = 0; cc < DH / 32; ++cc) {
                         float v[32];
                         tm_ld32(t_o + cc * 32, v);
-                        tm_wait_ld();
+                        tm_wait_ld<32>(v);
 #pragma unroll
                         for (int e = 0; e < 32; ++e) v[e] *= corr;
                         tm_st32(t_o + cc * 32, v);
@@ -386,7 +386,7 @@ k_flash_prefill_tc(const __grid_constant__ CUtensorMap qmap, const __grid_consta
             for (int cc = 0; cc < DH / 32; ++cc) {
                 float v[32];
                 tm_ld32(t_o + cc * 32, v);
-                tm_wait_ld();
+                tm_wait_ld<32>(v);
                 if (s_row < p.S) {
 #pragma unroll
                     for (int e = 0; e < 32; e += 8) {

@@ -71,7 +71,6 @@ __device__ __forceinline__ void tc_ld16(uint32_t taddr, float* v) {
 #pragma unroll
     for (int i = 0; i < 16; ++i) v[i] = __uint_as_float(r[i]);
 }
-__device__ __forceinline__ void tc_wait_ld() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
 
 // Shared-memory matrix descriptor of a K-major bf16 tile whose rows are 128 bytes (64 elements)
 // in the 128-byte swizzle: 8-row groups are 1024 bytes apart; the leading-dimension field is
@@ -168,7 +167,7 @@ __device__ __forceinline__ bool epi_plain(const GemmP& p, uint32_t taddr, int t,
         float v[32];
         tc_ld16(taddr + c, v);
         tc_ld16(taddr + c + 16, v + 16);
-        tc_wait_ld();
+        tm_wait_ld<32>(v);
         if (row_ok) {
             float4* dst = (float4*)(p.c_out + ((size_t)t * p.M + row) * p.N + n0 + c);
 #pragma unroll
@@ -194,7 +193,7 @@ __device__ __forceinline__ bool epi_swiglu(const GemmP& p, uint32_t taddr, int t
         float gu[64];
 #pragma unroll
         for (int g4 = 0; g4 < 4; ++g4) tc_ld16(taddr + c + g4 * 16, gu + g4 * 16);
-        tc_wait_ld();
+        tm_wait_ld<64>(gu);
         // PT-MoE: the 64 columns of a unit belong to one expert (its block is a multiple of 32 columns wide and starts on one)
         float wgt = 1.0f;
         if (p.gates && row_ok) wgt = p.gates[((size_t)t * p.M + row) * p.n_experts + (n0 + c) / p.expert_cols];
@@ -265,7 +264,7 @@ __device__ __forceinline__ bool epi_qkv(const GemmP& p, uint32_t taddr, int t, i
             dst = p.pool_l + (size_t)t * p.pool_tstride + kvoff + ((int64_t)kv * p.nkv + head) * p.ps * dh;
             st_ok = slot_ok;
         }
-        tc_wait_ld();
+        tm_wait_ld<16>(lo, hi);
         if (st_ok) {
             if (!is_v) {
 #pragma unroll
@@ -350,7 +349,7 @@ __device__ __forceinline__ bool epi_resid(const GemmP& p, uint32_t taddr, int t,
         tc_ld16(taddr + c + 16, v + 16);
         const int un = u + ((u & 1) ? 3 : 1);
         if (un < UNITS) fetch(un, hnxt);
-        tc_wait_ld();
+        tm_wait_ld<32>(v);
         __syncwarp();                                      // the previous unit's reads of the buffer are done
 #pragma unroll
         for (int j = 0; j < 8; ++j)
@@ -971,7 +970,7 @@ gemm_tc_pair_resid(const __grid_constant__ CUtensorMap ta, const __grid_constant
                 __syncwarp();                                               // every lane has its residual row: the box is free
                 const int un = u + ((u & 1) ? 3 : 1);
                 if (un < UNITS && n0 + un * 32 < p.N) issue_in(un);
-                tc_wait_ld();
+                tm_wait_ld<32>(v);
 #pragma unroll
                 for (int i = 0; i < 32; ++i) { v[i] = (v[i] + h[i]) * p.scale; if (row_ok) ssq += v[i] * v[i]; }
                 if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");   // the previous unit's stores have read their boxes

@@ -95,7 +95,6 @@ __device__ __forceinline__ void tm_st16(uint32_t taddr, const float* v) {
                    "r"(__float_as_uint(v[12])), "r"(__float_as_uint(v[13])), "r"(__float_as_uint(v[14])), "r"(__float_as_uint(v[15]))
                  : "memory");
 }
-__device__ __forceinline__ void tm_wait_ld() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
 __device__ __forceinline__ void tm_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 __device__ __forceinline__ float ex2f(float x) {
     float y;
@@ -374,7 +373,7 @@ k_decode_attn_e4m3_tc(const __grid_constant__ CUtensorMap kvmap, const Dec8TcP p
             if (ok) {
                 tc_fence_after();
                 tm_ld16(lane_base + bb * 16, sc);
-                tm_wait_ld();
+                tm_wait_ld<16>(sc);
                 tc_fence_before();
                 __syncwarp();
                 if (lane == 0) mbar_arrive(&bars[B_SEMPTY + bb]);  // the scores of tile j + 2 may overwrite this buffer
@@ -416,7 +415,7 @@ k_decode_attn_e4m3_tc(const __grid_constant__ CUtensorMap kvmap, const Dec8TcP p
                     tc_fence_after();
                     float ov[16];
                     tm_ld16(lane_base + 32, ov);
-                    tm_wait_ld();
+                    tm_wait_ld<16>(ov);
 #pragma unroll
                     for (int h = 0; h < 8; ++h) { ov[h] *= corr[h] * vcorr; ov[8 + h] *= corr[h] * vcorr; }
                     tm_st16(lane_base + 32, ov);
@@ -470,7 +469,7 @@ k_decode_attn_e4m3_tc(const __grid_constant__ CUtensorMap kvmap, const Dec8TcP p
             tc_fence_after();
             float ov[16];
             tm_ld16(lane_base + 32, ov);
-            tm_wait_ld();
+            tm_wait_ld<16>(ov);
             const float unit = v_ref * (1.0f / 64.0f);
             const int ns = p.nsplit[b];
 #pragma unroll
