@@ -73,6 +73,7 @@ pt_status pt_kernel_prefill_attn(const void* q, const void* pool_l, int64_t pool
  *                 V that is not finite may make earlier rows NaN (in a plain softmax as well), K that is not cannot
  *   q_len, kv_len DEVICE int32 [B]: a captured call may be replayed with other lengths.  Lengths out of range (negative,
  *                 kv_len < q_len, kv_len > maxp*ps, sum of q_len > M) are reported in `status` and nothing is written
+ *   maxp          columns of the block table: at most 2^31 - 128 keys (PT_ERR_UNSUPPORTED)
  *   impl          0 = tensor-memory kernel (tcgen05; head_dim 64 or 128, pages of a multiple of 16 tokens), 1 = plain
  *                 kernel, one warp per row and head (head_dim 32, 64, 128; any page size)
  *   scratch       device, 256-byte aligned, >= pt_kernel_chunk_attn_scratch_bytes: partial results of key ranges; contents

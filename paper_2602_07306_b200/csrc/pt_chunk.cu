@@ -133,6 +133,7 @@ extern "C" pt_status pt_kernel_chunk_attn(const void* q, const void* pool_l, int
     if (nq / nkv > 8) { set_error("more than 8 query heads per KV head"); return PT_ERR_UNSUPPORTED; }
     if (dh != 32 && dh != 64 && dh != 128) { set_error("head_dim %d not in {32, 64, 128}", dh); return PT_ERR_UNSUPPORTED; }
     if (ps < 8 || ps > 64 || ps % 8) { set_error("page size must be a multiple of 8 in [8, 64]"); return PT_ERR_INVALID_ARG; }
+    if ((int64_t)maxp * ps > 0x7fffffff - 127) { set_error("a block table of more than 2^31 - 128 keys"); return PT_ERR_UNSUPPORTED; }   // rounded up to tiles in 32 bits
     if (impl != 0 && impl != 1) { set_error("impl must be 0 or 1"); return PT_ERR_INVALID_ARG; }
     if (impl == 0 && !chunk_tc_supported(dh, ps)) { set_error("impl 0 needs head_dim 64 or 128 and pages of a multiple of 16 tokens"); return PT_ERR_UNSUPPORTED; }
     if ((uintptr_t)q % 16 || (uintptr_t)pool_l % 16 || pool_track_stride % 8 || (uintptr_t)out % 32 || (uintptr_t)scratch % 256) {
