@@ -744,6 +744,7 @@ def kernel_chunk_attn(q, pool_l, block_table, q_len, kv_len, *, nq, nkv, dh, ps,
         status = _new_status(index)
     assert out.get_device() == index and out.dtype is bf16 and out.shape == q.shape and out.is_contiguous()
     assert scratch.get_device() == index and status.get_device() == index and status.dtype is i32 and status.numel() >= 16
+    assert scratch.is_contiguous() and status.is_contiguous()
     if impl is None:
         impl = 0 if dh in (64, 128) and ps % 16 == 0 else 1
     _call(index, lib().pt_kernel_chunk_attn, q.data_ptr(), pool_l.data_ptr(), pool_l.stride(0), block_table.data_ptr(), maxp,
