@@ -186,7 +186,8 @@ pt_status pt_kv_slot(const pt_kv_cache* c, int32_t track, int32_t layer, int32_t
 /* A new sequence `dst` that shares the first `len` tokens of `src` (several answers of one prompt, a prompt that many
  * requests begin with): its table holds the pages of those tokens, and nothing is copied.  Shared pages are copied on
  * write: a forward call that would write to a page that another sequence shares first gives the sequence a page of its
- * own (with the earlier positions copied, on the call's stream, all sequences of the call in one launch); the last
+ * own (with the earlier positions copied, on the call's stream: one launch for every 448 pages of the call, and as many
+ * again for the scales of an E4M3 cache); the last
  * sequence left on a page keeps it.  Such pages count as new ones: PT_ERR_CACHE_FULL where the free list is too short.
  * A program that writes to the pool itself looks at pt_kv_page_refs first.  Host only.
  * PT_ERR_STATE: unknown `src`, or `dst` exists (src included); PT_ERR_INVALID_ARG: len outside [0, length of src]. */
@@ -310,8 +311,8 @@ pt_status pt_generate(pt_model* m, pt_kv_cache* c, const int32_t* dev_prompt, in
  * sum; u outside [0, 1) (or NaN) counts as the nearest end.  A temperature that is not a positive finite number chooses
  * greedily (the lowest index of the largest logit, probability 1); others count as the nearest value in [1e-30, 1e36].
  * NaN and -inf logits are masked; a row with nothing else gives token 0 and probability 0.  +inf logits share the whole
- * weight.  Weights are held as multiples of 2^-44 of the largest: a token more than 31 nats (after the temperature) below
- * it is never drawn.  The result does not depend on the batch, and every call with the same arguments gives the same bits.
+ * weight.  Weights are held as multiples of 2^-44 of the largest: a token more than 45 ln 2 = 31.19 nats (after the
+ * temperature) below it rounds to 0 and is never drawn.  The result does not depend on the batch, and every call with the same arguments gives the same bits.
  *   logits       device [n] rows of `vocab` values `row_stride` elements apart, fp32 or bf16 (dtype: a pt_dtype)
  *   u            device fp32 [n], the random numbers, uniform in [0, 1)
  *   temperature, top_p, min_p   device fp32 [n] or NULL (off; temperature 1);  top_k   device int32 [n] or NULL

@@ -70,12 +70,15 @@ pt_status pt_kernel_prefill_attn(const void* q, const void* pool_l, int64_t pool
  *   q, out        device bf16 [T][M][nq*dh], 16-byte and 32-byte aligned; rows behind the last sequence are not touched
  *   pool_l, block_table   as for pt_kernel_decode_attn (entries behind a sequence's last page are not read).  What lies
  *                 behind a sequence's last key is never used; a V of a later token of the sequence meets the weight 0, so
- *                 V that is not finite may make earlier rows NaN (in a plain softmax as well), K that is not cannot
+ *                 V that is not finite may make earlier rows NaN (in a plain softmax as well), K that is not cannot.
+ *                 A visible score that is NaN, or visible scores that are all -inf, make the row's head NaN
  *   q_len, kv_len DEVICE int32 [B]: a captured call may be replayed with other lengths.  Lengths out of range (negative,
  *                 kv_len < q_len, kv_len > maxp*ps, sum of q_len > M) are reported in `status` and nothing is written
  *   maxp          columns of the block table: at most 2^31 - 128 keys (PT_ERR_UNSUPPORTED)
  *   impl          0 = tensor-memory kernel (tcgen05; head_dim 64 or 128, pages of a multiple of 16 tokens), 1 = plain
- *                 kernel, one warp per row and head (head_dim 32, 64, 128; any page size)
+ *                 kernel, one warp per row and head (head_dim 32, 64, 128; any page size).  Scores, weights, sums and
+ *                 accumulators are fp32 in both; impl 0 rounds the weights to bf16 for the product with V (their sum is
+ *                 taken unrounded), and the output is rounded once
  *   scratch       device, 256-byte aligned, >= pt_kernel_chunk_attn_scratch_bytes: partial results of key ranges; contents
  *                 need not be kept, but calls that may run at the same time need one each
  *   status        device int32[16], zeroed by the caller; PT_ERR_DEVICE_BOUNDS also for a page id outside [0, num_pages)

@@ -18,6 +18,8 @@
 // group has one; in a segment of one, which is bound by the latency from a score to the next product, the groups take
 // turns on its key tiles with a running maximum, sum and accumulator each, and the first merges both at the end.  Barriers
 // count over all segments of a block, so the copies of the next segment start while the last one's output is being written.
+// Weights are rounded to bf16 for the product with V, the operand type that the tensor core takes beside a bf16 V (their sum
+// is taken unrounded; against 64 bits the outputs are off by 2.3e-3 of their size, 1.7e-3 of it the output's own rounding).
 // Every wait is bounded; on a timeout the block records PT_ERR_DEVICE_TIMEOUT and every role leaves.
 //
 // Measured (head_dim 128): eight users' speculated tokens over 2k keys (8 tracks, 8 heads) 101 us, 0.74 of the copy bandwidth; four

@@ -10,8 +10,8 @@
 // and the token is the lowest kept index whose cumulative weight, summed in index order, exceeds u times the kept sum.
 //
 // Weights are whole multiples of 2^-44: integer sums do not depend on their order, so neither the number of blocks nor
-// the order of atomics changes a result, and ties at a threshold are exact.  A weight below 2^-45 (31 nats under the
-// maximum) is zero: such a token is never drawn.  The exponential is evaluated in double; the multiple rounds it once,
+// the order of atomics changes a result, and ties at a threshold are exact.  A weight below 2^-45 (45 ln 2 = 31.19 nats under
+// the maximum) is zero: such a token is never drawn.  The exponential is evaluated in double; the multiple rounds it once,
 // an absolute error of 2^-45 against a sum of at least 1.
 //
 // Three ways to take a row.  For few rows, whose time is latency, a cluster of up to 8 blocks, which exchange what they found
@@ -25,7 +25,7 @@
 // sorts them and finishes the row alone.
 // Everything else (top-p over the whole vocabulary, a large k, no filter): a histogram of the distance to the maximum in
 // kBins bins bounds, from counts alone, which bins may hold the threshold: a weight in a bin is known to the bin's width,
-// 0.8 %, and so are the sums before and behind a bin.  One pass then sums the weights above those bins exactly and lists the
+// 0.8 % and half a unit, and so are the sums before and behind a bin.  One pass then sums the weights above those bins exactly and lists the
 // logits inside them, and one block sorts that list and cuts it.  Where the list is too long (many equal logits), or top-p
 // follows a large top-k, histograms with exact counts and weights narrow the threshold down to one key instead.
 //
