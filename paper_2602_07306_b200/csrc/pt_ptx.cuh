@@ -46,25 +46,6 @@ __device__ __forceinline__ void tc_commit(uint64_t* bar) {
                  " @e tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];\n}" ::"r"(smem_u32(bar)) : "memory");
 }
 
-template <int N>
-__device__ __forceinline__ void tm_pin(float* v) {
-#pragma unroll
-    for (int i = 0; i < N; i += 8)
-        asm volatile("" : "+f"(v[i]), "+f"(v[i + 1]), "+f"(v[i + 2]), "+f"(v[i + 3]), "+f"(v[i + 4]), "+f"(v[i + 5]), "+f"(v[i + 6]), "+f"(v[i + 7]) :: "memory");
-}
-// Waits for this thread's tensor-memory loads, which write the N registers of v (and of w).  To the compiler a load has written
-// them where it stands: naming them behind the wait keeps arithmetic on them from being moved in front of it.
-template <int N>
-__device__ __forceinline__ void tm_wait_ld(float* v) {
-    asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
-    tm_pin<N>(v);
-}
-template <int N>
-__device__ __forceinline__ void tm_wait_ld(float* v, float* w) {
-    tm_wait_ld<N>(v);
-    tm_pin<N>(w);
-}
-
 // status[0] = the first error code of a launch, status[1] = where it happened
 __device__ __forceinline__ void report(int* status, int code, int loc) {
     if (atomicCAS(status, 0, code) == 0) status[1] = loc;

@@ -27,6 +27,7 @@
 // issuing work, frees its tensor memory and exits.
 #include "pt_tc.h"
 #include "pt_ptx.cuh"
+#include "pt_tmem.cuh"
 
 namespace pt {
 

@@ -24,6 +24,7 @@
 
 #include "pt_tc.h"
 #include "pt_ptx.cuh"
+#include "pt_tmem.cuh"
 
 namespace pt {
 

@@ -7,6 +7,7 @@
 
 #include "pt_ptx.cuh"
 #include "pt_tc.h"
+#include "pt_tmem.cuh"
 
 namespace pt {
 

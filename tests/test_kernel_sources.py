@@ -22,8 +22,8 @@ def test_loads_of_tensor_memory_are_waited_for_by_name():
     """To the compiler a tensor-memory load has written its registers where it stands.  The one wait for such loads names them, so
     that no arithmetic on them is moved in front of it; no kernel has a wait of its own, and none discards what it loads."""
     waits = [(name, m.start()) for name, text in sources().items() for m in re.finditer(r"tcgen05\.wait::ld", text)]
-    assert [name for name, _ in waits] == ["pt_ptx.cuh"], waits
-    text = sources()["pt_ptx.cuh"]
+    assert [name for name, _ in waits] == ["pt_tmem.cuh"], waits
+    text = sources()["pt_tmem.cuh"]
     body = text[waits[0][1]:text.index("}", waits[0][1])]
     assert "tm_pin<N>(v);" in body and '"+f"(v[i])' in text
     for name, text in sources().items():
