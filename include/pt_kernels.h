@@ -162,6 +162,58 @@ pt_status pt_kernel_decode_attn_e4m3(const void* q, const void* codes_l, int64_t
                                      int32_t num_pages, void* out, int32_t impl, void* scratch, size_t scratch_bytes,
                                      void* status, void* stream);
 
+/* ---- the 4-bit cache format (pt_kv_dtype PT_KV_E2M1 in pt.h; the paper has no cache, the format is this library's) ----
+ * One layer's slab of such a pool, as these calls take it: pool_l device, 16-byte aligned; track t at pool_l +
+ * t*pool_track_stride BYTES (a multiple of 16); pages [num_pages][kv_head][ps/16] blocks of 16 tokens, 17*dh bytes each, in
+ * the order pt.h describes.  dh 64 or 128, ps a multiple of 16 up to 64.  All are asynchronous on `stream` and allocate
+ * nothing; `status` is device int32[16], zeroed by the caller. */
+
+/* Quantise the K and V of M new tokens into pages.
+ *   k, v          device bf16, 16-byte aligned: the nkv*dh values of (track t, row r) at t*track_stride + r*row_stride
+ *                 elements (multiples of 8; 0 is allowed)
+ *   slots         DEVICE int64 [M]: row r is token slots[r] % ps of page slots[r] / ps; a negative one is not cached.  No slot
+ *                 twice in a call (which row it then holds is not defined).  A page outside [0, num_pages) is
+ *                 reported in `status`, and its row is not cached
+ *   k_out, v_out  device bf16 [T][M][nkv*dh], 16-byte aligned, or both NULL: the values that the cache returns for every row
+ *                 (of rows that are not cached, too).  They may be k and v themselves where those lie the same way */
+pt_status pt_kernel_kv_write_e2m1(const void* k, const void* v, int64_t track_stride, int64_t row_stride, int32_t T, int32_t M,
+                                  int32_t nkv, int32_t dh, int32_t ps, int32_t num_pages, void* pool_l, int64_t pool_track_stride,
+                                  const int64_t* slots, void* k_out, void* v_out, void* status, void* stream);
+
+/* The cached values (code * scale, exact in bf16) of whole sequences, into pages of a cache in the model dtype.
+ *   block_table   device int32 [B][maxp]: the pages of sequence b (entries behind its last page are not read)
+ *   kv_len        DEVICE int32 [B]: keys to copy, from the first on (0: none).  A length outside [0, maxp*ps] or
+ *                 [0, out_maxp*out_ps] is reported in `status` and nothing is written
+ *   out_l         device bf16, 16-byte aligned: slabs out_track_stride elements (a multiple of 8) apart, each
+ *                 [out_pages][K|V][nkv][out_ps][dh]; out_ps a multiple of 8 in [8, 64].  Other slots are left as they are
+ *   out_table     device int32 [B][out_maxp]: the pages that sequence b goes to, none of them in two places
+ * A page number outside its pool is reported in `status`; what it names is neither read nor written.
+ * The two pools must not overlap. */
+pt_status pt_kernel_kv_read_e2m1(const void* pool_l, int64_t pool_track_stride, const int32_t* block_table, int32_t maxp, const int32_t* kv_len,
+                                 int32_t T, int32_t B, int32_t nkv, int32_t dh, int32_t ps, int32_t num_pages,
+                                 void* out_l, int64_t out_track_stride, const int32_t* out_table, int32_t out_maxp, int32_t out_ps, int32_t out_pages,
+                                 void* status, void* stream);
+
+/* Attention of one or a few new tokens per sequence over the 4-bit pages: the formula, the rows and the lengths of
+ * pt_kernel_chunk_attn above, K and V being code * scale.
+ *   q, out        device bf16 [T][M][nq*dh], 16-byte aligned; nq/nkv <= 8; rows behind the last sequence are not touched
+ *   q_len         DEVICE int32 [B]: new tokens of each sequence (none is allowed), or NULL: one each (M = B).  Any number is
+ *                 served; a block of 16 (token, head) rows reads the sequence's keys once
+ *   kv_len        DEVICE int32 [B], the new tokens' keys included.  Lengths out of range (negative, kv_len < q_len,
+ *                 kv_len > maxp*ps, sum of q_len > M) are reported in `status` and nothing is written
+ *   maxp          columns of the block table: at most 2^31 - 128 keys (PT_ERR_UNSUPPORTED).  A page number outside
+ *                 [0, num_pages) is reported in `status`; rows that see such a page hold no result
+ *   scratch       device, 256-byte aligned, >= pt_kernel_attn_e2m1_scratch_bytes: partial results of key ranges; contents
+ *                 need not be kept, but calls that may run at the same time need one each
+ * Scores, sums and accumulators are fp32; q (divided by the power of two at its row's largest magnitude) and the weights
+ * times the scales of V are rounded to fp16.  What lies behind a sequence's last key is never used; a V of a later token of
+ * the sequence meets the weight 0, so one that is not finite may make earlier rows NaN, a K cannot.  A visible score that is
+ * NaN, or visible scores that are all -inf, make the row's head NaN. */
+pt_status pt_kernel_attn_e2m1_scratch_bytes(int32_t T, int32_t nq, int32_t nkv, int32_t dh, size_t* bytes);
+pt_status pt_kernel_attn_e2m1(const void* q, const void* pool_l, int64_t pool_track_stride, const int32_t* block_table, int32_t maxp,
+                              const int32_t* q_len, const int32_t* kv_len, int32_t T, int32_t B, int32_t M, int32_t nq, int32_t nkv, int32_t dh,
+                              int32_t ps, int32_t num_pages, void* out, void* scratch, size_t scratch_bytes, void* status, void* stream);
+
 /* ---- the bounded wait, exercised ------------------------------------------------------------
  * Every device-side wait of the library (an mbarrier of a TMA -> MMA -> epilogue pipeline) gives up
  * after a time limit (2 s of device time, whatever the iteration counts), records PT_ERR_DEVICE_TIMEOUT with

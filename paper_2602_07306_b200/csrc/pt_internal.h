@@ -29,6 +29,7 @@ enum : int {
     LOC_EMBED_TOKEN = 19, LOC_SELFTEST_WAIT = 20,
     LOC_FLASH_PFULL = 15, LOC_FLASH_VFULL = 16, LOC_FLASH_SFULL = 17, LOC_FLASH_OREADY = 18,
     LOC_CHUNK_LEN = 21, LOC_CHUNK_PAGE = 22, LOC_CHUNK_WAIT = 23,
+    LOC_KV4_PAGE = 24, LOC_KV4_LEN = 25, LOC_KV4_WAIT = 26,
 };
 
 extern std::atomic<long long> g_launches;

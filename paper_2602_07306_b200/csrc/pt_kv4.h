@@ -1,0 +1,54 @@
+// The 4-bit storage format of the KV cache (pt_kv_dtype PT_KV_E2M1): write, read back, attention from the codes.
+#pragma once
+#include "pt_internal.h"
+
+namespace pt {
+
+// A page is [kv_head][slot / 16] blocks of 16 tokens: K codes, K scales, V codes, V scales (pt.h has the order inside).
+__host__ __device__ constexpr int kv4_codes(int dh) { return 8 * dh; }                 // bytes of 16 tokens' K (or V) codes
+__host__ __device__ constexpr int kv4_scales(int dh) { return 16 * (dh / 32); }        // and of their scales
+__host__ __device__ constexpr int kv4_block(int dh) { return 2 * (kv4_codes(dh) + kv4_scales(dh)); }
+inline bool kv4_supported(int dh, int ps) { return (dh == 64 || dh == 128) && ps % 16 == 0 && ps >= 16 && ps <= 64; }
+
+struct Kv4Slab {                      // one layer
+    char* pool_l; int64_t tstride;    // track 0; bytes between tracks
+    int nkv, ps, num_pages;
+};
+
+struct Kv4WriteP {
+    const __nv_bfloat16* k; const __nv_bfloat16* v;   // vector of (track, row, head) at t*tstride + row*row_stride + head*head_stride
+    int64_t tstride, row_stride, head_stride;
+    Kv4Slab slab;
+    const int64_t* slots;             // [M] page * ps + slot, negative: the row is not cached
+    __nv_bfloat16* k_out; __nv_bfloat16* v_out;       // [T][M][nkv*dh] the rounded values, may be null
+    int T, M;
+    int* status;
+};
+pt_status launch_kv4_write(const Kv4WriteP& p, int dh, cudaStream_t st);
+
+struct Kv4ReadP {
+    Kv4Slab slab;
+    const int32_t* bt; int maxp;
+    const int32_t* kvlen;             // [B]
+    __nv_bfloat16* out_l; int64_t out_tstride;        // pages [K|V][kv_head][out_ps][dh]; elements between tracks
+    const int32_t* obt; int omaxp; int ops, opages;
+    int T, B;
+    int* status;
+};
+pt_status launch_kv4_read(const Kv4ReadP& p, int dh, cudaStream_t st);
+
+struct Kv4AttnP {
+    const __nv_bfloat16* q;           // [T][M][nq*dh], the rows of sequence b behind those of sequence b - 1
+    __nv_bfloat16* o;
+    Kv4Slab slab;
+    const int32_t* bt; int maxp;
+    const int32_t* qlen;              // [B] new tokens; null: one each
+    const int32_t* kvlen;             // [B] keys cached, the new tokens' included
+    int T, B, M, nq;
+    float scale_log2;                 // log2(e) / sqrt(dh)
+    int* status;
+};
+size_t kv4_attn_scratch_bytes(int dh);
+pt_status launch_kv4_attn(const Kv4AttnP& p, int dh, void* scratch, cudaStream_t st);
+
+}  // namespace pt

@@ -105,6 +105,11 @@ _PROTOS = {
     "pt_kernel_chunk_attn": (_I32, [_P, _P, _I64, _P, _I32, _P, _P, _I32, _I32, _I32, _I32, _I32, _I32, _I32, _I32,
                                     _P, _I32, _P, _SZ, _P, _P]),
     "pt_kernel_kv_copy_pages": (_I32, [_P, _I32, _P, _I32, _I64, _I64, _P, _P, _I32, _P]),
+    "pt_kernel_kv_write_e2m1": (_I32, [_P, _P, _I64, _I64, _I32, _I32, _I32, _I32, _I32, _I32, _P, _I64, _P, _P, _P, _P, _P]),
+    "pt_kernel_kv_read_e2m1": (_I32, [_P, _I64, _P, _I32, _P, _I32, _I32, _I32, _I32, _I32, _I32, _P, _I64, _P, _I32, _I32, _I32, _P, _P]),
+    "pt_kernel_attn_e2m1_scratch_bytes": (_I32, [_I32, _I32, _I32, _I32, C.POINTER(_SZ)]),
+    "pt_kernel_attn_e2m1": (_I32, [_P, _P, _I64, _P, _I32, _P, _P, _I32, _I32, _I32, _I32, _I32, _I32, _I32, _I32,
+                                   _P, _P, _SZ, _P, _P]),
     "pt_kernel_wait_selftest": (_I32, [_P, C.c_uint64, _P]),
     "pt_last_error": (C.c_char_p, []),
 }
@@ -749,6 +754,121 @@ def kernel_chunk_attn(q, pool_l, block_table, q_len, kv_len, *, nq, nkv, dh, ps,
         impl = 0 if dh in (64, 128) and ps % 16 == 0 else 1
     _call(index, lib().pt_kernel_chunk_attn, q.data_ptr(), pool_l.data_ptr(), pool_l.stride(0), block_table.data_ptr(), maxp,
           q_len.data_ptr(), kv_len.data_ptr(), T, B, M, nq, nkv, dh, ps, pages, out.data_ptr(), impl,
+          scratch.data_ptr(), scratch.numel() * scratch.element_size(), status.data_ptr())
+    return out, status
+
+
+def _kv4_pool(pool_l, T, nkv, dh, ps, index):
+    """Checks one layer of an E2M1 pool: uint8 [T, pages, nkv, ps // 16, 17 * dh], contiguous but for the track stride."""
+    import torch
+    if pool_l.dtype is not torch.uint8 or pool_l.dim() != 5 or pool_l.shape[0] != T or tuple(pool_l.shape[2:]) != (nkv, ps // 16, 17 * dh) \
+            or not pool_l[0].is_contiguous() or pool_l.get_device() != index or index < 0 or pool_l.shape[1] < 1:
+        raise ValueError(f"pool: a uint8 CUDA tensor [{T}, pages, {nkv}, {ps // 16}, {17 * dh}] with contiguous tracks on the call's device is wanted")
+    return pool_l.stride(0) if T > 1 else 0
+
+
+def _kv4_ints(index, **arrays):
+    import torch
+    for name, (a, dtype, dim) in arrays.items():
+        if a.dtype is not dtype or a.dim() != dim or not a.is_contiguous() or a.get_device() != index:
+            raise ValueError(f"{name}: a contiguous {dtype} tensor of {dim} dimensions on CUDA device {index} is wanted")
+
+
+def _kv4_status(status, index):
+    import torch
+    if status is None:
+        return _new_status(index)
+    if status.dtype is not torch.int32 or status.numel() < 16 or not status.is_contiguous() or status.get_device() != index:
+        raise ValueError(f"status: a contiguous int32 tensor of 16 on CUDA device {index} is wanted")
+    return status
+
+
+def kernel_kv_write_e2m1(k, v, pool_l, slots, *, nkv, dh, ps, k_out=None, v_out=None, status=None):
+    """K and V of new tokens (bf16 CUDA [T, M, nkv*dh], rows and tracks may be strided, both alike) into the 4-bit pages pool_l
+    (uint8 [T, pages, nkv, ps/16, 17*dh]): row r to token slots[r] % ps of page slots[r] // ps (int64 CUDA [M]; negative:
+    not cached).  k_out, v_out (bf16 [T, M, nkv*dh]) receive the values that the cache then returns.  Returns status int32[16]."""
+    import torch
+    bf16, index = torch.bfloat16, k.get_device()
+    if k.dim() != 3 or k.dtype is not bf16 or v.dtype is not bf16 or k.shape != v.shape or k.stride() != v.stride() or k.shape[2] != nkv * dh \
+            or k.stride(2) != 1 or v.get_device() != index or index < 0:
+        raise ValueError("k, v: bf16 CUDA tensors [T, M, nkv*dh] of the same strides with contiguous values are wanted")
+    T, M, _ = k.shape
+    pstride = _kv4_pool(pool_l, T, nkv, dh, ps, index)
+    _kv4_ints(index, slots=(slots, torch.int64, 1))
+    if slots.numel() != M or (k_out is None) != (v_out is None):
+        raise ValueError("slots: one for each row; k_out and v_out: both or neither")
+    for a in (k_out, v_out):
+        if a is not None and (a.dtype is not bf16 or a.shape != k.shape or not a.is_contiguous() or a.get_device() != index):
+            raise ValueError("k_out, v_out: contiguous bf16 CUDA tensors of k's shape are wanted")
+    status = _kv4_status(status, index)
+    if M == 0:
+        return status
+    _call(index, lib().pt_kernel_kv_write_e2m1, k.data_ptr(), v.data_ptr(), k.stride(0) if T > 1 else 0, k.stride(1) if M > 1 else 0, T, M, nkv, dh, ps,
+          pool_l.shape[1], pool_l.data_ptr(), pstride, slots.data_ptr(), None if k_out is None else k_out.data_ptr(),
+          None if v_out is None else v_out.data_ptr(), status.data_ptr())
+    return status
+
+
+def kernel_kv_read_e2m1(pool_l, block_table, kv_len, out, out_table, *, nkv, dh, ps, status=None):
+    """The first kv_len[b] cached tokens of every sequence from 4-bit pages (pool_l as for kernel_kv_write_e2m1, block_table
+    int32 [B, maxp], kv_len int32 [B], all CUDA) into bf16 pages out [T, pages, 2, nkv, out_ps, dh] at out_table int32
+    [B, out_maxp].  Returns (out, status int32[16])."""
+    import torch
+    index = pool_l.get_device()
+    if out.dim() != 6 or out.dtype is not torch.bfloat16 or out.shape[2:4] != (2, nkv) or out.shape[5] != dh or out.get_device() != index \
+            or not out[0].is_contiguous():
+        raise ValueError("out: a bf16 CUDA tensor [T, pages, 2, nkv, out_ps, dh] with contiguous tracks is wanted")
+    T, opages, _, _, ops, _ = out.shape
+    pstride = _kv4_pool(pool_l, T, nkv, dh, ps, index)
+    _kv4_ints(index, block_table=(block_table, torch.int32, 2), kv_len=(kv_len, torch.int32, 1), out_table=(out_table, torch.int32, 2))
+    B = kv_len.numel()
+    if block_table.shape[0] != B or out_table.shape[0] != B:
+        raise ValueError("block_table, out_table: a row for each sequence is wanted")
+    status = _kv4_status(status, index)
+    _call(index, lib().pt_kernel_kv_read_e2m1, pool_l.data_ptr(), pstride, block_table.data_ptr(), block_table.shape[1], kv_len.data_ptr(), T, B, nkv, dh, ps,
+          pool_l.shape[1], out.data_ptr(), out.stride(0) if T > 1 else 0, out_table.data_ptr(), out_table.shape[1], ops, opages, status.data_ptr())
+    return out, status
+
+
+def attn_e2m1_scratch(T: int, nq: int, nkv: int, dh: int, device="cuda:0"):
+    """Scratch buffer for kernel_attn_e2m1 calls (one per stream that calls at the same time)."""
+    import torch
+    n = _SZ()
+    check(lib().pt_kernel_attn_e2m1_scratch_bytes(T, nq, nkv, dh, C.byref(n)))
+    return torch.empty(n.value, dtype=torch.uint8, device=device)
+
+
+def kernel_attn_e2m1(q, pool_l, block_table, kv_len, q_len=None, *, nq, nkv, dh, ps, out=None, scratch=None, status=None):
+    """Attention straight from 4-bit pages: q bf16 [T, M, nq*dh], rows packed by sequence; pool_l uint8 [T, pages, nkv, ps/16,
+    17*dh]; block_table int32 [B, maxp], kv_len int32 [B], q_len int32 [B] or None (one new token each), all CUDA.
+    Returns (out bf16 [T, M, nq*dh], status int32[16])."""
+    import torch
+    bf16, index = torch.bfloat16, q.get_device()
+    if q.dim() != 3 or q.dtype is not bf16 or not q.is_contiguous() or q.shape[2] != nq * dh:
+        raise ValueError("q: a contiguous bf16 CUDA tensor [T, M, nq*dh] is wanted")
+    T, M, _ = q.shape
+    pstride = _kv4_pool(pool_l, T, nkv, dh, ps, index)
+    _kv4_ints(index, block_table=(block_table, torch.int32, 2), kv_len=(kv_len, torch.int32, 1))
+    B = kv_len.numel()
+    if block_table.shape[0] != B:
+        raise ValueError("block_table: a row for each sequence is wanted")
+    if q_len is not None:
+        _kv4_ints(index, q_len=(q_len, torch.int32, 1))
+        if q_len.numel() != B:
+            raise ValueError("q_len: one for each sequence is wanted")
+    if out is None:
+        out = torch.empty_like(q)
+    elif out.dtype is not bf16 or out.shape != q.shape or not out.is_contiguous() or out.get_device() != index:
+        raise ValueError("out: a contiguous bf16 CUDA tensor of q's shape is wanted")
+    if scratch is None:
+        scratch = attn_e2m1_scratch(T, nq, nkv, dh, q.device)
+    elif scratch.get_device() != index or not scratch.is_contiguous():
+        raise ValueError("scratch: a contiguous tensor on the call's device is wanted")
+    status = _kv4_status(status, index)
+    if M == 0:
+        return out, status
+    _call(index, lib().pt_kernel_attn_e2m1, q.data_ptr(), pool_l.data_ptr(), pstride, block_table.data_ptr(), block_table.shape[1],
+          None if q_len is None else q_len.data_ptr(), kv_len.data_ptr(), T, B, M, nq, nkv, dh, ps, pool_l.shape[1], out.data_ptr(),
           scratch.data_ptr(), scratch.numel() * scratch.element_size(), status.data_ptr())
     return out, status
 
