@@ -1,5 +1,6 @@
 // Attention of one or a few new tokens per sequence straight from a 4-bit cache (pt_kv_dtype PT_KV_E2M1).
-// A warp per row and head, one key at a time.
+#include <algorithm>
+
 #include "pt_kv4.cuh"
 #include "pt_tc.h"
 #include "pt_ptx.cuh"
@@ -8,63 +9,622 @@ namespace pt {
 
 namespace {
 
-template <int DH>
-__global__ void __launch_bounds__(128) k_kv4_attn(const Kv4AttnP p) {
+constexpr int kTile = 32;                 // keys a warp takes at a time: two blocks of 16
+constexpr int kMaxBlocks = 160;           // thread blocks whose parts the scratch has room for
+constexpr int kSegCost = 2;               // cost of beginning a segment, in tiles
+constexpr uint32_t kSpin = 1u << 24;
+
+template <int DH, int NT> struct Cfg {
+    static constexpr int NG = DH / 32, RB = 8 * NT, BLK = kv4_block(DH);
+    static constexpr int WARPS = 12, STAGES = (NT == 1 ? 3 : 2) * (128 / DH), THREADS = WARPS * 32;
+    static constexpr int STAGE = 2 * BLK, RING = STAGES * STAGE;           // bytes of a warp's ring
+    static constexpr int ROW = DH + 4, PART = RB * ROW + 2 * RB;           // floats of a part: rows, then (reference, sum) of each
+    static constexpr int HEADS = WARPS * RING, BARS = HEADS + WARPS * PART * 4, SMEM = BARS + WARPS * STAGES * 8 + 16;
+    static_assert(PART * 4 <= RING && SMEM <= 227 * 1024 - 4096, "shared memory");
+};
+
+// A segment: the (token, head) rows [r0, r0 + rows) of one sequence, track and KV head, with the keys they see.
+struct SegInfo { int t, h, row0, r0, rows; };
+// What a thread block leaves for the merge: a part whose segment began before it (head) and one that goes on behind it (tail).
+struct Leftover { int head, tail, tail_begins; SegInfo seg; };
+
+template <int DH, int NT> struct Scratch {
+    static constexpr int PART = Cfg<DH, NT>::RB * (DH + 2);                // floats: rows, then (reference, sum) of each
+    Leftover* left;
+    float* parts;
+    __host__ __device__ explicit Scratch(void* p) : left((Leftover*)p), parts((float*)((char*)p + kMaxBlocks * 64)) {}
+    __device__ float* part(int block, int which) const { return parts + (size_t)(2 * block + which) * PART; }
+};
+
+__device__ __forceinline__ float ex2f(float x) {
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+__device__ __forceinline__ uint32_t half2_of(float a, float b) {
+    const __half2 h = __floats2half2_rn(a, b);
+    return *reinterpret_cast<const uint32_t*>(&h);
+}
+__device__ __forceinline__ uint32_t mul2(uint32_t a, uint32_t b) {
+    uint32_t d;
+    asm("mul.rn.f16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
+    return d;
+}
+__device__ __forceinline__ uint32_t transpose8x8(uint32_t a) {
+    uint32_t d;
+    asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(d) : "r"(a));
+    return d;
+}
+__device__ __forceinline__ void mma(float* c, uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+                 : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+// four scale bytes (low first) -> fp16 pairs (bytes 0 and 2), (bytes 1 and 3)
+__device__ __forceinline__ void scales4(uint32_t w, uint32_t& even, uint32_t& odd) { even = (w << 7) & 0x7f807f80u; odd = (w >> 1) & 0x7f807f80u; }
+template <int N> __device__ __forceinline__ void lds(uint32_t at, uint32_t* w) {
+    if constexpr (N == 4) asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]) : "r"(at));
+    else if constexpr (N == 2) asm volatile("ld.shared.v2.u32 {%0, %1}, [%2];" : "=r"(w[0]), "=r"(w[1]) : "r"(at));
+    else asm volatile("ld.shared.u32 %0, [%1];" : "=r"(w[0]) : "r"(at));
+}
+__device__ __forceinline__ void bulk_copy(uint32_t dst, const void* src, uint32_t bytes, uint64_t* bar) {
+    asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
+                 ::"r"(dst), "l"(src), "r"(bytes), "r"(smem_u32(bar)) : "memory");
+}
+
+// Where a warp is in the list of segments: (track, KV head), sequence, row block; and which of the segment's tiles are its own.
+struct Cursor {
+    int th, b, rb, S, K, n, lo, hi;
+    long long left;                        // units of cost of the warp's range behind this segment's
+};
+
+template <int DH, int NT> struct Walk {
+    const Kv4AttnP& p;
+    const int G;
+    __device__ Walk(const Kv4AttnP& p_) : p(p_), G(p_.nq / p_.slab.nkv) {}
+    __device__ int blocks_of(int S) const { return (S * G + Cfg<DH, NT>::RB - 1) / Cfg<DH, NT>::RB; }
+    // keys that the last row of row block rb sees
+    __device__ int seen(int S, int K, int rb) const { return K - S + (min(S * G, (rb + 1) * Cfg<DH, NT>::RB) - 1) / G + 1; }
+    __device__ int tiles(int S, int K, int rb) const { return (seen(S, K, rb) + kTile - 1) / kTile; }
+    __device__ void load(int b, int& S, int& K) const { S = p.qlen ? p.qlen[b] : 1; K = p.kvlen[b]; }
+    // the cursor at unit `in` of its segment; takes what the range has of it
+    __device__ void enter(Cursor& c, long long in) const {
+        c.n = tiles(c.S, c.K, c.rb);
+        const long long end = min((long long)c.n + kSegCost, in + c.left);
+        c.lo = (int)max(0ll, in - kSegCost);
+        c.hi = (int)max(0ll, end - kSegCost);
+        c.left -= end - in;
+    }
+    // to the next segment of the range with tiles in it; false: there is none
+    __device__ bool next(Cursor& c) const {
+        while (c.left > 0) {
+            if (++c.rb >= blocks_of(c.S)) {
+                c.rb = 0;
+                do {
+                    if (++c.b == p.B) { c.b = 0; ++c.th; }
+                    load(c.b, c.S, c.K);
+                } while (c.S == 0);
+            }
+            enter(c, 0);
+            if (c.lo < c.hi) return true;
+        }
+        return false;
+    }
+};
+
+template <int DH, int NT>
+__global__ void __launch_bounds__(Cfg<DH, NT>::THREADS, 1) k_kv4_attn(const Kv4AttnP p, void* scratch, const int per) {
+    using C = Cfg<DH, NT>;
+    constexpr int NG = C::NG, RB = C::RB;
+    extern __shared__ __align__(128) uint8_t smem[];
+    __shared__ long long pre[C::THREADS + 1];
+    __shared__ SegInfo info[2][C::WARPS];
+    __shared__ int flags[C::WARPS];                       // bit 0: a head part, 1: a tail part, 2: the tail's segment begins here
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, q4 = lane & 3;
+    uint64_t* bars = (uint64_t*)(smem + C::BARS) + warp * C::STAGES;
+    if (lane == 0) {
+        for (int i = 0; i < C::STAGES; ++i) mbar_init(&bars[i], 1);
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+    }
     grid_dep_wait();
     grid_dep_launch();
-    constexpr int PER = DH / 32;
-    const int64_t w = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 5);
-    const int lane = threadIdx.x & 31, t = blockIdx.y, nkv = p.slab.nkv, ps = p.slab.ps;
-    if (w >= (int64_t)p.M * p.nq) return;
-    const int r = (int)(w / p.nq), head = (int)(w % p.nq), kvh = head / (p.nq / nkv);
-    int b = -1, pos = 0;
-    int64_t row0 = 0;
+    const Walk<DH, NT> walk(p);
+    const int G = walk.G, nkv = p.slab.nkv, ps = p.slab.ps;
+    // ---- the plan: cost of every sequence, summed; this warp's range of the whole
     bool bad = false;
-    for (int i = 0; i < p.B; ++i) {
-        const int ql = p.qlen ? p.qlen[i] : 1, kl = p.kvlen[i];
-        if (ql < 0 || kl < ql || kl > (int64_t)p.maxp * ps) bad = true;
-        if (b < 0 && r < row0 + ql) { b = i; pos = kl - ql + (int)(r - row0); }
-        row0 += ql;
+    long long rows = 0;
+    kv4_scan(p.B, per, pre, [&](int b) {
+        int S, K;
+        walk.load(b, S, K);
+        if (S < 0 || K < S || K > (long long)p.maxp * ps || S > p.M) { bad = true; return 0ll; }
+        rows += S;
+        long long n = 0;
+        for (int rb = 0, nb = walk.blocks_of(S); rb < nb; ++rb) n += walk.tiles(S, K, rb) + kSegCost;
+        return n;
+    });
+    if (p.qlen) {                                         // all rows: no more than M
+        __shared__ unsigned long long all;
+        if (tid == 0) all = 0;
+        __syncthreads();
+        if (rows) atomicAdd(&all, (unsigned long long)rows);
+        __syncthreads();
+        bad = bad || all > (unsigned long long)p.M;
     }
-    if (bad || row0 > p.M) { if (lane == 0) report(p.status, PT_ERR_DEVICE_BOUNDS, LOC_KV4_LEN); return; }
-    if (b < 0) return;
-    const size_t at = ((size_t)t * p.M + r) * p.nq * DH + (size_t)head * DH;
-    float qv[PER], acc[PER] = {}, m = -INFINITY, l = 0.f;
-    for (int i = 0; i < PER; ++i) qv[i] = __bfloat162float(p.q[at + lane + 32 * i]) * p.scale_log2;
-    for (int j = 0; j <= pos; ++j) {
-        const int page = p.bt[(size_t)b * p.maxp + j / ps];
-        if (page < 0 || page >= p.slab.num_pages) { if (lane == 0) report(p.status, PT_ERR_DEVICE_BOUNDS, LOC_KV4_PAGE); return; }
-        const int sl = j % 16;
-        const char* kc = p.slab.pool_l + (size_t)t * p.slab.tstride + (((int64_t)page * nkv + kvh) * (ps / 16) + j % ps / 16) * kv4_block(DH);
-        const char* vc = kc + kv4_codes(DH) + kv4_scales(DH);
-        float s = 0.f, v[PER];
-        for (int i = 0; i < PER; ++i) {                      // dim 32 i + lane
-            uint32_t h[4];
-            kv4_codes8(*(const uint32_t*)(kc + kv4_k_word(DH, sl, i, lane >> 3)) >> (4 * (lane & 7)), h);
-            s += qv[i] * __low2float(*(const __half2*)h) * kv4_scale((uint8_t)kc[kv4_codes(DH) + kv4_k_scale(DH, sl, i)]);
-            kv4_codes8((uint32_t) * (const uint16_t*)(vc + kv4_v_half(DH, sl, i, lane >> 2)) >> (4 * (lane & 3)), h);
-            v[i] = __low2float(*(const __half2*)h) * kv4_scale((uint8_t)vc[kv4_codes(DH) + kv4_v_scale(DH, sl, i)]);
+    Scratch<DH, NT> sc(scratch);
+    if (__syncthreads_or(bad)) {
+        if (tid == 0) { report(p.status, PT_ERR_DEVICE_BOUNDS, LOC_KV4_LEN); sc.left[blockIdx.x] = Leftover{}; }
+        return;
+    }
+    const long long per_head = pre[C::THREADS], units = per_head * nkv * p.T;
+    const long long used = min((long long)gridDim.x, (units + C::WARPS - 1) / C::WARPS);      // blocks with work
+    Cursor cur{};
+    bool any = false;
+    if (blockIdx.x < used) {
+        const long long gw = (long long)blockIdx.x * C::WARPS + warp, all = used * C::WARPS;
+        const long long u0 = units / all * gw + units % all * gw / all, u1 = units / all * (gw + 1) + units % all * (gw + 1) / all;
+        if (u0 < u1) {
+            cur.th = (int)(u0 / per_head);
+            long long in = u0 - cur.th * per_head;
+            const int i = kv4_find(pre, C::THREADS, in);
+            in -= pre[i];
+            cur.left = u1 - u0;
+            for (cur.b = i * per;; ++cur.b) {
+                walk.load(cur.b, cur.S, cur.K);
+                bool here = false;
+                for (cur.rb = 0; cur.rb < walk.blocks_of(cur.S); ++cur.rb) {
+                    const int n = walk.tiles(cur.S, cur.K, cur.rb) + kSegCost;
+                    if (in < n) { here = true; break; }
+                    in -= n;
+                }
+                if (here) break;
+            }
+            walk.enter(cur, in);
+            any = cur.lo < cur.hi || walk.next(cur);
         }
-        for (int o = 16; o; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
-        const float nm = fmaxf(m, s), corr = exp2f(m - nm), wgt = exp2f(s - nm);
-        l = l * corr + wgt;
-        for (int i = 0; i < PER; ++i) acc[i] = acc[i] * corr + wgt * v[i];
-        m = nm;
     }
-    for (int i = 0; i < PER; ++i) p.o[at + lane + 32 * i] = __float2bfloat16_rn(acc[i] / l);
+    // ---- the ring: lanes 0 and 1 fetch a block of 16 keys each; pages are looked up one tile ahead
+    uint8_t* ring = smem + warp * C::RING;
+    Cursor ahead = cur;
+    int a_tile = cur.lo, a_page = -1;
+    bool a_any = any, bad_page = false;
+    auto look = [&]() {
+        const int key = a_tile * kTile + 16 * lane;
+        if (a_any && lane < 2 && key < walk.seen(ahead.S, ahead.K, ahead.rb)) a_page = p.bt[(size_t)ahead.b * p.maxp + key / ps];
+    };
+    look();
+    auto issue = [&](int slot) {
+        const int key = a_tile * kTile + 16 * lane;
+        bool go = lane < 2 && key < walk.seen(ahead.S, ahead.K, ahead.rb);
+        if (go && (a_page < 0 || a_page >= p.slab.num_pages)) { bad_page = true; go = false; }
+        const unsigned who = __ballot_sync(0xffffffffu, go);
+        if (lane == 0) mbar_expect_tx(&bars[slot], __popc(who) * C::BLK);
+        __syncwarp();
+        if (go) {
+            const int t = ahead.th / nkv, h = ahead.th - t * nkv;
+            const char* src = p.slab.pool_l + (size_t)t * p.slab.tstride + (((int64_t)a_page * nkv + h) * (ps / 16) + key % ps / 16) * C::BLK;
+            bulk_copy(smem_u32(ring + slot * C::STAGE + lane * C::BLK), src, C::BLK, &bars[slot]);
+        }
+        if (++a_tile == ahead.hi) { a_any = walk.next(ahead); a_tile = ahead.lo; }
+        look();
+    };
+    __syncwarp();
+    for (int s = 0; s < C::STAGES; ++s) if (a_any) issue(s);
+
+    int slot = 0, done = 0, my_flags = 0;
+    uint32_t parity = 0;
+    bool timed_out = false;
+    while (any && !timed_out) {
+        // ---- a segment: its queries
+        const int t = cur.th / nkv, h = cur.th - t * nkv, R = cur.S * G, r0 = cur.rb * RB;
+        int row0 = 0;                                     // first row of the sequence
+        if (p.qlen) {
+            for (int b = lane; b < cur.b; b += 32) row0 += p.qlen[b];
+#pragma unroll
+            for (int o = 16; o; o >>= 1) row0 += __shfl_xor_sync(0xffffffffu, row0, o);
+        } else {
+            row0 = cur.b;
+        }
+        uint32_t qf[NG][NT][4];
+        float unit[NT][2];
+        int lim[NT][2];
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+            const int r = r0 + nt * 8 + g, tok = r / G;
+            uint4 raw[NG];
+            uint32_t top = 0;
+#pragma unroll
+            for (int j = 0; j < NG; ++j) {
+                raw[j] = r < R ? *reinterpret_cast<const uint4*>(p.q + (((size_t)t * p.M + row0 + tok) * p.nq + h * G + (r - tok * G)) * DH + 32 * j + 8 * q4) : make_uint4(0, 0, 0, 0);
+                const uint32_t w[4] = {raw[j].x, raw[j].y, raw[j].z, raw[j].w};
+#pragma unroll
+                for (int i = 0; i < 4; ++i) top = __vmaxu2(top, w[i] & 0x7fff7fffu);
+            }
+            top = max(top & 0xffffu, top >> 16);
+            top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
+            top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
+            // divided by the power of two that puts the row's largest magnitude into [2^13, 2^14)
+            int e = (int)(top >> 7) - 127;
+            if (top >= 0x7f80u) e = 13;                   // not finite: as it is
+            e = max(e, -100);
+            const float inv = __uint_as_float((uint32_t)(13 - e + 127) << 23);
+            const float un = __uint_as_float((uint32_t)(e - 13 + 127) << 23) * p.scale_log2;
+#pragma unroll
+            for (int j = 0; j < NG; ++j) {
+                const uint32_t w[4] = {raw[j].x, raw[j].y, raw[j].z, raw[j].w};
+#pragma unroll
+                for (int i = 0; i < 4; ++i) qf[j][nt][i] = half2_of(__uint_as_float(w[i] << 16) * inv, __uint_as_float(w[i] & 0xffff0000u) * inv);
+            }
+#pragma unroll
+            for (int c = 0; c < 2; ++c) {
+                unit[nt][c] = __shfl_sync(0xffffffffu, un, (2 * q4 + c) * 4);
+                lim[nt][c] = cur.K - cur.S + min((r0 + nt * 8 + 2 * q4 + c) / G, cur.S - 1) + 1;
+            }
+        }
+        const int all_see = cur.K - cur.S + r0 / G + 1, seen = walk.seen(cur.S, cur.K, cur.rb);
+        float o[NG][2][NT][4] = {}, ref[NT][2], l[NT][2];
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+            for (int c = 0; c < 2; ++c) { ref[nt][c] = -INFINITY; l[nt][c] = 0.f; }
+        float boost = 14.f;
+        for (int tile = cur.lo; tile < cur.hi; ++tile) {
+            bool ok = false;
+            {
+                WaitClock clock;
+                for (uint32_t spin = 0; spin < kSpin; ++spin) {
+                    if (mbar_try(&bars[slot], parity)) { ok = true; break; }
+                    if ((spin & 255) == 255 && clock.expired()) break;
+                }
+            }
+            if (!__all_sync(0xffffffffu, ok)) { timed_out = true; break; }
+            const uint32_t base = smem_u32(ring + slot * C::STAGE);
+            const int key0 = tile * kTile;
+            // ---- scores
+            float s[2][NT][4] = {};
+#pragma unroll
+            for (int hb = 0; hb < 2; ++hb) {
+                const uint32_t kb = base + hb * C::BLK;
+                uint32_t kw[2][NG], ks[NG / 2];
+                lds<NG>(kb + g * (DH / 2) + q4 * (DH / 8), kw[0]);
+                lds<NG>(kb + (g + 8) * (DH / 2) + q4 * (DH / 8), kw[1]);
+                lds<NG / 2>(kb + kv4_codes(DH) + g * 2 * NG, ks);
+                float scf[2][NG];
+                if constexpr (NG == 4) {
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) {
+                        uint32_t even, odd;
+                        scales4(ks[i], even, odd);
+                        const float2 a = __half22float2(*reinterpret_cast<__half2*>(&even)), b = __half22float2(*reinterpret_cast<__half2*>(&odd));
+                        scf[i][0] = a.x; scf[i][2] = a.y; scf[i][1] = b.x; scf[i][3] = b.y;
+                    }
+                } else {
+                    uint32_t even, odd;
+                    scales4(ks[0], even, odd);
+                    const float2 a = __half22float2(*reinterpret_cast<__half2*>(&even)), b = __half22float2(*reinterpret_cast<__half2*>(&odd));
+                    scf[0][0] = a.x; scf[1][0] = a.y; scf[0][1] = b.x; scf[1][1] = b.y;
+                }
+#pragma unroll
+                for (int j = 0; j < NG; ++j) {
+                    uint32_t h0[4], h1[4];
+                    kv4_codes8(kw[0][j], h0);
+                    kv4_codes8(kw[1][j], h1);
+#pragma unroll
+                    for (int nt = 0; nt < NT; ++nt) {
+                        float c[4] = {};
+                        mma(c, h0[0], h1[0], h0[1], h1[1], qf[j][nt][0], qf[j][nt][1]);
+                        mma(c, h0[2], h1[2], h0[3], h1[3], qf[j][nt][2], qf[j][nt][3]);
+                        s[hb][nt][0] += c[0] * scf[0][j]; s[hb][nt][1] += c[1] * scf[0][j];
+                        s[hb][nt][2] += c[2] * scf[1][j]; s[hb][nt][3] += c[3] * scf[1][j];
+                    }
+                }
+            }
+            // ---- V's scales: bytes of keys 4 q4 .. + 3; nothing behind the last key counts
+            uint32_t vs[2][NG], high = 0;
+#pragma unroll
+            for (int hb = 0; hb < 2; ++hb) {
+                lds<NG>(base + hb * C::BLK + 2 * kv4_codes(DH) + kv4_scales(DH) + q4 * (DH / 8), vs[hb]);
+                if (key0 + kTile > seen) {
+                    const int nv = min(max(seen - (key0 + 16 * hb + 4 * q4), 0), 4);
+                    const uint32_t keep = nv == 4 ? 0xffffffffu : (1u << (8 * nv)) - 1u;
+#pragma unroll
+                    for (int j = 0; j < NG; ++j) vs[hb][j] &= keep;
+                }
+#pragma unroll
+                for (int j = 0; j < NG; ++j) high |= vs[hb][j];
+            }
+            float drop = 0.f;
+            if (__any_sync(0xffffffffu, high & 0x80808080u)) {    // a scale of 2 or more: weights times scales must stay below 2^16
+                float top = 0.f;
+#pragma unroll
+                for (int hb = 0; hb < 2; ++hb)
+#pragma unroll
+                    for (int j = 0; j < NG; ++j)
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) top = fmaxf(top, kv4_scale((vs[hb][j] >> (8 * i)) & 0xffu));
+#pragma unroll
+                for (int m = 1; m < 4; m <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, m));
+                const float fits = (float)max(0, 15 - ((int)(__float_as_uint(top) >> 23) - 127));
+                if (fits < boost) { drop = boost - fits; boost = fits; }
+            }
+            // ---- weights
+            const bool mask = key0 + kTile > all_see;
+            float corr[NT][2];
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                for (int c = 0; c < 2; ++c) {
+                    float mx = -INFINITY;
+#pragma unroll
+                    for (int hb = 0; hb < 2; ++hb)
+#pragma unroll
+                        for (int i = 0; i < 2; ++i) {
+                            float& x = s[hb][nt][2 * i + c];
+                            x *= unit[nt][c];
+                            if (mask && key0 + 16 * hb + 2 * g + i >= lim[nt][c]) x = -INFINITY;
+                            mx = fmaxf(mx, x);
+                        }
+                    mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 4));
+                    mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 8));
+                    mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 16));
+                    const float nr = fmaxf(ref[nt][c] + drop, mx - boost);       // -inf as long as there is nothing to see
+                    corr[nt][c] = nr == -INFINITY ? 1.f : ex2f(ref[nt][c] - nr);
+                    ref[nt][c] = nr;
+                    const float r = nr == -INFINITY ? 0.f : nr;
+                    float sum = 0.f;
+#pragma unroll
+                    for (int hb = 0; hb < 2; ++hb)
+#pragma unroll
+                        for (int i = 0; i < 2; ++i) { float& x = s[hb][nt][2 * i + c]; x = ex2f(x - r); sum += x; }
+                    l[nt][c] = l[nt][c] * corr[nt][c] + sum;
+                }
+            bool change = false;
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) change = change || corr[nt][0] != 1.f || corr[nt][1] != 1.f;
+            if (__any_sync(0xffffffffu, change)) {
+#pragma unroll
+                for (int j = 0; j < NG; ++j)
+#pragma unroll
+                    for (int mt = 0; mt < 2; ++mt)
+#pragma unroll
+                        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                            for (int i = 0; i < 4; ++i) o[j][mt][nt][i] *= corr[nt][i & 1];
+            }
+            // ---- weights times V
+#pragma unroll
+            for (int hb = 0; hb < 2; ++hb) {
+                const uint32_t vb = base + hb * C::BLK + kv4_codes(DH) + kv4_scales(DH);
+                uint32_t b0[NT], b1[NT];
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt) {
+                    b0[nt] = transpose8x8(half2_of(s[hb][nt][0], s[hb][nt][1]));
+                    b1[nt] = transpose8x8(half2_of(s[hb][nt][2], s[hb][nt][3]));
+                }
+                uint32_t x[4][NG / 2];                            // codes of keys 4 q4 + i
+                if constexpr (NG == 4) {
+                    uint32_t w[4];
+                    lds<4>(vb + lane * 16, w);
+                    x[0][0] = w[0]; x[0][1] = w[1]; x[1][0] = w[2]; x[1][1] = w[3];
+                    lds<4>(vb + 512 + lane * 16, w);
+                    x[2][0] = w[0]; x[2][1] = w[1]; x[3][0] = w[2]; x[3][1] = w[3];
+                } else {
+                    uint32_t w[4];
+                    lds<4>(vb + lane * 16, w);
+                    x[0][0] = w[0]; x[1][0] = w[1]; x[2][0] = w[2]; x[3][0] = w[3];
+                }
+#pragma unroll
+                for (int jj = 0; jj < NG / 2; ++jj) {
+                    constexpr uint32_t m = 0x0f0f0f0fu;
+                    uint32_t a0[4], a1[4], a2[4], a3[4];          // byte e / 2 of group 2 jj, then of group 2 jj + 1
+                    kv4_codes8((x[0][jj] & m) | ((x[2][jj] << 4) & ~m), a0);
+                    kv4_codes8(((x[0][jj] >> 4) & m) | (x[2][jj] & ~m), a1);
+                    kv4_codes8((x[1][jj] & m) | ((x[3][jj] << 4) & ~m), a2);
+                    kv4_codes8(((x[1][jj] >> 4) & m) | (x[3][jj] & ~m), a3);
+#pragma unroll
+                    for (int jl = 0; jl < 2; ++jl) {
+                        const int j = 2 * jj + jl;
+                        uint32_t even, odd;
+                        scales4(vs[hb][j], even, odd);
+#pragma unroll
+                        for (int nt = 0; nt < NT; ++nt) {
+                            const uint32_t p0 = mul2(b0[nt], even), p1 = mul2(b1[nt], odd);
+                            mma(o[j][0][nt], a0[2 * jl], a1[2 * jl], a2[2 * jl], a3[2 * jl], p0, p1);
+                            mma(o[j][1][nt], a0[2 * jl + 1], a1[2 * jl + 1], a2[2 * jl + 1], a3[2 * jl + 1], p0, p1);
+                        }
+                    }
+                }
+            }
+            __syncwarp();                                         // every lane is done with the slot
+            if (a_any) { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); issue(slot); }
+            ++done;
+            if (++slot == C::STAGES) { slot = 0; parity ^= 1; }
+        }
+        if (timed_out) break;
+        // ---- the end of the piece
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+            for (int c = 0; c < 2; ++c)
+#pragma unroll
+                for (int m = 4; m < 32; m <<= 1) l[nt][c] += __shfl_xor_sync(0xffffffffu, l[nt][c], m);
+        const bool begins = cur.lo == 0, ends = cur.hi == cur.n;
+        const SegInfo si{t, h, row0, r0, min(RB, R - r0)};
+        if (begins && ends) {                                     // all of the segment's keys: the result
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                for (int c = 0; c < 2; ++c) {
+                    const int r = nt * 8 + 2 * q4 + c;
+                    if (r >= si.rows) continue;
+                    const int tok = (r0 + r) / G, hd = r0 + r - tok * G;
+                    const float inv = 1.0f / l[nt][c];
+                    __nv_bfloat16* dst = p.o + (((size_t)t * p.M + row0 + tok) * p.nq + h * G + hd) * DH + 4 * g;
+#pragma unroll
+                    for (int j = 0; j < NG; ++j)
+                        *reinterpret_cast<uint2*>(dst + 32 * j) = make_uint2(kv4_bf16(o[j][0][nt][c] * inv, o[j][0][nt][2 + c] * inv),
+                                                                            kv4_bf16(o[j][1][nt][c] * inv, o[j][1][nt][2 + c] * inv));
+                }
+        } else {                                                  // a part: merged below, or by k_kv4_merge
+            float* part = ends ? (float*)(smem + C::HEADS) + warp * C::PART : (float*)ring;
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                for (int c = 0; c < 2; ++c) {
+                    const int r = nt * 8 + 2 * q4 + c;
+#pragma unroll
+                    for (int j = 0; j < NG; ++j)
+                        *reinterpret_cast<float4*>(part + r * C::ROW + 32 * j + 4 * g) = make_float4(o[j][0][nt][c], o[j][0][nt][2 + c], o[j][1][nt][c], o[j][1][nt][2 + c]);
+                    if (g == 0) { part[RB * C::ROW + 2 * r] = ref[nt][c]; part[RB * C::ROW + 2 * r + 1] = l[nt][c]; }
+                }
+            my_flags |= ends ? 1 : begins ? 6 : 2;
+            if (lane == 0) info[ends ? 0 : 1][warp] = si;
+        }
+        any = walk.next(cur);
+    }
+    if (timed_out) {
+        // give the copies that are still in flight a bounded chance to land, then give up
+        WaitClock clock;
+        for (int s2 = 0; s2 < C::STAGES; ++s2)
+            for (uint32_t spin = 0; spin < (1u << 16); ++spin) {
+                if (mbar_try(&bars[s2], 0) || mbar_try(&bars[s2], 1)) break;
+                if ((spin & 63) == 63 && clock.expired(100000000ull)) break;
+            }
+        if (lane == 0) report(p.status, PT_ERR_DEVICE_TIMEOUT, LOC_KV4_WAIT);
+        my_flags = 0;
+    }
+    if (bad_page) report(p.status, PT_ERR_DEVICE_BOUNDS, LOC_KV4_PAGE);
+    if (lane == 0) flags[warp] = my_flags;
+    __syncthreads();
+
+    // ---- parts of one segment side by side in this block's warps: to the result, or to one part for the merge
+    auto part_of = [&](int w, int which) { return which == 0 ? (const float*)(smem + C::HEADS) + w * C::PART : (const float*)(smem + w * C::RING); };
+    auto combine = [&](int w0, int w1, bool head, bool result, int which) {     // tails of warps w0 .. w1 - 1 and the head of warp w1, if `head`
+        const SegInfo si = head ? info[0][w1] : info[1][w0];
+        for (int i = tid; i < si.rows * (DH / 4); i += C::THREADS) {
+            const int r = i / (DH / 4), d = i % (DH / 4) * 4;
+            float top = -INFINITY, sum = 0.f;
+            float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+            for (int w = w0; w <= w1; ++w) {
+                if (w == w1 ? !head : !(flags[w] & 2)) continue;
+                top = fmaxf(top, part_of(w, w == w1 ? 0 : 1)[RB * C::ROW + 2 * r]);
+            }
+            for (int w = w0; w <= w1; ++w) {
+                if (w == w1 ? !head : !(flags[w] & 2)) continue;
+                const float* part = part_of(w, w == w1 ? 0 : 1);
+                const float m = part[RB * C::ROW + 2 * r], f = m == -INFINITY ? 0.f : ex2f(m - top);
+                const float4 x = *reinterpret_cast<const float4*>(part + r * C::ROW + d);
+                sum += part[RB * C::ROW + 2 * r + 1] * f;
+                acc.x += x.x * f; acc.y += x.y * f; acc.z += x.z * f; acc.w += x.w * f;
+            }
+            if (result) {
+                const int tok = (si.r0 + r) / G, hd = si.r0 + r - tok * G;
+                const float inv = 1.0f / sum;
+                *reinterpret_cast<uint2*>(p.o + (((size_t)si.t * p.M + si.row0 + tok) * p.nq + si.h * G + hd) * DH + d) =
+                    make_uint2(kv4_bf16(acc.x * inv, acc.y * inv), kv4_bf16(acc.z * inv, acc.w * inv));
+            } else {
+                float* to = sc.part(blockIdx.x, which);
+                *reinterpret_cast<float4*>(to + r * DH + d) = acc;
+                if (d == 0) { to[RB * DH + 2 * r] = top; to[RB * DH + 2 * r + 1] = sum; }
+            }
+        }
+    };
+    Leftover left{};
+    int first = 0;
+    bool begun = false, open = false;                             // the chain of parts: does it begin in this block; has it any
+    for (int w = 0; w < C::WARPS; ++w) {
+        const int f = flags[w];
+        if (f & 1) {
+            combine(open ? first : w, w, true, begun, 0);
+            if (!begun) left.head = 1;
+            open = begun = false;
+        }
+        if (f & 2) {
+            if (!open) { first = w; begun = (f & 4) != 0; open = true; }
+        }
+    }
+    if (open) {
+        combine(first, C::WARPS, false, false, 1);
+        left.tail = 1; left.tail_begins = begun; left.seg = info[1][first];
+    }
+    if (tid == 0) sc.left[blockIdx.x] = left;
+}
+
+// Merges the parts of the segments that thread blocks cut: block (c, r) has row r of the segment that begins in block c and
+// goes on behind it.
+constexpr int kMergeThreads = 256;
+template <int DH, int NT>
+__global__ void __launch_bounds__(kMergeThreads) k_kv4_merge(const Kv4AttnP p, void* scratch, const int blocks) {
+    constexpr int GROUPS = kMergeThreads / DH, RB = Cfg<DH, NT>::RB;
+    __shared__ float sh[GROUPS][DH + 2];
+    grid_dep_wait();
+    grid_dep_launch();
+    const Scratch<DH, NT> sc(scratch);
+    const Leftover first = sc.left[blockIdx.x];
+    const int r = blockIdx.y, d = threadIdx.x % DH, grp = threadIdx.x / DH;
+    if (!first.tail || !first.tail_begins || r >= first.seg.rows) return;
+    float top = -INFINITY, sum = 0.f, acc = 0.f;
+    for (int c = blockIdx.x, k = 0; c < blocks; ++c) {
+        const int which = c == (int)blockIdx.x || !sc.left[c].head;      // the head of the last block, the tails of the others
+        const bool last = which == 0;
+        if (which == 1 && !sc.left[c].tail) continue;                     // a block without work
+        if (k++ % GROUPS == grp) {
+            const float* part = sc.part(c, which);
+            const float m = part[RB * DH + 2 * r], ls = part[RB * DH + 2 * r + 1], x = part[r * DH + d];
+            const float nt = fmaxf(top, m), f0 = top == -INFINITY ? 0.f : ex2f(top - nt), f1 = m == -INFINITY ? 0.f : ex2f(m - nt);
+            acc = acc * f0 + x * f1;
+            sum = sum * f0 + ls * f1;
+            top = nt;
+        }
+        if (last) break;
+    }
+    sh[grp][d] = acc;
+    if (d == 0) { sh[grp][DH] = top; sh[grp][DH + 1] = sum; }
+    __syncthreads();
+    if (grp) return;
+    float all = -INFINITY;
+#pragma unroll
+    for (int i = 0; i < GROUPS; ++i) all = fmaxf(all, sh[i][DH]);
+    acc = sum = 0.f;
+#pragma unroll
+    for (int i = 0; i < GROUPS; ++i) {
+        const float f = sh[i][DH] == -INFINITY ? 0.f : ex2f(sh[i][DH] - all);
+        acc += sh[i][d] * f;
+        sum += sh[i][DH + 1] * f;
+    }
+    const int G = p.nq / p.slab.nkv, tok = (first.seg.r0 + r) / G, hd = first.seg.r0 + r - tok * G;
+    p.o[(((size_t)first.seg.t * p.M + first.seg.row0 + tok) * p.nq + first.seg.h * G + hd) * DH + d] = __float2bfloat16_rn(acc / sum);
+}
+
+template <int DH, int NT> pt_status launch_t(const Kv4AttnP& p, void* scratch, cudaStream_t st) {
+    using C = Cfg<DH, NT>;
+    static int sms_[kMaxDevices] = {};
+    int& sms = sms_[current_device()];
+    if (!sms) {
+        int n = 0;
+        cudaError_t e = cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, current_device());
+        if (e == cudaSuccess) e = cudaFuncSetAttribute(k_kv4_attn<DH, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, C::SMEM);
+        if (e != cudaSuccess) { set_error("4-bit attention setup: %s", cudaGetErrorString(e)); return PT_ERR_CUDA; }
+        sms = n;
+    }
+    const int blocks = std::min(sms, kMaxBlocks);
+    cudaError_t e = launch_dependent(k_kv4_attn<DH, NT>, dim3(blocks), dim3(C::THREADS), (size_t)C::SMEM, st, p, scratch, (p.B + C::THREADS - 1) / C::THREADS);
+    g_launches.fetch_add(1, std::memory_order_relaxed);
+    if (e == cudaSuccess && blocks > 1) {
+        e = launch_dependent(k_kv4_merge<DH, NT>, dim3(blocks - 1, C::RB), dim3(kMergeThreads), (size_t)0, st, p, scratch, blocks);
+        g_launches.fetch_add(1, std::memory_order_relaxed);
+    }
+    if (e != cudaSuccess) { set_error("4-bit attention launch: %s", cudaGetErrorString(e)); return PT_ERR_CUDA; }
+    return PT_OK;
 }
 
 }  // namespace
 
-size_t kv4_attn_scratch_bytes(int dh) { return (size_t)160 * 2 * 16 * (dh + 2) * 4; }
+size_t kv4_attn_scratch_bytes(int dh) { return (size_t)kMaxBlocks * 64 + (size_t)kMaxBlocks * 2 * 16 * (dh + 2) * 4; }
 
 pt_status launch_kv4_attn(const Kv4AttnP& p, int dh, void* scratch, cudaStream_t st) {
-    (void)scratch;
-    const dim3 grid((unsigned)(((int64_t)p.M * p.nq + 3) / 4), p.T);
-    const cudaError_t e = launch_dependent(dh == 64 ? k_kv4_attn<64> : k_kv4_attn<128>, grid, dim3(128), (size_t)0, st, p);
-    if (e != cudaSuccess) { set_error("k_kv4_attn launch: %s", cudaGetErrorString(e)); return PT_ERR_CUDA; }
-    g_launches.fetch_add(1, std::memory_order_relaxed);
-    return PT_OK;
+    const bool wide = p.qlen && (int64_t)p.M * (p.nq / p.slab.nkv) > 8 * (int64_t)p.B;
+    if (dh == 64) return wide ? launch_t<64, 2>(p, scratch, st) : launch_t<64, 1>(p, scratch, st);
+    return wide ? launch_t<128, 2>(p, scratch, st) : launch_t<128, 1>(p, scratch, st);
 }
 
 }  // namespace pt
