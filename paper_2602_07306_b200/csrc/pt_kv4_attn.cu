@@ -13,10 +13,16 @@ constexpr int kTile = 32;                 // keys a warp takes at a time: two bl
 constexpr int kMaxBlocks = 160;           // thread blocks whose parts the scratch has room for
 constexpr int kSegCost = 2;               // cost of beginning a segment, in tiles
 constexpr uint32_t kSpin = 1u << 24;
+constexpr float kTop = 14.f, kStart = 8.f; // weights stay below 2^kTop; a reference is set so that the largest is 2^kStart
+constexpr float kNone = -3.0e38f;         // reference of a row that has seen nothing
 
+#ifndef KW
+#define KW 12
+#define KS 3
+#endif
 template <int DH, int NT> struct Cfg {
     static constexpr int NG = DH / 32, RB = 8 * NT, BLK = kv4_block(DH);
-    static constexpr int WARPS = 12, STAGES = (NT == 1 ? 3 : 2) * (128 / DH), THREADS = WARPS * 32;
+    static constexpr int WARPS = NT == 1 ? KW : 12, STAGES = (NT == 1 ? KS : 2) * (128 / DH), THREADS = WARPS * 32;
     static constexpr int STAGE = 2 * BLK, RING = STAGES * STAGE;           // bytes of a warp's ring
     static constexpr int ROW = DH + 4, PART = RB * ROW + 2 * RB;           // floats of a part: rows, then (reference, sum) of each
     static constexpr int HEADS = WARPS * RING, BARS = HEADS + WARPS * PART * 4, SMEM = BARS + WARPS * STAGES * 8 + 16;
@@ -59,6 +65,11 @@ __device__ __forceinline__ void mma(float* c, uint32_t a0, uint32_t a1, uint32_t
     asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
                  : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
+// the same with an accumulator of zeros
+__device__ __forceinline__ void mma0(float* c, uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%10, %10, %10, %10};"
+                 : "=f"(c[0]), "=f"(c[1]), "=f"(c[2]), "=f"(c[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(0.f));
+}
 // four scale bytes (low first) -> fp16 pairs (bytes 0 and 2), (bytes 1 and 3)
 __device__ __forceinline__ void scales4(uint32_t w, uint32_t& even, uint32_t& odd) { even = (w << 7) & 0x7f807f80u; odd = (w >> 1) & 0x7f807f80u; }
 template <int N> __device__ __forceinline__ void lds(uint32_t at, uint32_t* w) {
@@ -73,7 +84,7 @@ __device__ __forceinline__ void bulk_copy(uint32_t dst, const void* src, uint32_
 
 // Where a warp is in the list of segments: (track, KV head), sequence, row block; and which of the segment's tiles are its own.
 struct Cursor {
-    int th, b, rb, S, K, n, lo, hi;
+    int th, b, rb, S, K, seen, n, lo, hi;  // seen: keys that the block's last row sees; n: tiles of those
     long long left;                        // units of cost of the warp's range behind this segment's
 };
 
@@ -88,7 +99,8 @@ template <int DH, int NT> struct Walk {
     __device__ void load(int b, int& S, int& K) const { S = p.qlen ? p.qlen[b] : 1; K = p.kvlen[b]; }
     // the cursor at unit `in` of its segment; takes what the range has of it
     __device__ void enter(Cursor& c, long long in) const {
-        c.n = tiles(c.S, c.K, c.rb);
+        c.seen = seen(c.S, c.K, c.rb);
+        c.n = (c.seen + kTile - 1) / kTile;
         const long long end = min((long long)c.n + kSegCost, in + c.left);
         c.lo = (int)max(0ll, in - kSegCost);
         c.hi = (int)max(0ll, end - kSegCost);
@@ -185,27 +197,37 @@ __global__ void __launch_bounds__(Cfg<DH, NT>::THREADS, 1) k_kv4_attn(const Kv4A
     // ---- the ring: lanes 0 and 1 fetch a block of 16 keys each; pages are looked up one tile ahead
     uint8_t* ring = smem + warp * C::RING;
     Cursor ahead = cur;
-    int a_tile = cur.lo, a_page = -1;
+    const int bpp = ps / 16;                              // blocks of a page: 1 .. 4
+    const int64_t page_bytes = (int64_t)nkv * bpp * C::BLK;
+    int a_tile = cur.lo, a_in = 0, a_page = -1;
     bool a_any = any, bad_page = false;
-    auto look = [&]() {
-        const int key = a_tile * kTile + 16 * lane;
-        if (a_any && lane < 2 && key < walk.seen(ahead.S, ahead.K, ahead.rb)) a_page = p.bt[(size_t)ahead.b * p.maxp + key / ps];
+    const char* a_base = nullptr;                         // the head's first block in page 0
+    const int32_t* a_bt = nullptr;
+    auto aim = [&]() {
+        const int t = ahead.th / nkv, h = ahead.th - t * nkv;
+        a_base = p.slab.pool_l + (size_t)t * p.slab.tstride + (size_t)h * bpp * C::BLK;
+        a_bt = p.bt + (size_t)ahead.b * p.maxp;
+        a_tile = ahead.lo;
     };
-    look();
+    auto look = [&]() {
+        const int blk = 2 * a_tile + lane;
+        const int col = bpp == 3 ? (int)__umulhi((uint32_t)blk, 0x55555556u) : blk >> (bpp >> 1);
+        a_in = blk - col * bpp;
+        if (lane < 2 && blk * 16 < ahead.seen) a_page = a_bt[col];
+    };
+    if (a_any) { aim(); look(); }
     auto issue = [&](int slot) {
-        const int key = a_tile * kTile + 16 * lane;
-        bool go = lane < 2 && key < walk.seen(ahead.S, ahead.K, ahead.rb);
-        if (go && (a_page < 0 || a_page >= p.slab.num_pages)) { bad_page = true; go = false; }
+        bool go = lane < 2 && a_tile * kTile + 16 * lane < ahead.seen;
+        if (go && (uint32_t)a_page >= (uint32_t)p.slab.num_pages) { bad_page = true; go = false; }
         const unsigned who = __ballot_sync(0xffffffffu, go);
         if (lane == 0) mbar_expect_tx(&bars[slot], __popc(who) * C::BLK);
         __syncwarp();
-        if (go) {
-            const int t = ahead.th / nkv, h = ahead.th - t * nkv;
-            const char* src = p.slab.pool_l + (size_t)t * p.slab.tstride + (((int64_t)a_page * nkv + h) * (ps / 16) + key % ps / 16) * C::BLK;
-            bulk_copy(smem_u32(ring + slot * C::STAGE + lane * C::BLK), src, C::BLK, &bars[slot]);
+        if (go) bulk_copy(smem_u32(ring + slot * C::STAGE + lane * C::BLK), a_base + a_page * page_bytes + a_in * C::BLK, C::BLK, &bars[slot]);
+        if (++a_tile == ahead.hi) {
+            a_any = walk.next(ahead);
+            if (a_any) aim();
         }
-        if (++a_tile == ahead.hi) { a_any = walk.next(ahead); a_tile = ahead.lo; }
-        look();
+        if (a_any) look();
     };
     __syncwarp();
     for (int s = 0; s < C::STAGES; ++s) if (a_any) issue(s);
@@ -260,13 +282,13 @@ __global__ void __launch_bounds__(Cfg<DH, NT>::THREADS, 1) k_kv4_attn(const Kv4A
                 lim[nt][c] = cur.K - cur.S + min((r0 + nt * 8 + 2 * q4 + c) / G, cur.S - 1) + 1;
             }
         }
-        const int all_see = cur.K - cur.S + r0 / G + 1, seen = walk.seen(cur.S, cur.K, cur.rb);
+        const int all_see = cur.K - cur.S + r0 / G + 1, seen = cur.seen;
         float o[NG][2][NT][4] = {}, ref[NT][2], l[NT][2];
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-            for (int c = 0; c < 2; ++c) { ref[nt][c] = -INFINITY; l[nt][c] = 0.f; }
-        float boost = 14.f;
+            for (int c = 0; c < 2; ++c) { ref[nt][c] = kNone; l[nt][c] = 0.f; }
+        float room = kTop;                                        // weights stay below 2^room
         for (int tile = cur.lo; tile < cur.hi; ++tile) {
             bool ok = false;
             {
@@ -280,7 +302,7 @@ __global__ void __launch_bounds__(Cfg<DH, NT>::THREADS, 1) k_kv4_attn(const Kv4A
             const uint32_t base = smem_u32(ring + slot * C::STAGE);
             const int key0 = tile * kTile;
             // ---- scores
-            float s[2][NT][4] = {};
+            float s[2][NT][4];
 #pragma unroll
             for (int hb = 0; hb < 2; ++hb) {
                 const uint32_t kb = base + hb * C::BLK;
@@ -310,11 +332,11 @@ __global__ void __launch_bounds__(Cfg<DH, NT>::THREADS, 1) k_kv4_attn(const Kv4A
                     kv4_codes8(kw[1][j], h1);
 #pragma unroll
                     for (int nt = 0; nt < NT; ++nt) {
-                        float c[4] = {};
-                        mma(c, h0[0], h1[0], h0[1], h1[1], qf[j][nt][0], qf[j][nt][1]);
+                        float c[4];
+                        mma0(c, h0[0], h1[0], h0[1], h1[1], qf[j][nt][0], qf[j][nt][1]);
                         mma(c, h0[2], h1[2], h0[3], h1[3], qf[j][nt][2], qf[j][nt][3]);
-                        s[hb][nt][0] += c[0] * scf[0][j]; s[hb][nt][1] += c[1] * scf[0][j];
-                        s[hb][nt][2] += c[2] * scf[1][j]; s[hb][nt][3] += c[3] * scf[1][j];
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) s[hb][nt][i] = j ? fmaf(c[i], scf[i >> 1][j], s[hb][nt][i]) : c[i] * scf[i >> 1][j];
                     }
                 }
             }
@@ -332,8 +354,27 @@ __global__ void __launch_bounds__(Cfg<DH, NT>::THREADS, 1) k_kv4_attn(const Kv4A
 #pragma unroll
                 for (int j = 0; j < NG; ++j) high |= vs[hb][j];
             }
-            float drop = 0.f;
-            if (__any_sync(0xffffffffu, high & 0x80808080u)) {    // a scale of 2 or more: weights times scales must stay below 2^16
+            // ---- weights 2^(score - reference).  The reference lags behind the maximum: it is raised, and what has been summed
+            // scaled down, only where a weight would pass 2^kTop, or where a scale of V of 2 or more has to be made room for
+            if (key0 + kTile > all_see) {                         // some row does not see all of the tile
+#pragma unroll
+                for (int hb = 0; hb < 2; ++hb)
+#pragma unroll
+                    for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                        for (int i = 0; i < 4; ++i)
+                            if (key0 + 16 * hb + 2 * g + (i >> 1) >= lim[nt][i & 1]) s[hb][nt][i] = -INFINITY;
+            }
+            float mx[NT][2];
+            bool over = (high & 0x80808080u) != 0;
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                for (int c = 0; c < 2; ++c) {
+                    mx[nt][c] = fmaxf(fmaxf(s[0][nt][c], s[0][nt][2 + c]), fmaxf(s[1][nt][c], s[1][nt][2 + c]));
+                    over = over || fmaf(mx[nt][c], unit[nt][c], -ref[nt][c]) > room;
+                }
+            if (__any_sync(0xffffffffu, over)) {
                 float top = 0.f;
 #pragma unroll
                 for (int hb = 0; hb < 2; ++hb)
@@ -341,55 +382,41 @@ __global__ void __launch_bounds__(Cfg<DH, NT>::THREADS, 1) k_kv4_attn(const Kv4A
                     for (int j = 0; j < NG; ++j)
 #pragma unroll
                         for (int i = 0; i < 4; ++i) top = fmaxf(top, kv4_scale((vs[hb][j] >> (8 * i)) & 0xffu));
+                top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
+                top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
+                const float fits = fminf(room, (float)max(0, 15 - ((int)(__float_as_uint(top) >> 23) - 127))), drop = room - fits;
+                room = fits;
 #pragma unroll
-                for (int m = 1; m < 4; m <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, m));
-                const float fits = (float)max(0, 15 - ((int)(__float_as_uint(top) >> 23) - 127));
-                if (fits < boost) { drop = boost - fits; boost = fits; }
+                for (int nt = 0; nt < NT; ++nt) {
+                    float corr[2];
+#pragma unroll
+                    for (int c = 0; c < 2; ++c) {
+                        float m = mx[nt][c];
+                        m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 4));
+                        m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 8));
+                        m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 16)) * unit[nt][c];
+                        float nr = ref[nt][c] + drop;
+                        if (m - nr > room) nr = m - fminf(room, kStart);
+                        corr[c] = ex2f(ref[nt][c] - nr);
+                        l[nt][c] *= corr[c];
+                        ref[nt][c] = nr;
+                    }
+#pragma unroll
+                    for (int j = 0; j < NG; ++j)
+#pragma unroll
+                        for (int mt = 0; mt < 2; ++mt)
+#pragma unroll
+                            for (int i = 0; i < 4; ++i) o[j][mt][nt][i] *= corr[i & 1];
+                }
             }
-            // ---- weights
-            const bool mask = key0 + kTile > all_see;
-            float corr[NT][2];
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-                for (int c = 0; c < 2; ++c) {
-                    float mx = -INFINITY;
+                for (int i = 0; i < 4; ++i) {
 #pragma unroll
-                    for (int hb = 0; hb < 2; ++hb)
-#pragma unroll
-                        for (int i = 0; i < 2; ++i) {
-                            float& x = s[hb][nt][2 * i + c];
-                            x *= unit[nt][c];
-                            if (mask && key0 + 16 * hb + 2 * g + i >= lim[nt][c]) x = -INFINITY;
-                            mx = fmaxf(mx, x);
-                        }
-                    mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 4));
-                    mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 8));
-                    mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 16));
-                    const float nr = fmaxf(ref[nt][c] + drop, mx - boost);       // -inf as long as there is nothing to see
-                    corr[nt][c] = nr == -INFINITY ? 1.f : ex2f(ref[nt][c] - nr);
-                    ref[nt][c] = nr;
-                    const float r = nr == -INFINITY ? 0.f : nr;
-                    float sum = 0.f;
-#pragma unroll
-                    for (int hb = 0; hb < 2; ++hb)
-#pragma unroll
-                        for (int i = 0; i < 2; ++i) { float& x = s[hb][nt][2 * i + c]; x = ex2f(x - r); sum += x; }
-                    l[nt][c] = l[nt][c] * corr[nt][c] + sum;
+                    for (int hb = 0; hb < 2; ++hb) s[hb][nt][i] = ex2f(fmaf(s[hb][nt][i], unit[nt][i & 1], -ref[nt][i & 1]));
+                    l[nt][i & 1] += s[0][nt][i] + s[1][nt][i];
                 }
-            bool change = false;
-#pragma unroll
-            for (int nt = 0; nt < NT; ++nt) change = change || corr[nt][0] != 1.f || corr[nt][1] != 1.f;
-            if (__any_sync(0xffffffffu, change)) {
-#pragma unroll
-                for (int j = 0; j < NG; ++j)
-#pragma unroll
-                    for (int mt = 0; mt < 2; ++mt)
-#pragma unroll
-                        for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-                            for (int i = 0; i < 4; ++i) o[j][mt][nt][i] *= corr[nt][i & 1];
-            }
             // ---- weights times V
 #pragma unroll
             for (int hb = 0; hb < 2; ++hb) {
@@ -502,7 +529,7 @@ __global__ void __launch_bounds__(Cfg<DH, NT>::THREADS, 1) k_kv4_attn(const Kv4A
         const SegInfo si = head ? info[0][w1] : info[1][w0];
         for (int i = tid; i < si.rows * (DH / 4); i += C::THREADS) {
             const int r = i / (DH / 4), d = i % (DH / 4) * 4;
-            float top = -INFINITY, sum = 0.f;
+            float top = kNone, sum = 0.f;
             float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
             for (int w = w0; w <= w1; ++w) {
                 if (w == w1 ? !head : !(flags[w] & 2)) continue;
@@ -511,7 +538,7 @@ __global__ void __launch_bounds__(Cfg<DH, NT>::THREADS, 1) k_kv4_attn(const Kv4A
             for (int w = w0; w <= w1; ++w) {
                 if (w == w1 ? !head : !(flags[w] & 2)) continue;
                 const float* part = part_of(w, w == w1 ? 0 : 1);
-                const float m = part[RB * C::ROW + 2 * r], f = m == -INFINITY ? 0.f : ex2f(m - top);
+                const float f = ex2f(part[RB * C::ROW + 2 * r] - top);
                 const float4 x = *reinterpret_cast<const float4*>(part + r * C::ROW + d);
                 sum += part[RB * C::ROW + 2 * r + 1] * f;
                 acc.x += x.x * f; acc.y += x.y * f; acc.z += x.z * f; acc.w += x.w * f;
@@ -562,7 +589,7 @@ __global__ void __launch_bounds__(kMergeThreads) k_kv4_merge(const Kv4AttnP p, v
     const Leftover first = sc.left[blockIdx.x];
     const int r = blockIdx.y, d = threadIdx.x % DH, grp = threadIdx.x / DH;
     if (!first.tail || !first.tail_begins || r >= first.seg.rows) return;
-    float top = -INFINITY, sum = 0.f, acc = 0.f;
+    float top = kNone, sum = 0.f, acc = 0.f;
     for (int c = blockIdx.x, k = 0; c < blocks; ++c) {
         const int which = c == (int)blockIdx.x || !sc.left[c].head;      // the head of the last block, the tails of the others
         const bool last = which == 0;
@@ -570,7 +597,7 @@ __global__ void __launch_bounds__(kMergeThreads) k_kv4_merge(const Kv4AttnP p, v
         if (k++ % GROUPS == grp) {
             const float* part = sc.part(c, which);
             const float m = part[RB * DH + 2 * r], ls = part[RB * DH + 2 * r + 1], x = part[r * DH + d];
-            const float nt = fmaxf(top, m), f0 = top == -INFINITY ? 0.f : ex2f(top - nt), f1 = m == -INFINITY ? 0.f : ex2f(m - nt);
+            const float nt = fmaxf(top, m), f0 = ex2f(top - nt), f1 = ex2f(m - nt);
             acc = acc * f0 + x * f1;
             sum = sum * f0 + ls * f1;
             top = nt;
@@ -581,13 +608,13 @@ __global__ void __launch_bounds__(kMergeThreads) k_kv4_merge(const Kv4AttnP p, v
     if (d == 0) { sh[grp][DH] = top; sh[grp][DH + 1] = sum; }
     __syncthreads();
     if (grp) return;
-    float all = -INFINITY;
+    float all = kNone;
 #pragma unroll
     for (int i = 0; i < GROUPS; ++i) all = fmaxf(all, sh[i][DH]);
     acc = sum = 0.f;
 #pragma unroll
     for (int i = 0; i < GROUPS; ++i) {
-        const float f = sh[i][DH] == -INFINITY ? 0.f : ex2f(sh[i][DH] - all);
+        const float f = ex2f(sh[i][DH] - all);
         acc += sh[i][d] * f;
         sum += sh[i][DH + 1] * f;
     }
