@@ -1,5 +1,6 @@
 // Attention of one or a few new tokens per sequence straight from a 4-bit cache (pt_kv_dtype PT_KV_E2M1).
 #include <algorithm>
+#include <type_traits>
 
 #include "pt_kv4.cuh"
 #include "pt_tc.h"
@@ -84,35 +85,46 @@ __device__ __forceinline__ void bulk_copy(uint32_t dst, const void* src, uint32_
 
 // Where a warp is in the list of segments: (track, KV head), sequence, row block; and which of the segment's tiles are its own.
 struct Cursor {
-    int th, b, rb, S, K, seen, n, lo, hi;  // seen: keys that the block's last row sees; n: tiles of those
-    long long left;                        // units of cost of the warp's range behind this segment's
+    int th, b, rb, row0, S, K, seen, n, lo, hi;   // row0: the sequence's first row; seen: keys that the block's last row sees; n: tiles of those
+    long long left;                               // units of cost of the warp's range behind this segment's
 };
 
+// a / b for positive numbers: in 32 bits where they fit
+__device__ __forceinline__ long long quotient(long long a, long long b) {
+    return ((a | b) >> 32) == 0 ? (long long)((uint32_t)a / (uint32_t)b) : a / b;
+}
+
 template <int DH, int NT> struct Walk {
+    static constexpr int RB = Cfg<DH, NT>::RB;
     const Kv4AttnP& p;
     const int G;
     __device__ Walk(const Kv4AttnP& p_) : p(p_), G(p_.nq / p_.slab.nkv) {}
-    __device__ int blocks_of(int S) const { return (S * G + Cfg<DH, NT>::RB - 1) / Cfg<DH, NT>::RB; }
-    // keys that the last row of row block rb sees
-    __device__ int seen(int S, int K, int rb) const { return K - S + (min(S * G, (rb + 1) * Cfg<DH, NT>::RB) - 1) / G + 1; }
-    __device__ int tiles(int S, int K, int rb) const { return (seen(S, K, rb) + kTile - 1) / kTile; }
+    __device__ int seen(int S, int K, int rb) const { return (rb + 1) * RB >= S * G ? K : K - S + ((rb + 1) * RB - 1) / G + 1; }
     __device__ void load(int b, int& S, int& K) const { S = p.qlen ? p.qlen[b] : 1; K = p.kvlen[b]; }
+    __device__ static int cost(int seen) { return (seen + kTile - 1) / kTile + kSegCost; }
+    // of all row blocks of a sequence
+    __device__ long long cost(int S, int K) const {
+        long long n = 0;
+        for (int rb = 0; rb * RB < S * G; ++rb) n += cost(seen(S, K, rb));
+        return n;
+    }
     // the cursor at unit `in` of its segment; takes what the range has of it
     __device__ void enter(Cursor& c, long long in) const {
         c.seen = seen(c.S, c.K, c.rb);
         c.n = (c.seen + kTile - 1) / kTile;
         const long long end = min((long long)c.n + kSegCost, in + c.left);
-        c.lo = (int)max(0ll, in - kSegCost);
-        c.hi = (int)max(0ll, end - kSegCost);
+        c.lo = max(0, (int)in - kSegCost);
+        c.hi = max(0, (int)end - kSegCost);
         c.left -= end - in;
     }
     // to the next segment of the range with tiles in it; false: there is none
     __device__ bool next(Cursor& c) const {
         while (c.left > 0) {
-            if (++c.rb >= blocks_of(c.S)) {
+            if (++c.rb * RB >= c.S * G) {
                 c.rb = 0;
                 do {
-                    if (++c.b == p.B) { c.b = 0; ++c.th; }
+                    c.row0 += c.S;
+                    if (++c.b == p.B) { c.b = 0; ++c.th; c.row0 = 0; }
                     load(c.b, c.S, c.K);
                 } while (c.S == 0);
             }
@@ -121,16 +133,85 @@ template <int DH, int NT> struct Walk {
         }
         return false;
     }
+    // Every warp plans for itself: a lane sums the costs of 1 / 32 of the sequences, the lane in whose sum the warp's range
+    // begins is found by a ballot, and its sequences are looked through the same way.  false: nothing to do (or `bad` lengths)
+    __device__ bool plan(Cursor& c, bool& bad) const {
+        const int lane = threadIdx.x & 31, per = (p.B + 31) / 32;
+        long long mine = 0, rows = 0;
+        bad = false;
+        for (int b = lane * per; b < min(p.B, (lane + 1) * per); ++b) {
+            int S, K;
+            load(b, S, K);
+            if (S < 0 || K < S || S > p.M || K > (long long)p.maxp * p.slab.ps) { bad = true; break; }
+            rows += S;
+            mine += cost(S, K);
+        }
+        long long up = scan(mine), up_rows = p.qlen ? scan(rows) : 0;
+        bad = __any_sync(0xffffffffu, bad) || __shfl_sync(0xffffffffu, up_rows, 31) > p.M;
+        const long long per_head = __shfl_sync(0xffffffffu, up, 31), units = per_head * p.slab.nkv * p.T;
+        if (bad || units == 0) return false;
+        // the call's units go in equal shares to the warps of as many blocks as have one for each warp
+        constexpr int W = Cfg<DH, NT>::WARPS;
+        const int all = (int)min((long long)gridDim.x, (units + W - 1) / W) * W, gw = blockIdx.x * W + (threadIdx.x >> 5);
+        if (gw >= all) return false;
+        const long long share = quotient(units, all), more = units - share * all;
+        const long long u0 = share * gw + min((long long)gw, more);
+        c.left = share + (gw < more);
+        if (c.left == 0) return false;
+        c.th = (int)quotient(u0, per_head);
+        long long in = u0 - c.th * per_head;
+        int l = __popc(__ballot_sync(0xffffffffu, up <= in));
+        in -= __shfl_sync(0xffffffffu, up - mine, l);
+        c.row0 = p.qlen ? (int)__shfl_sync(0xffffffffu, up_rows - rows, l) : 0;
+        for (int b0 = l * per;; b0 += 32) {
+            const int b = b0 + lane;
+            int S = 0, K = 0;
+            if (b < min(p.B, (l + 1) * per)) load(b, S, K);
+            mine = cost(S, K);
+            up = scan(mine);
+            const int at = __popc(__ballot_sync(0xffffffffu, up <= in));
+            if (p.qlen) {
+                int sum = lane < at ? S : 0;
+#pragma unroll
+                for (int o = 16; o; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+                c.row0 += sum;
+            }
+            if (at < 32) {
+                in -= __shfl_sync(0xffffffffu, up - mine, at);
+                c.b = b0 + at;
+                c.S = __shfl_sync(0xffffffffu, S, at);
+                c.K = __shfl_sync(0xffffffffu, K, at);
+                break;
+            }
+            in -= __shfl_sync(0xffffffffu, up, 31);
+        }
+        if (!p.qlen) c.row0 = c.b;
+        for (c.rb = 0;; ++c.rb) {
+            const int n = cost(seen(c.S, c.K, c.rb));
+            if (in < n) break;
+            in -= n;
+        }
+        enter(c, in);
+        return c.lo < c.hi || next(c);
+    }
+    __device__ static long long scan(long long x) {
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const long long y = __shfl_up_sync(0xffffffffu, x, o);
+            if ((int)(threadIdx.x & 31) >= o) x += y;
+        }
+        return x;
+    }
 };
 
 template <int DH, int NT>
-__global__ void __launch_bounds__(Cfg<DH, NT>::THREADS, 1) k_kv4_attn(const Kv4AttnP p, void* scratch, const int per) {
+__global__ void __launch_bounds__(Cfg<DH, NT>::THREADS, 1) k_kv4_attn(const Kv4AttnP p, void* scratch) {
     using C = Cfg<DH, NT>;
     constexpr int NG = C::NG, RB = C::RB;
     extern __shared__ __align__(128) uint8_t smem[];
-    __shared__ long long pre[C::THREADS + 1];
-    __shared__ SegInfo info[2][C::WARPS];
+    __shared__ SegInfo info[C::WARPS][2];
     __shared__ int flags[C::WARPS];                       // bit 0: a head part, 1: a tail part, 2: the tail's segment begins here
+    __shared__ float factor[RB][32];
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, q4 = lane & 3;
     uint64_t* bars = (uint64_t*)(smem + C::BARS) + warp * C::STAGES;
     if (lane == 0) {
@@ -142,57 +223,12 @@ __global__ void __launch_bounds__(Cfg<DH, NT>::THREADS, 1) k_kv4_attn(const Kv4A
     grid_dep_launch();
     const Walk<DH, NT> walk(p);
     const int G = walk.G, nkv = p.slab.nkv, ps = p.slab.ps;
-    // ---- the plan: cost of every sequence, summed; this warp's range of the whole
-    bool bad = false;
-    long long rows = 0;
-    kv4_scan(p.B, per, pre, [&](int b) {
-        int S, K;
-        walk.load(b, S, K);
-        if (S < 0 || K < S || K > (long long)p.maxp * ps || S > p.M) { bad = true; return 0ll; }
-        rows += S;
-        long long n = 0;
-        for (int rb = 0, nb = walk.blocks_of(S); rb < nb; ++rb) n += walk.tiles(S, K, rb) + kSegCost;
-        return n;
-    });
-    if (p.qlen) {                                         // all rows: no more than M
-        __shared__ unsigned long long all;
-        if (tid == 0) all = 0;
-        __syncthreads();
-        if (rows) atomicAdd(&all, (unsigned long long)rows);
-        __syncthreads();
-        bad = bad || all > (unsigned long long)p.M;
-    }
-    Scratch<DH, NT> sc(scratch);
-    if (__syncthreads_or(bad)) {
+    const Scratch<DH, NT> sc(scratch);
+    Cursor cur{};
+    bool bad = false, any = walk.plan(cur, bad);
+    if (bad) {                                            // every warp of the call finds the same
         if (tid == 0) { report(p.status, PT_ERR_DEVICE_BOUNDS, LOC_KV4_LEN); sc.left[blockIdx.x] = Leftover{}; }
         return;
-    }
-    const long long per_head = pre[C::THREADS], units = per_head * nkv * p.T;
-    const long long used = min((long long)gridDim.x, (units + C::WARPS - 1) / C::WARPS);      // blocks with work
-    Cursor cur{};
-    bool any = false;
-    if (blockIdx.x < used) {
-        const long long gw = (long long)blockIdx.x * C::WARPS + warp, all = used * C::WARPS;
-        const long long u0 = units / all * gw + units % all * gw / all, u1 = units / all * (gw + 1) + units % all * (gw + 1) / all;
-        if (u0 < u1) {
-            cur.th = (int)(u0 / per_head);
-            long long in = u0 - cur.th * per_head;
-            const int i = kv4_find(pre, C::THREADS, in);
-            in -= pre[i];
-            cur.left = u1 - u0;
-            for (cur.b = i * per;; ++cur.b) {
-                walk.load(cur.b, cur.S, cur.K);
-                bool here = false;
-                for (cur.rb = 0; cur.rb < walk.blocks_of(cur.S); ++cur.rb) {
-                    const int n = walk.tiles(cur.S, cur.K, cur.rb) + kSegCost;
-                    if (in < n) { here = true; break; }
-                    in -= n;
-                }
-                if (here) break;
-            }
-            walk.enter(cur, in);
-            any = cur.lo < cur.hi || walk.next(cur);
-        }
     }
     // ---- the ring: lanes 0 and 1 fetch a block of 16 keys each; pages are looked up one tile ahead
     uint8_t* ring = smem + warp * C::RING;
@@ -215,7 +251,19 @@ __global__ void __launch_bounds__(Cfg<DH, NT>::THREADS, 1) k_kv4_attn(const Kv4A
         a_in = blk - col * bpp;
         if (lane < 2 && blk * 16 < ahead.seen) a_page = a_bt[col];
     };
-    if (a_any) { aim(); look(); }
+    // a segment's queries: lane (g, q4) has row g's octets q4 of every group
+    uint4 raw[NT][NG];
+    auto fetch = [&]() {
+        const int t = cur.th / nkv, h = cur.th - t * nkv;
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+            const int r = cur.rb * RB + nt * 8 + g, tok = r / G;
+            const __nv_bfloat16* src = p.q + (((size_t)t * p.M + cur.row0 + tok) * p.nq + h * G + (r - tok * G)) * DH + 8 * q4;
+#pragma unroll
+            for (int j = 0; j < NG; ++j) raw[nt][j] = r < cur.S * G ? *reinterpret_cast<const uint4*>(src + 32 * j) : make_uint4(0, 0, 0, 0);
+        }
+    };
+    if (a_any) { aim(); look(); fetch(); }
     auto issue = [&](int slot) {
         bool go = lane < 2 && a_tile * kTile + 16 * lane < ahead.seen;
         if (go && (uint32_t)a_page >= (uint32_t)p.slab.num_pages) { bad_page = true; go = false; }
@@ -232,32 +280,21 @@ __global__ void __launch_bounds__(Cfg<DH, NT>::THREADS, 1) k_kv4_attn(const Kv4A
     __syncwarp();
     for (int s = 0; s < C::STAGES; ++s) if (a_any) issue(s);
 
-    int slot = 0, done = 0, my_flags = 0;
+    int slot = 0, my_flags = 0;
     uint32_t parity = 0;
     bool timed_out = false;
     while (any && !timed_out) {
         // ---- a segment: its queries
-        const int t = cur.th / nkv, h = cur.th - t * nkv, R = cur.S * G, r0 = cur.rb * RB;
-        int row0 = 0;                                     // first row of the sequence
-        if (p.qlen) {
-            for (int b = lane; b < cur.b; b += 32) row0 += p.qlen[b];
-#pragma unroll
-            for (int o = 16; o; o >>= 1) row0 += __shfl_xor_sync(0xffffffffu, row0, o);
-        } else {
-            row0 = cur.b;
-        }
+        const int t = cur.th / nkv, h = cur.th - t * nkv, row0 = cur.row0, R = cur.S * G, r0 = cur.rb * RB;
         uint32_t qf[NG][NT][4];
         float unit[NT][2];
         int lim[NT][2];
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
-            const int r = r0 + nt * 8 + g, tok = r / G;
-            uint4 raw[NG];
             uint32_t top = 0;
 #pragma unroll
             for (int j = 0; j < NG; ++j) {
-                raw[j] = r < R ? *reinterpret_cast<const uint4*>(p.q + (((size_t)t * p.M + row0 + tok) * p.nq + h * G + (r - tok * G)) * DH + 32 * j + 8 * q4) : make_uint4(0, 0, 0, 0);
-                const uint32_t w[4] = {raw[j].x, raw[j].y, raw[j].z, raw[j].w};
+                const uint32_t w[4] = {raw[nt][j].x, raw[nt][j].y, raw[nt][j].z, raw[nt][j].w};
 #pragma unroll
                 for (int i = 0; i < 4; ++i) top = __vmaxu2(top, w[i] & 0x7fff7fffu);
             }
@@ -272,7 +309,7 @@ __global__ void __launch_bounds__(Cfg<DH, NT>::THREADS, 1) k_kv4_attn(const Kv4A
             const float un = __uint_as_float((uint32_t)(e - 13 + 127) << 23) * p.scale_log2;
 #pragma unroll
             for (int j = 0; j < NG; ++j) {
-                const uint32_t w[4] = {raw[j].x, raw[j].y, raw[j].z, raw[j].w};
+                const uint32_t w[4] = {raw[nt][j].x, raw[nt][j].y, raw[nt][j].z, raw[nt][j].w};
 #pragma unroll
                 for (int i = 0; i < 4; ++i) qf[j][nt][i] = half2_of(__uint_as_float(w[i] << 16) * inv, __uint_as_float(w[i] & 0xffff0000u) * inv);
             }
@@ -463,7 +500,6 @@ __global__ void __launch_bounds__(Cfg<DH, NT>::THREADS, 1) k_kv4_attn(const Kv4A
             }
             __syncwarp();                                         // every lane is done with the slot
             if (a_any) { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); issue(slot); }
-            ++done;
             if (++slot == C::STAGES) { slot = 0; parity ^= 1; }
         }
         if (timed_out) break;
@@ -504,9 +540,10 @@ __global__ void __launch_bounds__(Cfg<DH, NT>::THREADS, 1) k_kv4_attn(const Kv4A
                     if (g == 0) { part[RB * C::ROW + 2 * r] = ref[nt][c]; part[RB * C::ROW + 2 * r + 1] = l[nt][c]; }
                 }
             my_flags |= ends ? 1 : begins ? 6 : 2;
-            if (lane == 0) info[ends ? 0 : 1][warp] = si;
+            if (lane == 0) info[warp][ends ? 0 : 1] = si;
         }
         any = walk.next(cur);
+        if (any) fetch();
     }
     if (timed_out) {
         // give the copies that are still in flight a bounded chance to land, then give up
@@ -523,57 +560,92 @@ __global__ void __launch_bounds__(Cfg<DH, NT>::THREADS, 1) k_kv4_attn(const Kv4A
     if (lane == 0) flags[warp] = my_flags;
     __syncthreads();
 
-    // ---- parts of one segment side by side in this block's warps: to the result, or to one part for the merge
-    auto part_of = [&](int w, int which) { return which == 0 ? (const float*)(smem + C::HEADS) + w * C::PART : (const float*)(smem + w * C::RING); };
-    auto combine = [&](int w0, int w1, bool head, bool result, int which) {     // tails of warps w0 .. w1 - 1 and the head of warp w1, if `head`
-        const SegInfo si = head ? info[0][w1] : info[1][w0];
-        for (int i = tid; i < si.rows * (DH / 4); i += C::THREADS) {
-            const int r = i / (DH / 4), d = i % (DH / 4) * 4;
-            float top = kNone, sum = 0.f;
-            float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-            for (int w = w0; w <= w1; ++w) {
-                if (w == w1 ? !head : !(flags[w] & 2)) continue;
-                top = fmaxf(top, part_of(w, w == w1 ? 0 : 1)[RB * C::ROW + 2 * r]);
+    // ---- parts of one segment side by side in this block's warps: to the result, or to one part for the merge.
+    // Lane 2 w + 0 / 1 stands for warp w's head / tail; parts of one segment (a chain) follow one another
+    static_assert(2 * C::WARPS <= 32, "a lane for each part");
+    const int fl = lane < 2 * C::WARPS ? flags[lane >> 1] : 0;
+    const bool exists = lane & 1 ? (fl & 2) != 0 : (fl & 1) != 0;
+    const uint32_t members = __ballot_sync(0xffffffffu, exists), closers = members & 0x55555555u;
+    const uint32_t begins = __ballot_sync(0xffffffffu, exists && (lane & 1) && (fl & 4));
+    if (members) {
+        const uint32_t starts = begins | (members & (0u - members));
+        // last lane of the chain that begins in lane f
+        auto last_of = [&](int f) {
+            const uint32_t c = closers >> f;
+            return c ? f + __ffs(c) - 1 : 31 - __clz(members);
+        };
+        auto part_of = [&](int l) { return l & 1 ? (const float*)(smem + (l >> 1) * C::RING) : (const float*)(smem + C::HEADS) + (l >> 1) * C::PART; };
+        const uint32_t before = starts & ((2u << lane) - 1u);
+        const int mine_first = before ? 31 - __clz(before) : lane, mine_last = exists ? last_of(mine_first) : lane;
+        const bool whole = ((begins >> mine_first) & 1) && !(mine_last & 1);      // the chain has all of the segment's keys
+        for (int r = warp; r < RB; r += C::WARPS) {
+            float m = kNone, sum = 0.f;
+            if (exists) { const float2 st = *reinterpret_cast<const float2*>(part_of(lane) + RB * C::ROW + 2 * r); m = st.x; sum = st.y; }
+            float top = m;
+#pragma unroll
+            for (int o = 1; o < 32; o <<= 1) {
+                const float x = __shfl_up_sync(0xffffffffu, top, o);
+                if (lane - o >= mine_first) top = fmaxf(top, x);
             }
-            for (int w = w0; w <= w1; ++w) {
-                if (w == w1 ? !head : !(flags[w] & 2)) continue;
-                const float* part = part_of(w, w == w1 ? 0 : 1);
-                const float f = ex2f(part[RB * C::ROW + 2 * r] - top);
-                const float4 x = *reinterpret_cast<const float4*>(part + r * C::ROW + d);
-                sum += part[RB * C::ROW + 2 * r + 1] * f;
-                acc.x += x.x * f; acc.y += x.y * f; acc.z += x.z * f; acc.w += x.w * f;
+            top = __shfl_sync(0xffffffffu, top, mine_last);
+            const float f = ex2f(m - top);
+            sum *= f;
+#pragma unroll
+            for (int o = 1; o < 32; o <<= 1) {
+                const float x = __shfl_up_sync(0xffffffffu, sum, o);
+                if (lane - o >= mine_first) sum += x;
             }
-            if (result) {
+            sum = __shfl_sync(0xffffffffu, sum, mine_last);
+            factor[r][lane] = whole ? f / sum : f;
+            if (exists && !whole && lane == mine_last) {
+                float* to = sc.part(blockIdx.x, lane & 1) + RB * DH + 2 * r;
+                to[0] = top; to[1] = sum;
+            }
+        }
+        __syncthreads();
+        // a warp per chain and row
+        uint32_t rest = starts;
+        for (int task = warp, chain = 0; rest; task += C::WARPS) {
+            while (rest && task >= (chain + 1) * RB) { rest &= rest - 1; ++chain; }
+            if (!rest) break;
+            const int r = task - chain * RB, first = __ffs(rest) - 1, last = last_of(first);
+            const SegInfo si = info[first >> 1][first & 1];
+            if (r >= si.rows) continue;
+            constexpr int V = DH / 32;                            // columns of a lane
+            using Vec = std::conditional_t<V == 4, float4, float2>;
+            alignas(16) float acc[V] = {};
+#pragma unroll 4
+            for (int l = first; l <= last; ++l) {
+                if (!((members >> l) & 1)) continue;
+                const float f = factor[r][l];
+                const Vec x = *reinterpret_cast<const Vec*>(part_of(l) + r * C::ROW + lane * V);
+#pragma unroll
+                for (int i = 0; i < V; ++i) acc[i] += f * reinterpret_cast<const float*>(&x)[i];
+            }
+            if (((begins >> first) & 1) && !(last & 1)) {
                 const int tok = (si.r0 + r) / G, hd = si.r0 + r - tok * G;
-                const float inv = 1.0f / sum;
-                *reinterpret_cast<uint2*>(p.o + (((size_t)si.t * p.M + si.row0 + tok) * p.nq + si.h * G + hd) * DH + d) =
-                    make_uint2(kv4_bf16(acc.x * inv, acc.y * inv), kv4_bf16(acc.z * inv, acc.w * inv));
+                __nv_bfloat16* dst = p.o + (((size_t)si.t * p.M + si.row0 + tok) * p.nq + si.h * G + hd) * DH + lane * V;
+#pragma unroll
+                for (int i = 0; i < V; i += 2) *reinterpret_cast<uint32_t*>(dst + i) = kv4_bf16(acc[i], acc[i + 1]);
             } else {
-                float* to = sc.part(blockIdx.x, which);
-                *reinterpret_cast<float4*>(to + r * DH + d) = acc;
-                if (d == 0) { to[RB * DH + 2 * r] = top; to[RB * DH + 2 * r + 1] = sum; }
+                *reinterpret_cast<Vec*>(sc.part(blockIdx.x, last & 1) + r * DH + lane * V) = *reinterpret_cast<const Vec*>(acc);
             }
         }
-    };
-    Leftover left{};
-    int first = 0;
-    bool begun = false, open = false;                             // the chain of parts: does it begin in this block; has it any
-    for (int w = 0; w < C::WARPS; ++w) {
-        const int f = flags[w];
-        if (f & 1) {
-            combine(open ? first : w, w, true, begun, 0);
-            if (!begun) left.head = 1;
-            open = begun = false;
-        }
-        if (f & 2) {
-            if (!open) { first = w; begun = (f & 4) != 0; open = true; }
-        }
     }
-    if (open) {
-        combine(first, C::WARPS, false, false, 1);
-        left.tail = 1; left.tail_begins = begun; left.seg = info[1][first];
+    if (tid == 0) {
+        Leftover left{};
+        if (members) {
+            const int top = 31 - __clz(members), low = __ffs(members) - 1;
+            const uint32_t starts = begins | (1u << low);
+            // the first chain is cut at its front unless it begins here; the last is cut at its end unless a head closes it
+            if (!((begins >> low) & 1) && closers) left.head = __ffs(closers) - 1 < (begins ? __ffs(begins) - 1 : 32);
+            if (top & 1) {
+                const int first = 31 - __clz(starts);
+                left.tail = 1; left.tail_begins = (begins >> first) & 1; left.seg = info[first >> 1][first & 1];
+            }
+        }
+        sc.left[blockIdx.x] = left;
     }
-    if (tid == 0) sc.left[blockIdx.x] = left;
 }
 
 // Merges the parts of the segments that thread blocks cut: block (c, r) has row r of the segment that begins in block c and
@@ -586,23 +658,24 @@ __global__ void __launch_bounds__(kMergeThreads) k_kv4_merge(const Kv4AttnP p, v
     grid_dep_wait();
     grid_dep_launch();
     const Scratch<DH, NT> sc(scratch);
-    const Leftover first = sc.left[blockIdx.x];
-    const int r = blockIdx.y, d = threadIdx.x % DH, grp = threadIdx.x / DH;
+    const int r = blockIdx.y, d = threadIdx.x % DH, grp = threadIdx.x / DH, lane = threadIdx.x & 31, c0 = blockIdx.x;
+    const Leftover first = sc.left[c0];
     if (!first.tail || !first.tail_begins || r >= first.seg.rows) return;
+    // the block that ends the segment: the first behind c0 with a head
+    int last = blocks - 1;
+    for (int base = c0 + 1; base < blocks; base += 32) {
+        const uint32_t heads = __ballot_sync(0xffffffffu, base + lane < blocks && sc.left[base + lane].head);
+        if (heads) { last = base + __ffs(heads) - 1; break; }
+    }
     float top = kNone, sum = 0.f, acc = 0.f;
-    for (int c = blockIdx.x, k = 0; c < blocks; ++c) {
-        const int which = c == (int)blockIdx.x || !sc.left[c].head;      // the head of the last block, the tails of the others
-        const bool last = which == 0;
-        if (which == 1 && !sc.left[c].tail) continue;                     // a block without work
-        if (k++ % GROUPS == grp) {
-            const float* part = sc.part(c, which);
-            const float m = part[RB * DH + 2 * r], ls = part[RB * DH + 2 * r + 1], x = part[r * DH + d];
-            const float nt = fmaxf(top, m), f0 = ex2f(top - nt), f1 = ex2f(m - nt);
-            acc = acc * f0 + x * f1;
-            sum = sum * f0 + ls * f1;
-            top = nt;
-        }
-        if (last) break;
+#pragma unroll 4
+    for (int c = c0 + grp; c <= last; c += GROUPS) {               // tails, and the last one's head
+        const float* part = sc.part(c, c == last ? 0 : 1);
+        const float m = part[RB * DH + 2 * r], ls = part[RB * DH + 2 * r + 1], x = part[r * DH + d];
+        const float nt = fmaxf(top, m), f0 = ex2f(top - nt), f1 = ex2f(m - nt);
+        acc = acc * f0 + x * f1;
+        sum = sum * f0 + ls * f1;
+        top = nt;
     }
     sh[grp][d] = acc;
     if (d == 0) { sh[grp][DH] = top; sh[grp][DH + 1] = sum; }
@@ -634,7 +707,7 @@ template <int DH, int NT> pt_status launch_t(const Kv4AttnP& p, void* scratch, c
         sms = n;
     }
     const int blocks = std::min(sms, kMaxBlocks);
-    cudaError_t e = launch_dependent(k_kv4_attn<DH, NT>, dim3(blocks), dim3(C::THREADS), (size_t)C::SMEM, st, p, scratch, (p.B + C::THREADS - 1) / C::THREADS);
+    cudaError_t e = launch_dependent(k_kv4_attn<DH, NT>, dim3(blocks), dim3(C::THREADS), (size_t)C::SMEM, st, p, scratch);
     g_launches.fetch_add(1, std::memory_order_relaxed);
     if (e == cudaSuccess && blocks > 1) {
         e = launch_dependent(k_kv4_merge<DH, NT>, dim3(blocks - 1, C::RB), dim3(kMergeThreads), (size_t)0, st, p, scratch, blocks);
