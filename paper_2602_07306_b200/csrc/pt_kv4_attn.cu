@@ -24,9 +24,10 @@ constexpr float kNone = -3.0e38f;         // reference of a row that has seen no
 template <int DH, int NT> struct Cfg {
     static constexpr int NG = DH / 32, RB = 8 * NT, BLK = kv4_block(DH);
     static constexpr int WARPS = NT == 1 ? KW : 12, STAGES = (NT == 1 ? KS : 2) * (128 / DH), THREADS = WARPS * 32;
+    static constexpr int SCALE_BYTES = kTile * NG * 6;      // a tile's scales, decoded: K as fp32, V as fp16 pairs
     static constexpr int STAGE = 2 * BLK, RING = STAGES * STAGE;           // bytes of a warp's ring
     static constexpr int ROW = DH + 4, PART = RB * ROW + 2 * RB;           // floats of a part: rows, then (reference, sum) of each
-    static constexpr int HEADS = WARPS * RING, BARS = HEADS + WARPS * PART * 4, SMEM = BARS + WARPS * STAGES * 8 + 16;
+    static constexpr int HEADS = WARPS * RING, SCALES = HEADS + WARPS * PART * 4, BARS = SCALES + WARPS * SCALE_BYTES, SMEM = BARS + WARPS * STAGES * 8 + 16;
     static_assert(PART * 4 <= RING && SMEM <= 227 * 1024 - 4096, "shared memory");
 };
 
@@ -215,7 +216,7 @@ __global__ void __launch_bounds__(Cfg<DH, NT>::THREADS, 1) k_kv4_attn(const Kv4A
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, q4 = lane & 3;
     uint64_t* bars = (uint64_t*)(smem + C::BARS) + warp * C::STAGES;
     if (lane == 0) {
-        for (int i = 0; i < C::STAGES; ++i) mbar_init(&bars[i], 1);
+        for (int i = 0; i < C::STAGES; ++i) mbar_init(&bars[i], 2);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
     }
@@ -233,23 +234,36 @@ __global__ void __launch_bounds__(Cfg<DH, NT>::THREADS, 1) k_kv4_attn(const Kv4A
     // ---- the ring: lanes 0 and 1 fetch a block of 16 keys each; pages are looked up one tile ahead
     uint8_t* ring = smem + warp * C::RING;
     Cursor ahead = cur;
-    const int bpp = ps / 16;                              // blocks of a page: 1 .. 4
-    const int64_t page_bytes = (int64_t)nkv * bpp * C::BLK;
-    int a_tile = cur.lo, a_in = 0, a_page = -1;
+    const int bpp = ps / 16, step_col = 2 / bpp, step_in = 2 % bpp;            // blocks of a page: 1 .. 4
+    const uint32_t page_bytes = (uint32_t)nkv * bpp * C::BLK;
+    int a_tile = 0, a_col = 0, a_in = 0, a_page = -1;
     bool a_any = any, bad_page = false;
     const char* a_base = nullptr;                         // the head's first block in page 0
     const int32_t* a_bt = nullptr;
+    auto look = [&]() { if (lane < 2 && a_tile * kTile + 16 * lane < ahead.seen) a_page = a_bt[a_col]; };
     auto aim = [&]() {
-        const int t = ahead.th / nkv, h = ahead.th - t * nkv;
+        const int t = ahead.th / nkv, h = ahead.th - t * nkv, blk = 2 * ahead.lo + lane;
         a_base = p.slab.pool_l + (size_t)t * p.slab.tstride + (size_t)h * bpp * C::BLK;
         a_bt = p.bt + (size_t)ahead.b * p.maxp;
         a_tile = ahead.lo;
+        a_col = blk / bpp; a_in = blk - a_col * bpp;
+        look();
     };
-    auto look = [&]() {
-        const int blk = 2 * a_tile + lane;
-        const int col = bpp == 3 ? (int)__umulhi((uint32_t)blk, 0x55555556u) : blk >> (bpp >> 1);
-        a_in = blk - col * bpp;
-        if (lane < 2 && blk * 16 < ahead.seen) a_page = a_bt[col];
+    auto issue = [&](int slot) {
+        if (lane < 2) {                                   // each expects its own bytes: none behind the last key
+            const bool some = a_tile * kTile + 16 * lane < ahead.seen, go = some && (uint32_t)a_page < (uint32_t)p.slab.num_pages;
+            bad_page |= some != go;
+            mbar_expect_tx(&bars[slot], go ? C::BLK : 0);
+            if (go) bulk_copy(smem_u32(ring + slot * C::STAGE + lane * C::BLK), a_base + (uint64_t)(uint32_t)a_page * page_bytes + a_in * C::BLK, C::BLK, &bars[slot]);
+        }
+        if (++a_tile == ahead.hi) {
+            a_any = walk.next(ahead);
+            if (a_any) aim();
+        } else {
+            a_col += step_col; a_in += step_in;
+            if (a_in >= bpp) { a_in -= bpp; ++a_col; }
+            look();
+        }
     };
     // a segment's queries: lane (g, q4) has row g's octets q4 of every group
     uint4 raw[NT][NG];
@@ -263,20 +277,7 @@ __global__ void __launch_bounds__(Cfg<DH, NT>::THREADS, 1) k_kv4_attn(const Kv4A
             for (int j = 0; j < NG; ++j) raw[nt][j] = r < cur.S * G ? *reinterpret_cast<const uint4*>(src + 32 * j) : make_uint4(0, 0, 0, 0);
         }
     };
-    if (a_any) { aim(); look(); fetch(); }
-    auto issue = [&](int slot) {
-        bool go = lane < 2 && a_tile * kTile + 16 * lane < ahead.seen;
-        if (go && (uint32_t)a_page >= (uint32_t)p.slab.num_pages) { bad_page = true; go = false; }
-        const unsigned who = __ballot_sync(0xffffffffu, go);
-        if (lane == 0) mbar_expect_tx(&bars[slot], __popc(who) * C::BLK);
-        __syncwarp();
-        if (go) bulk_copy(smem_u32(ring + slot * C::STAGE + lane * C::BLK), a_base + a_page * page_bytes + a_in * C::BLK, C::BLK, &bars[slot]);
-        if (++a_tile == ahead.hi) {
-            a_any = walk.next(ahead);
-            if (a_any) aim();
-        }
-        if (a_any) look();
-    };
+    if (a_any) { aim(); fetch(); }
     __syncwarp();
     for (int s = 0; s < C::STAGES; ++s) if (a_any) issue(s);
 
@@ -327,41 +328,60 @@ __global__ void __launch_bounds__(Cfg<DH, NT>::THREADS, 1) k_kv4_attn(const Kv4A
             for (int c = 0; c < 2; ++c) { ref[nt][c] = kNone; l[nt][c] = 0.f; }
         float room = kTop;                                        // weights stay below 2^room
         for (int tile = cur.lo; tile < cur.hi; ++tile) {
-            bool ok = false;
-            {
+            bool ok = mbar_try(&bars[slot], parity);
+            if (!__all_sync(0xffffffffu, ok)) {
                 WaitClock clock;
-                for (uint32_t spin = 0; spin < kSpin; ++spin) {
-                    if (mbar_try(&bars[slot], parity)) { ok = true; break; }
+                for (uint32_t spin = 0; spin < kSpin && !ok; ++spin) {
+                    ok = mbar_try(&bars[slot], parity);
                     if ((spin & 255) == 255 && clock.expired()) break;
                 }
+                if (!__all_sync(0xffffffffu, ok)) { timed_out = true; break; }
             }
-            if (!__all_sync(0xffffffffu, ok)) { timed_out = true; break; }
-            const uint32_t base = smem_u32(ring + slot * C::STAGE);
+            const uint32_t base = smem_u32(ring + slot * C::STAGE), dec = smem_u32(smem + C::SCALES + warp * C::SCALE_BYTES);
             const int key0 = tile * kTile;
+            // ---- the tile's scales, each decoded once: lane l has key l's of K and word l (block, q, group) of V's
+            uint32_t high;
+            {
+                const int hb = lane >> 4, l = lane & 15;
+                uint32_t kb = 0, vb = 0, even, odd;
+                if constexpr (NG == 4) {
+                    lds<1>(base + hb * C::BLK + kv4_codes(DH) + l * 4, &kb);
+                    lds<1>(base + hb * C::BLK + 2 * kv4_codes(DH) + kv4_scales(DH) + l * 4, &vb);
+                    if (key0 + kTile > seen) {                    // nothing behind the last key counts
+                        const int nv = min(max(seen - (key0 + 16 * hb + (l & ~3)), 0), 4);
+                        vb &= nv == 4 ? 0xffffffffu : (1u << (8 * nv)) - 1u;
+                    }
+                    scales4(kb, even, odd);
+                    const float2 a = __half22float2(*reinterpret_cast<__half2*>(&even)), b = __half22float2(*reinterpret_cast<__half2*>(&odd));
+                    asm volatile("st.shared.v4.f32 [%0], {%1, %2, %3, %4};" ::"r"(dec + lane * 16), "f"(a.x), "f"(b.x), "f"(a.y), "f"(b.y) : "memory");
+                    scales4(vb, even, odd);
+                    asm volatile("st.shared.v2.u32 [%0], {%1, %2};" ::"r"(dec + kTile * 16 + lane * 8), "r"(even), "r"(odd) : "memory");
+                } else if (l < 8) {                               // two groups: a word of K's has two keys, eight words of V's are a block's
+                    lds<1>(base + hb * C::BLK + kv4_codes(DH) + l * 4, &kb);
+                    lds<1>(base + hb * C::BLK + 2 * kv4_codes(DH) + kv4_scales(DH) + l * 4, &vb);
+                    if (key0 + kTile > seen) {
+                        const int nv = min(max(seen - (key0 + 16 * hb + 4 * (l >> 1)), 0), 4);
+                        vb &= nv == 4 ? 0xffffffffu : (1u << (8 * nv)) - 1u;
+                    }
+                    scales4(kb, even, odd);
+                    const float2 a = __half22float2(*reinterpret_cast<__half2*>(&even)), b = __half22float2(*reinterpret_cast<__half2*>(&odd));
+                    asm volatile("st.shared.v4.f32 [%0], {%1, %2, %3, %4};" ::"r"(dec + (hb * 8 + l) * 16), "f"(a.x), "f"(b.x), "f"(a.y), "f"(b.y) : "memory");
+                    scales4(vb, even, odd);
+                    asm volatile("st.shared.v2.u32 [%0], {%1, %2};" ::"r"(dec + kTile * 8 + (hb * 8 + l) * 8), "r"(even), "r"(odd) : "memory");
+                }
+                high = vb;
+                __syncwarp();
+            }
             // ---- scores
             float s[2][NT][4];
 #pragma unroll
             for (int hb = 0; hb < 2; ++hb) {
                 const uint32_t kb = base + hb * C::BLK;
-                uint32_t kw[2][NG], ks[NG / 2];
+                uint32_t kw[2][NG], ks[2 * NG];
                 lds<NG>(kb + g * (DH / 2) + q4 * (DH / 8), kw[0]);
                 lds<NG>(kb + (g + 8) * (DH / 2) + q4 * (DH / 8), kw[1]);
-                lds<NG / 2>(kb + kv4_codes(DH) + g * 2 * NG, ks);
-                float scf[2][NG];
-                if constexpr (NG == 4) {
-#pragma unroll
-                    for (int i = 0; i < 2; ++i) {
-                        uint32_t even, odd;
-                        scales4(ks[i], even, odd);
-                        const float2 a = __half22float2(*reinterpret_cast<__half2*>(&even)), b = __half22float2(*reinterpret_cast<__half2*>(&odd));
-                        scf[i][0] = a.x; scf[i][2] = a.y; scf[i][1] = b.x; scf[i][3] = b.y;
-                    }
-                } else {
-                    uint32_t even, odd;
-                    scales4(ks[0], even, odd);
-                    const float2 a = __half22float2(*reinterpret_cast<__half2*>(&even)), b = __half22float2(*reinterpret_cast<__half2*>(&odd));
-                    scf[0][0] = a.x; scf[1][0] = a.y; scf[0][1] = b.x; scf[1][1] = b.y;
-                }
+                lds<NG>(dec + (16 * hb + 2 * g) * NG * 4, ks);
+                lds<NG>(dec + (16 * hb + 2 * g + 1) * NG * 4, ks + NG);
 #pragma unroll
                 for (int j = 0; j < NG; ++j) {
                     uint32_t h0[4], h1[4];
@@ -373,23 +393,12 @@ __global__ void __launch_bounds__(Cfg<DH, NT>::THREADS, 1) k_kv4_attn(const Kv4A
                         mma0(c, h0[0], h1[0], h0[1], h1[1], qf[j][nt][0], qf[j][nt][1]);
                         mma(c, h0[2], h1[2], h0[3], h1[3], qf[j][nt][2], qf[j][nt][3]);
 #pragma unroll
-                        for (int i = 0; i < 4; ++i) s[hb][nt][i] = j ? fmaf(c[i], scf[i >> 1][j], s[hb][nt][i]) : c[i] * scf[i >> 1][j];
+                        for (int i = 0; i < 4; ++i) {
+                            const float f = __uint_as_float(ks[(i >> 1) * NG + j]);
+                            s[hb][nt][i] = j ? fmaf(c[i], f, s[hb][nt][i]) : c[i] * f;
+                        }
                     }
                 }
-            }
-            // ---- V's scales: bytes of keys 4 q4 .. + 3; nothing behind the last key counts
-            uint32_t vs[2][NG], high = 0;
-#pragma unroll
-            for (int hb = 0; hb < 2; ++hb) {
-                lds<NG>(base + hb * C::BLK + 2 * kv4_codes(DH) + kv4_scales(DH) + q4 * (DH / 8), vs[hb]);
-                if (key0 + kTile > seen) {
-                    const int nv = min(max(seen - (key0 + 16 * hb + 4 * q4), 0), 4);
-                    const uint32_t keep = nv == 4 ? 0xffffffffu : (1u << (8 * nv)) - 1u;
-#pragma unroll
-                    for (int j = 0; j < NG; ++j) vs[hb][j] &= keep;
-                }
-#pragma unroll
-                for (int j = 0; j < NG; ++j) high |= vs[hb][j];
             }
             // ---- weights 2^(score - reference).  The reference lags behind the maximum: it is raised, and what has been summed
             // scaled down, only where a weight would pass 2^kTop, or where a scale of V of 2 or more has to be made room for
@@ -414,13 +423,9 @@ __global__ void __launch_bounds__(Cfg<DH, NT>::THREADS, 1) k_kv4_attn(const Kv4A
             if (__any_sync(0xffffffffu, over)) {
                 float top = 0.f;
 #pragma unroll
-                for (int hb = 0; hb < 2; ++hb)
+                for (int i = 0; i < 4; ++i) top = fmaxf(top, kv4_scale((high >> (8 * i)) & 0xffu));
 #pragma unroll
-                    for (int j = 0; j < NG; ++j)
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) top = fmaxf(top, kv4_scale((vs[hb][j] >> (8 * i)) & 0xffu));
-                top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
-                top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
+                for (int m = 1; m < 32; m <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, m));
                 const float fits = fminf(room, (float)max(0, 15 - ((int)(__float_as_uint(top) >> 23) - 127))), drop = room - fits;
                 room = fits;
 #pragma unroll
@@ -458,7 +463,9 @@ __global__ void __launch_bounds__(Cfg<DH, NT>::THREADS, 1) k_kv4_attn(const Kv4A
 #pragma unroll
             for (int hb = 0; hb < 2; ++hb) {
                 const uint32_t vb = base + hb * C::BLK + kv4_codes(DH) + kv4_scales(DH);
-                uint32_t b0[NT], b1[NT];
+                uint32_t b0[NT], b1[NT], vs[2 * NG];              // scales of keys 4 q4 + (0, 2) and + (1, 3), group by group
+#pragma unroll
+                for (int i = 0; i < NG / 2; ++i) lds<4>(dec + kTile * NG * 4 + (hb * 4 + q4) * NG * 8 + i * 16, vs + 4 * i);
 #pragma unroll
                 for (int nt = 0; nt < NT; ++nt) {
                     b0[nt] = transpose8x8(half2_of(s[hb][nt][0], s[hb][nt][1]));
@@ -487,11 +494,9 @@ __global__ void __launch_bounds__(Cfg<DH, NT>::THREADS, 1) k_kv4_attn(const Kv4A
 #pragma unroll
                     for (int jl = 0; jl < 2; ++jl) {
                         const int j = 2 * jj + jl;
-                        uint32_t even, odd;
-                        scales4(vs[hb][j], even, odd);
 #pragma unroll
                         for (int nt = 0; nt < NT; ++nt) {
-                            const uint32_t p0 = mul2(b0[nt], even), p1 = mul2(b1[nt], odd);
+                            const uint32_t p0 = mul2(b0[nt], vs[2 * j]), p1 = mul2(b1[nt], vs[2 * j + 1]);
                             mma(o[j][0][nt], a0[2 * jl], a1[2 * jl], a2[2 * jl], a3[2 * jl], p0, p1);
                             mma(o[j][1][nt], a0[2 * jl + 1], a1[2 * jl + 1], a2[2 * jl + 1], a3[2 * jl + 1], p0, p1);
                         }
