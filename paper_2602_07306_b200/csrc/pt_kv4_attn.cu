@@ -20,10 +20,12 @@ constexpr float kNone = -3.0e38f;         // reference of a row that has seen no
 #ifndef KW
 #define KW 12
 #define KS 3
+#define KW2 8
+#define KS2 3
 #endif
 template <int DH, int NT> struct Cfg {
     static constexpr int NG = DH / 32, RB = 8 * NT, BLK = kv4_block(DH);
-    static constexpr int WARPS = NT == 1 ? KW : 12, STAGES = (NT == 1 ? KS : 2) * (128 / DH), THREADS = WARPS * 32;
+    static constexpr int WARPS = NT == 1 ? KW : KW2, STAGES = (NT == 1 ? KS : KS2) * (128 / DH), THREADS = WARPS * 32;
     static constexpr int SCALE_BYTES = kTile * NG * 6;      // a tile's scales, decoded: K as fp32, V as fp16 pairs
     static constexpr int STAGE = 2 * BLK, RING = STAGES * STAGE;           // bytes of a warp's ring
     static constexpr int ROW = DH + 4, PART = RB * ROW + 2 * RB;           // floats of a part: rows, then (reference, sum) of each
@@ -211,6 +213,7 @@ __global__ void __launch_bounds__(Cfg<DH, NT>::THREADS, 1) k_kv4_attn(const Kv4A
     constexpr int NG = C::NG, RB = C::RB;
     extern __shared__ __align__(128) uint8_t smem[];
     __shared__ SegInfo info[C::WARPS][2];
+    __shared__ Cursor cursors[C::WARPS][2];               // of what is computed, of what is fetched: read at a segment's ends only
     __shared__ int flags[C::WARPS];                       // bit 0: a head part, 1: a tail part, 2: the tail's segment begins here
     __shared__ float factor[RB][32];
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, q4 = lane & 3;
@@ -233,32 +236,42 @@ __global__ void __launch_bounds__(Cfg<DH, NT>::THREADS, 1) k_kv4_attn(const Kv4A
     }
     // ---- the ring: lanes 0 and 1 fetch a block of 16 keys each; pages are looked up one tile ahead
     uint8_t* ring = smem + warp * C::RING;
-    Cursor ahead = cur;
+    if (lane == 0) cursors[warp][0] = cursors[warp][1] = cur;
+    __syncwarp();
+    // the next segment of a cursor; registers hold no more of it than its tiles need
+    auto step = [&](Cursor& at, bool& some) {
+        Cursor c = at;
+        __syncwarp();
+        some = walk.next(c);
+        if (lane == 0) at = c;
+        __syncwarp();
+        return c;
+    };
     const int bpp = ps / 16, step_col = 2 / bpp, step_in = 2 % bpp;            // blocks of a page: 1 .. 4
     const uint32_t page_bytes = (uint32_t)nkv * bpp * C::BLK;
-    int a_tile = 0, a_col = 0, a_in = 0, a_page = -1;
+    int a_tile = 0, a_hi = 0, a_seen = 0, a_col = 0, a_in = 0, a_page = -1;
     bool a_any = any, bad_page = false;
     const char* a_base = nullptr;                         // the head's first block in page 0
     const int32_t* a_bt = nullptr;
-    auto look = [&]() { if (lane < 2 && a_tile * kTile + 16 * lane < ahead.seen) a_page = a_bt[a_col]; };
-    auto aim = [&]() {
+    auto look = [&]() { if (lane < 2 && a_tile * kTile + 16 * lane < a_seen) a_page = a_bt[a_col]; };
+    auto aim = [&](const Cursor& ahead) {
         const int t = ahead.th / nkv, h = ahead.th - t * nkv, blk = 2 * ahead.lo + lane;
         a_base = p.slab.pool_l + (size_t)t * p.slab.tstride + (size_t)h * bpp * C::BLK;
         a_bt = p.bt + (size_t)ahead.b * p.maxp;
-        a_tile = ahead.lo;
+        a_tile = ahead.lo; a_hi = ahead.hi; a_seen = ahead.seen;
         a_col = blk / bpp; a_in = blk - a_col * bpp;
         look();
     };
     auto issue = [&](int slot) {
         if (lane < 2) {                                   // each expects its own bytes: none behind the last key
-            const bool some = a_tile * kTile + 16 * lane < ahead.seen, go = some && (uint32_t)a_page < (uint32_t)p.slab.num_pages;
+            const bool some = a_tile * kTile + 16 * lane < a_seen, go = some && (uint32_t)a_page < (uint32_t)p.slab.num_pages;
             bad_page |= some != go;
             mbar_expect_tx(&bars[slot], go ? C::BLK : 0);
             if (go) bulk_copy(smem_u32(ring + slot * C::STAGE + lane * C::BLK), a_base + (uint64_t)(uint32_t)a_page * page_bytes + a_in * C::BLK, C::BLK, &bars[slot]);
         }
-        if (++a_tile == ahead.hi) {
-            a_any = walk.next(ahead);
-            if (a_any) aim();
+        if (++a_tile == a_hi) {
+            const Cursor c = step(cursors[warp][1], a_any);
+            if (a_any) aim(c);
         } else {
             a_col += step_col; a_in += step_in;
             if (a_in >= bpp) { a_in -= bpp; ++a_col; }
@@ -267,7 +280,7 @@ __global__ void __launch_bounds__(Cfg<DH, NT>::THREADS, 1) k_kv4_attn(const Kv4A
     };
     // a segment's queries: lane (g, q4) has row g's octets q4 of every group
     uint4 raw[NT][NG];
-    auto fetch = [&]() {
+    auto fetch = [&](const Cursor& cur) {
         const int t = cur.th / nkv, h = cur.th - t * nkv;
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
@@ -277,7 +290,7 @@ __global__ void __launch_bounds__(Cfg<DH, NT>::THREADS, 1) k_kv4_attn(const Kv4A
             for (int j = 0; j < NG; ++j) raw[nt][j] = r < cur.S * G ? *reinterpret_cast<const uint4*>(src + 32 * j) : make_uint4(0, 0, 0, 0);
         }
     };
-    if (a_any) { aim(); fetch(); }
+    if (a_any) { aim(cur); fetch(cur); }
     __syncwarp();
     for (int s = 0; s < C::STAGES; ++s) if (a_any) issue(s);
 
@@ -286,10 +299,8 @@ __global__ void __launch_bounds__(Cfg<DH, NT>::THREADS, 1) k_kv4_attn(const Kv4A
     bool timed_out = false;
     while (any && !timed_out) {
         // ---- a segment: its queries
-        const int t = cur.th / nkv, h = cur.th - t * nkv, row0 = cur.row0, R = cur.S * G, r0 = cur.rb * RB;
         uint32_t qf[NG][NT][4];
         float unit[NT][2];
-        int lim[NT][2];
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
             uint32_t top = 0;
@@ -315,19 +326,16 @@ __global__ void __launch_bounds__(Cfg<DH, NT>::THREADS, 1) k_kv4_attn(const Kv4A
                 for (int i = 0; i < 4; ++i) qf[j][nt][i] = half2_of(__uint_as_float(w[i] << 16) * inv, __uint_as_float(w[i] & 0xffff0000u) * inv);
             }
 #pragma unroll
-            for (int c = 0; c < 2; ++c) {
-                unit[nt][c] = __shfl_sync(0xffffffffu, un, (2 * q4 + c) * 4);
-                lim[nt][c] = cur.K - cur.S + min((r0 + nt * 8 + 2 * q4 + c) / G, cur.S - 1) + 1;
-            }
+            for (int c = 0; c < 2; ++c) unit[nt][c] = __shfl_sync(0xffffffffu, un, (2 * q4 + c) * 4);
         }
-        const int all_see = cur.K - cur.S + r0 / G + 1, seen = cur.seen;
+        const int seen = cursors[warp][0].seen, hi = cursors[warp][0].hi, all_see = cursors[warp][0].K - cursors[warp][0].S + cursors[warp][0].rb * RB / G + 1;
         float o[NG][2][NT][4] = {}, ref[NT][2], l[NT][2];
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
             for (int c = 0; c < 2; ++c) { ref[nt][c] = kNone; l[nt][c] = 0.f; }
         float room = kTop;                                        // weights stay below 2^room
-        for (int tile = cur.lo; tile < cur.hi; ++tile) {
+        for (int tile = cursors[warp][0].lo; tile < hi; ++tile) {
             bool ok = mbar_try(&bars[slot], parity);
             if (!__all_sync(0xffffffffu, ok)) {
                 WaitClock clock;
@@ -403,13 +411,18 @@ __global__ void __launch_bounds__(Cfg<DH, NT>::THREADS, 1) k_kv4_attn(const Kv4A
             // ---- weights 2^(score - reference).  The reference lags behind the maximum: it is raised, and what has been summed
             // scaled down, only where a weight would pass 2^kTop, or where a scale of V of 2 or more has to be made room for
             if (key0 + kTile > all_see) {                         // some row does not see all of the tile
+                const Cursor& at = cursors[warp][0];
 #pragma unroll
-                for (int hb = 0; hb < 2; ++hb)
+                for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-                    for (int nt = 0; nt < NT; ++nt)
+                    for (int c = 0; c < 2; ++c) {
+                        const int end = at.K - at.S + min((at.rb * RB + nt * 8 + 2 * q4 + c) / G, at.S - 1) + 1 - key0 - 2 * g;
 #pragma unroll
-                        for (int i = 0; i < 4; ++i)
-                            if (key0 + 16 * hb + 2 * g + (i >> 1) >= lim[nt][i & 1]) s[hb][nt][i] = -INFINITY;
+                        for (int hb = 0; hb < 2; ++hb)
+#pragma unroll
+                            for (int i = 0; i < 2; ++i)
+                                if (16 * hb + i >= end) s[hb][nt][2 * i + c] = -INFINITY;
+                    }
             }
             float mx[NT][2];
             bool over = (high & 0x80808080u) != 0;
@@ -515,8 +528,10 @@ __global__ void __launch_bounds__(Cfg<DH, NT>::THREADS, 1) k_kv4_attn(const Kv4A
             for (int c = 0; c < 2; ++c)
 #pragma unroll
                 for (int m = 4; m < 32; m <<= 1) l[nt][c] += __shfl_xor_sync(0xffffffffu, l[nt][c], m);
-        const bool begins = cur.lo == 0, ends = cur.hi == cur.n;
-        const SegInfo si{t, h, row0, r0, min(RB, R - r0)};
+        const Cursor at = cursors[warp][0];
+        const int t = at.th / nkv, h = at.th - t * nkv, r0 = at.rb * RB;
+        const bool begins = at.lo == 0, ends = at.hi == at.n;
+        const SegInfo si{t, h, at.row0, r0, min(RB, at.S * G - r0)};
         if (begins && ends) {                                     // all of the segment's keys: the result
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt)
@@ -526,7 +541,7 @@ __global__ void __launch_bounds__(Cfg<DH, NT>::THREADS, 1) k_kv4_attn(const Kv4A
                     if (r >= si.rows) continue;
                     const int tok = (r0 + r) / G, hd = r0 + r - tok * G;
                     const float inv = 1.0f / l[nt][c];
-                    __nv_bfloat16* dst = p.o + (((size_t)t * p.M + row0 + tok) * p.nq + h * G + hd) * DH + 4 * g;
+                    __nv_bfloat16* dst = p.o + (((size_t)t * p.M + si.row0 + tok) * p.nq + h * G + hd) * DH + 4 * g;
 #pragma unroll
                     for (int j = 0; j < NG; ++j)
                         *reinterpret_cast<uint2*>(dst + 32 * j) = make_uint2(kv4_bf16(o[j][0][nt][c] * inv, o[j][0][nt][2 + c] * inv),
@@ -547,8 +562,8 @@ __global__ void __launch_bounds__(Cfg<DH, NT>::THREADS, 1) k_kv4_attn(const Kv4A
             my_flags |= ends ? 1 : begins ? 6 : 2;
             if (lane == 0) info[warp][ends ? 0 : 1] = si;
         }
-        any = walk.next(cur);
-        if (any) fetch();
+        const Cursor c = step(cursors[warp][0], any);
+        if (any) fetch(c);
     }
     if (timed_out) {
         // give the copies that are still in flight a bounded chance to land, then give up
