@@ -20,17 +20,23 @@ constexpr float kNone = -3.0e38f;         // reference of a row that has seen no
 #ifndef KW
 #define KW 12
 #define KS 3
-#define KW2 8
-#define KS2 3
+#define KW2 12
+#define KS2 2
+#define KW3 8
+#define KS3 3
+#define KW4 8
+#define KS4 3
 #endif
 template <int DH, int NT> struct Cfg {
     static constexpr int NG = DH / 32, RB = 8 * NT, BLK = kv4_block(DH);
-    static constexpr int WARPS = NT == 1 ? KW : KW2, STAGES = (NT == 1 ? KS : KS2) * (128 / DH), THREADS = WARPS * 32;
-    static constexpr int SCALE_BYTES = kTile * NG * 6;      // a tile's scales, decoded: K as fp32, V as fp16 pairs
-    static constexpr int STAGE = 2 * BLK, RING = STAGES * STAGE;           // bytes of a warp's ring
-    static constexpr int ROW = DH + 4, PART = RB * ROW + 2 * RB;           // floats of a part: rows, then (reference, sum) of each
-    static constexpr int HEADS = WARPS * RING, SCALES = HEADS + WARPS * PART * 4, BARS = SCALES + WARPS * SCALE_BYTES, SMEM = BARS + WARPS * STAGES * 8 + 16;
-    static_assert(PART * 4 <= RING && SMEM <= 227 * 1024 - 4096, "shared memory");
+    static constexpr int WARPS = NT == 1 ? KW : NT == 2 ? KW2 : NT == 3 ? KW3 : KW4, STAGES = (NT == 1 ? KS : NT == 2 ? KS2 : NT == 3 ? KS3 : KS4) * (128 / DH), THREADS = WARPS * 32;
+    static constexpr bool QS = NT > 1;                                     // queries in shared memory instead of registers, head parts in the scratch instead of there
+    static constexpr int SCALE_BYTES = kTile * NG * 6;                     // a tile's scales, decoded: K as fp32, V as fp16 pairs
+    static constexpr int STAGE = 2 * BLK, ROW = DH + 4, PART = RB * ROW + 2 * RB;      // floats of a part: rows, then (reference, sum) of each
+    static constexpr int RING = STAGES * STAGE > PART * 4 ? STAGES * STAGE : PART * 4;  // bytes of a warp's ring, which its last part takes when it is empty
+    static constexpr int HEADS = WARPS * RING, SCALES = HEADS + (QS ? 0 : WARPS * PART * 4), QUERIES = SCALES + WARPS * SCALE_BYTES, BARS = QUERIES + (QS ? WARPS * NG * NT * 512 : 0);
+    static constexpr int SMEM = BARS + WARPS * STAGES * 8;
+    static_assert(SMEM <= 227 * 1024 - 6144, "shared memory");
 };
 
 // A segment: the (token, head) rows [r0, r0 + rows) of one sequence, track and KV head, with the keys they see.
@@ -39,11 +45,18 @@ struct SegInfo { int t, h, row0, r0, rows; };
 struct Leftover { int head, tail, tail_begins; SegInfo seg; };
 
 template <int DH, int NT> struct Scratch {
-    static constexpr int PART = Cfg<DH, NT>::RB * (DH + 2);                // floats: rows, then (reference, sum) of each
-    Leftover* left;
-    float* parts;
-    __host__ __device__ explicit Scratch(void* p) : left((Leftover*)p), parts((float*)((char*)p + kMaxBlocks * 64)) {}
-    __device__ float* part(int block, int which) const { return parts + (size_t)(2 * block + which) * PART; }
+    using C = Cfg<DH, NT>;
+    static constexpr int PART = C::RB * (DH + 2);                          // floats of a block's part: rows, then (reference, sum) of each
+    static constexpr size_t bytes = (size_t)kMaxBlocks * (64 + 2 * PART * 4 + (C::QS ? C::WARPS * C::PART * 4 : 0));
+    char* p;
+    __device__ explicit Scratch(void* p_) : p((char*)p_) {}
+    __device__ Leftover* left() const { return (Leftover*)p; }
+    __device__ float* part(int block, int which) const { return (float*)(p + kMaxBlocks * 64) + (size_t)(2 * block + which) * PART; }
+    // head part of a warp: its ring is still in use
+    __device__ float* head(int block, int warp, uint8_t* smem) const {
+        if (!C::QS) return (float*)(smem + C::HEADS) + warp * C::PART;
+        return (float*)(p + kMaxBlocks * (64 + 2 * PART * 4)) + (size_t)(block * C::WARPS + warp) * C::PART;
+    }
 };
 
 __device__ __forceinline__ float ex2f(float x) {
@@ -231,7 +244,7 @@ __global__ void __launch_bounds__(Cfg<DH, NT>::THREADS, 1) k_kv4_attn(const Kv4A
     Cursor cur{};
     bool bad = false, any = walk.plan(cur, bad);
     if (bad) {                                            // every warp of the call finds the same
-        if (tid == 0) { report(p.status, PT_ERR_DEVICE_BOUNDS, LOC_KV4_LEN); sc.left[blockIdx.x] = Leftover{}; }
+        if (tid == 0) { report(p.status, PT_ERR_DEVICE_BOUNDS, LOC_KV4_LEN); sc.left()[blockIdx.x] = Leftover{}; }
         return;
     }
     // ---- the ring: lanes 0 and 1 fetch a block of 16 keys each; pages are looked up one tile ahead
@@ -279,18 +292,15 @@ __global__ void __launch_bounds__(Cfg<DH, NT>::THREADS, 1) k_kv4_attn(const Kv4A
         }
     };
     // a segment's queries: lane (g, q4) has row g's octets q4 of every group
-    uint4 raw[NT][NG];
-    auto fetch = [&](const Cursor& cur) {
+    uint4 raw[NG];
+    auto fetch = [&](const Cursor& cur, int nt) {
         const int t = cur.th / nkv, h = cur.th - t * nkv;
+        const int r = cur.rb * RB + nt * 8 + g, tok = r / G;
+        const __nv_bfloat16* src = p.q + (((size_t)t * p.M + cur.row0 + tok) * p.nq + h * G + (r - tok * G)) * DH + 8 * q4;
 #pragma unroll
-        for (int nt = 0; nt < NT; ++nt) {
-            const int r = cur.rb * RB + nt * 8 + g, tok = r / G;
-            const __nv_bfloat16* src = p.q + (((size_t)t * p.M + cur.row0 + tok) * p.nq + h * G + (r - tok * G)) * DH + 8 * q4;
-#pragma unroll
-            for (int j = 0; j < NG; ++j) raw[nt][j] = r < cur.S * G ? *reinterpret_cast<const uint4*>(src + 32 * j) : make_uint4(0, 0, 0, 0);
-        }
+        for (int j = 0; j < NG; ++j) raw[j] = r < cur.S * G ? *reinterpret_cast<const uint4*>(src + 32 * j) : make_uint4(0, 0, 0, 0);
     };
-    if (a_any) { aim(cur); fetch(cur); }
+    if (a_any) { aim(cur); fetch(cur, 0); }
     __syncwarp();
     for (int s = 0; s < C::STAGES; ++s) if (a_any) issue(s);
 
@@ -299,14 +309,16 @@ __global__ void __launch_bounds__(Cfg<DH, NT>::THREADS, 1) k_kv4_attn(const Kv4A
     bool timed_out = false;
     while (any && !timed_out) {
         // ---- a segment: its queries
-        uint32_t qf[NG][NT][4];
+        uint32_t qf[C::QS ? 1 : NG][C::QS ? 1 : NT][4];
+        const uint32_t qs = smem_u32(smem + C::QUERIES + warp * NG * NT * 512 + lane * 16);
         float unit[NT][2];
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
+            if (nt) fetch(cursors[warp][0], nt);
             uint32_t top = 0;
 #pragma unroll
             for (int j = 0; j < NG; ++j) {
-                const uint32_t w[4] = {raw[nt][j].x, raw[nt][j].y, raw[nt][j].z, raw[nt][j].w};
+                const uint32_t w[4] = {raw[j].x, raw[j].y, raw[j].z, raw[j].w};
 #pragma unroll
                 for (int i = 0; i < 4; ++i) top = __vmaxu2(top, w[i] & 0x7fff7fffu);
             }
@@ -321,9 +333,16 @@ __global__ void __launch_bounds__(Cfg<DH, NT>::THREADS, 1) k_kv4_attn(const Kv4A
             const float un = __uint_as_float((uint32_t)(e - 13 + 127) << 23) * p.scale_log2;
 #pragma unroll
             for (int j = 0; j < NG; ++j) {
-                const uint32_t w[4] = {raw[nt][j].x, raw[nt][j].y, raw[nt][j].z, raw[nt][j].w};
+                const uint32_t w[4] = {raw[j].x, raw[j].y, raw[j].z, raw[j].w};
+                uint32_t f[4];
 #pragma unroll
-                for (int i = 0; i < 4; ++i) qf[j][nt][i] = half2_of(__uint_as_float(w[i] << 16) * inv, __uint_as_float(w[i] & 0xffff0000u) * inv);
+                for (int i = 0; i < 4; ++i) f[i] = half2_of(__uint_as_float(w[i] << 16) * inv, __uint_as_float(w[i] & 0xffff0000u) * inv);
+                if constexpr (C::QS) {                            // read back by the lane that wrote it
+                    asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(qs + (j * NT + nt) * 512), "r"(f[0]), "r"(f[1]), "r"(f[2]), "r"(f[3]) : "memory");
+                } else {
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) qf[j][nt][i] = f[i];
+                }
             }
 #pragma unroll
             for (int c = 0; c < 2; ++c) unit[nt][c] = __shfl_sync(0xffffffffu, un, (2 * q4 + c) * 4);
@@ -398,8 +417,15 @@ __global__ void __launch_bounds__(Cfg<DH, NT>::THREADS, 1) k_kv4_attn(const Kv4A
 #pragma unroll
                     for (int nt = 0; nt < NT; ++nt) {
                         float c[4];
-                        mma0(c, h0[0], h1[0], h0[1], h1[1], qf[j][nt][0], qf[j][nt][1]);
-                        mma(c, h0[2], h1[2], h0[3], h1[3], qf[j][nt][2], qf[j][nt][3]);
+                        uint32_t f[4];
+                        if constexpr (C::QS) {
+                            lds<4>(qs + (j * NT + nt) * 512, f);
+                        } else {
+#pragma unroll
+                            for (int i = 0; i < 4; ++i) f[i] = qf[j][nt][i];
+                        }
+                        mma0(c, h0[0], h1[0], h0[1], h1[1], f[0], f[1]);
+                        mma(c, h0[2], h1[2], h0[3], h1[3], f[2], f[3]);
 #pragma unroll
                         for (int i = 0; i < 4; ++i) {
                             const float f = __uint_as_float(ks[(i >> 1) * NG + j]);
@@ -548,7 +574,7 @@ __global__ void __launch_bounds__(Cfg<DH, NT>::THREADS, 1) k_kv4_attn(const Kv4A
                                                                             kv4_bf16(o[j][1][nt][c] * inv, o[j][1][nt][2 + c] * inv));
                 }
         } else {                                                  // a part: merged below, or by k_kv4_merge
-            float* part = ends ? (float*)(smem + C::HEADS) + warp * C::PART : (float*)ring;
+            float* part = ends ? sc.head(blockIdx.x, warp, smem) : (float*)ring;
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
@@ -563,7 +589,7 @@ __global__ void __launch_bounds__(Cfg<DH, NT>::THREADS, 1) k_kv4_attn(const Kv4A
             if (lane == 0) info[warp][ends ? 0 : 1] = si;
         }
         const Cursor c = step(cursors[warp][0], any);
-        if (any) fetch(c);
+        if (any) fetch(c, 0);
     }
     if (timed_out) {
         // give the copies that are still in flight a bounded chance to land, then give up
@@ -594,7 +620,7 @@ __global__ void __launch_bounds__(Cfg<DH, NT>::THREADS, 1) k_kv4_attn(const Kv4A
             const uint32_t c = closers >> f;
             return c ? f + __ffs(c) - 1 : 31 - __clz(members);
         };
-        auto part_of = [&](int l) { return l & 1 ? (const float*)(smem + (l >> 1) * C::RING) : (const float*)(smem + C::HEADS) + (l >> 1) * C::PART; };
+        auto part_of = [&](int l) { return l & 1 ? (const float*)(smem + (l >> 1) * C::RING) : (const float*)sc.head(blockIdx.x, l >> 1, smem); };
         const uint32_t before = starts & ((2u << lane) - 1u);
         const int mine_first = before ? 31 - __clz(before) : lane, mine_last = exists ? last_of(mine_first) : lane;
         const bool whole = ((begins >> mine_first) & 1) && !(mine_last & 1);      // the chain has all of the segment's keys
@@ -664,7 +690,7 @@ __global__ void __launch_bounds__(Cfg<DH, NT>::THREADS, 1) k_kv4_attn(const Kv4A
                 left.tail = 1; left.tail_begins = (begins >> first) & 1; left.seg = info[first >> 1][first & 1];
             }
         }
-        sc.left[blockIdx.x] = left;
+        sc.left()[blockIdx.x] = left;
     }
 }
 
@@ -679,12 +705,12 @@ __global__ void __launch_bounds__(kMergeThreads) k_kv4_merge(const Kv4AttnP p, v
     grid_dep_launch();
     const Scratch<DH, NT> sc(scratch);
     const int r = blockIdx.y, d = threadIdx.x % DH, grp = threadIdx.x / DH, lane = threadIdx.x & 31, c0 = blockIdx.x;
-    const Leftover first = sc.left[c0];
+    const Leftover first = sc.left()[c0];
     if (!first.tail || !first.tail_begins || r >= first.seg.rows) return;
     // the block that ends the segment: the first behind c0 with a head
     int last = blocks - 1;
     for (int base = c0 + 1; base < blocks; base += 32) {
-        const uint32_t heads = __ballot_sync(0xffffffffu, base + lane < blocks && sc.left[base + lane].head);
+        const uint32_t heads = __ballot_sync(0xffffffffu, base + lane < blocks && sc.left()[base + lane].head);
         if (heads) { last = base + __ffs(heads) - 1; break; }
     }
     float top = kNone, sum = 0.f, acc = 0.f;
@@ -739,12 +765,18 @@ template <int DH, int NT> pt_status launch_t(const Kv4AttnP& p, void* scratch, c
 
 }  // namespace
 
-size_t kv4_attn_scratch_bytes(int dh) { return (size_t)kMaxBlocks * 64 + (size_t)kMaxBlocks * 2 * 16 * (dh + 2) * 4; }
+template <int NT> constexpr size_t scratch_of(int dh) { return dh == 64 ? Scratch<64, NT>::bytes : Scratch<128, NT>::bytes; }
+size_t kv4_attn_scratch_bytes(int dh) { return std::max(std::max(scratch_of<1>(dh), scratch_of<2>(dh)), std::max(scratch_of<3>(dh), scratch_of<4>(dh))); }
+
+template <int DH> static pt_status launch_dh(const Kv4AttnP& p, int tiles, void* scratch, cudaStream_t st) {
+    return tiles <= 1 ? launch_t<DH, 1>(p, scratch, st) : tiles == 2 ? launch_t<DH, 2>(p, scratch, st) : tiles == 3 ? launch_t<DH, 3>(p, scratch, st) : launch_t<DH, 4>(p, scratch, st);
+}
 
 pt_status launch_kv4_attn(const Kv4AttnP& p, int dh, void* scratch, cudaStream_t st) {
-    const bool wide = p.qlen && (int64_t)p.M * (p.nq / p.slab.nkv) > 8 * (int64_t)p.B;
-    if (dh == 64) return wide ? launch_t<64, 2>(p, scratch, st) : launch_t<64, 1>(p, scratch, st);
-    return wide ? launch_t<128, 2>(p, scratch, st) : launch_t<128, 1>(p, scratch, st);
+    // row tiles of 8 for the mean number of (token, head) rows of a sequence: its keys are then read once
+    const int64_t rows = p.qlen ? ((int64_t)p.M * (p.nq / p.slab.nkv) + p.B - 1) / p.B : 1;
+    const int tiles = (int)std::min<int64_t>(4, (rows + 7) / 8);
+    return dh == 64 ? launch_dh<64>(p, tiles, scratch, st) : launch_dh<128>(p, tiles, scratch, st);
 }
 
 }  // namespace pt
