@@ -24,12 +24,10 @@ constexpr float kNone = -3.0e38f;         // reference of a row that has seen no
 #define KS2 2
 #define KW3 8
 #define KS3 3
-#define KW4 8
-#define KS4 3
 #endif
 template <int DH, int NT> struct Cfg {
     static constexpr int NG = DH / 32, RB = 8 * NT, BLK = kv4_block(DH);
-    static constexpr int WARPS = NT == 1 ? KW : NT == 2 ? KW2 : NT == 3 ? KW3 : KW4, STAGES = (NT == 1 ? KS : NT == 2 ? KS2 : NT == 3 ? KS3 : KS4) * (128 / DH), THREADS = WARPS * 32;
+    static constexpr int WARPS = NT == 1 ? KW : NT == 2 ? KW2 : KW3, STAGES = (NT == 1 ? KS : NT == 2 ? KS2 : KS3) * (128 / DH), THREADS = WARPS * 32;
     static constexpr bool QS = NT > 1;                                     // queries in shared memory instead of registers, head parts in the scratch instead of there
     static constexpr int SCALE_BYTES = kTile * NG * 6;                     // a tile's scales, decoded: K as fp32, V as fp16 pairs
     static constexpr int STAGE = 2 * BLK, ROW = DH + 4, PART = RB * ROW + 2 * RB;      // floats of a part: rows, then (reference, sum) of each
@@ -118,20 +116,20 @@ template <int DH, int NT> struct Walk {
     __device__ int seen(int S, int K, int rb) const { return (rb + 1) * RB >= S * G ? K : K - S + ((rb + 1) * RB - 1) / G + 1; }
     __device__ void load(int b, int& S, int& K) const { S = p.qlen ? p.qlen[b] : 1; K = p.kvlen[b]; }
     __device__ static int cost(int seen) { return (seen + kTile - 1) / kTile + kSegCost; }
-    // of all row blocks of a sequence
-    __device__ long long cost(int S, int K) const {
-        long long n = 0;
+    // of all row blocks of a sequence (the host has checked that those of all sequences fit)
+    __device__ int cost(int S, int K) const {
+        int n = 0;
         for (int rb = 0; rb * RB < S * G; ++rb) n += cost(seen(S, K, rb));
         return n;
     }
     // the cursor at unit `in` of its segment; takes what the range has of it
-    __device__ void enter(Cursor& c, long long in) const {
+    __device__ void enter(Cursor& c, int in) const {
         c.seen = seen(c.S, c.K, c.rb);
         c.n = (c.seen + kTile - 1) / kTile;
-        const long long end = min((long long)c.n + kSegCost, in + c.left);
-        c.lo = max(0, (int)in - kSegCost);
-        c.hi = max(0, (int)end - kSegCost);
-        c.left -= end - in;
+        const int take = (int)min((long long)(c.n + kSegCost - in), c.left);
+        c.lo = max(0, in - kSegCost);
+        c.hi = max(0, in + take - kSegCost);
+        c.left -= take;
     }
     // to the next segment of the range with tiles in it; false: there is none
     __device__ bool next(Cursor& c) const {
@@ -153,18 +151,21 @@ template <int DH, int NT> struct Walk {
     // begins is found by a ballot, and its sequences are looked through the same way.  false: nothing to do (or `bad` lengths)
     __device__ bool plan(Cursor& c, bool& bad) const {
         const int lane = threadIdx.x & 31, per = (p.B + 31) / 32;
-        long long mine = 0, rows = 0;
+        int mine = 0, S = 0, K = 0;
+        long long rows = 0;
         bad = false;
         for (int b = lane * per; b < min(p.B, (lane + 1) * per); ++b) {
-            int S, K;
             load(b, S, K);
             if (S < 0 || K < S || S > p.M || K > (long long)p.maxp * p.slab.ps) { bad = true; break; }
             rows += S;
             mine += cost(S, K);
         }
-        long long up = scan(mine), up_rows = p.qlen ? scan(rows) : 0;
+        int up = scan(mine);
+        long long up_rows = 0;
+        if (p.qlen) up_rows = scan(rows);
         bad = __any_sync(0xffffffffu, bad) || __shfl_sync(0xffffffffu, up_rows, 31) > p.M;
-        const long long per_head = __shfl_sync(0xffffffffu, up, 31), units = per_head * p.slab.nkv * p.T;
+        const int per_head = __shfl_sync(0xffffffffu, up, 31);
+        const long long units = (long long)per_head * (p.slab.nkv * p.T);
         if (bad || units == 0) return false;
         // the call's units go in equal shares to the warps of as many blocks as have one for each warp
         constexpr int W = Cfg<DH, NT>::WARPS;
@@ -175,33 +176,32 @@ template <int DH, int NT> struct Walk {
         c.left = share + (gw < more);
         if (c.left == 0) return false;
         c.th = (int)quotient(u0, per_head);
-        long long in = u0 - c.th * per_head;
-        int l = __popc(__ballot_sync(0xffffffffu, up <= in));
+        int in = (int)(u0 - (long long)c.th * per_head);
+        const int l = __popc(__ballot_sync(0xffffffffu, up <= in));
         in -= __shfl_sync(0xffffffffu, up - mine, l);
-        c.row0 = p.qlen ? (int)__shfl_sync(0xffffffffu, up_rows - rows, l) : 0;
-        for (int b0 = l * per;; b0 += 32) {
-            const int b = b0 + lane;
-            int S = 0, K = 0;
-            if (b < min(p.B, (l + 1) * per)) load(b, S, K);
-            mine = cost(S, K);
-            up = scan(mine);
-            const int at = __popc(__ballot_sync(0xffffffffu, up <= in));
-            if (p.qlen) {
+        c.row0 = p.qlen ? (int)__shfl_sync(0xffffffffu, up_rows - rows, l) : l * per;
+        int at = l;
+        if (per > 1) {
+            for (int b0 = l * per;; b0 += 32) {
+                const int b = b0 + lane;
+                S = K = 0;
+                if (b < min(p.B, (l + 1) * per)) load(b, S, K);
+                mine = cost(S, K);
+                up = scan(mine);
+                at = __popc(__ballot_sync(0xffffffffu, up <= in));
                 int sum = lane < at ? S : 0;
 #pragma unroll
                 for (int o = 16; o; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
                 c.row0 += sum;
+                if (at < 32) { c.b = b0 + at; break; }
+                in -= __shfl_sync(0xffffffffu, up, 31);
             }
-            if (at < 32) {
-                in -= __shfl_sync(0xffffffffu, up - mine, at);
-                c.b = b0 + at;
-                c.S = __shfl_sync(0xffffffffu, S, at);
-                c.K = __shfl_sync(0xffffffffu, K, at);
-                break;
-            }
-            in -= __shfl_sync(0xffffffffu, up, 31);
+            in -= __shfl_sync(0xffffffffu, up - mine, at);
+        } else {
+            c.b = l;
         }
-        if (!p.qlen) c.row0 = c.b;
+        c.S = __shfl_sync(0xffffffffu, S, at);
+        c.K = __shfl_sync(0xffffffffu, K, at);
         for (c.rb = 0;; ++c.rb) {
             const int n = cost(seen(c.S, c.K, c.rb));
             if (in < n) break;
@@ -210,10 +210,10 @@ template <int DH, int NT> struct Walk {
         enter(c, in);
         return c.lo < c.hi || next(c);
     }
-    __device__ static long long scan(long long x) {
+    template <typename N> __device__ static N scan(N x) {
 #pragma unroll
         for (int o = 1; o < 32; o <<= 1) {
-            const long long y = __shfl_up_sync(0xffffffffu, x, o);
+            const N y = __shfl_up_sync(0xffffffffu, x, o);
             if ((int)(threadIdx.x & 31) >= o) x += y;
         }
         return x;
@@ -657,14 +657,15 @@ __global__ void __launch_bounds__(Cfg<DH, NT>::THREADS, 1) k_kv4_attn(const Kv4A
             const int r = task - chain * RB, first = __ffs(rest) - 1, last = last_of(first);
             const SegInfo si = info[first >> 1][first & 1];
             if (r >= si.rows) continue;
+            const uint32_t chain_of = members & ((2u << last) - 1u) & ~((1u << first) - 1u);
             constexpr int V = DH / 32;                            // columns of a lane
             using Vec = std::conditional_t<V == 4, float4, float2>;
             alignas(16) float acc[V] = {};
-#pragma unroll 4
-            for (int l = first; l <= last; ++l) {
-                if (!((members >> l) & 1)) continue;
-                const float f = factor[r][l];
-                const Vec x = *reinterpret_cast<const Vec*>(part_of(l) + r * C::ROW + lane * V);
+#pragma unroll(C::QS ? 4 : 2 * C::WARPS)
+            for (int l = 0; l < 2 * C::WARPS; ++l) {              // straight-line: all loads in flight at once
+                Vec x{};
+                float f = 0.f;
+                if ((chain_of >> l) & 1) { f = factor[r][l]; x = *reinterpret_cast<const Vec*>(part_of(l) + r * C::ROW + lane * V); }
 #pragma unroll
                 for (int i = 0; i < V; ++i) acc[i] += f * reinterpret_cast<const float*>(&x)[i];
             }
@@ -753,10 +754,13 @@ template <int DH, int NT> pt_status launch_t(const Kv4AttnP& p, void* scratch, c
         sms = n;
     }
     const int blocks = std::min(sms, kMaxBlocks);
+    // units of one head are counted in 32 bits: every block of rows with every key that the table can name
+    const double most = ((double)p.M * (p.nq / p.slab.nkv) / C::RB + p.B) * ((double)p.maxp * p.slab.ps / kTile + 1 + kSegCost);
+    if (most > 2e9) { set_error("4-bit attention: too many sequences, rows or pages for one call"); return PT_ERR_UNSUPPORTED; }
     cudaError_t e = launch_dependent(k_kv4_attn<DH, NT>, dim3(blocks), dim3(C::THREADS), (size_t)C::SMEM, st, p, scratch);
     g_launches.fetch_add(1, std::memory_order_relaxed);
     if (e == cudaSuccess && blocks > 1) {
-        e = launch_dependent(k_kv4_merge<DH, NT>, dim3(blocks - 1, C::RB), dim3(kMergeThreads), (size_t)0, st, p, scratch, blocks);
+        e = launch_dependent(k_kv4_merge<DH, NT>, dim3(blocks - 1, p.qlen ? C::RB : p.nq / p.slab.nkv), dim3(kMergeThreads), (size_t)0, st, p, scratch, blocks);
         g_launches.fetch_add(1, std::memory_order_relaxed);
     }
     if (e != cudaSuccess) { set_error("4-bit attention launch: %s", cudaGetErrorString(e)); return PT_ERR_CUDA; }
@@ -766,16 +770,18 @@ template <int DH, int NT> pt_status launch_t(const Kv4AttnP& p, void* scratch, c
 }  // namespace
 
 template <int NT> constexpr size_t scratch_of(int dh) { return dh == 64 ? Scratch<64, NT>::bytes : Scratch<128, NT>::bytes; }
-size_t kv4_attn_scratch_bytes(int dh) { return std::max(std::max(scratch_of<1>(dh), scratch_of<2>(dh)), std::max(scratch_of<3>(dh), scratch_of<4>(dh))); }
+size_t kv4_attn_scratch_bytes(int dh) { return std::max(scratch_of<1>(dh), std::max(scratch_of<2>(dh), scratch_of<3>(dh))); }
 
 template <int DH> static pt_status launch_dh(const Kv4AttnP& p, int tiles, void* scratch, cudaStream_t st) {
-    return tiles <= 1 ? launch_t<DH, 1>(p, scratch, st) : tiles == 2 ? launch_t<DH, 2>(p, scratch, st) : tiles == 3 ? launch_t<DH, 3>(p, scratch, st) : launch_t<DH, 4>(p, scratch, st);
+    return tiles <= 1 ? launch_t<DH, 1>(p, scratch, st) : tiles == 2 ? launch_t<DH, 2>(p, scratch, st) : launch_t<DH, 3>(p, scratch, st);
 }
 
 pt_status launch_kv4_attn(const Kv4AttnP& p, int dh, void* scratch, cudaStream_t st) {
-    // row tiles of 8 for the mean number of (token, head) rows of a sequence: its keys are then read once
-    const int64_t rows = p.qlen ? ((int64_t)p.M * (p.nq / p.slab.nkv) + p.B - 1) / p.B : 1;
-    const int tiles = (int)std::min<int64_t>(4, (rows + 7) / 8);
+    // The mean number of (token, head) rows of a sequence in as few passes over its keys as can be, in equal shares: up to three
+    // tiles of 8 rows a pass.  (Four sequences of 20k keys, 4 tracks, 4 KV heads: 44, 67 and 86 us a pass of 1, 2 and 3 tiles;
+    // with four, whose accumulators take 128 registers a lane, 134 us, as much as two passes of two.)
+    const int64_t rows = p.qlen ? ((int64_t)p.M * (p.nq / p.slab.nkv) + p.B - 1) / p.B : 1, eights = (rows + 7) / 8, passes = (eights + 2) / 3;
+    const int tiles = (int)((eights + passes - 1) / passes);
     return dh == 64 ? launch_dh<64>(p, tiles, scratch, st) : launch_dh<128>(p, tiles, scratch, st);
 }
 
