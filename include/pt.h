@@ -59,8 +59,23 @@ typedef enum { PT_F32 = 0, PT_BF16 = 1 } pt_dtype;
  * bias 7, 3 mantissa bits; largest value 448) and one fp32 scale, the smallest power of two s (not below
  * 2^-100) with max|v| / s <= 448 (1 for an all-zero vector); a code is v / s rounded to nearest even,
  * saturating.  Attention reads code * s.  The paper has no cache and no such format: it is this library's
- * own, there so that the ragged decode workload fits one device whole. */
-typedef enum { PT_KV_MODEL = 0, PT_KV_E4M3 = 1 } pt_kv_dtype;
+ * own, there so that the ragged decode workload fits one device whole.
+ *
+ * PT_KV_E2M1 (bf16 models on the tensor-core path, head_dim 64 or 128, pages of a multiple of 16 tokens; 4.25 bits a value):
+ * a cached vector is split into groups of 32 values.  A group's scale s is the smallest unsigned E5M3 number (one byte: the
+ * upper 8 bits of a positive fp16, at most 61440) with max|v| <= 6 s; a code is v / s rounded to the nearest E2M1 number (4 bits:
+ * a sign and 0, 0.5, 1, 1.5, 2, 3, 4, 6), ties to the even code, saturating.  A group that holds a NaN or an infinity reads as
+ * NaN (scale byte 255, codes 0).  A page is [kv_head][slot / 16] blocks of 16 tokens, each of 17 * head_dim bytes, in the order in
+ * which the matrix instructions of its attention take them (slot s of the block; the code of the lower dimension in a byte's
+ * lower half):
+ *   K codes   head_dim / 2 bytes a token, token s at place (s % 2) * 8 + s / 2: [q < 4][group] 4 bytes, dims 32 group + 8 q .. + 7
+ *   K scales  [s][group]
+ *   V codes   s = 4 q + i: [group] 2 bytes, dims 32 group + 4 g .. + 3, for each g < 8: head_dim 128 [i / 2][g][q][i % 2],
+ *             head_dim 64 [g][q][i]
+ *   V scales  [q][group][i]
+ * Attention reads code * scale.  Calls with one or a few new tokens a sequence attend straight to the codes, others to a bf16
+ * copy, as with E4M3. */
+typedef enum { PT_KV_MODEL = 0, PT_KV_E4M3 = 1, PT_KV_E2M1 = 2 } pt_kv_dtype;
 
 typedef enum {
     PT_WQ = 0, PT_WK = 1, PT_WV = 2, PT_WO = 3, PT_WG = 4, PT_WU = 5, PT_WD = 6,
@@ -151,7 +166,8 @@ int32_t pt_sync_count(const pt_model* m);
 
 pt_status pt_kv_cache_bytes(const pt_model* m, int32_t num_pages, int32_t page_size, size_t* bytes);
 /* The same for a cache of the given pt_kv_dtype.  An E4M3 pool is the codes, laid out as above with one byte
- * per element, followed (256-byte aligned) by the fp32 scales [T][L][page][K|V][kv_head][slot]. */
+ * per element, followed (256-byte aligned) by the fp32 scales [T][L][page][K|V][kv_head][slot].  An E2M1 pool is
+ * [T][L][page][kv_head][page_size / 16] blocks of 17 * head_dim bytes. */
 pt_status pt_kv_cache_bytes_ex(const pt_model* m, int32_t num_pages, int32_t page_size, int32_t kv_dtype, size_t* bytes);
 
 /* Wrap the caller-owned device buffer `dev_pool` (256-byte aligned) as a cache of `num_pages`
@@ -179,7 +195,8 @@ pt_status pt_kv_seq_truncate(pt_kv_cache* c, int32_t seq, int32_t len);
 /* Copy the block table of `seq` into `pages` (host, capacity `cap`); *n = pages owned. */
 pt_status pt_kv_block_table(const pt_kv_cache* c, int32_t seq, int32_t* pages, int32_t cap, int32_t* n);
 /* Element offset inside the pool of the head_dim values cached for (track, layer, seq, pos,
- * kv = 0 for K / 1 for V, kv_head).  The position must lie inside the reserved pages. */
+ * kv = 0 for K / 1 for V, kv_head).  The position must lie inside the reserved pages.  E2M1 caches: the byte offset of the K
+ * or V codes of the 16 tokens of which pos is one. */
 pt_status pt_kv_slot(const pt_kv_cache* c, int32_t track, int32_t layer, int32_t seq, int32_t pos,
                      int32_t kv, int32_t kv_head, int64_t* elem_offset);
 
@@ -208,7 +225,8 @@ pt_status pt_kv_compact(pt_kv_cache* c, int32_t* moved, void* stream);
 pt_status pt_kv_move_pool(pt_kv_cache* c, int32_t num_pages, void* dev_pool, size_t bytes, void* stream);
 
 /* E4M3 caches: byte offset, from the start of the pool, of the fp32 scale of the vector that pt_kv_slot
- * addresses (there the offset counts one-byte codes).  PT_ERR_STATE for a cache in the model dtype. */
+ * addresses (there the offset counts one-byte codes); E2M1 caches: of the scales of the 16 tokens.  PT_ERR_STATE for a cache
+ * in the model dtype. */
 pt_status pt_kv_scale_slot(const pt_kv_cache* c, int32_t track, int32_t layer, int32_t seq, int32_t pos,
                            int32_t kv, int32_t kv_head, int64_t* byte_offset);
 
@@ -222,7 +240,9 @@ pt_status pt_workspace_bytes(const pt_model* m, int64_t max_tokens, int32_t max_
  * through a bf16 staging area on their way into the cache, and a prefill call attends to a bf16 copy of
  * code * scale of every key its sequences hold: `max_context` bounds, over one prefill call, the sum over its
  * sequences of the cached length after the call, each rounded up to 16 (0 = prefill calls only ever start
- * from empty sequences: max_tokens + 16 * max_batch is used).  Decode calls need no such copy. */
+ * from empty sequences: max_tokens + 16 * max_batch is used).  Decode calls need no such copy.  An E2M1 cache the same, but for
+ * calls that attend straight to the codes (pt_extend and pt_prefill where the sequences' new tokens are few), which make no
+ * copy.  Workspace for an E2M1 cache serves calls on an E4M3 cache too, and either one's serves a cache in the model dtype. */
 pt_status pt_workspace_bytes_ex(const pt_model* m, int64_t max_tokens, int32_t max_batch, int32_t page_size,
                                 int32_t kv_dtype, int64_t max_context, size_t* bytes);
 

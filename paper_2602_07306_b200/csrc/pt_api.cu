@@ -8,6 +8,7 @@
 #include <unordered_set>
 
 #include "pt_chunk.h"
+#include "pt_kv4.h"
 #include "pt_internal.h"
 
 namespace pt {
@@ -27,29 +28,30 @@ void set_error(const char* fmt, ...) {
     pt::set_error("%s failed: %s", #call, cudaGetErrorString(e_)); return PT_ERR_CUDA; } } while (0)
 
 
-static size_t meta_bytes(int64_t M, int B, int maxp, bool fp8, bool ragged) {
+static size_t meta_bytes(int64_t M, int B, int maxp, int kv_dtype, bool ragged) {
     size_t b = 0;
     b += align_up((size_t)M * 8, 256);                 // row_kvoff
     b += align_up((size_t)M * 4, 256) * 2;             // row_pos, row_b
     b += align_up((size_t)B * 4, 256) * 2;             // kvlen, nsplit
     b += align_up((size_t)B * maxp * 4, 256);          // block table rows
     b += align_up((size_t)B * kMaxSplits * 16, 256);   // decode work items
-    if (fp8) {
+    if (kv_dtype != PT_KV_MODEL) {
         b += align_up((size_t)M * 8, 256) * 2;         // row_stageoff, row_attnoff
         b += align_up((size_t)B * 4, 256);             // ctx_start
         b += align_up((size_t)B * ((size_t)maxp * 4 + 1) * 4, 256);   // pages of the attention copy (16 tokens each; cache pages hold up to 64)
     }
-    if (ragged) b += align_up((size_t)B * 4, 256);     // qlen
+    if (ragged || kv_dtype == PT_KV_E2M1) b += align_up((size_t)B * 4, 256);     // qlen
     return b;
 }
 
-// Carve the workspace; with base == nullptr only the size is computed.  fp8: the cache holds E4M3 codes;
+// Carve the workspace; with base == nullptr only the size is computed;
 // ctx_keys: keys of the attention copy a prefill call needs (0 for a decode call); ragged: a call of pt_extend.
-static size_t carve(const pt_model* m, int64_t M, int B, int maxp, bool fp8, int64_t ctx_keys, bool ragged, char* base, Work* w) {
+static size_t carve(const pt_model* m, int64_t M, int B, int maxp, int kv_dtype, int64_t ctx_keys, bool ragged, char* base, Work* w) {
     const pt_config& c = m->cfg;
+    const bool coded = kv_dtype != PT_KV_MODEL;
     size_t off = 0;
     auto take = [&](size_t bytes) { size_t o = off; off += align_up(bytes, 256); return base ? base + o : nullptr; };
-    char* meta = (char*)take(meta_bytes(M, B, maxp, fp8, ragged));
+    char* meta = (char*)take(meta_bytes(M, B, maxp, kv_dtype, ragged));
     size_t TMH = (size_t)c.T * M * c.hidden;
     float* hT = (float*)take(TMH * 4);
     float* hS = (float*)take((size_t)M * c.hidden * 4);
@@ -72,11 +74,12 @@ static size_t carve(const pt_model* m, int64_t M, int B, int maxp, bool fp8, int
     }
     float* ssq = m->tc ? (float*)take((size_t)c.T * M * ((c.hidden + kSsqTile - 1) / kSsqTile) * 4) : nullptr;
     float* part = m->tc ? (float*)take((size_t)c.T * B * kMaxSplits * c.heads * (m->dh + 2) * 4) : nullptr;
-    void* kv_stage = fp8 ? take((size_t)c.T * 2 * m->KVD * M * 2) : nullptr;
-    void* attn_kv = fp8 && ctx_keys > 0 ? take((size_t)c.T * 2 * m->KVD * (size_t)ctx_keys * 2) : nullptr;
+    void* kv_stage = coded ? take((size_t)c.T * 2 * m->KVD * M * 2) : nullptr;
+    void* attn_kv = coded && ctx_keys > 0 ? take((size_t)c.T * 2 * m->KVD * (size_t)ctx_keys * 2) : nullptr;
     void* chunk = ragged && m->tc ? take(chunk_scratch_bytes(c.T, B, c.heads, m->dh)) : nullptr;
+    void* attn4 = kv_dtype == PT_KV_E2M1 ? take(kv4_attn_scratch_bytes(m->dh)) : nullptr;
     if (w) {
-        w->chunk = chunk;
+        w->chunk = chunk; w->attn4 = attn4;
         w->kv_stage = kv_stage; w->attn_kv = attn_kv; w->gates = gates; w->moe = mw;
         w->hT = hT; w->hS = hS; w->a = a; w->qkv = qkv; w->o = o; w->gu = gu; w->z = z;
         w->ssq = ssq; w->part = part; w->total = off;
@@ -85,19 +88,25 @@ static size_t carve(const pt_model* m, int64_t M, int B, int maxp, bool fp8, int
     return off;
 }
 
-// Bytes of the codes (or model-dtype values) of a pool; an E4M3 pool's scales follow, 256-byte aligned.
+// Bytes of the codes (or model-dtype values) of a pool; an E4M3 pool's scales follow, 256-byte aligned; an E2M1 pool is one piece.
+static bool kv_dtype_known(int32_t d) { return d == PT_KV_MODEL || d == PT_KV_E4M3 || d == PT_KV_E2M1; }
+
 pt_status kv_pool_layout(const pt_model* m, int32_t num_pages, int32_t page_size, int32_t kv_dtype,
                          size_t* codes_bytes, size_t* total) {
     if (!m) PT_FAIL(PT_ERR_INVALID_ARG, "null argument");
     if (num_pages < 1) PT_FAIL(PT_ERR_INVALID_ARG, "num_pages must be >= 1");
     if (page_size < 8 || page_size > 64 || page_size % 8) PT_FAIL(PT_ERR_INVALID_ARG, "page_size must be a multiple of 8 in [8, 64]");
-    if (kv_dtype != PT_KV_MODEL && kv_dtype != PT_KV_E4M3) PT_FAIL(PT_ERR_INVALID_ARG, "kv_dtype must be PT_KV_MODEL or PT_KV_E4M3");
+    if (!kv_dtype_known(kv_dtype)) PT_FAIL(PT_ERR_INVALID_ARG, "kv_dtype must be PT_KV_MODEL, PT_KV_E4M3 or PT_KV_E2M1");
     const size_t vecs = (size_t)m->cfg.T * m->cfg.L * num_pages * 2 * m->cfg.kv_heads * page_size;
     if (kv_dtype == PT_KV_E4M3) {
         if (!m->tc) PT_FAIL(PT_ERR_UNSUPPORTED, "an E4M3 cache needs a bf16 model on the tensor-core path");
         if (m->dh != 128 || page_size % 16) PT_FAIL(PT_ERR_UNSUPPORTED, "an E4M3 cache needs head_dim 128 and pages of a multiple of 16 tokens");
         *codes_bytes = align_up(vecs * m->dh, 256);
         *total = *codes_bytes + vecs * 4;
+    } else if (kv_dtype == PT_KV_E2M1) {
+        if (!m->tc) PT_FAIL(PT_ERR_UNSUPPORTED, "an E2M1 cache needs a bf16 model on the tensor-core path");
+        if (!kv4_supported(m->dh, page_size)) PT_FAIL(PT_ERR_UNSUPPORTED, "an E2M1 cache needs head_dim 64 or 128 and pages of a multiple of 16 tokens");
+        *codes_bytes = *total = vecs / 32 * kv4_block(m->dh);      // a block has 16 tokens' K and V
     } else {
         *codes_bytes = vecs * m->dh * m->esz;
         *total = *codes_bytes;
@@ -364,9 +373,9 @@ pt_status pt_kv_cache_alloc_ex(const pt_model* m, int32_t num_pages, int32_t pag
     if (!c) PT_FAIL(PT_ERR_INVALID_ARG, "out of host memory");
     c->m = m; c->num_pages = num_pages; c->ps = page_size; c->pool = (char*)dev_pool; c->bytes = bytes;
     c->kv_dtype = kv_dtype;
-    c->esz = kv_dtype == PT_KV_E4M3 ? 1 : m->esz;
+    c->esz = c->coded() ? 1 : m->esz;
     c->scales = kv_dtype == PT_KV_E4M3 ? (float*)((char*)dev_pool + codes) : nullptr;
-    c->page_elems = (int64_t)2 * m->cfg.kv_heads * page_size * m->dh;
+    c->page_elems = kv_dtype == PT_KV_E2M1 ? (int64_t)m->cfg.kv_heads * (page_size / 16) * kv4_block(m->dh) : (int64_t)2 * m->cfg.kv_heads * page_size * m->dh;
     c->slab_elems = c->page_elems * num_pages;
     for (int i = 0; i < num_pages; ++i) c->free_list.push_back(i);
     c->ref.assign(num_pages, 0);
@@ -435,8 +444,12 @@ pt_status pt_kv_block_table(const pt_kv_cache* c, int32_t seq, int32_t* pages, i
     return PT_OK;
 }
 
-// Offset, inside one (track, layer) slab, of the head_dim values of (page, kv, head, slot).
+// Offset, inside one (track, layer) slab, of the head_dim values of (page, kv, head, slot); E2M1: of the 16 tokens' codes.
 static inline int64_t slab_offset(const pt_kv_cache* c, int32_t page, int kv, int head, int slot) {
+    if (c->kv_dtype == PT_KV_E2M1) {
+        const int dh = c->m->dh;
+        return (((int64_t)page * c->m->cfg.kv_heads + head) * (c->ps / 16) + slot / 16) * kv4_block(dh) + kv * (kv4_codes(dh) + kv4_scales(dh));
+    }
     return (((int64_t)page * 2 + kv) * c->m->cfg.kv_heads + head) * c->ps * c->m->dh + (int64_t)slot * c->m->dh;
 }
 
@@ -457,11 +470,11 @@ pt_status pt_kv_slot(const pt_kv_cache* c, int32_t track, int32_t layer, int32_t
 pt_status pt_kv_scale_slot(const pt_kv_cache* c, int32_t track, int32_t layer, int32_t seq, int32_t pos,
                            int32_t kv, int32_t kv_head, int64_t* byte_offset) {
     if (!c || !byte_offset) PT_FAIL(PT_ERR_INVALID_ARG, "null argument");
-    if (c->kv_dtype != PT_KV_E4M3) PT_FAIL(PT_ERR_STATE, "the cache holds no scales");
+    if (!c->coded()) PT_FAIL(PT_ERR_STATE, "the cache holds no scales");
     int64_t elem = 0;
     pt_status s = pt_kv_slot(c, track, layer, seq, pos, kv, kv_head, &elem);
     if (s != PT_OK) return s;
-    *byte_offset = ((char*)c->scales - c->pool) + (elem / c->m->dh) * 4;
+    *byte_offset = c->kv_dtype == PT_KV_E2M1 ? elem + kv4_codes(c->m->dh) : ((char*)c->scales - c->pool) + (elem / c->m->dh) * 4;
     return PT_OK;
 }
 
@@ -478,11 +491,10 @@ pt_status pt_workspace_bytes_ex(const pt_model* m, int64_t max_tokens, int32_t m
                                 int32_t kv_dtype, int64_t max_context, size_t* bytes) {
     if (!m || !bytes) PT_FAIL(PT_ERR_INVALID_ARG, "null argument");
     if (max_tokens < 1 || max_batch < 1 || max_batch > max_tokens || page_size < 8 || max_context < 0) PT_FAIL(PT_ERR_INVALID_ARG, "bad sizes");
-    if (kv_dtype != PT_KV_MODEL && kv_dtype != PT_KV_E4M3) PT_FAIL(PT_ERR_INVALID_ARG, "kv_dtype must be PT_KV_MODEL or PT_KV_E4M3");
+    if (!kv_dtype_known(kv_dtype)) PT_FAIL(PT_ERR_INVALID_ARG, "kv_dtype must be PT_KV_MODEL, PT_KV_E4M3 or PT_KV_E2M1");
     int maxp = (m->cfg.max_pos + page_size - 1) / page_size;
-    const bool fp8 = kv_dtype == PT_KV_E4M3;
-    const int64_t ctx = fp8 ? std::max<int64_t>(max_context, max_tokens + 16 * (int64_t)max_batch) : 0;
-    *bytes = carve(m, max_tokens, max_batch, maxp, fp8, ctx, false, nullptr, nullptr);
+    const int64_t ctx = kv_dtype != PT_KV_MODEL ? std::max<int64_t>(max_context, max_tokens + 16 * (int64_t)max_batch) : 0;
+    *bytes = carve(m, max_tokens, max_batch, maxp, kv_dtype, ctx, false, nullptr, nullptr);
     return PT_OK;
 }
 
@@ -491,9 +503,8 @@ pt_status pt_extend_workspace_bytes(const pt_model* m, int64_t max_tokens, int32
     pt_status s = pt_workspace_bytes_ex(m, max_tokens, max_batch, page_size, kv_dtype, max_context, bytes);   // checks the arguments
     if (s != PT_OK) return s;
     const int maxp = (m->cfg.max_pos + page_size - 1) / page_size;
-    const bool fp8 = kv_dtype == PT_KV_E4M3;
-    const int64_t ctx = fp8 ? std::max<int64_t>(max_context, max_tokens + 16 * (int64_t)max_batch) : 0;
-    *bytes = carve(m, max_tokens, max_batch, maxp, fp8, ctx, true, nullptr, nullptr);
+    const int64_t ctx = kv_dtype != PT_KV_MODEL ? std::max<int64_t>(max_context, max_tokens + 16 * (int64_t)max_batch) : 0;
+    *bytes = carve(m, max_tokens, max_batch, maxp, kv_dtype, ctx, true, nullptr, nullptr);
     return PT_OK;
 }
 
@@ -541,18 +552,27 @@ static pt_status forward(pt_model* m, pt_kv_cache* c, const void* x, int64_t x_s
     pages_needed += cow.pages_needed;
     if (pages_needed > c->free_list.size()) PT_FAIL(PT_ERR_CACHE_FULL, "call needs %zu new pages, %zu free", pages_needed, c->free_list.size());
     int maxp = (maxlen + c->ps - 1) / c->ps;
-    const bool fp8 = c->kv_dtype == PT_KV_E4M3;
-    if (fp8 && !m->tc) PT_FAIL(PT_ERR_UNSUPPORTED, "an E4M3 cache needs the tensor-core path");
-    // E4M3 cache, prefill: the attention kernel reads a bf16 copy of code * scale of every key of the call's sequences
+    const bool coded = c->coded(), four = c->kv_dtype == PT_KV_E2M1;
+    if (coded && !m->tc) PT_FAIL(PT_ERR_UNSUPPORTED, "an E4M3 or E2M1 cache needs the tensor-core path");
+    bool direct = four && decode;
+    if (four && !decode) {
+        std::vector<int32_t> lens(B);
+        for (int b = 0; b < B; ++b) {
+            auto it = c->seqs.find(seq_ids[b]);
+            lens[b] = (it == c->seqs.end() ? 0 : it->second.len) + adds[b];
+        }
+        direct = kv4_direct(lens.data(), adds.data(), B, m->G);
+    }
+    // E4M3 or E2M1 cache, prefill: the attention kernel reads a bf16 copy of code * scale of every key of the call's sequences
     int64_t ctx_keys = 0;
-    if (fp8 && !decode)
+    if (coded && !decode && !direct)
         for (int b = 0; b < B; ++b) {
             auto it = c->seqs.find(seq_ids[b]);
             int len = it == c->seqs.end() ? 0 : it->second.len;
             ctx_keys += ((int64_t)len + news(b) + 15) / 16 * 16;
         }
     Call k{};
-    size_t need_ws = carve(m, M, B, maxp, fp8, ctx_keys, ragged, (char*)workspace, &k.w);
+    size_t need_ws = carve(m, M, B, maxp, c->kv_dtype, ctx_keys, ragged, (char*)workspace, &k.w);
     if (ws_bytes < need_ws) PT_FAIL(PT_ERR_BUFFER_TOO_SMALL, "workspace: %zu < %zu bytes", ws_bytes, need_ws);
     if (!cow.entries.empty()) {
         pt_status s = launch_copy_pages(c, c->pool, c->scales, c->num_pages, c->pool, c->scales, c->num_pages, cow.src.data(), cow.dst.data(),
@@ -567,7 +587,7 @@ static pt_status forward(pt_model* m, pt_kv_cache* c, const void* x, int64_t x_s
         if (s != PT_OK) return s;
     }
     // per-call metadata, one upload
-    size_t mb = meta_bytes(M, B, maxp, fp8, ragged);
+    size_t mb = meta_bytes(M, B, maxp, c->kv_dtype, ragged);
     m->meta_host.assign(mb, 0);
     char* hb = m->meta_host.data();
     char* db = (char*)workspace;
@@ -593,13 +613,13 @@ static pt_status forward(pt_model* m, pt_kv_cache* c, const void* x, int64_t x_s
             int pos = s.len + t;
             h_pos[r] = pos;
             h_b[r] = b;
-            h_kvoff[r] = slab_offset(c, s.pages[pos / c->ps], 0, 0, pos % c->ps);
+            h_kvoff[r] = four ? (int64_t)s.pages[pos / c->ps] * c->ps + pos % c->ps : slab_offset(c, s.pages[pos / c->ps], 0, 0, pos % c->ps);
         }
     }
     size_t o_stageoff = 0, o_attnoff = 0, o_start = 0, o_btattn = 0;
     const int maxp_attn = (maxlen + 15) / 16;
     int max_start = 0;
-    if (fp8) {
+    if (coded) {
         o_stageoff = sect((size_t)M * 8); o_attnoff = sect((size_t)M * 8); o_start = sect((size_t)B * 4);
         o_btattn = sect((size_t)B * maxp_attn * 4);
         int64_t* h_stage = (int64_t*)(hb + o_stageoff);
@@ -623,10 +643,10 @@ static pt_status forward(pt_model* m, pt_kv_cache* c, const void* x, int64_t x_s
             base += np;
         }
     }
-    const size_t o_qlen = ragged ? sect((size_t)B * 4) : 0;
-    if (ragged) std::memcpy(hb + o_qlen, n_tok, (size_t)B * 4);
+    const size_t o_qlen = ragged || four ? sect((size_t)B * 4) : 0;
+    if (ragged || four) std::memcpy(hb + o_qlen, adds.data(), (size_t)B * 4);
     int n_items = 0, max_splits = 1;
-    if (decode) plan_decode_splits(h_len, B, c->ps, (int64_t)g.T * g.kv_heads, h_items, h_nsp, &n_items, &max_splits);
+    if (decode && !four) plan_decode_splits(h_len, B, c->ps, (int64_t)g.T * g.kv_heads, h_items, h_nsp, &n_items, &max_splits);
     cudaStream_t st = (cudaStream_t)stream;
     PT_CUDA(cudaMemcpyAsync(db, hb, mb, cudaMemcpyHostToDevice, st));
     k.w.meta.row_kvoff = (const int64_t*)(db + o_kvoff);
@@ -635,7 +655,7 @@ static pt_status forward(pt_model* m, pt_kv_cache* c, const void* x, int64_t x_s
     k.w.meta.kvlen = (const int32_t*)(db + o_len);
     k.w.meta.bt = (const int32_t*)(db + o_bt);
     k.w.meta.maxp = maxp;
-    if (fp8) {
+    if (coded) {
         k.w.meta.row_stageoff = (const int64_t*)(db + o_stageoff);
         k.w.meta.row_attnoff = (const int64_t*)(db + o_attnoff);
         k.w.meta.ctx_start = (const int32_t*)(db + o_start);
@@ -644,8 +664,8 @@ static pt_status forward(pt_model* m, pt_kv_cache* c, const void* x, int64_t x_s
         k.w.meta.attn_pages = (int32_t)(ctx_keys / 16);
         k.w.meta.max_start = max_start;
     }
-    k.ragged = ragged;
-    k.w.meta.qlen = ragged ? (const int32_t*)(db + o_qlen) : nullptr;
+    k.ragged = ragged; k.direct = direct;
+    k.w.meta.qlen = ragged || four ? (const int32_t*)(db + o_qlen) : nullptr;
     k.m = m; k.c = c; k.B = B; k.S = S; k.M = (int)M; k.x = x; k.x_stride = x_stride;
     k.out = (float*)out_h; k.st = st; k.decode = decode;
     k.n_items = n_items; k.max_splits = max_splits;

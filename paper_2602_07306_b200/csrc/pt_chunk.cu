@@ -103,7 +103,7 @@ pt_status launch_chunk_attn_call(Call& k, const __nv_bfloat16* q, const __nv_bfl
     p.T = g.T; p.B = k.B; p.M = k.M; p.nq = g.heads; p.nkv = g.kv_heads;
     p.scale_log2 = 1.4426950408889634f / sqrtf((float)m->dh);
     p.status = m->status();
-    if (k.c->kv_dtype == PT_KV_E4M3) {      // over the bf16 copy of code * scale, as a prefill
+    if (k.c->coded()) {                     // over the bf16 copy of code * scale, as a prefill
         p.pool_l = (const __nv_bfloat16*)k.w.attn_kv; p.pool_tstride = (int64_t)k.w.meta.attn_pages * 2 * m->KVD * 16;
         p.bt = k.w.meta.bt_attn; p.maxp = k.w.meta.maxp_attn; p.ps = 16; p.num_pages = k.w.meta.attn_pages;
     } else {

@@ -103,12 +103,13 @@ struct pt_kv_cache {
     const pt_model* m;
     int32_t num_pages, ps;
     int32_t kv_dtype;                     // pt_kv_dtype
-    size_t esz;                           // bytes per cached element: the model's, or 1 for E4M3 codes
+    size_t esz;                           // bytes per cached element: the model's, 1 for E4M3 codes; E2M1: 1, its sizes below are bytes
     char* pool;
     float* scales;                        // E4M3: [T][L][page][K|V][kv_head][slot] behind the codes; else null
     size_t bytes;
     int64_t page_elems;                   // 2 * nkv * ps * dh
     int64_t slab_elems;                   // num_pages * page_elems : one (track, layer)
+    bool coded() const { return kv_dtype != PT_KV_MODEL; }   // K and V pass through the bf16 staging area
     int64_t slab_vecs() const { return slab_elems / m->dh; }   // cached vectors (= scales) of one (track, layer)
     std::deque<int32_t> free_list;
     std::vector<int32_t> ref;             // sequences that own each page (0: on the free list)
@@ -119,19 +120,19 @@ namespace pt {
 
 // Per-call device metadata (lives at the head of the workspace).
 struct Meta {
-    const int64_t* row_kvoff;   // [M] element offset, inside a (track, layer) slab, of K head 0 of the row's slot
+    const int64_t* row_kvoff;   // [M] element offset, inside a (track, layer) slab, of K head 0 of the row's slot; E2M1: page * ps + slot
     const int32_t* row_pos;     // [M] absolute position of the row's token
     const int32_t* row_b;       // [M] batch row
     const int32_t* kvlen;       // [B] cached length including this call's tokens
     const int32_t* bt;          // [B][maxp] block table rows
     int32_t maxp;
-    // E4M3 caches only
+    // E4M3 and E2M1 caches only
     const int64_t* row_stageoff;  // [M] row * head_dim: where the QKV epilogue puts the row's K head 0 in the staging area
     const int64_t* row_attnoff;   // [M] prefill: offset of the row's slot (K head 0) inside a track's slab of the attention copy
     const int32_t* bt_attn;       // [B][maxp_attn] 16-token pages of the attention copy
     const int32_t* ctx_start;     // [B] keys cached before the call (prefill)
     int32_t maxp_attn, attn_pages, max_start;
-    const int32_t* qlen;          // [B] ragged calls: new tokens per sequence
+    const int32_t* qlen;          // [B] ragged calls, and prefill calls on an E2M1 cache: new tokens per sequence
 };
 
 // PT-MoE with permuted tokens: R = moe_rows() rows per track, every (token, chosen expert) one row, experts in runs of
@@ -158,11 +159,12 @@ struct Work {
     void* z;        // [T][M][F]
     float* ssq;     // [T][M][H/kSsqTile] partial sums of squares (tc)
     float* part;    // decode split-KV partials
-    void* kv_stage; // E4M3 caches: [T][K|V][kv_head][M][dh] bf16, this call's K and V as projected
+    void* kv_stage; // E4M3 and E2M1 caches: [T][K|V][kv_head][M][dh] bf16, this call's K and V as projected
     MoeWork moe;    // PT-MoE, permuted-token path (prefill calls of 512 rows or more)
     float* gates;   // PT-MoE: [T][M][E] routing weights of the current layer (0 for the experts a token did not choose)
     void* chunk;    // ragged calls: scratch of the chunk attention
-    void* attn_kv;  // E4M3 caches, prefill: [T][page][K|V][kv_head][16][dh] bf16 copy of code * scale of every key attended to
+    void* attn4;    // E2M1 caches: scratch of the attention from the codes
+    void* attn_kv;  // E4M3 and E2M1 caches, prefill: [T][page][K|V][kv_head][16][dh] bf16 copy of code * scale of every key attended to
     size_t total;
 };
 
@@ -176,6 +178,7 @@ struct Call {
     Work w;
     cudaStream_t st;
     bool decode;
+    bool direct;              // E2M1 caches: attention straight from the codes, without the bf16 copy
     bool ragged;              // S differs between sequences: rows are packed, meta.qlen holds the counts (S is unused)
     // decode split plan (host): items of (b, first key, key count)
     int n_items, max_splits;

@@ -217,6 +217,56 @@ pt_status launch_kv4_read(const Kv4ReadP& p, int dh, cudaStream_t st) {
     return PT_OK;
 }
 
+static Kv4Slab slab_of(const Call& k, int layer) {
+    const pt_kv_cache* c = k.c;
+    const pt_config& g = k.m->cfg;
+    return {c->pool + (size_t)layer * c->slab_elems, (int64_t)g.L * c->slab_elems, g.kv_heads, c->ps, c->num_pages};
+}
+
+pt_status launch_kv4_write_call(Call& k, int layer) {
+    const pt_model* m = k.m;
+    const pt_config& g = m->cfg;
+    Kv4WriteP p{};
+    p.k = (const __nv_bfloat16*)k.w.kv_stage; p.v = p.k + (int64_t)m->KVD * k.M;      // [T][K|V][kv_head][M][dh]
+    p.tstride = (int64_t)2 * m->KVD * k.M; p.head_stride = (int64_t)k.M * m->dh; p.row_stride = m->dh;
+    p.slab = slab_of(k, layer);
+    p.slots = k.w.meta.row_kvoff; p.T = g.T; p.M = k.M; p.status = m->status();
+    return launch_kv4_write(p, m->dh, k.st);
+}
+
+pt_status launch_kv4_read_call(Call& k, int layer) {
+    const pt_model* m = k.m;
+    Kv4ReadP p{};
+    p.slab = slab_of(k, layer);
+    p.bt = k.w.meta.bt; p.maxp = k.w.meta.maxp; p.kvlen = k.w.meta.kvlen;
+    p.out_l = (__nv_bfloat16*)k.w.attn_kv; p.out_tstride = (int64_t)k.w.meta.attn_pages * 2 * m->KVD * 16;
+    p.obt = k.w.meta.bt_attn; p.omaxp = k.w.meta.maxp_attn; p.ops = 16; p.opages = k.w.meta.attn_pages;
+    p.T = m->cfg.T; p.B = k.B; p.status = m->status();
+    return launch_kv4_read(p, m->dh, k.st);
+}
+
+pt_status launch_kv4_attn_call(Call& k, const __nv_bfloat16* q, int layer, __nv_bfloat16* o) {
+    const pt_model* m = k.m;
+    Kv4AttnP p{};
+    p.q = q; p.o = o; p.slab = slab_of(k, layer);
+    p.bt = k.w.meta.bt; p.maxp = k.w.meta.maxp; p.qlen = k.decode ? nullptr : k.w.meta.qlen; p.kvlen = k.w.meta.kvlen;
+    p.T = m->cfg.T; p.B = k.B; p.M = k.M; p.nq = m->cfg.heads;
+    p.scale_log2 = 1.4426950408889634f / sqrtf((float)m->dh);
+    p.status = m->status();
+    return launch_kv4_attn(p, m->dh, k.w.attn4, k.st);
+}
+
+// The attention from the codes reads a sequence's keys once for every 24 (token, head) rows; the other way writes the bf16 copy
+// and reads it, at the cost of about three such passes.
+bool kv4_direct(const int32_t* lens, const int32_t* n_new, int B, int G) {
+    double passes = 0, once = 0;
+    for (int b = 0; b < B; ++b) {
+        passes += (double)lens[b] * (((int64_t)n_new[b] * G + 23) / 24);
+        once += lens[b];
+    }
+    return passes <= 3 * once;
+}
+
 }  // namespace pt
 
 #include "pt_kernels.h"

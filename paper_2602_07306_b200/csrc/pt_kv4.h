@@ -51,4 +51,12 @@ struct Kv4AttnP {
 size_t kv4_attn_scratch_bytes(int dh);
 pt_status launch_kv4_attn(const Kv4AttnP& p, int dh, void* scratch, cudaStream_t st);
 
+
+// one layer of a forward call on an E2M1 cache
+pt_status launch_kv4_write_call(Call& k, int layer);
+pt_status launch_kv4_read_call(Call& k, int layer);               // all of the call's keys into the bf16 copy
+pt_status launch_kv4_attn_call(Call& k, const __nv_bfloat16* q, int layer, __nv_bfloat16* o);
+// whether a call with n_new[b] new tokens on sequences that then have lens[b] keys attends straight to the codes
+bool kv4_direct(const int32_t* lens, const int32_t* n_new, int B, int G);
+
 }  // namespace pt

@@ -483,7 +483,7 @@ pt_status launch_kv_dequant_ctx(Call& k, int layer) {
     return PT_OK;
 }
 
-// Prefill attention of a call on an E4M3 cache: the tensor-memory kernel over the bf16 copy of code * scale.
+// Prefill attention of a call on an E4M3 or E2M1 cache: the tensor-memory kernel over the bf16 copy of code * scale.
 pt_status launch_flash_prefill_e4m3(Call& k, const __nv_bfloat16* q, __nv_bfloat16* o) {
     const pt_model* m = k.m;
     const pt_config& g = m->cfg;

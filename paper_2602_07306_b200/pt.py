@@ -20,7 +20,7 @@ STATUS = {0: "PT_OK", 1: "PT_ERR_INVALID_ARG", 2: "PT_ERR_BAD_CONFIG", 3: "PT_ER
           4: "PT_ERR_BUFFER_TOO_SMALL", 5: "PT_ERR_CACHE_FULL", 6: "PT_ERR_MISALIGNED", 7: "PT_ERR_CUDA",
           8: "PT_ERR_DEVICE_BOUNDS", 9: "PT_ERR_DEVICE_TIMEOUT", 10: "PT_ERR_STATE"}
 PT_F32, PT_BF16 = 0, 1
-PT_KV_MODEL, PT_KV_E4M3 = 0, 1
+PT_KV_MODEL, PT_KV_E4M3, PT_KV_E2M1 = 0, 1, 2
 KIND = {"wq": 0, "wk": 1, "wv": 2, "wo": 3, "wg": 4, "wu": 5, "wd": 6, "g1": 7, "g2": 8, "wr": 9}
 
 
@@ -280,11 +280,12 @@ class Model:
         return lib().pt_sync_count(self.h)
 
     def new_cache(self, num_pages: int, page_size: int = 16, free_order=None, kv_dtype: str = "model") -> "Cache":
-        """kv_dtype "model" keeps K and V in the model dtype, "e4m3" stores 8-bit codes and one scale per vector."""
+        """kv_dtype "model" keeps K and V in the model dtype, "e4m3" stores 8-bit codes and one scale per vector, "e2m1" 4-bit
+        codes and one scale for 32 values (PT_KV_E2M1 in include/pt.h)."""
         return Cache(self, num_pages, page_size, free_order, kv_dtype=kv_dtype)
 
     def workspace(self, tokens: int, batch: int, page_size: int, kv_dtype: int = PT_KV_MODEL, context: int = 0):
-        """Workspace for calls of up to `tokens` tokens / `batch` sequences; with an E4M3 cache `context` bounds the
+        """Workspace for calls of up to `tokens` tokens / `batch` sequences; with an E4M3 or E2M1 cache `context` bounds the
         keys a prefill call attends to (sum over its sequences of the length after the call, each rounded up to 16)."""
         key = self.ws_key + (0, 0) if len(self.ws_key) == 3 else self.ws_key
         if (self.ws is None or tokens > key[0] or batch > key[1] or page_size < key[2] or kv_dtype > key[3] or context > key[4]):
@@ -321,7 +322,7 @@ class Model:
         ids, pids = _i32arr(seq_ids)
         assert len(ids) == B
         ctx = 0
-        if cache.kv_dtype == PT_KV_E4M3:
+        if cache.kv_dtype != PT_KV_MODEL:
             ctx = sum((cache.length(int(s)) + S + 15) // 16 * 16 for s in ids)
         ws = self.workspace(B * S, B, cache.page_size, cache.kv_dtype, ctx)
         with torch.cuda.device(self.device):
@@ -344,7 +345,7 @@ class Model:
             out = torch.empty((M, H), dtype=torch.float32, device=self.device)
         assert out.is_cuda and out.dtype == torch.float32 and out.is_contiguous() and out.numel() == M * H
         ctx = 0
-        if cache.kv_dtype == PT_KV_E4M3:
+        if cache.kv_dtype != PT_KV_MODEL:
             ctx = sum((cache.length(int(s)) + int(n) + 15) // 16 * 16 for s, n in zip(ids, cnt))
         key = _grown(self.ext_key, (M, len(ids), cache.page_size, cache.kv_dtype, ctx))
         if self.ext_ws is None or key != self.ext_key:
@@ -478,7 +479,7 @@ class Cache:
     def __init__(self, model: Model, num_pages: int, page_size: int = 16, free_order=None, fill=None, kv_dtype: str = "model"):
         torch = model.torch
         self.model, self.num_pages, self.page_size = model, num_pages, page_size
-        self.kv_dtype = {"model": PT_KV_MODEL, "e4m3": PT_KV_E4M3}[kv_dtype]
+        self.kv_dtype = {"model": PT_KV_MODEL, "e4m3": PT_KV_E4M3, "e2m1": PT_KV_E2M1}[kv_dtype]
         n = _SZ()
         check(lib().pt_kv_cache_bytes_ex(model.h, num_pages, page_size, self.kv_dtype, C.byref(n)))
         self.bytes = n.value
@@ -490,8 +491,13 @@ class Cache:
             check(lib().pt_kv_set_free_list(self.h, p, len(a)))
 
     def _new_pool(self, num_pages: int, nbytes: int):
-        """(pool, codes, scales) of a pool in the cache's format; codes and scales are None in the model dtype."""
+        """(pool, codes, scales) of a pool in the cache's format; codes and scales are None in the model dtype.  E2M1: codes
+        has the blocks [T, L, pages, kv_heads, page / 16, bytes], scales is None."""
         model, torch = self.model, self.model.torch
+        if self.kv_dtype == PT_KV_E2M1:
+            c = model.cfg
+            pool = torch.empty(nbytes, dtype=torch.uint8, device=model.device)
+            return pool, pool.view(c.T, c.L, num_pages, c.kv_heads, self.page_size // 16, 17 * (c.hidden // c.heads)), None
         if self.kv_dtype != PT_KV_E4M3:
             return torch.empty(nbytes // (2 if model.dtype == "bf16" else 4), dtype=model.tdtype, device=model.device), None, None
         # one byte buffer: the codes, then the fp32 scales (views)
@@ -570,16 +576,24 @@ class Cache:
         return v.value
 
     def scale_slot(self, t: int, l: int, seq: int, pos: int, kv: int, head: int) -> int:
-        """E4M3 caches: byte offset inside the pool of the fp32 scale of the vector `slot` addresses."""
+        """E4M3 caches: byte offset inside the pool of the fp32 scale of the vector `slot` addresses (E2M1: of the scales of its
+        16 tokens)."""
         v = _I64()
         check(lib().pt_kv_scale_slot(self.h, t, l, seq, pos, kv, head, C.byref(v)))
         return v.value
 
     def dequantized(self):
-        """E4M3 caches: code * scale of the whole pool as a float32 CUDA tensor [T, L, pages, 2, kv_heads, page, dh]."""
+        """E4M3 and E2M1 caches: code * scale of the whole pool as a float32 CUDA tensor [T, L, pages, 2, kv_heads, page, dh]."""
         torch = self.model.torch
         c = self.model.cfg
         dh = c.hidden // c.heads
+        if self.kv_dtype == PT_KV_E2M1:
+            dev = dict(dtype=torch.int32, device=self.model.device)
+            pages = torch.arange(self.num_pages, **dev)[:, None]
+            out = torch.empty((c.T * c.L, self.num_pages, 2, c.kv_heads, self.page_size, dh), dtype=torch.bfloat16, device=self.model.device)
+            kernel_kv_read_e2m1(self.codes.flatten(0, 1), pages, torch.full((self.num_pages,), self.page_size, **dev), out, pages,
+                                nkv=c.kv_heads, dh=dh, ps=self.page_size)
+            return out.float().view((c.T, c.L) + out.shape[1:])
         shape = (c.T, c.L, self.num_pages, 2, c.kv_heads, self.page_size)
         codes = self.codes.view(torch.float8_e4m3fn).to(torch.float32).view(shape + (dh,))
         return codes * self.scales.view(shape + (1,))

@@ -139,3 +139,40 @@ def test_the_binding_checks_shapes_types_and_devices(monkeypatch):
             with pytest.raises((ValueError, RuntimeError)):
                 fn(**(good | kw), **shape)
         assert len(launched) == before + 1
+
+
+def test_cache_layout_and_offsets(lib):
+    cfg = pt.pt_config(2, 2, 4, 512, 4, 2, 352, 10000.0, 1e-6, pt.PT_BF16, 0, 900, 0, 0, 0)
+    h, c = C.c_void_p(), C.c_void_p()
+    assert lib.pt_model_create(C.byref(cfg), C.byref(h)) == 0
+    n, m = C.c_size_t(), C.c_size_t()
+    pages, ps, dh = 7, 32, 128
+    assert lib.pt_kv_cache_bytes_ex(h, pages, ps, pt.PT_KV_E2M1, C.byref(n)) == 0
+    assert n.value == 2 * 4 * pages * 2 * (ps // 16) * kv4.block_bytes(dh)
+    assert lib.pt_kv_cache_bytes_ex(h, pages, 24, pt.PT_KV_E2M1, C.byref(m)) == 3
+    assert lib.pt_kv_cache_bytes_ex(h, pages, ps, 3, C.byref(m)) == 1
+    assert lib.pt_kv_cache_alloc_ex(h, pages, ps, pt.PT_KV_E2M1, FAKE, n.value - 1, C.byref(c)) == 4
+    assert lib.pt_kv_cache_alloc_ex(h, pages, ps, pt.PT_KV_E2M1, FAKE, n.value, C.byref(c)) == 0
+    assert lib.pt_kv_seq_reserve(c, 5, 100) == 0
+    off, sc = C.c_int64(), C.c_int64()
+    blk = kv4.block_bytes(dh)
+    for track, layer, pos, kv, head in ((0, 0, 0, 0, 0), (1, 3, 99, 1, 1), (0, 2, 47, 0, 1), (1, 0, 16, 1, 0)):
+        assert lib.pt_kv_slot(c, track, layer, 5, pos, kv, head, C.byref(off)) == 0
+        assert lib.pt_kv_scale_slot(c, track, layer, 5, pos, kv, head, C.byref(sc)) == 0
+        want = ((((track * 4 + layer) * pages + pos // ps) * 2 + head) * 2 + pos % ps // 16) * blk + kv * blk // 2
+        assert off.value == want and sc.value == want + 8 * dh
+    # workspace: one for this format serves the others
+    sizes = []
+    for d in (pt.PT_KV_MODEL, pt.PT_KV_E4M3, pt.PT_KV_E2M1):
+        assert lib.pt_workspace_bytes_ex(h, 64, 2, 16, d, 500, C.byref(m)) == 0
+        e = C.c_size_t()
+        assert lib.pt_extend_workspace_bytes(h, 64, 2, 16, d, 500, C.byref(e)) == 0
+        sizes.append((m.value, e.value))
+    assert sizes[0] < sizes[1] < sizes[2] and sizes[0][1] < sizes[1][1] < sizes[2][1]
+    lib.pt_kv_cache_free(c)
+    lib.pt_model_destroy(h)
+    for bad in (dict(dtype=pt.PT_F32), dict(flags=1), dict(heads=16, kv=8)):      # fp32, the plain kernels, head_dim 32
+        cfg = pt.pt_config(2, 2, 4, 512, bad.get("heads", 4), bad.get("kv", 2), 352, 10000.0, 1e-6, bad.get("dtype", pt.PT_BF16), 0, 900, bad.get("flags", 0), 0, 0)
+        assert lib.pt_model_create(C.byref(cfg), C.byref(h)) == 0
+        assert lib.pt_kv_cache_bytes_ex(h, pages, ps, pt.PT_KV_E2M1, C.byref(n)) == 3
+        lib.pt_model_destroy(h)
