@@ -1,10 +1,10 @@
 // The 4-bit storage format of the KV cache (pt_kv_dtype PT_KV_E2M1): new tokens' K and V into its pages, and sequences back out.
 //   k_kv4_write   a thread has eight consecutive values of a vector, four threads a group of 32: the group's maximum takes two
-//                 shuffles, its scale is the smallest E5M3 number s with max <= 6 s, and eight codes are one word of K or two
-//                 half words of V
+//                 shuffles
 //   k_kv4_read    a warp has one head's K and V of 16 tokens, in the order in which they lie: 16 bytes a lane and load
 // Both move bytes and compute little.
 #include <algorithm>
+#include <type_traits>
 
 #include "pt_kv4.cuh"
 #include "pt_tc.h"
@@ -19,7 +19,7 @@ constexpr int kThreads = 256;
 // The code of v / s for the group's scale s, given r = 1 / s rounded: ties between codes have to be met exactly.  v has 8
 // significant bits and a tie times s has 7, so v / s is either a tie or at least 2^-8 of it away; v * r is off by 2^-23, and
 // rounding it to 12 bits returns to the tie.
-__device__ __forceinline__ float kv4_quotient(float v, float r) { return __uint_as_float((__float_as_uint(v * r) + 0x800u) & ~0xfffu); }
+__device__ __forceinline__ float kv4_divided(float v, float r) { return __uint_as_float((__float_as_uint(v * r) + 0x800u) & ~0xfffu); }
 __device__ __forceinline__ uint32_t kv4_encode8(const float* y) {
     uint32_t w;
     asm("{\n .reg .b8 a, b, c, d;\n cvt.rn.satfinite.e2m1x2.f32 a, %2, %1;\n cvt.rn.satfinite.e2m1x2.f32 b, %4, %3;\n"
@@ -28,22 +28,8 @@ __device__ __forceinline__ uint32_t kv4_encode8(const float* y) {
     return w;
 }
 
-template <int DH>
-__global__ void __launch_bounds__(kThreads) k_kv4_write(const Kv4WriteP p) {
-    constexpr int PER = DH / 8;                                    // threads of a vector
-    grid_dep_wait();
-    grid_dep_launch();
-    const int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x;
-    const int oct = (int)(i % PER), group = oct >> 2, q = oct & 3;
-    const int64_t vec = i / PER;                                   // (row, head, K|V)
-    const int t = blockIdx.y, nkv = p.slab.nkv;
-    const int64_t heads = (int64_t)2 * nkv;
-    const bool live = vec < p.M * heads;                           // every lane takes part in the shuffles
-    const int64_t row = live ? vec / heads : 0;
-    const int kvh = (int)(vec - row * heads), head = live ? kvh % nkv : 0;
-    const bool is_v = kvh >= nkv;
-    const __nv_bfloat16* src = (is_v ? p.v : p.k) + (size_t)t * p.tstride + row * p.row_stride + head * p.head_stride + oct * 8;
-    const uint4 raw = live ? *reinterpret_cast<const uint4*>(src) : make_uint4(0, 0, 0, 0);
+// Eight values of a vector: their codes (one word, the lowest value's lowest), and the byte of the group's scale.
+__device__ __forceinline__ uint32_t kv4_encode(const uint4& raw, uint32_t& byte) {
     const uint32_t w[4] = {raw.x, raw.y, raw.z, raw.w};
     // magnitudes as whole numbers: a NaN is above infinity, which is above the rest
     uint32_t top = 0;
@@ -55,137 +41,220 @@ __global__ void __launch_bounds__(kThreads) k_kv4_write(const Kv4WriteP p) {
     const bool bad = top >= 0x7f80u;
     const float amax = bad ? 0.f : __uint_as_float(top << 16);
     // amax / 6 cut to 4 significant bits, or the next number where that is too small (the product is exact)
-    uint32_t byte = (uint32_t)__half_as_ushort(__float2half_rz(fminf(amax * (1.0f / 6.0f), 61440.f))) >> 7;
+    byte = (uint32_t)__half_as_ushort(__float2half_rz(fminf(amax * (1.0f / 6.0f), 61440.f))) >> 7;
     if (byte < 247 && 6.0f * kv4_scale(byte) < amax) ++byte;
     const float s = kv4_scale(byte), r = s > 0.f ? 1.0f / s : 0.f;
     float y[8];
 #pragma unroll
     for (int a = 0; a < 4; ++a) {
-        y[2 * a] = kv4_quotient(__uint_as_float(w[a] << 16), r);
-        y[2 * a + 1] = kv4_quotient(__uint_as_float(w[a] & 0xffff0000u), r);
+        y[2 * a] = kv4_divided(__uint_as_float(w[a] << 16), r);
+        y[2 * a + 1] = kv4_divided(__uint_as_float(w[a] & 0xffff0000u), r);
     }
-    const uint32_t code = bad ? 0u : kv4_encode8(y);
-    if (bad) byte = 255;
-    if (!live) return;
-    __nv_bfloat16* val = is_v ? p.v_out : p.k_out;
-    if (val) {
-        uint32_t h[4];
-        kv4_codes8(code, h);
-        const float sv = kv4_scale(byte);
-        *reinterpret_cast<uint4*>(val + (((size_t)t * p.M + row) * nkv + head) * DH + oct * 8) =
-            make_uint4(kv4_value2(h[0], sv), kv4_value2(h[1], sv), kv4_value2(h[2], sv), kv4_value2(h[3], sv));
+    if (bad) { byte = 255; return 0u; }
+    return kv4_encode8(y);
+}
+
+// A block has 16 rows of one track and head.  Tokens that follow one another lie side by side in a block of the cache, but
+// each in pieces of 8 bytes (V) and 16 (K): the rows' codes meet in shared memory and go out piece by piece in the order of
+// the cache, as if row 0's slot were followed by the others.  Where it is not, the same pieces go to the same places less
+// well together.
+template <int DH>
+__global__ void __launch_bounds__(2 * DH) k_kv4_write(const Kv4WriteP p) {
+    constexpr int PER = DH / 8, THREADS = 2 * DH, NG = DH / 32;    // threads of a vector; 16 vectors
+    constexpr int KP = DH / 8, VP = DH / 16;                       // bytes of a piece
+    __shared__ __align__(16) uint8_t img[2][16][DH / 2];           // K, V: a token's pieces in order
+    __shared__ __align__(16) uint8_t scales[2][16][NG];
+    __shared__ int64_t where[16];                                  // byte of the token's cache block in the track's slab, -1: nowhere
+    __shared__ int slot_in[16];                                    // its slot in that block
+    grid_dep_wait();
+    grid_dep_launch();
+    const int tid = threadIdx.x, r = tid / PER, oct = tid % PER, group = oct >> 2, q = oct & 3;
+    const int head = blockIdx.y, t = blockIdx.z, nkv = p.slab.nkv;
+    const int64_t row = (int64_t)blockIdx.x * 16 + r;
+    const bool live = row < p.M;                                   // every lane takes part in the shuffles
+    uint4 raw[2] = {};
+    if (live) {
+        const size_t at = (size_t)t * p.tstride + row * p.row_stride + head * p.head_stride + oct * 8;
+        raw[0] = *reinterpret_cast<const uint4*>(p.k + at);
+        raw[1] = *reinterpret_cast<const uint4*>(p.v + at);
     }
-    const int64_t slot = p.slots[row];
-    if (slot < 0) return;
-    if (slot >= (int64_t)p.slab.num_pages * p.slab.ps) { report(p.status, PT_ERR_DEVICE_BOUNDS, LOC_KV4_PAGE); return; }
-    const int64_t page = slot / p.slab.ps;
-    const int in = (int)(slot - page * p.slab.ps), sl = in & 15;
-    char* blk = p.slab.pool_l + (size_t)t * p.slab.tstride + ((page * nkv + head) * (p.slab.ps / 16) + in / 16) * kv4_block(DH);
-    if (is_v) {
-        blk += kv4_codes(DH) + kv4_scales(DH);
-        *reinterpret_cast<uint16_t*>(blk + kv4_v_half(DH, sl, group, 2 * q)) = (uint16_t)code;
-        *reinterpret_cast<uint16_t*>(blk + kv4_v_half(DH, sl, group, 2 * q + 1)) = (uint16_t)(code >> 16);
-        if (q == 0) blk[kv4_codes(DH) + kv4_v_scale(DH, sl, group)] = (char)byte;
-    } else {
-        *reinterpret_cast<uint32_t*>(blk + kv4_k_word(DH, sl, group, q)) = code;
-        if (q == 0) blk[kv4_codes(DH) + kv4_k_scale(DH, sl, group)] = (char)byte;
+    if (tid < 16) {
+        const int64_t row_t = (int64_t)blockIdx.x * 16 + tid, slot = row_t < p.M ? p.slots[row_t] : -1;
+        int64_t to = -1;
+        int in = tid;
+        if (slot >= (int64_t)p.slab.num_pages * p.slab.ps) {
+            report(p.status, PT_ERR_DEVICE_BOUNDS, LOC_KV4_PAGE);
+        } else if (slot >= 0) {
+            const int64_t page = slot / p.slab.ps;
+            in = (int)(slot - page * p.slab.ps);
+            to = ((page * nkv + head) * (p.slab.ps / 16) + in / 16) * kv4_block(DH);
+        }
+        where[tid] = to;
+        slot_in[tid] = in & 15;
+    }
+#pragma unroll
+    for (int x = 0; x < 2; ++x) {
+        uint32_t byte;
+        const uint32_t code = kv4_encode(raw[x], byte);
+        __nv_bfloat16* val = x ? p.v_out : p.k_out;
+        if (val && live) {
+            uint32_t h[4];
+            kv4_codes8(code, h);
+            const float s = kv4_scale(byte);
+            *reinterpret_cast<uint4*>(val + (((size_t)t * p.M + row) * nkv + head) * DH + oct * 8) =
+                make_uint4(kv4_value2(h[0], s), kv4_value2(h[1], s), kv4_value2(h[2], s), kv4_value2(h[3], s));
+        }
+        if (x == 0) {
+            *reinterpret_cast<uint32_t*>(&img[0][r][q * KP + group * 4]) = code;
+        } else {
+            *reinterpret_cast<uint16_t*>(&img[1][r][2 * q * VP + group * 2]) = (uint16_t)code;
+            *reinterpret_cast<uint16_t*>(&img[1][r][(2 * q + 1) * VP + group * 2]) = (uint16_t)(code >> 16);
+        }
+        if (q == 0) scales[x][r][group] = (uint8_t)byte;
+    }
+    __syncthreads();
+    char* const slab = p.slab.pool_l + (size_t)t * p.slab.tstride;
+    const int first = slot_in[0];
+    auto row_of = [&](int s) { return (s - first) & 15; };         // the row that has slot s if they follow row 0
+    for (int i = tid; i < 128 + 64 + 16 * NG + 16; i += THREADS) {
+        if (i < 128) {                                             // V codes
+            const int s = DH == 128 ? 4 * (i / 2 % 4) + 2 * (i / 64) + i % 2 : 4 * (i / 4 % 4) + i % 4, g = DH == 128 ? i / 8 % 8 : i / 16;
+            const int w = row_of(s);
+            if (where[w] < 0) continue;
+            char* dst = slab + where[w] + kv4_codes(DH) + kv4_scales(DH) + kv4_v_half(DH, slot_in[w], 0, g);
+            if constexpr (DH == 128) *reinterpret_cast<uint2*>(dst) = *reinterpret_cast<const uint2*>(&img[1][w][g * VP]);
+            else *reinterpret_cast<uint32_t*>(dst) = *reinterpret_cast<const uint32_t*>(&img[1][w][g * VP]);
+        } else if (i < 192) {                                      // K codes
+            const int x = i - 128, at = x / 4, w = row_of(at % 8 * 2 + at / 8);
+            if (where[w] < 0) continue;
+            char* dst = slab + where[w] + kv4_k_word(DH, slot_in[w], 0, x % 4);
+            if constexpr (DH == 128) *reinterpret_cast<uint4*>(dst) = *reinterpret_cast<const uint4*>(&img[0][w][x % 4 * KP]);
+            else *reinterpret_cast<uint2*>(dst) = *reinterpret_cast<const uint2*>(&img[0][w][x % 4 * KP]);
+        } else if (i < 192 + 16 * NG) {                            // V scales, a byte each
+            const int x = i - 192, s = x / (4 * NG) * 4 + x % 4, j = x / 4 % NG, w = row_of(s);
+            if (where[w] < 0) continue;
+            slab[where[w] + 2 * kv4_codes(DH) + kv4_scales(DH) + kv4_v_scale(DH, slot_in[w], j)] = (char)scales[1][w][j];
+        } else {                                                   // K scales, a token's together
+            const int w = row_of(i - 192 - 16 * NG);
+            if (where[w] < 0) continue;
+            char* dst = slab + where[w] + kv4_codes(DH) + kv4_k_scale(DH, slot_in[w], 0);
+            if constexpr (DH == 128) *reinterpret_cast<uint32_t*>(dst) = *reinterpret_cast<const uint32_t*>(scales[0][w]);
+            else *reinterpret_cast<uint16_t*>(dst) = *reinterpret_cast<const uint16_t*>(scales[0][w]);
+        }
     }
 }
 
+template <int N> struct alignas(N * 4) Words { uint32_t w[N]; };
+
+// A warp has a run of units (track, 16-token block of the call, head), heads fastest; it finds the start of its run by itself.
 template <int DH>
-__global__ void __launch_bounds__(kThreads) k_kv4_read(const Kv4ReadP p, const int per) {
+__global__ void __launch_bounds__(kThreads) k_kv4_read(const Kv4ReadP p) {
     constexpr int NG = DH / 32;
-    __shared__ long long pre[kThreads + 1];
+    using Code = std::conditional_t<NG == 4, uint4, uint2>;        // a lane's codes of a token of K
     grid_dep_wait();
     grid_dep_launch();
-    const int lane = threadIdx.x & 31, nkv = p.slab.nkv, ps = p.slab.ps;
+    const int lane = threadIdx.x & 31, nkv = p.slab.nkv, ps = p.slab.ps, g = lane >> 2, q = lane & 3;
+    const int per = (p.B + 31) / 32;
     bool bad = false;
-    kv4_scan(p.B, per, pre, [&](int b) {
-        const int n = p.kvlen[b];
-        if (n < 0 || n > (int64_t)p.maxp * ps || n > (int64_t)p.omaxp * p.ops) { bad = true; return 0; }
-        return (n + 15) >> 4;
-    });
-    if (__syncthreads_or(bad)) { if (bad) report(p.status, PT_ERR_DEVICE_BOUNDS, LOC_KV4_LEN); return; }
-    // units: (track, 16-token block of the call, head), heads fastest; a warp has a run of them
-    const long long blocks = pre[kThreads], units = blocks * nkv * p.T;
+    int mine = 0, n = 0;
+    for (int b = lane * per; b < min(p.B, (lane + 1) * per); ++b) {
+        n = p.kvlen[b];
+        if (n < 0 || n > (int64_t)p.maxp * ps || n > (int64_t)p.omaxp * p.ops) { bad = true; break; }
+        mine += (n + 15) >> 4;
+    }
+    if (__any_sync(0xffffffffu, bad)) { if (bad && blockIdx.x == 0) report(p.status, PT_ERR_DEVICE_BOUNDS, LOC_KV4_LEN); return; }
+    const int up = kv4_scan(mine), blocks = __shfl_sync(0xffffffffu, up, 31);
+    const long long per_track = (long long)blocks * nkv, units = per_track * p.T;
     const long long warps = (long long)gridDim.x * (kThreads / 32), w = (long long)blockIdx.x * (kThreads / 32) + (threadIdx.x >> 5);
-    long long u = units * w / warps;
-    const long long end = units * (w + 1) / warps;
-    if (u >= end) return;
-    int t = (int)(u / (blocks * nkv)), head = (int)(u % nkv);
-    long long blk = u / nkv - (long long)t * blocks;
-    int b = 0, n = 0, at = 0;                              // sequence, its keys, its block
-    auto seek = [&]() {
-        const int i = kv4_find(pre, kThreads, blk);
-        long long rest = blk - pre[i];
-        for (b = i * per;; ++b) {
-            n = p.kvlen[b];
-            const int have = (n + 15) >> 4;
-            if (rest < have) break;
-            rest -= have;
-        }
-        at = (int)rest;
-    };
-    seek();
-    for (; u < end; ++u) {
-        const int page = p.bt[(size_t)b * p.maxp + at * 16 / ps];
-        // lane l < 16: where token l of the block goes (elements from the track's slab, K; -1: nowhere)
-        int64_t to = -1;
+    const long long share = kv4_quotient(units, warps), more = units - share * warps;
+    long long left = share + (w < more);
+    if (left == 0) return;
+    const long long u = share * w + min(w, more);
+    int t = (int)kv4_quotient(u, per_track);
+    const long long in = u - t * per_track;
+    int blk = (int)kv4_quotient(in, nkv), head = (int)(in - (long long)blk * nkv);
+    int b, at;                                                     // sequence, its block
+    {
+        const int l = __popc(__ballot_sync(0xffffffffu, up <= blk));
+        at = blk - __shfl_sync(0xffffffffu, up - mine, l);
+        b = l * per;
+        n = per > 1 ? p.kvlen[b] : __shfl_sync(0xffffffffu, n, l);
+        while (at >= (n + 15) >> 4) { at -= (n + 15) >> 4; n = p.kvlen[++b]; }
+    }
+    // lane l < 16 has where token l of the block goes: elements from the track's slab (head 0, K); -1: nowhere
+    int page;
+    int64_t to;
+    auto look = [&]() {
+        page = p.bt[(size_t)b * p.maxp + at * 16 / ps];
+        to = -1;
         if (lane < 16 && at * 16 + lane < n) {
             const int pos = at * 16 + lane, opage = p.obt[(size_t)b * p.omaxp + pos / p.ops];
-            if (opage < 0 || opage >= p.opages) report(p.status, PT_ERR_DEVICE_BOUNDS, LOC_KV4_PAGE);
-            else to = (((int64_t)opage * 2 * nkv + head) * p.ops + pos % p.ops) * DH;
+            if ((uint32_t)opage >= (uint32_t)p.opages) report(p.status, PT_ERR_DEVICE_BOUNDS, LOC_KV4_PAGE);
+            else to = ((int64_t)opage * 2 * nkv * p.ops + pos % p.ops) * DH;
         }
-        if (page < 0 || page >= p.slab.num_pages) {
+        if ((uint32_t)page >= (uint32_t)p.slab.num_pages) {
             if (lane == 0) report(p.status, PT_ERR_DEVICE_BOUNDS, LOC_KV4_PAGE);
+            page = 0; to = -1;
+        }
+    };
+    look();
+    for (;;) {
+        const char* src = p.slab.pool_l + (size_t)t * p.slab.tstride + (((int64_t)page * nkv + head) * (ps / 16) + at * 16 % ps / 16) * kv4_block(DH);
+        const char* vsrc = src + kv4_codes(DH) + kv4_scales(DH);
+        // K: tokens 2 g and 2 g + 1, V: tokens 4 q .. 4 q + 3; all loads first
+        Words<NG> kc[2];
+        Words<4> vc[NG / 2];                                       // dh 128: of two tokens each; dh 64: of four
+        Words<NG / 2> ks;
+        Words<NG> vs;
+#pragma unroll
+        for (int i = 0; i < 2; ++i) *reinterpret_cast<Code*>(&kc[i]) = __ldcs(reinterpret_cast<const Code*>(src + kv4_k_word(DH, 2 * g + i, 0, q)));
+        if constexpr (NG == 4) {
+            *reinterpret_cast<uint4*>(&vc[0]) = __ldcs(reinterpret_cast<const uint4*>(vsrc + lane * 16));
+            *reinterpret_cast<uint4*>(&vc[1]) = __ldcs(reinterpret_cast<const uint4*>(vsrc + 512 + lane * 16));
+            *reinterpret_cast<uint2*>(&ks) = *reinterpret_cast<const uint2*>(src + kv4_codes(DH) + g * 8);
+            *reinterpret_cast<uint4*>(&vs) = *reinterpret_cast<const uint4*>(vsrc + kv4_codes(DH) + q * 16);
         } else {
-            const char* src = p.slab.pool_l + (size_t)t * p.slab.tstride + (((int64_t)page * nkv + head) * (ps / 16) + at * 16 % ps / 16) * kv4_block(DH);
-            __nv_bfloat16* out = p.out_l + (size_t)t * p.out_tstride;
-            const int64_t v_off = (int64_t)nkv * p.ops * DH;
-            const char* ksc = src + kv4_codes(DH);
-            const char* vcodes = ksc + kv4_scales(DH);
-            const char* vsc = vcodes + kv4_codes(DH);
-            const int g = lane >> 2, q = lane & 3;
+            *reinterpret_cast<uint4*>(&vc[0]) = __ldcs(reinterpret_cast<const uint4*>(vsrc + lane * 16));
+            ks.w[0] = *reinterpret_cast<const uint32_t*>(src + kv4_codes(DH) + g * 4);
+            *reinterpret_cast<uint2*>(&vs) = *reinterpret_cast<const uint2*>(vsrc + kv4_codes(DH) + q * 8);
+        }
+        __nv_bfloat16* out = p.out_l + (size_t)t * p.out_tstride + (size_t)head * p.ops * DH;
+        const int64_t v_off = (int64_t)nkv * p.ops * DH;
 #pragma unroll
-            for (int i = 0; i < 2; ++i) {                  // K: tokens 2 g and 2 g + 1
-                const int tok = 2 * g + i;
-                const int64_t dst = __shfl_sync(0xffffffffu, to, tok);
-                uint32_t c[NG];
-#pragma unroll
-                for (int j = 0; j < NG; ++j) c[j] = *reinterpret_cast<const uint32_t*>(src + kv4_k_word(DH, tok, j, q));
-                if (dst < 0) continue;
+        for (int i = 0; i < 2; ++i) {
+            const int64_t dst = __shfl_sync(0xffffffffu, to, 2 * g + i);
+            if (dst >= 0) {
 #pragma unroll
                 for (int j = 0; j < NG; ++j) {
-                    const float s = kv4_scale((uint8_t)ksc[kv4_k_scale(DH, tok, j)]);
+                    const int x = i * NG + j;
+                    const float s = kv4_scale((ks.w[x / 4] >> (x % 4 * 8)) & 0xffu);
                     uint32_t h[4];
-                    kv4_codes8(c[j], h);
+                    kv4_codes8(kc[i].w[j], h);
                     *reinterpret_cast<uint4*>(out + dst + 32 * j + 8 * q) = make_uint4(kv4_value2(h[0], s), kv4_value2(h[1], s), kv4_value2(h[2], s), kv4_value2(h[3], s));
                 }
             }
+        }
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {                  // V: tokens 4 q .. 4 q + 3
-                const int tok = 4 * q + i;
-                const int64_t dst = __shfl_sync(0xffffffffu, to, tok);
-                uint32_t c[NG / 2];
-#pragma unroll
-                for (int j = 0; j < NG / 2; ++j) c[j] = *reinterpret_cast<const uint32_t*>(vcodes + kv4_v_half(DH, tok, 2 * j, g));
-                if (dst < 0) continue;
+        for (int i = 0; i < 4; ++i) {
+            const int64_t dst = __shfl_sync(0xffffffffu, to, 4 * q + i);
+            if (dst >= 0) {
 #pragma unroll
                 for (int j = 0; j < NG; ++j) {
-                    const float s = kv4_scale((uint8_t)vsc[kv4_v_scale(DH, tok, j)]);
+                    const uint32_t c = NG == 4 ? vc[i / 2 % (NG / 2)].w[i % 2 * 2 + j / 2] : vc[0].w[i];
+                    const float s = kv4_scale((vs.w[j] >> (8 * i)) & 0xffu);
                     uint32_t h[2];
-                    kv4_codes4(j & 1 ? c[j / 2] >> 16 : c[j / 2], h);
+                    kv4_codes4(j & 1 ? c >> 16 : c, h);
                     *reinterpret_cast<uint2*>(out + dst + v_off + 32 * j + 4 * g) = make_uint2(kv4_value2(h[0], s), kv4_value2(h[1], s));
                 }
             }
         }
+        if (--left == 0) break;
         if (++head == nkv) {
             head = 0;
-            ++at; ++blk;
-            if (at * 16 >= n && u + 1 < end) {
-                if (blk == blocks) { blk = 0; ++t; }
-                seek();
-            }
+            ++at;
+            if (++blk == blocks) { blk = 0; ++t; b = -1; at = n = 0; }
+            while (at * 16 >= n) { n = p.kvlen[++b]; at = 0; }
+            look();
         }
     }
 }
@@ -200,18 +269,19 @@ int sm_count() {
 }  // namespace
 
 pt_status launch_kv4_write(const Kv4WriteP& p, int dh, cudaStream_t st) {
-    const int64_t blocks = ((int64_t)p.M * 2 * p.slab.nkv * (dh / 8) + kThreads - 1) / kThreads;
-    if (blocks > 0x7fffffff || p.T > 65535) { set_error("too many rows or tracks for one call"); return PT_ERR_UNSUPPORTED; }
-    const cudaError_t e = launch_dependent(dh == 64 ? k_kv4_write<64> : k_kv4_write<128>, dim3((unsigned)blocks, p.T), dim3(kThreads), (size_t)0, st, p);
+    if (p.T > 65535) { set_error("too many tracks for one call"); return PT_ERR_UNSUPPORTED; }
+    const cudaError_t e = launch_dependent(dh == 64 ? k_kv4_write<64> : k_kv4_write<128>, dim3((p.M + 15) / 16, p.slab.nkv, p.T), dim3(2 * dh), (size_t)0, st, p);
     if (e != cudaSuccess) { set_error("k_kv4_write launch: %s", cudaGetErrorString(e)); return PT_ERR_CUDA; }
     g_launches.fetch_add(1, std::memory_order_relaxed);
     return PT_OK;
 }
 
 pt_status launch_kv4_read(const Kv4ReadP& p, int dh, cudaStream_t st) {
-    const int64_t most = ((int64_t)p.T * p.B * (((int64_t)p.maxp * p.slab.ps + 15) / 16) * p.slab.nkv + kThreads / 32 - 1) / (kThreads / 32);
-    const int blocks = (int)std::min<int64_t>(most, (int64_t)sm_count() * 8);
-    const cudaError_t e = launch_dependent(dh == 64 ? k_kv4_read<64> : k_kv4_read<128>, dim3(blocks), dim3(kThreads), (size_t)0, st, p, (p.B + kThreads - 1) / kThreads);
+    const double blocks_most = (double)p.B * ((double)p.maxp * p.slab.ps / 16 + 1);      // of one track: counted in 32 bits
+    if (blocks_most > 2e9) { set_error("too many sequences or pages for one call"); return PT_ERR_UNSUPPORTED; }
+    const double warps = std::min(blocks_most * p.T * p.slab.nkv, (double)sm_count() * 64);
+    const int blocks = ((int)warps + kThreads / 32 - 1) / (kThreads / 32);
+    const cudaError_t e = launch_dependent(dh == 64 ? k_kv4_read<64> : k_kv4_read<128>, dim3(blocks), dim3(kThreads), (size_t)0, st, p);
     if (e != cudaSuccess) { set_error("k_kv4_read launch: %s", cudaGetErrorString(e)); return PT_ERR_CUDA; }
     g_launches.fetch_add(1, std::memory_order_relaxed);
     return PT_OK;

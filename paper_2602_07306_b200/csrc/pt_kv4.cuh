@@ -34,36 +34,18 @@ __device__ __forceinline__ uint32_t kv4_value2(uint32_t h, float s) {
     return kv4_bf16(f.x * s, f.y * s);
 }
 
-// Running sums of a count per sequence over a whole block: thread i has those of sequences i * per .. (i + 1) * per - 1.
-// after the call: pre[i] = the counts of the sequences before thread i's, pre[blockDim.x] = all of them
-template <typename F>
-__device__ __forceinline__ void kv4_scan(int B, int per, long long* pre, F count) {
-    const int tid = threadIdx.x, n = blockDim.x, lane = tid & 31, warp = tid >> 5;
-    __shared__ long long sums[32];
-    long long mine = 0;
-    for (int b = tid * per; b < min(B, (tid + 1) * per); ++b) mine += count(b);
-    long long up = mine;
+// Running sums over the lanes of a warp, the lane's own included.
+template <typename N> __device__ __forceinline__ N kv4_scan(N x) {
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
-        const long long x = __shfl_up_sync(0xffffffffu, up, o);
-        if (lane >= o) up += x;
+        const N y = __shfl_up_sync(0xffffffffu, x, o);
+        if ((int)(threadIdx.x & 31) >= o) x += y;
     }
-    if (lane == 31) sums[warp] = up;
-    __syncthreads();
-    long long before = 0;
-    for (int w = 0; w < warp; ++w) before += sums[w];
-    pre[tid] = before + up - mine;
-    if (tid == n - 1) pre[n] = before + up;
-    __syncthreads();
+    return x;
 }
-// the last i with pre[i] <= u (0 <= u < pre[n])
-__device__ __forceinline__ int kv4_find(const long long* pre, int n, long long u) {
-    int lo = 0, hi = n;
-    while (hi - lo > 1) {
-        const int mid = (lo + hi) >> 1;
-        if (pre[mid] <= u) lo = mid; else hi = mid;
-    }
-    return lo;
+// a / b for positive numbers: in 32 bits where they fit
+__device__ __forceinline__ long long kv4_quotient(long long a, long long b) {
+    return ((a | b) >> 32) == 0 ? (long long)((uint32_t)a / (uint32_t)b) : a / b;
 }
 
 }  // namespace pt

@@ -103,11 +103,6 @@ struct Cursor {
     long long left;                               // units of cost of the warp's range behind this segment's
 };
 
-// a / b for positive numbers: in 32 bits where they fit
-__device__ __forceinline__ long long quotient(long long a, long long b) {
-    return ((a | b) >> 32) == 0 ? (long long)((uint32_t)a / (uint32_t)b) : a / b;
-}
-
 template <int DH, int NT> struct Walk {
     static constexpr int RB = Cfg<DH, NT>::RB;
     const Kv4AttnP& p;
@@ -160,9 +155,9 @@ template <int DH, int NT> struct Walk {
             rows += S;
             mine += cost(S, K);
         }
-        int up = scan(mine);
+        int up = kv4_scan(mine);
         long long up_rows = 0;
-        if (p.qlen) up_rows = scan(rows);
+        if (p.qlen) up_rows = kv4_scan(rows);
         bad = __any_sync(0xffffffffu, bad) || __shfl_sync(0xffffffffu, up_rows, 31) > p.M;
         const int per_head = __shfl_sync(0xffffffffu, up, 31);
         const long long units = (long long)per_head * (p.slab.nkv * p.T);
@@ -171,11 +166,11 @@ template <int DH, int NT> struct Walk {
         constexpr int W = Cfg<DH, NT>::WARPS;
         const int all = (int)min((long long)gridDim.x, (units + W - 1) / W) * W, gw = blockIdx.x * W + (threadIdx.x >> 5);
         if (gw >= all) return false;
-        const long long share = quotient(units, all), more = units - share * all;
+        const long long share = kv4_quotient(units, all), more = units - share * all;
         const long long u0 = share * gw + min((long long)gw, more);
         c.left = share + (gw < more);
         if (c.left == 0) return false;
-        c.th = (int)quotient(u0, per_head);
+        c.th = (int)kv4_quotient(u0, per_head);
         int in = (int)(u0 - (long long)c.th * per_head);
         const int l = __popc(__ballot_sync(0xffffffffu, up <= in));
         in -= __shfl_sync(0xffffffffu, up - mine, l);
@@ -187,7 +182,7 @@ template <int DH, int NT> struct Walk {
                 S = K = 0;
                 if (b < min(p.B, (l + 1) * per)) load(b, S, K);
                 mine = cost(S, K);
-                up = scan(mine);
+                up = kv4_scan(mine);
                 at = __popc(__ballot_sync(0xffffffffu, up <= in));
                 int sum = lane < at ? S : 0;
 #pragma unroll
@@ -209,14 +204,6 @@ template <int DH, int NT> struct Walk {
         }
         enter(c, in);
         return c.lo < c.hi || next(c);
-    }
-    template <typename N> __device__ static N scan(N x) {
-#pragma unroll
-        for (int o = 1; o < 32; o <<= 1) {
-            const N y = __shfl_up_sync(0xffffffffu, x, o);
-            if ((int)(threadIdx.x & 31) >= o) x += y;
-        }
-        return x;
     }
 };
 
