@@ -773,19 +773,34 @@ def kernel_chunk_attn(q, pool_l, block_table, q_len, kv_len, *, nq, nkv, dh, ps,
 
 
 def _kv4_pool(pool_l, T, nkv, dh, ps, index):
-    """Checks one layer of an E2M1 pool: uint8 [T, pages, nkv, ps // 16, 17 * dh], contiguous but for the track stride."""
+    """Checks one layer of an E2M1 pool: uint8 [T, pages, nkv, ps // 16, 17 * dh], contiguous but for the track stride.
+    Returns (pages, bytes between tracks)."""
     import torch
-    if pool_l.dtype is not torch.uint8 or pool_l.dim() != 5 or pool_l.shape[0] != T or tuple(pool_l.shape[2:]) != (nkv, ps // 16, 17 * dh) \
-            or not pool_l[0].is_contiguous() or pool_l.get_device() != index or index < 0 or pool_l.shape[1] < 1:
-        raise ValueError(f"pool: a uint8 CUDA tensor [{T}, pages, {nkv}, {ps // 16}, {17 * dh}] with contiguous tracks on the call's device is wanted")
-    return pool_l.stride(0) if T > 1 else 0
+    shape = pool_l.shape
+    if len(shape) == 5:
+        tracks, pages, heads, blocks, size = shape
+        if pool_l.is_contiguous():
+            stride = pages * heads * blocks * size
+        else:
+            stride, *rest = pool_l.stride()
+            if rest != [heads * blocks * size, blocks * size, size, 1]:
+                tracks = -1
+        if tracks == T and heads == nkv and blocks * 16 == ps and size == 17 * dh and pages and pool_l.dtype is torch.uint8 and pool_l.get_device() == index:
+            return pages, stride if T > 1 else 0
+    raise ValueError(f"pool: a uint8 CUDA tensor [{T}, pages, {nkv}, {ps // 16}, {17 * dh}] with contiguous tracks on the call's device is wanted")
 
 
-def _kv4_ints(index, **arrays):
+def _kv4_int(name, a, shape, dtype, index):
+    if a.shape != shape or a.dtype is not dtype or a.get_device() != index or not a.is_contiguous():
+        raise ValueError(f"{name}: a contiguous {dtype} tensor of shape {tuple(shape)} on CUDA device {index} is wanted")
+    return a.data_ptr()
+
+
+def _kv4_table(name, a, rows, index):
     import torch
-    for name, (a, dtype, dim) in arrays.items():
-        if a.dtype is not dtype or a.dim() != dim or not a.is_contiguous() or a.get_device() != index:
-            raise ValueError(f"{name}: a contiguous {dtype} tensor of {dim} dimensions on CUDA device {index} is wanted")
+    if a.dim() != 2 or a.shape[0] != rows or a.dtype is not torch.int32 or a.get_device() != index or not a.is_contiguous():
+        raise ValueError(f"{name}: a contiguous int32 tensor [{rows}, columns] on CUDA device {index} is wanted")
+    return a.data_ptr(), a.shape[1]
 
 
 def _kv4_status(status, index):
@@ -802,24 +817,23 @@ def kernel_kv_write_e2m1(k, v, pool_l, slots, *, nkv, dh, ps, k_out=None, v_out=
     (uint8 [T, pages, nkv, ps/16, 17*dh]): row r to token slots[r] % ps of page slots[r] // ps (int64 CUDA [M]; negative:
     not cached).  k_out, v_out (bf16 [T, M, nkv*dh]) receive the values that the cache then returns.  Returns status int32[16]."""
     import torch
-    bf16, index = torch.bfloat16, k.get_device()
-    if k.dim() != 3 or k.dtype is not bf16 or v.dtype is not bf16 or k.shape != v.shape or k.stride() != v.stride() or k.shape[2] != nkv * dh \
-            or k.stride(2) != 1 or v.get_device() != index or index < 0:
+    bf16, index, shape, stride = torch.bfloat16, k.get_device(), k.shape, k.stride()
+    if len(shape) != 3 or shape[2] != nkv * dh or stride[2] != 1 or k.dtype is not bf16 or index < 0 \
+            or v.dtype is not bf16 or v.shape != shape or v.stride() != stride or v.get_device() != index:
         raise ValueError("k, v: bf16 CUDA tensors [T, M, nkv*dh] of the same strides with contiguous values are wanted")
-    T, M, _ = k.shape
-    pstride = _kv4_pool(pool_l, T, nkv, dh, ps, index)
-    _kv4_ints(index, slots=(slots, torch.int64, 1))
-    if slots.numel() != M or (k_out is None) != (v_out is None):
-        raise ValueError("slots: one for each row; k_out and v_out: both or neither")
-    for a in (k_out, v_out):
-        if a is not None and (a.dtype is not bf16 or a.shape != k.shape or not a.is_contiguous() or a.get_device() != index):
-            raise ValueError("k_out, v_out: contiguous bf16 CUDA tensors of k's shape are wanted")
+    T, M, _ = shape
+    pages, pstride = _kv4_pool(pool_l, T, nkv, dh, ps, index)
+    at = _kv4_int("slots", slots, (M,), torch.int64, index)
+    ko = vo = None
+    if k_out is not None or v_out is not None:
+        for a in (k_out, v_out):
+            if a is None or a.dtype is not bf16 or a.shape != shape or not a.is_contiguous() or a.get_device() != index:
+                raise ValueError("k_out, v_out: both or neither, contiguous bf16 CUDA tensors of k's shape")
+        ko, vo = k_out.data_ptr(), v_out.data_ptr()
     status = _kv4_status(status, index)
-    if M == 0:
-        return status
-    _call(index, lib().pt_kernel_kv_write_e2m1, k.data_ptr(), v.data_ptr(), k.stride(0) if T > 1 else 0, k.stride(1) if M > 1 else 0, T, M, nkv, dh, ps,
-          pool_l.shape[1], pool_l.data_ptr(), pstride, slots.data_ptr(), None if k_out is None else k_out.data_ptr(),
-          None if v_out is None else v_out.data_ptr(), status.data_ptr())
+    if M:
+        _call(index, lib().pt_kernel_kv_write_e2m1, k.data_ptr(), v.data_ptr(), stride[0] if T > 1 else 0, stride[1] if M > 1 else 0, T, M, nkv, dh, ps,
+              pages, pool_l.data_ptr(), pstride, at, ko, vo, status.data_ptr())
     return status
 
 
@@ -828,19 +842,26 @@ def kernel_kv_read_e2m1(pool_l, block_table, kv_len, out, out_table, *, nkv, dh,
     int32 [B, maxp], kv_len int32 [B], all CUDA) into bf16 pages out [T, pages, 2, nkv, out_ps, dh] at out_table int32
     [B, out_maxp].  Returns (out, status int32[16])."""
     import torch
-    index = pool_l.get_device()
-    if out.dim() != 6 or out.dtype is not torch.bfloat16 or out.shape[2:4] != (2, nkv) or out.shape[5] != dh or out.get_device() != index \
-            or not out[0].is_contiguous():
+    index, shape = pool_l.get_device(), out.shape
+    if len(shape) != 6 or out.dtype is not torch.bfloat16 or out.get_device() != index or index < 0:
+        raise ValueError("out: a bf16 CUDA tensor [T, pages, 2, nkv, out_ps, dh] on the pool's device is wanted")
+    T, opages, two, heads, ops, width = shape
+    if out.is_contiguous():
+        ostride = 2 * opages * heads * ops * width
+    else:
+        ostride, *rest = out.stride()
+        if rest != [2 * heads * ops * width, heads * ops * width, ops * width, width, 1]:
+            two = 0
+    if two != 2 or heads != nkv or width != dh or not T or not opages:
         raise ValueError("out: a bf16 CUDA tensor [T, pages, 2, nkv, out_ps, dh] with contiguous tracks is wanted")
-    T, opages, _, _, ops, _ = out.shape
-    pstride = _kv4_pool(pool_l, T, nkv, dh, ps, index)
-    _kv4_ints(index, block_table=(block_table, torch.int32, 2), kv_len=(kv_len, torch.int32, 1), out_table=(out_table, torch.int32, 2))
+    pages, pstride = _kv4_pool(pool_l, T, nkv, dh, ps, index)
     B = kv_len.numel()
-    if block_table.shape[0] != B or out_table.shape[0] != B:
-        raise ValueError("block_table, out_table: a row for each sequence is wanted")
+    lens = _kv4_int("kv_len", kv_len, (B,), torch.int32, index)
+    bt, maxp = _kv4_table("block_table", block_table, B, index)
+    obt, omaxp = _kv4_table("out_table", out_table, B, index)
     status = _kv4_status(status, index)
-    _call(index, lib().pt_kernel_kv_read_e2m1, pool_l.data_ptr(), pstride, block_table.data_ptr(), block_table.shape[1], kv_len.data_ptr(), T, B, nkv, dh, ps,
-          pool_l.shape[1], out.data_ptr(), out.stride(0) if T > 1 else 0, out_table.data_ptr(), out_table.shape[1], ops, opages, status.data_ptr())
+    _call(index, lib().pt_kernel_kv_read_e2m1, pool_l.data_ptr(), pstride, bt, maxp, lens, T, B, nkv, dh, ps, pages, out.data_ptr(), ostride if T > 1 else 0,
+          obt, omaxp, ops, opages, status.data_ptr())
     return out, status
 
 
@@ -857,33 +878,27 @@ def kernel_attn_e2m1(q, pool_l, block_table, kv_len, q_len=None, *, nq, nkv, dh,
     17*dh]; block_table int32 [B, maxp], kv_len int32 [B], q_len int32 [B] or None (one new token each), all CUDA.
     Returns (out bf16 [T, M, nq*dh], status int32[16])."""
     import torch
-    bf16, index = torch.bfloat16, q.get_device()
-    if q.dim() != 3 or q.dtype is not bf16 or not q.is_contiguous() or q.shape[2] != nq * dh:
+    bf16, index, shape = torch.bfloat16, q.get_device(), q.shape
+    if len(shape) != 3 or shape[2] != nq * dh or q.dtype is not bf16 or not q.is_contiguous() or index < 0:
         raise ValueError("q: a contiguous bf16 CUDA tensor [T, M, nq*dh] is wanted")
-    T, M, _ = q.shape
-    pstride = _kv4_pool(pool_l, T, nkv, dh, ps, index)
-    _kv4_ints(index, block_table=(block_table, torch.int32, 2), kv_len=(kv_len, torch.int32, 1))
+    T, M, _ = shape
+    pages, pstride = _kv4_pool(pool_l, T, nkv, dh, ps, index)
     B = kv_len.numel()
-    if block_table.shape[0] != B:
-        raise ValueError("block_table: a row for each sequence is wanted")
-    if q_len is not None:
-        _kv4_ints(index, q_len=(q_len, torch.int32, 1))
-        if q_len.numel() != B:
-            raise ValueError("q_len: one for each sequence is wanted")
+    lens = _kv4_int("kv_len", kv_len, (B,), torch.int32, index)
+    news = None if q_len is None else _kv4_int("q_len", q_len, (B,), torch.int32, index)
+    bt, maxp = _kv4_table("block_table", block_table, B, index)
     if out is None:
         out = torch.empty_like(q)
-    elif out.dtype is not bf16 or out.shape != q.shape or not out.is_contiguous() or out.get_device() != index:
+    elif out.dtype is not bf16 or out.shape != shape or not out.is_contiguous() or out.get_device() != index:
         raise ValueError("out: a contiguous bf16 CUDA tensor of q's shape is wanted")
     if scratch is None:
         scratch = attn_e2m1_scratch(T, nq, nkv, dh, q.device)
     elif scratch.get_device() != index or not scratch.is_contiguous():
         raise ValueError("scratch: a contiguous tensor on the call's device is wanted")
     status = _kv4_status(status, index)
-    if M == 0:
-        return out, status
-    _call(index, lib().pt_kernel_attn_e2m1, q.data_ptr(), pool_l.data_ptr(), pstride, block_table.data_ptr(), block_table.shape[1],
-          None if q_len is None else q_len.data_ptr(), kv_len.data_ptr(), T, B, M, nq, nkv, dh, ps, pool_l.shape[1], out.data_ptr(),
-          scratch.data_ptr(), scratch.numel() * scratch.element_size(), status.data_ptr())
+    if M:
+        _call(index, lib().pt_kernel_attn_e2m1, q.data_ptr(), pool_l.data_ptr(), pstride, bt, maxp, news, lens, T, B, M, nq, nkv, dh, ps, pages,
+              out.data_ptr(), scratch.data_ptr(), scratch.nbytes, status.data_ptr())
     return out, status
 
 
