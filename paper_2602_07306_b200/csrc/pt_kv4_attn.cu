@@ -13,6 +13,7 @@ namespace {
 constexpr int kTile = 32;                 // keys a warp takes at a time: two blocks of 16
 constexpr int kMaxBlocks = 160;           // thread blocks whose parts the scratch has room for
 constexpr int kSegCost = 2;               // cost of beginning a segment, in tiles
+constexpr int kWholeTiles = 3;            // tiles of a warp up to which a block takes a whole segment: 1000 keys 11.1 us (12.8 cut up), 1500 keys 12.8 (12.0)
 constexpr uint32_t kSpin = 1u << 24;
 constexpr float kTop = 14.f, kStart = 8.f; // weights stay below 2^kTop; a reference is set so that the largest is 2^kStart
 constexpr float kNone = -3.0e38f;         // reference of a row that has seen nothing
@@ -107,10 +108,11 @@ template <int DH, int NT> struct Walk {
     static constexpr int RB = Cfg<DH, NT>::RB;
     const Kv4AttnP& p;
     const int G;
-    __device__ Walk(const Kv4AttnP& p_) : p(p_), G(p_.nq / p_.slab.nkv) {}
+    const bool whole;                             // a block takes one whole segment
+    __device__ Walk(const Kv4AttnP& p_, bool w) : p(p_), G(p_.nq / p_.slab.nkv), whole(w) {}
     __device__ int seen(int S, int K, int rb) const { return (rb + 1) * RB >= S * G ? K : K - S + ((rb + 1) * RB - 1) / G + 1; }
     __device__ void load(int b, int& S, int& K) const { S = p.qlen ? p.qlen[b] : 1; K = p.kvlen[b]; }
-    __device__ static int cost(int seen) { return (seen + kTile - 1) / kTile + kSegCost; }
+    __device__ int cost(int seen) const { return whole ? 1 : (seen + kTile - 1) / kTile + kSegCost; }
     // of all row blocks of a sequence (the host has checked that those of all sequences fit)
     __device__ int cost(int S, int K) const {
         int n = 0;
@@ -164,12 +166,17 @@ template <int DH, int NT> struct Walk {
         if (bad || units == 0) return false;
         // the call's units go in equal shares to the warps of as many blocks as have one for each warp
         constexpr int W = Cfg<DH, NT>::WARPS;
-        const int all = (int)min((long long)gridDim.x, (units + W - 1) / W) * W, gw = blockIdx.x * W + (threadIdx.x >> 5);
-        if (gw >= all) return false;
-        const long long share = kv4_quotient(units, all), more = units - share * all;
-        const long long u0 = share * gw + min((long long)gw, more);
-        c.left = share + (gw < more);
-        if (c.left == 0) return false;
+        long long u0 = blockIdx.x;
+        if (whole) {
+            if (u0 >= units) return false;
+        } else {
+            const int all = (int)min((long long)gridDim.x, (units + W - 1) / W) * W, gw = blockIdx.x * W + (threadIdx.x >> 5);
+            if (gw >= all) return false;
+            const long long share = kv4_quotient(units, all), more = units - share * all;
+            u0 = share * gw + min((long long)gw, more);
+            c.left = share + (gw < more);
+            if (c.left == 0) return false;
+        }
         c.th = (int)kv4_quotient(u0, per_head);
         int in = (int)(u0 - (long long)c.th * per_head);
         const int l = __popc(__ballot_sync(0xffffffffu, up <= in));
@@ -202,13 +209,21 @@ template <int DH, int NT> struct Walk {
             if (in < n) break;
             in -= n;
         }
+        if (whole) {                                               // its tiles in equal shares to the block's warps
+            const int w = threadIdx.x >> 5;
+            c.seen = seen(c.S, c.K, c.rb);
+            c.n = (c.seen + kTile - 1) / kTile;
+            c.lo = (int)((long long)c.n * w / W); c.hi = (int)((long long)c.n * (w + 1) / W);
+            c.left = 0;
+            return c.lo < c.hi;
+        }
         enter(c, in);
         return c.lo < c.hi || next(c);
     }
 };
 
 template <int DH, int NT>
-__global__ void __launch_bounds__(Cfg<DH, NT>::THREADS, 1) k_kv4_attn(const Kv4AttnP p, void* scratch) {
+__global__ void __launch_bounds__(Cfg<DH, NT>::THREADS, 1) k_kv4_attn(const Kv4AttnP p, void* scratch, const bool whole) {
     using C = Cfg<DH, NT>;
     constexpr int NG = C::NG, RB = C::RB;
     extern __shared__ __align__(128) uint8_t smem[];
@@ -225,7 +240,7 @@ __global__ void __launch_bounds__(Cfg<DH, NT>::THREADS, 1) k_kv4_attn(const Kv4A
     }
     grid_dep_wait();
     grid_dep_launch();
-    const Walk<DH, NT> walk(p);
+    const Walk<DH, NT> walk(p, whole);
     const int G = walk.G, nkv = p.slab.nkv, ps = p.slab.ps;
     const Scratch<DH, NT> sc(scratch);
     Cursor cur{};
@@ -744,9 +759,12 @@ template <int DH, int NT> pt_status launch_t(const Kv4AttnP& p, void* scratch, c
     // units of one head are counted in 32 bits: every block of rows with every key that the table can name
     const double most = ((double)p.M * (p.nq / p.slab.nkv) / C::RB + p.B) * ((double)p.maxp * p.slab.ps / kTile + 1 + kSegCost);
     if (most > 2e9) { set_error("4-bit attention: too many sequences, rows or pages for one call"); return PT_ERR_UNSUPPORTED; }
-    cudaError_t e = launch_dependent(k_kv4_attn<DH, NT>, dim3(blocks), dim3(C::THREADS), (size_t)C::SMEM, st, p, scratch);
+    // Few segments of few keys: a block for each, and no second launch
+    const double segments = ((double)p.M * (p.nq / p.slab.nkv) / C::RB + p.B) * p.slab.nkv * p.T;
+    const bool whole = segments <= blocks && (int64_t)p.maxp * p.slab.ps <= kWholeTiles * kTile * C::WARPS;
+    cudaError_t e = launch_dependent(k_kv4_attn<DH, NT>, dim3(whole ? (unsigned)segments : blocks), dim3(C::THREADS), (size_t)C::SMEM, st, p, scratch, whole);
     g_launches.fetch_add(1, std::memory_order_relaxed);
-    if (e == cudaSuccess && blocks > 1) {
+    if (e == cudaSuccess && !whole && blocks > 1) {
         e = launch_dependent(k_kv4_merge<DH, NT>, dim3(blocks - 1, p.qlen ? C::RB : p.nq / p.slab.nkv), dim3(kMergeThreads), (size_t)0, st, p, scratch, blocks);
         g_launches.fetch_add(1, std::memory_order_relaxed);
     }
