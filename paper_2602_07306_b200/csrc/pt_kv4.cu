@@ -1,6 +1,5 @@
 // The 4-bit storage format of the KV cache (pt_kv_dtype PT_KV_E2M1): new tokens' K and V into its pages, and sequences back out.
-//   k_kv4_write   a thread has eight consecutive values of a vector, four threads a group of 32: the group's maximum takes two
-//                 shuffles
+//   k_kv4_write   a thread has sixteen consecutive values of a vector, two threads a group of 32
 //   k_kv4_read    a warp has one head's K and V of 16 tokens, in the order in which they lie: 16 bytes a lane and load
 // Both move bytes and compute little.
 #include <algorithm>
@@ -17,9 +16,12 @@ namespace {
 constexpr int kThreads = 256;
 
 // The code of v / s for the group's scale s, given r = 1 / s rounded: ties between codes have to be met exactly.  v has 8
-// significant bits and a tie times s has 7, so v / s is either a tie or at least 2^-8 of it away; v * r is off by 2^-23, and
-// rounding it to 12 bits returns to the tie.
-__device__ __forceinline__ float kv4_divided(float v, float r) { return __uint_as_float((__float_as_uint(v * r) + 0x800u) & ~0xfffu); }
+// significant bits and a tie times s has 7, so v / s is either a tie (0.25 .. 5) or at least 2^-8 of it away; v * r is off by
+// 2^-22 of it, and a sum with 1.5 * 2^10 rounds it to multiples of 2^-13, which returns to the tie.  The sign stays, of zeros too.
+__device__ __forceinline__ float kv4_divided(float v, float r) {
+    constexpr float kRound = 1536.f;
+    return __uint_as_float(__float_as_uint(fmaf(v, r, kRound) - kRound) | (__float_as_uint(v) & 0x80000000u));
+}
 __device__ __forceinline__ uint32_t kv4_encode8(const float* y) {
     uint32_t w;
     asm("{\n .reg .b8 a, b, c, d;\n cvt.rn.satfinite.e2m1x2.f32 a, %2, %1;\n cvt.rn.satfinite.e2m1x2.f32 b, %4, %3;\n"
@@ -28,30 +30,33 @@ __device__ __forceinline__ uint32_t kv4_encode8(const float* y) {
     return w;
 }
 
-// Eight values of a vector: their codes (one word, the lowest value's lowest), and the byte of the group's scale.
-__device__ __forceinline__ uint32_t kv4_encode(const uint4& raw, uint32_t& byte) {
-    const uint32_t w[4] = {raw.x, raw.y, raw.z, raw.w};
+// Sixteen values of a vector, half of a group (its other half is the lane's neighbour's): their codes in two words (the
+// lowest value's lowest), and the byte of the group's scale.
+__device__ __forceinline__ uint2 kv4_encode(const uint4* raw, uint32_t& byte) {
+    const uint32_t w[8] = {raw[0].x, raw[0].y, raw[0].z, raw[0].w, raw[1].x, raw[1].y, raw[1].z, raw[1].w};
     // magnitudes as whole numbers: a NaN is above infinity, which is above the rest
     uint32_t top = 0;
 #pragma unroll
-    for (int a = 0; a < 4; ++a) top = __vmaxu2(top, w[a] & 0x7fff7fffu);
+    for (int a = 0; a < 8; ++a) top = __vmaxu2(top, w[a] & 0x7fff7fffu);
+    top = __vmaxu2(top, __shfl_xor_sync(0xffffffffu, top, 1));
     top = max(top & 0xffffu, top >> 16);
-    top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
-    top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
     const bool bad = top >= 0x7f80u;
     const float amax = bad ? 0.f : __uint_as_float(top << 16);
     // amax / 6 cut to 4 significant bits, or the next number where that is too small (the product is exact)
     byte = (uint32_t)__half_as_ushort(__float2half_rz(fminf(amax * (1.0f / 6.0f), 61440.f))) >> 7;
     if (byte < 247 && 6.0f * kv4_scale(byte) < amax) ++byte;
-    const float s = kv4_scale(byte), r = s > 0.f ? 1.0f / s : 0.f;
-    float y[8];
+    const float s = kv4_scale(byte);
+    float r;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(s));           // off by 2^-23: see kv4_divided
+    if (byte == 0) r = 0.f;
+    float y[16];
 #pragma unroll
-    for (int a = 0; a < 4; ++a) {
+    for (int a = 0; a < 8; ++a) {
         y[2 * a] = kv4_divided(__uint_as_float(w[a] << 16), r);
         y[2 * a + 1] = kv4_divided(__uint_as_float(w[a] & 0xffff0000u), r);
     }
-    if (bad) { byte = 255; return 0u; }
-    return kv4_encode8(y);
+    if (bad) { byte = 255; return make_uint2(0u, 0u); }
+    return make_uint2(kv4_encode8(y), kv4_encode8(y + 8));
 }
 
 // A block has 16 rows of one track and head.  Tokens that follow one another lie side by side in a block of the cache, but
@@ -59,8 +64,8 @@ __device__ __forceinline__ uint32_t kv4_encode(const uint4& raw, uint32_t& byte)
 // the cache, as if row 0's slot were followed by the others.  Where it is not, the same pieces go to the same places less
 // well together.
 template <int DH>
-__global__ void __launch_bounds__(2 * DH) k_kv4_write(const Kv4WriteP p) {
-    constexpr int PER = DH / 8, THREADS = 2 * DH, NG = DH / 32;    // threads of a vector; 16 vectors
+__global__ void __launch_bounds__(DH) k_kv4_write(const Kv4WriteP p) {
+    constexpr int PER = DH / 16, THREADS = DH, NG = DH / 32;       // threads of a vector; 16 vectors
     constexpr int KP = DH / 8, VP = DH / 16;                       // bytes of a piece
     __shared__ __align__(16) uint8_t img[2][16][DH / 2];           // K, V: a token's pieces in order
     __shared__ __align__(16) uint8_t scales[2][16][NG];
@@ -68,16 +73,20 @@ __global__ void __launch_bounds__(2 * DH) k_kv4_write(const Kv4WriteP p) {
     __shared__ int slot_in[16];                                    // its slot in that block
     grid_dep_wait();
     grid_dep_launch();
-    const int tid = threadIdx.x, r = tid / PER, oct = tid % PER, group = oct >> 2, q = oct & 3;
+    const int tid = threadIdx.x, r = tid / PER, part = tid % PER, group = part >> 1, half = part & 1;
     const int head = blockIdx.y, t = blockIdx.z, nkv = p.slab.nkv;
     const int64_t row = (int64_t)blockIdx.x * 16 + r;
     const bool live = row < p.M;                                   // every lane takes part in the shuffles
-    uint4 raw[2] = {};
+    uint4 raw[2][2] = {};
     if (live) {
-        const size_t at = (size_t)t * p.tstride + row * p.row_stride + head * p.head_stride + oct * 8;
-        raw[0] = *reinterpret_cast<const uint4*>(p.k + at);
-        raw[1] = *reinterpret_cast<const uint4*>(p.v + at);
+        const size_t at = (size_t)t * p.tstride + row * p.row_stride + head * p.head_stride + part * 16;
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {
+            const uint4* src = reinterpret_cast<const uint4*>((x ? p.v : p.k) + at);
+            raw[x][0] = src[0]; raw[x][1] = src[1];
+        }
     }
+    const size_t out_at = (((size_t)t * p.M + row) * nkv + head) * DH + part * 16;
     if (tid < 16) {
         const int64_t row_t = (int64_t)blockIdx.x * 16 + tid, slot = row_t < p.M ? p.slots[row_t] : -1;
         int64_t to = -1;
@@ -95,22 +104,28 @@ __global__ void __launch_bounds__(2 * DH) k_kv4_write(const Kv4WriteP p) {
 #pragma unroll
     for (int x = 0; x < 2; ++x) {
         uint32_t byte;
-        const uint32_t code = kv4_encode(raw[x], byte);
-        __nv_bfloat16* val = x ? p.v_out : p.k_out;
-        if (val && live) {
-            uint32_t h[4];
-            kv4_codes8(code, h);
+        const uint2 code = kv4_encode(raw[x], byte);
+        if (p.k_out && live) {
             const float s = kv4_scale(byte);
-            *reinterpret_cast<uint4*>(val + (((size_t)t * p.M + row) * nkv + head) * DH + oct * 8) =
-                make_uint4(kv4_value2(h[0], s), kv4_value2(h[1], s), kv4_value2(h[2], s), kv4_value2(h[3], s));
+            uint4* val = reinterpret_cast<uint4*>((x ? p.v_out : p.k_out) + out_at);
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                uint32_t h[4];
+                kv4_codes8(i ? code.y : code.x, h);
+                val[i] = make_uint4(kv4_value2(h[0], s), kv4_value2(h[1], s), kv4_value2(h[2], s), kv4_value2(h[3], s));
+            }
         }
-        if (x == 0) {
-            *reinterpret_cast<uint32_t*>(&img[0][r][q * KP + group * 4]) = code;
-        } else {
-            *reinterpret_cast<uint16_t*>(&img[1][r][2 * q * VP + group * 2]) = (uint16_t)code;
-            *reinterpret_cast<uint16_t*>(&img[1][r][(2 * q + 1) * VP + group * 2]) = (uint16_t)(code >> 16);
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const uint32_t c = i ? code.y : code.x;
+            if (x == 0) {
+                *reinterpret_cast<uint32_t*>(&img[0][r][(2 * half + i) * KP + group * 4]) = c;
+            } else {
+                *reinterpret_cast<uint16_t*>(&img[1][r][(4 * half + 2 * i) * VP + group * 2]) = (uint16_t)c;
+                *reinterpret_cast<uint16_t*>(&img[1][r][(4 * half + 2 * i + 1) * VP + group * 2]) = (uint16_t)(c >> 16);
+            }
         }
-        if (q == 0) scales[x][r][group] = (uint8_t)byte;
+        if (half == 0) scales[x][r][group] = (uint8_t)byte;
     }
     __syncthreads();
     char* const slab = p.slab.pool_l + (size_t)t * p.slab.tstride;
@@ -270,7 +285,7 @@ int sm_count() {
 
 pt_status launch_kv4_write(const Kv4WriteP& p, int dh, cudaStream_t st) {
     if (p.T > 65535) { set_error("too many tracks for one call"); return PT_ERR_UNSUPPORTED; }
-    const cudaError_t e = launch_dependent(dh == 64 ? k_kv4_write<64> : k_kv4_write<128>, dim3((p.M + 15) / 16, p.slab.nkv, p.T), dim3(2 * dh), (size_t)0, st, p);
+    const cudaError_t e = launch_dependent(dh == 64 ? k_kv4_write<64> : k_kv4_write<128>, dim3((p.M + 15) / 16, p.slab.nkv, p.T), dim3(dh), (size_t)0, st, p);
     if (e != cudaSuccess) { set_error("k_kv4_write launch: %s", cudaGetErrorString(e)); return PT_ERR_CUDA; }
     g_launches.fetch_add(1, std::memory_order_relaxed);
     return PT_OK;
