@@ -746,6 +746,9 @@ __global__ void __launch_bounds__(kMergeThreads) k_kv4_merge(const Kv4AttnP p, v
 
 template <int DH, int NT> pt_status launch_t(const Kv4AttnP& p, void* scratch, cudaStream_t st) {
     using C = Cfg<DH, NT>;
+    // units of one head are counted in 32 bits: every block of rows with every key that the table can name
+    const double most = ((double)p.M * (p.nq / p.slab.nkv) / C::RB + p.B) * ((double)p.maxp * p.slab.ps / kTile + 1 + kSegCost);
+    if (most > 2e9) { set_error("4-bit attention: too many sequences, rows or pages for one call"); return PT_ERR_UNSUPPORTED; }
     static int sms_[kMaxDevices] = {};
     int& sms = sms_[current_device()];
     if (!sms) {
@@ -756,9 +759,6 @@ template <int DH, int NT> pt_status launch_t(const Kv4AttnP& p, void* scratch, c
         sms = n;
     }
     const int blocks = std::min(sms, kMaxBlocks);
-    // units of one head are counted in 32 bits: every block of rows with every key that the table can name
-    const double most = ((double)p.M * (p.nq / p.slab.nkv) / C::RB + p.B) * ((double)p.maxp * p.slab.ps / kTile + 1 + kSegCost);
-    if (most > 2e9) { set_error("4-bit attention: too many sequences, rows or pages for one call"); return PT_ERR_UNSUPPORTED; }
     // Few segments of few keys: a block for each, and no second launch
     const double segments = ((double)p.M * (p.nq / p.slab.nkv) / C::RB + p.B) * p.slab.nkv * p.T;
     const bool whole = segments <= blocks && (int64_t)p.maxp * p.slab.ps <= kWholeTiles * kTile * C::WARPS;

@@ -376,3 +376,94 @@ def test_write_read_and_attend_together():
         top = torch.nan_to_num(flat.float()).abs().amax()
         d = (out.float() - want.float()).abs()
         assert (d <= 2.0 ** -7 * want.float().abs() + (2.0 ** -8 + 2.0 ** -10 + 2.0 ** -12) * top).all(), d.max()
+
+
+@pytest.mark.parametrize("T,nq,nkv,dh,q_len,kv_len", [(2, 4, 2, 128, None, [301, 40, 17]), (1, 8, 8, 64, [3, 0, 1], [90, 5, 33]), (1, 8, 2, 128, [9, 20], [64, 300])])
+def test_attention_of_short_sequences_under_a_wide_table(T, nq, nkv, dh, q_len, kv_len):
+    """Few short segments take a thread block each where the table says that they are short, and are cut up where it does not."""
+    import torch
+    pool, values, bt = cache(T, nkv, dh, 16, kv_len, 11)
+    ql = [1] * len(kv_len) if q_len is None else q_len
+    q = queries(T, sum(ql), nq, dh, 11)
+    want, bound = reference(q, values, bt, ql, kv_len, 16)
+    for columns in (bt.shape[1], 500):
+        wide = np.full((len(kv_len), columns), -5, np.int32)
+        wide[:, :bt.shape[1]] = bt
+        got, st = attend(q, pool, wide, kv_len, q_len, 16, nkv)
+        d = np.abs(got.float().cpu().numpy().astype(np.float64) - want)
+        assert st == [0, 0] and np.isfinite(d).all() and (d <= bound).all(), columns
+
+
+def test_calls_without_work():
+    """Sequences without new tokens, or without keys, leave everything as it was."""
+    import torch
+    from paper_2602_07306_b200 import pt
+    pool, values, bt = cache(1, 2, 64, 16, [30, 10], 12)
+    q = queries(1, 3, 4, 64, 12)
+    out = torch.full((1, 3, 256), 7.0, dtype=torch.bfloat16, device="cuda")
+    for ql, kl in (([0, 0], [30, 10]), ([0, 0], [0, 0])):
+        got, st = attend(q, pool, bt, kl, ql, 16, 2, out=out)
+        assert st == [0, 0] and (got == 7).all()
+    dp = torch.from_numpy(pool).cuda()
+    k = torch.randn((1, 5, 128), device="cuda").bfloat16()
+    st = pt.kernel_kv_write_e2m1(k, k, dp, torch.full((5,), -1, dtype=torch.int64, device="cuda"), nkv=2, dh=64, ps=16)
+    assert st[0] == 0 and np.array_equal(dp.cpu().numpy(), pool)
+    e = torch.empty((1, 0, 128), dtype=torch.bfloat16, device="cuda")
+    assert pt.kernel_kv_write_e2m1(e, e, dp, torch.empty(0, dtype=torch.int64, device="cuda"), nkv=2, dh=64, ps=16)[0] == 0
+
+
+def test_pools_beyond_32_bit_offsets():
+    """Pages more than 2^32 bytes into a track's slab, and a second track behind them."""
+    import torch
+    from paper_2602_07306_b200 import pt
+    nkv, dh, ps, n = 8, 128, 64, 150
+    pages = (1 << 32) // (nkv * (ps // 16) * 17 * dh) + 40
+    pool = torch.empty((2, pages, nkv, ps // 16, 17 * dh), dtype=torch.uint8, device="cuda")
+    rng = np.random.default_rng(0)
+    bt = np.array([[pages - 1, pages - 30, pages - 7]], np.int32)
+    pool[:, torch.from_numpy(bt[0]).long().cuda()] = 255
+    k, v = (I.round_to_bf16(rng.standard_normal((2, n, nkv, dh)).astype(np.float32)) for _ in range(2))
+    pos = np.arange(n)
+    slots = bt[0, pos // ps].astype(np.int64) * ps + pos % ps
+    shape = dict(nkv=nkv, dh=dh, ps=ps)
+    st = pt.kernel_kv_write_e2m1(bf(k).view(2, n, -1), bf(v).view(2, n, -1), pool, torch.from_numpy(slots).cuda(), **shape)
+    assert st[0] == 0
+    near = np.zeros((2, 3, nkv, ps // 16, 17 * dh), np.uint8)
+    near[:] = 255
+    for p in range(n):
+        for h in range(nkv):
+            kv4.put(near, p // ps, h, p % ps, k[:, p, h], v[:, p, h])
+    assert np.array_equal(pool[:, torch.from_numpy(bt[0]).long().cuda()].cpu().numpy(), near)
+    values = kv4.get(near)
+    out = torch.zeros((2, 10, 2, nkv, 16, dh), dtype=torch.bfloat16, device="cuda")
+    _, st = pt.kernel_kv_read_e2m1(pool, i32(bt), i32([n]), out, i32([np.arange(10)]), **shape)
+    assert st[0] == 0
+    flat = np.moveaxis(out.float().cpu().numpy(), 4, 2).reshape(2, 160, 2, nkv, dh)[:, :n]
+    np.testing.assert_array_equal(flat, np.moveaxis(values, 4, 2).reshape(2, 3 * ps, 2, nkv, dh)[:, :n])
+    q = queries(2, 2, nkv, dh, 3)
+    want, bound = reference(q, values, np.array([[0, 1, 2]], np.int32), [2], [n], ps)
+    got, st = pt.kernel_attn_e2m1(bf(q).view(2, 2, -1), pool, i32(bt), i32([n]), i32([2]), nq=nkv, **shape)
+    d = np.abs(got.view(2, 2, nkv, dh).float().cpu().numpy().astype(np.float64) - want)
+    assert st[0] == 0 and (d <= bound).all()
+
+
+def test_two_streams_at_once():
+    """Calls on two streams, each with a scratch of its own, give what they give alone."""
+    import torch
+    from paper_2602_07306_b200 import pt
+    cases = []
+    for seed in (1, 2):
+        pool, values, bt = cache(2, 4, 128, 16, [700 + 100 * seed, 900, 33], seed)
+        cases.append(dict(q=bf(queries(2, 3, 16, 128, seed)).view(2, 3, -1), pool_l=torch.from_numpy(pool).cuda(), block_table=i32(bt),
+                          kv_len=i32([700 + 100 * seed, 900, 33]), nq=16, nkv=4, dh=128, ps=16, scratch=pt.attn_e2m1_scratch(2, 16, 4, 128)))
+    alone = [pt.kernel_attn_e2m1(**c)[0].clone() for c in cases]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in cases]
+    outs = [[torch.empty_like(c["q"]) for _ in range(20)] for c in cases]
+    for i in range(20):
+        for s, c, o in zip(streams, cases, outs):
+            with torch.cuda.stream(s):
+                pt.kernel_attn_e2m1(**c, out=o[i])
+    torch.cuda.synchronize()
+    for a, o in zip(alone, outs):
+        assert all(torch.equal(a, x) for x in o)

@@ -79,11 +79,11 @@ def test_refusals(lib):
                  (6, dict(pool=odd)), (6, dict(pts=8)), (6, dict(k=odd)), (6, dict(v=odd)), (6, dict(ko=odd, vo=FAKE)), (6, dict(ts=4)), (6, dict(rs=12)),
                  (6, dict(slots=odd)), (6, dict(status=at(0x10002)))]),
             (R, [(1, dict(out=None)), (1, dict(obt=None)), (1, dict(kv=None)), (1, dict(B=0)), (1, dict(maxp=0)), (1, dict(omaxp=0)), (1, dict(opages=0)), (1, dict(ots=-8)),
-                 (1, dict(ops=12)), (1, dict(ops=72)), (1, dict(pts=-16)), (3, dict(dh=32)), (3, dict(ps=40)), (3, dict(maxp=1 << 27)), (3, dict(omaxp=1 << 28)),
+                 (1, dict(ops=12)), (1, dict(ops=72)), (1, dict(pts=-16)), (3, dict(dh=32)), (3, dict(ps=40)), (3, dict(maxp=1 << 27)), (3, dict(omaxp=1 << 28)), (3, dict(B=1 << 20, maxp=1 << 20)),
                  (6, dict(out=odd)), (6, dict(ots=4)), (6, dict(pool=odd)), (6, dict(bt=at(0x10002))), (6, dict(kv=at(0x10002)))]),
             (A, [(1, dict(q=None)), (1, dict(kv=None)), (1, dict(scratch=None)), (1, dict(B=0)), (1, dict(M=0)), (1, dict(M=(1 << 26) + 1)), (1, dict(nq=7)), (1, dict(nq=0)),
                  (1, dict(ql=None)), (1, dict(maxp=0)), (3, dict(nq=18)), (3, dict(dh=32)), (3, dict(ps=8)), (3, dict(maxp=1 << 27)), (4, dict(bytes=n.value - 1)),
-                 (6, dict(q=odd)), (6, dict(out=odd)), (6, dict(scratch=at(0x10080))), (6, dict(pool=odd)), (6, dict(pts=24)), (6, dict(ql=at(0x10002)))])):
+                 (3, dict(B=1 << 20, M=1 << 20, maxp=1 << 20)), (6, dict(q=odd)), (6, dict(out=odd)), (6, dict(scratch=at(0x10080))), (6, dict(pool=odd)), (6, dict(pts=24)), (6, dict(ql=at(0x10002)))])):
         for code, kw in refused:
             assert call(**kw) == code, (call, kw, lib.pt_last_error())
     assert lib.pt_kernel_attn_e2m1_scratch_bytes(2, 8, 2, 96, C.byref(n)) == 1
