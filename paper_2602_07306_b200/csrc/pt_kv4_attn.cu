@@ -1,4 +1,26 @@
 // Attention of one or a few new tokens per sequence straight from a 4-bit cache (pt_kv_dtype PT_KV_E2M1).
+//
+//   out[r] = sum_j 2^(s_rj - m_r) v_j / sum_j 2^(s_rj - m_r),   s_rj = log2(e) / sqrt(dh) q_r . k_j,
+//   k_j[d] = code * scale of d's group of 32, v_j likewise; r runs over the (token, head) rows of a sequence and KV head.
+//
+// What bounds it: 17 bytes bring 32 values, so at the copy rate an SM has 2.3 cycles for every 100 values, and the codes'
+// way into the matrix instructions is what takes time, not the bytes.  So:
+//  * The products run on mma.sync m16n8k16 in f16 with the cached vectors on the 16-row side and the rows r on the 8-column
+//    side: K^T q and V^T p take their 4-bit operand from registers, where cvt.rn.f16x2.e2m1x2 puts two codes an instruction.
+//    (tcgen05 takes its operands from shared memory or tensor memory: 4-bit codes would be converted in registers all the
+//    same, written and fetched again, and its block scales are powers of two, which these are not.)
+//  * The order of a block of 16 tokens is that of the instruction's operands: a lane loads its codes of K (two tokens, 32 dims
+//    each) and V (four tokens, 16 dims each) with 128-bit loads free of bank conflicts.  Of V a byte holds two dims of one
+//    token and the operand wants two tokens of one dim: eight codes of two tokens change places in four instructions.
+//  * A scale of K multiplies the partial score of its group in fp32, a scale of V the weights, once for 32 dims: codes enter
+//    the products as they are.  The weights are f16: their reference (m above) lags behind the maximum by up to 2^6 and is
+//    chosen so that weight times scale stays below 2^16; a scale of V of 2 or more makes room by raising it.  q is divided
+//    by a power of two that puts a row's largest magnitude at 2^13, K codes are below 8, sums are fp32.
+//  * A warp works alone: a ring of 32-key stages filled by bulk copies (a block of 16 tokens, K, V and scales, is one piece
+//    of 17 * dh bytes), its own plan from the device's lengths, its own contiguous share of all key tiles of the call, so
+//    that no barrier stands in the loop and a captured call may be replayed with other lengths.  A segment (sequence, track, KV
+//    head, 8 to 24 rows) that is cut leaves parts (sums, reference): those of a block's warps are merged in its shared
+//    memory, those of several blocks by k_kv4_merge.  Twelve warps of 168 registers: three a scheduler are enough.
 #include <algorithm>
 #include <type_traits>
 
