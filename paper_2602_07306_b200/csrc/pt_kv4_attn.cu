@@ -724,12 +724,14 @@ __global__ void __launch_bounds__(Cfg<DH, NT>::THREADS, 1) k_kv4_attn(const Kv4A
 constexpr int kMergeThreads = 256;
 template <int DH, int NT>
 __global__ void __launch_bounds__(kMergeThreads) k_kv4_merge(const Kv4AttnP p, void* scratch, const int blocks) {
-    constexpr int GROUPS = kMergeThreads / DH, RB = Cfg<DH, NT>::RB;
-    __shared__ float sh[GROUPS][DH + 2];
+    constexpr int WARPS = kMergeThreads / 32, RB = Cfg<DH, NT>::RB, V = DH / 32;      // columns of a lane
+    using Vec = std::conditional_t<V == 4, float4, float2>;
+    __shared__ __align__(16) float sums[WARPS][DH];
+    __shared__ float tops[WARPS], dens[WARPS];
     grid_dep_wait();
     grid_dep_launch();
     const Scratch<DH, NT> sc(scratch);
-    const int r = blockIdx.y, d = threadIdx.x % DH, grp = threadIdx.x / DH, lane = threadIdx.x & 31, c0 = blockIdx.x;
+    const int r = blockIdx.y, lane = threadIdx.x & 31, warp = threadIdx.x >> 5, c0 = blockIdx.x;
     const Leftover first = sc.left()[c0];
     if (!first.tail || !first.tail_begins || r >= first.seg.rows) return;
     // the block that ends the segment: the first behind c0 with a head
@@ -738,32 +740,36 @@ __global__ void __launch_bounds__(kMergeThreads) k_kv4_merge(const Kv4AttnP p, v
         const uint32_t heads = __ballot_sync(0xffffffffu, base + lane < blocks && sc.left()[base + lane].head);
         if (heads) { last = base + __ffs(heads) - 1; break; }
     }
-    float top = kNone, sum = 0.f, acc = 0.f;
+    float top = kNone, sum = 0.f;
+    alignas(16) float acc[V] = {};
 #pragma unroll 4
-    for (int c = c0 + grp; c <= last; c += GROUPS) {               // tails, and the last one's head
+    for (int c = c0 + warp; c <= last; c += WARPS) {               // tails, and the last one's head: a warp each
         const float* part = sc.part(c, c == last ? 0 : 1);
-        const float m = part[RB * DH + 2 * r], ls = part[RB * DH + 2 * r + 1], x = part[r * DH + d];
-        const float nt = fmaxf(top, m), f0 = ex2f(top - nt), f1 = ex2f(m - nt);
-        acc = acc * f0 + x * f1;
-        sum = sum * f0 + ls * f1;
+        const float2 st = *reinterpret_cast<const float2*>(part + RB * DH + 2 * r);
+        const Vec x = *reinterpret_cast<const Vec*>(part + r * DH + lane * V);
+        const float nt = fmaxf(top, st.x), f0 = ex2f(top - nt), f1 = ex2f(st.x - nt);
+#pragma unroll
+        for (int i = 0; i < V; ++i) acc[i] = acc[i] * f0 + reinterpret_cast<const float*>(&x)[i] * f1;
+        sum = sum * f0 + st.y * f1;
         top = nt;
     }
-    sh[grp][d] = acc;
-    if (d == 0) { sh[grp][DH] = top; sh[grp][DH + 1] = sum; }
+    *reinterpret_cast<Vec*>(&sums[warp][lane * V]) = *reinterpret_cast<const Vec*>(acc);
+    if (lane == 0) { tops[warp] = top; dens[warp] = sum; }
     __syncthreads();
-    if (grp) return;
-    float all = kNone;
+    const int d = threadIdx.x;
+    if (d >= DH) return;
+    float all = kNone, o = 0.f;
+    sum = 0.f;
 #pragma unroll
-    for (int i = 0; i < GROUPS; ++i) all = fmaxf(all, sh[i][DH]);
-    acc = sum = 0.f;
+    for (int i = 0; i < WARPS; ++i) all = fmaxf(all, tops[i]);
 #pragma unroll
-    for (int i = 0; i < GROUPS; ++i) {
-        const float f = ex2f(sh[i][DH] - all);
-        acc += sh[i][d] * f;
-        sum += sh[i][DH + 1] * f;
+    for (int i = 0; i < WARPS; ++i) {
+        const float f = ex2f(tops[i] - all);
+        o += sums[i][d] * f;
+        sum += dens[i] * f;
     }
     const int G = p.nq / p.slab.nkv, tok = (first.seg.r0 + r) / G, hd = first.seg.r0 + r - tok * G;
-    p.o[(((size_t)first.seg.t * p.M + first.seg.row0 + tok) * p.nq + first.seg.h * G + hd) * DH + d] = __float2bfloat16_rn(acc / sum);
+    p.o[(((size_t)first.seg.t * p.M + first.seg.row0 + tok) * p.nq + first.seg.h * G + hd) * DH + d] = __float2bfloat16_rn(o / sum);
 }
 
 template <int DH, int NT> pt_status launch_t(const Kv4AttnP& p, void* scratch, cudaStream_t st) {
