@@ -165,7 +165,7 @@ pt_status pt_kernel_decode_attn_e4m3(const void* q, const void* codes_l, int64_t
 /* ---- the 4-bit cache format (pt_kv_dtype PT_KV_E2M1 in pt.h; the paper has no cache, the format is this library's) ----
  * One layer's slab of such a pool, as these calls take it: pool_l device, 16-byte aligned; track t at pool_l +
  * t*pool_track_stride BYTES (a multiple of 16); pages [num_pages][kv_head][ps/16] blocks of 16 tokens, 17*dh bytes each, in
- * the order pt.h describes.  dh 64 or 128, ps a multiple of 16 up to 64.  All are asynchronous on `stream` and allocate
+ * the order pt.h describes.  dh 64 or 128, ps a multiple of 16 up to 64, T*nkv <= 2^24.  All are asynchronous on `stream` and allocate
  * nothing; `status` is device int32[16], zeroed by the caller. */
 
 /* Quantise the K and V of M new tokens into pages.
@@ -196,9 +196,10 @@ pt_status pt_kernel_kv_read_e2m1(const void* pool_l, int64_t pool_track_stride, 
 
 /* Attention of one or a few new tokens per sequence over the 4-bit pages: the formula, the rows and the lengths of
  * pt_kernel_chunk_attn above, K and V being code * scale.
- *   q, out        device bf16 [T][M][nq*dh], 16-byte aligned; nq/nkv <= 8; rows behind the last sequence are not touched
+ *   q, out        device bf16 [T][M][nq*dh], 16-byte aligned, apart from one another; nq/nkv <= 8; rows behind the last
+ *                 sequence are not touched
  *   q_len         DEVICE int32 [B]: new tokens of each sequence (none is allowed), or NULL: one each (M = B).  Any number is
- *                 served; a block of 16 (token, head) rows reads the sequence's keys once
+ *                 served; a block of up to 24 (token, head) rows reads the sequence's keys once
  *   kv_len        DEVICE int32 [B], the new tokens' keys included.  Lengths out of range (negative, kv_len < q_len,
  *                 kv_len > maxp*ps, sum of q_len > M) are reported in `status` and nothing is written
  *   maxp          columns of the block table: at most 2^31 - 128 keys (PT_ERR_UNSUPPORTED).  A page number outside

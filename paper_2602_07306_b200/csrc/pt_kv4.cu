@@ -1,7 +1,9 @@
 // The 4-bit storage format of the KV cache (pt_kv_dtype PT_KV_E2M1): new tokens' K and V into its pages, and sequences back out.
 //   k_kv4_write   a thread has sixteen consecutive values of a vector, two threads a group of 32
 //   k_kv4_read    a warp has one head's K and V of 16 tokens, in the order in which they lie: 16 bytes a lane and load
-// Both move bytes and compute little.
+// Both are bound by the bytes they move.  Measured (a plain copy: 6.4 TB/s): 8192 tokens of 8 tracks and 8 KV heads of 128 with their
+// values out 99.5 us (608 MB, 6.1 TB/s; with eight values a thread and codes written where they fell 184), contexts of 28 sequences of
+// 0.8-4k keys read back 105 us (638 MB, 6.1 TB/s).
 #include <algorithm>
 #include <type_traits>
 
@@ -284,7 +286,6 @@ int sm_count() {
 }  // namespace
 
 pt_status launch_kv4_write(const Kv4WriteP& p, int dh, cudaStream_t st) {
-    if (p.T > 65535) { set_error("too many tracks for one call"); return PT_ERR_UNSUPPORTED; }
     const cudaError_t e = launch_dependent(dh == 64 ? k_kv4_write<64> : k_kv4_write<128>, dim3((p.M + 15) / 16, p.slab.nkv, p.T), dim3(dh), (size_t)0, st, p);
     if (e != cudaSuccess) { set_error("k_kv4_write launch: %s", cudaGetErrorString(e)); return PT_ERR_CUDA; }
     g_launches.fetch_add(1, std::memory_order_relaxed);
@@ -361,7 +362,8 @@ bool kv4_direct(const int32_t* lens, const int32_t* n_new, int B, int G) {
 using namespace pt;
 
 static pt_status check_shape(const void* pool_l, int64_t stride, int32_t T, int32_t nkv, int32_t dh, int32_t ps, int32_t num_pages) {
-    if (T < 1 || nkv < 1 || num_pages < 1 || stride < 0 || nkv > 65535) { set_error("bad sizes"); return PT_ERR_INVALID_ARG; }
+    if (T < 1 || nkv < 1 || num_pages < 1 || stride < 0) { set_error("bad sizes"); return PT_ERR_INVALID_ARG; }
+    if (T > 65535 || nkv > 65535 || (int64_t)T * nkv > 1 << 24) { set_error("more than 2^24 heads of all tracks, or 65535 tracks or heads"); return PT_ERR_UNSUPPORTED; }
     if (dh != 64 && dh != 128) { set_error("an E2M1 cache needs head_dim 64 or 128"); return PT_ERR_UNSUPPORTED; }
     if (ps < 16 || ps > 64 || ps % 16) { set_error("an E2M1 cache needs pages of a multiple of 16 tokens, 64 at most"); return PT_ERR_UNSUPPORTED; }
     if ((uintptr_t)pool_l % 16 || stride % 16) { set_error("the pool must be 16-byte aligned, its track stride a multiple of 16 bytes"); return PT_ERR_MISALIGNED; }
@@ -416,6 +418,7 @@ extern "C" pt_status pt_kernel_attn_e2m1(const void* q, const void* pool_l, int6
                                          const int32_t* q_len, const int32_t* kv_len, int32_t T, int32_t B, int32_t M, int32_t nq, int32_t nkv, int32_t dh,
                                          int32_t ps, int32_t num_pages, void* out, void* scratch, size_t scratch_bytes, void* status, void* stream) {
     if (!q || !pool_l || !block_table || !kv_len || !out || !scratch || !status) { set_error("null argument"); return PT_ERR_INVALID_ARG; }
+    if (q == out) { set_error("out must not overlap q"); return PT_ERR_INVALID_ARG; }
     if (B < 1 || M < 1 || M > (1 << 26) || nq < 1 || nkv < 1 || nq % nkv || maxp < 1 || (!q_len && M != B)) { set_error("bad sizes"); return PT_ERR_INVALID_ARG; }
     pt_status s = check_shape(pool_l, pool_track_stride, T, nkv, dh, ps, num_pages);
     if (s != PT_OK) return s;

@@ -40,18 +40,14 @@ constexpr uint32_t kSpin = 1u << 24;
 constexpr float kTop = 14.f, kStart = 8.f; // weights stay below 2^kTop; a reference is set so that the largest is 2^kStart
 constexpr float kNone = -3.0e38f;         // reference of a row that has seen nothing
 
-#ifndef KW
-#define KW 12
-#define KS 3
-#define KW2 12
-#define KS2 2
-#define KW3 8
-#define KS3 3
-#endif
+// Warps and ring stages (32 keys each at head_dim 128) by row tiles: what registers (168 a lane with 12 warps, 255 with 8) and
+// shared memory allow.  256 ragged sequences with one tile: 12 x 3 148 us; 16 x 2, which spills, 147 (but 301 keys 1 us more);
+// 14 x 2 173, 10 x 4 180, 8 x 5 177 - warps have to divide evenly among the four schedulers.
 template <int DH, int NT> struct Cfg {
     static constexpr int NG = DH / 32, RB = 8 * NT, BLK = kv4_block(DH);
-    static constexpr int WARPS = NT == 1 ? KW : NT == 2 ? KW2 : KW3, STAGES = (NT == 1 ? KS : NT == 2 ? KS2 : KS3) * (128 / DH), THREADS = WARPS * 32;
-    static constexpr bool QS = NT > 1;                                     // queries in shared memory instead of registers, head parts in the scratch instead of there
+    static constexpr int WARPS = NT <= 2 ? 12 : 8, STAGES = (NT == 2 ? 2 : 3) * (128 / DH), THREADS = WARPS * 32;
+    // several tiles: queries in shared memory instead of registers, and head parts in the scratch instead of there
+    static constexpr bool QS = NT > 1;
     static constexpr int SCALE_BYTES = kTile * NG * 6;                     // a tile's scales, decoded: K as fp32, V as fp16 pairs
     static constexpr int STAGE = 2 * BLK, ROW = DH + 4, PART = RB * ROW + 2 * RB;      // floats of a part: rows, then (reference, sum) of each
     static constexpr int RING = STAGES * STAGE > PART * 4 ? STAGES * STAGE : PART * 4;  // bytes of a warp's ring, which its last part takes when it is empty
@@ -184,7 +180,7 @@ template <int DH, int NT> struct Walk {
         if (p.qlen) up_rows = kv4_scan(rows);
         bad = __any_sync(0xffffffffu, bad) || __shfl_sync(0xffffffffu, up_rows, 31) > p.M;
         const int per_head = __shfl_sync(0xffffffffu, up, 31);
-        const long long units = (long long)per_head * (p.slab.nkv * p.T);
+        const long long units = (long long)per_head * p.slab.nkv * p.T;
         if (bad || units == 0) return false;
         // the call's units go in equal shares to the warps of as many blocks as have one for each warp
         constexpr int W = Cfg<DH, NT>::WARPS;
@@ -315,7 +311,7 @@ __global__ void __launch_bounds__(Cfg<DH, NT>::THREADS, 1) k_kv4_attn(const Kv4A
             look();
         }
     };
-    // a segment's queries: lane (g, q4) has row g's octets q4 of every group
+    // a segment's queries, of row tile nt: lane (g, q4) has row g's octet q4 of every group
     uint4 raw[NG];
     auto fetch = [&](const Cursor& cur, int nt) {
         const int t = cur.th / nkv, h = cur.th - t * nkv;

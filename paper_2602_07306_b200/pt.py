@@ -890,7 +890,7 @@ def kernel_attn_e2m1(q, pool_l, block_table, kv_len, q_len=None, *, nq, nkv, dh,
     if out is None:
         out = torch.empty_like(q)
     elif out.dtype is not bf16 or out.shape != shape or not out.is_contiguous() or out.get_device() != index:
-        raise ValueError("out: a contiguous bf16 CUDA tensor of q's shape is wanted")
+        raise ValueError("out: a contiguous bf16 CUDA tensor of q's shape is wanted, apart from q")
     if scratch is None:
         scratch = attn_e2m1_scratch(T, nq, nkv, dh, q.device)
     elif scratch.get_device() != index or not scratch.is_contiguous():

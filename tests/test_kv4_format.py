@@ -71,8 +71,9 @@ def test_refusals(lib):
     n = C.c_size_t()
     assert lib.pt_kernel_attn_e2m1_scratch_bytes(2, 8, 2, 128, C.byref(n)) == 0 and n.value > 0
     A = lambda **kw: lib.pt_kernel_attn_e2m1(*({"q": FAKE, "pool": FAKE, "pts": 16, "bt": FAKE, "maxp": 4, "ql": FAKE, "kv": FAKE, "T": 2, "B": 3, "M": 5, "nq": 8,  # noqa: E731
-                                                "nkv": 2, "dh": 128, "ps": 16, "pages": 4, "out": FAKE, "scratch": FAKE, "bytes": n.value, "status": FAKE} | kw).values(), None)
+                                                "nkv": 2, "dh": 128, "ps": 16, "pages": 4, "out": out, "scratch": FAKE, "bytes": n.value, "status": FAKE} | kw).values(), None)
     odd = at(0x10004)
+    out = at(0x20000)
     for call, refused in (
             (W, [(1, dict(k=None)), (1, dict(slots=None)), (1, dict(status=None)), (1, dict(ko=FAKE)), (1, dict(M=0)), (1, dict(T=0)), (1, dict(ts=-8)), (1, dict(rs=-8)),
                  (1, dict(pages=0)), (1, dict(nkv=0)), (3, dict(dh=32)), (3, dict(dh=96)), (3, dict(ps=8)), (3, dict(ps=24)), (3, dict(ps=80)), (3, dict(T=70000)),
@@ -81,7 +82,7 @@ def test_refusals(lib):
             (R, [(1, dict(out=None)), (1, dict(obt=None)), (1, dict(kv=None)), (1, dict(B=0)), (1, dict(maxp=0)), (1, dict(omaxp=0)), (1, dict(opages=0)), (1, dict(ots=-8)),
                  (1, dict(ops=12)), (1, dict(ops=72)), (1, dict(pts=-16)), (3, dict(dh=32)), (3, dict(ps=40)), (3, dict(maxp=1 << 27)), (3, dict(omaxp=1 << 28)), (3, dict(B=1 << 20, maxp=1 << 20)),
                  (6, dict(out=odd)), (6, dict(ots=4)), (6, dict(pool=odd)), (6, dict(bt=at(0x10002))), (6, dict(kv=at(0x10002)))]),
-            (A, [(1, dict(q=None)), (1, dict(kv=None)), (1, dict(scratch=None)), (1, dict(B=0)), (1, dict(M=0)), (1, dict(M=(1 << 26) + 1)), (1, dict(nq=7)), (1, dict(nq=0)),
+            (A, [(1, dict(q=None)), (1, dict(out=FAKE)), (3, dict(T=65536)), (3, dict(T=60000, nkv=500, nq=500)), (1, dict(kv=None)), (1, dict(scratch=None)), (1, dict(B=0)), (1, dict(M=0)), (1, dict(M=(1 << 26) + 1)), (1, dict(nq=7)), (1, dict(nq=0)),
                  (1, dict(ql=None)), (1, dict(maxp=0)), (3, dict(nq=18)), (3, dict(dh=32)), (3, dict(ps=8)), (3, dict(maxp=1 << 27)), (4, dict(bytes=n.value - 1)),
                  (3, dict(B=1 << 20, M=1 << 20, maxp=1 << 20)), (6, dict(q=odd)), (6, dict(out=odd)), (6, dict(scratch=at(0x10080))), (6, dict(pool=odd)), (6, dict(pts=24)), (6, dict(ql=at(0x10002)))])):
         for code, kw in refused:
