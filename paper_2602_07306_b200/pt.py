@@ -772,10 +772,9 @@ def kernel_chunk_attn(q, pool_l, block_table, q_len, kv_len, *, nq, nkv, dh, ps,
     return out, status
 
 
-def _kv4_pool(pool_l, T, nkv, dh, ps, index):
+def _kv4_pool(torch, pool_l, T, nkv, dh, ps, index):
     """Checks one layer of an E2M1 pool: uint8 [T, pages, nkv, ps // 16, 17 * dh], contiguous but for the track stride.
-    Returns (pages, bytes between tracks)."""
-    import torch
+    Returns (pages, bytes between tracks).  (torch is handed on: an import in every helper costs as much as its checks.)"""
     shape = pool_l.shape
     if len(shape) == 5:
         tracks, pages, heads, blocks, size = shape
@@ -796,15 +795,14 @@ def _kv4_int(name, a, shape, dtype, index):
     return a.data_ptr()
 
 
-def _kv4_table(name, a, rows, index):
-    import torch
-    if a.dim() != 2 or a.shape[0] != rows or a.dtype is not torch.int32 or a.get_device() != index or not a.is_contiguous():
+def _kv4_table(torch, name, a, rows, index):
+    shape = a.shape
+    if len(shape) != 2 or shape[0] != rows or a.dtype is not torch.int32 or a.get_device() != index or not a.is_contiguous():
         raise ValueError(f"{name}: a contiguous int32 tensor [{rows}, columns] on CUDA device {index} is wanted")
-    return a.data_ptr(), a.shape[1]
+    return a.data_ptr(), shape[1]
 
 
-def _kv4_status(status, index):
-    import torch
+def _kv4_status(torch, status, index):
     if status is None:
         return _new_status(index)
     if status.dtype is not torch.int32 or status.numel() < 16 or not status.is_contiguous() or status.get_device() != index:
@@ -822,7 +820,7 @@ def kernel_kv_write_e2m1(k, v, pool_l, slots, *, nkv, dh, ps, k_out=None, v_out=
             or v.dtype is not bf16 or v.shape != shape or v.stride() != stride or v.get_device() != index:
         raise ValueError("k, v: bf16 CUDA tensors [T, M, nkv*dh] of the same strides with contiguous values are wanted")
     T, M, _ = shape
-    pages, pstride = _kv4_pool(pool_l, T, nkv, dh, ps, index)
+    pages, pstride = _kv4_pool(torch, pool_l, T, nkv, dh, ps, index)
     at = _kv4_int("slots", slots, (M,), torch.int64, index)
     ko = vo = None
     if k_out is not None or v_out is not None:
@@ -830,7 +828,7 @@ def kernel_kv_write_e2m1(k, v, pool_l, slots, *, nkv, dh, ps, k_out=None, v_out=
             if a is None or a.dtype is not bf16 or a.shape != shape or not a.is_contiguous() or a.get_device() != index:
                 raise ValueError("k_out, v_out: both or neither, contiguous bf16 CUDA tensors of k's shape")
         ko, vo = k_out.data_ptr(), v_out.data_ptr()
-    status = _kv4_status(status, index)
+    status = _kv4_status(torch, status, index)
     if M:
         _call(index, lib().pt_kernel_kv_write_e2m1, k.data_ptr(), v.data_ptr(), stride[0] if T > 1 else 0, stride[1] if M > 1 else 0, T, M, nkv, dh, ps,
               pages, pool_l.data_ptr(), pstride, at, ko, vo, status.data_ptr())
@@ -854,12 +852,12 @@ def kernel_kv_read_e2m1(pool_l, block_table, kv_len, out, out_table, *, nkv, dh,
             two = 0
     if two != 2 or heads != nkv or width != dh or not T or not opages:
         raise ValueError("out: a bf16 CUDA tensor [T, pages, 2, nkv, out_ps, dh] with contiguous tracks is wanted")
-    pages, pstride = _kv4_pool(pool_l, T, nkv, dh, ps, index)
+    pages, pstride = _kv4_pool(torch, pool_l, T, nkv, dh, ps, index)
     B = kv_len.numel()
     lens = _kv4_int("kv_len", kv_len, (B,), torch.int32, index)
-    bt, maxp = _kv4_table("block_table", block_table, B, index)
-    obt, omaxp = _kv4_table("out_table", out_table, B, index)
-    status = _kv4_status(status, index)
+    bt, maxp = _kv4_table(torch, "block_table", block_table, B, index)
+    obt, omaxp = _kv4_table(torch, "out_table", out_table, B, index)
+    status = _kv4_status(torch, status, index)
     _call(index, lib().pt_kernel_kv_read_e2m1, pool_l.data_ptr(), pstride, bt, maxp, lens, T, B, nkv, dh, ps, pages, out.data_ptr(), ostride if T > 1 else 0,
           obt, omaxp, ops, opages, status.data_ptr())
     return out, status
@@ -882,11 +880,11 @@ def kernel_attn_e2m1(q, pool_l, block_table, kv_len, q_len=None, *, nq, nkv, dh,
     if len(shape) != 3 or shape[2] != nq * dh or q.dtype is not bf16 or not q.is_contiguous() or index < 0:
         raise ValueError("q: a contiguous bf16 CUDA tensor [T, M, nq*dh] is wanted")
     T, M, _ = shape
-    pages, pstride = _kv4_pool(pool_l, T, nkv, dh, ps, index)
+    pages, pstride = _kv4_pool(torch, pool_l, T, nkv, dh, ps, index)
     B = kv_len.numel()
     lens = _kv4_int("kv_len", kv_len, (B,), torch.int32, index)
     news = None if q_len is None else _kv4_int("q_len", q_len, (B,), torch.int32, index)
-    bt, maxp = _kv4_table("block_table", block_table, B, index)
+    bt, maxp = _kv4_table(torch, "block_table", block_table, B, index)
     if out is None:
         out = torch.empty_like(q)
     elif out.dtype is not bf16 or out.shape != shape or not out.is_contiguous() or out.get_device() != index:
@@ -895,7 +893,7 @@ def kernel_attn_e2m1(q, pool_l, block_table, kv_len, q_len=None, *, nq, nkv, dh,
         scratch = attn_e2m1_scratch(T, nq, nkv, dh, q.device)
     elif scratch.get_device() != index or not scratch.is_contiguous():
         raise ValueError("scratch: a contiguous tensor on the call's device is wanted")
-    status = _kv4_status(status, index)
+    status = _kv4_status(torch, status, index)
     if M:
         _call(index, lib().pt_kernel_attn_e2m1, q.data_ptr(), pool_l.data_ptr(), pstride, bt, maxp, news, lens, T, B, M, nq, nkv, dh, ps, pages,
               out.data_ptr(), scratch.data_ptr(), scratch.nbytes, status.data_ptr())
