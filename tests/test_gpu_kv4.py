@@ -467,3 +467,54 @@ def test_two_streams_at_once():
     torch.cuda.synchronize()
     for a, o in zip(alone, outs):
         assert all(torch.equal(a, x) for x in o)
+
+
+def test_a_captured_step_replayed():
+    """Write, attention and read back of one decode step in a graph: replayed with other tokens, slots and lengths."""
+    import torch
+    from paper_2602_07306_b200 import pt
+    T, B, nq, nkv, dh, ps = 2, 3, 8, 2, 128, 16
+    rng = np.random.default_rng(4)
+    bt = rng.permutation(30)[:B * 8].reshape(B, 8).astype(np.int32)
+    shape = dict(nkv=nkv, dh=dh, ps=ps)
+    pool = torch.zeros((T, 30, nkv, 1, 17 * dh), dtype=torch.uint8, device="cuda")
+    first = np.concatenate([bt[b, np.arange(60) // ps] * ps + np.arange(60) % ps for b in range(B)]).astype(np.int64)
+    k0, v0 = (bf(rng.standard_normal((T, B * 60, nkv * dh))) for _ in range(2))
+    pt.kernel_kv_write_e2m1(k0, v0, pool, torch.from_numpy(first).cuda(), **shape)
+    k, v, q = (torch.zeros((T, B, h * dh), dtype=torch.bfloat16, device="cuda") for h in (nkv, nkv, nq))
+    slots, lens, table = torch.full((B,), -1, dtype=torch.int64, device="cuda"), i32([60] * B), i32(bt)
+    out, flat = torch.zeros_like(q), torch.zeros((T, B * 8, 2, nkv, 16, dh), dtype=torch.bfloat16, device="cuda")
+    obt, scratch, status = i32(np.arange(B * 8).reshape(B, 8)), pt.attn_e2m1_scratch(T, nq, nkv, dh), torch.zeros(16, dtype=torch.int32, device="cuda")
+
+    def step():
+        pt.kernel_kv_write_e2m1(k, v, pool, slots, status=status, **shape)
+        pt.kernel_attn_e2m1(q, pool, table, lens, nq=nq, out=out, scratch=scratch, status=status, **shape)
+        pt.kernel_kv_read_e2m1(pool, table, lens, flat, obt, status=status, **shape)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        step()
+        side.synchronize()
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g, stream=side):
+            step()
+    torch.cuda.current_stream().wait_stream(side)
+    for n in (61, 62, 63):
+        for x in (k, v, q):
+            x.copy_(bf(rng.standard_normal(x.shape)))
+        slots.copy_(torch.from_numpy((bt[:, (n - 1) // ps] * ps + (n - 1) % ps).astype(np.int64)))
+        lens.copy_(i32([n] * B))
+        g.replay()
+        torch.cuda.synchronize()
+        got, copy = out.clone(), flat.clone()
+        other = torch.empty_like(out)
+        pt.kernel_attn_e2m1(q, pool, table, lens, nq=nq, out=other, **shape)
+        want, _ = pt.kernel_chunk_attn(q, copy, obt, i32([1] * B), lens, nq=nq, nkv=nkv, dh=dh, ps=16)
+        assert status[0] == 0 and torch.equal(got, other)
+        top = copy.float().abs().amax()
+        assert ((got.float() - want.float()).abs() <= 2.0 ** -7 * want.float().abs() + (2.0 ** -8 + 2.0 ** -10 + 2.0 ** -12) * top).all()
+        values = kv4.get(pool.cpu().numpy())
+        for b in range(B):
+            last = values[:, bt[b, (n - 1) // ps], :, :, (n - 1) % ps]
+            np.testing.assert_array_equal(last[:, 0].reshape(T, -1), kv4.values(*kv4.quantize(k[:, b].float().cpu().numpy().reshape(T, nkv, dh))).reshape(T, -1))
+            np.testing.assert_array_equal(copy.float().cpu().numpy()[:, b * 8 + (n - 1) // 16, :, :, (n - 1) % 16], last)
