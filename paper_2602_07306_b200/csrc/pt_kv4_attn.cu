@@ -12,8 +12,8 @@
 //  * The order of a block of 16 tokens is that of the instruction's operands: a lane loads its codes of K (two tokens, 32 dims
 //    each) and V (four tokens, 16 dims each) with 128-bit loads free of bank conflicts.  Of V a byte holds two dims of one
 //    token and the operand wants two tokens of one dim: eight codes of two tokens change places in four instructions.
-//  * A scale of K multiplies the partial score of its group in fp32, a scale of V the weights, once for 32 dims: codes enter
-//    the products as they are.  The weights are f16: their reference (m above) lags behind the maximum by up to 2^6 and is
+//  * A scale of K multiplies the partial score of its group in fp32 (with several row tiles: its codes, exactly), a scale of V
+//    the weights, once for 32 dims: codes enter the products as they are.  The weights are f16: their reference (m above) lags behind the maximum by up to 2^6 and is
 //    chosen so that weight times scale stays below 2^16; a scale of V of 2 or more makes room by raising it.  q is divided
 //    by a power of two that puts a row's largest magnitude at 2^13, K codes are below 8, sums are fp32.
 //  * A warp works alone: a ring of 32-key stages filled by bulk copies (a block of 16 tokens, K, V and scales, is one piece
@@ -48,6 +48,8 @@ template <int DH, int NT> struct Cfg {
     static constexpr int WARPS = NT <= 2 ? 12 : 8, STAGES = (NT == 2 ? 2 : 3) * (128 / DH), THREADS = WARPS * 32;
     // several tiles: queries in shared memory instead of registers, and head parts in the scratch instead of there
     static constexpr bool QS = NT > 1;
+    // K's scales multiply its codes, 64 instructions a tile, instead of the partial scores, 32 for each row tile (20 rows: 84 to 82 us)
+    static constexpr bool KOP = NT > 1;
     static constexpr int SCALE_BYTES = kTile * NG * 6;                     // a tile's scales, decoded: K as fp32, V as fp16 pairs
     static constexpr int STAGE = 2 * BLK, ROW = DH + 4, PART = RB * ROW + 2 * RB;      // floats of a part: rows, then (reference, sum) of each
     static constexpr int RING = STAGES * STAGE > PART * 4 ? STAGES * STAGE : PART * 4;  // bytes of a warp's ring, which its last part takes when it is empty
@@ -89,6 +91,19 @@ __device__ __forceinline__ uint32_t mul2(uint32_t a, uint32_t b) {
     uint32_t d;
     asm("mul.rn.f16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
     return d;
+}
+// K's scales of a word as the scores take them, in order: fp32, or (OP: they multiply the operand) fp16 pairs of 2^-4 of each,
+// which keeps six times the largest inside fp16 and the product with a code exact
+template <bool OP> __device__ __forceinline__ void k_scales(uint32_t even, uint32_t odd, uint32_t* f) {
+    if constexpr (OP) {
+        even = mul2(even, 0x2c002c00u);
+        odd = mul2(odd, 0x2c002c00u);
+        f[0] = __byte_perm(even, even, 0x1010); f[1] = __byte_perm(odd, odd, 0x1010);
+        f[2] = __byte_perm(even, even, 0x3232); f[3] = __byte_perm(odd, odd, 0x3232);
+    } else {
+        const float2 a = __half22float2(*reinterpret_cast<__half2*>(&even)), b = __half22float2(*reinterpret_cast<__half2*>(&odd));
+        f[0] = __float_as_uint(a.x); f[1] = __float_as_uint(b.x); f[2] = __float_as_uint(a.y); f[3] = __float_as_uint(b.y);
+    }
 }
 __device__ __forceinline__ uint32_t transpose8x8(uint32_t a) {
     uint32_t d;
@@ -350,7 +365,7 @@ __global__ void __launch_bounds__(Cfg<DH, NT>::THREADS, 1) k_kv4_attn(const Kv4A
             if (top >= 0x7f80u) e = 13;                   // not finite: as it is
             e = max(e, -100);
             const float inv = __uint_as_float((uint32_t)(13 - e + 127) << 23);
-            const float un = __uint_as_float((uint32_t)(e - 13 + 127) << 23) * p.scale_log2;
+            const float un = __uint_as_float((uint32_t)(e - 13 + 127) << 23) * (C::KOP ? 16.f * p.scale_log2 : p.scale_log2);
 #pragma unroll
             for (int j = 0; j < NG; ++j) {
                 const uint32_t w[4] = {raw[j].x, raw[j].y, raw[j].z, raw[j].w};
@@ -390,7 +405,7 @@ __global__ void __launch_bounds__(Cfg<DH, NT>::THREADS, 1) k_kv4_attn(const Kv4A
             uint32_t high;
             {
                 const int hb = lane >> 4, l = lane & 15;
-                uint32_t kb = 0, vb = 0, even, odd;
+                uint32_t kb = 0, vb = 0, even, odd, f[4];
                 if constexpr (NG == 4) {
                     lds<1>(base + hb * C::BLK + kv4_codes(DH) + l * 4, &kb);
                     lds<1>(base + hb * C::BLK + 2 * kv4_codes(DH) + kv4_scales(DH) + l * 4, &vb);
@@ -399,8 +414,8 @@ __global__ void __launch_bounds__(Cfg<DH, NT>::THREADS, 1) k_kv4_attn(const Kv4A
                         vb &= nv == 4 ? 0xffffffffu : (1u << (8 * nv)) - 1u;
                     }
                     scales4(kb, even, odd);
-                    const float2 a = __half22float2(*reinterpret_cast<__half2*>(&even)), b = __half22float2(*reinterpret_cast<__half2*>(&odd));
-                    asm volatile("st.shared.v4.f32 [%0], {%1, %2, %3, %4};" ::"r"(dec + lane * 16), "f"(a.x), "f"(b.x), "f"(a.y), "f"(b.y) : "memory");
+                    k_scales<C::KOP>(even, odd, f);
+                    asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(dec + lane * 16), "r"(f[0]), "r"(f[1]), "r"(f[2]), "r"(f[3]) : "memory");
                     scales4(vb, even, odd);
                     asm volatile("st.shared.v2.u32 [%0], {%1, %2};" ::"r"(dec + kTile * 16 + lane * 8), "r"(even), "r"(odd) : "memory");
                 } else if (l < 8) {                               // two groups: a word of K's has two keys, eight words of V's are a block's
@@ -411,8 +426,8 @@ __global__ void __launch_bounds__(Cfg<DH, NT>::THREADS, 1) k_kv4_attn(const Kv4A
                         vb &= nv == 4 ? 0xffffffffu : (1u << (8 * nv)) - 1u;
                     }
                     scales4(kb, even, odd);
-                    const float2 a = __half22float2(*reinterpret_cast<__half2*>(&even)), b = __half22float2(*reinterpret_cast<__half2*>(&odd));
-                    asm volatile("st.shared.v4.f32 [%0], {%1, %2, %3, %4};" ::"r"(dec + (hb * 8 + l) * 16), "f"(a.x), "f"(b.x), "f"(a.y), "f"(b.y) : "memory");
+                    k_scales<C::KOP>(even, odd, f);
+                    asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(dec + (hb * 8 + l) * 16), "r"(f[0]), "r"(f[1]), "r"(f[2]), "r"(f[3]) : "memory");
                     scales4(vb, even, odd);
                     asm volatile("st.shared.v2.u32 [%0], {%1, %2};" ::"r"(dec + kTile * 8 + (hb * 8 + l) * 8), "r"(even), "r"(odd) : "memory");
                 }
@@ -434,6 +449,10 @@ __global__ void __launch_bounds__(Cfg<DH, NT>::THREADS, 1) k_kv4_attn(const Kv4A
                     uint32_t h0[4], h1[4];
                     kv4_codes8(kw[0][j], h0);
                     kv4_codes8(kw[1][j], h1);
+                    if constexpr (C::KOP) {
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) { h0[i] = mul2(h0[i], ks[j]); h1[i] = mul2(h1[i], ks[NG + j]); }
+                    }
 #pragma unroll
                     for (int nt = 0; nt < NT; ++nt) {
                         float c[4];
@@ -444,12 +463,18 @@ __global__ void __launch_bounds__(Cfg<DH, NT>::THREADS, 1) k_kv4_attn(const Kv4A
 #pragma unroll
                             for (int i = 0; i < 4; ++i) f[i] = qf[j][nt][i];
                         }
-                        mma0(c, h0[0], h1[0], h0[1], h1[1], f[0], f[1]);
-                        mma(c, h0[2], h1[2], h0[3], h1[3], f[2], f[3]);
+                        if constexpr (C::KOP) {
+                            if (j) mma(s[hb][nt], h0[0], h1[0], h0[1], h1[1], f[0], f[1]);
+                            else mma0(s[hb][nt], h0[0], h1[0], h0[1], h1[1], f[0], f[1]);
+                            mma(s[hb][nt], h0[2], h1[2], h0[3], h1[3], f[2], f[3]);
+                        } else {
+                            mma0(c, h0[0], h1[0], h0[1], h1[1], f[0], f[1]);
+                            mma(c, h0[2], h1[2], h0[3], h1[3], f[2], f[3]);
 #pragma unroll
-                        for (int i = 0; i < 4; ++i) {
-                            const float f = __uint_as_float(ks[(i >> 1) * NG + j]);
-                            s[hb][nt][i] = j ? fmaf(c[i], f, s[hb][nt][i]) : c[i] * f;
+                            for (int i = 0; i < 4; ++i) {
+                                const float f = __uint_as_float(ks[(i >> 1) * NG + j]);
+                                s[hb][nt][i] = j ? fmaf(c[i], f, s[hb][nt][i]) : c[i] * f;
+                            }
                         }
                     }
                 }
@@ -807,7 +832,7 @@ template <int DH> static pt_status launch_dh(const Kv4AttnP& p, int tiles, void*
 
 pt_status launch_kv4_attn(const Kv4AttnP& p, int dh, void* scratch, cudaStream_t st) {
     // The mean number of (token, head) rows of a sequence in as few passes over its keys as can be, in equal shares: up to three
-    // tiles of 8 rows a pass.  (Four sequences of 20k keys, 4 tracks, 4 KV heads: 44, 67 and 86 us a pass of 1, 2 and 3 tiles;
+    // tiles of 8 rows a pass.  (Four sequences of 20k keys, 4 tracks, 4 KV heads: 43, 67 and 83 us a pass of 1, 2 and 3 tiles;
     // with four, whose accumulators take 128 registers a lane, 134 us, as much as two passes of two.)
     const int64_t rows = p.qlen ? ((int64_t)p.M * (p.nq / p.slab.nkv) + p.B - 1) / p.B : 1, eights = (rows + 7) / 8, passes = (eights + 2) / 3;
     const int tiles = (int)((eights + passes - 1) / passes);
