@@ -494,6 +494,30 @@ __global__ void __launch_bounds__(Cfg<DH, NT>::THREADS, 1) k_kv4_attn(const Kv4A
                             for (int i = 0; i < 2; ++i)
                                 if (16 * hb + i >= end) s[hb][nt][2 * i + c] = -INFINITY;
                     }
+                // a group of V that is not finite must not meet the weights 0 of rows that do not see it: its codes are 0, its
+                // scale is made 0, and the others' sums become NaN here
+                const uint32_t nan = __vcmpeq4(high, 0xffffffffu);
+                if (__any_sync(0xffffffffu, nan != 0)) {
+                    uint32_t even, odd;
+                    high &= ~nan;
+                    scales4(high, even, odd);
+                    const int hb = lane >> 4, l = lane & 15;
+                    if (l < 4 * NG) asm volatile("st.shared.v2.u32 [%0], {%1, %2};" ::"r"(dec + kTile * NG * 4 + (hb * 4 * NG + l) * 8), "r"(even), "r"(odd) : "memory");
+                    __syncwarp();
+                    const int mine = nan ? 16 * hb + l / NG * 4 + (__ffs(nan) - 1) / 8 : kTile;
+#pragma unroll
+                    for (int j = 0; j < NG; ++j) {
+                        const int first = __reduce_min_sync(0xffffffffu, l % NG == j ? mine : kTile);
+#pragma unroll
+                        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                            for (int c = 0; c < 2; ++c)
+                                if (first < kTile && key0 + first <= at.K - at.S + min((at.rb * RB + nt * 8 + 2 * q4 + c) / G, at.S - 1)) {
+#pragma unroll
+                                    for (int mt = 0; mt < 2; ++mt) o[j][mt][nt][c] = o[j][mt][nt][2 + c] = __uint_as_float(0x7fffffffu);
+                                }
+                    }
+                }
             }
             float mx[NT][2];
             bool over = (high & 0x80808080u) != 0;

@@ -303,6 +303,32 @@ def test_attention_nan_and_infinities():
     assert np.isnan(got2[0, 3]).all() and np.array_equal(got2[0, 2], got[0, 2], equal_nan=True) and np.array_equal(got2[1:4], got[1:4])
 
 
+@pytest.mark.parametrize("nq,nkv,dh,S,K", [(2, 2, 128, 8, 60), (2, 2, 64, 5, 33), (8, 2, 128, 4, 70), (8, 2, 64, 4, 200), (16, 2, 128, 3, 50), (10, 2, 64, 4, 31), (4, 1, 128, 40, 90),
+                                          (1, 1, 64, 70, 70), (2, 1, 128, 3, 3000)])
+def test_attention_values_that_are_not_finite_stay_with_the_rows_that_see_them(nq, nkv, dh, S, K):
+    """The same call with zeros in their groups gives the other rows, and the other columns, bit for bit."""
+    G, mid = nq // nkv, K - S + S // 2
+    def make(fill):
+        def at(x, bt):
+            for key, head, group, value in ((mid, 0, 1, fill and np.nan), (mid, nkv - 1, 0, fill and -np.inf), (K - 1, nkv - 1, dh // 32 - 1, fill and np.inf)):
+                x[1, 0, bt[0, key // 16], head, key % 16, 32 * group:32 * group + 32] = 0
+                x[1, 0, bt[0, key // 16], head, key % 16, 32 * group + 7] = value
+        return at
+    q = queries(1, S, nq, dh, 8)
+    got = []
+    for fill in (0, 1):
+        pool, _, bt = cache(1, nkv, dh, 16, [K], 8, make=make(fill))
+        out, st = attend(q, pool, bt, [K], [S], 16, nkv)
+        assert st == [0, 0]
+        got.append(out.float().cpu().numpy()[0])
+    want = got[0]
+    assert np.isfinite(want).all()
+    want[S // 2:, :G, 32:64] = np.nan
+    want[S // 2:, nq - G:, :32] = np.nan
+    want[S - 1:, nq - G:, dh - 32:] = np.nan
+    assert np.array_equal(got[1], want, equal_nan=True)
+
+
 def test_attention_bad_pages_and_lengths_are_reported():
     pool, values, bt = cache(2, 2, 128, 16, [60, 40, 20], 4)
     q = queries(2, 3, 4, 128, 4)
