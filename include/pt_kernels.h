@@ -207,7 +207,9 @@ pt_status pt_kernel_kv_read_e2m1(const void* pool_l, int64_t pool_track_stride, 
  *   scratch       device, 256-byte aligned, >= pt_kernel_attn_e2m1_scratch_bytes: partial results of key ranges; contents
  *                 need not be kept, but calls that may run at the same time need one each
  * Scores, sums and accumulators are fp32; q (divided by the power of two at its row's largest magnitude) and the weights
- * times the scales of V are rounded to fp16.  What lies behind a sequence's last key is never used, and a K or V that is not
+ * times the scales of V (divided by a power of two near the largest among the 32 keys 32 i .. 32 i + 31 and the 32 columns of
+ * a group) are rounded to fp16.  A weight times a scale of less than 2^-28 of the row's largest weight times that largest scale
+ * may be lost, and so may a scale of less than 2^-20 of it; nothing depends on the scales of other groups or tiles.  What lies behind a sequence's last key is never used, and a K or V that is not
  * finite touches no row that does not see it.  A visible score that is NaN, or visible scores that are all -inf, make the
  * row's head NaN; a visible V that is not finite the 32 columns of its group. */
 pt_status pt_kernel_attn_e2m1_scratch_bytes(int32_t T, int32_t nq, int32_t nkv, int32_t dh, size_t* bytes);

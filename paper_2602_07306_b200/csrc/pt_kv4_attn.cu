@@ -13,9 +13,11 @@
 //    each) and V (four tokens, 16 dims each) with 128-bit loads free of bank conflicts.  Of V a byte holds two dims of one
 //    token and the operand wants two tokens of one dim: eight codes of two tokens change places in four instructions.
 //  * A scale of K multiplies the partial score of its group in fp32 (with several row tiles: its codes, exactly), a scale of V
-//    the weights, once for 32 dims: codes enter the products as they are.  The weights are f16: their reference (m above) lags behind the maximum by up to 2^6 and is
-//    chosen so that weight times scale stays below 2^16; a scale of V of 2 or more makes room by raising it.  q is divided
-//    by a power of two that puts a row's largest magnitude at 2^13, K codes are below 8, sums are fp32.
+//    the weights, once for 32 dims.  Weight times scale is one f16 number, kept within f16's normal range from both sides: the
+//    weights' reference (m above) lags behind the maximum by up to 2^6, so that a part's largest weight is 2^8 to 2^14, and the
+//    scales of a group of 32 columns are divided by a power of two that puts the largest of the tile's into [2^-5, 2).  The fp32
+//    sums of the group carry that power and are rescaled, exactly, where it changes, which in ordinary data is once a segment.
+//    q is divided by a power of two that puts a row's largest magnitude at 2^13, K codes are below 8, sums are fp32.
 //  * A warp works alone: a ring of 32-key stages filled by bulk copies (a block of 16 tokens, K, V and scales, is one piece
 //    of 17 * dh bytes), its own plan from the device's lengths, its own contiguous share of all key tiles of the call, so
 //    that no barrier stands in the loop and a captured call may be replayed with other lengths.  A segment (sequence, track, KV
@@ -38,6 +40,10 @@ constexpr int kSegCost = 2;               // cost of beginning a segment, in til
 constexpr int kWholeTiles = 3;            // tiles of a warp up to which a block takes a whole segment: 1000 keys 11.1 us (12.8 cut up), 1500 keys 12.8 (12.0)
 constexpr uint32_t kSpin = 1u << 24;
 constexpr float kTop = 14.f, kStart = 8.f; // weights stay below 2^kTop; a reference is set so that the largest is 2^kStart
+// V's unit 2^e of a group (e >= -14): the tile's largest scale of the group is in [2^(e - kBand), 2^(e + 1)), as fp16 bits in the
+// upper half of a word from (e + 15 - kBand) << 26 on
+constexpr int kBand = 5;
+constexpr uint32_t kBandBits = (uint32_t)(kBand + 1) << 26;
 constexpr float kNone = -3.0e38f;         // reference of a row that has seen nothing
 
 // Warps and ring stages (32 keys each at head_dim 128) by row tiles: what registers (168 a lane with 12 warps, 255 with 8) and
@@ -121,6 +127,11 @@ __device__ __forceinline__ void mma0(float* c, uint32_t a0, uint32_t a1, uint32_
 }
 // four scale bytes (low first) -> fp16 pairs (bytes 0 and 2), (bytes 1 and 3)
 __device__ __forceinline__ void scales4(uint32_t w, uint32_t& even, uint32_t& odd) { even = (w << 7) & 0x7f807f80u; odd = (w >> 1) & 0x7f807f80u; }
+// the largest of them, in the upper half of a word whose lower half is below every border of a comparison
+__device__ __forceinline__ uint32_t top_scale(uint32_t even, uint32_t odd) {
+    const uint32_t m = __vmaxu2(even, odd);
+    return __vmaxu2(m, m << 16);
+}
 template <int N> __device__ __forceinline__ void lds(uint32_t at, uint32_t* w) {
     if constexpr (N == 4) asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]) : "r"(at));
     else if constexpr (N == 2) asm volatile("ld.shared.v2.u32 {%0, %1}, [%2];" : "=r"(w[0]), "=r"(w[1]) : "r"(at));
@@ -388,7 +399,8 @@ __global__ void __launch_bounds__(Cfg<DH, NT>::THREADS, 1) k_kv4_attn(const Kv4A
         for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
             for (int c = 0; c < 2; ++c) { ref[nt][c] = kNone; l[nt][c] = 0.f; }
-        float room = kTop;                                        // weights stay below 2^room
+        int e_v = -14;                                            // V's unit of group lane % NG
+        uint32_t inv_v = 0x74007400u;                             // 2^-e_v, an fp16 pair
         for (int tile = cursors[warp][0].lo; tile < hi; ++tile) {
             bool ok = mbar_try(&bars[slot], parity);
             if (!__all_sync(0xffffffffu, ok)) {
@@ -403,6 +415,7 @@ __global__ void __launch_bounds__(Cfg<DH, NT>::THREADS, 1) k_kv4_attn(const Kv4A
             const int key0 = tile * kTile;
             // ---- the tile's scales, each decoded once: lane l has key l's of K and word l (block, q, group) of V's
             uint32_t high;
+            bool over;                                            // a scale of V out of its unit's band
             {
                 const int hb = lane >> 4, l = lane & 15;
                 uint32_t kb = 0, vb = 0, even, odd, f[4];
@@ -417,7 +430,7 @@ __global__ void __launch_bounds__(Cfg<DH, NT>::THREADS, 1) k_kv4_attn(const Kv4A
                     k_scales<C::KOP>(even, odd, f);
                     asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(dec + lane * 16), "r"(f[0]), "r"(f[1]), "r"(f[2]), "r"(f[3]) : "memory");
                     scales4(vb, even, odd);
-                    asm volatile("st.shared.v2.u32 [%0], {%1, %2};" ::"r"(dec + kTile * 16 + lane * 8), "r"(even), "r"(odd) : "memory");
+                    asm volatile("st.shared.v2.u32 [%0], {%1, %2};" ::"r"(dec + kTile * 16 + lane * 8), "r"(mul2(even, inv_v)), "r"(mul2(odd, inv_v)) : "memory");
                 } else if (l < 8) {                               // two groups: a word of K's has two keys, eight words of V's are a block's
                     lds<1>(base + hb * C::BLK + kv4_codes(DH) + l * 4, &kb);
                     lds<1>(base + hb * C::BLK + 2 * kv4_codes(DH) + kv4_scales(DH) + l * 4, &vb);
@@ -429,9 +442,13 @@ __global__ void __launch_bounds__(Cfg<DH, NT>::THREADS, 1) k_kv4_attn(const Kv4A
                     k_scales<C::KOP>(even, odd, f);
                     asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(dec + (hb * 8 + l) * 16), "r"(f[0]), "r"(f[1]), "r"(f[2]), "r"(f[3]) : "memory");
                     scales4(vb, even, odd);
-                    asm volatile("st.shared.v2.u32 [%0], {%1, %2};" ::"r"(dec + kTile * 8 + (hb * 8 + l) * 8), "r"(even), "r"(odd) : "memory");
+                    asm volatile("st.shared.v2.u32 [%0], {%1, %2};" ::"r"(dec + kTile * 8 + (hb * 8 + l) * 8), "r"(mul2(even, inv_v)), "r"(mul2(odd, inv_v)) : "memory");
+                } else {
+                    even = odd = 0;
                 }
                 high = vb;
+                const uint32_t top = top_scale(even, odd);        // of four keys: seldom out of the band where the tile's is in it
+                over = top && top - ((uint32_t)(e_v + 15 - kBand) << 26) >= kBandBits;
                 __syncwarp();
             }
             // ---- scores
@@ -480,7 +497,7 @@ __global__ void __launch_bounds__(Cfg<DH, NT>::THREADS, 1) k_kv4_attn(const Kv4A
                 }
             }
             // ---- weights 2^(score - reference).  The reference lags behind the maximum: it is raised, and what has been summed
-            // scaled down, only where a weight would pass 2^kTop, or where a scale of V of 2 or more has to be made room for
+            // scaled down, only where a weight would pass 2^kTop
             if (key0 + kTile > all_see) {                         // some row does not see all of the tile
                 const Cursor& at = cursors[warp][0];
 #pragma unroll
@@ -502,7 +519,7 @@ __global__ void __launch_bounds__(Cfg<DH, NT>::THREADS, 1) k_kv4_attn(const Kv4A
                     high &= ~nan;
                     scales4(high, even, odd);
                     const int hb = lane >> 4, l = lane & 15;
-                    if (l < 4 * NG) asm volatile("st.shared.v2.u32 [%0], {%1, %2};" ::"r"(dec + kTile * NG * 4 + (hb * 4 * NG + l) * 8), "r"(even), "r"(odd) : "memory");
+                    if (l < 4 * NG) asm volatile("st.shared.v2.u32 [%0], {%1, %2};" ::"r"(dec + kTile * NG * 4 + (hb * 4 * NG + l) * 8), "r"(mul2(even, inv_v)), "r"(mul2(odd, inv_v)) : "memory");
                     __syncwarp();
                     const int mine = nan ? 16 * hb + l / NG * 4 + (__ffs(nan) - 1) / 8 : kTile;
 #pragma unroll
@@ -520,22 +537,34 @@ __global__ void __launch_bounds__(Cfg<DH, NT>::THREADS, 1) k_kv4_attn(const Kv4A
                 }
             }
             float mx[NT][2];
-            bool over = (high & 0x80808080u) != 0;
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
                 for (int c = 0; c < 2; ++c) {
                     mx[nt][c] = fmaxf(fmaxf(s[0][nt][c], s[0][nt][2 + c]), fmaxf(s[1][nt][c], s[1][nt][2 + c]));
-                    over = over || fmaf(mx[nt][c], unit[nt][c], -ref[nt][c]) > room;
+                    over = over || fmaf(mx[nt][c], unit[nt][c], -ref[nt][c]) > kTop;
                 }
             if (__any_sync(0xffffffffu, over)) {
-                float top = 0.f;
+                // V's units: those whose band the tile's largest scale (a NaN does not count) has left move there
+                float shift[NG];
+                {
+                    uint32_t even, odd;
+                    scales4(high & ~__vcmpeq4(high, 0xffffffffu), even, odd);
+                    uint32_t top = top_scale(even, odd);
 #pragma unroll
-                for (int i = 0; i < 4; ++i) top = fmaxf(top, kv4_scale((high >> (8 * i)) & 0xffu));
+                    for (int m = NG; m < 32; m <<= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, m));
+                    const int was = e_v;
+                    if (top && top - ((uint32_t)(e_v + 15 - kBand) << 26) >= kBandBits) {
+                        e_v = max((int)(top >> 26) - 15, -14);
+                        inv_v = (e_v < 15 ? (uint32_t)(15 - e_v) << 10 : 0x200u) * 0x10001u;
+                    }
 #pragma unroll
-                for (int m = 1; m < 32; m <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, m));
-                const float fits = fminf(room, (float)max(0, 15 - ((int)(__float_as_uint(top) >> 23) - 127))), drop = room - fits;
-                room = fits;
+                    for (int j = 0; j < NG; ++j) shift[j] = __uint_as_float((uint32_t)(__shfl_sync(0xffffffffu, was - e_v, j) + 127) << 23);
+                    scales4(high, even, odd);
+                    const int hb = lane >> 4, l = lane & 15;
+                    if (l < 4 * NG) asm volatile("st.shared.v2.u32 [%0], {%1, %2};" ::"r"(dec + kTile * NG * 4 + (hb * 4 * NG + l) * 8), "r"(mul2(even, inv_v)), "r"(mul2(odd, inv_v)) : "memory");
+                    __syncwarp();
+                }
 #pragma unroll
                 for (int nt = 0; nt < NT; ++nt) {
                     float corr[2];
@@ -545,8 +574,8 @@ __global__ void __launch_bounds__(Cfg<DH, NT>::THREADS, 1) k_kv4_attn(const Kv4A
                         m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 4));
                         m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 8));
                         m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, 16)) * unit[nt][c];
-                        float nr = ref[nt][c] + drop;
-                        if (m - nr > room) nr = m - fminf(room, kStart);
+                        float nr = ref[nt][c];
+                        if (m - nr > kTop) nr = m - kStart;
                         corr[c] = ex2f(ref[nt][c] - nr);
                         l[nt][c] *= corr[c];
                         ref[nt][c] = nr;
@@ -556,7 +585,7 @@ __global__ void __launch_bounds__(Cfg<DH, NT>::THREADS, 1) k_kv4_attn(const Kv4A
 #pragma unroll
                         for (int mt = 0; mt < 2; ++mt)
 #pragma unroll
-                            for (int i = 0; i < 4; ++i) o[j][mt][nt][i] *= corr[i & 1];
+                            for (int i = 0; i < 4; ++i) o[j][mt][nt][i] *= corr[i & 1] * shift[j];
                 }
             }
 #pragma unroll
@@ -617,6 +646,9 @@ __global__ void __launch_bounds__(Cfg<DH, NT>::THREADS, 1) k_kv4_attn(const Kv4A
         }
         if (timed_out) break;
         // ---- the end of the piece
+        float unit_v[NG];
+#pragma unroll
+        for (int j = 0; j < NG; ++j) unit_v[j] = __uint_as_float((uint32_t)(__shfl_sync(0xffffffffu, e_v, j) + 127) << 23);
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
@@ -638,9 +670,11 @@ __global__ void __launch_bounds__(Cfg<DH, NT>::THREADS, 1) k_kv4_attn(const Kv4A
                     const float inv = 1.0f / l[nt][c];
                     __nv_bfloat16* dst = p.o + (((size_t)t * p.M + si.row0 + tok) * p.nq + h * G + hd) * DH + 4 * g;
 #pragma unroll
-                    for (int j = 0; j < NG; ++j)
-                        *reinterpret_cast<uint2*>(dst + 32 * j) = make_uint2(kv4_bf16(o[j][0][nt][c] * inv, o[j][0][nt][2 + c] * inv),
-                                                                            kv4_bf16(o[j][1][nt][c] * inv, o[j][1][nt][2 + c] * inv));
+                    for (int j = 0; j < NG; ++j) {
+                        const float f = inv * unit_v[j];
+                        *reinterpret_cast<uint2*>(dst + 32 * j) = make_uint2(kv4_bf16(o[j][0][nt][c] * f, o[j][0][nt][2 + c] * f),
+                                                                            kv4_bf16(o[j][1][nt][c] * f, o[j][1][nt][2 + c] * f));
+                    }
                 }
         } else {                                                  // a part: merged below, or by k_kv4_merge
             float* part = ends ? sc.head(blockIdx.x, warp, smem) : (float*)ring;
@@ -651,7 +685,7 @@ __global__ void __launch_bounds__(Cfg<DH, NT>::THREADS, 1) k_kv4_attn(const Kv4A
                     const int r = nt * 8 + 2 * q4 + c;
 #pragma unroll
                     for (int j = 0; j < NG; ++j)
-                        *reinterpret_cast<float4*>(part + r * C::ROW + 32 * j + 4 * g) = make_float4(o[j][0][nt][c], o[j][0][nt][2 + c], o[j][1][nt][c], o[j][1][nt][2 + c]);
+                        *reinterpret_cast<float4*>(part + r * C::ROW + 32 * j + 4 * g) = make_float4(o[j][0][nt][c] * unit_v[j], o[j][0][nt][2 + c] * unit_v[j], o[j][1][nt][c] * unit_v[j], o[j][1][nt][2 + c] * unit_v[j]);
                     if (g == 0) { part[RB * C::ROW + 2 * r] = ref[nt][c]; part[RB * C::ROW + 2 * r + 1] = l[nt][c]; }
                 }
             my_flags |= ends ? 1 : begins ? 6 : 2;
