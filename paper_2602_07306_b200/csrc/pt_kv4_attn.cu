@@ -28,7 +28,7 @@
 
 #include "pt_kv4.cuh"
 #include "pt_tc.h"
-#include "pt_ptx.cuh"
+#include "pt_ring.cuh"
 
 namespace pt {
 
@@ -350,7 +350,7 @@ __global__ void __launch_bounds__(Cfg<DH, NT>::THREADS, 1) k_kv4_attn(const Kv4A
     __syncwarp();
     for (int s = 0; s < C::STAGES; ++s) if (a_any) issue(s);
 
-    int slot = 0, my_flags = 0;
+    int slot = 0, my_flags = 0, pending = 0;              // pending: tiles of the range that a wait that gave up has left
     uint32_t parity = 0;
     bool timed_out = false;
     while (any && !timed_out) {
@@ -409,7 +409,7 @@ __global__ void __launch_bounds__(Cfg<DH, NT>::THREADS, 1) k_kv4_attn(const Kv4A
                     ok = mbar_try(&bars[slot], parity);
                     if ((spin & 255) == 255 && clock.expired()) break;
                 }
-                if (!__all_sync(0xffffffffu, ok)) { timed_out = true; break; }
+                if (!__all_sync(0xffffffffu, ok)) { timed_out = true; pending = hi - tile; break; }
             }
             const uint32_t base = smem_u32(ring + slot * C::STAGE), dec = smem_u32(smem + C::SCALES + warp * C::SCALE_BYTES);
             const int key0 = tile * kTile;
@@ -695,13 +695,12 @@ __global__ void __launch_bounds__(Cfg<DH, NT>::THREADS, 1) k_kv4_attn(const Kv4A
         if (any) fetch(c, 0);
     }
     if (timed_out) {
-        // give the copies that are still in flight a bounded chance to land, then give up
-        WaitClock clock;
-        for (int s2 = 0; s2 < C::STAGES; ++s2)
-            for (uint32_t spin = 0; spin < (1u << 16); ++spin) {
-                if (mbar_try(&bars[s2], 0) || mbar_try(&bars[s2], 1)) break;
-                if ((spin & 63) == 63 && clock.expired(100000000ull)) break;
-            }
+        while (pending < C::STAGES) {                     // the ring is kept as full as the range's rest allows
+            const Cursor c = step(cursors[warp][0], any);
+            if (!any) break;
+            pending += c.hi - c.lo;
+        }
+        drain_ring(bars, C::STAGES, slot, parity, pending);
         if (lane == 0) report(p.status, PT_ERR_DEVICE_TIMEOUT, LOC_KV4_WAIT);
         my_flags = 0;
     }

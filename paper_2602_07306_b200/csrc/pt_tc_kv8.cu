@@ -10,7 +10,7 @@
 #include <cuda_fp8.h>
 
 #include "pt_tc.h"
-#include "pt_ptx.cuh"
+#include "pt_ring.cuh"
 
 namespace pt {
 
@@ -280,8 +280,8 @@ k_decode_attn_e4m3(const __grid_constant__ CUtensorMap kvmap, const Dec8P pp) {
 #pragma unroll
     for (int s = 0; s < kDecStages; ++s) { int gi = warp + 4 * s; if (gi < npages) issue(gi); else cp_async_commit(); }
     bool timed_out = false;
-    int it = 0;
-    for (int gi = warp; gi < npages; gi += 4, ++it) {
+    int it = 0, gi = warp;
+    for (; gi < npages; gi += 4, ++it) {
         const int slot = it % kDecStages;
         const uint32_t parity = (it / kDecStages) & 1;
         bool ok = false;
@@ -375,13 +375,7 @@ k_decode_attn_e4m3(const __grid_constant__ CUtensorMap kvmap, const Dec8P pp) {
     }
     cp_async_wait<0>();
     if (timed_out) {
-        // give the copies this warp still has in flight a bounded chance to land, then give up
-        WaitClock clock;
-        for (int s2 = 0; s2 < kDecStages; ++s2)
-            for (uint32_t spin = 0; spin < (1u << 16); ++spin) {
-                if (mbar_try(&wbar[s2], 0) || mbar_try(&wbar[s2], 1)) break;
-                if ((spin & 63) == 63 && clock.expired(100000000ull)) break;
-            }
+        drain_ring(wbar, kDecStages, it % kDecStages, (it / kDecStages) & 1, (npages - gi + 3) / 4);
         if (lane == 0) report(p.status, PT_ERR_DEVICE_TIMEOUT, LOC_DECODE_PAGE);
     }
     if (bad_page) report(p.status, PT_ERR_DEVICE_BOUNDS, LOC_DECODE_PAGE);
