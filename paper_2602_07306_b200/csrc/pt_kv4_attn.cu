@@ -700,7 +700,7 @@ __global__ void __launch_bounds__(Cfg<DH, NT>::THREADS, 1) k_kv4_attn(const Kv4A
             if (!any) break;
             pending += c.hi - c.lo;
         }
-        drain_ring(bars, C::STAGES, slot, parity, pending);
+        drain_ring(bars, C::STAGES, slot, pending);
         if (lane == 0) report(p.status, PT_ERR_DEVICE_TIMEOUT, LOC_KV4_WAIT);
         my_flags = 0;
     }

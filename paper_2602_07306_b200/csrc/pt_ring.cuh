@@ -6,15 +6,17 @@
 
 namespace pt {
 
-// Each of the `pending` stages of a ring that were filled and not yet consumed gets a bounded time to land: they are those from
-// stage `slot` on, whose copies complete its phase `parity` (stages before `slot`: the next phase).  The other parity of a stage
-// says nothing, it is that of a phase long complete.
-__device__ __forceinline__ void drain_ring(uint64_t* bars, int stages, int slot, uint32_t parity, int pending) {
-    for (int i = 0; i < stages && i < pending; ++i) {
+// Stages of a ring, `n` of them from stage s on, get a bounded time to land.  Of a barrier's two parities one is always that of its
+// last complete phase, for which a poll says yes at once; copies under way complete the phase of the other.  (A stage without any
+// takes the whole time.  To count those under way costs two of the decode kernels registers in their loops, 3 to 8 % of their time:
+// they drain all.)
+__device__ __forceinline__ void drain_ring(uint64_t* bars, int stages, int s, int n) {
+    for (int i = 0; i < stages && i < n; ++i) {
         WaitClock clock;
-        for (uint32_t spin = 0; spin < (1u << 20) && !mbar_try(&bars[slot], parity); ++spin)
+        const uint32_t flying = mbar_try(&bars[s], 1) ? 0u : 1u;
+        for (uint32_t spin = 0; spin < (1u << 16) && !mbar_try(&bars[s], flying); ++spin)
             if ((spin & 63) == 63 && clock.expired(100000000ull)) break;
-        if (++slot == stages) { slot = 0; parity ^= 1u; }
+        if (++s == stages) s = 0;
     }
 }
 

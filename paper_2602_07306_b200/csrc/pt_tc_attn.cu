@@ -356,8 +356,8 @@ k_decode_attn_tma(const __grid_constant__ CUtensorMap kvmap, const AttnP p) {
     if (lane == 0)
         for (int s = 0; s < kDecStages; ++s) { int gi = warp + 4 * s; if (gi < npages) issue(gi); }
     bool timed_out = false;
-    int it = 0, gi = warp;
-    for (; gi < npages; gi += 4, ++it) {
+    int it = 0;
+    for (int gi = warp; gi < npages; gi += 4, ++it) {
         const int slot = it % kDecStages;
         const uint32_t parity = (it / kDecStages) & 1;
         bool ok = false;
@@ -435,7 +435,7 @@ k_decode_attn_tma(const __grid_constant__ CUtensorMap kvmap, const AttnP p) {
         }
     }
     if (timed_out) {
-        drain_ring(wbar, kDecStages, it % kDecStages, (it / kDecStages) & 1, (npages - gi + 3) / 4);
+        drain_ring(wbar, kDecStages, 0, kDecStages);
         if (lane == 0) report(p.status, PT_ERR_DEVICE_TIMEOUT, LOC_DECODE_PAGE);
     }
     if (bad_page) report(p.status, PT_ERR_DEVICE_BOUNDS, LOC_DECODE_PAGE);
