@@ -28,6 +28,7 @@
 // products; a softmax takes 1.5 to 1.8k, bound by instruction issue, and waits for its own tile's products before and after.
 // Scores in halves of 64 keys with two buffers per tile took 843 us (a product of 64 columns costs nearly one of 128).
 #include "pt_chunk.h"
+#include "pt_ring.cuh"
 #include "pt_tcgen05.cuh"
 
 namespace pt {
@@ -369,10 +370,6 @@ k_chunk_tc(const __grid_constant__ CUtensorMap qmap, const __grid_constant__ CUt
             }
         }
         if (bad_page) report(p.status, PT_ERR_DEVICE_BOUNDS, LOC_CHUNK_PAGE);
-        if (!ok) {                                                 // copies still in flight get a bounded time to land
-            WaitClock clock;
-            for (uint32_t i = 0; i < (1u << 16) && !clock.expired(100000000ull); ++i) __nanosleep(64);
-        }
     } else if (warp == 2) {
         // ------------------------------------------------------------------ the walk
         Walk wk;
@@ -648,6 +645,7 @@ k_chunk_tc(const __grid_constant__ CUtensorMap qmap, const __grid_constant__ CUt
     }
     tc_fence_before();
     __syncthreads();
+    if (*abort_flag) settle_copies();
     if (warp == 2) {
         tc_fence_after();
         asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem_base), "r"(512) : "memory");

@@ -20,4 +20,10 @@ __device__ __forceinline__ void drain_ring(uint64_t* bars, int stages, int s, in
     }
 }
 
+// The same where copies, and products that read what they brought, belong to several warps: whatever is under way gets 100 ms.
+__device__ __forceinline__ void settle_copies() {
+    WaitClock clock;
+    for (uint32_t i = 0; i < (1u << 20) && !clock.expired(100000000ull); ++i) __nanosleep(1000);
+}
+
 }  // namespace pt

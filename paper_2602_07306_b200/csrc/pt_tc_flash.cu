@@ -14,6 +14,7 @@
 // by more than 2^8 (the accumulator is then rescaled in tensor memory), so rescales are rare.
 // Every mbarrier wait is bounded; on a timeout the CTA records PT_ERR_DEVICE_TIMEOUT, every role
 // leaves its loop, and tensor memory is freed before exit.
+#include "pt_ring.cuh"
 #include "pt_tcgen05.cuh"
 
 namespace pt {
@@ -401,6 +402,7 @@ k_flash_prefill_tc(const __grid_constant__ CUtensorMap qmap, const __grid_consta
     }
     tc_fence_before();
     __syncthreads();
+    if (*abort_flag) settle_copies();
     if (warp == 2) {
         tc_fence_after();
         asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem_base), "r"(512) : "memory");

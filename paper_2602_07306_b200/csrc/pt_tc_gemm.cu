@@ -26,7 +26,7 @@
 // Every mbarrier wait is bounded; on a timeout the CTA records PT_ERR_DEVICE_TIMEOUT, stops
 // issuing work, frees its tensor memory and exits.
 #include "pt_tc.h"
-#include "pt_ptx.cuh"
+#include "pt_ring.cuh"
 #include "pt_tmem.cuh"
 
 namespace pt {
@@ -621,6 +621,7 @@ gemm_tc(const __grid_constant__ CUtensorMap ta, const __grid_constant__ CUtensor
     }
     tc_fence_before();
     __syncthreads();
+    if (*abort_flag) settle_copies();
     if (warp == 1) {
         tc_fence_after();
         asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem_base), "r"(2 * BN) : "memory");
@@ -796,6 +797,7 @@ gemm_tc_pair(const __grid_constant__ CUtensorMap ta, const __grid_constant__ CUt
     }
     tc_fence_before();
     __syncthreads();
+    if (*abort_flag) settle_copies();
     cluster_sync_all();                                     // the partner's shared and tensor memory are in use until both are here
     if (warp == 1) {
         tc_fence_after();
@@ -1015,6 +1017,7 @@ gemm_tc_pair_resid(const __grid_constant__ CUtensorMap ta, const __grid_constant
     }
     tc_fence_before();
     __syncthreads();
+    if (*abort_flag) settle_copies();
     cluster_sync_all();                                     // the partner's shared and tensor memory are in use until both are here
     if (warp == 1) {
         tc_fence_after();

@@ -23,7 +23,7 @@
 #include <cuda_fp8.h>
 
 #include "pt_tc.h"
-#include "pt_ptx.cuh"
+#include "pt_ring.cuh"
 #include "pt_tmem.cuh"
 
 namespace pt {
@@ -492,6 +492,7 @@ k_decode_attn_e4m3_tc(const __grid_constant__ CUtensorMap kvmap, const Dec8TcP p
     }
     tc_fence_before();
     __syncthreads();
+    if (*abort_flag) settle_copies();
     if (warp == 1) {
         tc_fence_after();
         asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem_base), "r"(64) : "memory");

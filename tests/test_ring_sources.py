@@ -46,3 +46,13 @@ def test_the_stages_under_way():
             for consumed in range(total):
                 flying = {n % stages for n in range(consumed, min(total, consumed + stages))}
                 assert {(consumed + i) % stages for i in range(min(stages, total - consumed))} == flying
+
+
+def test_blocks_whose_waits_gave_up_let_their_copies_land():
+    """Every kernel with an abort flag asks it when all of its warps have met at the end, before tensor memory is freed."""
+    found = 0
+    for name, text in sources().items():
+        for m in re.finditer(r"__syncthreads\(\);\n((?:(?!__syncthreads).)*?)tcgen05\.dealloc", text, re.S):
+            assert m.group(1).lstrip().startswith("if (*abort_flag) settle_copies();"), (name, m.group(1))
+            found += 1
+    assert found == 6
