@@ -242,9 +242,19 @@ pt_status pt_workspace_bytes(const pt_model* m, int64_t max_tokens, int32_t max_
  * sequences of the cached length after the call, each rounded up to 16 (0 = prefill calls only ever start
  * from empty sequences: max_tokens + 16 * max_batch is used).  Decode calls need no such copy.  An E2M1 cache the same, but for
  * calls that attend straight to the codes (pt_extend and pt_prefill where the sequences' new tokens are few), which make no
- * copy.  Workspace for an E2M1 cache serves calls on an E4M3 cache too, and either one's serves a cache in the model dtype. */
+ * copy (pt_call_context).  Workspace for an E2M1 cache serves calls on an E4M3 cache too, and either one's serves a cache in the model dtype. */
 pt_status pt_workspace_bytes_ex(const pt_model* m, int64_t max_tokens, int32_t max_batch, int32_t page_size,
                                 int32_t kv_dtype, int64_t max_context, size_t* bytes);
+
+/* What a pt_extend call with n_tokens[b] new tokens of sequence seq_ids[b] (host arrays, or a pt_prefill call with S for each)
+ * would need, from the sequences' present lengths; nothing is launched or changed.
+ *   max_context  the least max_context that serves the call: the keys of its bf16 copy, 0 where it makes none (a cache in the
+ *                model dtype, or calls that attend straight to the codes of an E2M1 cache)
+ *   pass_rows    may be NULL.  E2M1 caches: the (token, head) rows of a sequence and KV head for which a call that attends
+ *                straight to the codes reads its keys once (8, 16 or 24); 0 for every other call
+ * The path and the rows are chosen by the rows of each sequence weighted with its keys. */
+pt_status pt_call_context(const pt_kv_cache* c, int32_t B, const int32_t* n_tokens, const int32_t* seq_ids, int64_t* max_context,
+                          int32_t* pass_rows);
 
 /* Algorithm 1 over B sequences of S new tokens each.
  *   x         device, 16-byte aligned, model dtype, [T][B][S][hidden]; track t starts at

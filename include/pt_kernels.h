@@ -199,7 +199,8 @@ pt_status pt_kernel_kv_read_e2m1(const void* pool_l, int64_t pool_track_stride, 
  *   q, out        device bf16 [T][M][nq*dh], 16-byte aligned, apart from one another; nq/nkv <= 8; rows behind the last
  *                 sequence are not touched
  *   q_len         DEVICE int32 [B]: new tokens of each sequence (none is allowed), or NULL: one each (M = B).  Any number is
- *                 served; a block of up to 24 (token, head) rows reads the sequence's keys once
+ *                 served; a pass over a sequence's keys serves 8, 16 or 24 of its (token, head) rows, the same number for all
+ *                 sequences of the call, chosen by the mean of their rows (the lengths are the device's)
  *   kv_len        DEVICE int32 [B], the new tokens' keys included.  Lengths out of range (negative, kv_len < q_len,
  *                 kv_len > maxp*ps, sum of q_len > M) are reported in `status` and nothing is written
  *   maxp          columns of the block table: at most 2^31 - 128 keys (PT_ERR_UNSUPPORTED).  A page number outside

@@ -508,6 +508,36 @@ pt_status pt_extend_workspace_bytes(const pt_model* m, int64_t max_tokens, int32
     return PT_OK;
 }
 
+// Keys of the bf16 copy that a prefill or ragged call on a coded cache makes; *direct as in Call.
+static int64_t context_of(const pt_kv_cache* c, const int32_t* n_new, const int32_t* seq_ids, int32_t B, int* direct) {
+    std::vector<int32_t> lens(B);
+    int64_t keys = 0;
+    for (int b = 0; b < B; ++b) {
+        auto it = c->seqs.find(seq_ids[b]);
+        lens[b] = (it == c->seqs.end() ? 0 : it->second.len) + n_new[b];
+        keys += ((int64_t)lens[b] + 15) / 16 * 16;
+    }
+    *direct = c->kv_dtype == PT_KV_E2M1 ? kv4_plan(lens.data(), n_new, B, c->m->G) : 0;
+    return *direct ? 0 : keys;
+}
+
+pt_status pt_call_context(const pt_kv_cache* c, int32_t B, const int32_t* n_tokens, const int32_t* seq_ids, int64_t* max_context, int32_t* pass_rows) try {
+    if (!c || !n_tokens || !seq_ids || !max_context) PT_FAIL(PT_ERR_INVALID_ARG, "null argument");
+    if (B < 1) PT_FAIL(PT_ERR_INVALID_ARG, "B must be >= 1");
+    for (int b = 0; b < B; ++b) {
+        if (n_tokens[b] < 1) PT_FAIL(PT_ERR_INVALID_ARG, "sequence %d of the call has %d new tokens", b, n_tokens[b]);
+        auto it = c->seqs.find(seq_ids[b]);
+        const int64_t len = it == c->seqs.end() ? 0 : it->second.len;
+        if (len + n_tokens[b] > c->m->cfg.max_pos) PT_FAIL(PT_ERR_INVALID_ARG, "sequence %d would reach position %lld >= max_pos %d", seq_ids[b], (long long)(len + n_tokens[b] - 1), c->m->cfg.max_pos);
+    }
+    int direct = 0;
+    *max_context = c->coded() ? context_of(c, n_tokens, seq_ids, B, &direct) : 0;
+    if (pass_rows) *pass_rows = 8 * direct;
+    return PT_OK;
+} catch (const std::bad_alloc&) {
+    PT_FAIL(PT_ERR_INVALID_ARG, "out of host memory");
+}
+
 // S new tokens for each of the B sequences, or n_tok[b] of them for sequence b (ragged: n_tok != null, rows packed).
 static pt_status forward(pt_model* m, pt_kv_cache* c, const void* x, int64_t x_stride, int32_t B, int32_t S,
                          const int32_t* n_tok, const int32_t* seq_ids, void* out_h, void* workspace, size_t ws_bytes, void* stream,
@@ -554,23 +584,9 @@ static pt_status forward(pt_model* m, pt_kv_cache* c, const void* x, int64_t x_s
     int maxp = (maxlen + c->ps - 1) / c->ps;
     const bool coded = c->coded(), four = c->kv_dtype == PT_KV_E2M1;
     if (coded && !m->tc) PT_FAIL(PT_ERR_UNSUPPORTED, "an E4M3 or E2M1 cache needs the tensor-core path");
-    bool direct = four && decode;
-    if (four && !decode) {
-        std::vector<int32_t> lens(B);
-        for (int b = 0; b < B; ++b) {
-            auto it = c->seqs.find(seq_ids[b]);
-            lens[b] = (it == c->seqs.end() ? 0 : it->second.len) + adds[b];
-        }
-        direct = kv4_direct(lens.data(), adds.data(), B, m->G);
-    }
+    int direct = four;                                             // a decode step: one row tile
     // E4M3 or E2M1 cache, prefill: the attention kernel reads a bf16 copy of code * scale of every key of the call's sequences
-    int64_t ctx_keys = 0;
-    if (coded && !decode && !direct)
-        for (int b = 0; b < B; ++b) {
-            auto it = c->seqs.find(seq_ids[b]);
-            int len = it == c->seqs.end() ? 0 : it->second.len;
-            ctx_keys += ((int64_t)len + news(b) + 15) / 16 * 16;
-        }
+    const int64_t ctx_keys = coded && !decode ? context_of(c, adds.data(), seq_ids, B, &direct) : 0;
     Call k{};
     size_t need_ws = carve(m, M, B, maxp, c->kv_dtype, ctx_keys, ragged, (char*)workspace, &k.w);
     if (ws_bytes < need_ws) PT_FAIL(PT_ERR_BUFFER_TOO_SMALL, "workspace: %zu < %zu bytes", ws_bytes, need_ws);

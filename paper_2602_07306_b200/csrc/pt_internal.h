@@ -178,7 +178,7 @@ struct Call {
     Work w;
     cudaStream_t st;
     bool decode;
-    bool direct;              // E2M1 caches: attention straight from the codes, without the bf16 copy
+    int direct;               // E2M1 caches: attention straight from the codes, without the bf16 copy, by this many row tiles a pass
     bool ragged;              // S differs between sequences: rows are packed, meta.qlen holds the counts (S is unused)
     // decode split plan (host): items of (b, first key, key count)
     int n_items, max_splits;

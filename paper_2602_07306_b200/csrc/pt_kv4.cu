@@ -338,21 +338,28 @@ pt_status launch_kv4_attn_call(Call& k, const __nv_bfloat16* q, int layer, __nv_
     Kv4AttnP p{};
     p.q = q; p.o = o; p.slab = slab_of(k, layer);
     p.bt = k.w.meta.bt; p.maxp = k.w.meta.maxp; p.qlen = k.decode ? nullptr : k.w.meta.qlen; p.kvlen = k.w.meta.kvlen;
-    p.T = m->cfg.T; p.B = k.B; p.M = k.M; p.nq = m->cfg.heads;
+    p.T = m->cfg.T; p.B = k.B; p.M = k.M; p.nq = m->cfg.heads; p.tiles = k.direct;
     p.scale_log2 = 1.4426950408889634f / sqrtf((float)m->dh);
     p.status = m->status();
     return launch_kv4_attn(p, m->dh, k.w.attn4, k.st);
 }
 
-// The attention from the codes reads a sequence's keys once for every 24 (token, head) rows; the other way writes the bf16 copy
-// and reads it, at the cost of about three such passes.
-bool kv4_direct(const int32_t* lens, const int32_t* n_new, int B, int G) {
-    double passes = 0, once = 0;
+// The attention from the codes reads a sequence's keys once a pass of 8, 16 or 24 (token, head) rows, which takes a time of 1, 1.6 or
+// 2 (four sequences of 20k keys, 4 tracks, 4 KV heads: 34, 54 and 67 us a pass beside a start of 10); the call has one of the three,
+// the one that is best over all of its sequences.  The other way writes the bf16 copy and reads it: a time of 6, at 64 rows and a
+// little more that of three passes of 24.
+int kv4_plan(const int32_t* lens, const int32_t* n_new, int B, int G) {
+    constexpr double kPass[3] = {1.0, 1.6, 2.0}, kCopy = 6.0;
+    double passes[3] = {}, once = 0;
     for (int b = 0; b < B; ++b) {
-        passes += (double)lens[b] * (((int64_t)n_new[b] * G + 23) / 24);
+        const int64_t eights = ((int64_t)n_new[b] * G + 7) / 8;
+        for (int i = 0; i < 3; ++i) passes[i] += (double)lens[b] * (double)((eights + i) / (i + 1));
         once += lens[b];
     }
-    return passes <= 3 * once;
+    int best = 0;
+    for (int i = 1; i < 3; ++i)
+        if (passes[i] * kPass[i] < passes[best] * kPass[best]) best = i;
+    return passes[best] * kPass[best] <= kCopy * once ? best + 1 : 0;
 }
 
 }  // namespace pt
@@ -432,6 +439,7 @@ extern "C" pt_status pt_kernel_attn_e2m1(const void* q, const void* pool_l, int6
     p.q = (const __nv_bfloat16*)q; p.o = (__nv_bfloat16*)out;
     p.slab = {(char*)pool_l, pool_track_stride, nkv, ps, num_pages};
     p.bt = block_table; p.maxp = maxp; p.qlen = q_len; p.kvlen = kv_len; p.T = T; p.B = B; p.M = M; p.nq = nq;
+    p.tiles = q_len ? kv4_mean_tiles((int64_t)M * (nq / nkv), B) : 1;
     p.scale_log2 = 1.4426950408889634f / sqrtf((float)dh);
     p.status = (int*)status;
     return launch_kv4_attn(p, dh, scratch, (cudaStream_t)stream);

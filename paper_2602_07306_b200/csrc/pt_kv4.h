@@ -46,8 +46,10 @@ struct Kv4AttnP {
     const int32_t* kvlen;             // [B] keys cached, the new tokens' included
     int T, B, M, nq;
     float scale_log2;                 // log2(e) / sqrt(dh)
+    int tiles;                        // row tiles a pass, 1 .. 3
     int* status;
 };
+int kv4_mean_tiles(int64_t rows, int B);                           // for `rows` (token, head) rows of a KV head whose lengths are not known
 size_t kv4_attn_scratch_bytes(int dh);
 pt_status launch_kv4_attn(const Kv4AttnP& p, int dh, void* scratch, cudaStream_t st);
 
@@ -56,7 +58,8 @@ pt_status launch_kv4_attn(const Kv4AttnP& p, int dh, void* scratch, cudaStream_t
 pt_status launch_kv4_write_call(Call& k, int layer);
 pt_status launch_kv4_read_call(Call& k, int layer);               // all of the call's keys into the bf16 copy
 pt_status launch_kv4_attn_call(Call& k, const __nv_bfloat16* q, int layer, __nv_bfloat16* o);
-// whether a call with n_new[b] new tokens on sequences that then have lens[b] keys attends straight to the codes
-bool kv4_direct(const int32_t* lens, const int32_t* n_new, int B, int G);
+// How a call with n_new[b] new tokens on sequences that then have lens[b] keys attends: straight to the codes with `tiles` row tiles
+// a pass (1 .. 3), or (0) to a bf16 copy.  G: query heads per KV head.
+int kv4_plan(const int32_t* lens, const int32_t* n_new, int B, int G);
 
 }  // namespace pt

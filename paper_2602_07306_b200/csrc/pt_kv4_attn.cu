@@ -883,17 +883,20 @@ template <int DH, int NT> pt_status launch_t(const Kv4AttnP& p, void* scratch, c
 template <int NT> constexpr size_t scratch_of(int dh) { return dh == 64 ? Scratch<64, NT>::bytes : Scratch<128, NT>::bytes; }
 size_t kv4_attn_scratch_bytes(int dh) { return std::max(scratch_of<1>(dh), std::max(scratch_of<2>(dh), scratch_of<3>(dh))); }
 
-template <int DH> static pt_status launch_dh(const Kv4AttnP& p, int tiles, void* scratch, cudaStream_t st) {
-    return tiles <= 1 ? launch_t<DH, 1>(p, scratch, st) : tiles == 2 ? launch_t<DH, 2>(p, scratch, st) : launch_t<DH, 3>(p, scratch, st);
+template <int DH> static pt_status launch_dh(const Kv4AttnP& p, void* scratch, cudaStream_t st) {
+    return p.tiles <= 1 ? launch_t<DH, 1>(p, scratch, st) : p.tiles == 2 ? launch_t<DH, 2>(p, scratch, st) : launch_t<DH, 3>(p, scratch, st);
+}
+
+// The mean number of rows of a sequence in as few passes over its keys as can be, in equal shares: up to three tiles of 8 rows a
+// pass.  (Four sequences of 20k keys, 4 tracks, 4 KV heads: 44, 66 and 83 us a pass of 1, 2 and 3 tiles; with four, whose
+// accumulators take 128 registers a lane, 134 us, as much as two passes of two.)
+int kv4_mean_tiles(int64_t rows, int B) {
+    const int64_t eights = ((rows + B - 1) / B + 7) / 8, passes = (eights + 2) / 3;
+    return (int)((eights + passes - 1) / passes);
 }
 
 pt_status launch_kv4_attn(const Kv4AttnP& p, int dh, void* scratch, cudaStream_t st) {
-    // The mean number of (token, head) rows of a sequence in as few passes over its keys as can be, in equal shares: up to three
-    // tiles of 8 rows a pass.  (Four sequences of 20k keys, 4 tracks, 4 KV heads: 43, 67 and 83 us a pass of 1, 2 and 3 tiles;
-    // with four, whose accumulators take 128 registers a lane, 134 us, as much as two passes of two.)
-    const int64_t rows = p.qlen ? ((int64_t)p.M * (p.nq / p.slab.nkv) + p.B - 1) / p.B : 1, eights = (rows + 7) / 8, passes = (eights + 2) / 3;
-    const int tiles = (int)((eights + passes - 1) / passes);
-    return dh == 64 ? launch_dh<64>(p, tiles, scratch, st) : launch_dh<128>(p, tiles, scratch, st);
+    return dh == 64 ? launch_dh<64>(p, scratch, st) : launch_dh<128>(p, scratch, st);
 }
 
 }  // namespace pt

@@ -83,6 +83,7 @@ _PROTOS = {
     "pt_kv_page_refs": (_I32, [_P, _I32, C.POINTER(_I32)]),
     "pt_kv_compact": (_I32, [_P, C.POINTER(_I32), _P]),
     "pt_kv_move_pool": (_I32, [_P, _I32, _P, _SZ, _P]),
+    "pt_call_context": (_I32, [_P, _I32, C.POINTER(_I32), C.POINTER(_I32), C.POINTER(_I64), C.POINTER(_I32)]),
     "pt_extend_workspace_bytes": (_I32, [_P, _I64, _I32, _I32, _I32, _I64, C.POINTER(_SZ)]),
     "pt_extend": (_I32, [_P, _P, _P, _I64, _I32, C.POINTER(_I32), C.POINTER(_I32), _P, _P, _SZ, _P]),
     "pt_sample": (_I32, [_P, _I32, _I64, _I64, _I32, _P, _P, _P, _P, _P, _P, _P, _P]),
