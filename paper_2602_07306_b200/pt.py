@@ -287,7 +287,7 @@ class Model:
 
     def workspace(self, tokens: int, batch: int, page_size: int, kv_dtype: int = PT_KV_MODEL, context: int = 0):
         """Workspace for calls of up to `tokens` tokens / `batch` sequences; with an E4M3 or E2M1 cache `context` bounds the
-        keys a prefill call attends to (sum over its sequences of the length after the call, each rounded up to 16)."""
+        keys of which a prefill call makes a copy (Cache.call_context)."""
         key = self.ws_key + (0, 0) if len(self.ws_key) == 3 else self.ws_key
         if (self.ws is None or tokens > key[0] or batch > key[1] or page_size < key[2] or kv_dtype > key[3] or context > key[4]):
             tokens, batch, context = max(tokens, key[0]), max(batch, key[1]), max(context, key[4])
@@ -322,9 +322,7 @@ class Model:
             out = torch.empty((B, S, H), dtype=torch.float32, device=self.device)
         ids, pids = _i32arr(seq_ids)
         assert len(ids) == B
-        ctx = 0
-        if cache.kv_dtype != PT_KV_MODEL:
-            ctx = sum((cache.length(int(s)) + S + 15) // 16 * 16 for s in ids)
+        ctx = cache.call_context(np.full(B, S, np.int32), ids) if cache.kv_dtype != PT_KV_MODEL else 0
         ws = self.workspace(B * S, B, cache.page_size, cache.kv_dtype, ctx)
         with torch.cuda.device(self.device):
             check(lib().pt_prefill(self.h, cache.h, x.data_ptr(), stride, B, S, pids, out.data_ptr(),
@@ -345,9 +343,7 @@ class Model:
         if out is None:
             out = torch.empty((M, H), dtype=torch.float32, device=self.device)
         assert out.is_cuda and out.dtype == torch.float32 and out.is_contiguous() and out.numel() == M * H
-        ctx = 0
-        if cache.kv_dtype != PT_KV_MODEL:
-            ctx = sum((cache.length(int(s)) + int(n) + 15) // 16 * 16 for s, n in zip(ids, cnt))
+        ctx = cache.call_context(cnt, ids) if cache.kv_dtype != PT_KV_MODEL else 0
         key = _grown(self.ext_key, (M, len(ids), cache.page_size, cache.kv_dtype, ctx))
         if self.ext_ws is None or key != self.ext_key:
             n = _SZ()
@@ -523,6 +519,15 @@ class Cache:
 
     def release(self, seq: int):
         check(lib().pt_kv_seq_release(self.h, seq))
+
+    def call_context(self, n_tokens, seq_ids) -> int:
+        """Keys of the bf16 copy that Model.prefill or Model.extend would make for n_tokens[b] new tokens of sequence seq_ids[b]; 0: none."""
+        cnt, pcnt = _i32arr(n_tokens)
+        ids, pids = _i32arr(seq_ids)
+        assert len(ids) == len(cnt)
+        v = _I64()
+        check(lib().pt_call_context(self.h, len(ids), pcnt, pids, C.byref(v), None))
+        return v.value
 
     def truncate(self, seq: int, n: int):
         check(lib().pt_kv_seq_truncate(self.h, seq, n))

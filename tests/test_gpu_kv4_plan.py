@@ -5,6 +5,7 @@ import numpy as np
 import pytest
 
 from paper_2602_07306_b200 import pt
+from tests import helpers as Hp
 from tests.test_gpu_kv4_model import Run, draw, four, setup    # noqa: F401  (a fixture)
 
 pytestmark = pytest.mark.gpu
@@ -37,4 +38,22 @@ def test_uneven_calls_follow_the_oracle(four, H, nq, nkv):     # noqa: F811
     assert rows_a_pass(r, n, ids)[0] == 0 and rows_a_pass(r, n, ids)[1] == sum((r.c.length(s) + k + 15) // 16 * 16 for s, k in zip(ids, n))
     r.extend(draw(wl, rng, sum(n)), n, ids)
     r.check(f"uneven calls, heads {nq}/{nkv}")
+    m.close()
+
+
+def test_calls_straight_to_the_codes_reserve_no_copy():
+    """Speculated tokens and short prompts on long contexts: the workspaces have no room for the bf16 copy that is not made."""
+    wl, ws, m = setup(256, 2, 1)
+    rng, n = np.random.default_rng(4), pt._SZ()
+    c = m.new_cache(200, 16, kv_dtype="e2m1")
+    m.prefill(c, Hp.to_dev(m, draw(wl, rng, 3, 800)), [0, 1, 2])
+    assert c.call_context([800] * 3, [3, 4, 5]) == 2400 and c.call_context([5, 1, 1], [0, 1, 2]) == 0
+    m.ws, m.ws_key = None, (0, 0, 0)                           # as a server that has another model object for its decode steps
+    m.extend(c, Hp.to_dev(m, draw(wl, rng, 7)), [5, 1, 1], [0, 1, 2])
+    m.prefill(c, Hp.to_dev(m, draw(wl, rng, 3, 2)), [0, 1, 2])
+    pt.check(pt.lib().pt_extend_workspace_bytes(m.h, 7, 3, 16, pt.PT_KV_E2M1, 0, C.byref(n)))
+    assert m.ext_ws.numel() == n.value and m.ext_key[4] == 0
+    pt.check(pt.lib().pt_workspace_bytes_ex(m.h, 6, 3, 16, pt.PT_KV_E2M1, 0, C.byref(n)))
+    assert m.ws.numel() == n.value and m.ws_key[4] == 0
+    assert m.device_status() == (0, 0)
     m.close()
