@@ -864,8 +864,9 @@ def kernel_kv_read_e2m1(pool_l, block_table, kv_len, out, out_table, *, nkv, dh,
     bt, maxp = _kv4_table(torch, "block_table", block_table, B, index)
     obt, omaxp = _kv4_table(torch, "out_table", out_table, B, index)
     status = _kv4_status(torch, status, index)
-    _call(index, lib().pt_kernel_kv_read_e2m1, pool_l.data_ptr(), pstride, bt, maxp, lens, T, B, nkv, dh, ps, pages, out.data_ptr(), ostride if T > 1 else 0,
-          obt, omaxp, ops, opages, status.data_ptr())
+    if B:
+        _call(index, lib().pt_kernel_kv_read_e2m1, pool_l.data_ptr(), pstride, bt, maxp, lens, T, B, nkv, dh, ps, pages, out.data_ptr(),
+              ostride if T > 1 else 0, obt, omaxp, ops, opages, status.data_ptr())
     return out, status
 
 
