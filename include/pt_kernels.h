@@ -172,10 +172,12 @@ pt_status pt_kernel_decode_attn_e4m3(const void* q, const void* codes_l, int64_t
  *   k, v          device bf16, 16-byte aligned: the nkv*dh values of (track t, row r) at t*track_stride + r*row_stride
  *                 elements (multiples of 8; 0 is allowed)
  *   slots         DEVICE int64 [M]: row r is token slots[r] % ps of page slots[r] / ps; a negative one is not cached.  No slot
- *                 twice in a call (which row it then holds is not defined).  A page outside [0, num_pages) is
+ *                 twice in a call (what it then holds is not defined: pieces of either row).  A page outside [0, num_pages) is
  *                 reported in `status`, and its row is not cached
  *   k_out, v_out  device bf16 [T][M][nkv*dh], 16-byte aligned, or both NULL: the values that the cache returns for every row
- *                 (of rows that are not cached, too).  They may be k and v themselves where those lie the same way */
+ *                 (of rows that are not cached, too).  They may be k and v themselves where those lie the same way, and are
+ *                 else apart from them and from one another
+ * Tracks that overlap in the pool are refused, as are those of out_l below. */
 pt_status pt_kernel_kv_write_e2m1(const void* k, const void* v, int64_t track_stride, int64_t row_stride, int32_t T, int32_t M,
                                   int32_t nkv, int32_t dh, int32_t ps, int32_t num_pages, void* pool_l, int64_t pool_track_stride,
                                   const int64_t* slots, void* k_out, void* v_out, void* status, void* stream);

@@ -295,6 +295,7 @@ pt_status launch_kv4_write(const Kv4WriteP& p, int dh, cudaStream_t st) {
 pt_status launch_kv4_read(const Kv4ReadP& p, int dh, cudaStream_t st) {
     const double blocks_most = (double)p.B * ((double)p.maxp * p.slab.ps / 16 + 1);      // of one track: counted in 32 bits
     if (blocks_most > 2e9) { set_error("too many sequences or pages for one call"); return PT_ERR_UNSUPPORTED; }
+    if (p.T > 1 && p.out_tstride < (int64_t)p.opages * 2 * p.slab.nkv * p.ops * dh) { set_error("the tracks of the output overlap"); return PT_ERR_INVALID_ARG; }
     // Short runs: warps that run side by side then read and write side by side.  (Four contexts of 9-16k keys, 8 tracks, 4 KV heads:
     // 195 us with a run for each of 64 warps an SM, 173 us with 512.)
     const double warps = std::min(blocks_most * p.T * p.slab.nkv, (double)sm_count() * 512);
@@ -393,6 +394,16 @@ extern "C" pt_status pt_kernel_kv_write_e2m1(const void* k, const void* v, int64
     p.k = (const __nv_bfloat16*)k; p.v = (const __nv_bfloat16*)v; p.tstride = track_stride; p.row_stride = row_stride; p.head_stride = dh;
     p.slab = {(char*)pool_l, pool_track_stride, nkv, ps, num_pages};
     p.slots = slots; p.k_out = (__nv_bfloat16*)k_out; p.v_out = (__nv_bfloat16*)v_out; p.T = T; p.M = M; p.status = (int*)status;
+    if (T > 1 && pool_track_stride < (int64_t)num_pages * nkv * (ps / 16) * kv4_block(dh)) { set_error("the pool's tracks overlap"); return PT_ERR_INVALID_ARG; }
+    if (k_out) {
+        const int64_t row = (int64_t)nkv * dh;
+        const double in = ((double)(T - 1) * track_stride + (double)(M - 1) * row_stride + row) * 2, out = (double)T * M * row * 2;
+        const bool alike = (M == 1 || row_stride == row) && (T == 1 || track_stride == M * row);
+        for (const void* from : {k, v})
+            for (const void* to : {(const void*)k_out, (const void*)v_out})
+                if (kv4_meet(from, in, to, out) && !(from == to && alike)) { set_error("k_out and v_out are k and v, alike in their strides, or apart from them"); return PT_ERR_INVALID_ARG; }
+        if (kv4_meet(k_out, out, v_out, out)) { set_error("k_out and v_out overlap"); return PT_ERR_INVALID_ARG; }
+    }
     return launch_kv4_write(p, dh, (cudaStream_t)stream);
 }
 

@@ -15,6 +15,12 @@ struct Kv4Slab {                      // one layer
     int nkv, ps, num_pages;
 };
 
+// whether two stretches of memory share a byte
+inline bool kv4_meet(const void* a, double bytes_a, const void* b, double bytes_b) {
+    const double x = (double)(uintptr_t)a, y = (double)(uintptr_t)b;                // below 2^53 where an address is one
+    return x < y + bytes_b && y < x + bytes_a;
+}
+
 struct Kv4WriteP {
     const __nv_bfloat16* k; const __nv_bfloat16* v;   // vector of (track, row, head) at t*tstride + row*row_stride + head*head_stride
     int64_t tstride, row_stride, head_stride;

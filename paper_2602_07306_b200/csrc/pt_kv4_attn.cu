@@ -855,6 +855,8 @@ template <int DH, int NT> pt_status launch_t(const Kv4AttnP& p, void* scratch, c
     // units of one head are counted in 32 bits: every block of rows with every key that the table can name
     const double most = ((double)p.M * (p.nq / p.slab.nkv) / C::RB + p.B) * ((double)p.maxp * p.slab.ps / kTile + 1 + kSegCost);
     if (most > 2e9) { set_error("4-bit attention: too many sequences, rows or pages for one call"); return PT_ERR_UNSUPPORTED; }
+    const double bytes = (double)p.T * p.M * p.nq * DH * 2;
+    if (kv4_meet(p.q, bytes, p.o, bytes)) { set_error("out must not overlap q"); return PT_ERR_INVALID_ARG; }
     static int sms_[kMaxDevices] = {};
     int& sms = sms_[current_device()];
     if (!sms) {

@@ -24,3 +24,29 @@ def test_calls_of_nothing_launch_nothing(monkeypatch):
     empty = z(2, 0, 256)
     assert pt.kernel_attn_e2m1(empty, pool, z(0, 2, dtype=i32), none, none, nq=4, out=empty, scratch=z(1 << 20, dtype=torch.uint8), status=status, **shape) == (empty, status)
     assert not launched
+
+
+def at(n):
+    return C.c_void_p(n)
+
+
+def test_memory_that_is_written_twice_or_read_as_it_is_written(lib):
+    n, A0, B0 = C.c_size_t(), 1 << 20, 1 << 24
+    assert lib.pt_kernel_attn_e2m1_scratch_bytes(2, 8, 2, 128, C.byref(n)) == 0
+
+    def attn(q, out):                                          # 2 tracks x 5 rows x 8 heads of 128: 20480 bytes
+        return lib.pt_kernel_attn_e2m1(at(q), at(B0), 1 << 20, at(B0), 4, at(B0), at(B0), 2, 3, 5, 8, 2, 128, 16, 4, at(out), at(B0), n.value, at(B0), None)
+    for d in (16, 20464, -16, -20464):
+        assert attn(A0, A0 + d) == 1 and b"overlap" in lib.pt_last_error()
+
+    def write(k, v, ko, vo, ts=3 * 256, rs=256, pts=1 << 20):  # 2 tracks x 3 rows x 2 heads of 128: 3072 bytes
+        return lib.pt_kernel_kv_write_e2m1(at(k), at(v), ts, rs, 2, 3, 2, 128, 16, 4, at(B0), pts, at(B0), at(ko), at(vo), at(B0), None)
+    far = A0 + (1 << 18)
+    for a in ((A0, far, A0 + 16, far + 16), (A0, far, A0 + 3056, A0 + 8192), (A0, far, A0 + 8192, far - 3056), (A0, far, A0 + 8192, A0 + 8192), (A0, far, A0 + 8192, A0 + 8192 + 3056)):
+        assert write(*a) == 1, a
+    assert write(A0, far, A0, far, rs=264) == 1 and write(A0, far, A0, far, ts=0) == 1
+    assert write(A0, far, A0 + 8192, far + 8192, pts=4 * 2 * 17 * 128 - 16) == 1 and b"tracks overlap" in lib.pt_last_error()
+
+    def read(ots):
+        return lib.pt_kernel_kv_read_e2m1(at(B0), 0, at(B0), 4, at(B0), 2, 3, 2, 64, 32, 4, at(A0), ots, at(B0), 5, 24, 7, at(B0), None)
+    assert read(7 * 2 * 2 * 24 * 64 - 8) == 1 and read(0) == 1
