@@ -702,14 +702,18 @@ pt_status pt_extend(pt_model* m, pt_kv_cache* c, const void* x, int64_t x_track_
 
 pt_status pt_prefill(pt_model* m, pt_kv_cache* c, const void* x, int64_t x_track_stride,
                      int32_t B, int32_t S, const int32_t* seq_ids, void* out_h,
-                     void* workspace, size_t ws_bytes, void* stream) {
+                     void* workspace, size_t ws_bytes, void* stream) try {
     return forward(m, c, x, x_track_stride, B, S, nullptr, seq_ids, out_h, workspace, ws_bytes, stream, false);
+} catch (const std::bad_alloc&) {
+    PT_FAIL(PT_ERR_INVALID_ARG, "out of host memory");
 }
 
 pt_status pt_decode_step(pt_model* m, pt_kv_cache* c, const void* x, int64_t x_track_stride,
                          int32_t B, const int32_t* seq_ids, void* out_h,
-                         void* workspace, size_t ws_bytes, void* stream) {
+                         void* workspace, size_t ws_bytes, void* stream) try {
     return forward(m, c, x, x_track_stride, B, 1, nullptr, seq_ids, out_h, workspace, ws_bytes, stream, true);
+} catch (const std::bad_alloc&) {
+    PT_FAIL(PT_ERR_INVALID_ARG, "out of host memory");
 }
 
 pt_status pt_set_debug_tap(pt_model* m, int32_t layer, void* dev_buf) {
