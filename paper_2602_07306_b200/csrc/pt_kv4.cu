@@ -2,7 +2,7 @@
 //   k_kv4_write   a thread has sixteen consecutive values of a vector, two threads a group of 32
 //   k_kv4_read    a warp has one head's K and V of 16 tokens, in the order in which they lie: 16 bytes a lane and load
 // Both are bound by the bytes they move.  Measured (a plain copy: 6.4 TB/s): 8192 tokens of 8 tracks and 8 KV heads of 128 with their
-// values out 99.5 us (608 MB, 6.1 TB/s; with eight values a thread and codes written where they fell 184), contexts of 28 sequences of
+// values out 99 us (608 MB, 6.1 TB/s; 105-107 for passes in a row on warmer boxes; with eight values a thread and codes written where they fell 184), contexts of 28 sequences of
 // 0.8-4k keys read back 105 us (638 MB, 6.1 TB/s).
 #include <algorithm>
 #include <type_traits>

@@ -4,25 +4,32 @@
 //   k_j[d] = code * scale of d's group of 32, v_j likewise; r runs over the (token, head) rows of a sequence and KV head.
 //
 // What bounds it: 17 bytes bring 32 values, so at the copy rate an SM has 2.3 cycles for every 100 values, and the codes'
-// way into the matrix instructions is what takes time, not the bytes.  So:
+// way into the matrix instructions takes more than that.  No unit is full (256 ragged sequences, 149 us: issue slots 57 %, ALU 57,
+// tensor pipe 28, DRAM 60; 4 x 5 tokens of 9-31k keys, 75 us: 41, 32, 37, 26): the time is that of dependent steps, with three
+// warps a scheduler to cover them, or two.  So:
 //  * The products run on mma.sync m16n8k16 in f16 with the cached vectors on the 16-row side and the rows r on the 8-column
 //    side: K^T q and V^T p take their 4-bit operand from registers, where cvt.rn.f16x2.e2m1x2 puts two codes an instruction.
 //    (tcgen05 takes its operands from shared memory or tensor memory: 4-bit codes would be converted in registers all the
-//    same, written and fetched again, and its block scales are powers of two, which these are not.)
+//    same, written and fetched again, and its block scales are powers of two, which these are not.  With one row tile that looks
+//    like more work than it takes away.  With several, where K's codes are converted and scaled once for all rows here too, it
+//    would take the products and the accumulators off the warps.  Neither is built or measured.)
 //  * The order of a block of 16 tokens is that of the instruction's operands: a lane loads its codes of K (two tokens, 32 dims
 //    each) and V (four tokens, 16 dims each) with 128-bit loads free of bank conflicts.  Of V a byte holds two dims of one
 //    token and the operand wants two tokens of one dim: eight codes of two tokens change places in four instructions.
 //  * A scale of K multiplies the partial score of its group in fp32 (with several row tiles: its codes, exactly), a scale of V
 //    the weights, once for 32 dims.  Weight times scale is one f16 number, kept within f16's normal range from both sides: the
 //    weights' reference (m above) lags behind the maximum by up to 2^6, so that a part's largest weight is 2^8 to 2^14, and the
-//    scales of a group of 32 columns are divided by a power of two that puts the largest of the tile's into [2^-5, 2).  The fp32
+//    scales of a group of 32 columns are divided by a power of two that puts the largest of the tile's into [2^-5, 2).  (So 2^-28 of
+//    the row's largest weight times that scale is the least that f16 holds; 256 ragged sequences take 149.5 us with it and 148.9
+//    with the scales as they are, which loses the small weights behind a dominant key.)  The fp32
 //    sums of the group carry that power and are rescaled, exactly, where it changes, which in ordinary data is once a segment.
 //    q is divided by a power of two that puts a row's largest magnitude at 2^13, K codes are below 8, sums are fp32.
 //  * A warp works alone: a ring of 32-key stages filled by bulk copies (a block of 16 tokens, K, V and scales, is one piece
 //    of 17 * dh bytes), its own plan from the device's lengths, its own contiguous share of all key tiles of the call, so
 //    that no barrier stands in the loop and a captured call may be replayed with other lengths.  A segment (sequence, track, KV
-//    head, 8 to 24 rows) that is cut leaves parts (sums, reference): those of a block's warps are merged in its shared
-//    memory, those of several blocks by k_kv4_merge.  Twelve warps of 168 registers: three a scheduler are enough.
+//    head, a block of 8, 16 or 24 rows, the last one shorter) that is cut leaves parts (sums, reference): those of a block's warps
+//    are merged in its shared memory, those of several blocks by k_kv4_merge.  Twelve warps of 168 registers with one and two row
+//    tiles, eight of up to 255 with three.
 #include <algorithm>
 #include <type_traits>
 
