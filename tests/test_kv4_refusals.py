@@ -39,13 +39,13 @@ def test_memory_that_is_written_twice_or_read_as_it_is_written(lib):
     for d in (16, 20464, -16, -20464):
         assert attn(A0, A0 + d) == 1 and b"overlap" in lib.pt_last_error()
 
-    def write(k, v, ko, vo, ts=3 * 256, rs=256, pts=1 << 20):  # 2 tracks x 3 rows x 2 heads of 128: 3072 bytes
-        return lib.pt_kernel_kv_write_e2m1(at(k), at(v), ts, rs, 2, 3, 2, 128, 16, 4, at(B0), pts, at(B0), at(ko), at(vo), at(B0), None)
-    far = A0 + (1 << 18)
-    for a in ((A0, far, A0 + 16, far + 16), (A0, far, A0 + 3056, A0 + 8192), (A0, far, A0 + 8192, far - 3056), (A0, far, A0 + 8192, A0 + 8192), (A0, far, A0 + 8192, A0 + 8192 + 3056)):
+    def write(k, v, ko, vo, ts=4 * 256, rs=256, pts=1 << 20):  # 2 tracks x 4 rows x 2 heads of 128: 4096 bytes
+        return lib.pt_kernel_kv_write_e2m1(at(k), at(v), ts, rs, 2, 4, 2, 128, 16, 4, at(B0), pts, at(B0), at(ko), at(vo), at(B0), None)
+    far, out = A0 + (1 << 18), A0 + 8192
+    for a in ((A0, far, A0 + 16, far + 16), (A0, far, A0 + 4080, out), (A0, far, out, far - 4080), (A0, far, out, out), (A0, far, out, out + 4080)):
         assert write(*a) == 1, a
     assert write(A0, far, A0, far, rs=264) == 1 and write(A0, far, A0, far, ts=0) == 1
-    assert write(A0, far, A0 + 8192, far + 8192, pts=4 * 2 * 17 * 128 - 16) == 1 and b"tracks overlap" in lib.pt_last_error()
+    assert write(A0, far, out, far + 8192, pts=4 * 2 * 17 * 128 - 16) == 1 and b"tracks overlap" in lib.pt_last_error()
 
     def read(ots):
         return lib.pt_kernel_kv_read_e2m1(at(B0), 0, at(B0), 4, at(B0), 2, 3, 2, 64, 32, 4, at(A0), ots, at(B0), 5, 24, 7, at(B0), None)
